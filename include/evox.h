@@ -509,6 +509,122 @@ int evox_profile(evox_state *state, int enable);
 int evox_profile_read(evox_state *state, double *fused_ms, int64_t *fused_launches,
                       int64_t *improved_rows);
 
+/* ---------------------------------------------------------------------------
+ * Populations of networks (the neuroevolution of Sec. VII-B and VII-C: PGPE on
+ * a CNN's weights, CMA-ES on a 3-layer MLP of 1,830 parameters).
+ *
+ * An individual is a network: its parameters are a row of a population matrix,
+ * a layer's weights [n_out][n_in] and its vectors lie at the same place of
+ * every row, so a layer's operand is a base pointer and the row pitch
+ * (w_stride, b_stride, ...).  Activations are [M][n] row-major; network g < G
+ * owns the rows off[g] .. off[g + 1) of them (off: device, int32 [G + 1], not
+ * decreasing; entries are clamped to [0, M], rows of no network are left
+ * alone) or, with off null, M / G rows each (M a multiple of G).  A network
+ * may own no row.
+ *
+ * All operands of a call have one element type, sums are in fp32 (fp64 for the
+ * fitness) and each result is rounded once.  Pointers and pitches need no more
+ * than the element's own alignment; all offsets are 64 bits.  Outputs must not
+ * overlap inputs, but for y = r (equal pitch) and dx = dy of the norm.  The
+ * calls read no device memory on the host, allocate nothing, can be captured
+ * in a graph, and give the same bits on every run.
+ * ------------------------------------------------------------------------- */
+enum evox_dtype { EVOX_F32 = 0, EVOX_BF16 = 1, EVOX_F16 = 2 };
+
+/* act(z): z, max(z, 0), tanh z, z Phi(z) (the normal distribution function, by
+ * erf), z / (1 + exp(-z)).  NaN stays NaN. */
+enum evox_act { EVOX_ACT_NONE = 0, EVOX_ACT_RELU = 1, EVOX_ACT_TANH = 2, EVOX_ACT_GELU = 3, EVOX_ACT_SILU = 4 };
+
+/* One layer of G networks (pitches and strides in elements). */
+typedef struct evox_layer {
+    int32_t dtype;      /* enum evox_dtype */
+    int32_t act;        /* enum evox_act */
+    int64_t G, M;       /* networks, 1 .. 2^20; rows of all of them, 0 .. 2^31 - 1 */
+    int64_t n_in, n_out;/* 1 .. 2^20 */
+    const int32_t *off; /* device [G + 1], or null: M / G rows each */
+    int32_t x_shared;   /* nonzero (off null): x has M / G rows, which every network reads */
+    int64_t ldx;        /* row pitch of x, >= n_in */
+    int64_t ldw, w_stride; /* row pitch of W, >= n_in; from W_g to W_(g+1), 0 or >= n_out rows' extent */
+    int64_t b_stride;   /* from b_g to b_(g+1) */
+    int64_t ldr, ldz, ldy; /* row pitches of r, z and y (or dy), >= n_out */
+    int64_t lddx;       /* row pitch of dx, >= n_in */
+    int64_t lddw, dw_stride, db_stride; /* of the weights' gradient */
+} evox_layer;
+
+/* z = x W_g^T + b_g, y = act(z) + r for every row, in one pass over x and W
+ * (the rows' own network's weights).  b, r and z may be null: no bias, no
+ * residual, pre-activations not kept.  w_stride = 0 (b_stride = 0): all
+ * networks use the one W (b). */
+int evox_linear(const evox_layer *layer, const void *x, const void *w, const void *b, const void *r, void *z,
+                void *y, void *hip_stream);
+
+/* The gradient of evox_linear.  With d = dy act'(z) (z as evox_linear stored
+ * it, unused for EVOX_ACT_NONE):
+ *     dx = d W_g;   dW_g = d^T x and db_g = sum of d over the rows of g
+ * (zero for a network without rows); the residual's gradient is dy itself.
+ * relu has slope 0 at 0.  Any of dx, dw, db may be null.  In 16 bits d is
+ * rounded once to the element type before the products.  EVOX_EINVAL for dx
+ * with x_shared (data has no gradient), and for w_stride = 0 with G > 1
+ * (give the one network's rows as G = 1).  scratch: device,
+ * evox_linear_grad_scratch_bytes(layer) bytes, 256-byte aligned. */
+size_t evox_linear_grad_scratch_bytes(const evox_layer *layer);
+int evox_linear_grad(const evox_layer *layer, const void *x, const void *w, const void *z, const void *dy, void *dx,
+                     void *dw, void *db, void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/* A norm over the D elements of every row, with a gain and a shift per
+ * network (pitches and strides in elements). */
+typedef struct evox_norm {
+    int32_t dtype;      /* enum evox_dtype */
+    int64_t G, M, D;    /* networks, rows, row length 1 .. EVOX_MAX_D */
+    const int32_t *off; /* as evox_layer */
+    int64_t ldx, ldy;   /* row pitches of x and y (of the gradient: dy), >= D */
+    int64_t lddx;       /* row pitch of dx, >= D */
+    int64_t p_stride;   /* from gamma_g to gamma_(g+1), and for beta */
+    int64_t dp_stride;  /* the same for dgamma and dbeta */
+    float eps;          /* > 0 */
+} evox_norm;
+
+/* Layer norm: y = (x - mean) rstd gamma_g + beta_g with the row's mean and
+ * rstd = 1 / sqrt(var + eps), var = mean of (x - mean)^2, taken from the row
+ * in registers.  mean and rstd (device, fp32 [M]) may be null. */
+int evox_layernorm(const evox_norm *norm, const void *x, const void *gamma, const void *beta, void *y, float *mean,
+                   float *rstd, void *hip_stream);
+
+/* Its gradient.  With h = (x - mean) rstd, a = dy gamma_g:
+ *     dx = rstd (a - mean_row(a) - h mean_row(a h)),
+ *     dgamma_g = sum of dy h, dbeta_g = sum of dy over the rows of g
+ * (zero for a network without rows; dgamma and dbeta both or neither null;
+ * dx may be null).  Rows are summed in a fixed order.  EVOX_EINVAL for
+ * p_stride = 0 or dp_stride = 0 with G > 1. */
+size_t evox_layernorm_grad_scratch_bytes(const evox_norm *norm);
+int evox_layernorm_grad(const evox_norm *norm, const void *x, const void *gamma, const float *mean,
+                        const float *rstd, const void *dy, void *dx, void *dgamma, void *dbeta, void *scratch,
+                        size_t scratch_bytes, void *hip_stream);
+
+/* Rows of logits over C classes. */
+typedef struct evox_classes {
+    int32_t dtype;      /* enum evox_dtype */
+    int64_t G, M, C;    /* networks, rows, classes 1 .. EVOX_MAX_D */
+    const int32_t *off; /* as evox_layer */
+    int32_t labels_shared; /* nonzero (off null): M / G labels, the same for every network */
+    int64_t ldz, lddz;  /* row pitches of the logits and of their gradient, >= C */
+} evox_classes;
+
+/* Cross-entropy as fitness: for the rows i of network g with 0 <= label_i < C
+ * (the others do not count), loss_i = log sum_c exp(z_ic) - z_i,label_i and
+ *     fit[g] = mean of loss_i (NaN for a network without such rows: last in
+ *              the argmin order),
+ *     dz_ic = (exp(z_ic) / sum_c exp(z_ic) - [c = label_i]) / count_g, and 0
+ *             in rows that do not count,
+ * fit device fp32 [G], labels device int32.  dz may be null, or the logits
+ * themselves (equal pitch).  Logits of -inf are classes left out (probability
+ * 0; a label among them gives loss +inf); a row of nothing else, or with +inf
+ * or NaN, gives NaN.  scratch: device, evox_xent_scratch_bytes bytes, 256-byte
+ * aligned. */
+size_t evox_xent_scratch_bytes(const evox_classes *classes);
+int evox_xent(const evox_classes *classes, const void *logits, const int32_t *labels, float *fit, void *dz,
+              void *scratch, size_t scratch_bytes, void *hip_stream);
+
 const char *evox_strerror(int code);
 const char *evox_last_error(void);
 

@@ -18,6 +18,8 @@ FN_IDS = {"sphere": SPHERE, "ackley": ACKLEY, "rastrigin": RASTRIGIN, "griewank"
 PSO, CSO, DE, ES, PGPE, MAES, NSGA2 = 0, 1, 2, 3, 4, 5, 6
 OK, EINVAL, EHIP, ENOSPC, EALIGN = 0, -1, -2, -3, -4
 MAX_D = 32768
+F32, BF16, F16 = range(3)
+ACT_NONE, ACT_RELU, ACT_TANH, ACT_GELU, ACT_SILU = range(5)
 
 # every symbol include/evox.h declares
 EXPORTS = (
@@ -33,6 +35,9 @@ EXPORTS = (
     "evox_permutation_scratch_bytes",
     "evox_permutation", "evox_argsort_u32",
     "evox_profile", "evox_profile_read", "evox_strerror", "evox_last_error",
+    "evox_linear", "evox_linear_grad_scratch_bytes", "evox_linear_grad",
+    "evox_layernorm", "evox_layernorm_grad_scratch_bytes", "evox_layernorm_grad",
+    "evox_xent_scratch_bytes", "evox_xent",
 )
 
 
@@ -65,6 +70,29 @@ class Buffers(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("x", "v", "pbest", "pfit", "fit", "gbest", "xbar", "mat",
                                                 "sigma", "obj", "front", "crowd")] + [
         ("scratch", ctypes.c_void_p), ("scratch_bytes", ctypes.c_size_t)]
+
+
+class Layer(ctypes.Structure):
+    """evox_layer: one layer of G networks."""
+    _fields_ = [("dtype", ctypes.c_int32), ("act", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("G", "M", "n_in", "n_out")] + [
+        ("off", ctypes.c_void_p), ("x_shared", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("ldx", "ldw", "w_stride", "b_stride", "ldr", "ldz", "ldy", "lddx", "lddw",
+                                      "dw_stride", "db_stride")]
+
+
+class Norm(ctypes.Structure):
+    """evox_norm: a norm over rows with a gain and a shift per network."""
+    _fields_ = [("dtype", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("G", "M", "D")] + [
+        ("off", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("ldx", "ldy", "lddx", "p_stride", "dp_stride")] + [("eps", ctypes.c_float)]
+
+
+class Classes(ctypes.Structure):
+    """evox_classes: rows of logits."""
+    _fields_ = [("dtype", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("G", "M", "C")] + [
+        ("off", ctypes.c_void_p), ("labels_shared", ctypes.c_int32), ("ldz", ctypes.c_int64),
+        ("lddz", ctypes.c_int64)]
 
 
 _lib = None
@@ -117,6 +145,14 @@ def lib():
             "evox_philox_fill": ([u64, u32, u32, u32, i64, P, P], i32),
             "evox_profile": ([P, i32], i32),
             "evox_profile_read": ([P, P, P, P], i32),
+            "evox_linear": ([P] * 8, i32),
+            "evox_linear_grad_scratch_bytes": ([P], sz),
+            "evox_linear_grad": ([P] * 9 + [sz, P], i32),
+            "evox_layernorm": ([P] * 8, i32),
+            "evox_layernorm_grad_scratch_bytes": ([P], sz),
+            "evox_layernorm_grad": ([P] * 10 + [sz, P], i32),
+            "evox_xent_scratch_bytes": ([P], sz),
+            "evox_xent": ([P] * 6 + [sz, P], i32),
             "evox_strerror": ([i32], ctypes.c_char_p),
             "evox_last_error": ([], ctypes.c_char_p),
         }
@@ -205,6 +241,223 @@ def evox_sgemm(A, B, C, trans_a=False, trans_b=False, alpha=1.0, beta=0.0, strea
     _check(lib().evox_sgemm(int(trans_a), int(trans_b), M, N, K, alpha, _ptr(A), A.stride(0), _ptr(B),
                             B.stride(0), beta, _ptr(C), C.stride(0), _stream(stream)))
     return C
+
+
+# ---------------------------------------------------------------------------
+# Populations of networks.  Weights and vectors are views of the parameter
+# rows ([G, n_out, n_in] and [G, n] tensors whose last dimension is dense);
+# activations are [M, n] tensors with dense rows.
+# ---------------------------------------------------------------------------
+def _dtype(t):
+    name = str(t.dtype)
+    if name not in ("torch.float32", "torch.bfloat16", "torch.float16"):
+        raise EvoxError(EINVAL, f"element type {name}: float32, bfloat16 or float16")
+    return (F32, BF16, F16)[("torch.float32", "torch.bfloat16", "torch.float16").index(name)]
+
+
+def _view(what, t, like, *shape):
+    """A tensor (or None) of this shape, of like's type and device, with dense rows."""
+    if t is None:
+        return
+    if t.dtype != like.dtype or t.device != like.device:
+        raise EvoxError(EINVAL, f"{what}: {t.dtype} on {t.device}, needs {like.dtype} on {like.device}")
+    if tuple(t.shape) != shape:
+        raise EvoxError(EINVAL, f"{what} has shape {tuple(t.shape)}, needs {shape}")
+    if t.numel() and shape[-1] > 1 and t.stride(-1) != 1:
+        raise EvoxError(EINVAL, f"{what}: rows are not dense")
+
+
+def _pitch(t, n):
+    """The row pitch of an [M, n] tensor (of one row, or none: n)."""
+    return n if t is None or t.shape[-2] <= 1 else t.stride(-2)
+
+
+def _offsets(off, like, G):
+    if off is None:
+        return None
+    import torch
+    if off.dtype != torch.int32 or off.device != like.device or tuple(off.shape) != (G + 1,) or not off.is_contiguous():
+        raise EvoxError(EINVAL, f"off: a dense int32 tensor of {G + 1} on {like.device}")
+    return off.data_ptr()
+
+
+def _net_stride(t):
+    return t.stride(0) if t is not None and t.shape[0] > 1 else 0
+
+
+def _scratch(nbytes, like, scratch, stream):
+    """The caller's scratch, or one of this size that lives until the stream is done with it."""
+    import torch
+    if nbytes == 0:
+        _check(EINVAL)
+    if scratch is None:
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+        if stream is not None:
+            scratch.record_stream(stream)
+    elif scratch.device != like.device or not scratch.is_contiguous():
+        raise EvoxError(EINVAL, f"scratch: a dense tensor on {like.device}")
+    return scratch, scratch.numel() * scratch.element_size()
+
+
+def _layer(x, w, y, act, off):
+    """The layer of weights w [G, n_out, n_in] between x and y (or dy)."""
+    if w.dim() != 3 or x.dim() != 2 or y.dim() != 2:
+        raise EvoxError(EINVAL, "w must be [G, n_out, n_in], x and y [rows, n]")
+    G, n_out, n_in = w.shape
+    M = y.shape[0]
+    shared = off is None and G > 1 and x.shape[0] != M
+    _view("x", x, w, M // G if shared else M, n_in)
+    _view("w", w, w, G, n_out, n_in)
+    _view("y", y, w, M, n_out)
+    if shared and M % G:
+        raise EvoxError(EINVAL, f"{M} rows for {G} networks")
+    return Layer(dtype=_dtype(w), act=act, G=G, M=M, n_in=n_in, n_out=n_out, off=_offsets(off, w, G),
+                 x_shared=int(shared), ldx=_pitch(x, n_in), ldw=_pitch(w, n_in), w_stride=_net_stride(w),
+                 ldy=_pitch(y, n_out))
+
+
+def evox_linear(x, w, y, b=None, r=None, z=None, off=None, act=ACT_NONE, stream=None):
+    """y = act(x W_g^T + b_g) + r for the rows of every network g.
+
+    x [M, n_in] (or [M / G, n_in]: every network on the same rows), w [G, n_out,
+    n_in], b [G, n_out], r, z, y [M, n_out]; off int32 [G + 1]: network g has
+    rows off[g] .. off[g + 1), by default M / G each.  z receives the
+    pre-activations (for evox_linear_grad)."""
+    p = _layer(x, w, y, act, off)
+    _view("b", b, w, p.G, p.n_out)
+    _view("r", r, w, p.M, p.n_out)
+    _view("z", z, w, p.M, p.n_out)
+    p.b_stride, p.ldr, p.ldz = _net_stride(b), _pitch(r, p.n_out), _pitch(z, p.n_out)
+    _check(lib().evox_linear(ctypes.byref(p), _ptr(x), _ptr(w), _ptr(b), _ptr(r), _ptr(z), _ptr(y), _stream(stream)))
+    return y
+
+
+def evox_linear_grad_scratch(x, w, dy):
+    """Scratch for evox_linear_grad calls of these shapes."""
+    return _scratch(lib().evox_linear_grad_scratch_bytes(ctypes.byref(_layer(x, w, dy, ACT_NONE, _any_off(x, w, dy)))),
+                    w, None, None)[0]
+
+
+def _any_off(x, w, y):
+    """Row offsets for sizing a scratch, which does not depend on them: needed
+    only where the rows are not as many for every network."""
+    import torch
+    G, M = w.shape[0], y.shape[0]
+    return torch.zeros(G + 1, dtype=torch.int32, device=w.device) if x.shape[0] == M and M % G else None
+
+
+def evox_linear_grad(x, w, dy, z=None, dx=None, dw=None, db=None, off=None, act=ACT_NONE, scratch=None, stream=None):
+    """The gradient of evox_linear from dy and the stored z: dx [M, n_in], dw [G,
+    n_out, n_in], db [G, n_out], each where given (the residual's is dy)."""
+    p = _layer(x, w, dy, act, off)
+    _view("z", z, w, p.M, p.n_out)
+    _view("dx", dx, w, p.M, p.n_in)
+    _view("dw", dw, w, p.G, p.n_out, p.n_in)
+    _view("db", db, w, p.G, p.n_out)
+    p.ldz, p.lddx, p.lddw = _pitch(z, p.n_out), _pitch(dx, p.n_in), _pitch(dw, p.n_in)
+    p.dw_stride, p.db_stride = _net_stride(dw), _net_stride(db)
+    scratch, nbytes = _scratch(lib().evox_linear_grad_scratch_bytes(ctypes.byref(p)), w, scratch, stream)
+    _check(lib().evox_linear_grad(ctypes.byref(p), _ptr(x), _ptr(w), _ptr(z), _ptr(dy), _ptr(dx), _ptr(dw), _ptr(db),
+                                  _ptr(scratch), nbytes, _stream(stream)))
+    return dx, dw, db
+
+
+def _norm(x, gamma, off, eps):
+    if x.dim() != 2 or gamma.dim() != 2:
+        raise EvoxError(EINVAL, "x must be [M, D], gamma [G, D]")
+    M, D = x.shape
+    _view("x", x, x, M, D)
+    _view("gamma", gamma, x, gamma.shape[0], D)
+    return Norm(dtype=_dtype(x), G=gamma.shape[0], M=M, D=D, off=_offsets(off, x, gamma.shape[0]), ldx=_pitch(x, D),
+                p_stride=_net_stride(gamma), eps=eps)
+
+
+def _stat(what, t, x):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or t.device != x.device or tuple(t.shape) != (x.shape[0],)
+                          or not t.is_contiguous()):
+        raise EvoxError(EINVAL, f"{what}: a dense float32 tensor of {x.shape[0]} on {x.device}")
+
+
+def evox_layernorm(x, gamma, beta, y, mean=None, rstd=None, off=None, eps=1e-5, stream=None):
+    """y = (x - mean) rstd gamma_g + beta_g over the rows of x [M, D], with gamma and
+    beta [G, D]; mean and rstd (float32 [M]) receive the rows' statistics."""
+    p = _norm(x, gamma, off, eps)
+    _view("beta", beta, x, p.G, p.D)
+    _view("y", y, x, p.M, p.D)
+    if _net_stride(beta) != p.p_stride:
+        raise EvoxError(EINVAL, "gamma and beta have different strides")
+    _stat("mean", mean, x)
+    _stat("rstd", rstd, x)
+    p.ldy = _pitch(y, p.D)
+    _check(lib().evox_layernorm(ctypes.byref(p), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
+                                _stream(stream)))
+    return y
+
+
+def evox_layernorm_grad_scratch(x, gamma):
+    """Scratch for evox_layernorm_grad calls of these shapes."""
+    import torch
+    G = gamma.shape[0]
+    off = torch.zeros(G + 1, dtype=torch.int32, device=x.device) if x.shape[0] % G else None
+    return _scratch(lib().evox_layernorm_grad_scratch_bytes(ctypes.byref(_norm(x, gamma, off, 1.0))), x, None, None)[0]
+
+
+def evox_layernorm_grad(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=None, off=None, scratch=None,
+                        stream=None):
+    """The gradient of evox_layernorm: dx [M, D], dgamma and dbeta [G, D], where given."""
+    p = _norm(x, gamma, off, 1.0)
+    _view("dy", dy, x, p.M, p.D)
+    _view("dx", dx, x, p.M, p.D)
+    _view("dgamma", dgamma, x, p.G, p.D)
+    _view("dbeta", dbeta, x, p.G, p.D)
+    if _net_stride(dgamma) != _net_stride(dbeta):
+        raise EvoxError(EINVAL, "dgamma and dbeta have different strides")
+    _stat("mean", mean, x)
+    _stat("rstd", rstd, x)
+    p.ldy, p.lddx, p.dp_stride = _pitch(dy, p.D), _pitch(dx, p.D), _net_stride(dgamma)
+    scratch, nbytes = _scratch(lib().evox_layernorm_grad_scratch_bytes(ctypes.byref(p)), x, scratch, stream)
+    _check(lib().evox_layernorm_grad(ctypes.byref(p), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(dx),
+                                     _ptr(dgamma), _ptr(dbeta), _ptr(scratch), nbytes, _stream(stream)))
+    return dx, dgamma, dbeta
+
+
+def _classes(logits, G, off, shared):
+    if logits.dim() != 2:
+        raise EvoxError(EINVAL, "logits must be [M, C]")
+    M, C = logits.shape
+    _view("logits", logits, logits, M, C)
+    return Classes(dtype=_dtype(logits), G=G, M=M, C=C, off=_offsets(off, logits, G), labels_shared=int(shared),
+                   ldz=_pitch(logits, C))
+
+
+def evox_xent_scratch(logits, fit):
+    """Scratch for evox_xent calls of these shapes."""
+    import torch
+    G = fit.shape[0]
+    off = torch.zeros(G + 1, dtype=torch.int32, device=fit.device) if logits.shape[0] % G else None
+    return _scratch(lib().evox_xent_scratch_bytes(ctypes.byref(_classes(logits, G, off, False))), logits, None, None)[0]
+
+
+def evox_xent(logits, labels, fit, dz=None, off=None, scratch=None, stream=None):
+    """fit[g] = mean cross-entropy of network g's rows of logits [M, C] against labels
+    (int32 [M], or [M / G]: the same for every network; rows whose label is outside
+    0 .. C-1 do not count), and its gradient dz [M, C] where given."""
+    import torch
+    G, M = fit.shape[0], logits.shape[0]
+    shared = off is None and G > 1 and labels.shape[0] != M
+    if (fit.dtype != torch.float32 or fit.device != logits.device or fit.dim() != 1 or not fit.is_contiguous()):
+        raise EvoxError(EINVAL, f"fit: a dense float32 vector on {logits.device}")
+    if (labels.dtype != torch.int32 or labels.device != logits.device or not labels.is_contiguous()
+            or tuple(labels.shape) != ((M // G if shared else M),)):
+        raise EvoxError(EINVAL, f"labels: a dense int32 tensor of {M} (or {M} / {G}) on {logits.device}")
+    p = _classes(logits, G, off, shared)
+    _view("dz", dz, logits, M, p.C)
+    p.lddz = _pitch(dz, p.C)
+    scratch, nbytes = _scratch(lib().evox_xent_scratch_bytes(ctypes.byref(p)), logits, scratch, stream)
+    _check(lib().evox_xent(ctypes.byref(p), _ptr(logits), _ptr(labels), _ptr(fit), _ptr(dz), _ptr(scratch), nbytes,
+                           _stream(stream)))
+    return fit
 
 
 def evox_nsga2_sort(F, front, crowd, scratch=None, stream=None):

@@ -8,12 +8,14 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <limits>
 #include <mutex>
 #include <utility>
 #include <vector>
 
 #include "evox_launch.hpp"
+#include "evox_net.hpp"
 
 using namespace evox;
 
@@ -504,6 +506,130 @@ int cso_refresh(evox_state *s, bool refit)
         return hip_fail(e, "select");
     if ((e = launch_cso_mean(mean_args(s, pl.colsum_grid), s->stream)) != hipSuccess)
         return hip_fail(e, "swarm mean");
+    return EVOX_OK;
+}
+
+}  // namespace
+
+namespace {
+
+// Populations of networks: the checks the calls share.  Offsets in device
+// memory are not read here (the kernels clamp them).
+int check_rows(int32_t dtype, int64_t G, int64_t M, const int32_t *off, bool shared, NetRows *rows)
+{
+    if (dtype != EVOX_F32 && dtype != EVOX_BF16 && dtype != EVOX_F16)
+        return fail(EVOX_EINVAL, "unknown dtype %d", dtype);
+    if (G < 1 || G > kNetMaxG) return fail(EVOX_EINVAL, "G = %lld out of range [1, 2^20]", (long long)G);
+    if (M < 0 || M > INT32_MAX) return fail(EVOX_EINVAL, "M = %lld out of range [0, 2^31)", (long long)M);
+    if (!off && M % G) return fail(EVOX_EINVAL, "M = %lld rows are no multiple of G = %lld", (long long)M, (long long)G);
+    if (off && shared) return fail(EVOX_EINVAL, "rows shared by the networks are as many for each: no offsets");
+    if ((uintptr_t)off & 3u) return fail(EVOX_EALIGN, "off is misaligned");
+    *rows = NetRows{off, G, M, M / G};
+    return EVOX_OK;
+}
+
+bool element_aligned(int32_t dtype, std::initializer_list<const void *> ptrs)
+{
+    for (const void *p : ptrs)
+        if ((uintptr_t)p & (dtype == EVOX_F32 ? 3u : 1u)) return false;
+    return true;
+}
+
+// Pitches and strides stay below 2^40 elements and the last element of `rows`
+// rows (`nets` networks) within 2^46, so no offset overflows.
+bool pitch_ok(int64_t pitch, int64_t n, int64_t rows)
+{
+    return pitch >= n && pitch < ((int64_t)1 << 40) && rows <= ((int64_t)1 << 46) / pitch;
+}
+bool stride_ok(int64_t stride, int64_t extent, int64_t nets)
+{
+    return nets == 1 || (stride >= extent && stride < ((int64_t)1 << 40) && nets <= ((int64_t)1 << 46) / stride);
+}
+
+int check_layer(const evox_layer *l, NetRows *rows)
+{
+    if (!l) return fail(EVOX_EINVAL, "layer is null");
+    const int rc = check_rows(l->dtype, l->G, l->M, l->off, l->x_shared != 0, rows);
+    if (rc != EVOX_OK) return rc;
+    if (l->act < 0 || l->act >= ACT_COUNT) return fail(EVOX_EINVAL, "unknown act %d", l->act);
+    if (l->n_in < 1 || l->n_in > kNetMaxWidth || l->n_out < 1 || l->n_out > kNetMaxWidth)
+        return fail(EVOX_EINVAL, "n_in = %lld, n_out = %lld: need 1 .. 2^20", (long long)l->n_in, (long long)l->n_out);
+    return EVOX_OK;
+}
+
+LinearGradArgs grad_args(const evox_layer *l, const NetRows &rows)
+{
+    LinearGradArgs a{};
+    a.rows = rows;
+    a.dtype = l->dtype;
+    a.act = l->act;
+    a.x_shared = l->x_shared;
+    a.n_in = l->n_in;
+    a.n_out = l->n_out;
+    a.ldx = l->ldx;
+    a.ldw = l->ldw;
+    a.w_stride = l->w_stride;
+    a.ldz = l->ldz;
+    a.lddy = l->ldy;
+    a.lddx = l->lddx;
+    a.lddw = l->lddw;
+    a.dw_stride = l->dw_stride;
+    a.db_stride = l->db_stride;
+    return a;
+}
+
+int check_norm(const evox_norm *p, NetRows *rows)
+{
+    if (!p) return fail(EVOX_EINVAL, "norm is null");
+    const int rc = check_rows(p->dtype, p->G, p->M, p->off, false, rows);
+    if (rc != EVOX_OK) return rc;
+    if (p->D < 1 || p->D > EVOX_MAX_D)
+        return fail(EVOX_EINVAL, "D = %lld out of range [1, %d]", (long long)p->D, EVOX_MAX_D);
+    return EVOX_OK;
+}
+
+NormArgs norm_args(const evox_norm *p, const NetRows &rows)
+{
+    NormArgs a{};
+    a.rows = rows;
+    a.dtype = p->dtype;
+    a.D = p->D;
+    a.ldx = p->ldx;
+    a.ldy = p->ldy;
+    a.lddx = p->lddx;
+    a.p_stride = p->p_stride;
+    a.dp_stride = p->dp_stride;
+    a.eps = p->eps;
+    return a;
+}
+
+int check_classes(const evox_classes *c, NetRows *rows)
+{
+    if (!c) return fail(EVOX_EINVAL, "classes is null");
+    const int rc = check_rows(c->dtype, c->G, c->M, c->off, c->labels_shared != 0, rows);
+    if (rc != EVOX_OK) return rc;
+    if (c->C < 1 || c->C > EVOX_MAX_D)
+        return fail(EVOX_EINVAL, "C = %lld out of range [1, %d]", (long long)c->C, EVOX_MAX_D);
+    return EVOX_OK;
+}
+
+XentArgs xent_args(const evox_classes *c, const NetRows &rows)
+{
+    XentArgs a{};
+    a.rows = rows;
+    a.dtype = c->dtype;
+    a.labels_shared = c->labels_shared;
+    a.C = c->C;
+    a.ldz = c->ldz;
+    a.lddz = c->lddz;
+    return a;
+}
+
+int check_scratch(const void *scratch, size_t have, size_t need)
+{
+    if (!scratch) return fail(EVOX_EINVAL, "scratch is required");
+    if ((uintptr_t)scratch & 255u) return fail(EVOX_EALIGN, "scratch is not 256-byte aligned");
+    if (have < need) return fail(EVOX_ENOSPC, "scratch has %zu bytes, needs %zu", have, need);
     return EVOX_OK;
 }
 
@@ -1504,6 +1630,189 @@ int evox_profile_read(evox_state *s, double *fused_ms, int64_t *fused_launches, 
     if (fused_ms) *fused_ms = ms;
     if (fused_launches) *fused_launches = s->prof_gens;
     if (improved_rows) *improved_rows = (int64_t)(h.improved - s->improved_base);
+    return EVOX_OK;
+}
+
+int evox_linear(const evox_layer *l, const void *x, const void *w, const void *b, const void *r, void *z, void *y,
+                void *hip_stream)
+{
+    NetRows rows;
+    const int rc = check_layer(l, &rows);
+    if (rc != EVOX_OK) return rc;
+    if (l->M == 0) return EVOX_OK;
+    if (!x || !w || !y) return fail(EVOX_EINVAL, "x, w and y are required");
+    if (!element_aligned(l->dtype, {x, w, b, r, z, y})) return fail(EVOX_EALIGN, "an operand is misaligned");
+    if (!pitch_ok(l->ldx, l->n_in, l->M) || !pitch_ok(l->ldw, l->n_in, l->n_out) ||
+        (r && !pitch_ok(l->ldr, l->n_out, l->M)) || (z && !pitch_ok(l->ldz, l->n_out, l->M)) ||
+        !pitch_ok(l->ldy, l->n_out, l->M))
+        return fail(EVOX_EINVAL, "a row pitch is below the row length or too large");
+    if ((l->w_stride && !stride_ok(l->w_stride, (l->n_out - 1) * l->ldw + l->n_in, l->G)) ||
+        (b && l->b_stride && !stride_ok(l->b_stride, l->n_out, l->G)))
+        return fail(EVOX_EINVAL, "w_stride or b_stride is below a network's extent or too large");
+    LinearArgs a{};
+    a.rows = rows;
+    a.dtype = l->dtype;
+    a.act = l->act;
+    a.x_shared = l->x_shared;
+    a.n_in = l->n_in;
+    a.n_out = l->n_out;
+    a.x = x;
+    a.w = w;
+    a.b = b;
+    a.r = r;
+    a.z = z;
+    a.y = y;
+    a.ldx = l->ldx;
+    a.ldw = l->ldw;
+    a.w_stride = l->w_stride;
+    a.b_stride = l->b_stride;
+    a.ldr = l->ldr;
+    a.ldz = l->ldz;
+    a.ldy = l->ldy;
+    const hipError_t e = launch_linear(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "linear");
+    return EVOX_OK;
+}
+
+size_t evox_linear_grad_scratch_bytes(const evox_layer *l)
+{
+    NetRows rows;
+    if (check_layer(l, &rows) != EVOX_OK) return 0;
+    return round256(linear_grad_scratch(grad_args(l, rows)));
+}
+
+int evox_linear_grad(const evox_layer *l, const void *x, const void *w, const void *z, const void *dy, void *dx,
+                     void *dw, void *db, void *scratch, size_t scratch_bytes, void *hip_stream)
+{
+    NetRows rows;
+    int rc = check_layer(l, &rows);
+    if (rc != EVOX_OK) return rc;
+    if (dx && l->x_shared) return fail(EVOX_EINVAL, "rows shared by the networks have no dx");
+    const bool some = l->M > 0;
+    if (some && (!dy || (dw && !x) || (dx && !w) || (l->act != EVOX_ACT_NONE && !z)))
+        return fail(EVOX_EINVAL, "dy, x (for dw), w (for dx) and z (for an activation) are required");
+    if (!element_aligned(l->dtype, {x, w, z, dy, dx, dw, db})) return fail(EVOX_EALIGN, "an operand is misaligned");
+    if ((dw && (!pitch_ok(l->ldx, l->n_in, l->M) || !pitch_ok(l->lddw, l->n_in, l->n_out))) ||
+        (dx && (!pitch_ok(l->ldw, l->n_in, l->n_out) || !pitch_ok(l->lddx, l->n_in, l->M))) ||
+        !pitch_ok(l->ldy, l->n_out, l->M) || (l->act != EVOX_ACT_NONE && !pitch_ok(l->ldz, l->n_out, l->M)))
+        return fail(EVOX_EINVAL, "a row pitch is below the row length or too large");
+    if ((dx && !stride_ok(l->w_stride, (l->n_out - 1) * l->ldw + l->n_in, l->G)) ||
+        (dw && !stride_ok(l->dw_stride, (l->n_out - 1) * l->lddw + l->n_in, l->G)) ||
+        (db && !stride_ok(l->db_stride, l->n_out, l->G)))
+        return fail(EVOX_EINVAL, "w_stride, dw_stride or db_stride is below a network's extent or too large");
+    LinearGradArgs a = grad_args(l, rows);
+    rc = check_scratch(scratch, scratch_bytes, round256(linear_grad_scratch(a)));
+    if (rc != EVOX_OK) return rc;
+    a.x = x;
+    a.w = w;
+    a.z = z;
+    a.dy = dy;
+    a.dx = some ? dx : nullptr;
+    a.dw = dw;
+    a.db = db;
+    a.scratch = scratch;
+    const hipError_t e = launch_linear_grad(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "linear gradient");
+    return EVOX_OK;
+}
+
+int evox_layernorm(const evox_norm *p, const void *x, const void *gamma, const void *beta, void *y, float *mean,
+                   float *rstd, void *hip_stream)
+{
+    NetRows rows;
+    const int rc = check_norm(p, &rows);
+    if (rc != EVOX_OK) return rc;
+    if (!(p->eps > 0.0f)) return fail(EVOX_EINVAL, "eps must be > 0");
+    if (p->M == 0) return EVOX_OK;
+    if (!x || !gamma || !beta || !y) return fail(EVOX_EINVAL, "x, gamma, beta and y are required");
+    if (!element_aligned(p->dtype, {x, gamma, beta, y}) || !element_aligned(EVOX_F32, {mean, rstd}))
+        return fail(EVOX_EALIGN, "an operand is misaligned");
+    if (!pitch_ok(p->ldx, p->D, p->M) || !pitch_ok(p->ldy, p->D, p->M))
+        return fail(EVOX_EINVAL, "a row pitch is below the row length or too large");
+    if (p->p_stride && !stride_ok(p->p_stride, p->D, p->G))
+        return fail(EVOX_EINVAL, "p_stride is below D or too large");
+    NormArgs a = norm_args(p, rows);
+    a.x = x;
+    a.gamma = gamma;
+    a.beta = beta;
+    a.y = y;
+    a.mean = mean;
+    a.rstd = rstd;
+    const hipError_t e = launch_layernorm(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "layer norm");
+    return EVOX_OK;
+}
+
+size_t evox_layernorm_grad_scratch_bytes(const evox_norm *p)
+{
+    NetRows rows;
+    if (check_norm(p, &rows) != EVOX_OK) return 0;
+    return round256(layernorm_grad_scratch(norm_args(p, rows)));
+}
+
+int evox_layernorm_grad(const evox_norm *p, const void *x, const void *gamma, const float *mean, const float *rstd,
+                        const void *dy, void *dx, void *dgamma, void *dbeta, void *scratch, size_t scratch_bytes,
+                        void *hip_stream)
+{
+    NetRows rows;
+    int rc = check_norm(p, &rows);
+    if (rc != EVOX_OK) return rc;
+    const bool some = p->M > 0;
+    if (!dgamma != !dbeta) return fail(EVOX_EINVAL, "dgamma and dbeta go together");
+    if (some && (!x || !gamma || !mean || !rstd || !dy))
+        return fail(EVOX_EINVAL, "x, gamma, mean, rstd and dy are required");
+    if (!element_aligned(p->dtype, {x, gamma, dy, dx, dgamma, dbeta}) || !element_aligned(EVOX_F32, {mean, rstd}))
+        return fail(EVOX_EALIGN, "an operand is misaligned");
+    if (!pitch_ok(p->ldx, p->D, p->M) || !pitch_ok(p->ldy, p->D, p->M) || (dx && !pitch_ok(p->lddx, p->D, p->M)))
+        return fail(EVOX_EINVAL, "a row pitch is below the row length or too large");
+    if (!stride_ok(p->p_stride, p->D, p->G) || (dgamma && !stride_ok(p->dp_stride, p->D, p->G)))
+        return fail(EVOX_EINVAL, "p_stride or dp_stride is below D or too large");
+    NormArgs a = norm_args(p, rows);
+    rc = check_scratch(scratch, scratch_bytes, round256(layernorm_grad_scratch(a)));
+    if (rc != EVOX_OK) return rc;
+    a.x = x;
+    a.gamma = gamma;
+    a.mean_in = mean;
+    a.rstd_in = rstd;
+    a.dy = dy;
+    a.dx = some ? dx : nullptr;
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
+    a.scratch = scratch;
+    const hipError_t e = launch_layernorm_grad(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "layer norm gradient");
+    return EVOX_OK;
+}
+
+size_t evox_xent_scratch_bytes(const evox_classes *c)
+{
+    NetRows rows;
+    if (check_classes(c, &rows) != EVOX_OK) return 0;
+    return round256(xent_scratch(xent_args(c, rows)));
+}
+
+int evox_xent(const evox_classes *c, const void *logits, const int32_t *labels, float *fit, void *dz, void *scratch,
+              size_t scratch_bytes, void *hip_stream)
+{
+    NetRows rows;
+    int rc = check_classes(c, &rows);
+    if (rc != EVOX_OK) return rc;
+    const bool some = c->M > 0;
+    if (!fit || (some && (!logits || !labels))) return fail(EVOX_EINVAL, "logits, labels and fit are required");
+    if (!element_aligned(c->dtype, {logits, dz}) || !element_aligned(EVOX_F32, {labels, fit}))
+        return fail(EVOX_EALIGN, "an operand is misaligned");
+    if (!pitch_ok(c->ldz, c->C, c->M) || (dz && !pitch_ok(c->lddz, c->C, c->M)))
+        return fail(EVOX_EINVAL, "a row pitch is below the row length or too large");
+    XentArgs a = xent_args(c, rows);
+    rc = check_scratch(scratch, scratch_bytes, round256(xent_scratch(a)));
+    if (rc != EVOX_OK) return rc;
+    a.logits = logits;
+    a.labels = labels;
+    a.fit = fit;
+    a.dz = some ? dz : nullptr;
+    a.scratch = scratch;
+    const hipError_t e = launch_xent(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "cross-entropy");
     return EVOX_OK;
 }
 
