@@ -79,6 +79,47 @@ hipError_t net_dispatch(int32_t dtype, F &&f)
     return f(f16_t{});
 }
 
+// Sixteen bytes of a row: loads and stores need only the element's alignment
+// (gfx950 takes a dwordx4 at any address).
+template <typename T>
+struct NetVec {
+    static constexpr int N = 16 / (int)sizeof(T);
+    typedef T reg __attribute__((ext_vector_type(N)));
+    typedef T mem __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
+// Elements [c N, c N + N) of a row of n, `fill` past its end.
+template <typename T>
+__device__ __forceinline__ typename NetVec<T>::reg load_chunk(const T *row, int c, int n, T fill)
+{
+    constexpr int N = NetVec<T>::N;
+    const int at = c * N;
+    if (at + N <= n) return *reinterpret_cast<const typename NetVec<T>::mem *>(row + at);
+    typename NetVec<T>::reg v;
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = at + j < n ? row[at + j] : fill;
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_chunk(T *row, int c, int n, typename NetVec<T>::reg v)
+{
+    constexpr int N = NetVec<T>::N;
+    const int at = c * N;
+    if (at + N <= n) {
+        *reinterpret_cast<typename NetVec<T>::mem *>(row + at) = v;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (at + j < n) row[at + j] = v[j];
+}
+
+__device__ __forceinline__ int64_t net_off(const NetRows &r, int64_t g)
+{
+    const int64_t o = r.off[g];
+    return o < 0 ? 0 : o > r.M ? r.M : o;
+}
+
 // The rows [lo, hi) of network g, within [0, M] whatever off holds.
 __device__ __forceinline__ void net_rows(const NetRows &r, int64_t g, int64_t *lo, int64_t *hi)
 {
@@ -87,23 +128,79 @@ __device__ __forceinline__ void net_rows(const NetRows &r, int64_t g, int64_t *l
         *hi = *lo + r.n;
         return;
     }
-    const int64_t a = r.off[g], b = r.off[g + 1];
-    *lo = a < 0 ? 0 : a > r.M ? r.M : a;
-    *hi = b < *lo ? *lo : b > r.M ? r.M : b;
+    const int64_t b = net_off(r, g + 1);
+    *lo = net_off(r, g);
+    *hi = b < *lo ? *lo : b;
 }
 
 // The network of a row: the last g with off[g] <= row (networks without rows
 // share their offset with the next), or -1 where the row belongs to none.
-__device__ __forceinline__ int64_t net_of_row(const NetRows &r, int64_t row)
+__device__ __forceinline__ int net_of_row(const NetRows &r, int64_t row)
 {
-    if (!r.off) return row / r.n;
-    int64_t lo = -1, hi = r.G;  // off[lo] <= row < off[hi]
+    if (!r.off) return (int)((uint32_t)row / (uint32_t)r.n);
+    int lo = -1, hi = (int)r.G;  // off[lo] <= row < off[hi]
     while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) / 2;
+        const int mid = (lo + hi) / 2;
         if (r.off[mid] <= row) lo = mid;
         else hi = mid;
     }
     return lo >= 0 && row < r.off[lo + 1] ? lo : -1;
+}
+
+// Tiles of 2^sh rows that stay within a network, numbered so that a network's
+// first tile needs its own offset alone: T(g) = (off[g] >> sh) + g.  T grows by
+// at least the network's tile count from one network to the next (by one more
+// where its rows do not fill their tiles), so (M >> sh) + G numbers hold all,
+// some of them of no rows.  With as many rows for each, T(g) = g ceil(n / 2^sh).
+struct NetTile {
+    int g;           // -1: no rows
+    int index;       // of the network's tiles
+    int64_t lo, hi;  // rows
+};
+__host__ __device__ __forceinline__ int64_t net_tiles(const NetRows &r, int sh)
+{
+    const int64_t per = (r.n + ((int64_t)1 << sh) - 1) >> sh;
+    return r.off ? (r.M >> sh) + r.G : r.G * per;
+}
+__device__ __forceinline__ int64_t net_first_tile(const NetRows &r, int sh, int64_t g)
+{
+    return r.off ? (net_off(r, g) >> sh) + g : g * ((r.n + ((int64_t)1 << sh) - 1) >> sh);
+}
+// The tile's network by 64 probes at a time, one per lane (all lanes of the
+// wave must call with the same t).
+__device__ __forceinline__ NetTile net_tile(const NetRows &r, int sh, int64_t t)
+{
+    NetTile o;
+    o.g = -1;
+    if (!r.off) {
+        const uint32_t per = (uint32_t)((r.n + ((int64_t)1 << sh) - 1) >> sh);
+        const uint32_t g = (uint32_t)t / per;
+        o.index = (int)((uint32_t)t - g * per);
+        o.lo = (int64_t)g * r.n + ((int64_t)o.index << sh);
+        o.hi = (int64_t)(g + 1) * r.n;
+        o.g = (int)g;
+    } else {
+        int lo = 0, hi = (int)r.G;
+        const int lane = threadIdx.x % 64;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 63) / 64, p = lo + lane * step;
+            const bool in = p < hi && net_first_tile(r, sh, p) <= t;
+            const int n = __popcll(__ballot(in));
+            if (n == 0) return o;
+            lo += (n - 1) * step;
+            hi = lo + step < hi ? lo + step : hi;
+        }
+        int64_t a, b;
+        net_rows(r, lo, &a, &b);
+        const int64_t i = t - ((a >> sh) + lo);
+        o.lo = a + (i << sh);
+        o.hi = b;
+        o.index = (int)i;
+        if (i < 0 || o.lo >= b) return o;
+        o.g = lo;
+    }
+    if (o.hi > o.lo + ((int64_t)1 << sh)) o.hi = o.lo + ((int64_t)1 << sh);
+    return o;
 }
 
 __device__ __forceinline__ float act_value(int act, float z)

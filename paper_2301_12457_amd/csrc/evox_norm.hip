@@ -1,131 +1,496 @@
-// Layer norm and cross-entropy over the rows of a population of networks, one
-// thread per row (or per column of a network's gradient).
+// Layer norm and cross-entropy over the rows of a population of networks.
+//
+// All four kernels are bound by memory: they read every row once, keep it in
+// registers, and write their results once.  A row lies over L lanes (a power
+// of two, 4 .. 64, or a block of 256 .. 1024 threads), each with NIT chunks of
+// 16 bytes; row sums are butterflies over the L lanes (and LDS across waves)
+// in fp32.
 #include "evox_net.hpp"
 
 namespace evox {
 
 namespace {
 
-unsigned net_grid(int64_t n)
+// Lanes per row and chunks per lane for n elements in chunks of N: two chunks
+// per lane up to a wave per row, then up to four (eight at 1024 threads).
+struct RowShape {
+    int L, nit, threads;
+};
+RowShape row_shape(int64_t n, int N)
 {
-    const int64_t b = (n + 255) / 256;
-    return (unsigned)(b < 1 ? 1 : b > ((int64_t)1 << 20) ? (int64_t)1 << 20 : b);
+    const int64_t chunks = (n + N - 1) / N;
+    RowShape s{4, 1, 256};
+    while (s.L < 64 && chunks > 2 * s.L) s.L *= 2;
+    while (s.L >= 64 && s.L < 1024 && chunks > 4 * s.L) s.L = s.L == 64 ? 256 : 2 * s.L;
+    while (chunks > (int64_t)s.nit * s.L) s.nit *= 2;
+    if (s.L > 256) s.threads = s.L;
+    return s;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_layernorm(NormArgs a)
+// f(integral NIT, bool WIDE): the instantiation of a shape.
+template <int V>
+struct Int {
+    static constexpr int v = V;
+};
+template <typename F>
+hipError_t with_shape(const RowShape &s, F &&f)
 {
-    for (int64_t m = (int64_t)blockIdx.x * 256 + threadIdx.x; m < a.rows.M; m += (int64_t)gridDim.x * 256) {
-        const int64_t g = net_of_row(a.rows, m);
-        if (g < 0) continue;
-        const T *x = (const T *)a.x + m * a.ldx, *ga = (const T *)a.gamma + g * a.p_stride,
-                *be = (const T *)a.beta + g * a.p_stride;
-        T *y = (T *)a.y + m * a.ldy;
-        float s = 0.0f, v = 0.0f;
-        for (int64_t j = 0; j < a.D; ++j) s += (float)x[j];
-        const float mean = s / (float)a.D;
-        for (int64_t j = 0; j < a.D; ++j) {
-            const float c = (float)x[j] - mean;
-            v = fmaf(c, c, v);
+    if (s.L <= 64) {
+        if (s.nit == 1) f(Int<1>{}, Int<0>{});
+        else if (s.nit == 2) f(Int<2>{}, Int<0>{});
+        else f(Int<4>{}, Int<0>{});
+    } else {
+        if (s.nit <= 2) f(Int<2>{}, Int<1>{});
+        else if (s.nit == 4) f(Int<4>{}, Int<1>{});
+        else f(Int<8>{}, Int<1>{});
+    }
+    return hipGetLastError();
+}
+
+// Sums (maxima) over the L lanes of a row; wide rows are a whole block, whose
+// waves meet in LDS.
+template <bool WIDE, bool MAX>
+__device__ __forceinline__ float row_all(float v, int L, float *lds)
+{
+    for (int o = WIDE ? 32 : L / 2; o > 0; o /= 2) {
+        const float w = __shfl_xor(v, o);
+        v = MAX ? fmaxf(v, w) : v + w;
+    }
+    if constexpr (WIDE) {
+        const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+        __syncthreads();
+        if (threadIdx.x % 64 == 0) lds[wave] = v;
+        __syncthreads();
+        v = lds[0];
+        for (int w = 1; w < waves; ++w) v = MAX ? fmaxf(v, lds[w]) : v + lds[w];
+    }
+    return v;
+}
+template <bool WIDE>
+__device__ __forceinline__ void row_sum2(float &a, float &b, int L, float2 *lds)
+{
+    for (int o = WIDE ? 32 : L / 2; o > 0; o /= 2) {
+        a += __shfl_xor(a, o);
+        b += __shfl_xor(b, o);
+    }
+    if constexpr (WIDE) {
+        const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+        __syncthreads();
+        if (threadIdx.x % 64 == 0) lds[wave] = make_float2(a, b);
+        __syncthreads();
+        float2 v = lds[0];
+        for (int w = 1; w < waves; ++w) {
+            v.x += lds[w].x;
+            v.y += lds[w].y;
         }
-        const float rstd = 1.0f / sqrtf(v / (float)a.D + a.eps);
-        for (int64_t j = 0; j < a.D; ++j)
-            y[j] = (T)fmaf(((float)x[j] - mean) * rstd, (float)ga[j], (float)be[j]);
+        a = v.x;
+        b = v.y;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Layer norm: the mean first, then the variance of the centred row (both from
+// the row in registers, so a large mean costs no digits).
+// ---------------------------------------------------------------------------
+template <typename T, int NIT, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int L)
+{
+    constexpr int N = NetVec<T>::N;
+    __shared__ float lds[16];
+    const int lane = threadIdx.x & (L - 1), D = (int)a.D;
+    const int64_t m = WIDE ? blockIdx.x : (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const bool live = m < a.rows.M;
+    const T *x = (const T *)a.x + m * a.ldx;
+    typename NetVec<T>::reg v[NIT];
+    if (live)
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if ((lane + i * L) * N < D) v[i] = load_chunk(x, lane + i * L, D, (T)0.0f);
+    const int g = live ? net_of_row(a.rows, m) : -1;
+    if (WIDE && g < 0) return;
+    float s = 0.0f;
+    if (live)
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if ((lane + i * L) * N < D)
+#pragma unroll
+                for (int j = 0; j < N; ++j) s += (float)v[i][j];
+    const float inv = 1.0f / (float)D, mean = row_all<WIDE, false>(s, L, lds) * inv;
+    s = 0.0f;
+    if (live)
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if ((lane + i * L) * N < D)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float c = (lane + i * L) * N + j < D ? (float)v[i][j] - mean : 0.0f;
+                    s = fmaf(c, c, s);
+                }
+    const float rstd = 1.0f / sqrtf(row_all<WIDE, false>(s, L, lds) * inv + a.eps);
+    if (g < 0) return;
+    const T *ga = (const T *)a.gamma + g * a.p_stride, *be = (const T *)a.beta + g * a.p_stride;
+    T *y = (T *)a.y + m * a.ldy;
+#pragma unroll
+    for (int i = 0; i < NIT; ++i) {
+        const int c = lane + i * L;
+        if (c * N < D) {
+            const auto gv = load_chunk(ga, c, D, (T)0.0f), bv = load_chunk(be, c, D, (T)0.0f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[i][j] = (T)fmaf(((float)v[i][j] - mean) * rstd, (float)gv[j], (float)bv[j]);
+            store_chunk(y, c, D, v[i]);
+        }
+    }
+    if (lane == 0) {
         if (a.mean) a.mean[m] = mean;
         if (a.rstd) a.rstd[m] = rstd;
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_layernorm_dx(NormArgs a)
+// ---------------------------------------------------------------------------
+// Its gradient.  A block takes a tile of one network's rows: every lane keeps
+// the sums of dy h and dy of its own columns over the rows it meets, the row
+// slots of the block add theirs in order, and the tile's sums go to the
+// scratch ([tile][2][D]); k_layernorm_params adds a network's tiles in order.
+// Rows whose chunks and sums do not fit the registers together (fp32, eight
+// chunks per lane) are read a second time.
+// ---------------------------------------------------------------------------
+template <typename T, int NIT, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a, int L, int sh)
 {
-    for (int64_t m = (int64_t)blockIdx.x * 256 + threadIdx.x; m < a.rows.M; m += (int64_t)gridDim.x * 256) {
-        const int64_t g = net_of_row(a.rows, m);
-        if (g < 0) continue;
-        const T *x = (const T *)a.x + m * a.ldx, *dy = (const T *)a.dy + m * a.ldy,
-                *ga = (const T *)a.gamma + g * a.p_stride;
-        T *dx = (T *)a.dx + m * a.lddx;
-        const float mean = a.mean_in[m], rstd = a.rstd_in[m];
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int64_t j = 0; j < a.D; ++j) {
-            const float p = (float)dy[j] * (float)ga[j];
-            s1 += p;
-            s2 = fmaf(p, ((float)x[j] - mean) * rstd, s2);
+    constexpr int N = NetVec<T>::N;
+    constexpr bool kHold = NIT * (8 + 2 * N) <= 96;
+    extern __shared__ float sums[];  // [256 / L - 1 row slots][2][NIT][N][L] (narrow rows)
+    __shared__ float2 lds[16];
+    const NetTile t = net_tile(a.rows, sh, blockIdx.x);
+    if (t.g < 0) return;
+    const int lane = threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : 256 / L, D = (int)a.D;
+    const T *ga = (const T *)a.gamma + t.g * a.p_stride;
+    float sg[NIT][N], sb[NIT][N];
+#pragma unroll
+    for (int i = 0; i < NIT; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) sg[i][j] = sb[i][j] = 0.0f;
+    const float inv = 1.0f / (float)D;
+    // every slot makes as many rounds (the row sums need all lanes)
+    for (int64_t m0 = t.lo; m0 < t.hi; m0 += slots) {
+        const int64_t m = m0 + slot;
+        const bool live = m < t.hi;
+        const T *x = (const T *)a.x + m * a.ldx, *dy = (const T *)a.dy + m * a.ldy;
+        typename NetVec<T>::reg xv[kHold ? NIT : 1], dv[kHold ? NIT : 1];
+        float mean = 0.0f, rstd = 0.0f, s1 = 0.0f, s2 = 0.0f;
+        if (live) {
+            mean = a.mean_in[m];
+            rstd = a.rstd_in[m];
+#pragma unroll
+            for (int i = 0; i < NIT; ++i) {
+                const int c = lane + i * L, k = kHold ? i : 0;
+                if (c * N >= D) continue;
+                xv[k] = load_chunk(x, c, D, (T)0.0f);
+                dv[k] = load_chunk(dy, c, D, (T)0.0f);
+                if constexpr (!kHold) {
+                    const auto gv = load_chunk(ga, c, D, (T)0.0f);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float p = (float)dv[k][j] * (float)gv[j];
+                        s1 += p;
+                        s2 = fmaf(p, ((float)xv[k][j] - mean) * rstd, s2);
+                    }
+                }
+            }
+            if constexpr (kHold)
+#pragma unroll
+                for (int i = 0; i < NIT; ++i) {
+                    const int c = lane + i * L;
+                    if (c * N >= D) continue;
+                    const auto gv = load_chunk(ga, c, D, (T)0.0f);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float p = (float)dv[i][j] * (float)gv[j];
+                        s1 += p;
+                        s2 = fmaf(p, ((float)xv[i][j] - mean) * rstd, s2);
+                    }
+                }
         }
-        s1 /= (float)a.D;
-        s2 /= (float)a.D;
-        for (int64_t j = 0; j < a.D; ++j)
-            dx[j] = (T)(rstd * ((float)dy[j] * (float)ga[j] - s1 - ((float)x[j] - mean) * rstd * s2));
+        row_sum2<WIDE>(s1, s2, L, lds);
+        if (!live) continue;
+        s1 *= inv;
+        s2 *= inv;
+#pragma unroll
+        for (int i = 0; i < NIT; ++i) {
+            const int c = lane + i * L, k = kHold ? i : 0;
+            if (c * N >= D) continue;
+            if constexpr (!kHold) {
+                xv[0] = load_chunk(x, c, D, (T)0.0f);
+                dv[0] = load_chunk(dy, c, D, (T)0.0f);
+            }
+            const auto gv = load_chunk(ga, c, D, (T)0.0f);
+            typename NetVec<T>::reg out;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float h = ((float)xv[k][j] - mean) * rstd, d = (float)dv[k][j];
+                sg[i][j] = fmaf(d, h, sg[i][j]);
+                sb[i][j] += d;
+                out[j] = (T)(rstd * (fmaf(d, (float)gv[j], -s1) - h * s2));
+            }
+            if (a.dx) store_chunk((T *)a.dx + m * a.lddx, c, D, out);
+        }
     }
+    if (!a.dgamma) return;
+    if constexpr (!WIDE) {
+        if (slot > 0)
+#pragma unroll
+            for (int i = 0; i < NIT; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    sums[((((slot - 1) * 2 + 0) * NIT + i) * N + j) * L + lane] = sg[i][j];
+                    sums[((((slot - 1) * 2 + 1) * NIT + i) * N + j) * L + lane] = sb[i][j];
+                }
+        __syncthreads();
+        if (slot > 0) return;
+        for (int r = 0; r < slots - 1; ++r)
+#pragma unroll
+            for (int i = 0; i < NIT; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    sg[i][j] += sums[(((r * 2 + 0) * NIT + i) * N + j) * L + lane];
+                    sb[i][j] += sums[(((r * 2 + 1) * NIT + i) * N + j) * L + lane];
+                }
+    }
+    float *part = (float *)a.scratch + (int64_t)blockIdx.x * 2 * D;
+#pragma unroll
+    for (int i = 0; i < NIT; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int e = (lane + i * L) * N + j;
+            if (e < D) {
+                part[e] = sg[i][j];
+                part[D + e] = sb[i][j];
+            }
+        }
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_layernorm_dp(NormArgs a)
+__global__ __launch_bounds__(256) void k_layernorm_params(NormArgs a, int sh)
 {
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < a.rows.G * a.D; q += (int64_t)gridDim.x * 256) {
-        const int64_t g = q / a.D, j = q % a.D;
+    const int64_t g = blockIdx.y;
+    const int e = blockIdx.x * 256 + threadIdx.x, D = (int)a.D;
+    if (e >= 2 * D) return;
+    for (int64_t gg = g; gg < a.rows.G; gg += gridDim.y) {
         int64_t lo, hi;
-        net_rows(a.rows, g, &lo, &hi);
-        float sg = 0.0f, sb = 0.0f;
-        for (int64_t m = lo; m < hi; ++m) {
-            const float dy = (float)((const T *)a.dy)[m * a.ldy + j];
-            const float h = ((float)((const T *)a.x)[m * a.ldx + j] - a.mean_in[m]) * a.rstd_in[m];
-            sb += dy;
-            sg = fmaf(dy, h, sg);
-        }
-        ((T *)a.dgamma)[g * a.dp_stride + j] = (T)sg;
-        ((T *)a.dbeta)[g * a.dp_stride + j] = (T)sb;
+        net_rows(a.rows, gg, &lo, &hi);
+        const int64_t t0 = net_first_tile(a.rows, sh, gg), n = (hi - lo + ((int64_t)1 << sh) - 1) >> sh;
+        const float *part = (const float *)a.scratch + t0 * 2 * D + e;
+        float s = 0.0f;
+        for (int64_t t = 0; t < n; ++t) s += part[t * 2 * D];
+        if (e < D) ((T *)a.dgamma)[gg * a.dp_stride + e] = (T)s;
+        else ((T *)a.dbeta)[gg * a.dp_stride + e - D] = (T)s;
     }
 }
+
+// Rows per tile of the gradient, as a power of two: 64 at most (its sums are
+// then 4 % or less of the rows' traffic), fewer where that leaves less than
+// about four blocks per CU.
+int norm_tile_shift(const NormArgs &a)
+{
+    int sh = 6;
+    while (sh > 3 && (a.rows.M >> sh) < 1024) --sh;
+    return sh;
+}
+
+// ---------------------------------------------------------------------------
+// Cross-entropy.  A block takes a tile of one network's rows; a row's logits
+// stay in registers from the maximum to the gradient.  The tile's loss (fp64)
+// and count go to the scratch and are added per network in order.  The
+// gradient needs the network's count first: where a tile is the whole network
+// the block counts the labels itself, else k_xent_count has.
+// ---------------------------------------------------------------------------
+constexpr int kCountShift = 12;  // labels per block of k_xent_count
 
 __device__ __forceinline__ int xent_label(const XentArgs &a, int64_t g, int64_t m)
 {
     return a.labels[a.labels_shared ? m - g * a.rows.n : m];
 }
+__device__ __forceinline__ bool xent_counts(const XentArgs &a, int label) { return label >= 0 && label < a.C; }
 
-// Fitness of a network, and its count of rows (in the scratch).
-template <typename T>
-__global__ __launch_bounds__(256) void k_xent_fit(XentArgs a)
+struct XentScratch {
+    double *loss;    // [tiles]
+    int32_t *count;  // [tiles] rows that count
+    int32_t *labels; // [tiles of 2^kCountShift rows] the same, before the gradient
+};
+__host__ __device__ __forceinline__ XentScratch xent_layout(const XentArgs &a, int sh)
 {
-    for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < a.rows.G; g += (int64_t)gridDim.x * 256) {
-        int64_t lo, hi, count = 0;
-        net_rows(a.rows, g, &lo, &hi);
-        double sum = 0.0;
-        for (int64_t m = lo; m < hi; ++m) {
-            const T *z = (const T *)a.logits + m * a.ldz;
-            const int lab = xent_label(a, g, m);
-            if (lab < 0 || lab >= a.C) continue;
-            float top = -INFINITY, s = 0.0f;
-            for (int64_t c = 0; c < a.C; ++c) top = fmaxf(top, (float)z[c]);
-            for (int64_t c = 0; c < a.C; ++c) s += expf((float)z[c] - top);
-            sum += (double)(logf(s) + (top - (float)z[lab]));
+    const int64_t n = net_tiles(a.rows, sh);
+    XentScratch s;
+    s.loss = (double *)a.scratch;
+    s.count = (int32_t *)(s.loss + n);
+    s.labels = s.count + n;
+    return s;
+}
+
+__global__ __launch_bounds__(256) void k_xent_count(XentArgs a, int sh)
+{
+    __shared__ int waves[4];
+    const NetTile t = net_tile(a.rows, kCountShift, blockIdx.x);
+    if (t.g < 0) return;
+    int n = 0;
+    for (int64_t m = t.lo + threadIdx.x; m < t.hi; m += 256) n += xent_counts(a, xent_label(a, t.g, m));
+    for (int o = 32; o > 0; o /= 2) n += __shfl_xor(n, o);
+    if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) xent_layout(a, sh).labels[blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
+}
+
+// Tiles of 2^sh rows; whole: a tile is a whole network (rows may be more).
+template <typename T, int NIT, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, int sh, bool whole)
+{
+    constexpr int N = NetVec<T>::N;
+    __shared__ float lds[16];
+    __shared__ double wave_loss[16];
+    __shared__ int wave_count[16];
+    NetTile t;
+    if (whole) {
+        t.g = blockIdx.x;
+        t.lo = t.g * a.rows.n;
+        t.hi = t.lo + a.rows.n;
+    } else {
+        t = net_tile(a.rows, sh, blockIdx.x);
+        if (t.g < 0) return;
+    }
+    const int lane = threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : 256 / L, C = (int)a.C;
+    float scale = 0.0f;
+    if (a.dz) {
+        int n = 0;
+        const int wl = threadIdx.x % 64;
+        if (whole) {
+            for (int64_t m = t.lo + wl; m < t.hi; m += 64) n += xent_counts(a, xent_label(a, t.g, m));
+        } else {
+            int64_t lo, hi;
+            net_rows(a.rows, t.g, &lo, &hi);
+            const int64_t t0 = net_first_tile(a.rows, kCountShift, t.g),
+                          k = (hi - lo + ((int64_t)1 << kCountShift) - 1) >> kCountShift;
+            const int32_t *labels = xent_layout(a, sh).labels;
+            for (int64_t i = wl; i < k; i += 64) n += labels[t0 + i];
+        }
+        for (int o = 32; o > 0; o /= 2) n += __shfl_xor(n, o);
+        scale = 1.0f / (float)n;  // not used where no row counts
+    }
+    double loss = 0.0;
+    int count = 0;
+    for (int64_t m0 = t.lo; m0 < t.hi; m0 += slots) {
+        const int64_t m = m0 + slot;
+        const bool live = m < t.hi;
+        const T *z = (const T *)a.logits + m * a.ldz;
+        const int label = live ? xent_label(a, t.g, m) : -1;
+        const bool counts = live && xent_counts(a, label);
+        typename NetVec<T>::reg v[NIT];
+        float top = -INFINITY, sum = 0.0f;
+        if (counts)
+#pragma unroll
+            for (int i = 0; i < NIT; ++i)
+                if ((lane + i * L) * N < C) v[i] = load_chunk(z, lane + i * L, C, (T)-INFINITY);
+        // the label's logit, before the gradient may take its place
+        const float at = counts ? (float)z[label] : 0.0f;
+        if (counts)
+#pragma unroll
+            for (int i = 0; i < NIT; ++i)
+                if ((lane + i * L) * N < C)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) top = fmaxf(top, (float)v[i][j]);
+        top = row_all<WIDE, true>(top, L, lds);
+        float e[NIT][N];
+        if (counts)
+#pragma unroll
+            for (int i = 0; i < NIT; ++i)
+                if ((lane + i * L) * N < C)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        // past the row's end v is -inf: nothing, but in a row of -inf alone, all NaN anyway
+                        e[i][j] = expf((float)v[i][j] - top);
+                        sum += e[i][j];
+                    }
+        sum = row_all<WIDE, false>(sum, L, lds);
+        if (lane == 0 && counts) {
+            loss += (double)(logf(sum) + (top - at));
             ++count;
         }
-        a.fit[g] = (float)(sum / (double)count);
-        ((float *)a.scratch)[g] = (float)count;
+        if (a.dz && live) {
+            T *dz = (T *)a.dz + m * a.lddz;
+            const float f = scale / sum;
+#pragma unroll
+            for (int i = 0; i < NIT; ++i) {
+                const int c = lane + i * L;
+                if (c * N >= C) continue;
+                typename NetVec<T>::reg out;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float p = e[i][j] * f;
+                    out[j] = counts ? (T)(c * N + j == label ? fmaf(e[i][j] / sum, scale, -scale) : p) : (T)0.0f;
+                }
+                store_chunk(dz, c, C, out);
+            }
+        }
+    }
+    // the slots' losses in a fixed order: over the lanes, then the waves
+    for (int o = 32; o > 0; o /= 2) {
+        loss += __shfl_xor(loss, o);
+        count += __shfl_xor(count, o);
+    }
+    const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    if (threadIdx.x % 64 == 0) {
+        wave_loss[wave] = loss;
+        wave_count[wave] = count;
+    }
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    for (int w = 1; w < waves; ++w) {
+        loss += wave_loss[w];
+        count += wave_count[w];
+    }
+    if (whole) {
+        a.fit[t.g] = (float)(loss / (double)count);
+    } else {
+        const XentScratch s = xent_layout(a, sh);
+        s.loss[blockIdx.x] = loss;
+        s.count[blockIdx.x] = count;
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_xent_grad(XentArgs a)
+// fit[g] from the network's tiles, a wave per network.
+__global__ __launch_bounds__(256) void k_xent_fit(XentArgs a, int sh)
 {
-    for (int64_t m = (int64_t)blockIdx.x * 256 + threadIdx.x; m < a.rows.M; m += (int64_t)gridDim.x * 256) {
-        const int64_t g = net_of_row(a.rows, m);
-        if (g < 0) continue;
-        const T *z = (const T *)a.logits + m * a.ldz;
-        T *dz = (T *)a.dz + m * a.lddz;
-        const int lab = xent_label(a, g, m);
-        if (lab < 0 || lab >= a.C) {
-            for (int64_t c = 0; c < a.C; ++c) dz[c] = (T)0.0f;
-            continue;
-        }
-        float top = -INFINITY, s = 0.0f;
-        for (int64_t c = 0; c < a.C; ++c) top = fmaxf(top, (float)z[c]);
-        for (int64_t c = 0; c < a.C; ++c) s += expf((float)z[c] - top);
-        const float count = ((const float *)a.scratch)[g];
-        for (int64_t c = 0; c < a.C; ++c)
-            dz[c] = (T)((expf((float)z[c] - top) / s - (c == lab ? 1.0f : 0.0f)) / count);
+    const int64_t g = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (g >= a.rows.G) return;
+    int64_t lo, hi;
+    net_rows(a.rows, g, &lo, &hi);
+    const int64_t t0 = net_first_tile(a.rows, sh, g), k = (hi - lo + ((int64_t)1 << sh) - 1) >> sh;
+    const XentScratch s = xent_layout(a, sh);
+    double loss = 0.0;
+    int64_t count = 0;
+    for (int64_t i = threadIdx.x % 64; i < k; i += 64) {
+        loss += s.loss[t0 + i];
+        count += s.count[t0 + i];
     }
+    for (int o = 32; o > 0; o /= 2) {
+        loss += __shfl_xor(loss, o);
+        count += __shfl_xor(count, o);
+    }
+    if (threadIdx.x % 64 == 0) a.fit[g] = (float)(loss / (double)count);
+}
+
+// Whether every network is one block's: as many rows for each, and either
+// networks enough to fill the chip or little work in each.
+bool xent_whole(const XentArgs &a)
+{
+    return !a.rows.off && a.rows.n <= 4096 && (a.rows.G >= 1024 || a.rows.n * a.C <= 16384);
+}
+// Rows per tile, as a power of two: 64 of a short row; a wide row's tile is at
+// least two rows, for about eight blocks per CU.
+int xent_tile_shift(const XentArgs &a)
+{
+    int sh = 6;
+    while (sh > 1 && (a.rows.M >> sh) < 2048) --sh;
+    return sh;
 }
 
 }  // namespace
@@ -133,32 +498,66 @@ __global__ __launch_bounds__(256) void k_xent_grad(XentArgs a)
 hipError_t launch_layernorm(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
-        hipLaunchKernelGGL((k_layernorm<decltype(t)>), dim3(net_grid(a.rows.M)), dim3(256), 0, s, a);
-        return hipGetLastError();
+        using T = decltype(t);
+        const RowShape r = row_shape(a.D, NetVec<T>::N);
+        const int64_t per = r.L <= 64 ? 256 / r.L : 1;
+        return with_shape(r, [&](auto nit, auto wide) {
+            hipLaunchKernelGGL((k_layernorm<T, nit.v, wide.v>), dim3((unsigned)((a.rows.M + per - 1) / per)),
+                               dim3(r.threads), 0, s, a, r.L);
+        });
     });
 }
 
-size_t layernorm_grad_scratch(const NormArgs &) { return 256; }
+size_t layernorm_grad_scratch(const NormArgs &a)
+{
+    return 8 * (size_t)((a.rows.M >> norm_tile_shift(a)) + a.rows.G) * (size_t)a.D;
+}
 
 hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = decltype(t);
-        if (a.dgamma)  // first: dx may take dy's place
-            hipLaunchKernelGGL((k_layernorm_dp<T>), dim3(net_grid(a.rows.G * a.D)), dim3(256), 0, s, a);
-        if (a.dx && a.rows.M) hipLaunchKernelGGL((k_layernorm_dx<T>), dim3(net_grid(a.rows.M)), dim3(256), 0, s, a);
+        const RowShape r = row_shape(a.D, NetVec<T>::N);
+        const int sh = norm_tile_shift(a);
+        const int64_t tiles = net_tiles(a.rows, sh);
+        hipError_t e = hipSuccess;
+        if (a.rows.M > 0)
+            e = with_shape(r, [&](auto nit, auto wide) {
+                const size_t lds = wide.v ? 0 : sizeof(float) * 2 * nit.v * NetVec<T>::N * (256 - r.L);
+                hipLaunchKernelGGL((k_layernorm_grad<T, nit.v, wide.v>), dim3((unsigned)tiles), dim3(r.threads), lds, s,
+                                   a, r.L, sh);
+            });
+        if (e != hipSuccess || !a.dgamma) return e;
+        const unsigned gy = (unsigned)(a.rows.G < 32768 ? a.rows.G : 32768);
+        hipLaunchKernelGGL((k_layernorm_params<T>), dim3((unsigned)((2 * a.D + 255) / 256), gy), dim3(256), 0, s, a, sh);
         return hipGetLastError();
     });
 }
 
-size_t xent_scratch(const XentArgs &a) { return 4 * (size_t)a.rows.G; }
+size_t xent_scratch(const XentArgs &a)
+{
+    return 12 * (size_t)((a.rows.M >> xent_tile_shift(a)) + a.rows.G) +
+           4 * (size_t)((a.rows.M >> kCountShift) + a.rows.G);
+}
 
 hipError_t launch_xent(const XentArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL((k_xent_fit<T>), dim3(net_grid(a.rows.G)), dim3(256), 0, s, a);
-        if (a.dz && a.rows.M) hipLaunchKernelGGL((k_xent_grad<T>), dim3(net_grid(a.rows.M)), dim3(256), 0, s, a);
+        const RowShape r = row_shape(a.C, NetVec<T>::N);
+        const bool whole = xent_whole(a);
+        const int sh = xent_tile_shift(a);
+        if (a.dz && !whole)
+            hipLaunchKernelGGL(k_xent_count, dim3((unsigned)net_tiles(a.rows, kCountShift)), dim3(256), 0, s, a, sh);
+        hipError_t e = hipSuccess;
+        if (a.rows.M > 0 || whole)
+            e = with_shape(r, [&](auto nit, auto wide) {
+                hipLaunchKernelGGL((k_xent<T, nit.v, wide.v>),
+                                   dim3((unsigned)(whole ? a.rows.G : net_tiles(a.rows, sh))), dim3(r.threads), 0, s, a,
+                                   r.L, sh, whole);
+            });
+        if (e != hipSuccess || whole) return e;
+        hipLaunchKernelGGL(k_xent_fit, dim3((unsigned)((a.rows.G + 3) / 4)), dim3(256), 0, s, a, sh);
         return hipGetLastError();
     });
 }
