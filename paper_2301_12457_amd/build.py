@@ -1,8 +1,9 @@
 """Build the gfx950 HIP library paper_2301_12457_amd/libevox.so in-tree.
 
 Every translation unit is compiled by hipcc for gfx950 only, in parallel:
-two per benchmark function (evox_fn.hip and evox_res.hip with -DEVOX_FN=<id>), the
-function-independent kernels (evox_common.hip) and the C ABI
+two per benchmark function (evox_fn.hip and evox_res.hip with -DEVOX_FN=<id>), one
+per element type of the networks' layers (evox_linear_tile.hip with
+-DEVOX_NET_TYPE=<id>), the function-independent kernels (evox_common.hip) and the C ABI
 (evox_api.cpp), then linked into one shared library.
 
 Flags: -ffp-contract=off (fused multiply-adds only where fmaf() is written,
@@ -23,6 +24,7 @@ BUILD_DIR = os.path.join(HERE, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 N_FN = 6
+N_NET_TYPES = 3
 
 COMMON_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
@@ -41,6 +43,8 @@ def _units():
     units.append((os.path.join(CSRC, "evox_maes.hip"), "evox_maes.o", []))
     units.append((os.path.join(CSRC, "evox_nsga2.hip"), "evox_nsga2.o", []))
     units.append((os.path.join(CSRC, "evox_linear.hip"), "evox_linear.o", []))
+    for ty in range(N_NET_TYPES):
+        units.append((os.path.join(CSRC, "evox_linear_tile.hip"), f"evox_linear_tile{ty}.o", [f"-DEVOX_NET_TYPE={ty}"]))
     units.append((os.path.join(CSRC, "evox_norm.hip"), "evox_norm.o", []))
     units.append((os.path.join(CSRC, "evox_api.cpp"), "evox_api.o", ["-x", "hip"]))
     return units

@@ -1,14 +1,11 @@
 // Linear layers of a population of networks: y = act(x W_g^T + b_g) + r and
 // its gradient.
-#include <type_traits>
-
-#include "evox_net.hpp"
+#include "evox_tile.hpp"
 
 namespace evox {
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
 typedef _Float16 f16x4u __attribute__((ext_vector_type(4), aligned(2)));
@@ -27,12 +24,6 @@ struct Quad<f16_t> {
     typedef f16x4u mem;
 };
 
-unsigned net_grid(int64_t n)
-{
-    const int64_t b = (n + 255) / 256;
-    return (unsigned)(b < 1 ? 1 : b > ((int64_t)1 << 20) ? (int64_t)1 << 20 : b);
-}
-
 // ---------------------------------------------------------------------------
 // One 16 x 16 tile of products over 16 bytes of K per lane: lane l brings
 // elements k = KV (l / 16) .. + KV of row l % 16 of either operand (any split of
@@ -44,21 +35,6 @@ struct Mma {
     typedef typename NetVec<T>::reg reg;
     static constexpr int KV = NetVec<T>::N, KS = 4 * KV;  // k per lane, per step
 };
-__device__ __forceinline__ f32x4 mma16(NetVec<bf16_t>::reg a, NetVec<bf16_t>::reg b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma16(NetVec<f16_t>::reg a, NetVec<f16_t>::reg b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma16(NetVec<float>::reg a, NetVec<float>::reg b, f32x4 c)
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-    return c;
-}
-
 // The epilogue of four neighbouring outputs o .. o + 3 of row m: bias,
 // pre-activation, activation, residual, one rounding each.
 template <typename T>
@@ -120,7 +96,7 @@ __global__ __launch_bounds__(256) void k_linear_thin(LinearArgs a, int sh, uint3
     __shared__ f32x4 part[WK > 1 ? 4 / WK * (WK - 1) * RB * NB * 64 : 1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, l16 = lane % 16,
               q = lane / 16, wk = wave % WK, wt = wave / WK;
-    const int64_t unit = (int64_t)blockIdx.x * (4 / WK) + wt;
+    const int64_t unit = net_block() * (4 / WK) + wt;
     NetTile t;
     t.g = -1;
     const int64_t tile = unit / out_tiles;
@@ -203,52 +179,96 @@ __global__ __launch_bounds__(256) void k_linear_thin(LinearArgs a, int sh, uint3
     }
 }
 
-// d = dy act'(z), rounded to the element type.
-template <typename T>
-__device__ __forceinline__ float grad_of_z(const LinearGradArgs &a, int64_t m, int64_t o)
-{
-    const float d = (float)((const T *)a.dy)[m * a.lddy + o];
-    if (a.act == ACT_NONE) return d;
-    return d * act_slope(a.act, (float)((const T *)a.z)[m * a.ldz + o]);
-}
+// d = dy act'(z), rounded to the element type (where a.act is not none and a
+// product needs it), and the tiles' column sums of the unrounded d (where db is
+// wanted): a block takes 2^kDzShift rows of a network and 256 chunks of 16 bytes
+// of their columns, L lanes to a row, and adds its row slots in order.
+constexpr int kDzShift = 6;
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_dx(LinearGradArgs a)
+__global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int L, T *d, int64_t ldd, float *sums)
 {
-    const T *w = (const T *)a.w;
-    T *dx = (T *)a.dx;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < a.rows.M * a.n_in; q += (int64_t)gridDim.x * 256) {
-        const int64_t m = q / a.n_in, i = q % a.n_in, g = net_of_row(a.rows, m);
-        if (g < 0) continue;
-        float s = 0.0f;
-        for (int64_t o = 0; o < a.n_out; ++o)
-            s = fmaf((float)(T)grad_of_z<T>(a, m, o), (float)w[g * a.w_stride + o * a.ldw + i], s);
-        dx[m * a.lddx + i] = (T)s;
-    }
+    constexpr int N = NetVec<T>::N;
+    typedef typename NetVec<T>::reg reg;
+    extern __shared__ float slots_sum[];  // [256 / L - 1][N][L]
+    const int64_t cols = (a.n_out + 256 * N - 1) / (256 * N), tile = net_block() / cols;
+    const NetTile t = net_tile(a.rows, kDzShift, tile);
+    if (t.g < 0) return;
+    const int lane = threadIdx.x & (L - 1), slot = threadIdx.x / L, slots = 256 / L, n = (int)a.n_out,
+              c = (int)(net_block() - tile * cols) * 256 + lane;
+    float s[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = 0.0f;
+    if (c * N < n)
+        for (int64_t m = t.lo + slot; m < t.hi; m += slots) {
+            const reg dy = load_chunk((const T *)a.dy + m * a.lddy, c, n, (T)0.0f);
+            if (a.act == ACT_NONE) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) s[j] += (float)dy[j];
+                continue;
+            }
+            const reg z = load_chunk((const T *)a.z + m * a.ldz, c, n, (T)0.0f);
+            reg out;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float v = (float)dy[j] * act_slope(a.act, (float)z[j]);
+                s[j] += v;
+                out[j] = (T)v;
+            }
+            if (d) store_chunk(d + m * ldd, c, n, out);
+        }
+    if (!sums) return;
+    if (slot > 0)
+#pragma unroll
+        for (int j = 0; j < N; ++j) slots_sum[((slot - 1) * N + j) * L + lane] = s[j];
+    __syncthreads();
+    if (slot > 0 || c * N >= n) return;
+    for (int r = 0; r < slots - 1; ++r)
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] += slots_sum[(r * N + j) * L + lane];
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (c * N + j < n) sums[tile * n + c * N + j] = s[j];
 }
 
-// Column n_in of a network's gradient is db.
+// db from a network's tiles, in order.
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_dw(LinearGradArgs a)
+__global__ __launch_bounds__(256) void k_linear_db(LinearGradArgs a, const float *sums)
 {
-    const T *x = (const T *)a.x;
-    T *dw = (T *)a.dw, *db = (T *)a.db;
-    const int64_t cols = a.n_in + 1;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < a.rows.G * a.n_out * cols;
-         q += (int64_t)gridDim.x * 256) {
-        const int64_t i = q % cols, o = q / cols % a.n_out, g = q / cols / a.n_out;
-        if (i < a.n_in ? !dw : !db) continue;
+    const int o = blockIdx.x * 256 + threadIdx.x;
+    if (o >= a.n_out) return;
+    for (int64_t g = blockIdx.y; g < a.rows.G; g += gridDim.y) {
         int64_t lo, hi;
         net_rows(a.rows, g, &lo, &hi);
+        const int64_t t0 = net_first_tile(a.rows, kDzShift, g), n = (hi - lo + (1 << kDzShift) - 1) >> kDzShift;
         float s = 0.0f;
-        for (int64_t m = lo; m < hi; ++m) {
-            const float d = grad_of_z<T>(a, m, o);
-            if (i == a.n_in) s += d;
-            else s = fmaf((float)(T)d, (float)x[(a.x_shared ? m - lo : m) * a.ldx + i], s);
-        }
-        if (i == a.n_in) db[g * a.db_stride + o] = (T)s;
-        else dw[g * a.dw_stride + o * a.lddw + i] = (T)s;
+        for (int64_t t = 0; t < n; ++t) s += sums[(t0 + t) * a.n_out + o];
+        ((T *)a.db)[g * a.db_stride + o] = (T)s;
     }
+}
+
+// The scratch: d, then the tiles' column sums.
+struct GradScratch {
+    int64_t ldd;
+    size_t sums, end;
+};
+GradScratch grad_layout(const LinearGradArgs &a)
+{
+    GradScratch g;
+    const size_t e = a.dtype == NET_F32 ? 4 : 2;
+    g.ldd = (a.n_out + 7) / 8 * 8;
+    g.sums = (e * (size_t)a.rows.M * (size_t)g.ldd + 255) / 256 * 256;
+    g.end = g.sums + 4 * ((size_t)(a.rows.M >> kDzShift) + (size_t)a.rows.G) * (size_t)a.n_out;
+    return g;
+}
+
+// Tiles of 64 where either side of the result is no more than that or larger
+// ones would leave CUs without a block; of 256 (16 bits) where they fill the chip.
+int tile_size(int32_t dtype, int64_t ni, int64_t nj, int64_t results)
+{
+    if (ni <= 64 || nj <= 64 || results < (int64_t)256 * 128 * 128) return 0;
+    if (dtype != NET_F32 && ni >= 192 && nj >= 192 && results >= (int64_t)512 * 256 * 256) return 2;
+    return 1;
 }
 
 }  // namespace
@@ -256,21 +276,23 @@ __global__ __launch_bounds__(256) void k_linear_dw(LinearGradArgs a)
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
-        using T = decltype(t);
-        // rows of a wave's tile by the mean rows per network
+        using T = typename NetElement<t.value>::type;
         const int64_t mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
+        if (mean > 32 && a.n_out > 32 && a.n_in >= 64)
+            return launch_linear_tiles<t.value>(a, tile_size(a.dtype, a.n_out, mean, a.rows.M * a.n_out), s);
+        // rows of a wave's tile by the mean rows per network
         const int rb = mean <= 16 ? 1 : mean <= 32 ? 2 : 4, sh = rb == 1 ? 4 : rb == 2 ? 5 : 6, nb = rb == 1 ? 1 : 2;
         const uint32_t out_tiles = (uint32_t)((a.n_out + 16 * nb - 1) / (16 * nb));
         const int64_t units = net_tiles(a.rows, sh) * out_tiles;
         const int64_t steps = (a.n_in + Mma<T>::KS - 1) / Mma<T>::KS;
         const bool split = units < 4096 && steps >= 16;
-        const unsigned blocks = (unsigned)(split ? units : (units + 3) / 4);
+        const dim3 blocks = net_grid(split ? units : (units + 3) / 4);
         auto go = [&](auto r, auto n) {
             if (split)
-                hipLaunchKernelGGL((k_linear_thin<T, r.value, n.value, 4>), dim3(blocks), dim3(256), 0, s, a, sh,
+                hipLaunchKernelGGL((k_linear_thin<T, r.value, n.value, 4>), blocks, dim3(256), 0, s, a, sh,
                                    out_tiles, units);
             else
-                hipLaunchKernelGGL((k_linear_thin<T, r.value, n.value, 1>), dim3(blocks), dim3(256), 0, s, a, sh,
+                hipLaunchKernelGGL((k_linear_thin<T, r.value, n.value, 1>), blocks, dim3(256), 0, s, a, sh,
                                    out_tiles, units);
         };
         using std::integral_constant;
@@ -281,17 +303,40 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
     });
 }
 
-size_t linear_grad_scratch(const LinearGradArgs &) { return 256; }
+size_t linear_grad_scratch(const LinearGradArgs &a) { return grad_layout(a).end; }
 
 hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
-        if (a.dx && a.rows.M)
-            hipLaunchKernelGGL((k_linear_dx<decltype(t)>), dim3(net_grid(a.rows.M * a.n_in)), dim3(256), 0, s, a);
-        if (a.dw || a.db)
-            hipLaunchKernelGGL((k_linear_dw<decltype(t)>), dim3(net_grid(a.rows.G * a.n_out * (a.n_in + 1))),
-                               dim3(256), 0, s, a);
-        return hipGetLastError();
+        using T = typename NetElement<t.value>::type;
+        constexpr int N = NetVec<T>::N;
+        const GradScratch l = grad_layout(a);
+        const bool own = a.act != ACT_NONE && (a.dx || a.dw);
+        T *d = own ? (T *)a.scratch : nullptr;
+        float *sums = a.db ? (float *)((char *)a.scratch + l.sums) : nullptr;
+        hipError_t e = hipSuccess;
+        if (a.rows.M > 0 && (d || sums)) {
+            int L = 4;
+            while (L < 256 && L * N < a.n_out) L *= 2;
+            const int64_t cols = (a.n_out + 256 * N - 1) / (256 * N);
+            hipLaunchKernelGGL((k_linear_dz<T>), net_grid(net_tiles(a.rows, kDzShift) * cols), dim3(256),
+                               sizeof(float) * N * (256 - L), s, a, L, d, l.ldd, sums);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+        if (a.db) {
+            hipLaunchKernelGGL((k_linear_db<T>),
+                               dim3((unsigned)((a.n_out + 255) / 256), (unsigned)(a.rows.G < 32768 ? a.rows.G : 32768)),
+                               dim3(256), 0, s, a, sums);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
+        const void *dd = own ? d : a.dy;
+        const int64_t ldd = own ? l.ldd : a.lddy, mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
+        if (a.dx)
+            e = launch_linear_dx_tiles<t.value>(a, dd, ldd, tile_size(a.dtype, a.n_in, mean, a.rows.M * a.n_in), s);
+        if (e == hipSuccess && a.dw)
+            e = launch_linear_dw_tiles<t.value>(a, dd, ldd,
+                                                tile_size(a.dtype, a.n_in, a.n_out, a.rows.G * a.n_in * a.n_out), s);
+        return e;
     });
 }
 

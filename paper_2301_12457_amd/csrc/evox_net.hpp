@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace evox {
 
@@ -67,16 +68,38 @@ hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s);
 size_t xent_scratch(const XentArgs &a);
 hipError_t launch_xent(const XentArgs &a, hipStream_t s);
 
+// The large cases: tiles through LDS (one file per element type).  size 0, 1, 2:
+// tiles of 64, 128 or (16 bits) 256 a side.  d: dy act'(z) in the element type.
+template <int TYPE>
+hipError_t launch_linear_tiles(const LinearArgs &a, int size, hipStream_t s);
+template <int TYPE>
+hipError_t launch_linear_dx_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, int size, hipStream_t s);
+template <int TYPE>
+hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, int size, hipStream_t s);
+
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
-// Type-dependent launches: f is called with a value of the element type.
+template <int TYPE>
+struct NetElement {
+    typedef f16_t type;
+};
+template <>
+struct NetElement<NET_F32> {
+    typedef float type;
+};
+template <>
+struct NetElement<NET_BF16> {
+    typedef bf16_t type;
+};
+
+// Type-dependent launches: f is called with an integral constant, the type.
 template <typename F>
 hipError_t net_dispatch(int32_t dtype, F &&f)
 {
-    if (dtype == NET_F32) return f(float{});
-    if (dtype == NET_BF16) return f(bf16_t{});
-    return f(f16_t{});
+    if (dtype == NET_F32) return f(std::integral_constant<int, NET_F32>{});
+    if (dtype == NET_BF16) return f(std::integral_constant<int, NET_BF16>{});
+    return f(std::integral_constant<int, NET_F16>{});
 }
 
 // Sixteen bytes of a row: loads and stores need only the element's alignment
@@ -119,6 +142,15 @@ __device__ __forceinline__ int64_t net_off(const NetRows &r, int64_t g)
     const int64_t o = r.off[g];
     return o < 0 ? 0 : o > r.M ? r.M : o;
 }
+
+// Grids of any number of blocks: HIP bounds the threads of a grid dimension by
+// 2^32, so the blocks are laid over two.
+inline dim3 net_grid(int64_t blocks)
+{
+    const int64_t x = (int64_t)1 << 20;
+    return blocks <= x ? dim3((unsigned)blocks) : dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+__device__ __forceinline__ int64_t net_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // The rows [lo, hi) of network g, within [0, M] whatever off holds.
 __device__ __forceinline__ void net_rows(const NetRows &r, int64_t g, int64_t *lo, int64_t *hi)
@@ -172,6 +204,7 @@ __device__ __forceinline__ NetTile net_tile(const NetRows &r, int sh, int64_t t)
 {
     NetTile o;
     o.g = -1;
+    if (t >= net_tiles(r, sh)) return o;
     if (!r.off) {
         const uint32_t per = (uint32_t)((r.n + ((int64_t)1 << sh) - 1) >> sh);
         const uint32_t g = (uint32_t)t / per;

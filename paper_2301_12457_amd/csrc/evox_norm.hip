@@ -32,7 +32,7 @@ template <int V>
 struct Int {
     static constexpr int v = V;
 };
-template <typename F>
+template <typename T, typename F>
 hipError_t with_shape(const RowShape &s, F &&f)
 {
     if (s.L <= 64) {
@@ -42,7 +42,7 @@ hipError_t with_shape(const RowShape &s, F &&f)
     } else {
         if (s.nit <= 2) f(Int<2>{}, Int<1>{});
         else if (s.nit == 4) f(Int<4>{}, Int<1>{});
-        else f(Int<8>{}, Int<1>{});
+        else if constexpr (sizeof(T) == 4) f(Int<8>{}, Int<1>{});  // 16 bits: 4 x 1024 chunks hold EVOX_MAX_D
     }
     return hipGetLastError();
 }
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
     constexpr int N = NetVec<T>::N;
     __shared__ float lds[16];
     const int lane = threadIdx.x & (L - 1), D = (int)a.D;
-    const int64_t m = WIDE ? blockIdx.x : (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const int64_t m = WIDE ? net_block() : net_block() * (256 / L) + threadIdx.x / L;
     const bool live = m < a.rows.M;
     const T *x = (const T *)a.x + m * a.ldx;
     typename NetVec<T>::reg v[NIT];
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
         for (int i = 0; i < NIT; ++i)
             if ((lane + i * L) * N < D) v[i] = load_chunk(x, lane + i * L, D, (T)0.0f);
     const int g = live ? net_of_row(a.rows, m) : -1;
-    if (WIDE && g < 0) return;
+    if (WIDE && g < 0) return;  // the whole block
     float s = 0.0f;
     if (live)
 #pragma unroll
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a
     constexpr bool kHold = NIT * (8 + 2 * N) <= 96;
     extern __shared__ float sums[];  // [256 / L - 1 row slots][2][NIT][N][L] (narrow rows)
     __shared__ float2 lds[16];
-    const NetTile t = net_tile(a.rows, sh, blockIdx.x);
+    const NetTile t = net_tile(a.rows, sh, net_block());
     if (t.g < 0) return;
     const int lane = threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : 256 / L, D = (int)a.D;
     const T *ga = (const T *)a.gamma + t.g * a.p_stride;
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a
                     sb[i][j] += sums[(((r * 2 + 1) * NIT + i) * N + j) * L + lane];
                 }
     }
-    float *part = (float *)a.scratch + (int64_t)blockIdx.x * 2 * D;
+    float *part = (float *)a.scratch + net_block() * 2 * D;
 #pragma unroll
     for (int i = 0; i < NIT; ++i)
 #pragma unroll
@@ -330,14 +330,14 @@ __host__ __device__ __forceinline__ XentScratch xent_layout(const XentArgs &a, i
 __global__ __launch_bounds__(256) void k_xent_count(XentArgs a, int sh)
 {
     __shared__ int waves[4];
-    const NetTile t = net_tile(a.rows, kCountShift, blockIdx.x);
+    const NetTile t = net_tile(a.rows, kCountShift, net_block());
     if (t.g < 0) return;
     int n = 0;
     for (int64_t m = t.lo + threadIdx.x; m < t.hi; m += 256) n += xent_counts(a, xent_label(a, t.g, m));
     for (int o = 32; o > 0; o /= 2) n += __shfl_xor(n, o);
     if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = n;
     __syncthreads();
-    if (threadIdx.x == 0) xent_layout(a, sh).labels[blockIdx.x] = waves[0] + waves[1] + waves[2] + waves[3];
+    if (threadIdx.x == 0) xent_layout(a, sh).labels[net_block()] = waves[0] + waves[1] + waves[2] + waves[3];
 }
 
 // Tiles of 2^sh rows; whole: a tile is a whole network (rows may be more).
@@ -350,11 +350,12 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, i
     __shared__ int wave_count[16];
     NetTile t;
     if (whole) {
-        t.g = blockIdx.x;
+        if (net_block() >= a.rows.G) return;
+        t.g = (int)net_block();
         t.lo = t.g * a.rows.n;
         t.hi = t.lo + a.rows.n;
     } else {
-        t = net_tile(a.rows, sh, blockIdx.x);
+        t = net_tile(a.rows, sh, net_block());
         if (t.g < 0) return;
     }
     const int lane = threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : 256 / L, C = (int)a.C;
@@ -451,8 +452,8 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, i
         a.fit[t.g] = (float)(loss / (double)count);
     } else {
         const XentScratch s = xent_layout(a, sh);
-        s.loss[blockIdx.x] = loss;
-        s.count[blockIdx.x] = count;
+        s.loss[net_block()] = loss;
+        s.count[net_block()] = count;
     }
 }
 
@@ -498,11 +499,11 @@ int xent_tile_shift(const XentArgs &a)
 hipError_t launch_layernorm(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
-        using T = decltype(t);
+        using T = typename NetElement<t.value>::type;
         const RowShape r = row_shape(a.D, NetVec<T>::N);
         const int64_t per = r.L <= 64 ? 256 / r.L : 1;
-        return with_shape(r, [&](auto nit, auto wide) {
-            hipLaunchKernelGGL((k_layernorm<T, nit.v, wide.v>), dim3((unsigned)((a.rows.M + per - 1) / per)),
+        return with_shape<T>(r, [&](auto nit, auto wide) {
+            hipLaunchKernelGGL((k_layernorm<T, nit.v, wide.v>), net_grid((a.rows.M + per - 1) / per),
                                dim3(r.threads), 0, s, a, r.L);
         });
     });
@@ -516,15 +517,15 @@ size_t layernorm_grad_scratch(const NormArgs &a)
 hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
-        using T = decltype(t);
+        using T = typename NetElement<t.value>::type;
         const RowShape r = row_shape(a.D, NetVec<T>::N);
         const int sh = norm_tile_shift(a);
         const int64_t tiles = net_tiles(a.rows, sh);
         hipError_t e = hipSuccess;
         if (a.rows.M > 0)
-            e = with_shape(r, [&](auto nit, auto wide) {
+            e = with_shape<T>(r, [&](auto nit, auto wide) {
                 const size_t lds = wide.v ? 0 : sizeof(float) * 2 * nit.v * NetVec<T>::N * (256 - r.L);
-                hipLaunchKernelGGL((k_layernorm_grad<T, nit.v, wide.v>), dim3((unsigned)tiles), dim3(r.threads), lds, s,
+                hipLaunchKernelGGL((k_layernorm_grad<T, nit.v, wide.v>), net_grid(tiles), dim3(r.threads), lds, s,
                                    a, r.L, sh);
             });
         if (e != hipSuccess || !a.dgamma) return e;
@@ -543,17 +544,17 @@ size_t xent_scratch(const XentArgs &a)
 hipError_t launch_xent(const XentArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
-        using T = decltype(t);
+        using T = typename NetElement<t.value>::type;
         const RowShape r = row_shape(a.C, NetVec<T>::N);
         const bool whole = xent_whole(a);
         const int sh = xent_tile_shift(a);
         if (a.dz && !whole)
-            hipLaunchKernelGGL(k_xent_count, dim3((unsigned)net_tiles(a.rows, kCountShift)), dim3(256), 0, s, a, sh);
+            hipLaunchKernelGGL(k_xent_count, net_grid(net_tiles(a.rows, kCountShift)), dim3(256), 0, s, a, sh);
         hipError_t e = hipSuccess;
         if (a.rows.M > 0 || whole)
-            e = with_shape(r, [&](auto nit, auto wide) {
+            e = with_shape<T>(r, [&](auto nit, auto wide) {
                 hipLaunchKernelGGL((k_xent<T, nit.v, wide.v>),
-                                   dim3((unsigned)(whole ? a.rows.G : net_tiles(a.rows, sh))), dim3(r.threads), 0, s, a,
+                                   net_grid(whole ? a.rows.G : net_tiles(a.rows, sh)), dim3(r.threads), 0, s, a,
                                    r.L, sh, whole);
             });
         if (e != hipSuccess || whole) return e;

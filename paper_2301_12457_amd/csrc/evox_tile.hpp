@@ -1,0 +1,475 @@
+// Matrix products of the layers' large cases: tiles staged through LDS into the
+// bf16 / f16 matrix cores.
+//
+// A block computes D[j][i] = sum_k P[i][k] Q[j][k] for a BJ x BI tile of a
+// row-major result: i runs along the result's rows (its contiguous dimension),
+// so that a lane's four results of a 16 x 16 tile are neighbours.  Either
+// operand is k-contiguous (element (r, k) at r ld + k) or k-major (k ld + r),
+// and is staged as rows of K: a k-major operand is transposed in registers, 8 k
+// by 4 (fp32: 2) rows per thread, on its way to LDS.
+//
+// 16 bits: LDS rows of 64 k (128 bytes) in eight 16-byte chunks, chunk c of row
+// r at c ^ f(r), f(r) = (r ^ r / 4) mod 8: the eight lanes that an LDS access
+// serves at a time touch different chunks both when they read 8 consecutive rows
+// (matrix operands, k-contiguous writes) and when they write every fourth row
+// (k-major writes).
+//
+// 32 bits: an element is the exact sum of three bf16 numbers x = h + m + l (each
+// the rounding of what the ones before leave), staged as three planes; of the
+// nine products of pieces the six down to 2^-18 are summed, the rest are below
+// 2^-25 of the term.  Six bf16 products cost 6/16 of an fp32 one.  Sums cannot
+// overflow and no piece is infinite below 2^56; a block that meets a larger
+// number or an infinity computes its tile again with fp32 products
+// (v_mfma_f32_16x16x4f32).  A NaN is one in its own row either way.  A number
+// below 2^-100 loses its bits under 2^-126, as fp32 with flushed subnormals does.
+#pragma once
+
+#include "evox_net.hpp"
+
+namespace evox {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ f32x4 mma16(NetVec<bf16_t>::reg a, NetVec<bf16_t>::reg b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(NetVec<f16_t>::reg a, NetVec<f16_t>::reg b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(NetVec<float>::reg a, NetVec<float>::reg b, f32x4 c)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+
+constexpr float kTileBig = 0x1p56f;
+
+// The two numbers rounded to bf16, packed; the three pieces of a pair.
+__device__ __forceinline__ uint32_t net_pack_bf16(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
+}
+__device__ __forceinline__ void net_split2(float a, float b, uint32_t &h, uint32_t &m, uint32_t &l)
+{
+    h = net_pack_bf16(a, b);
+    const float a1 = a - __uint_as_float(h << 16), b1 = b - __uint_as_float(h & 0xffff0000u);
+    m = net_pack_bf16(a1, b1);
+    l = net_pack_bf16(a1 - __uint_as_float(m << 16), b1 - __uint_as_float(m & 0xffff0000u));
+}
+
+// K per staged tile and bytes of one staged operand of R rows.
+template <typename T>
+constexpr int kTileK = sizeof(T) == 4 ? 32 : 64;
+template <typename T, int R>
+constexpr int kStageBytes = sizeof(T) == 4 ? 3 * 64 * R : 128 * R;
+
+// LDS byte of chunk c (8 k) of row r.
+__device__ __forceinline__ int chunk16(int r, int c) { return r * 128 + ((c ^ ((r ^ (r >> 2)) & 7)) << 4); }
+__device__ __forceinline__ int chunk32(int r, int c)
+{
+    return (r >> 1) * 128 + (((r & 1) << 2 | (c ^ ((r >> 1) & 3))) << 4);
+}
+
+// One operand's next K tile in registers: TH threads, R rows of which n exist.
+// k-contiguous rows past n repeat row n - 1 and k-major ones are zero (neither
+// reaches a result); k past K is zero.
+template <typename T, bool MAJOR, int R, int TH>
+struct Stage;
+
+template <typename T, int R, int TH>
+struct Stage16c {
+    static constexpr int P = R * 8 / TH;
+    u32x4 v[P];
+    const T *row[P];
+    __device__ __forceinline__ void init(const T *src, int64_t ld, int n)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int r = threadIdx.x / 8 + p * (TH / 8);
+            row[p] = src + (int64_t)(r < n ? r : n - 1) * ld;
+        }
+    }
+    __device__ __forceinline__ void load(int64_t k0, int64_t K)
+    {
+        const int c = threadIdx.x % 8;
+        if (k0 + 64 <= K) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) v[p] = *reinterpret_cast<const u32x4u *>(row[p] + k0 + 8 * c);
+        } else {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                v[p] = __builtin_bit_cast(u32x4, load_chunk(row[p] + k0, c, (int)(K - k0), (T)0.0f));
+        }
+    }
+    __device__ __forceinline__ void store(char *lds, float &)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            *reinterpret_cast<u32x4 *>(lds + chunk16(threadIdx.x / 8 + p * (TH / 8), threadIdx.x % 8)) = v[p];
+    }
+};
+
+template <typename T, int R, int TH>
+struct Stage16m {
+    static constexpr int P = R * 2 / TH, kQuads = R / 4;
+    u32x2 v[P][8];
+    const T *src;
+    int64_t ld;
+    int n;
+    __device__ __forceinline__ void init(const T *s, int64_t l, int rows)
+    {
+        src = s;
+        ld = l;
+        n = rows;
+    }
+    __device__ __forceinline__ void load(int64_t k0, int64_t K)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int q = threadIdx.x + p * TH, r = q % kQuads * 4, k = q / kQuads * 8;
+            const T *at = src + (k0 + k) * ld + r;
+            if (k0 + k + 8 <= K && r + 4 <= n) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[p][j] = *reinterpret_cast<const u32x2u *>(at + j * ld);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    T e[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) e[x] = k0 + k + j < K && r + x < n ? at[j * ld + x] : (T)0.0f;
+                    v[p][j] = __builtin_bit_cast(u32x2, e);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char *lds, float &)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int q = threadIdx.x + p * TH, r = q % kQuads * 4, c = q / kQuads;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                u32x4 t;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    t[j] = __builtin_amdgcn_perm(v[p][2 * j + 1][x / 2], v[p][2 * j][x / 2],
+                                                 x % 2 ? 0x07060302u : 0x05040100u);
+                *reinterpret_cast<u32x4 *>(lds + chunk16(r + x, c)) = t;
+            }
+        }
+    }
+};
+
+// The pieces of 8 consecutive k of row r into their planes.
+template <int R>
+__device__ __forceinline__ void store_pieces(char *lds, int r, int c, const float *f, float &big)
+{
+    u32x4 h, m, l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        big = fmaxf(big, fmaxf(fabsf(f[2 * j]), fabsf(f[2 * j + 1])));
+        uint32_t a, b, d;
+        net_split2(f[2 * j], f[2 * j + 1], a, b, d);
+        h[j] = a;
+        m[j] = b;
+        l[j] = d;
+    }
+    char *at = lds + chunk32(r, c);
+    *reinterpret_cast<u32x4 *>(at) = h;
+    *reinterpret_cast<u32x4 *>(at + 64 * R) = m;
+    *reinterpret_cast<u32x4 *>(at + 128 * R) = l;
+}
+
+template <int R, int TH>
+struct Stage32c {
+    static constexpr int P = R * 4 / TH;
+    f32x4 v[P][2];
+    const float *row[P];
+    __device__ __forceinline__ void init(const float *src, int64_t ld, int n)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int r = threadIdx.x / 4 + p * (TH / 4);
+            row[p] = src + (int64_t)(r < n ? r : n - 1) * ld;
+        }
+    }
+    __device__ __forceinline__ void load(int64_t k0, int64_t K)
+    {
+        const int c = threadIdx.x % 4;
+        if (k0 + 32 <= K) {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    v[p][h] = *reinterpret_cast<const NetVec<float>::mem *>(row[p] + k0 + 8 * c + 4 * h);
+        } else {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) v[p][h] = load_chunk(row[p] + k0, 2 * c + h, (int)(K - k0), 0.0f);
+        }
+    }
+    __device__ __forceinline__ void store(char *lds, float &big)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = v[p][j / 4][j % 4];
+            store_pieces<R>(lds, threadIdx.x / 4 + p * (TH / 4), threadIdx.x % 4, f, big);
+        }
+    }
+};
+
+template <int R, int TH>
+struct Stage32m {
+    static constexpr int P = R * 2 / TH, kPairs = R / 2;
+    f32x2 v[P][8];
+    const float *src;
+    int64_t ld;
+    int n;
+    __device__ __forceinline__ void init(const float *s, int64_t l, int rows)
+    {
+        src = s;
+        ld = l;
+        n = rows;
+    }
+    __device__ __forceinline__ void load(int64_t k0, int64_t K)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int q = threadIdx.x + p * TH, r = q % kPairs * 2, k = q / kPairs * 8;
+            const float *at = src + (k0 + k) * ld + r;
+            if (k0 + k + 8 <= K && r + 2 <= n) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[p][j] = *reinterpret_cast<const f32x2u *>(at + j * ld);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) v[p][j][x] = k0 + k + j < K && r + x < n ? at[j * ld + x] : 0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char *lds, float &big)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int q = threadIdx.x + p * TH, r = q % kPairs * 2, c = q / kPairs;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float f[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = v[p][j][x];
+                store_pieces<R>(lds, r + x, c, f, big);
+            }
+        }
+    }
+};
+template <int R, int TH>
+struct Stage<float, false, R, TH> : Stage32c<R, TH> {};
+template <int R, int TH>
+struct Stage<float, true, R, TH> : Stage32m<R, TH> {};
+template <typename T, int R, int TH>
+struct Stage<T, false, R, TH> : Stage16c<T, R, TH> {};
+template <typename T, int R, int TH>
+struct Stage<T, true, R, TH> : Stage16m<T, R, TH> {};
+
+// An operand's tile: element (r, k) for r < n, k < K.
+template <typename T>
+struct TileOp {
+    const T *p;
+    int64_t ld;
+    int n;
+};
+
+// The tile's product and its results.  Waves: WI along i by WJ along j, each
+// TI x TJ tiles of 16 x 16.
+template <typename T, bool PM, bool QM, int BI, int BJ, int WI, int WJ>
+struct TileProduct {
+    static constexpr int kThreads = 64 * WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, BK = kTileK<T>;
+    static constexpr bool kSplit = sizeof(T) == 4;
+    static constexpr int kBuffers = kSplit ? 1 : 2;
+    static constexpr int kBuffer = kStageBytes<T, BI> + kStageBytes<T, BJ>;
+    static constexpr int kPitch = BI / WI + 4;  // floats per row of a wave's results in LDS, 16 rows at a time
+    static constexpr int kOutBytes = WI * WJ * 16 * kPitch * 4;
+    static constexpr int kLds = kBuffers * kBuffer > kOutBytes ? kBuffers * kBuffer : kOutBytes;
+
+    f32x4 acc[TI][TJ];
+    int wi, wj, l16, q;
+
+    __device__ __forceinline__ TileProduct()
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        wi = wave % WI;
+        wj = wave / WI;
+        l16 = threadIdx.x % 16;
+        q = threadIdx.x % 64 / 16;
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) acc[i][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    __device__ __forceinline__ void compute16(const char *lds)
+    {
+        typedef typename NetVec<T>::reg reg;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            reg p[TI], s[TJ];
+#pragma unroll
+            for (int i = 0; i < TI; ++i)
+                p[i] = *reinterpret_cast<const reg *>(lds + chunk16((wi * TI + i) * 16 + l16, 4 * h + q));
+#pragma unroll
+            for (int j = 0; j < TJ; ++j)
+                s[j] = *reinterpret_cast<const reg *>(lds + kStageBytes<T, BI> + chunk16((wj * TJ + j) * 16 + l16, 4 * h + q));
+#pragma unroll
+            for (int j = 0; j < TJ; ++j)
+#pragma unroll
+                for (int i = 0; i < TI; ++i) acc[i][j] = mma16(p[i], s[j], acc[i][j]);
+        }
+    }
+    __device__ __forceinline__ void compute32(const char *lds)
+    {
+        typedef NetVec<bf16_t>::reg reg;
+        reg p[TI][3], s[3];
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+                p[i][u] = *reinterpret_cast<const reg *>(lds + u * 64 * BI + chunk32((wi * TI + i) * 16 + l16, q));
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+                s[u] = *reinterpret_cast<const reg *>(lds + kStageBytes<T, BI> + u * 64 * BJ +
+                                                      chunk32((wj * TJ + j) * 16 + l16, q));
+            // the small products first
+#pragma unroll
+            for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+                for (int u = 0; u <= sum; ++u)
+#pragma unroll
+                    for (int i = 0; i < TI; ++i) acc[i][j] = mma16(p[i][u], s[sum - u], acc[i][j]);
+        }
+    }
+
+    // With fp32 products, straight from memory.
+    __device__ __forceinline__ void again(const TileOp<T> &P, const TileOp<T> &Q, int64_t K)
+    {
+        clear();
+        auto at = [&](const TileOp<T> &o, bool major, int r, int64_t k) -> float {
+            if (k >= K) return 0.0f;
+            r = r < o.n ? r : o.n - 1;
+            return (float)(major ? o.p[k * o.ld + r] : o.p[(int64_t)r * o.ld + k]);
+        };
+#pragma unroll 1
+        for (int64_t k = 0; k < K; k += 4) {
+            float p[TI], s[TJ];
+#pragma unroll
+            for (int i = 0; i < TI; ++i) p[i] = at(P, PM, (wi * TI + i) * 16 + l16, k + q);
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) s[j] = at(Q, QM, (wj * TJ + j) * 16 + l16, k + q);
+#pragma unroll
+            for (int j = 0; j < TJ; ++j)
+#pragma unroll
+                for (int i = 0; i < TI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[i], s[j], acc[i][j], 0, 0, 0);
+        }
+    }
+
+    // The whole product; ends with all waves past their last use of LDS.
+    __device__ __forceinline__ void run(const TileOp<T> &P, const TileOp<T> &Q, int64_t K, char *lds)
+    {
+        Stage<T, PM, BI, kThreads> sp;
+        Stage<T, QM, BJ, kThreads> sq;
+        clear();
+        if (K <= 0) return;
+        sp.init(P.p, P.ld, P.n);
+        sq.init(Q.p, Q.ld, Q.n);
+        float big = 0.0f;
+        const int64_t tiles = (K + BK - 1) / BK;
+        sp.load(0, K);
+        sq.load(0, K);
+        if constexpr (kSplit) {
+            for (int64_t t = 0; t < tiles; ++t) {
+                if (t) __syncthreads();
+                sp.store(lds, big);
+                sq.store(lds + kStageBytes<T, BI>, big);
+                __syncthreads();
+                if (t + 1 < tiles) {
+                    sp.load((t + 1) * BK, K);
+                    sq.load((t + 1) * BK, K);
+                }
+                compute32(lds);
+            }
+            if (__syncthreads_or(!(big < kTileBig))) again(P, Q, K);
+        } else {
+            sp.store(lds, big);
+            sq.store(lds + kStageBytes<T, BI>, big);
+            if (tiles > 1) {
+                sp.load(BK, K);
+                sq.load(BK, K);
+            }
+            __syncthreads();
+            for (int64_t t = 0; t < tiles; ++t) {
+                if (t + 1 < tiles) {
+                    char *next = lds + (t + 1) % 2 * kBuffer;
+                    sp.store(next, big);
+                    sq.store(next + kStageBytes<T, BI>, big);
+                    if (t + 2 < tiles) {
+                        sp.load((t + 2) * BK, K);
+                        sq.load((t + 2) * BK, K);
+                    }
+                }
+                compute16(lds + t % 2 * kBuffer);
+                __syncthreads();
+            }
+        }
+    }
+
+    // The results, 16 rows of every wave at a time through LDS (the wave's own
+    // part of it): out(j, i, v, n) gets n <= N neighbours i .. i + n - 1 of row j,
+    // N of them 16 bytes of the element type, a row's in consecutive lanes.
+    template <typename F>
+    __device__ __forceinline__ void results(int ni, int nj, char *lds, F &&out)
+    {
+        constexpr int N = NetVec<T>::N, kRow = BI / WI, kLanes = kRow / N, kRows = 64 / kLanes;
+        float *mine = reinterpret_cast<float *>(lds) + (wj * WI + wi) * 16 * kPitch;
+        const int lane = threadIdx.x % 64, c = lane % kLanes * N, i = wi * kRow + c;
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+#pragma unroll
+            for (int k = 0; k < TI; ++k) *reinterpret_cast<f32x4 *>(mine + l16 * kPitch + k * 16 + 4 * q) = acc[k][j];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+            for (int r = lane / kLanes; r < 16; r += kRows) {
+                const int row = (wj * TJ + j) * 16 + r;
+                if (row >= nj || i >= ni) continue;
+                float v[N];
+#pragma unroll
+                for (int e = 0; e < N; e += 4) {
+                    const f32x4 t = *reinterpret_cast<const f32x4 *>(mine + r * kPitch + c + e);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) v[e + x] = t[x];
+                }
+                out(row, i, v, ni - i < N ? ni - i : N);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+    }
+};
+
+}  // namespace evox
