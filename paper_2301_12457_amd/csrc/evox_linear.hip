@@ -58,8 +58,10 @@ __device__ __forceinline__ void linear_out(const LinearArgs &a, int g, int64_t m
             for (int j = 0; j < 4; ++j) t[j] = (T)v[j];
             *reinterpret_cast<quad *>(z) = t;
         }
+        float f[4] = {v[0], v[1], v[2], v[3]};
+        act_values<sizeof(T) == 2, 4>(a.act, f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = act_value(a.act, v[j]);
+        for (int j = 0; j < 4; ++j) v[j] = f[j];
         if (r) {
             t = *reinterpret_cast<const quad *>(r);
 #pragma unroll
@@ -75,7 +77,7 @@ __device__ __forceinline__ void linear_out(const LinearArgs &a, int g, int64_t m
         if (o + j >= n) continue;
         float s = v[j] + (b ? (float)b[j] : 0.0f);
         if (z) z[j] = (T)s;
-        s = act_value(a.act, s);
+        s = act_value<sizeof(T) == 2>(a.act, s);
         y[j] = (T)(s + (r ? (float)r[j] : 0.0f));
     }
 }
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(256) void k_linear_thin(LinearArgs a, int sh, uint3
 // product needs it), and the tiles' column sums of the unrounded d (where db is
 // wanted): a block takes 2^kDzShift rows of a network and 256 chunks of 16 bytes
 // of their columns, L lanes to a row, and adds its row slots in order.
-constexpr int kDzShift = 6;
+constexpr int kDzShift = 4;
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int L, T *d, int64_t ldd, float *sums)
@@ -208,12 +210,16 @@ __global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int L, T *d
                 continue;
             }
             const reg z = load_chunk((const T *)a.z + m * a.ldz, c, n, (T)0.0f);
+            float v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = (float)z[j];
+            act_slopes<sizeof(T) == 2, N>(a.act, v);
             reg out;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float v = (float)dy[j] * act_slope(a.act, (float)z[j]);
-                s[j] += v;
-                out[j] = (T)v;
+                v[j] *= (float)dy[j];
+                s[j] += v[j];
+                out[j] = (T)v[j];
             }
             if (d) store_chunk(d + m * ldd, c, n, out);
         }

@@ -34,30 +34,6 @@ __device__ __forceinline__ void unit_ij(int64_t u, int64_t ti, int64_t tj, int64
     *j = band * w + in % w;
 }
 
-__device__ __forceinline__ void act_values(int act, float *v)
-{
-    constexpr int N = NetVec<Elem>::N;
-    switch (act) {
-    case ACT_RELU:
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = act_value(ACT_RELU, v[e]);
-        break;
-    case ACT_TANH:
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = act_value(ACT_TANH, v[e]);
-        break;
-    case ACT_GELU:
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = act_value(ACT_GELU, v[e]);
-        break;
-    case ACT_SILU:
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = act_value(ACT_SILU, v[e]);
-        break;
-    default: break;
-    }
-}
-
 typedef NetVec<Elem>::reg Reg;
 typedef NetVec<Elem>::mem Mem;
 
@@ -118,7 +94,7 @@ __global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ) void k_li
         const int64_t m = t.lo + j;
         if (b) add_row(b + i, v, n);
         if (a.z) store_row((Elem *)a.z + m * a.ldz + i0 + i, v, n);
-        act_values(a.act, v);
+        act_values<sizeof(Elem) == 2, NetVec<Elem>::N>(a.act, v);
         if (a.r) add_row((const Elem *)a.r + m * a.ldr + i0 + i, v, n);
         store_row((Elem *)a.y + m * a.ldy + i0 + i, v, n);
     });

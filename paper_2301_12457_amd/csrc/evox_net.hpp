@@ -236,33 +236,114 @@ __device__ __forceinline__ NetTile net_tile(const NetRows &r, int sh, int64_t t)
     return o;
 }
 
+// Activations and their slopes.  For results of 16 bits the hardware's exp2
+// and reciprocal (1 ulp) stand in for expf and the division, and the normal
+// distribution's upper tail is Q(x) = e^(-x^2/2) t (a1 + .. + a5 t^4) / 2, t = 1 /
+// (1 + p x / sqrt 2) (Abramowitz and Stegun 7.1.26: 7.5e-8 off at most, and a
+// tail without cancellation); tanh below 0.15 is its series.  A GELU is then 14
+// multiply-adds and two transcendental instructions instead of about 60
+// instructions of erff, 268M of which cost more than a quarter of the layer that
+// they follow (16x2048 rows 4096x4096).
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+// Q(|z|) and e^(-z^2/2).
+__device__ __forceinline__ float normal_tail(float z, float *e)
+{
+    *e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.0f));
+    float p = fmaf(t, 1.061405429f, -1.453152027f);
+    p = fmaf(t, p, 1.421413741f);
+    p = fmaf(t, p, -0.284496736f);
+    p = fmaf(t, p, 0.254829592f);
+    return 0.5f * p * t * *e;
+}
+
+template <bool FAST>
 __device__ __forceinline__ float act_value(int act, float z)
 {
     switch (act) {
     case ACT_RELU: return z < 0.0f ? 0.0f : z;  // NaN passes
-    case ACT_TANH: return tanhf(z);
-    case ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-    case ACT_SILU: return z / (1.0f + expf(-z));
+    case ACT_TANH: {
+        if constexpr (!FAST) return tanhf(z);
+        const float s = z * z, t = exp_fast(-2.0f * fabsf(z)), r = (1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t);
+        const float near = z * fmaf(s, fmaf(s, fmaf(s, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+        return s < 0.0225f ? near : copysignf(r, z);
+    }
+    case ACT_GELU: {
+        if constexpr (!FAST) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+        float e;
+        const float q = normal_tail(z, &e);  // NaN where z is
+        return fmaf(-fminf(fabsf(z), 30.0f), q, fmaxf(z, 0.0f));
+    }
+    case ACT_SILU:
+        if constexpr (!FAST) return z / (1.0f + expf(-z));
+        return fmaxf(z, -126.0f) * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
     default: return z;
     }
 }
 
+template <bool FAST>
 __device__ __forceinline__ float act_slope(int act, float z)
 {
+    const float zc = fminf(fmaxf(z, -126.0f), 126.0f);  // infinities have slope 0 or 1
     switch (act) {
     case ACT_RELU: return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
     case ACT_TANH: {
+        if constexpr (FAST) {
+            const float t = exp_fast(-2.0f * fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + t);
+            return 4.0f * t * r * r;
+        }
         const float t = tanhf(z);
         return (1.0f - t) * (1.0f + t);
     }
-    case ACT_GELU:
-        return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+    case ACT_GELU: {
+        if constexpr (FAST) {
+            float e;
+            const float q = normal_tail(z, &e);
+            return fmaf(zc * 0.39894228f, e, z < 0.0f ? q : 1.0f - q);
+        }
+        return 0.5f * (1.0f + erff(z * 0.70710678f)) + zc * 0.39894228f * expf(-0.5f * z * z);
+    }
     case ACT_SILU: {
-        const float s = 1.0f / (1.0f + expf(-z));
-        return s * (1.0f + z * (1.0f - s));
+        const float s = FAST ? __builtin_amdgcn_rcpf(1.0f + exp_fast(-z)) : 1.0f / (1.0f + expf(-z));
+        return s * (1.0f + zc * (1.0f - s));
     }
     default: return 1.0f;
     }
+}
+
+// N neighbours at a time: one branch for all of them.
+template <bool FAST, int N>
+__device__ __forceinline__ void act_values(int act, float *v)
+{
+#define EVOX_ACT_ALL(A)                                             \
+    case A:                                                         \
+        _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] = act_value<FAST>(A, v[e]); \
+        break;
+    switch (act) {
+        EVOX_ACT_ALL(ACT_RELU)
+        EVOX_ACT_ALL(ACT_TANH)
+        EVOX_ACT_ALL(ACT_GELU)
+        EVOX_ACT_ALL(ACT_SILU)
+    default: break;
+    }
+#undef EVOX_ACT_ALL
+}
+template <bool FAST, int N>
+__device__ __forceinline__ void act_slopes(int act, float *z)
+{
+#define EVOX_ACT_ALL(A)                                             \
+    case A:                                                         \
+        _Pragma("unroll") for (int e = 0; e < N; ++e) z[e] = act_slope<FAST>(A, z[e]); \
+        break;
+    switch (act) {
+        EVOX_ACT_ALL(ACT_NONE)
+        EVOX_ACT_ALL(ACT_RELU)
+        EVOX_ACT_ALL(ACT_TANH)
+        EVOX_ACT_ALL(ACT_GELU)
+        EVOX_ACT_ALL(ACT_SILU)
+    }
+#undef EVOX_ACT_ALL
 }
 
 }  // namespace evox

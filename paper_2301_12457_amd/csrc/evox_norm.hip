@@ -312,6 +312,21 @@ __device__ __forceinline__ int xent_label(const XentArgs &a, int64_t g, int64_t 
 }
 __device__ __forceinline__ bool xent_counts(const XentArgs &a, int label) { return label >= 0 && label < a.C; }
 
+// e^(v - top) for v <= top, by the hardware's exp2 (1 ulp).  Of fp32 logits the
+// rounding of (v - top) log2 e is put back (e^x = 2^h (1 + l ln 2), h + l the
+// whole product); of 16-bit logits it stays: far below the probability's own
+// rounding.  v - top comes first (its parts may be the type's lowest value).  Of
+// -inf 0, of NaN NaN.
+template <typename T>
+__device__ __forceinline__ float exp_below(float v, float top)
+{
+    const float x = v - top, c = fmaxf(x, -200.0f);
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(x * 1.44269502f);
+    const float l = fmaf(c, 1.92596299e-8f, fmaf(c, 1.44269502f, -(c * 1.44269502f)));
+    const float e = __builtin_amdgcn_exp2f(x * 1.44269502f);
+    return fmaf(e, l * 0.69314718f, e);
+}
+
 struct XentScratch {
     double *loss;    // [tiles]
     int32_t *count;  // [tiles] rows that count
@@ -407,7 +422,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, i
 #pragma unroll
                     for (int j = 0; j < N; ++j) {
                         // past the row's end v is -inf: nothing, but in a row of -inf alone, all NaN anyway
-                        e[i][j] = expf((float)v[i][j] - top);
+                        e[i][j] = exp_below<T>((float)v[i][j], top);
                         sum += e[i][j];
                     }
         sum = row_all<WIDE, false>(sum, L, lds);
@@ -417,6 +432,12 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, i
         }
         if (a.dz && live) {
             T *dz = (T *)a.dz + m * a.lddz;
+            if (!counts) {
+#pragma unroll
+                for (int i = 0; i < NIT; ++i)
+                    if ((lane + i * L) * N < C) store_chunk(dz, lane + i * L, C, (typename NetVec<T>::reg){});
+                continue;
+            }
             const float f = scale / sum;
 #pragma unroll
             for (int i = 0; i < NIT; ++i) {
@@ -424,10 +445,11 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, i
                 if (c * N >= C) continue;
                 typename NetVec<T>::reg out;
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float p = e[i][j] * f;
-                    out[j] = counts ? (T)(c * N + j == label ? fmaf(e[i][j] / sum, scale, -scale) : p) : (T)0.0f;
-                }
+                for (int j = 0; j < N; ++j) out[j] = (T)(e[i][j] * f);
+                if (c == label / N)  // the label's chunk: (p - 1) scale, rounded once
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (j == label % N) out[j] = (T)fmaf(e[i][j], f, -scale);
                 store_chunk(dz, c, C, out);
             }
         }
