@@ -73,7 +73,7 @@ using Product = TileProduct<Elem, PM, QM, B, B, TileShape<B>::WI, TileShape<B>::
 
 // y = act(x W^T + b) + r: i = output, j = row, k = input.
 template <int B>
-__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ) void k_linear_tile(LinearArgs a, int64_t ti,
+__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ, 2) void k_linear_tile(LinearArgs a, int64_t ti,
                                                                                      int64_t tj, int64_t units)
 {
     __shared__ __attribute__((aligned(16))) char lds[Product<B, false, false>::kLds];
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ) void k_li
 
 // dx = d W: i = input, j = row, k = output.
 template <int B>
-__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ) void k_linear_dx_tile(LinearGradArgs a, const Elem *d,
+__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ, 2) void k_linear_dx_tile(LinearGradArgs a, const Elem *d,
                                                                                       int64_t ldd, int64_t ti,
                                                                                       int64_t tj, int64_t units)
 {
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ) void k_li
 
 // dW = d^T x: i = input, j = output, k = row of the network.
 template <int B>
-__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ) void k_linear_dw_tile(LinearGradArgs a, const Elem *d,
+__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ, 2) void k_linear_dw_tile(LinearGradArgs a, const Elem *d,
                                                                                      int64_t ldd, int64_t ti, int64_t tj,
                                                                                      int64_t units)
 {

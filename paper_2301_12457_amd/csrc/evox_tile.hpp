@@ -67,6 +67,10 @@ __device__ __forceinline__ void net_split2(float a, float b, uint32_t &h, uint32
     l = net_pack_bf16(a1 - __uint_as_float(m << 16), b1 - __uint_as_float(m & 0xffff0000u));
 }
 
+// A barrier for LDS alone: __syncthreads() also waits for the global loads in
+// flight, which here are the next tiles' operands.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // K per staged tile and bytes of one staged operand of R rows.
 template <typename T>
 constexpr int kTileK = sizeof(T) == 4 ? 32 : 64;
@@ -88,7 +92,7 @@ struct Stage;
 
 template <typename T, int R, int TH>
 struct Stage16c {
-    static constexpr int P = R * 8 / TH;
+    static constexpr int P = R * 8 / TH, kLoads = P, kStores = P;
     u32x4 v[P];
     const T *row[P];
     __device__ __forceinline__ void init(const T *src, int64_t ld, int n)
@@ -99,29 +103,31 @@ struct Stage16c {
             row[p] = src + (int64_t)(r < n ? r : n - 1) * ld;
         }
     }
+    __device__ __forceinline__ bool whole() const { return true; }
+    __device__ __forceinline__ void load_piece(int p, int64_t k0)  // k0 + 64 <= K
+    {
+        v[p] = *reinterpret_cast<const u32x4u *>(row[p] + k0 + 8 * (threadIdx.x % 8));
+    }
     __device__ __forceinline__ void load(int64_t k0, int64_t K)
     {
-        const int c = threadIdx.x % 8;
         if (k0 + 64 <= K) {
 #pragma unroll
-            for (int p = 0; p < P; ++p) v[p] = *reinterpret_cast<const u32x4u *>(row[p] + k0 + 8 * c);
-        } else {
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-                v[p] = __builtin_bit_cast(u32x4, load_chunk(row[p] + k0, c, (int)(K - k0), (T)0.0f));
+            for (int p = 0; p < P; ++p) load_piece(p, k0);
+            return;
         }
-    }
-    __device__ __forceinline__ void store(char *lds, float &)
-    {
 #pragma unroll
         for (int p = 0; p < P; ++p)
-            *reinterpret_cast<u32x4 *>(lds + chunk16(threadIdx.x / 8 + p * (TH / 8), threadIdx.x % 8)) = v[p];
+            v[p] = __builtin_bit_cast(u32x4, load_chunk(row[p] + k0, threadIdx.x % 8, (int)(K - k0), (T)0.0f));
+    }
+    __device__ __forceinline__ void store_piece(int p, char *lds)
+    {
+        *reinterpret_cast<u32x4 *>(lds + chunk16(threadIdx.x / 8 + p * (TH / 8), threadIdx.x % 8)) = v[p];
     }
 };
 
 template <typename T, int R, int TH>
 struct Stage16m {
-    static constexpr int P = R * 2 / TH, kQuads = R / 4;
+    static constexpr int P = R * 2 / TH, kQuads = R / 4, kLoads = 8 * P, kStores = 4 * P;
     u32x2 v[P][8];
     const T *src;
     int64_t ld;
@@ -131,6 +137,12 @@ struct Stage16m {
         src = s;
         ld = l;
         n = rows;
+    }
+    __device__ __forceinline__ bool whole() const { return n == R; }
+    __device__ __forceinline__ void load_piece(int i, int64_t k0)  // and all R rows exist
+    {
+        const int p = i / 8, j = i % 8, q = threadIdx.x + p * TH;
+        v[p][j] = *reinterpret_cast<const u32x2u *>(src + (k0 + q / kQuads * 8 + j) * ld + q % kQuads * 4);
     }
     __device__ __forceinline__ void load(int64_t k0, int64_t K)
     {
@@ -152,21 +164,14 @@ struct Stage16m {
             }
         }
     }
-    __device__ __forceinline__ void store(char *lds, float &)
+    __device__ __forceinline__ void store_piece(int i, char *lds)
     {
+        const int p = i / 4, x = i % 4, q = threadIdx.x + p * TH, r = q % kQuads * 4, c = q / kQuads;
+        u32x4 t;
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int q = threadIdx.x + p * TH, r = q % kQuads * 4, c = q / kQuads;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                u32x4 t;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    t[j] = __builtin_amdgcn_perm(v[p][2 * j + 1][x / 2], v[p][2 * j][x / 2],
-                                                 x % 2 ? 0x07060302u : 0x05040100u);
-                *reinterpret_cast<u32x4 *>(lds + chunk16(r + x, c)) = t;
-            }
-        }
+        for (int j = 0; j < 4; ++j)
+            t[j] = __builtin_amdgcn_perm(v[p][2 * j + 1][x / 2], v[p][2 * j][x / 2], x % 2 ? 0x07060302u : 0x05040100u);
+        *reinterpret_cast<u32x4 *>(lds + chunk16(r + x, c)) = t;
     }
 };
 
@@ -324,22 +329,52 @@ struct TileProduct {
             for (int j = 0; j < TJ; ++j) acc[i][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    __device__ __forceinline__ void compute16(const char *lds)
+    // One K tile (64 k) of 16-bit products in 2 TJ slots of TI products: slot k
+    // reads the operand of slot k + 2, and with kNext writes a share of the next
+    // tile to LDS (first half of the slots) or loads a share of the one after
+    // (second half).  The order is held by the scheduling barriers: left to itself
+    // the compiler reads one operand and waits for it before every TI products,
+    // and writes and loads in a burst.
+    template <bool kNext, typename SP, typename SQ>
+    __device__ __forceinline__ void compute16(const char *lds, char *next, SP &sp, SQ &sq, int64_t k0)
     {
         typedef typename NetVec<T>::reg reg;
+        constexpr int kSlots = 2 * TJ, kW = SP::kStores + SQ::kStores, kV = SP::kLoads + SQ::kLoads;
+        reg p[2][TI], s[3];
+        auto read_p = [&](int h, int i) {
+            p[h][i] = *reinterpret_cast<const reg *>(lds + chunk16((wi * TI + i) * 16 + l16, 4 * h + q));
+        };
+        auto read_s = [&](int k) {
+            s[k % 3] = *reinterpret_cast<const reg *>(lds + kStageBytes<T, BI> +
+                                                      chunk16((wj * TJ + k % TJ) * 16 + l16, 4 * (k / TJ) + q));
+        };
+        read_s(0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            reg p[TI], s[TJ];
+        for (int i = 0; i < TI; ++i) read_p(0, i);
+        read_s(1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < TI; ++i)
-                p[i] = *reinterpret_cast<const reg *>(lds + chunk16((wi * TI + i) * 16 + l16, 4 * h + q));
+        for (int k = 0; k < kSlots; ++k) {
+            if (k + 2 < kSlots) read_s(k + 2);
+            if (k < TJ)
 #pragma unroll
-            for (int j = 0; j < TJ; ++j)
-                s[j] = *reinterpret_cast<const reg *>(lds + kStageBytes<T, BI> + chunk16((wj * TJ + j) * 16 + l16, 4 * h + q));
+                for (int i = TI * k / TJ; i < TI * (k + 1) / TJ; ++i) read_p(1, i);
+            if constexpr (kNext) {
+                if (k < TJ) {
 #pragma unroll
-            for (int j = 0; j < TJ; ++j)
+                    for (int w = kW * k / TJ; w < kW * (k + 1) / TJ; ++w)
+                        if (w < SP::kStores) sp.store_piece(w, next);
+                        else sq.store_piece(w - SP::kStores, next + kStageBytes<T, BI>);
+                } else {
 #pragma unroll
-                for (int i = 0; i < TI; ++i) acc[i][j] = mma16(p[i], s[j], acc[i][j]);
+                    for (int v = kV * (k - TJ) / TJ; v < kV * (k - TJ + 1) / TJ; ++v)
+                        if (v < SP::kLoads) sp.load_piece(v, k0);
+                        else sq.load_piece(v - SP::kLoads, k0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < TI; ++i) acc[i][k % TJ] = mma16(p[k / TJ][i], s[k % 3], acc[i][k % TJ]);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     __device__ __forceinline__ void compute32(const char *lds)
@@ -390,6 +425,15 @@ struct TileProduct {
         }
     }
 
+    template <typename SP, typename SQ>
+    __device__ __forceinline__ void store_all(char *lds, SP &sp, SQ &sq)
+    {
+#pragma unroll
+        for (int w = 0; w < SP::kStores; ++w) sp.store_piece(w, lds);
+#pragma unroll
+        for (int w = 0; w < SQ::kStores; ++w) sq.store_piece(w, lds + kStageBytes<T, BI>);
+    }
+
     // The whole product; ends with all waves past their last use of LDS.
     __device__ __forceinline__ void run(const TileOp<T> &P, const TileOp<T> &Q, int64_t K, char *lds)
     {
@@ -405,10 +449,10 @@ struct TileProduct {
         sq.load(0, K);
         if constexpr (kSplit) {
             for (int64_t t = 0; t < tiles; ++t) {
-                if (t) __syncthreads();
+                if (t) lds_barrier();
                 sp.store(lds, big);
                 sq.store(lds + kStageBytes<T, BI>, big);
-                __syncthreads();
+                lds_barrier();
                 if (t + 1 < tiles) {
                     sp.load((t + 1) * BK, K);
                     sq.load((t + 1) * BK, K);
@@ -417,25 +461,29 @@ struct TileProduct {
             }
             if (__syncthreads_or(!(big < kTileBig))) again(P, Q, K);
         } else {
-            sp.store(lds, big);
-            sq.store(lds + kStageBytes<T, BI>, big);
+            store_all(lds, sp, sq);
             if (tiles > 1) {
                 sp.load(BK, K);
                 sq.load(BK, K);
             }
-            __syncthreads();
-            for (int64_t t = 0; t < tiles; ++t) {
+            lds_barrier();
+            int64_t t = 0;
+            // while the tile two ahead is whole
+            if (sp.whole() && sq.whole())
+                for (const int64_t full = K / BK; t + 2 < full; ++t) {
+                    compute16<true>(lds + t % 2 * kBuffer, lds + (t + 1) % 2 * kBuffer, sp, sq, (t + 2) * BK);
+                    lds_barrier();
+                }
+            for (; t < tiles; ++t) {
                 if (t + 1 < tiles) {
-                    char *next = lds + (t + 1) % 2 * kBuffer;
-                    sp.store(next, big);
-                    sq.store(next + kStageBytes<T, BI>, big);
+                    store_all(lds + (t + 1) % 2 * kBuffer, sp, sq);
                     if (t + 2 < tiles) {
                         sp.load((t + 2) * BK, K);
                         sq.load((t + 2) * BK, K);
                     }
                 }
-                compute16(lds + t % 2 * kBuffer);
-                __syncthreads();
+                compute16<false>(lds + t % 2 * kBuffer, nullptr, sp, sq, 0);
+                lds_barrier();
             }
         }
     }
