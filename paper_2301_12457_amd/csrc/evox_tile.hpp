@@ -52,6 +52,19 @@ __device__ __forceinline__ f32x4 mma16(NetVec<float>::reg a, NetVec<float>::reg 
     return c;
 }
 
+// One 32 x 32 tile over 16 k: lane l brings k = 8 (l / 32) .. + 8 of row l % 32 of
+// either operand and receives rows 8 b + 4 (l / 32) .. + 4 (b = 0 .. 3) of A
+// against row l % 32 of B.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ f32x16 mma32(NetVec<bf16_t>::reg a, NetVec<bf16_t>::reg b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma32(NetVec<f16_t>::reg a, NetVec<f16_t>::reg b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
 constexpr float kTileBig = 0x1p56f;
 
 // The two numbers rounded to bf16, packed; the three pieces of a pair.
@@ -299,37 +312,41 @@ struct TileOp {
 };
 
 // The tile's product and its results.  Waves: WI along i by WJ along j, each
-// TI x TJ tiles of 16 x 16.
+// TI x TJ tiles of S x S (16 bits: 32, which read each operand register half as
+// often as tiles of 16 would, and leave more registers: the gradient of 64x512
+// 1024x1024 312 -> 288 us).
 template <typename T, bool PM, bool QM, int BI, int BJ, int WI, int WJ>
 struct TileProduct {
-    static constexpr int kThreads = 64 * WI * WJ, TI = BI / WI / 16, TJ = BJ / WJ / 16, BK = kTileK<T>;
+    static constexpr int kThreads = 64 * WI * WJ, BK = kTileK<T>;
     static constexpr bool kSplit = sizeof(T) == 4;
+    static constexpr int S = kSplit ? 16 : 32, TI = BI / WI / S, TJ = BJ / WJ / S;
+    typedef typename std::conditional<kSplit, f32x4, f32x16>::type Acc;
     static constexpr int kBuffers = kSplit ? 1 : 2;
     static constexpr int kBuffer = kStageBytes<T, BI> + kStageBytes<T, BJ>;
-    static constexpr int kPitch = BI / WI + 4;  // floats per row of a wave's results in LDS, 16 rows at a time
-    static constexpr int kOutBytes = WI * WJ * 16 * kPitch * 4;
+    static constexpr int kPitch = BI / WI + 4;  // floats per row of a wave's results in LDS, S rows at a time
+    static constexpr int kOutBytes = WI * WJ * S * kPitch * 4;
     static constexpr int kLds = kBuffers * kBuffer > kOutBytes ? kBuffers * kBuffer : kOutBytes;
 
-    f32x4 acc[TI][TJ];
-    int wi, wj, l16, q;
+    Acc acc[TI][TJ];
+    int wi, wj, row, q;  // the lane's row of a tile and k group
 
     __device__ __forceinline__ TileProduct()
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         wi = wave % WI;
         wj = wave / WI;
-        l16 = threadIdx.x % 16;
-        q = threadIdx.x % 64 / 16;
+        row = threadIdx.x % S;
+        q = threadIdx.x % 64 / S;
     }
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int i = 0; i < TI; ++i)
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) acc[i][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+            for (int j = 0; j < TJ; ++j) acc[i][j] = (Acc)(0.0f);
     }
 
-    // One K tile (64 k) of 16-bit products in 2 TJ slots of TI products: slot k
+    // One K tile (64 k) of 16-bit products in 4 TJ slots of TI products: slot k
     // reads the operand of slot k + 2, and with kNext writes a share of the next
     // tile to LDS (first half of the slots) or loads a share of the one after
     // (second half).  The order is held by the scheduling barriers: left to itself
@@ -339,14 +356,14 @@ struct TileProduct {
     __device__ __forceinline__ void compute16(const char *lds, char *next, SP &sp, SQ &sq, int64_t k0)
     {
         typedef typename NetVec<T>::reg reg;
-        constexpr int kSlots = 2 * TJ, kW = SP::kStores + SQ::kStores, kV = SP::kLoads + SQ::kLoads;
+        constexpr int kSlots = 4 * TJ, kHalf = 2 * TJ, kW = SP::kStores + SQ::kStores, kV = SP::kLoads + SQ::kLoads;
         reg p[2][TI], s[3];
         auto read_p = [&](int h, int i) {
-            p[h][i] = *reinterpret_cast<const reg *>(lds + chunk16((wi * TI + i) * 16 + l16, 4 * h + q));
+            p[h % 2][i] = *reinterpret_cast<const reg *>(lds + chunk16((wi * TI + i) * 32 + row, 2 * h + q));
         };
         auto read_s = [&](int k) {
             s[k % 3] = *reinterpret_cast<const reg *>(lds + kStageBytes<T, BI> +
-                                                      chunk16((wj * TJ + k % TJ) * 16 + l16, 4 * (k / TJ) + q));
+                                                      chunk16((wj * TJ + k % TJ) * 32 + row, 2 * (k / TJ) + q));
         };
         read_s(0);
 #pragma unroll
@@ -356,24 +373,24 @@ struct TileProduct {
 #pragma unroll
         for (int k = 0; k < kSlots; ++k) {
             if (k + 2 < kSlots) read_s(k + 2);
-            if (k < TJ)
+            if (k < 3 * TJ)
 #pragma unroll
-                for (int i = TI * k / TJ; i < TI * (k + 1) / TJ; ++i) read_p(1, i);
+                for (int i = TI * (k % TJ) / TJ; i < TI * (k % TJ + 1) / TJ; ++i) read_p(k / TJ + 1, i);
             if constexpr (kNext) {
-                if (k < TJ) {
+                if (k < kHalf) {
 #pragma unroll
-                    for (int w = kW * k / TJ; w < kW * (k + 1) / TJ; ++w)
+                    for (int w = kW * k / kHalf; w < kW * (k + 1) / kHalf; ++w)
                         if (w < SP::kStores) sp.store_piece(w, next);
                         else sq.store_piece(w - SP::kStores, next + kStageBytes<T, BI>);
                 } else {
 #pragma unroll
-                    for (int v = kV * (k - TJ) / TJ; v < kV * (k - TJ + 1) / TJ; ++v)
+                    for (int v = kV * (k - kHalf) / kHalf; v < kV * (k - kHalf + 1) / kHalf; ++v)
                         if (v < SP::kLoads) sp.load_piece(v, k0);
                         else sq.load_piece(v - SP::kLoads, k0);
                 }
             }
 #pragma unroll
-            for (int i = 0; i < TI; ++i) acc[i][k % TJ] = mma16(p[k / TJ][i], s[k % 3], acc[i][k % TJ]);
+            for (int i = 0; i < TI; ++i) acc[i][k % TJ] = mma32(p[k / TJ % 2][i], s[k % 3], acc[i][k % TJ]);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -385,13 +402,13 @@ struct TileProduct {
         for (int i = 0; i < TI; ++i)
 #pragma unroll
             for (int u = 0; u < 3; ++u)
-                p[i][u] = *reinterpret_cast<const reg *>(lds + u * 64 * BI + chunk32((wi * TI + i) * 16 + l16, q));
+                p[i][u] = *reinterpret_cast<const reg *>(lds + u * 64 * BI + chunk32((wi * TI + i) * 16 + row, q));
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
 #pragma unroll
             for (int u = 0; u < 3; ++u)
                 s[u] = *reinterpret_cast<const reg *>(lds + kStageBytes<T, BI> + u * 64 * BJ +
-                                                      chunk32((wj * TJ + j) * 16 + l16, q));
+                                                      chunk32((wj * TJ + j) * 16 + row, q));
             // the small products first
 #pragma unroll
             for (int sum = 2; sum >= 0; --sum)
@@ -415,9 +432,9 @@ struct TileProduct {
         for (int64_t k = 0; k < K; k += 4) {
             float p[TI], s[TJ];
 #pragma unroll
-            for (int i = 0; i < TI; ++i) p[i] = at(P, PM, (wi * TI + i) * 16 + l16, k + q);
+            for (int i = 0; i < TI; ++i) p[i] = at(P, PM, (wi * TI + i) * 16 + row, k + q);
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) s[j] = at(Q, QM, (wj * TJ + j) * 16 + l16, k + q);
+            for (int j = 0; j < TJ; ++j) s[j] = at(Q, QM, (wj * TJ + j) * 16 + row, k + q);
 #pragma unroll
             for (int j = 0; j < TJ; ++j)
 #pragma unroll
@@ -488,24 +505,31 @@ struct TileProduct {
         }
     }
 
-    // The results, 16 rows of every wave at a time through LDS (the wave's own
+    // The results, S rows of every wave at a time through LDS (the wave's own
     // part of it): out(j, i, v, n) gets n <= N neighbours i .. i + n - 1 of row j,
     // N of them 16 bytes of the element type, a row's in consecutive lanes.
     template <typename F>
     __device__ __forceinline__ void results(int ni, int nj, char *lds, F &&out)
     {
         constexpr int N = NetVec<T>::N, kRow = BI / WI, kLanes = kRow / N, kRows = 64 / kLanes;
-        float *mine = reinterpret_cast<float *>(lds) + (wj * WI + wi) * 16 * kPitch;
+        float *mine = reinterpret_cast<float *>(lds) + (wj * WI + wi) * S * kPitch;
         const int lane = threadIdx.x % 64, c = lane % kLanes * N, i = wi * kRow + c;
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
 #pragma unroll
-            for (int k = 0; k < TI; ++k) *reinterpret_cast<f32x4 *>(mine + l16 * kPitch + k * 16 + 4 * q) = acc[k][j];
+            for (int k = 0; k < TI; ++k)
+#pragma unroll
+                for (int b = 0; b < S * S / 256; ++b) {  // the lane's quads of the tile
+                    f32x4 t;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[e] = acc[k][j][4 * b + e];
+                    *reinterpret_cast<f32x4 *>(mine + row * kPitch + k * S + 8 * b + 4 * q) = t;
+                }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
-            for (int r = lane / kLanes; r < 16; r += kRows) {
-                const int row = (wj * TJ + j) * 16 + r;
-                if (row >= nj || i >= ni) continue;
+            for (int r = lane / kLanes; r < S; r += kRows) {
+                const int rj = (wj * TJ + j) * S + r;
+                if (rj >= nj || i >= ni) continue;
                 float v[N];
 #pragma unroll
                 for (int e = 0; e < N; e += 4) {
@@ -513,7 +537,7 @@ struct TileProduct {
 #pragma unroll
                     for (int x = 0; x < 4; ++x) v[e + x] = t[x];
                 }
-                out(row, i, v, ni - i < N ? ni - i : N);
+                out(rj, i, v, ni - i < N ? ni - i : N);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
