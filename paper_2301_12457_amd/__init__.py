@@ -246,43 +246,73 @@ def evox_sgemm(A, B, C, trans_a=False, trans_b=False, alpha=1.0, beta=0.0, strea
 # ---------------------------------------------------------------------------
 # Populations of networks.  Weights and vectors are views of the parameter
 # rows ([G, n_out, n_in] and [G, n] tensors whose last dimension is dense);
-# activations are [M, n] tensors with dense rows.
+# activations are [M, n] tensors with dense rows.  A control step is one row per
+# network and a few microseconds of GPU time, so the checks are one comparison per
+# tensor and name what is wrong only once something is.
 # ---------------------------------------------------------------------------
+_DTYPES = {}
+
+
 def _dtype(t):
-    name = str(t.dtype)
-    if name not in ("torch.float32", "torch.bfloat16", "torch.float16"):
-        raise EvoxError(EINVAL, f"element type {name}: float32, bfloat16 or float16")
-    return (F32, BF16, F16)[("torch.float32", "torch.bfloat16", "torch.float16").index(name)]
+    """The element type's id."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise EvoxError(EINVAL, f"element type {t.dtype}: float32, bfloat16 or float16")
+    return d
 
 
-def _view(what, t, like, *shape):
-    """A tensor (or None) of this shape, of like's type and device, with dense rows."""
+def _view(what, t, like, shape):
+    """Checks a tensor (or None): this shape, like's type and device, dense rows.  Its address."""
     if t is None:
-        return
+        return None
+    if (t.dtype is like.dtype and t.shape == shape and (t.stride(-1) == 1 or shape[-1] == 1)
+            and t.get_device() == like.get_device()):
+        return t.data_ptr()
     if t.dtype != like.dtype or t.device != like.device:
         raise EvoxError(EINVAL, f"{what}: {t.dtype} on {t.device}, needs {like.dtype} on {like.device}")
-    if tuple(t.shape) != shape:
-        raise EvoxError(EINVAL, f"{what} has shape {tuple(t.shape)}, needs {shape}")
-    if t.numel() and shape[-1] > 1 and t.stride(-1) != 1:
+    if tuple(t.shape) != tuple(shape):
+        raise EvoxError(EINVAL, f"{what} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    if t.numel():
         raise EvoxError(EINVAL, f"{what}: rows are not dense")
+    return t.data_ptr()
 
 
-def _pitch(t, n):
-    """The row pitch of an [M, n] tensor (of one row, or none: n)."""
-    return n if t is None or t.shape[-2] <= 1 else t.stride(-2)
-
-
-def _offsets(off, like, G):
-    if off is None:
+def _vector(what, t, dtype, n, like):
+    """Checks a dense vector (or None) of n elements on like's device.  Its address."""
+    if t is None:
         return None
-    import torch
-    if off.dtype != torch.int32 or off.device != like.device or tuple(off.shape) != (G + 1,) or not off.is_contiguous():
-        raise EvoxError(EINVAL, f"off: a dense int32 tensor of {G + 1} on {like.device}")
-    return off.data_ptr()
+    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise EvoxError(EINVAL, f"{what}: a dense {dtype} tensor of {n} on {like.device}")
+    return t.data_ptr()
+
+
+def _pitch(t):
+    """The row pitch of an [M, n] tensor (of one row, or none: n)."""
+    shape = t.shape
+    return t.stride(-2) if shape[-2] > 1 else shape[-1]
 
 
 def _net_stride(t):
-    return t.stride(0) if t is not None and t.shape[0] > 1 else 0
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _offsets(off, like, G):
+    import torch
+    return _vector("off", off, torch.int32, G + 1, like)
+
+
+def _raw_stream(stream):
+    """The HIP stream of a call: the given one, or the current one of the current device."""
+    import torch
+    if stream is not None:
+        return stream.cuda_stream
+    try:  # what torch.cuda.current_stream().cuda_stream returns, without the object (3 us)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    except AttributeError:
+        return torch.cuda.current_stream().cuda_stream
 
 
 def _scratch(nbytes, like, scratch, stream):
@@ -294,7 +324,7 @@ def _scratch(nbytes, like, scratch, stream):
         scratch = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
         if stream is not None:
             scratch.record_stream(stream)
-    elif scratch.device != like.device or not scratch.is_contiguous():
+    elif scratch.get_device() != like.get_device() or not scratch.is_contiguous():
         raise EvoxError(EINVAL, f"scratch: a dense tensor on {like.device}")
     return scratch, scratch.numel() * scratch.element_size()
 
@@ -303,17 +333,15 @@ def _layer(x, w, y, act, off):
     """The layer of weights w [G, n_out, n_in] between x and y (or dy)."""
     if w.dim() != 3 or x.dim() != 2 or y.dim() != 2:
         raise EvoxError(EINVAL, "w must be [G, n_out, n_in], x and y [rows, n]")
-    G, n_out, n_in = w.shape
-    M = y.shape[0]
+    (G, n_out, n_in), M = w.shape, y.shape[0]
     shared = off is None and G > 1 and x.shape[0] != M
-    _view("x", x, w, M // G if shared else M, n_in)
-    _view("w", w, w, G, n_out, n_in)
-    _view("y", y, w, M, n_out)
     if shared and M % G:
         raise EvoxError(EINVAL, f"{M} rows for {G} networks")
-    return Layer(dtype=_dtype(w), act=act, G=G, M=M, n_in=n_in, n_out=n_out, off=_offsets(off, w, G),
-                 x_shared=int(shared), ldx=_pitch(x, n_in), ldw=_pitch(w, n_in), w_stride=_net_stride(w),
-                 ldy=_pitch(y, n_out))
+    _view("w", w, w, w.shape)
+    _view("x", x, w, (M // G if shared else M, n_in))
+    _view("y", y, w, (M, n_out))
+    return Layer(_dtype(w), act, G, M, n_in, n_out, _offsets(off, w, G), shared, _pitch(x), _pitch(w), _net_stride(w),
+                 0, 0, 0, _pitch(y))
 
 
 def evox_linear(x, w, y, b=None, r=None, z=None, off=None, act=ACT_NONE, stream=None):
@@ -324,79 +352,82 @@ def evox_linear(x, w, y, b=None, r=None, z=None, off=None, act=ACT_NONE, stream=
     rows off[g] .. off[g + 1), by default M / G each.  z receives the
     pre-activations (for evox_linear_grad)."""
     p = _layer(x, w, y, act, off)
-    _view("b", b, w, p.G, p.n_out)
-    _view("r", r, w, p.M, p.n_out)
-    _view("z", z, w, p.M, p.n_out)
-    p.b_stride, p.ldr, p.ldz = _net_stride(b), _pitch(r, p.n_out), _pitch(z, p.n_out)
-    _check(lib().evox_linear(ctypes.byref(p), _ptr(x), _ptr(w), _ptr(b), _ptr(r), _ptr(z), _ptr(y), _stream(stream)))
+    rows = y.shape
+    if b is not None:
+        _view("b", b, w, (p.G, p.n_out))
+        p.b_stride = _net_stride(b)
+    if r is not None:
+        _view("r", r, w, rows)
+        p.ldr = _pitch(r)
+    if z is not None:
+        _view("z", z, w, rows)
+        p.ldz = _pitch(z)
+    rc = lib().evox_linear(ctypes.byref(p), x.data_ptr(), w.data_ptr(), None if b is None else b.data_ptr(),
+                           None if r is None else r.data_ptr(), None if z is None else z.data_ptr(), y.data_ptr(),
+                           _raw_stream(stream))
+    if rc != OK:
+        _check(rc)
     return y
 
 
 def evox_linear_grad_scratch(x, w, dy):
-    """Scratch for evox_linear_grad calls of these shapes."""
-    return _scratch(lib().evox_linear_grad_scratch_bytes(ctypes.byref(_layer(x, w, dy, ACT_NONE, _any_off(x, w, dy)))),
-                    w, None, None)[0]
-
-
-def _any_off(x, w, y):
-    """Row offsets for sizing a scratch, which does not depend on them: needed
-    only where the rows are not as many for every network."""
+    """Scratch for evox_linear_grad calls of these shapes (any activation and offsets)."""
     import torch
-    G, M = w.shape[0], y.shape[0]
-    return torch.zeros(G + 1, dtype=torch.int32, device=w.device) if x.shape[0] == M and M % G else None
+    G, M = w.shape[0], dy.shape[0]
+    off = torch.zeros(G + 1, dtype=torch.int32, device=w.device) if x.shape[0] == M and M % G else None
+    p = _layer(x, w, dy, ACT_NONE, off)
+    return _scratch(lib().evox_linear_grad_scratch_bytes(ctypes.byref(p)), w, None, None)[0]
 
 
 def evox_linear_grad(x, w, dy, z=None, dx=None, dw=None, db=None, off=None, act=ACT_NONE, scratch=None, stream=None):
     """The gradient of evox_linear from dy and the stored z: dx [M, n_in], dw [G,
     n_out, n_in], db [G, n_out], each where given (the residual's is dy)."""
     p = _layer(x, w, dy, act, off)
-    _view("z", z, w, p.M, p.n_out)
-    _view("dx", dx, w, p.M, p.n_in)
-    _view("dw", dw, w, p.G, p.n_out, p.n_in)
-    _view("db", db, w, p.G, p.n_out)
-    p.ldz, p.lddx, p.lddw = _pitch(z, p.n_out), _pitch(dx, p.n_in), _pitch(dw, p.n_in)
-    p.dw_stride, p.db_stride = _net_stride(dw), _net_stride(db)
+    z_at = _view("z", z, w, dy.shape)
+    dx_at = _view("dx", dx, w, (p.M, p.n_in))
+    dw_at = _view("dw", dw, w, w.shape)
+    db_at = _view("db", db, w, (p.G, p.n_out))
+    if z is not None:
+        p.ldz = _pitch(z)
+    if dx is not None:
+        p.lddx = _pitch(dx)
+    if dw is not None:
+        p.lddw, p.dw_stride = _pitch(dw), _net_stride(dw)
+    if db is not None:
+        p.db_stride = _net_stride(db)
     scratch, nbytes = _scratch(lib().evox_linear_grad_scratch_bytes(ctypes.byref(p)), w, scratch, stream)
-    _check(lib().evox_linear_grad(ctypes.byref(p), _ptr(x), _ptr(w), _ptr(z), _ptr(dy), _ptr(dx), _ptr(dw), _ptr(db),
-                                  _ptr(scratch), nbytes, _stream(stream)))
+    _check(lib().evox_linear_grad(ctypes.byref(p), x.data_ptr(), w.data_ptr(), z_at, dy.data_ptr(), dx_at, dw_at,
+                                  db_at, scratch.data_ptr(), nbytes, _raw_stream(stream)))
     return dx, dw, db
 
 
 def _norm(x, gamma, off, eps):
     if x.dim() != 2 or gamma.dim() != 2:
         raise EvoxError(EINVAL, "x must be [M, D], gamma [G, D]")
-    M, D = x.shape
-    _view("x", x, x, M, D)
-    _view("gamma", gamma, x, gamma.shape[0], D)
-    return Norm(dtype=_dtype(x), G=gamma.shape[0], M=M, D=D, off=_offsets(off, x, gamma.shape[0]), ldx=_pitch(x, D),
-                p_stride=_net_stride(gamma), eps=eps)
-
-
-def _stat(what, t, x):
-    import torch
-    if t is not None and (t.dtype != torch.float32 or t.device != x.device or tuple(t.shape) != (x.shape[0],)
-                          or not t.is_contiguous()):
-        raise EvoxError(EINVAL, f"{what}: a dense float32 tensor of {x.shape[0]} on {x.device}")
+    (M, D), G = x.shape, gamma.shape[0]
+    _view("x", x, x, x.shape)
+    _view("gamma", gamma, x, (G, D))
+    return Norm(_dtype(x), G, M, D, _offsets(off, x, G), _pitch(x), 0, 0, _net_stride(gamma), 0, eps)
 
 
 def evox_layernorm(x, gamma, beta, y, mean=None, rstd=None, off=None, eps=1e-5, stream=None):
     """y = (x - mean) rstd gamma_g + beta_g over the rows of x [M, D], with gamma and
     beta [G, D]; mean and rstd (float32 [M]) receive the rows' statistics."""
+    import torch
     p = _norm(x, gamma, off, eps)
-    _view("beta", beta, x, p.G, p.D)
-    _view("y", y, x, p.M, p.D)
+    _view("beta", beta, x, gamma.shape)
+    _view("y", y, x, x.shape)
     if _net_stride(beta) != p.p_stride:
         raise EvoxError(EINVAL, "gamma and beta have different strides")
-    _stat("mean", mean, x)
-    _stat("rstd", rstd, x)
-    p.ldy = _pitch(y, p.D)
-    _check(lib().evox_layernorm(ctypes.byref(p), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y), _ptr(mean), _ptr(rstd),
-                                _stream(stream)))
+    p.ldy = _pitch(y)
+    _check(lib().evox_layernorm(ctypes.byref(p), x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), y.data_ptr(),
+                                _vector("mean", mean, torch.float32, p.M, x),
+                                _vector("rstd", rstd, torch.float32, p.M, x), _raw_stream(stream)))
     return y
 
 
 def evox_layernorm_grad_scratch(x, gamma):
-    """Scratch for evox_layernorm_grad calls of these shapes."""
+    """Scratch for evox_layernorm_grad calls of these shapes (any offsets)."""
     import torch
     G = gamma.shape[0]
     off = torch.zeros(G + 1, dtype=torch.int32, device=x.device) if x.shape[0] % G else None
@@ -406,19 +437,24 @@ def evox_layernorm_grad_scratch(x, gamma):
 def evox_layernorm_grad(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=None, off=None, scratch=None,
                         stream=None):
     """The gradient of evox_layernorm: dx [M, D], dgamma and dbeta [G, D], where given."""
+    import torch
     p = _norm(x, gamma, off, 1.0)
-    _view("dy", dy, x, p.M, p.D)
-    _view("dx", dx, x, p.M, p.D)
-    _view("dgamma", dgamma, x, p.G, p.D)
-    _view("dbeta", dbeta, x, p.G, p.D)
-    if _net_stride(dgamma) != _net_stride(dbeta):
-        raise EvoxError(EINVAL, "dgamma and dbeta have different strides")
-    _stat("mean", mean, x)
-    _stat("rstd", rstd, x)
-    p.ldy, p.lddx, p.dp_stride = _pitch(dy, p.D), _pitch(dx, p.D), _net_stride(dgamma)
+    dy_at = _view("dy", dy, x, x.shape)
+    dx_at = _view("dx", dx, x, x.shape)
+    dg_at = _view("dgamma", dgamma, x, gamma.shape)
+    db_at = _view("dbeta", dbeta, x, gamma.shape)
+    p.ldy = _pitch(dy)
+    if dx is not None:
+        p.lddx = _pitch(dx)
+    if dgamma is not None and dbeta is not None:
+        p.dp_stride = _net_stride(dgamma)
+        if p.dp_stride != _net_stride(dbeta):
+            raise EvoxError(EINVAL, "dgamma and dbeta have different strides")
     scratch, nbytes = _scratch(lib().evox_layernorm_grad_scratch_bytes(ctypes.byref(p)), x, scratch, stream)
-    _check(lib().evox_layernorm_grad(ctypes.byref(p), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(dx),
-                                     _ptr(dgamma), _ptr(dbeta), _ptr(scratch), nbytes, _stream(stream)))
+    _check(lib().evox_layernorm_grad(ctypes.byref(p), x.data_ptr(), gamma.data_ptr(),
+                                     _vector("mean", mean, torch.float32, p.M, x),
+                                     _vector("rstd", rstd, torch.float32, p.M, x), dy_at, dx_at, dg_at, db_at,
+                                     scratch.data_ptr(), nbytes, _raw_stream(stream)))
     return dx, dgamma, dbeta
 
 
@@ -426,13 +462,12 @@ def _classes(logits, G, off, shared):
     if logits.dim() != 2:
         raise EvoxError(EINVAL, "logits must be [M, C]")
     M, C = logits.shape
-    _view("logits", logits, logits, M, C)
-    return Classes(dtype=_dtype(logits), G=G, M=M, C=C, off=_offsets(off, logits, G), labels_shared=int(shared),
-                   ldz=_pitch(logits, C))
+    _view("logits", logits, logits, logits.shape)
+    return Classes(_dtype(logits), G, M, C, _offsets(off, logits, G), shared, _pitch(logits), 0)
 
 
 def evox_xent_scratch(logits, fit):
-    """Scratch for evox_xent calls of these shapes."""
+    """Scratch for evox_xent calls of these shapes (any offsets)."""
     import torch
     G = fit.shape[0]
     off = torch.zeros(G + 1, dtype=torch.int32, device=fit.device) if logits.shape[0] % G else None
@@ -444,19 +479,19 @@ def evox_xent(logits, labels, fit, dz=None, off=None, scratch=None, stream=None)
     (int32 [M], or [M / G]: the same for every network; rows whose label is outside
     0 .. C-1 do not count), and its gradient dz [M, C] where given."""
     import torch
+    if fit.dim() != 1 or labels.dim() != 1:
+        raise EvoxError(EINVAL, "fit and labels are vectors")
     G, M = fit.shape[0], logits.shape[0]
     shared = off is None and G > 1 and labels.shape[0] != M
-    if (fit.dtype != torch.float32 or fit.device != logits.device or fit.dim() != 1 or not fit.is_contiguous()):
-        raise EvoxError(EINVAL, f"fit: a dense float32 vector on {logits.device}")
-    if (labels.dtype != torch.int32 or labels.device != logits.device or not labels.is_contiguous()
-            or tuple(labels.shape) != ((M // G if shared else M),)):
-        raise EvoxError(EINVAL, f"labels: a dense int32 tensor of {M} (or {M} / {G}) on {logits.device}")
+    fit_at = _vector("fit", fit, torch.float32, G, logits)
+    labels_at = _vector("labels", labels, torch.int32, M // G if shared else M, logits)
     p = _classes(logits, G, off, shared)
-    _view("dz", dz, logits, M, p.C)
-    p.lddz = _pitch(dz, p.C)
+    dz_at = _view("dz", dz, logits, logits.shape)
+    if dz is not None:
+        p.lddz = _pitch(dz)
     scratch, nbytes = _scratch(lib().evox_xent_scratch_bytes(ctypes.byref(p)), logits, scratch, stream)
-    _check(lib().evox_xent(ctypes.byref(p), _ptr(logits), _ptr(labels), _ptr(fit), _ptr(dz), _ptr(scratch), nbytes,
-                           _stream(stream)))
+    _check(lib().evox_xent(ctypes.byref(p), logits.data_ptr(), labels_at, fit_at, dz_at, scratch.data_ptr(), nbytes,
+                           _raw_stream(stream)))
     return fit
 
 

@@ -232,39 +232,208 @@ __global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int L, T *d
     for (int r = 0; r < slots - 1; ++r)
 #pragma unroll
         for (int j = 0; j < N; ++j) s[j] += slots_sum[(r * N + j) * L + lane];
+    if (t.only) {
+        reg out;
+#pragma unroll
+        for (int j = 0; j < N; ++j) out[j] = (T)s[j];
+        store_chunk((T *)a.db + t.g * a.db_stride, c, n, out);
+        return;
+    }
+    sums += net_slot(t.lo, t.index, kDzShift) * n + c * N;
 #pragma unroll
     for (int j = 0; j < N; ++j)
-        if (c * N + j < n) sums[tile * n + c * N + j] = s[j];
+        if (c * N + j < n) sums[j] = s[j];
 }
 
-// db from a network's tiles, in order.
+// Sums over a network's rows: dw[o][i] (n_in of them per output; 0: none), then db.
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_db(LinearGradArgs a, const float *sums)
+struct GradSums {
+    T *dw, *db;
+    int64_t n_out, n_in, lddw, dw_stride, db_stride;
+    __device__ void operator()(int64_t g, int64_t e, float s) const
+    {
+        if (e >= n_out * n_in) {
+            if (db) db[g * db_stride + e - n_out * n_in] = (T)s;
+        } else if (dw) {
+            const int64_t o = (int64_t)((uint32_t)e / (uint32_t)n_in);
+            dw[g * dw_stride + o * lddw + e - o * n_in] = (T)s;
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------
+// The whole gradient of narrow layers (both widths at most 64) in one pass: a
+// block takes 2^sh rows of one network, W stays in LDS, and 16 rows per wave at a
+// time d = dy act'(z) (not rounded: all of it is fp32 here) and x pass through
+// LDS into the fp32 matrix cores; every operand is read once and dx written
+// once.  Wave w has rows 16 w .. + 16 of dx, and of the dw tiles every WAVES-th.
+// Bound by memory: fp32 4096x32 rows 32x32 moves 101 MB.
+// ---------------------------------------------------------------------------
+constexpr int kNarrow = 64;
+
+template <typename T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGradArgs a, int sh, float *part)
 {
-    const int o = blockIdx.x * 256 + threadIdx.x;
-    if (o >= a.n_out) return;
-    for (int64_t g = blockIdx.y; g < a.rows.G; g += gridDim.y) {
-        int64_t lo, hi;
-        net_rows(a.rows, g, &lo, &hi);
-        const int64_t t0 = net_first_tile(a.rows, kDzShift, g), n = (hi - lo + (1 << kDzShift) - 1) >> kDzShift;
-        float s = 0.0f;
-        for (int64_t t = 0; t < n; ++t) s += sums[(t0 + t) * a.n_out + o];
-        ((T *)a.db)[g * a.db_stride + o] = (T)s;
+    constexpr int N = NetVec<T>::N, TH = 64 * WAVES, R = 16 * WAVES, kDw = 16 / WAVES;
+    typedef typename NetVec<T>::reg reg;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const NetTile t = net_tile(a.rows, sh, net_block());
+    if (t.g < 0) return;
+    const int ni = (int)a.n_in, no = (int)a.n_out, ti = (ni + 15) / 16, to = (no + 15) / 16, pi = ti * 16 + 4,
+              po = to * 16 + 4;
+    float *W = lds, *X = W + (a.dx ? to * 16 * pi : 0), *D = X + R * pi;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l16 = tid % 16, q = tid % 64 / 16;
+    // n elements of a row of the type (or zeros) to a row of LDS, padded with zeros to whole tiles
+    auto put = [&](float *row, int c, reg v) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4 *>(row + c * N + j) = (f32x4){(float)v[j], (float)v[j + 1], (float)v[j + 2], (float)v[j + 3]};
+    };
+    const int ci = ti * 16 / N, co = to * 16 / N;  // chunks per padded row
+    if (a.dx) {
+        const T *w = (const T *)a.w + t.g * a.w_stride;
+#pragma unroll 2
+        for (int k = tid; k < to * 16 * ci; k += TH) {
+            const int o = k / ci, c = k - o * ci;
+            put(W + o * pi, c, o < no ? load_chunk(w + o * a.ldw, c, ni, (T)0.0f) : (reg){});
+        }
+    }
+    f32x4 dw[kDw];
+#pragma unroll
+    for (int s = 0; s < kDw; ++s) dw[s] = (f32x4)(0.0f);
+    float db = 0.0f;
+    const int64_t x0 = a.x_shared ? (int64_t)t.g * a.rows.n : 0;
+    for (int64_t m0 = t.lo; m0 < t.hi; m0 += R) {
+        if (m0 > t.lo) __syncthreads();
+        // two chunks of d per round, their loads first
+#pragma unroll 1
+        for (int k0 = tid; k0 < R * co; k0 += 2 * TH) {
+            reg dy[2] = {}, z[2] = {};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int k = k0 + u * TH, r = k / co, c = k - r * co;
+                if (k >= R * co || m0 + r >= t.hi) continue;
+                dy[u] = load_chunk((const T *)a.dy + (m0 + r) * a.lddy, c, no, (T)0.0f);
+                if (a.act != ACT_NONE) z[u] = load_chunk((const T *)a.z + (m0 + r) * a.ldz, c, no, (T)0.0f);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int k = k0 + u * TH, r = k / co, c = k - r * co;
+                if (k >= R * co) continue;
+                float v[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = (float)z[u][j];
+                act_slopes<sizeof(T) == 2, N>(a.act, v);
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] *= (float)dy[u][j];
+#pragma unroll
+                for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4 *>(D + r * po + c * N + j) = (f32x4){v[j], v[j + 1], v[j + 2], v[j + 3]};
+            }
+        }
+        if (a.dw)
+#pragma unroll 2
+            for (int k = tid; k < R * ci; k += TH) {
+                const int r = k / ci, c = k - r * ci;
+                put(X + r * pi, c, m0 + r < t.hi ? load_chunk((const T *)a.x + (m0 + r - x0) * a.ldx, c, ni, (T)0.0f) : (reg){});
+            }
+        __syncthreads();
+        if (a.dx) {
+            const int64_t m = m0 + wave * 16 + l16;
+            const float *d = D + (wave * 16 + l16) * po;
+            for (int i = 0; i < ti; ++i) {
+                f32x4 acc = (f32x4)(0.0f);
+                for (int k = 0; k < to; ++k) {
+                    const f32x4 b = *reinterpret_cast<const f32x4 *>(d + k * 16 + 4 * q);
+                    f32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = W[(k * 16 + 4 * q + e) * pi + i * 16 + l16];
+                    acc = mma16(w, b, acc);
+                }
+                if (m < t.hi) {
+                    T *dx = (T *)a.dx + m * a.lddx + i * 16 + 4 * q;
+                    if (i * 16 + 4 * q + 4 <= ni) {
+                        typename Quad<T>::mem v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = (T)acc[e];
+                        *reinterpret_cast<typename Quad<T>::mem *>(dx) = v;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (i * 16 + 4 * q + e < ni) dx[e] = (T)acc[e];
+                    }
+                }
+            }
+        }
+        if (a.dw)
+#pragma unroll
+            for (int s = 0; s < kDw; ++s) {
+                const int u = wave + s * WAVES;
+                if (u >= ti * to) continue;
+                const int o = u / ti, i = u - o * ti;
+#pragma unroll 1
+                for (int k = 0; k < R; k += 16) {
+                    f32x4 p, d;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[e] = X[(k + 4 * q + e) * pi + i * 16 + l16];
+                        d[e] = D[(k + 4 * q + e) * po + o * 16 + l16];
+                    }
+                    dw[s] = mma16(p, d, dw[s]);
+                }
+            }
+        if (tid < no) {
+#pragma unroll 4
+            for (int r = 0; r < R; ++r) db += D[r * po + tid];
+        }
+    }
+    // the results, or this tile's sums
+    float *sums = part + net_slot(t.lo, t.index, sh) * no * (ni + 1);
+    if (a.dw)
+#pragma unroll
+        for (int s = 0; s < kDw; ++s) {
+            const int u = wave + s * WAVES;
+            if (u >= ti * to) continue;
+            const int o = u / ti * 16 + l16, i = (u - u / ti * ti) * 16 + 4 * q;
+            if (o < no)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (i + e >= ni) continue;
+                    if (t.only) ((T *)a.dw)[t.g * a.dw_stride + o * a.lddw + i + e] = (T)dw[s][e];
+                    else sums[o * ni + i + e] = dw[s][e];
+                }
+        }
+    if (a.db && tid < no) {
+        if (t.only) ((T *)a.db)[t.g * a.db_stride + tid] = (T)db;
+        else sums[no * ni + tid] = db;
     }
 }
 
-// The scratch: d, then the tiles' column sums.
+// Rows per tile of the narrow gradient, as a power of two: about 2048 tiles, of
+// 64 .. 4096 rows.
+int narrow_shift(const LinearGradArgs &a)
+{
+    int sh = 6;
+    while (sh < 12 && (a.rows.M >> sh) > 2048) ++sh;
+    return sh;
+}
+bool narrow(const LinearGradArgs &a) { return a.n_in <= kNarrow && a.n_out <= kNarrow; }
+
+// The scratch: d, then the tiles' column sums; of narrow layers, the tiles' sums.
 struct GradScratch {
-    int64_t ldd;
-    size_t sums, end;
+    int64_t ldd = 0;
+    size_t sums = 0, end = 0;
 };
 GradScratch grad_layout(const LinearGradArgs &a)
 {
     GradScratch g;
+    if (narrow(a)) {
+        g.sums = 0;
+        g.end = 4 * (size_t)net_slots(a.rows.M, narrow_shift(a)) * (size_t)(a.n_out * (a.n_in + 1));
+        return g;
+    }
     const size_t e = a.dtype == NET_F32 ? 4 : 2;
     g.ldd = (a.n_out + 7) / 8 * 8;
     g.sums = (e * (size_t)a.rows.M * (size_t)g.ldd + 255) / 256 * 256;
-    g.end = g.sums + 4 * ((size_t)(a.rows.M >> kDzShift) + (size_t)a.rows.G) * (size_t)a.n_out;
+    g.end = g.sums + 4 * (size_t)net_slots(a.rows.M, kDzShift) * (size_t)a.n_out;
     return g;
 }
 
@@ -317,10 +486,27 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         using T = typename NetElement<t.value>::type;
         constexpr int N = NetVec<T>::N;
         const GradScratch l = grad_layout(a);
+        const int64_t mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
+        hipError_t e = hipSuccess;
+        if (narrow(a)) {
+            const int sh = narrow_shift(a);
+            float *part = (float *)a.scratch;
+            auto go = [&](auto waves) {
+                const int64_t ti = (a.n_in + 15) / 16 * 16, to = (a.n_out + 15) / 16 * 16;
+                const size_t lds = sizeof(float) * ((a.dx ? to * (ti + 4) : 0) + 16 * waves.value * (ti + 4 + to + 4));
+                hipLaunchKernelGGL((k_linear_grad_narrow<T, waves.value>), net_grid(net_tiles(a.rows, sh)),
+                                   dim3(64 * waves.value), lds, s, a, sh, part);
+                return hipGetLastError();
+            };
+            if (a.rows.M > 0)
+                e = mean <= 32 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
+            if (e != hipSuccess || (!a.dw && !a.db) || (a.rows.M > 0 && !a.rows.off && net_single(a.rows, sh))) return e;
+            return launch_net_sums(a.rows, part, a.n_out * (a.n_in + 1), sh, s,
+                                   GradSums<T>{(T *)a.dw, (T *)a.db, a.n_out, a.n_in, a.lddw, a.dw_stride, a.db_stride});
+        }
         const bool own = a.act != ACT_NONE && (a.dx || a.dw);
         T *d = own ? (T *)a.scratch : nullptr;
         float *sums = a.db ? (float *)((char *)a.scratch + l.sums) : nullptr;
-        hipError_t e = hipSuccess;
         if (a.rows.M > 0 && (d || sums)) {
             int L = 4;
             while (L < 256 && L * N < a.n_out) L *= 2;
@@ -329,14 +515,13 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
                                sizeof(float) * N * (256 - L), s, a, L, d, l.ldd, sums);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        if (a.db) {
-            hipLaunchKernelGGL((k_linear_db<T>),
-                               dim3((unsigned)((a.n_out + 255) / 256), (unsigned)(a.rows.G < 32768 ? a.rows.G : 32768)),
-                               dim3(256), 0, s, a, sums);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
+        if (a.db && !(a.rows.M > 0 && !a.rows.off && net_single(a.rows, kDzShift))) {
+            e = launch_net_sums(a.rows, sums, a.n_out, kDzShift, s,
+                                GradSums<T>{nullptr, (T *)a.db, a.n_out, 0, 0, 0, a.db_stride});
+            if (e != hipSuccess) return e;
         }
         const void *dd = own ? d : a.dy;
-        const int64_t ldd = own ? l.ldd : a.lddy, mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
+        const int64_t ldd = own ? l.ldd : a.lddy;
         if (a.dx)
             e = launch_linear_dx_tiles<t.value>(a, dd, ldd, tile_size(a.dtype, a.n_in, mean, a.rows.M * a.n_in), s);
         if (e == hipSuccess && a.dw)

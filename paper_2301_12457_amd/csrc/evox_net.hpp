@@ -188,6 +188,7 @@ struct NetTile {
     int g;           // -1: no rows
     int index;       // of the network's tiles
     int64_t lo, hi;  // rows
+    bool only;       // the network has no other tile
 };
 __host__ __device__ __forceinline__ int64_t net_tiles(const NetRows &r, int sh)
 {
@@ -212,6 +213,7 @@ __device__ __forceinline__ NetTile net_tile(const NetRows &r, int sh, int64_t t)
         o.lo = (int64_t)g * r.n + ((int64_t)o.index << sh);
         o.hi = (int64_t)(g + 1) * r.n;
         o.g = (int)g;
+        o.only = per == 1;
     } else {
         int lo = 0, hi = (int)r.G;
         const int lane = threadIdx.x % 64;
@@ -231,9 +233,55 @@ __device__ __forceinline__ NetTile net_tile(const NetRows &r, int sh, int64_t t)
         o.index = (int)i;
         if (i < 0 || o.lo >= b) return o;
         o.g = lo;
+        o.only = b - a <= ((int64_t)1 << sh);
     }
     if (o.hi > o.lo + ((int64_t)1 << sh)) o.hi = o.lo + ((int64_t)1 << sh);
     return o;
+}
+
+// Sums over a network's rows: the network's only tile writes its result, several
+// leave fp32 partial sums, added in the tiles' order by k_net_sums.  A partial's
+// place is its tile's first row over 2^sh, doubled, plus one after the network's
+// first tile: a network of several tiles covers whole blocks of 2^sh rows, so no
+// two such tiles meet, and 2 (M / 2^sh + 1) places are enough for any offsets
+// (a place per tile would be one per network, even of a single row).
+__device__ __forceinline__ int64_t net_slot(int64_t lo, int index, int sh) { return 2 * (lo >> sh) + (index > 0); }
+__host__ __device__ __forceinline__ int64_t net_slots(int64_t M, int sh) { return 2 * ((M >> sh) + 1); }
+// Whether every network has at most one tile, for certain.
+inline bool net_single(const NetRows &r, int sh) { return r.off ? r.M <= ((int64_t)1 << sh) : r.n <= ((int64_t)1 << sh); }
+
+// out(g, e, sum) for the networks of several tiles and those without rows (sum
+// 0): 64 elements by 4 shares of the tiles per block.
+template <typename F>
+__global__ __launch_bounds__(256) void k_net_sums(NetRows rows, const float *part, int64_t width, int sh, F out)
+{
+    __shared__ float share[3][64];
+    const int64_t e = (int64_t)blockIdx.x * 64 + threadIdx.x % 64;
+    const int w = threadIdx.x / 64;
+    for (int64_t g = blockIdx.y; g < rows.G; g += gridDim.y) {
+        int64_t lo, hi;
+        net_rows(rows, g, &lo, &hi);
+        const int64_t n = (hi - lo + ((int64_t)1 << sh) - 1) >> sh, per = (n + 3) / 4;
+        if (n == 1) continue;
+        float s = 0.0f;
+        if (e < width) {
+            const int64_t t1 = (w + 1) * per < n ? (w + 1) * per : n;
+#pragma unroll 4
+            for (int64_t t = w * per; t < t1; ++t) s += part[net_slot(lo + (t << sh), (int)t, sh) * width + e];
+        }
+        if (w > 0) share[w - 1][threadIdx.x % 64] = s;
+        __syncthreads();
+        if (w == 0 && e < width) out(g, e, s + share[0][threadIdx.x] + share[1][threadIdx.x] + share[2][threadIdx.x]);
+        __syncthreads();
+    }
+}
+template <typename F>
+hipError_t launch_net_sums(const NetRows &rows, const float *part, int64_t width, int sh, hipStream_t s, F out)
+{
+    hipLaunchKernelGGL((k_net_sums<F>),
+                       dim3((unsigned)((width + 63) / 64), (unsigned)(rows.G < 32768 ? rows.G : 32768)), dim3(256), 0, s,
+                       rows, part, width, sh, out);
+    return hipGetLastError();
 }
 
 // Activations and their slopes.  For results of 16 bits the hardware's exp2

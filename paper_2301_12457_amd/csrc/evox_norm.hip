@@ -149,8 +149,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
 // ---------------------------------------------------------------------------
 // Its gradient.  A block takes a tile of one network's rows: every lane keeps
 // the sums of dy h and dy of its own columns over the rows it meets, the row
-// slots of the block add theirs in order, and the tile's sums go to the
-// scratch ([tile][2][D]); k_layernorm_params adds a network's tiles in order.
+// slots of the block add theirs in order; k_net_sums adds a network's tiles.
 // Rows whose chunks and sums do not fit the registers together (fp32, eight
 // chunks per lane) are read a second time.
 // ---------------------------------------------------------------------------
@@ -256,36 +255,41 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a
                     sb[i][j] += sums[(((r * 2 + 1) * NIT + i) * N + j) * L + lane];
                 }
     }
-    float *part = (float *)a.scratch + net_block() * 2 * D;
+    float *part = (float *)a.scratch + net_slot(t.lo, t.index, sh) * 2 * D;
 #pragma unroll
-    for (int i = 0; i < NIT; ++i)
+    for (int i = 0; i < NIT; ++i) {
+        const int c = lane + i * L;
+        if (c * N >= D) continue;
+        if (t.only) {
+            typename NetVec<T>::reg g, b;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int e = (lane + i * L) * N + j;
-            if (e < D) {
-                part[e] = sg[i][j];
-                part[D + e] = sb[i][j];
+            for (int j = 0; j < N; ++j) {
+                g[j] = (T)sg[i][j];
+                b[j] = (T)sb[i][j];
             }
+            store_chunk((T *)a.dgamma + t.g * a.dp_stride, c, D, g);
+            store_chunk((T *)a.dbeta + t.g * a.dp_stride, c, D, b);
+            continue;
         }
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (c * N + j < D) {
+                part[c * N + j] = sg[i][j];
+                part[D + c * N + j] = sb[i][j];
+            }
+    }
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_layernorm_params(NormArgs a, int sh)
-{
-    const int64_t g = blockIdx.y;
-    const int e = blockIdx.x * 256 + threadIdx.x, D = (int)a.D;
-    if (e >= 2 * D) return;
-    for (int64_t gg = g; gg < a.rows.G; gg += gridDim.y) {
-        int64_t lo, hi;
-        net_rows(a.rows, gg, &lo, &hi);
-        const int64_t t0 = net_first_tile(a.rows, sh, gg), n = (hi - lo + ((int64_t)1 << sh) - 1) >> sh;
-        const float *part = (const float *)a.scratch + t0 * 2 * D + e;
-        float s = 0.0f;
-        for (int64_t t = 0; t < n; ++t) s += part[t * 2 * D];
-        if (e < D) ((T *)a.dgamma)[gg * a.dp_stride + e] = (T)s;
-        else ((T *)a.dbeta)[gg * a.dp_stride + e - D] = (T)s;
+struct NormSums {
+    T *dgamma, *dbeta;
+    int64_t stride, D;
+    __device__ void operator()(int64_t g, int64_t e, float s) const
+    {
+        if (e < D) dgamma[g * stride + e] = (T)s;
+        else dbeta[g * stride + e - D] = (T)s;
     }
-}
+};
 
 // Rows per tile of the gradient, as a power of two: 64 at most (its sums are
 // then 4 % or less of the rows' traffic), fewer where that leaves less than
@@ -533,7 +537,7 @@ hipError_t launch_layernorm(const NormArgs &a, hipStream_t s)
 
 size_t layernorm_grad_scratch(const NormArgs &a)
 {
-    return 8 * (size_t)((a.rows.M >> norm_tile_shift(a)) + a.rows.G) * (size_t)a.D;
+    return 8 * (size_t)net_slots(a.rows.M, norm_tile_shift(a)) * (size_t)a.D;
 }
 
 hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
@@ -550,10 +554,9 @@ hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
                 hipLaunchKernelGGL((k_layernorm_grad<T, nit.v, wide.v>), net_grid(tiles), dim3(r.threads), lds, s,
                                    a, r.L, sh);
             });
-        if (e != hipSuccess || !a.dgamma) return e;
-        const unsigned gy = (unsigned)(a.rows.G < 32768 ? a.rows.G : 32768);
-        hipLaunchKernelGGL((k_layernorm_params<T>), dim3((unsigned)((2 * a.D + 255) / 256), gy), dim3(256), 0, s, a, sh);
-        return hipGetLastError();
+        if (e != hipSuccess || !a.dgamma || (a.rows.M > 0 && !a.rows.off && net_single(a.rows, sh))) return e;
+        return launch_net_sums(a.rows, (const float *)a.scratch, 2 * a.D, sh, s,
+                               NormSums<T>{(T *)a.dgamma, (T *)a.dbeta, a.dp_stride, a.D});
     });
 }
 
