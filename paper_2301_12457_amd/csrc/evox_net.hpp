@@ -111,25 +111,32 @@ struct NetVec {
     typedef T mem __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
 
-// Elements [c N, c N + N) of a row of n, `fill` past its end.
-template <typename T>
+// Elements [c N, c N + N) of a row of n, `fill` past its end.  NT: with the
+// streaming hint.
+template <typename T, bool NT = false>
 __device__ __forceinline__ typename NetVec<T>::reg load_chunk(const T *row, int c, int n, T fill)
 {
     constexpr int N = NetVec<T>::N;
     const int at = c * N;
-    if (at + N <= n) return *reinterpret_cast<const typename NetVec<T>::mem *>(row + at);
+    if (at + N <= n) {
+        const auto *p = reinterpret_cast<const typename NetVec<T>::mem *>(row + at);
+        if constexpr (NT) return __builtin_nontemporal_load(p);
+        else return *p;
+    }
     typename NetVec<T>::reg v;
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = at + j < n ? row[at + j] : fill;
     return v;
 }
-template <typename T>
+template <typename T, bool NT = false>
 __device__ __forceinline__ void store_chunk(T *row, int c, int n, typename NetVec<T>::reg v)
 {
     constexpr int N = NetVec<T>::N;
     const int at = c * N;
     if (at + N <= n) {
-        *reinterpret_cast<typename NetVec<T>::mem *>(row + at) = v;
+        auto *p = reinterpret_cast<typename NetVec<T>::mem *>(row + at);
+        if constexpr (NT) __builtin_nontemporal_store((typename NetVec<T>::mem)v, p);
+        else *p = v;
         return;
     }
 #pragma unroll
@@ -236,6 +243,12 @@ __device__ __forceinline__ NetTile net_tile(const NetRows &r, int sh, int64_t t)
         o.only = b - a <= ((int64_t)1 << sh);
     }
     if (o.hi > o.lo + ((int64_t)1 << sh)) o.hi = o.lo + ((int64_t)1 << sh);
+    // the same in every lane: scalar registers, and scalar bases for the rows' addresses
+    o.g = __builtin_amdgcn_readfirstlane(o.g);
+    o.index = __builtin_amdgcn_readfirstlane(o.index);
+    o.lo = __builtin_amdgcn_readfirstlane((int)o.lo);
+    o.hi = __builtin_amdgcn_readfirstlane((int)o.hi);
+    o.only = __builtin_amdgcn_readfirstlane((int)o.only);
     return o;
 }
 

@@ -16,11 +16,11 @@ namespace {
 struct RowShape {
     int L, nit, threads;
 };
-RowShape row_shape(int64_t n, int N)
+RowShape row_shape(int64_t n, int N, int per)
 {
     const int64_t chunks = (n + N - 1) / N;
     RowShape s{4, 1, 256};
-    while (s.L < 64 && chunks > 2 * s.L) s.L *= 2;
+    while (s.L < 64 && chunks > per * s.L) s.L *= 2;
     while (s.L >= 64 && s.L < 1024 && chunks > 4 * s.L) s.L = s.L == 64 ? 256 : 2 * s.L;
     while (chunks > (int64_t)s.nit * s.L) s.nit *= 2;
     if (s.L > 256) s.threads = s.L;
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
             const auto gv = load_chunk(ga, c, D, (T)0.0f), bv = load_chunk(be, c, D, (T)0.0f);
 #pragma unroll
             for (int j = 0; j < N; ++j) v[i][j] = (T)fmaf(((float)v[i][j] - mean) * rstd, (float)gv[j], (float)bv[j]);
-            store_chunk(y, c, D, v[i]);
+            store_chunk<T, true>(y, c, D, v[i]);
         }
     }
     if (lane == 0) {
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a
                 sb[i][j] += d;
                 out[j] = (T)(rstd * (fmaf(d, (float)gv[j], -s1) - h * s2));
             }
-            if (a.dx) store_chunk((T *)a.dx + m * a.lddx, c, D, out);
+            if (a.dx) store_chunk<T, true>((T *)a.dx + m * a.lddx, c, D, out);
         }
     }
     if (!a.dgamma) return;
@@ -297,7 +297,7 @@ struct NormSums {
 int norm_tile_shift(const NormArgs &a)
 {
     int sh = 6;
-    while (sh > 3 && (a.rows.M >> sh) < 1024) --sh;
+    while (sh > 3 && (a.rows.M >> sh) < 512) --sh;
     return sh;
 }
 
@@ -361,9 +361,12 @@ __global__ __launch_bounds__(256) void k_xent_count(XentArgs a, int sh)
 
 // Tiles of 2^sh rows; whole: a tile is a whole network (rows may be more).
 template <typename T, int NIT, bool WIDE>
-__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, int sh, bool whole)
+__global__ __launch_bounds__(WIDE ? 1024 : 256, WIDE && NIT <= 4 ? 8 : 1) void k_xent(XentArgs a, int L, int sh, bool whole)
 {
     constexpr int N = NetVec<T>::N;
+    // fp32 exponentials take their logits' registers; those of long 16-bit rows are
+    // computed again, so that two blocks of 1024 threads fit a CU
+    constexpr bool kAgain = sizeof(T) == 2 && NIT == 4;
     __shared__ float lds[16];
     __shared__ double wave_loss[16];
     __shared__ int wave_count[16];
@@ -418,16 +421,23 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, i
 #pragma unroll
                     for (int j = 0; j < N; ++j) top = fmaxf(top, (float)v[i][j]);
         top = row_all<WIDE, true>(top, L, lds);
-        float e[NIT][N];
+        // past the row's end v is -inf: nothing, but in a row of -inf alone, all NaN anyway
+        float e16[kAgain || sizeof(T) == 4 ? 1 : NIT][N];
+        auto e = [&](int i, int j) -> float {
+            if constexpr (sizeof(T) == 4) return v[i][j];
+            else if constexpr (kAgain) return exp_below<T>((float)v[i][j], top);
+            else return e16[i][j];
+        };
         if (counts)
 #pragma unroll
             for (int i = 0; i < NIT; ++i)
                 if ((lane + i * L) * N < C)
 #pragma unroll
                     for (int j = 0; j < N; ++j) {
-                        // past the row's end v is -inf: nothing, but in a row of -inf alone, all NaN anyway
-                        e[i][j] = exp_below<T>((float)v[i][j], top);
-                        sum += e[i][j];
+                        const float p = exp_below<T>((float)v[i][j], top);
+                        if constexpr (sizeof(T) == 4) v[i][j] = p;
+                        else if constexpr (!kAgain) e16[i][j] = p;
+                        sum += p;
                     }
         sum = row_all<WIDE, false>(sum, L, lds);
         if (lane == 0 && counts) {
@@ -439,7 +449,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, i
             if (!counts) {
 #pragma unroll
                 for (int i = 0; i < NIT; ++i)
-                    if ((lane + i * L) * N < C) store_chunk(dz, lane + i * L, C, (typename NetVec<T>::reg){});
+                    if ((lane + i * L) * N < C) store_chunk<T, true>(dz, lane + i * L, C, (typename NetVec<T>::reg){});
                 continue;
             }
             const float f = scale / sum;
@@ -449,12 +459,12 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_xent(XentArgs a, int L, i
                 if (c * N >= C) continue;
                 typename NetVec<T>::reg out;
 #pragma unroll
-                for (int j = 0; j < N; ++j) out[j] = (T)(e[i][j] * f);
+                for (int j = 0; j < N; ++j) out[j] = (T)(e(i, j) * f);
                 if (c == label / N)  // the label's chunk: (p - 1) scale, rounded once
 #pragma unroll
                     for (int j = 0; j < N; ++j)
-                        if (j == label % N) out[j] = (T)fmaf(e[i][j], f, -scale);
-                store_chunk(dz, c, C, out);
+                        if (j == label % N) out[j] = (T)fmaf(e(i, j), f, -scale);
+                store_chunk<T, true>(dz, c, C, out);
             }
         }
     }
@@ -526,7 +536,7 @@ hipError_t launch_layernorm(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N);
+        const RowShape r = row_shape(a.D, NetVec<T>::N, 4);
         const int64_t per = r.L <= 64 ? 256 / r.L : 1;
         return with_shape<T>(r, [&](auto nit, auto wide) {
             hipLaunchKernelGGL((k_layernorm<T, nit.v, wide.v>), net_grid((a.rows.M + per - 1) / per),
@@ -544,7 +554,7 @@ hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N);
+        const RowShape r = row_shape(a.D, NetVec<T>::N, 2);
         const int sh = norm_tile_shift(a);
         const int64_t tiles = net_tiles(a.rows, sh);
         hipError_t e = hipSuccess;
@@ -570,7 +580,7 @@ hipError_t launch_xent(const XentArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.C, NetVec<T>::N);
+        const RowShape r = row_shape(a.C, NetVec<T>::N, 2);
         const bool whole = xent_whole(a);
         const int sh = xent_tile_shift(a);
         if (a.dz && !whole)
