@@ -437,15 +437,6 @@ GradScratch grad_layout(const LinearGradArgs &a)
     return g;
 }
 
-// Tiles of 64 where either side of the result is no more than that or larger
-// ones would leave CUs without a block; of 256 (16 bits) where they fill the chip.
-int tile_size(int32_t dtype, int64_t ni, int64_t nj, int64_t results)
-{
-    if (ni <= 64 || nj <= 64 || results < (int64_t)256 * 128 * 128) return 0;
-    if (dtype != NET_F32 && ni >= 192 && nj >= 192 && results >= (int64_t)512 * 256 * 256) return 2;
-    return 1;
-}
-
 }  // namespace
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
@@ -454,7 +445,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
         using T = typename NetElement<t.value>::type;
         const int64_t mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
         if (mean > 32 && a.n_out > 32 && a.n_in >= 64)
-            return launch_linear_tiles<t.value>(a, tile_size(a.dtype, a.n_out, mean, a.rows.M * a.n_out), s);
+            return launch_linear_tiles<t.value>(a, s);
         // rows of a wave's tile by the mean rows per network
         const int rb = mean <= 16 ? 1 : mean <= 32 ? 2 : 4, sh = rb == 1 ? 4 : rb == 2 ? 5 : 6, nb = rb == 1 ? 1 : 2;
         const uint32_t out_tiles = (uint32_t)((a.n_out + 16 * nb - 1) / (16 * nb));
@@ -522,11 +513,8 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         }
         const void *dd = own ? d : a.dy;
         const int64_t ldd = own ? l.ldd : a.lddy;
-        if (a.dx)
-            e = launch_linear_dx_tiles<t.value>(a, dd, ldd, tile_size(a.dtype, a.n_in, mean, a.rows.M * a.n_in), s);
-        if (e == hipSuccess && a.dw)
-            e = launch_linear_dw_tiles<t.value>(a, dd, ldd,
-                                                tile_size(a.dtype, a.n_in, a.n_out, a.rows.G * a.n_in * a.n_out), s);
+        if (a.dx) e = launch_linear_dx_tiles<t.value>(a, dd, ldd, s);
+        if (e == hipSuccess && a.dw) e = launch_linear_dw_tiles<t.value>(a, dd, ldd, s);
         return e;
     });
 }

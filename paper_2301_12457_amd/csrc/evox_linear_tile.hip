@@ -37,14 +37,7 @@ __device__ __forceinline__ void unit_ij(int64_t u, int64_t ti, int64_t tj, int64
 typedef NetVec<Elem>::reg Reg;
 typedef NetVec<Elem>::mem Mem;
 
-// n <= N neighbours of a row: added to v, and rounded from v.
-__device__ __forceinline__ void add_row(const Elem *p, float *v, int n)
-{
-    constexpr int N = NetVec<Elem>::N;
-    const Reg t = load_chunk(p, 0, n, (Elem)0.0f);
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] += (float)t[e];
-}
+// n <= N neighbours of a row rounded from v.
 __device__ __forceinline__ void store_row(Elem *p, const float *v, int n)
 {
     constexpr int N = NetVec<Elem>::N;
@@ -54,81 +47,106 @@ __device__ __forceinline__ void store_row(Elem *p, const float *v, int n)
     store_chunk(p, 0, n, t);
 }
 
-template <int B>
-struct TileShape;
-template <>
-struct TileShape<64> {
-    static constexpr int WI = 1, WJ = 2, sh = 6;
+// Results as they are (the gradients).
+struct PlainOut {
+    Elem *p;
+    int64_t ld;
+    __device__ __forceinline__ void begin(int, int) {}
+    __device__ __forceinline__ Reg load(int, int, int) { return (Reg){}; }
+    __device__ __forceinline__ void store(int j, int i, float *v, int n, Reg) { store_row(p + j * ld + i, v, n); }
 };
-template <>
-struct TileShape<128> {
-    static constexpr int WI = 2, WJ = 2, sh = 7;
+// The layer's epilogue; the pointers are at the tile's origin.
+struct LayerOut {
+    const Elem *b, *r;
+    Elem *z, *y;
+    int64_t ldr, ldz, ldy;
+    int act;
+    Reg bias;
+    __device__ __forceinline__ void begin(int i, int n) { bias = b ? load_chunk(b + i, 0, n, (Elem)0.0f) : (Reg){}; }
+    __device__ __forceinline__ Reg load(int j, int i, int n)
+    {
+        return r ? load_chunk(r + j * ldr + i, 0, n, (Elem)0.0f) : (Reg){};
+    }
+    __device__ __forceinline__ void store(int j, int i, float *v, int n, Reg res)
+    {
+        constexpr int N = NetVec<Elem>::N;
+        if (b)
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] += (float)bias[e];
+        if (z) store_row(z + j * ldz + i, v, n);
+        act_values<sizeof(Elem) == 2, N>(act, v);
+        if (r)
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] += (float)res[e];
+        store_row(y + j * ldy + i, v, n);
+    }
 };
-template <>
-struct TileShape<256> {
-    [[maybe_unused]] static constexpr int WI = 4, WJ = 2, sh = 8;  // 16 bits
+
+// Tile shapes, BI x BJ by WI x WJ waves.
+template <int ID>
+struct Shape {
+    static constexpr bool k32 = sizeof(Elem) == 4;
+    static constexpr int BI = ID == 0 ? 64 : ID == 1 ? 128 : 256;
+    static constexpr int BJ = k32 ? (ID == 3 ? 128 : 64) : ID == 0 ? 64 : ID == 3 ? 256 : 128;
+    static constexpr int WI = BI / 64, WJ = 2, kThreads = 64 * WI * WJ;
+    static constexpr int sh = BJ == 64 ? 6 : BJ == 128 ? 7 : 8;
 };
-template <int B, bool PM, bool QM>
-using Product = TileProduct<Elem, PM, QM, B, B, TileShape<B>::WI, TileShape<B>::WJ>;
+template <int ID, bool PM, bool QM>
+using Product = TileProduct<Elem, PM, QM, Shape<ID>::BI, Shape<ID>::BJ, Shape<ID>::WI, Shape<ID>::WJ>;
 
 // y = act(x W^T + b) + r: i = output, j = row, k = input.
-template <int B>
-__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ, 2) void k_linear_tile(LinearArgs a, int64_t ti,
+template <int ID>
+__global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_tile(LinearArgs a, int64_t ti,
                                                                                      int64_t tj, int64_t units)
 {
-    __shared__ __attribute__((aligned(16))) char lds[Product<B, false, false>::kLds];
+    __shared__ __attribute__((aligned(16))) char lds[Product<ID, false, false>::kLds];
     const int64_t u = xcd_unit(units);
     if (u < 0) return;
     int64_t it, jt;
     unit_ij(u, ti, tj, &it, &jt);
-    const NetTile t = net_tile(a.rows, TileShape<B>::sh, jt);
+    const NetTile t = net_tile(a.rows, Shape<ID>::sh, jt);
     if (t.g < 0) return;
-    const int i0 = (int)it * B, ni = min((int)a.n_out - i0, B), nj = (int)(t.hi - t.lo);
+    const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_out - i0, Shape<ID>::BI), nj = (int)(t.hi - t.lo);
     const int64_t x0 = a.x_shared ? t.lo - t.g * a.rows.n : t.lo;
     const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + i0 * a.ldw, a.ldw, ni},
         Q{(const Elem *)a.x + x0 * a.ldx, a.ldx, nj};
-    Product<B, false, false> p;
+    Product<ID, false, false> p;
     p.run(P, Q, a.n_in, lds);
-    const Elem *b = a.b ? (const Elem *)a.b + t.g * a.b_stride + i0 : nullptr;
-    p.results(ni, nj, lds, [&](int j, int i, float *v, int n) {
-        const int64_t m = t.lo + j;
-        if (b) add_row(b + i, v, n);
-        if (a.z) store_row((Elem *)a.z + m * a.ldz + i0 + i, v, n);
-        act_values<sizeof(Elem) == 2, NetVec<Elem>::N>(a.act, v);
-        if (a.r) add_row((const Elem *)a.r + m * a.ldr + i0 + i, v, n);
-        store_row((Elem *)a.y + m * a.ldy + i0 + i, v, n);
-    });
+    LayerOut out{a.b ? (const Elem *)a.b + t.g * a.b_stride + i0 : nullptr,
+                 a.r ? (const Elem *)a.r + t.lo * a.ldr + i0 : nullptr,
+                 a.z ? (Elem *)a.z + t.lo * a.ldz + i0 : nullptr, (Elem *)a.y + t.lo * a.ldy + i0,
+                 a.ldr, a.ldz, a.ldy, a.act, {}};
+    p.results(ni, nj, lds, out);
 }
 
 // dx = d W: i = input, j = row, k = output.
-template <int B>
-__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ, 2) void k_linear_dx_tile(LinearGradArgs a, const Elem *d,
+template <int ID>
+__global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(LinearGradArgs a, const Elem *d,
                                                                                       int64_t ldd, int64_t ti,
                                                                                       int64_t tj, int64_t units)
 {
-    __shared__ __attribute__((aligned(16))) char lds[Product<B, true, false>::kLds];
+    __shared__ __attribute__((aligned(16))) char lds[Product<ID, true, false>::kLds];
     const int64_t u = xcd_unit(units);
     if (u < 0) return;
     int64_t it, jt;
     unit_ij(u, ti, tj, &it, &jt);
-    const NetTile t = net_tile(a.rows, TileShape<B>::sh, jt);
+    const NetTile t = net_tile(a.rows, Shape<ID>::sh, jt);
     if (t.g < 0) return;
-    const int i0 = (int)it * B, ni = min((int)a.n_in - i0, B), nj = (int)(t.hi - t.lo);
+    const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_in - i0, Shape<ID>::BI), nj = (int)(t.hi - t.lo);
     const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + i0, a.ldw, ni}, Q{d + t.lo * ldd, ldd, nj};
-    Product<B, true, false> p;
+    Product<ID, true, false> p;
     p.run(P, Q, a.n_out, lds);
-    p.results(ni, nj, lds, [&](int j, int i, float *v, int n) {
-        store_row((Elem *)a.dx + (t.lo + j) * a.lddx + i0 + i, v, n);
-    });
+    PlainOut out{(Elem *)a.dx + t.lo * a.lddx + i0, a.lddx};
+    p.results(ni, nj, lds, out);
 }
 
 // dW = d^T x: i = input, j = output, k = row of the network.
-template <int B>
-__global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ, 2) void k_linear_dw_tile(LinearGradArgs a, const Elem *d,
+template <int ID>
+__global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dw_tile(LinearGradArgs a, const Elem *d,
                                                                                      int64_t ldd, int64_t ti, int64_t tj,
                                                                                      int64_t units)
 {
-    __shared__ __attribute__((aligned(16))) char lds[Product<B, true, true>::kLds];
+    __shared__ __attribute__((aligned(16))) char lds[Product<ID, true, true>::kLds];
     const int64_t u = xcd_unit(units);
     if (u < 0) return;
     const int64_t per = banded(tj) * ti, g = u / per;
@@ -136,23 +154,56 @@ __global__ __launch_bounds__(64 * TileShape<B>::WI * TileShape<B>::WJ, 2) void k
     unit_ij(u - g * per, ti, tj, &it, &jt);
     if (jt >= tj) return;
     net_rows(a.rows, g, &lo, &hi);
-    const int i0 = (int)it * B, ni = min((int)a.n_in - i0, B), j0 = (int)jt * B, nj = min((int)a.n_out - j0, B);
+    const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_in - i0, Shape<ID>::BI), j0 = (int)jt * Shape<ID>::BJ,
+              nj = min((int)a.n_out - j0, Shape<ID>::BJ);
     const TileOp<Elem> P{(const Elem *)a.x + (a.x_shared ? 0 : lo) * a.ldx + i0, a.ldx, ni}, Q{d + lo * ldd + j0, ldd, nj};
-    Product<B, true, true> p;
+    Product<ID, true, true> p;
     p.run(P, Q, hi - lo, lds);
-    p.results(ni, nj, lds, [&](int j, int i, float *v, int n) {
-        store_row((Elem *)a.dw + g * a.dw_stride + (j0 + j) * a.lddw + i0 + i, v, n);
-    });
+    PlainOut out{(Elem *)a.dw + g * a.dw_stride + j0 * a.lddw + i0, a.lddw};
+    p.results(ni, nj, lds, out);
 }
 
-// f(tile side) for size 0, 1, 2.
-template <typename F>
-hipError_t with_tile(int size, F &&f)
+// The shape with the least estimated time: rounds of resident blocks times a
+// block's work, its products plus 96 of them per row of K staged (which is how
+// the shapes' times compare where all fill the chip: bf16 16x2048 4096x4096 1543,
+// 1406, 1183 us in shapes 1, 2, 3, fp32 16x256 2048x2048 267, 260, 190; where
+// they do not, the smaller win: fp32 4096 rows 1024x1024 64, 63, 77, bf16 1024 rows
+// 1024x1024 15 in shape 0, then 19, 22, 32).  jt(BJ): tiles along j.  A CU holds
+// (by LDS and registers) 3, 2, 1, 1 blocks of the fp32 shapes and 5, 2, 1, 1 of the
+// 16-bit ones.
+template <typename F, typename J>
+hipError_t with_shape(int64_t ni, J &&jt, F &&f)
 {
-    if (size == 0) return f(std::integral_constant<int, 64>{});
-    if constexpr (sizeof(Elem) == 2)
-        if (size == 2) return f(std::integral_constant<int, 256>{});
-    return f(std::integral_constant<int, 128>{});
+    constexpr int per32[4] = {3, 2, 1, 1}, per16[4] = {5, 2, 1, 1};
+    int best = 0;
+    double least = 0.0;
+    auto cost = [&](auto id) {
+        typedef Shape<id.value> S;
+        const int per = S::k32 ? per32[id.value] : per16[id.value];
+        const int64_t blocks = (ni + S::BI - 1) / S::BI * jt(S::BJ), slots = 256 * per;
+        const double rounds = blocks < slots ? (double)((blocks + 255) / 256) : (double)per * ((blocks + slots - 1) / slots);
+        const double c = rounds * ((double)S::BI * S::BJ + 96.0 * (S::BI + S::BJ));
+        if (id.value == 0 || c < least) {
+            least = c;
+            best = id.value;
+        }
+    };
+    using std::integral_constant;
+    cost(integral_constant<int, 0>{});
+    cost(integral_constant<int, 1>{});
+    cost(integral_constant<int, 2>{});
+    cost(integral_constant<int, 3>{});
+    switch (best) {
+    case 0: return f(integral_constant<int, 0>{});
+    case 1: return f(integral_constant<int, 1>{});
+    case 2: return f(integral_constant<int, 2>{});
+    default: return f(integral_constant<int, 3>{});
+    }
+}
+// Tiles of BJ rows over the networks: ragged ones leave half a tile each, on average.
+auto row_tiles(const NetRows &r)
+{
+    return [&r](int BJ) { return r.off ? r.M / BJ + (r.G + 1) / 2 : r.G * ((r.n + BJ - 1) / BJ); };
 }
 template <typename G, typename K, typename... A>
 hipError_t launch_tiles(K *kernel, int64_t units, hipStream_t s, A... args)
@@ -164,37 +215,36 @@ hipError_t launch_tiles(K *kernel, int64_t units, hipStream_t s, A... args)
 }  // namespace
 
 template <>
-hipError_t launch_linear_tiles<EVOX_NET_TYPE>(const LinearArgs &a, int size, hipStream_t s)
+hipError_t launch_linear_tiles<EVOX_NET_TYPE>(const LinearArgs &a, hipStream_t s)
 {
-    return with_tile(size, [&](auto b) {
-        constexpr int B = b.value;
-        typedef Product<B, false, false> G;
-        const int64_t ti = (a.n_out + B - 1) / B, tj = net_tiles(a.rows, TileShape<B>::sh);
-        return launch_tiles<G>(k_linear_tile<B>, banded(tj) * ti, s, a, ti, tj);
+    return with_shape(a.n_out, row_tiles(a.rows), [&](auto id) {
+        constexpr int ID = id.value, B = Shape<ID>::BI;
+        typedef Product<ID, false, false> G;
+        const int64_t ti = (a.n_out + B - 1) / B, tj = net_tiles(a.rows, Shape<ID>::sh);
+        return launch_tiles<G>(k_linear_tile<ID>, banded(tj) * ti, s, a, ti, tj);
     });
 }
 
 template <>
-hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, int size,
-                                                 hipStream_t s)
+hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, hipStream_t s)
 {
-    return with_tile(size, [&](auto b) {
-        constexpr int B = b.value;
-        typedef Product<B, true, false> G;
-        const int64_t ti = (a.n_in + B - 1) / B, tj = net_tiles(a.rows, TileShape<B>::sh);
-        return launch_tiles<G>(k_linear_dx_tile<B>, banded(tj) * ti, s, a, (const Elem *)d, ldd, ti, tj);
+    return with_shape(a.n_in, row_tiles(a.rows), [&](auto id) {
+        constexpr int ID = id.value, B = Shape<ID>::BI;
+        typedef Product<ID, true, false> G;
+        const int64_t ti = (a.n_in + B - 1) / B, tj = net_tiles(a.rows, Shape<ID>::sh);
+        return launch_tiles<G>(k_linear_dx_tile<ID>, banded(tj) * ti, s, a, (const Elem *)d, ldd, ti, tj);
     });
 }
 
 template <>
-hipError_t launch_linear_dw_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, int size,
-                                                 hipStream_t s)
+hipError_t launch_linear_dw_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, hipStream_t s)
 {
-    return with_tile(size, [&](auto b) {
-        constexpr int B = b.value;
-        typedef Product<B, true, true> G;
-        const int64_t ti = (a.n_in + B - 1) / B, tj = (a.n_out + B - 1) / B;
-        return launch_tiles<G>(k_linear_dw_tile<B>, a.rows.G * banded(tj) * ti, s, a, (const Elem *)d, ldd, ti, tj);
+    const auto out_tiles = [&](int BJ) { return a.rows.G * ((a.n_out + BJ - 1) / BJ); };
+    return with_shape(a.n_in, out_tiles, [&](auto id) {
+        constexpr int ID = id.value, B = Shape<ID>::BI, BJ = Shape<ID>::BJ;
+        typedef Product<ID, true, true> G;
+        const int64_t ti = (a.n_in + B - 1) / B, tj = (a.n_out + BJ - 1) / BJ;
+        return launch_tiles<G>(k_linear_dw_tile<ID>, a.rows.G * banded(tj) * ti, s, a, (const Elem *)d, ldd, ti, tj);
     });
 }
 

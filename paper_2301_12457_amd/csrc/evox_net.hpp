@@ -68,14 +68,14 @@ hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s);
 size_t xent_scratch(const XentArgs &a);
 hipError_t launch_xent(const XentArgs &a, hipStream_t s);
 
-// The large cases: tiles through LDS (one file per element type).  size 0, 1, 2:
-// tiles of 64, 128 or (16 bits) 256 a side.  d: dy act'(z) in the element type.
+// The large cases: tiles through LDS (one file per element type).  d: dy act'(z)
+// in the element type.
 template <int TYPE>
-hipError_t launch_linear_tiles(const LinearArgs &a, int size, hipStream_t s);
+hipError_t launch_linear_tiles(const LinearArgs &a, hipStream_t s);
 template <int TYPE>
-hipError_t launch_linear_dx_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, int size, hipStream_t s);
+hipError_t launch_linear_dx_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, hipStream_t s);
 template <int TYPE>
-hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, int size, hipStream_t s);
+hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, hipStream_t s);
 
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;

@@ -6,7 +6,7 @@
 // so that a lane's four results of a 16 x 16 tile are neighbours.  Either
 // operand is k-contiguous (element (r, k) at r ld + k) or k-major (k ld + r),
 // and is staged as rows of K: a k-major operand is transposed in registers, 8 k
-// by 4 (fp32: 2) rows per thread, on its way to LDS.
+// by 4 rows per thread (fp32: by 1), on its way to LDS.
 //
 // 16 bits: LDS rows of 64 k (128 bytes) in eight 16-byte chunks, chunk c of row
 // r at c ^ f(r), f(r) = (r ^ r / 4) mod 8: the eight lanes that an LDS access
@@ -20,7 +20,7 @@
 // 2^-25 of the term.  Six bf16 products cost 6/16 of an fp32 one.  Sums cannot
 // overflow and no piece is infinite below 2^56; a block that meets a larger
 // number or an infinity computes its tile again with fp32 products
-// (v_mfma_f32_16x16x4f32).  A NaN is one in its own row either way.  A number
+// (v_mfma_f32_32x32x2f32).  A NaN is one in its own row either way.  A number
 // below 2^-100 loses its bits under 2^-126, as fp32 with flushed subnormals does.
 #pragma once
 
@@ -132,7 +132,7 @@ struct Stage16c {
         for (int p = 0; p < P; ++p)
             v[p] = __builtin_bit_cast(u32x4, load_chunk(row[p] + k0, threadIdx.x % 8, (int)(K - k0), (T)0.0f));
     }
-    __device__ __forceinline__ void store_piece(int p, char *lds)
+    __device__ __forceinline__ void store_piece(int p, char *lds, float &)
     {
         *reinterpret_cast<u32x4 *>(lds + chunk16(threadIdx.x / 8 + p * (TH / 8), threadIdx.x % 8)) = v[p];
     }
@@ -140,11 +140,13 @@ struct Stage16c {
 
 template <typename T, int R, int TH>
 struct Stage16m {
-    static constexpr int P = R * 2 / TH, kQuads = R / 4, kLoads = 8 * P, kStores = 4 * P;
+    static constexpr int P = (R * 2 + TH - 1) / TH, kQuads = R / 4, kLoads = 8 * P, kStores = 4 * P;
     u32x2 v[P][8];
     const T *src;
     int64_t ld;
     int n;
+    // threads past the patches repeat the first ones' work
+    static __device__ __forceinline__ int thread() { return R * 2 < TH ? threadIdx.x % (R * 2) : threadIdx.x; }
     __device__ __forceinline__ void init(const T *s, int64_t l, int rows)
     {
         src = s;
@@ -154,14 +156,14 @@ struct Stage16m {
     __device__ __forceinline__ bool whole() const { return n == R; }
     __device__ __forceinline__ void load_piece(int i, int64_t k0)  // and all R rows exist
     {
-        const int p = i / 8, j = i % 8, q = threadIdx.x + p * TH;
+        const int p = i / 8, j = i % 8, q = thread() + p * TH;
         v[p][j] = *reinterpret_cast<const u32x2u *>(src + (k0 + q / kQuads * 8 + j) * ld + q % kQuads * 4);
     }
     __device__ __forceinline__ void load(int64_t k0, int64_t K)
     {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int q = threadIdx.x + p * TH, r = q % kQuads * 4, k = q / kQuads * 8;
+            const int q = thread() + p * TH, r = q % kQuads * 4, k = q / kQuads * 8;
             const T *at = src + (k0 + k) * ld + r;
             if (k0 + k + 8 <= K && r + 4 <= n) {
 #pragma unroll
@@ -177,9 +179,9 @@ struct Stage16m {
             }
         }
     }
-    __device__ __forceinline__ void store_piece(int i, char *lds)
+    __device__ __forceinline__ void store_piece(int i, char *lds, float &)
     {
-        const int p = i / 4, x = i % 4, q = threadIdx.x + p * TH, r = q % kQuads * 4, c = q / kQuads;
+        const int p = i / 4, x = i % 4, q = thread() + p * TH, r = q % kQuads * 4, c = q / kQuads;
         u32x4 t;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -210,88 +212,82 @@ __device__ __forceinline__ void store_pieces(char *lds, int r, int c, const floa
 
 template <int R, int TH>
 struct Stage32c {
-    static constexpr int P = R * 4 / TH;
+    static constexpr int P = (R * 4 + TH - 1) / TH, kStores = P;
     f32x4 v[P][2];
     const float *row[P];
+    // threads past the chunks repeat the first ones' work
+    static __device__ __forceinline__ int thread() { return R * 4 < TH ? threadIdx.x % (R * 4) : threadIdx.x; }
     __device__ __forceinline__ void init(const float *src, int64_t ld, int n)
     {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int r = threadIdx.x / 4 + p * (TH / 4);
+            const int r = thread() / 4 + p * (TH / 4);
             row[p] = src + (int64_t)(r < n ? r : n - 1) * ld;
         }
     }
+    __device__ __forceinline__ bool whole() const { return true; }
+    __device__ __forceinline__ void load_piece(int p, int64_t k0)  // k0 + 32 <= K
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            v[p][h] = *reinterpret_cast<const NetVec<float>::mem *>(row[p] + k0 + 8 * (thread() % 4) + 4 * h);
+    }
     __device__ __forceinline__ void load(int64_t k0, int64_t K)
     {
-        const int c = threadIdx.x % 4;
         if (k0 + 32 <= K) {
 #pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    v[p][h] = *reinterpret_cast<const NetVec<float>::mem *>(row[p] + k0 + 8 * c + 4 * h);
-        } else {
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) v[p][h] = load_chunk(row[p] + k0, 2 * c + h, (int)(K - k0), 0.0f);
+            for (int p = 0; p < P; ++p) load_piece(p, k0);
+            return;
         }
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) v[p][h] = load_chunk(row[p] + k0, 2 * (thread() % 4) + h, (int)(K - k0), 0.0f);
     }
-    __device__ __forceinline__ void store(char *lds, float &big)
+    __device__ __forceinline__ void store_piece(int p, char *lds, float &big)
     {
+        float f[8];
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            float f[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = v[p][j / 4][j % 4];
-            store_pieces<R>(lds, threadIdx.x / 4 + p * (TH / 4), threadIdx.x % 4, f, big);
-        }
+        for (int j = 0; j < 8; ++j) f[j] = v[p][j / 4][j % 4];
+        store_pieces<R>(lds, thread() / 4 + p * (TH / 4), thread() % 4, f, big);
     }
 };
 
+// k-major: 8 k of one row per thread and piece, a wave's loads 256 bytes of a k.
 template <int R, int TH>
 struct Stage32m {
-    static constexpr int P = R * 2 / TH, kPairs = R / 2;
-    f32x2 v[P][8];
+    static constexpr int P = (R * 4 + TH - 1) / TH, kStores = P;
+    float v[P][8];
     const float *src;
     int64_t ld;
     int n;
+    static __device__ __forceinline__ int thread() { return R * 4 < TH ? threadIdx.x % (R * 4) : threadIdx.x; }
     __device__ __forceinline__ void init(const float *s, int64_t l, int rows)
     {
         src = s;
         ld = l;
         n = rows;
     }
+    __device__ __forceinline__ bool whole() const { return n == R; }
+    __device__ __forceinline__ void load_piece(int p, int64_t k0)  // and all R rows exist
+    {
+        const int q = thread() + p * TH;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[p][j] = src[(k0 + q / R * 8 + j) * ld + q % R];
+    }
     __device__ __forceinline__ void load(int64_t k0, int64_t K)
     {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int q = threadIdx.x + p * TH, r = q % kPairs * 2, k = q / kPairs * 8;
-            const float *at = src + (k0 + k) * ld + r;
-            if (k0 + k + 8 <= K && r + 2 <= n) {
+            const int q = thread() + p * TH, r = q % R, k = q / R * 8;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[p][j] = *reinterpret_cast<const f32x2u *>(at + j * ld);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) v[p][j][x] = k0 + k + j < K && r + x < n ? at[j * ld + x] : 0.0f;
-            }
+            for (int j = 0; j < 8; ++j) v[p][j] = k0 + k + j < K && r < n ? src[(k0 + k + j) * ld + r] : 0.0f;
         }
     }
-    __device__ __forceinline__ void store(char *lds, float &big)
+    __device__ __forceinline__ void store_piece(int p, char *lds, float &big)
     {
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int q = threadIdx.x + p * TH, r = q % kPairs * 2, c = q / kPairs;
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                float f[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = v[p][j][x];
-                store_pieces<R>(lds, r + x, c, f, big);
-            }
-        }
+        const int q = thread() + p * TH;
+        store_pieces<R>(lds, q % R, q / R, v[p], big);
     }
 };
 template <int R, int TH>
@@ -312,22 +308,21 @@ struct TileOp {
 };
 
 // The tile's product and its results.  Waves: WI along i by WJ along j, each
-// TI x TJ tiles of S x S (16 bits: 32, which read each operand register half as
-// often as tiles of 16 would, and leave more registers: the gradient of 64x512
+// TI x TJ tiles of 32 x 32 (which read each operand register half as often as
+// tiles of 16 would, and leave more registers: the bf16 gradient of 64x512
 // 1024x1024 312 -> 288 us).
 template <typename T, bool PM, bool QM, int BI, int BJ, int WI, int WJ>
 struct TileProduct {
     static constexpr int kThreads = 64 * WI * WJ, BK = kTileK<T>;
     static constexpr bool kSplit = sizeof(T) == 4;
-    static constexpr int S = kSplit ? 16 : 32, TI = BI / WI / S, TJ = BJ / WJ / S;
-    typedef typename std::conditional<kSplit, f32x4, f32x16>::type Acc;
-    static constexpr int kBuffers = kSplit ? 1 : 2;
+    static constexpr int S = 32, TI = BI / WI / S, TJ = BJ / WJ / S;
+    static constexpr int kBuffers = 2;
     static constexpr int kBuffer = kStageBytes<T, BI> + kStageBytes<T, BJ>;
     static constexpr int kPitch = BI / WI + 4;  // floats per row of a wave's results in LDS, S rows at a time
     static constexpr int kOutBytes = WI * WJ * S * kPitch * 4;
     static constexpr int kLds = kBuffers * kBuffer > kOutBytes ? kBuffers * kBuffer : kOutBytes;
 
-    Acc acc[TI][TJ];
+    f32x16 acc[TI][TJ];
     int wi, wj, row, q;  // the lane's row of a tile and k group
 
     __device__ __forceinline__ TileProduct()
@@ -343,7 +338,7 @@ struct TileProduct {
 #pragma unroll
         for (int i = 0; i < TI; ++i)
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) acc[i][j] = (Acc)(0.0f);
+            for (int j = 0; j < TJ; ++j) acc[i][j] = (f32x16)(0.0f);
     }
 
     // One K tile (64 k) of 16-bit products in 4 TJ slots of TI products: slot k
@@ -353,7 +348,7 @@ struct TileProduct {
     // the compiler reads one operand and waits for it before every TI products,
     // and writes and loads in a burst.
     template <bool kNext, typename SP, typename SQ>
-    __device__ __forceinline__ void compute16(const char *lds, char *next, SP &sp, SQ &sq, int64_t k0)
+    __device__ __forceinline__ void compute16(const char *lds, char *next, SP &sp, SQ &sq, int64_t k0, float &big)
     {
         typedef typename NetVec<T>::reg reg;
         constexpr int kSlots = 4 * TJ, kHalf = 2 * TJ, kW = SP::kStores + SQ::kStores, kV = SP::kLoads + SQ::kLoads;
@@ -380,8 +375,8 @@ struct TileProduct {
                 if (k < kHalf) {
 #pragma unroll
                     for (int w = kW * k / kHalf; w < kW * (k + 1) / kHalf; ++w)
-                        if (w < SP::kStores) sp.store_piece(w, next);
-                        else sq.store_piece(w - SP::kStores, next + kStageBytes<T, BI>);
+                        if (w < SP::kStores) sp.store_piece(w, next, big);
+                        else sq.store_piece(w - SP::kStores, next + kStageBytes<T, BI>, big);
                 } else {
 #pragma unroll
                     for (int v = kV * (k - kHalf) / kHalf; v < kV * (k - kHalf + 1) / kHalf; ++v)
@@ -394,29 +389,71 @@ struct TileProduct {
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    __device__ __forceinline__ void compute32(const char *lds)
+    // The same for a K tile (32 k) of fp32: two halves of 16 k with TJ slots each, a
+    // slot the six products of the pieces for TI tiles.  A share of the next tile is
+    // split, written and its registers loaded again in one slot, its vector
+    // instructions in the shadow of the matrix ones.
+    template <bool kNext, typename SP, typename SQ>
+    __device__ __forceinline__ void compute32(const char *lds, char *next, SP &sp, SQ &sq, int64_t k0, float &big)
     {
         typedef NetVec<bf16_t>::reg reg;
-        reg p[TI][3], s[3];
-#pragma unroll
-        for (int i = 0; i < TI; ++i)
-#pragma unroll
-            for (int u = 0; u < 3; ++u)
-                p[i][u] = *reinterpret_cast<const reg *>(lds + u * 64 * BI + chunk32((wi * TI + i) * 16 + row, q));
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) {
+        constexpr int kSlots = 2 * TJ, kW = SP::kStores + SQ::kStores;
+        reg p[2][TI][3], s[2][3];
+        auto read_p = [&](int h, int i) {
 #pragma unroll
             for (int u = 0; u < 3; ++u)
-                s[u] = *reinterpret_cast<const reg *>(lds + kStageBytes<T, BI> + u * 64 * BJ +
-                                                      chunk32((wj * TJ + j) * 16 + row, q));
+                p[h][i][u] = *reinterpret_cast<const reg *>(lds + u * 64 * BI + chunk32((wi * TI + i) * S + row, 2 * h + q));
+        };
+        auto read_s = [&](int k) {
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+                s[k % 2][u] = *reinterpret_cast<const reg *>(lds + kStageBytes<T, BI> + u * 64 * BJ +
+                                                             chunk32((wj * TJ + k % TJ) * S + row, 2 * (k / TJ) + q));
+        };
+        read_s(0);
+#pragma unroll
+        for (int i = 0; i < TI; ++i) read_p(0, i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kSlots; ++k) {
+            if (k + 1 < kSlots) read_s(k + 1);
+            if (k < TJ)
+#pragma unroll
+                for (int i = TI * k / TJ; i < TI * (k + 1) / TJ; ++i) read_p(1, i);
+            if constexpr (kNext) {
+#pragma unroll
+                for (int w = kW * k / kSlots; w < kW * (k + 1) / kSlots; ++w) {
+                    if (w < SP::kStores) {
+                        sp.store_piece(w, next, big);
+                        sp.load_piece(w, k0);
+                    } else {
+                        sq.store_piece(w - SP::kStores, next + kStageBytes<T, BI>, big);
+                        sq.load_piece(w - SP::kStores, k0);
+                    }
+                }
+            }
             // the small products first
 #pragma unroll
             for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
                 for (int u = 0; u <= sum; ++u)
 #pragma unroll
-                    for (int i = 0; i < TI; ++i) acc[i][j] = mma16(p[i][u], s[sum - u], acc[i][j]);
+                    for (int i = 0; i < TI; ++i)
+                        acc[i][k % TJ] = mma32(p[k / TJ][i][u], s[k % 2][sum - u], acc[i][k % TJ]);
+            if constexpr (kNext)
+#pragma unroll
+                for (int m = 0; m < 6 * TI; ++m) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+                }
+            __builtin_amdgcn_sched_barrier(0);
         }
+    }
+    template <bool kNext, typename SP, typename SQ>
+    __device__ __forceinline__ void compute(const char *lds, char *next, SP &sp, SQ &sq, int64_t k0, float &big)
+    {
+        if constexpr (kSplit) compute32<kNext>(lds, next, sp, sq, k0, big);
+        else compute16<kNext>(lds, next, sp, sq, k0, big);
     }
 
     // With fp32 products, straight from memory.
@@ -429,26 +466,26 @@ struct TileProduct {
             return (float)(major ? o.p[k * o.ld + r] : o.p[(int64_t)r * o.ld + k]);
         };
 #pragma unroll 1
-        for (int64_t k = 0; k < K; k += 4) {
+        for (int64_t k = 0; k < K; k += 2) {
             float p[TI], s[TJ];
 #pragma unroll
-            for (int i = 0; i < TI; ++i) p[i] = at(P, PM, (wi * TI + i) * 16 + row, k + q);
+            for (int i = 0; i < TI; ++i) p[i] = at(P, PM, (wi * TI + i) * S + row, k + q);
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) s[j] = at(Q, QM, (wj * TJ + j) * 16 + row, k + q);
+            for (int j = 0; j < TJ; ++j) s[j] = at(Q, QM, (wj * TJ + j) * S + row, k + q);
 #pragma unroll
             for (int j = 0; j < TJ; ++j)
 #pragma unroll
-                for (int i = 0; i < TI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[i], s[j], acc[i][j], 0, 0, 0);
+                for (int i = 0; i < TI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(p[i], s[j], acc[i][j], 0, 0, 0);
         }
     }
 
     template <typename SP, typename SQ>
-    __device__ __forceinline__ void store_all(char *lds, SP &sp, SQ &sq)
+    __device__ __forceinline__ void store_all(char *lds, SP &sp, SQ &sq, float &big)
     {
 #pragma unroll
-        for (int w = 0; w < SP::kStores; ++w) sp.store_piece(w, lds);
+        for (int w = 0; w < SP::kStores; ++w) sp.store_piece(w, lds, big);
 #pragma unroll
-        for (int w = 0; w < SQ::kStores; ++w) sq.store_piece(w, lds + kStageBytes<T, BI>);
+        for (int w = 0; w < SQ::kStores; ++w) sq.store_piece(w, lds + kStageBytes<T, BI>, big);
     }
 
     // The whole product; ends with all waves past their last use of LDS.
@@ -464,80 +501,75 @@ struct TileProduct {
         const int64_t tiles = (K + BK - 1) / BK;
         sp.load(0, K);
         sq.load(0, K);
-        if constexpr (kSplit) {
-            for (int64_t t = 0; t < tiles; ++t) {
-                if (t) lds_barrier();
-                sp.store(lds, big);
-                sq.store(lds + kStageBytes<T, BI>, big);
-                lds_barrier();
-                if (t + 1 < tiles) {
-                    sp.load((t + 1) * BK, K);
-                    sq.load((t + 1) * BK, K);
-                }
-                compute32(lds);
-            }
-            if (__syncthreads_or(!(big < kTileBig))) again(P, Q, K);
-        } else {
-            store_all(lds, sp, sq);
-            if (tiles > 1) {
-                sp.load(BK, K);
-                sq.load(BK, K);
-            }
-            lds_barrier();
-            int64_t t = 0;
-            // while the tile two ahead is whole
-            if (sp.whole() && sq.whole())
-                for (const int64_t full = K / BK; t + 2 < full; ++t) {
-                    compute16<true>(lds + t % 2 * kBuffer, lds + (t + 1) % 2 * kBuffer, sp, sq, (t + 2) * BK);
-                    lds_barrier();
-                }
-            for (; t < tiles; ++t) {
-                if (t + 1 < tiles) {
-                    store_all(lds + (t + 1) % 2 * kBuffer, sp, sq);
-                    if (t + 2 < tiles) {
-                        sp.load((t + 2) * BK, K);
-                        sq.load((t + 2) * BK, K);
-                    }
-                }
-                compute16<false>(lds + t % 2 * kBuffer, nullptr, sp, sq, 0);
-                lds_barrier();
-            }
+        store_all(lds, sp, sq, big);
+        if (tiles > 1) {
+            sp.load(BK, K);
+            sq.load(BK, K);
         }
+        lds_barrier();
+        int64_t t = 0;
+        // while the tile two ahead is whole
+        if (sp.whole() && sq.whole())
+            for (const int64_t full = K / BK; t + 2 < full; ++t) {
+                compute<true>(lds + t % 2 * kBuffer, lds + (t + 1) % 2 * kBuffer, sp, sq, (t + 2) * BK, big);
+                lds_barrier();
+            }
+        for (; t < tiles; ++t) {
+            if (t + 1 < tiles) {
+                store_all(lds + (t + 1) % 2 * kBuffer, sp, sq, big);
+                if (t + 2 < tiles) {
+                    sp.load((t + 2) * BK, K);
+                    sq.load((t + 2) * BK, K);
+                }
+            }
+            compute<false>(lds + t % 2 * kBuffer, nullptr, sp, sq, 0, big);
+            lds_barrier();
+        }
+        if constexpr (kSplit)
+            if (__syncthreads_or(!(big < kTileBig))) again(P, Q, K);
     }
 
-    // The results, S rows of every wave at a time through LDS (the wave's own
-    // part of it): out(j, i, v, n) gets n <= N neighbours i .. i + n - 1 of row j,
-    // N of them 16 bytes of the element type, a row's in consecutive lanes.
+    // The results, S rows of every wave at a time through LDS (the wave's own part
+    // of it).  A lane gets n <= N neighbours i .. i + n - 1 of a row j at a time (N:
+    // 16 bytes of the element type, a row's in consecutive lanes), always the same
+    // i: out.begin(i, n) loads what belongs to the columns once, out.load(j, i, n)
+    // what belongs to the row (for all of a lane's rows before the first is done, so
+    // that their latencies overlap), out.store(j, i, v, n, loaded) is the result.
     template <typename F>
-    __device__ __forceinline__ void results(int ni, int nj, char *lds, F &&out)
+    __device__ __forceinline__ void results(int ni, int nj, char *lds, F &out)
     {
-        constexpr int N = NetVec<T>::N, kRow = BI / WI, kLanes = kRow / N, kRows = 64 / kLanes;
+        constexpr int N = NetVec<T>::N, kRow = BI / WI, kLanes = kRow / N, kRows = 64 / kLanes, kIter = S / kRows;
         float *mine = reinterpret_cast<float *>(lds) + (wj * WI + wi) * S * kPitch;
-        const int lane = threadIdx.x % 64, c = lane % kLanes * N, i = wi * kRow + c;
+        const int lane = threadIdx.x % 64, c = lane % kLanes * N, i = wi * kRow + c, n = ni - i < N ? ni - i : N;
+        if (n > 0) out.begin(i, n);
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
+            typename NetVec<T>::reg loaded[kIter];
+            const int r0 = (wj * TJ + j) * S + lane / kLanes;
+#pragma unroll
+            for (int it = 0; it < kIter; ++it)
+                if (r0 + it * kRows < nj && n > 0) loaded[it] = out.load(r0 + it * kRows, i, n);
 #pragma unroll
             for (int k = 0; k < TI; ++k)
 #pragma unroll
-                for (int b = 0; b < S * S / 256; ++b) {  // the lane's quads of the tile
+                for (int b = 0; b < 4; ++b) {  // the lane's quads of the tile
                     f32x4 t;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) t[e] = acc[k][j][4 * b + e];
                     *reinterpret_cast<f32x4 *>(mine + row * kPitch + k * S + 8 * b + 4 * q) = t;
                 }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 1
-            for (int r = lane / kLanes; r < S; r += kRows) {
-                const int rj = (wj * TJ + j) * S + r;
-                if (rj >= nj || i >= ni) continue;
+#pragma unroll
+            for (int it = 0; it < kIter; ++it) {
+                if (r0 + it * kRows >= nj || n <= 0) continue;
                 float v[N];
 #pragma unroll
                 for (int e = 0; e < N; e += 4) {
-                    const f32x4 t = *reinterpret_cast<const f32x4 *>(mine + r * kPitch + c + e);
+                    const f32x4 t = *reinterpret_cast<const f32x4 *>(mine + (lane / kLanes + it * kRows) * kPitch + c + e);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) v[e + x] = t[x];
                 }
-                out(rj, i, v, ni - i < N ? ni - i : N);
+                out.store(r0 + it * kRows, i, v, n, loaded[it]);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
