@@ -524,7 +524,8 @@ int evox_profile_read(evox_state *state, double *fused_ms, int64_t *fused_launch
  *
  * All operands of a call have one element type, sums are in fp32 (fp64 for the
  * fitness) and each result is rounded once.  Pointers and pitches need no more
- * than the element's own alignment; all offsets are 64 bits.  Outputs must not
+ * than the element's own alignment; row pitches are below 2^31 elements, strides
+ * below 2^40, and all offsets 64 bits.  Outputs must not
  * overlap inputs, but for y = r (equal pitch) and dx = dy of the norm.  The
  * calls read no device memory on the host, allocate nothing, can be captured
  * in a graph, and give the same bits on every run.

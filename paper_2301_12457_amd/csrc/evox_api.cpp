@@ -535,11 +535,11 @@ bool element_aligned(int32_t dtype, std::initializer_list<const void *> ptrs)
     return true;
 }
 
-// Pitches and strides stay below 2^40 elements and the last element of `rows`
-// rows (`nets` networks) within 2^46, so no offset overflows.
+// Row pitches stay below 2^31 elements, strides below 2^40, and the last element
+// of `rows` rows (`nets` networks) within 2^46, so no offset overflows.
 bool pitch_ok(int64_t pitch, int64_t n, int64_t rows)
 {
-    return pitch >= n && pitch < ((int64_t)1 << 40) && rows <= ((int64_t)1 << 46) / pitch;
+    return pitch >= n && pitch <= INT32_MAX && rows <= ((int64_t)1 << 46) / pitch;
 }
 bool stride_ok(int64_t stride, int64_t extent, int64_t nets)
 {

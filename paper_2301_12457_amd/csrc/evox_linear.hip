@@ -35,50 +35,34 @@ struct Mma {
     typedef typename NetVec<T>::reg reg;
     static constexpr int KV = NetVec<T>::N, KS = 4 * KV;  // k per lane, per step
 };
-// The epilogue of four neighbouring outputs o .. o + 3 of row m: bias,
-// pre-activation, activation, residual, one rounding each.
+// Up to four neighbours p[0 .. n), zeros after them.
 template <typename T>
-__device__ __forceinline__ void linear_out(const LinearArgs &a, int g, int64_t m, int o, f32x4 v)
+__device__ __forceinline__ f32x4 load_quad(const T *p, int n)
 {
-    typedef typename Quad<T>::mem quad;
-    const int n = (int)a.n_out;
-    if (o >= n) return;
-    const T *b = a.b ? (const T *)a.b + g * a.b_stride + o : nullptr;
-    const T *r = a.r ? (const T *)a.r + m * a.ldr + o : nullptr;
-    T *z = a.z ? (T *)a.z + m * a.ldz + o : nullptr, *y = (T *)a.y + m * a.ldy + o;
-    if (o + 4 <= n) {
-        quad t;
-        if (b) {
-            t = *reinterpret_cast<const quad *>(b);
+    f32x4 v = (f32x4)(0.0f);
+    if (n >= 4) {
+        const typename Quad<T>::mem t = *reinterpret_cast<const typename Quad<T>::mem *>(p);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += (float)t[j];
-        }
-        if (z) {
+        for (int j = 0; j < 4; ++j) v[j] = (float)t[j];
+    } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) t[j] = (T)v[j];
-            *reinterpret_cast<quad *>(z) = t;
-        }
-        float f[4] = {v[0], v[1], v[2], v[3]};
-        act_values<sizeof(T) == 2, 4>(a.act, f);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = f[j];
-        if (r) {
-            t = *reinterpret_cast<const quad *>(r);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] += (float)t[j];
-        }
+        for (int j = 0; j < 3; ++j)
+            if (j < n) v[j] = (float)p[j];
+    }
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_quad(T *p, int n, f32x4 v)
+{
+    if (n >= 4) {
+        typename Quad<T>::mem t;
 #pragma unroll
         for (int j = 0; j < 4; ++j) t[j] = (T)v[j];
-        *reinterpret_cast<quad *>(y) = t;
-        return;
-    }
+        *reinterpret_cast<typename Quad<T>::mem *>(p) = t;
+    } else {
 #pragma unroll
-    for (int j = 0; j < 3; ++j) {
-        if (o + j >= n) continue;
-        float s = v[j] + (b ? (float)b[j] : 0.0f);
-        if (z) z[j] = (T)s;
-        s = act_value<sizeof(T) == 2>(a.act, s);
-        y[j] = (T)(s + (r ? (float)r[j] : 0.0f));
+        for (int j = 0; j < 3; ++j)
+            if (j < n) p[j] = (T)v[j];
     }
 }
 
@@ -109,17 +93,26 @@ __global__ __launch_bounds__(256) void k_linear_thin(LinearArgs a, int sh, uint3
     for (int r = 0; r < RB; ++r)
 #pragma unroll
         for (int n = 0; n < NB; ++n) acc[r][n] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 bias[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int o = o0 + n * 16 + 4 * q;
+        bias[n] = t.g >= 0 && a.b && wk == 0 ? load_quad((const T *)a.b + t.g * a.b_stride + o, (int)a.n_out - o) : (f32x4)(0.0f);
+    }
     if (t.g >= 0) {
         const int K = (int)a.n_in, steps = (K + KS - 1) / KS, per = (steps + WK - 1) / WK, s1 = min(steps, (wk + 1) * per),
                   full = min(s1, K / KS);
         const int64_t x0 = a.x_shared ? (int64_t)t.g * a.rows.n : 0;
-        const T *xr[RB], *wr[NB];
+        // (row pitches are below 2^31: one multiply-add per address)
+        const T *xr[RB], *wr[NB], *xb = (const T *)a.x + (t.lo - x0) * a.ldx + q * KV,
+                                  *wb = (const T *)a.w + t.g * a.w_stride + o0 * a.ldw + q * KV;
+        const int rows = (int)(t.hi - t.lo), outs = (int)a.n_out - o0;
 #pragma unroll
         for (int r = 0; r < RB; ++r)
-            xr[r] = (const T *)a.x + (min(t.lo + r * 16 + l16, t.hi - 1) - x0) * a.ldx + q * KV;
+            xr[r] = xb + (int64_t)min(r * 16 + l16, rows - 1) * (int)a.ldx;
 #pragma unroll
         for (int n = 0; n < NB; ++n)
-            wr[n] = (const T *)a.w + t.g * a.w_stride + min((int64_t)o0 + n * 16 + l16, a.n_out - 1) * a.ldw + q * KV;
+            wr[n] = wb + (int64_t)min(n * 16 + l16, outs - 1) * (int)a.ldw;
         typedef typename NetVec<T>::mem mem;
         auto steps_of = [&](int s, auto count) {
             constexpr int C = decltype(count)::value;
@@ -172,12 +165,36 @@ __global__ __launch_bounds__(256) void k_linear_thin(LinearArgs a, int sh, uint3
                 for (int n = 0; n < NB; ++n) acc[r][n] += part[(((wt * (WK - 1) + k - 1) * RB + r) * NB + n) * 64 + lane];
     }
     if (t.g < 0) return;
+    // a lane's rows l16, l16 + 16, ... of the tile, its outputs o0 + 4 q, + 16, ...
+    const int rows = (int)(t.hi - t.lo) - l16, outs = (int)a.n_out - o0 - 4 * q;
+    T *y = (T *)a.y + t.lo * a.ldy + o0 + (int64_t)l16 * (int)a.ldy + 4 * q;
+    T *z = a.z ? (T *)a.z + t.lo * a.ldz + o0 + (int64_t)l16 * (int)a.ldz + 4 * q : nullptr;
+    // the residual's loads all before the first store (which may take its place)
+    f32x4 res[RB][NB];
+    if (a.r) {
+        const T *from = (const T *)a.r + t.lo * a.ldr + o0 + (int64_t)l16 * (int)a.ldr + 4 * q;
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+                if (r * 16 < rows) res[r][n] = load_quad(from + r * 16 * a.ldr + n * 16, outs - n * 16);
+    }
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-        const int64_t m = t.lo + r * 16 + l16;
-        if (m < t.hi)
+        if (r * 16 >= rows) continue;
 #pragma unroll
-            for (int n = 0; n < NB; ++n) linear_out<T>(a, t.g, m, o0 + n * 16 + 4 * q, acc[r][n]);
+        for (int n = 0; n < NB; ++n) {
+            if (outs <= n * 16) continue;
+            f32x4 v = acc[r][n] + bias[n];
+            if (z) store_quad(z + r * 16 * a.ldz + n * 16, outs - n * 16, v);
+            if (a.act != ACT_NONE) {
+                float f[4] = {v[0], v[1], v[2], v[3]};
+                act_values<sizeof(T) == 2, 4>(a.act, f);
+                v = (f32x4){f[0], f[1], f[2], f[3]};
+            }
+            if (a.r) v += res[r][n];
+            store_quad(y + r * 16 * a.ldy + n * 16, outs - n * 16, v);
+        }
     }
 }
 
@@ -271,10 +288,10 @@ struct GradSums {
 // ---------------------------------------------------------------------------
 constexpr int kNarrow = 64;
 
-template <typename T, int WAVES>
+template <typename T, int WAVES, int F>
 __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGradArgs a, int sh, float *part)
 {
-    constexpr int N = NetVec<T>::N, TH = 64 * WAVES, R = 16 * WAVES, kDw = 16 / WAVES;
+    constexpr int N = NetVec<T>::N, TH = 64 * WAVES, R = 16 * WAVES * F, kDw = F > 1 ? 1 : 16 / WAVES;
     typedef typename NetVec<T>::reg reg;
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const NetTile t = net_tile(a.rows, sh, net_block());
@@ -288,7 +305,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
 #pragma unroll
         for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4 *>(row + c * N + j) = (f32x4){(float)v[j], (float)v[j + 1], (float)v[j + 2], (float)v[j + 3]};
     };
-    const int ci = ti * 16 / N, co = to * 16 / N;  // chunks per padded row
+    const int ci = ti * 16 / N, co = to * 16 / N, shares = TH / (to * 16);  // chunks per padded row; threads per column
     if (a.dx) {
         const T *w = (const T *)a.w + t.g * a.w_stride;
 #pragma unroll 2
@@ -336,9 +353,10 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
                 put(X + r * pi, c, m0 + r < t.hi ? load_chunk((const T *)a.x + (m0 + r - x0) * a.ldx, c, ni, (T)0.0f) : (reg){});
             }
         __syncthreads();
-        if (a.dx) {
-            const int64_t m = m0 + wave * 16 + l16;
-            const float *d = D + (wave * 16 + l16) * po;
+        if (a.dx)
+            for (int f = 0; f < F; ++f) {
+            const int64_t m = m0 + (wave * F + f) * 16 + l16;
+            const float *d = D + ((wave * F + f) * 16 + l16) * po;
             for (int i = 0; i < ti; ++i) {
                 f32x4 acc = (f32x4)(0.0f);
                 for (int k = 0; k < to; ++k) {
@@ -366,11 +384,11 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
         if (a.dw)
 #pragma unroll
             for (int s = 0; s < kDw; ++s) {
-                const int u = wave + s * WAVES;
+                const int u = F > 1 ? 0 : wave + s * WAVES;
                 if (u >= ti * to) continue;
-                const int o = u / ti, i = u - o * ti;
+                const int o = u / ti, i = u - o * ti, k0 = F > 1 ? wave * 16 * F : 0;
 #pragma unroll 1
-                for (int k = 0; k < R; k += 16) {
+                for (int k = k0; k < k0 + (F > 1 ? 16 * F : R); k += 16) {
                     f32x4 p, d;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -380,10 +398,22 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
                     dw[s] = mma16(p, d, dw[s]);
                 }
             }
-        if (tid < no) {
+        // db: a column per thread, the rows shared by the threads left over
+        if (tid < shares * to * 16) {
 #pragma unroll 4
-            for (int r = 0; r < R; ++r) db += D[r * po + tid];
+            for (int r = tid / (to * 16); r < R; r += shares) db += D[r * po + tid % (to * 16)];
         }
+    }
+    __syncthreads();
+    float *const join = X;  // [TH] db, then (F > 1) [WAVES][64] of the dw tile's quads
+    join[tid] = db;
+    if constexpr (F > 1) *reinterpret_cast<f32x4 *>(join + TH + 4 * tid) = dw[0];
+    __syncthreads();
+    for (int s = 1; tid < no && s < shares; ++s) db += join[s * to * 16 + tid];
+    if constexpr (F > 1) {
+        if (wave == 0)
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) dw[0] += *reinterpret_cast<const f32x4 *>(join + TH + 4 * (w * 64 + tid));
     }
     // the results, or this tile's sums
     float *sums = part + net_slot(t.lo, t.index, sh) * no * (ni + 1);
@@ -391,7 +421,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
 #pragma unroll
         for (int s = 0; s < kDw; ++s) {
             const int u = wave + s * WAVES;
-            if (u >= ti * to) continue;
+            if (u >= ti * to) continue;  // (F > 1: wave 0 alone)
             const int o = u / ti * 16 + l16, i = (u - u / ti * ti) * 16 + 4 * q;
             if (o < no)
 #pragma unroll
@@ -416,6 +446,93 @@ int narrow_shift(const LinearGradArgs &a)
     return sh;
 }
 bool narrow(const LinearGradArgs &a) { return a.n_in <= kNarrow && a.n_out <= kNarrow; }
+
+// ---------------------------------------------------------------------------
+// Gradient products of a short sum: dx of few outputs (DW = false: rows m of a
+// tile, k the outputs) and dw of few rows per network (rows o, k the network's
+// rows).  Either is out[r][c] = sum_k p[k][c] q(r, k) with p and the result dense
+// along c, so the matrix cores' tiles would be mostly padding and the bytes bound
+// it: a thread takes four rows by one chunk of 16 bytes of columns, the block 16
+// rows (a tile's, or outputs) by L chunks.  For sums of at most 8 outputs or 4
+// rows over at least 64 columns: the whole gradient of 1566 networks' 2 rows
+// 304x1 takes 25 us, 101 in tiles; of 100,000 rows 1000x16 (bf16) 163, in tiles 143.
+// ---------------------------------------------------------------------------
+constexpr int kShortRows = 16, kShortShift = 4, kShortOutputs = 8, kShortMean = 4;
+
+template <typename T, bool DW>
+__global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T *d, int64_t ldd, int L, int64_t units)
+{
+    constexpr int N = NetVec<T>::N;
+    typedef typename NetVec<T>::reg reg;
+    const int64_t cols = (a.n_in + L * N - 1) / (L * N), unit = net_block() / cols;
+    const int lane = threadIdx.x & (L - 1), slot = threadIdx.x / L, slots = 256 / L, ni = (int)a.n_in,
+              c = (int)(net_block() - unit * cols) * L + lane;
+    if (unit >= units) return;
+    int g, R;
+    int64_t K;
+    const T *p, *q;
+    T *out;
+    int64_t ldp, ldo;
+    if constexpr (DW) {
+        const int64_t tiles = (a.n_out + kShortRows - 1) / kShortRows;
+        g = (int)(unit / tiles);
+        const int o0 = (int)(unit - g * tiles) * kShortRows;
+        int64_t lo, hi;
+        net_rows(a.rows, g, &lo, &hi);
+        R = min((int)a.n_out - o0, kShortRows);
+        K = hi - lo;
+        p = (const T *)a.x + (a.x_shared ? 0 : lo) * a.ldx;
+        ldp = a.ldx;
+        q = d + lo * ldd + o0;
+        out = (T *)a.dw + g * a.dw_stride + o0 * a.lddw;
+        ldo = a.lddw;
+    } else {
+        const NetTile t = net_tile(a.rows, kShortShift, unit);
+        if (t.g < 0) return;
+        R = (int)(t.hi - t.lo);
+        K = a.n_out;
+        p = (const T *)a.w + t.g * a.w_stride;
+        ldp = a.ldw;
+        q = d + t.lo * ldd;
+        out = (T *)a.dx + t.lo * a.lddx;
+        ldo = a.lddx;
+    }
+    if (c * N >= ni) return;
+    for (int r0 = slot * 4; r0 < R; r0 += slots * 4) {
+        float acc[4][N];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[r][j] = 0.0f;
+        const int rows = R - r0;
+        // four k at a time (zeros past the last)
+        for (int64_t k = 0; k < K; k += 4) {
+            const int left = K - k < 4 ? (int)(K - k) : 4;
+            reg pv[4];
+            f32x4 qv[4];  // DW: [k] over rows, else [row] over k
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pv[e] = e < left ? load_chunk(p + (k + e) * ldp, c, ni, (T)0.0f) : (reg){};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if constexpr (DW) qv[e] = e < left ? load_quad(q + (k + e) * ldd + r0, rows) : (f32x4)(0.0f);
+                else qv[e] = e < rows ? load_quad(q + (r0 + e) * ldd + k, left) : (f32x4)(0.0f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[r][j] = fmaf(DW ? qv[e][r] : qv[r][e], (float)pv[e][j], acc[r][j]);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (r >= rows) continue;
+            reg v;
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = (T)acc[r][j];
+            store_chunk(out + (r0 + r) * ldo, c, ni, v);
+        }
+    }
+}
 
 // The scratch: d, then the tiles' column sums; of narrow layers, the tiles' sums.
 struct GradScratch {
@@ -447,7 +564,8 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
         if (mean > 32 && a.n_out > 32 && a.n_in >= 64)
             return launch_linear_tiles<t.value>(a, s);
         // rows of a wave's tile by the mean rows per network
-        const int rb = mean <= 16 ? 1 : mean <= 32 ? 2 : 4, sh = rb == 1 ? 4 : rb == 2 ? 5 : 6, nb = rb == 1 ? 1 : 2;
+        const bool few_steps = a.n_in <= 2 * Mma<T>::KS && (sizeof(T) == 2 || a.n_out <= 16);
+        const int rb = mean <= 16 ? 1 : mean <= 32 || few_steps ? 2 : 4, sh = rb == 1 ? 4 : rb == 2 ? 5 : 6, nb = rb == 1 || a.n_out <= 16 ? 1 : 2;
         const uint32_t out_tiles = (uint32_t)((a.n_out + 16 * nb - 1) / (16 * nb));
         const int64_t units = net_tiles(a.rows, sh) * out_tiles;
         const int64_t steps = (a.n_in + Mma<T>::KS - 1) / Mma<T>::KS;
@@ -463,7 +581,9 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
         };
         using std::integral_constant;
         if (rb == 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+        else if (rb == 2 && nb == 1) go(integral_constant<int, 2>{}, integral_constant<int, 1>{});
         else if (rb == 2) go(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+        else if (nb == 1) go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
         else go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
         return hipGetLastError();
     });
@@ -482,15 +602,20 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         if (narrow(a)) {
             const int sh = narrow_shift(a);
             float *part = (float *)a.scratch;
-            auto go = [&](auto waves) {
+            auto go = [&](auto waves, auto f) {
                 const int64_t ti = (a.n_in + 15) / 16 * 16, to = (a.n_out + 15) / 16 * 16;
-                const size_t lds = sizeof(float) * ((a.dx ? to * (ti + 4) : 0) + 16 * waves.value * (ti + 4 + to + 4));
-                hipLaunchKernelGGL((k_linear_grad_narrow<T, waves.value>), net_grid(net_tiles(a.rows, sh)),
+                const size_t lds = sizeof(float) * ((a.dx ? to * (ti + 4) : 0) + 16 * waves.value * f.value * (ti + 4 + to + 4));
+                hipLaunchKernelGGL((k_linear_grad_narrow<T, waves.value, f.value>), net_grid(net_tiles(a.rows, sh)),
                                    dim3(64 * waves.value), lds, s, a, sh, part);
                 return hipGetLastError();
             };
             if (a.rows.M > 0)
-                e = mean <= 32 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
+            {
+                using std::integral_constant;
+                if (mean <= 32) e = go(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+                else if (mean > 128 && a.n_in <= 16 && a.n_out <= 16) e = go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+                else e = go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+            }
             if (e != hipSuccess || (!a.dw && !a.db) || (a.rows.M > 0 && !a.rows.off && net_single(a.rows, sh))) return e;
             return launch_net_sums(a.rows, part, a.n_out * (a.n_in + 1), sh, s,
                                    GradSums<T>{(T *)a.dw, (T *)a.db, a.n_out, a.n_in, a.lddw, a.dw_stride, a.db_stride});
@@ -499,11 +624,11 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         T *d = own ? (T *)a.scratch : nullptr;
         float *sums = a.db ? (float *)((char *)a.scratch + l.sums) : nullptr;
         if (a.rows.M > 0 && (d || sums)) {
-            int L = 4;
-            while (L < 256 && L * N < a.n_out) L *= 2;
-            const int64_t cols = (a.n_out + 256 * N - 1) / (256 * N);
-            hipLaunchKernelGGL((k_linear_dz<T>), net_grid(net_tiles(a.rows, kDzShift) * cols), dim3(256),
-                               sizeof(float) * N * (256 - L), s, a, L, d, l.ldd, sums);
+            int Lz = 4;
+            while (Lz < 256 && Lz * N < a.n_out) Lz *= 2;
+            const int64_t cz = (a.n_out + 256 * N - 1) / (256 * N);
+            hipLaunchKernelGGL((k_linear_dz<T>), net_grid(net_tiles(a.rows, kDzShift) * cz), dim3(256),
+                               sizeof(float) * N * (256 - Lz), s, a, Lz, d, l.ldd, sums);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
         if (a.db && !(a.rows.M > 0 && !a.rows.off && net_single(a.rows, kDzShift))) {
@@ -513,9 +638,26 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         }
         const void *dd = own ? d : a.dy;
         const int64_t ldd = own ? l.ldd : a.lddy;
-        if (a.dx) e = launch_linear_dx_tiles<t.value>(a, dd, ldd, s);
-        if (e == hipSuccess && a.dw) e = launch_linear_dw_tiles<t.value>(a, dd, ldd, s);
-        return e;
+        // short sums: of few outputs (dx) or rows (dw); else tiles
+        int L = 1;
+        while (L < 256 && L * N < a.n_in) L *= 2;
+        const int64_t cols = (a.n_in + L * N - 1) / (L * N);
+        if (a.dx && a.n_out <= kShortOutputs && a.n_in >= 64) {
+            const int64_t units = net_tiles(a.rows, kShortShift);
+            hipLaunchKernelGGL((k_linear_short<T, false>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, ldd,
+                               L, units);
+            e = hipGetLastError();
+        } else if (a.dx) {
+            e = launch_linear_dx_tiles<t.value>(a, dd, ldd, s);
+        }
+        if (e != hipSuccess || !a.dw) return e;
+        if (mean <= kShortMean && a.n_in >= 64) {
+            const int64_t units = a.rows.G * ((a.n_out + kShortRows - 1) / kShortRows);
+            hipLaunchKernelGGL((k_linear_short<T, true>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, ldd,
+                               L, units);
+            return hipGetLastError();
+        }
+        return launch_linear_dw_tiles<t.value>(a, dd, ldd, s);
     });
 }
 

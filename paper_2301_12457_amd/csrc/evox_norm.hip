@@ -2,7 +2,7 @@
 //
 // All four kernels are bound by memory: they read every row once, keep it in
 // registers, and write their results once.  A row lies over L lanes (a power
-// of two, 4 .. 64, or a block of 256 .. 1024 threads), each with NIT chunks of
+// of two, 1 .. 64, or a block of 256 .. 1024 threads), each with NIT chunks of
 // 16 bytes; row sums are butterflies over the L lanes (and LDS across waves)
 // in fp32.
 #include "evox_net.hpp"
@@ -11,15 +11,15 @@ namespace evox {
 
 namespace {
 
-// Lanes per row and chunks per lane for n elements in chunks of N: two chunks
-// per lane up to a wave per row, then up to four (eight at 1024 threads).
+// Lanes per row and chunks per lane for n elements in chunks of N: `per` chunks
+// per lane up to a wave per row (`least` lanes at least), then up to four (eight at 1024 threads).
 struct RowShape {
     int L, nit, threads;
 };
-RowShape row_shape(int64_t n, int N, int per)
+RowShape row_shape(int64_t n, int N, int per, int least)
 {
     const int64_t chunks = (n + N - 1) / N;
-    RowShape s{4, 1, 256};
+    RowShape s{least, 1, 256};
     while (s.L < 64 && chunks > per * s.L) s.L *= 2;
     while (s.L >= 64 && s.L < 1024 && chunks > 4 * s.L) s.L = s.L == 64 ? 256 : 2 * s.L;
     while (chunks > (int64_t)s.nit * s.L) s.nit *= 2;
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
 // ---------------------------------------------------------------------------
 // Its gradient.  A block takes a tile of one network's rows: every lane keeps
 // the sums of dy h and dy of its own columns over the rows it meets, the row
-// slots of the block add theirs in order; k_net_sums adds a network's tiles.
+// slots of the block add theirs in a fixed order; k_net_sums adds a network's tiles.
 // Rows whose chunks and sums do not fit the registers together (fp32, eight
 // chunks per lane) are read a second time.
 // ---------------------------------------------------------------------------
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a
 {
     constexpr int N = NetVec<T>::N;
     constexpr bool kHold = NIT * (8 + 2 * N) <= 96;
-    extern __shared__ float sums[];  // [256 / L - 1 row slots][2][NIT][N][L] (narrow rows)
+    extern __shared__ float sums[];  // [3 waves][2][NIT][N][L] (narrow rows)
     __shared__ float2 lds[16];
     const NetTile t = net_tile(a.rows, sh, net_block());
     if (t.g < 0) return;
@@ -236,17 +236,28 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a
     }
     if (!a.dgamma) return;
     if constexpr (!WIDE) {
-        if (slot > 0)
+        // over the slots of a wave in registers, then the waves in order
+        for (int o = L; o < 64; o *= 2)
 #pragma unroll
             for (int i = 0; i < NIT; ++i)
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    sums[((((slot - 1) * 2 + 0) * NIT + i) * N + j) * L + lane] = sg[i][j];
-                    sums[((((slot - 1) * 2 + 1) * NIT + i) * N + j) * L + lane] = sb[i][j];
+                    sg[i][j] += __shfl_xor(sg[i][j], o);
+                    sb[i][j] += __shfl_xor(sb[i][j], o);
+                }
+        const int wave = threadIdx.x / 64, wl = threadIdx.x % 64;
+        if (wave > 0 && wl < L)
+#pragma unroll
+            for (int i = 0; i < NIT; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    sums[((((wave - 1) * 2 + 0) * NIT + i) * N + j) * L + lane] = sg[i][j];
+                    sums[((((wave - 1) * 2 + 1) * NIT + i) * N + j) * L + lane] = sb[i][j];
                 }
         __syncthreads();
-        if (slot > 0) return;
-        for (int r = 0; r < slots - 1; ++r)
+        if (threadIdx.x >= L) return;
+#pragma unroll
+        for (int r = 0; r < 3; ++r)
 #pragma unroll
             for (int i = 0; i < NIT; ++i)
 #pragma unroll
@@ -296,8 +307,9 @@ struct NormSums {
 // about four blocks per CU.
 int norm_tile_shift(const NormArgs &a)
 {
+    const int least = a.D > 2048 ? 0 : 3;  // rows over a block or waves: few of them fill neither registers nor chip
     int sh = 6;
-    while (sh > 3 && (a.rows.M >> sh) < 512) --sh;
+    while (sh > least && (a.rows.M >> sh) < 512) --sh;
     return sh;
 }
 
@@ -536,7 +548,7 @@ hipError_t launch_layernorm(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N, 4);
+        const RowShape r = row_shape(a.D, NetVec<T>::N, 4, 1);
         const int64_t per = r.L <= 64 ? 256 / r.L : 1;
         return with_shape<T>(r, [&](auto nit, auto wide) {
             hipLaunchKernelGGL((k_layernorm<T, nit.v, wide.v>), net_grid((a.rows.M + per - 1) / per),
@@ -554,13 +566,13 @@ hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N, 2);
+        const RowShape r = row_shape(a.D, NetVec<T>::N, 2, 4);
         const int sh = norm_tile_shift(a);
         const int64_t tiles = net_tiles(a.rows, sh);
         hipError_t e = hipSuccess;
         if (a.rows.M > 0)
             e = with_shape<T>(r, [&](auto nit, auto wide) {
-                const size_t lds = wide.v ? 0 : sizeof(float) * 2 * nit.v * NetVec<T>::N * (256 - r.L);
+                const size_t lds = wide.v ? 0 : sizeof(float) * 2 * nit.v * NetVec<T>::N * 3 * r.L;
                 hipLaunchKernelGGL((k_layernorm_grad<T, nit.v, wide.v>), net_grid(tiles), dim3(r.threads), lds, s,
                                    a, r.L, sh);
             });
@@ -580,7 +592,7 @@ hipError_t launch_xent(const XentArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.C, NetVec<T>::N, 2);
+        const RowShape r = row_shape(a.C, NetVec<T>::N, 2, 1);
         const bool whole = xent_whole(a);
         const int sh = xent_tile_shift(a);
         if (a.dz && !whole)
