@@ -534,10 +534,47 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
     }
 }
 
-// The scratch: d, then the tiles' column sums; of narrow layers, the tiles' sums.
+// dx and dw of so few tiles that most CUs would idle through a long K: its shares
+// are summed by blocks of their own, into fp32 partial results that are then added
+// in order.  Decided by the sizes alone (the scratch is sized by them), for tiles
+// of 64 a side.
+int grad_splits(int64_t tiles, int64_t K)
+{
+    int64_t s = 512 / (tiles < 1 ? 1 : tiles);
+    if (s > K / 256) s = K / 256;
+    return s < 2 ? 1 : s > 16 ? 16 : (int)s;
+}
+int dx_splits(const LinearGradArgs &a)
+{
+    const int64_t rows = (a.rows.M + 63) / 64;
+    return grad_splits((a.n_in + 63) / 64 * (rows > a.rows.G ? rows : a.rows.G), a.n_out);
+}
+int dw_splits(const LinearGradArgs &a)
+{
+    return grad_splits(a.rows.G * ((a.n_in + 63) / 64) * ((a.n_out + 63) / 64), (a.rows.M + a.rows.G - 1) / a.rows.G);
+}
+
+// out[r][c] = sum over the splits, of `rows` rows of n at part[z][r][c]; row r is at
+// (r / per) stride + (r % per) ld of the result.  Rows of no network stay.
+template <typename T>
+__global__ __launch_bounds__(256) void k_linear_join(NetRows rows, const float *part, int splits, int64_t count, int64_t n,
+                                                     T *out, int64_t per, int64_t stride, int64_t ld, bool by_row)
+{
+    const int64_t total = count * n;
+    for (int64_t e = net_block() * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * gridDim.y * 256) {
+        const int64_t r = e / n, c = e - r * n;
+        if (by_row && rows.off && net_of_row(rows, r) < 0) continue;
+        float s = part[e];
+        for (int z = 1; z < splits; ++z) s += part[z * total + e];
+        out[r / per * stride + r % per * ld + c] = (T)s;
+    }
+}
+
+// The scratch: d, then the tiles' column sums, then the partial products; of narrow
+// layers, the tiles' sums.
 struct GradScratch {
     int64_t ldd = 0;
-    size_t sums = 0, end = 0;
+    size_t sums = 0, part = 0, end = 0;
 };
 GradScratch grad_layout(const LinearGradArgs &a)
 {
@@ -550,7 +587,10 @@ GradScratch grad_layout(const LinearGradArgs &a)
     const size_t e = a.dtype == NET_F32 ? 4 : 2;
     g.ldd = (a.n_out + 7) / 8 * 8;
     g.sums = (e * (size_t)a.rows.M * (size_t)g.ldd + 255) / 256 * 256;
-    g.end = g.sums + 4 * (size_t)net_slots(a.rows.M, kDzShift) * (size_t)a.n_out;
+    g.part = (g.sums + 4 * (size_t)net_slots(a.rows.M, kDzShift) * (size_t)a.n_out + 255) / 256 * 256;
+    const size_t dx = dx_splits(a) > 1 ? (size_t)dx_splits(a) * (size_t)a.rows.M * (size_t)a.n_in : 0;
+    const size_t dw = dw_splits(a) > 1 ? (size_t)dw_splits(a) * (size_t)(a.rows.G * a.n_out) * (size_t)a.n_in : 0;
+    g.end = g.part + 4 * (dx > dw ? dx : dw);
     return g;
 }
 
@@ -563,12 +603,19 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
         const int64_t mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
         if (mean > 32 && a.n_out > 32 && a.n_in >= 64)
             return launch_linear_tiles<t.value>(a, s);
-        // rows of a wave's tile by the mean rows per network
+        // rows of a wave's tile by the mean rows per network (few k steps of 16 bits or
+        // outputs: smaller tiles, more waves at a time); one 16 x 16 tile where
+        // larger ones would leave most of the chip without a wave
         const bool few_steps = a.n_in <= 2 * Mma<T>::KS && (sizeof(T) == 2 || a.n_out <= 16);
-        const int rb = mean <= 16 ? 1 : mean <= 32 || few_steps ? 2 : 4, sh = rb == 1 ? 4 : rb == 2 ? 5 : 6, nb = rb == 1 || a.n_out <= 16 ? 1 : 2;
-        const uint32_t out_tiles = (uint32_t)((a.n_out + 16 * nb - 1) / (16 * nb));
-        const int64_t units = net_tiles(a.rows, sh) * out_tiles;
+        int rb = mean <= 16 ? 1 : mean <= 32 || few_steps ? 2 : 4, nb = rb == 1 || a.n_out <= 16 ? 1 : 2;
         const int64_t steps = (a.n_in + Mma<T>::KS - 1) / Mma<T>::KS;
+        const auto units_of = [&](int r, int n) {
+            return net_tiles(a.rows, r == 1 ? 4 : r == 2 ? 5 : 6) * ((a.n_out + 16 * n - 1) / (16 * n));
+        };
+        if (steps >= 16 && units_of(rb, nb) < 512) rb = nb = 1;
+        const int sh = rb == 1 ? 4 : rb == 2 ? 5 : 6;
+        const uint32_t out_tiles = (uint32_t)((a.n_out + 16 * nb - 1) / (16 * nb));
+        const int64_t units = units_of(rb, nb);
         const bool split = units < 4096 && steps >= 16;
         const dim3 blocks = net_grid(split ? units : (units + 3) / 4);
         auto go = [&](auto r, auto n) {
@@ -638,6 +685,7 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         }
         const void *dd = own ? d : a.dy;
         const int64_t ldd = own ? l.ldd : a.lddy;
+        float *part = (float *)((char *)a.scratch + l.part);
         // short sums: of few outputs (dx) or rows (dw); else tiles
         int L = 1;
         while (L < 256 && L * N < a.n_in) L *= 2;
@@ -648,7 +696,13 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
                                L, units);
             e = hipGetLastError();
         } else if (a.dx) {
-            e = launch_linear_dx_tiles<t.value>(a, dd, ldd, s);
+            const int splits = dx_splits(a);
+            e = launch_linear_dx_tiles<t.value>(a, dd, ldd, splits, part, s);
+            if (e == hipSuccess && splits > 1) {
+                hipLaunchKernelGGL((k_linear_join<T>), net_grid((a.rows.M * a.n_in + 255) / 256), dim3(256), 0, s, a.rows,
+                                   part, splits, a.rows.M, a.n_in, (T *)a.dx, a.rows.M, (int64_t)0, a.lddx, true);
+                e = hipGetLastError();
+            }
         }
         if (e != hipSuccess || !a.dw) return e;
         if (mean <= kShortMean && a.n_in >= 64) {
@@ -657,7 +711,13 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
                                L, units);
             return hipGetLastError();
         }
-        return launch_linear_dw_tiles<t.value>(a, dd, ldd, s);
+        const int splits = dw_splits(a);
+        e = launch_linear_dw_tiles<t.value>(a, dd, ldd, splits, part, s);
+        if (e != hipSuccess || splits == 1) return e;
+        const int64_t rows = a.rows.G * a.n_out;
+        hipLaunchKernelGGL((k_linear_join<T>), net_grid((rows * a.n_in + 255) / 256), dim3(256), 0, s, a.rows, part, splits,
+                           rows, a.n_in, (T *)a.dw, a.n_out, a.dw_stride, a.lddw, false);
+        return hipGetLastError();
     });
 }
 

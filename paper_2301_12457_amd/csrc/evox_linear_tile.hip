@@ -55,6 +55,27 @@ struct PlainOut {
     __device__ __forceinline__ Reg load(int, int, int) { return (Reg){}; }
     __device__ __forceinline__ void store(int j, int i, float *v, int n, Reg) { store_row(p + j * ld + i, v, n); }
 };
+// One share's sums of K, in fp32.
+struct PartOut {
+    float *p;
+    int64_t ld;
+    __device__ __forceinline__ void begin(int, int) {}
+    __device__ __forceinline__ Reg load(int, int, int) { return (Reg){}; }
+    __device__ __forceinline__ void store(int j, int i, float *v, int n, Reg)
+    {
+#pragma unroll
+        for (int e = 0; e < NetVec<Elem>::N; ++e)
+            if (e < n) p[j * ld + i + e] = v[e];
+    }
+};
+// Share z of K: whole K tiles.
+__device__ __forceinline__ void share_of(int64_t K, int splits, int z, int64_t *k0, int64_t *k1)
+{
+    const int64_t per = (K + splits * kTileK<Elem> - 1) / (splits * kTileK<Elem>) * kTileK<Elem>;
+    *k0 = z * per < K ? z * per : K;
+    *k1 = *k0 + per < K ? *k0 + per : K;
+}
+
 // The layer's epilogue; the pointers are at the tile's origin.
 struct LayerOut {
     const Elem *b, *r;
@@ -122,20 +143,26 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_tile(LinearAr
 // dx = d W: i = input, j = row, k = output.
 template <int ID>
 __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(LinearGradArgs a, const Elem *d,
-                                                                                      int64_t ldd, int64_t ti,
-                                                                                      int64_t tj, int64_t units)
+                                                                                      int64_t ldd, int64_t ti, int64_t tj,
+                                                                                      int splits, float *part, int64_t units)
 {
     __shared__ __attribute__((aligned(16))) char lds[Product<ID, true, false>::kLds];
-    const int64_t u = xcd_unit(units);
-    if (u < 0) return;
-    int64_t it, jt;
+    const int64_t us = xcd_unit(units), u = us / splits;
+    if (us < 0) return;
+    int64_t it, jt, k0, k1;
     unit_ij(u, ti, tj, &it, &jt);
+    share_of(a.n_out, splits, (int)(us - u * splits), &k0, &k1);
     const NetTile t = net_tile(a.rows, Shape<ID>::sh, jt);
     if (t.g < 0) return;
     const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_in - i0, Shape<ID>::BI), nj = (int)(t.hi - t.lo);
-    const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + i0, a.ldw, ni}, Q{d + t.lo * ldd, ldd, nj};
+    const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + k0 * a.ldw + i0, a.ldw, ni}, Q{d + t.lo * ldd + k0, ldd, nj};
     Product<ID, true, false> p;
-    p.run(P, Q, a.n_out, lds);
+    p.run(P, Q, k1 - k0, lds);
+    if (splits > 1) {
+        PartOut out{part + ((us - u * splits) * a.rows.M + t.lo) * a.n_in + i0, a.n_in};
+        p.results(ni, nj, lds, out);
+        return;
+    }
     PlainOut out{(Elem *)a.dx + t.lo * a.lddx + i0, a.lddx};
     p.results(ni, nj, lds, out);
 }
@@ -143,22 +170,28 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(Linea
 // dW = d^T x: i = input, j = output, k = row of the network.
 template <int ID>
 __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dw_tile(LinearGradArgs a, const Elem *d,
-                                                                                     int64_t ldd, int64_t ti, int64_t tj,
-                                                                                     int64_t units)
+                                                                                      int64_t ldd, int64_t ti, int64_t tj,
+                                                                                      int splits, float *part, int64_t units)
 {
     __shared__ __attribute__((aligned(16))) char lds[Product<ID, true, true>::kLds];
-    const int64_t u = xcd_unit(units);
-    if (u < 0) return;
+    const int64_t us = xcd_unit(units), u = us / splits, z = us - u * splits;
+    if (us < 0) return;
     const int64_t per = banded(tj) * ti, g = u / per;
-    int64_t it, jt, lo, hi;
+    int64_t it, jt, lo, hi, k0, k1;
     unit_ij(u - g * per, ti, tj, &it, &jt);
     if (jt >= tj) return;
     net_rows(a.rows, g, &lo, &hi);
+    share_of(hi - lo, splits, (int)z, &k0, &k1);
     const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_in - i0, Shape<ID>::BI), j0 = (int)jt * Shape<ID>::BJ,
               nj = min((int)a.n_out - j0, Shape<ID>::BJ);
-    const TileOp<Elem> P{(const Elem *)a.x + (a.x_shared ? 0 : lo) * a.ldx + i0, a.ldx, ni}, Q{d + lo * ldd + j0, ldd, nj};
+    const TileOp<Elem> P{(const Elem *)a.x + ((a.x_shared ? 0 : lo) + k0) * a.ldx + i0, a.ldx, ni}, Q{d + (lo + k0) * ldd + j0, ldd, nj};
     Product<ID, true, true> p;
-    p.run(P, Q, hi - lo, lds);
+    p.run(P, Q, k1 - k0, lds);
+    if (splits > 1) {
+        PartOut out{part + ((z * a.rows.G + g) * a.n_out + j0) * a.n_in + i0, a.n_in};
+        p.results(ni, nj, lds, out);
+        return;
+    }
     PlainOut out{(Elem *)a.dw + g * a.dw_stride + j0 * a.lddw + i0, a.lddw};
     p.results(ni, nj, lds, out);
 }
@@ -226,26 +259,32 @@ hipError_t launch_linear_tiles<EVOX_NET_TYPE>(const LinearArgs &a, hipStream_t s
 }
 
 template <>
-hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, hipStream_t s)
+hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, int splits, float *part, hipStream_t s)
 {
-    return with_shape(a.n_in, row_tiles(a.rows), [&](auto id) {
+    const auto go = [&](auto id) {
         constexpr int ID = id.value, B = Shape<ID>::BI;
         typedef Product<ID, true, false> G;
         const int64_t ti = (a.n_in + B - 1) / B, tj = net_tiles(a.rows, Shape<ID>::sh);
-        return launch_tiles<G>(k_linear_dx_tile<ID>, banded(tj) * ti, s, a, (const Elem *)d, ldd, ti, tj);
-    });
+        return launch_tiles<G>(k_linear_dx_tile<ID>, banded(tj) * ti * splits, s, a, (const Elem *)d, ldd, ti, tj, splits,
+                               part);
+    };
+    if (splits > 1) return go(std::integral_constant<int, 0>{});
+    return with_shape(a.n_in, row_tiles(a.rows), go);
 }
 
 template <>
-hipError_t launch_linear_dw_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, hipStream_t s)
+hipError_t launch_linear_dw_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, int splits, float *part, hipStream_t s)
 {
     const auto out_tiles = [&](int BJ) { return a.rows.G * ((a.n_out + BJ - 1) / BJ); };
-    return with_shape(a.n_in, out_tiles, [&](auto id) {
+    const auto go = [&](auto id) {
         constexpr int ID = id.value, B = Shape<ID>::BI, BJ = Shape<ID>::BJ;
         typedef Product<ID, true, true> G;
         const int64_t ti = (a.n_in + B - 1) / B, tj = (a.n_out + BJ - 1) / BJ;
-        return launch_tiles<G>(k_linear_dw_tile<ID>, a.rows.G * banded(tj) * ti, s, a, (const Elem *)d, ldd, ti, tj);
-    });
+        return launch_tiles<G>(k_linear_dw_tile<ID>, a.rows.G * banded(tj) * ti * splits, s, a, (const Elem *)d, ldd, ti, tj,
+                               splits, part);
+    };
+    if (splits > 1) return go(std::integral_constant<int, 0>{});
+    return with_shape(a.n_in, out_tiles, go);
 }
 
 }  // namespace evox

@@ -69,13 +69,15 @@ size_t xent_scratch(const XentArgs &a);
 hipError_t launch_xent(const XentArgs &a, hipStream_t s);
 
 // The large cases: tiles through LDS (one file per element type).  d: dy act'(z)
-// in the element type.
+// in the element type.  splits > 1: K in so many shares, partial results to part[z].
 template <int TYPE>
 hipError_t launch_linear_tiles(const LinearArgs &a, hipStream_t s);
 template <int TYPE>
-hipError_t launch_linear_dx_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, hipStream_t s);
+hipError_t launch_linear_dx_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, int splits, float *part,
+                                  hipStream_t s);
 template <int TYPE>
-hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, hipStream_t s);
+hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, int splits, float *part,
+                                  hipStream_t s);
 
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;

@@ -12,16 +12,17 @@ namespace evox {
 namespace {
 
 // Lanes per row and chunks per lane for n elements in chunks of N: `per` chunks
-// per lane up to a wave per row (`least` lanes at least), then up to four (eight at 1024 threads).
+// per lane up to a wave per row (`least` lanes at least) and `wide` up to 1024 (then
+// as many as it takes).
 struct RowShape {
     int L, nit, threads;
 };
-RowShape row_shape(int64_t n, int N, int per, int least)
+RowShape row_shape(int64_t n, int N, int per, int least, int wide)
 {
     const int64_t chunks = (n + N - 1) / N;
     RowShape s{least, 1, 256};
     while (s.L < 64 && chunks > per * s.L) s.L *= 2;
-    while (s.L >= 64 && s.L < 1024 && chunks > 4 * s.L) s.L = s.L == 64 ? 256 : 2 * s.L;
+    while (s.L >= 64 && s.L < 1024 && chunks > (s.L == 64 ? 4 : wide) * s.L) s.L = s.L == 64 ? 256 : 2 * s.L;
     while (chunks > (int64_t)s.nit * s.L) s.nit *= 2;
     if (s.L > 256) s.threads = s.L;
     return s;
@@ -302,13 +303,13 @@ struct NormSums {
     }
 };
 
-// Rows per tile of the gradient, as a power of two: 64 at most (its sums are
-// then 4 % or less of the rows' traffic), fewer where that leaves less than
+// Rows per tile of the gradient, as a power of two: 64 (its sums are then 4 % or
+// less of the rows' traffic), 256 of a few columns, fewer where that leaves less than
 // about four blocks per CU.
 int norm_tile_shift(const NormArgs &a)
 {
     const int least = a.D > 2048 ? 0 : 3;  // rows over a block or waves: few of them fill neither registers nor chip
-    int sh = 6;
+    int sh = a.D <= 16 ? 8 : 6;  // (a lane per row: as many rows as threads)
     while (sh > least && (a.rows.M >> sh) < 512) --sh;
     return sh;
 }
@@ -533,11 +534,11 @@ bool xent_whole(const XentArgs &a)
 {
     return !a.rows.off && a.rows.n <= 4096 && (a.rows.G >= 1024 || a.rows.n * a.C <= 16384);
 }
-// Rows per tile, as a power of two: 64 of a short row; a wide row's tile is at
-// least two rows, for about eight blocks per CU.
+// Rows per tile, as a power of two: 256 (a lane each, of rows of a few classes),
+// fewer where that leaves less than about eight blocks per CU.
 int xent_tile_shift(const XentArgs &a)
 {
-    int sh = 6;
+    int sh = 8;
     while (sh > 1 && (a.rows.M >> sh) < 2048) --sh;
     return sh;
 }
@@ -548,7 +549,7 @@ hipError_t launch_layernorm(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N, 4, 1);
+        const RowShape r = row_shape(a.D, NetVec<T>::N, 4, 1, 4);
         const int64_t per = r.L <= 64 ? 256 / r.L : 1;
         return with_shape<T>(r, [&](auto nit, auto wide) {
             hipLaunchKernelGGL((k_layernorm<T, nit.v, wide.v>), net_grid((a.rows.M + per - 1) / per),
@@ -566,7 +567,7 @@ hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N, 2, 4);
+        const RowShape r = row_shape(a.D, NetVec<T>::N, 2, 1, sizeof(T) == 2 ? 2 : 4);
         const int sh = norm_tile_shift(a);
         const int64_t tiles = net_tiles(a.rows, sh);
         hipError_t e = hipSuccess;
@@ -592,7 +593,7 @@ hipError_t launch_xent(const XentArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.C, NetVec<T>::N, 2, 1);
+        const RowShape r = row_shape(a.C, NetVec<T>::N, 2, 1, 4);
         const bool whole = xent_whole(a);
         const int sh = xent_tile_shift(a);
         if (a.dz && !whole)
