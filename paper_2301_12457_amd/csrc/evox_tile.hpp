@@ -142,29 +142,32 @@ template <typename T, int R, int TH>
 struct Stage16m {
     static constexpr int P = (R * 2 + TH - 1) / TH, kQuads = R / 4, kLoads = 8 * P, kStores = 4 * P;
     u32x2 v[P][8];
-    const T *src;
+    const T *base[P];  // the thread's patches at k = 0
     int64_t ld;
     int n;
     // threads past the patches repeat the first ones' work
     static __device__ __forceinline__ int thread() { return R * 2 < TH ? threadIdx.x % (R * 2) : threadIdx.x; }
     __device__ __forceinline__ void init(const T *s, int64_t l, int rows)
     {
-        src = s;
         ld = l;
         n = rows;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int q = thread() + p * TH;
+            base[p] = s + (int64_t)(q / kQuads * 8) * l + q % kQuads * 4;
+        }
     }
     __device__ __forceinline__ bool whole() const { return n == R; }
     __device__ __forceinline__ void load_piece(int i, int64_t k0)  // and all R rows exist
     {
-        const int p = i / 8, j = i % 8, q = thread() + p * TH;
-        v[p][j] = *reinterpret_cast<const u32x2u *>(src + (k0 + q / kQuads * 8 + j) * ld + q % kQuads * 4);
+        v[i / 8][i % 8] = *reinterpret_cast<const u32x2u *>(base[i / 8] + (k0 + i % 8) * ld);
     }
     __device__ __forceinline__ void load(int64_t k0, int64_t K)
     {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const int q = thread() + p * TH, r = q % kQuads * 4, k = q / kQuads * 8;
-            const T *at = src + (k0 + k) * ld + r;
+            const T *at = base[p] + k0 * ld;
             if (k0 + k + 8 <= K && r + 4 <= n) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[p][j] = *reinterpret_cast<const u32x2u *>(at + j * ld);
@@ -258,22 +261,25 @@ template <int R, int TH>
 struct Stage32m {
     static constexpr int P = (R * 4 + TH - 1) / TH, kStores = P;
     float v[P][8];
-    const float *src;
+    const float *base[P];  // the thread's elements at k = 0
     int64_t ld;
     int n;
     static __device__ __forceinline__ int thread() { return R * 4 < TH ? threadIdx.x % (R * 4) : threadIdx.x; }
     __device__ __forceinline__ void init(const float *s, int64_t l, int rows)
     {
-        src = s;
         ld = l;
         n = rows;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int q = thread() + p * TH;
+            base[p] = s + (int64_t)(q / R * 8) * l + q % R;
+        }
     }
     __device__ __forceinline__ bool whole() const { return n == R; }
     __device__ __forceinline__ void load_piece(int p, int64_t k0)  // and all R rows exist
     {
-        const int q = thread() + p * TH;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[p][j] = src[(k0 + q / R * 8 + j) * ld + q % R];
+        for (int j = 0; j < 8; ++j) v[p][j] = base[p][(k0 + j) * ld];
     }
     __device__ __forceinline__ void load(int64_t k0, int64_t K)
     {
@@ -281,7 +287,7 @@ struct Stage32m {
         for (int p = 0; p < P; ++p) {
             const int q = thread() + p * TH, r = q % R, k = q / R * 8;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[p][j] = k0 + k + j < K && r < n ? src[(k0 + k + j) * ld + r] : 0.0f;
+            for (int j = 0; j < 8; ++j) v[p][j] = k0 + k + j < K && r < n ? base[p][(k0 + j) * ld] : 0.0f;
         }
     }
     __device__ __forceinline__ void store_piece(int p, char *lds, float &big)
