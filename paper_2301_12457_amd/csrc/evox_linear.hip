@@ -305,12 +305,13 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
 #pragma unroll
         for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4 *>(row + c * N + j) = (f32x4){(float)v[j], (float)v[j + 1], (float)v[j + 2], (float)v[j + 3]};
     };
-    const int ci = ti * 16 / N, co = to * 16 / N, shares = TH / (to * 16);  // chunks per padded row; threads per column
+    // (k / ci and k / co by a multiplication, exact for k < 65536 / 15)
+    const int ci = ti * 16 / N, co = to * 16 / N, mi = (65535 + ci) / ci, mo = (65535 + co) / co, shares = TH / (to * 16);  // chunks per padded row; threads per column
     if (a.dx) {
         const T *w = (const T *)a.w + t.g * a.w_stride;
 #pragma unroll 2
         for (int k = tid; k < to * 16 * ci; k += TH) {
-            const int o = k / ci, c = k - o * ci;
+            const int o = (k * mi >> 16), c = k - o * ci;
             put(W + o * pi, c, o < no ? load_chunk(w + o * a.ldw, c, ni, (T)0.0f) : (reg){});
         }
     }
@@ -327,14 +328,14 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
             reg dy[2] = {}, z[2] = {};
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int k = k0 + u * TH, r = k / co, c = k - r * co;
+                const int k = k0 + u * TH, r = (k * mo >> 16), c = k - r * co;
                 if (k >= R * co || m0 + r >= t.hi) continue;
                 dy[u] = load_chunk((const T *)a.dy + (m0 + r) * a.lddy, c, no, (T)0.0f);
                 if (a.act != ACT_NONE) z[u] = load_chunk((const T *)a.z + (m0 + r) * a.ldz, c, no, (T)0.0f);
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int k = k0 + u * TH, r = k / co, c = k - r * co;
+                const int k = k0 + u * TH, r = (k * mo >> 16), c = k - r * co;
                 if (k >= R * co) continue;
                 float v[N];
 #pragma unroll
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
         if (a.dw)
 #pragma unroll 2
             for (int k = tid; k < R * ci; k += TH) {
-                const int r = k / ci, c = k - r * ci;
+                const int r = (k * mi >> 16), c = k - r * ci;
                 put(X + r * pi, c, m0 + r < t.hi ? load_chunk((const T *)a.x + (m0 + r - x0) * a.ldx, c, ni, (T)0.0f) : (reg){});
             }
         __syncthreads();

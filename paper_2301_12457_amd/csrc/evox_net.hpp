@@ -309,6 +309,15 @@ hipError_t launch_net_sums(const NetRows &rows, const float *part, int64_t width
 // they follow (16x2048 rows 4096x4096).
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
+// e^x within 2 ulp for results that are normal numbers: the rounding of x log2 e
+// put back, e^x = 2^h (1 + l ln 2).
+__device__ __forceinline__ float exp_near(float x)
+{
+    const float c = fmaxf(x, -200.0f), l = fmaf(c, 1.92596299e-8f, fmaf(c, 1.44269502f, -(c * 1.44269502f)));
+    const float e = __builtin_amdgcn_exp2f(x * 1.44269502f);
+    return fmaf(e, l * 0.69314718f, e);
+}
+
 // Q(|z|) and e^(-z^2/2).
 __device__ __forceinline__ float normal_tail(float z, float *e)
 {
@@ -351,13 +360,9 @@ __device__ __forceinline__ float act_slope(int act, float z)
     const float zc = fminf(fmaxf(z, -126.0f), 126.0f);  // infinities have slope 0 or 1
     switch (act) {
     case ACT_RELU: return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
-    case ACT_TANH: {
-        if constexpr (FAST) {
-            const float t = exp_fast(-2.0f * fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + t);
-            return 4.0f * t * r * r;
-        }
-        const float t = tanhf(z);
-        return (1.0f - t) * (1.0f + t);
+    case ACT_TANH: {  // 4 t / (1 + t)^2, t = e^(-2 |z|): no cancellation either way
+        const float t = FAST ? exp_fast(-2.0f * fabsf(z)) : exp_near(-2.0f * fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + t);
+        return 4.0f * t * r * r;
     }
     case ACT_GELU: {
         if constexpr (FAST) {

@@ -329,19 +329,14 @@ __device__ __forceinline__ int xent_label(const XentArgs &a, int64_t g, int64_t 
 }
 __device__ __forceinline__ bool xent_counts(const XentArgs &a, int label) { return label >= 0 && label < a.C; }
 
-// e^(v - top) for v <= top, by the hardware's exp2 (1 ulp).  Of fp32 logits the
-// rounding of (v - top) log2 e is put back (e^x = 2^h (1 + l ln 2), h + l the
-// whole product); of 16-bit logits it stays: far below the probability's own
-// rounding.  v - top comes first (its parts may be the type's lowest value).  Of
-// -inf 0, of NaN NaN.
+// e^(v - top) for v <= top: of fp32 logits within 2 ulp, of 16-bit ones with the
+// rounding of the exponent left in, far below the probability's own.  v - top
+// comes first (its parts may be the type's lowest value).  Of -inf 0, of NaN NaN.
 template <typename T>
 __device__ __forceinline__ float exp_below(float v, float top)
 {
-    const float x = v - top, c = fmaxf(x, -200.0f);
-    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(x * 1.44269502f);
-    const float l = fmaf(c, 1.92596299e-8f, fmaf(c, 1.44269502f, -(c * 1.44269502f)));
-    const float e = __builtin_amdgcn_exp2f(x * 1.44269502f);
-    return fmaf(e, l * 0.69314718f, e);
+    if constexpr (sizeof(T) == 2) return exp_fast(v - top);
+    else return exp_near(v - top);
 }
 
 struct XentScratch {
