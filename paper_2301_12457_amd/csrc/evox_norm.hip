@@ -388,7 +388,20 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256, WIDE && NIT <= 4 ? 8 : 1) void k
         t = net_tile(a.rows, sh, net_block());
         if (t.g < 0) return;
     }
-    const int lane = threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : 256 / L, C = (int)a.C;
+    const int lane = threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : blockDim.x / L,
+              C = (int)a.C;
+    // narrow rows: the first one's logits are on their way while the labels are
+    // counted (a wide row's registers would not last)
+    typename NetVec<T>::reg first[WIDE ? 1 : NIT];
+    int label = -1;
+    if constexpr (!WIDE)
+        if (t.lo + slot < t.hi) {
+            label = xent_label(a, t.g, t.lo + slot);
+#pragma unroll
+            for (int i = 0; i < NIT; ++i)
+                if ((lane + i * L) * N < C)
+                    first[i] = load_chunk((const T *)a.logits + (t.lo + slot) * a.ldz, lane + i * L, C, (T)-INFINITY);
+        }
     float scale = 0.0f;
     if (a.dz) {
         int n = 0;
@@ -411,17 +424,23 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256, WIDE && NIT <= 4 ? 8 : 1) void k
     for (int64_t m0 = t.lo; m0 < t.hi; m0 += slots) {
         const int64_t m = m0 + slot;
         const bool live = m < t.hi;
-        const T *z = (const T *)a.logits + m * a.ldz;
-        const int label = live ? xent_label(a, t.g, m) : -1;
+        if ((WIDE || m0 > t.lo) && live) label = xent_label(a, t.g, m);
         const bool counts = live && xent_counts(a, label);
         typename NetVec<T>::reg v[NIT];
-        float top = -INFINITY, sum = 0.0f;
         if (counts)
 #pragma unroll
-            for (int i = 0; i < NIT; ++i)
-                if ((lane + i * L) * N < C) v[i] = load_chunk(z, lane + i * L, C, (T)-INFINITY);
+            for (int i = 0; i < NIT; ++i) {
+                if ((lane + i * L) * N >= C) continue;
+                if constexpr (!WIDE)
+                    if (m0 == t.lo) {
+                        v[i] = first[i];
+                        continue;
+                    }
+                v[i] = load_chunk((const T *)a.logits + m * a.ldz, lane + i * L, C, (T)-INFINITY);
+            }
+        float top = -INFINITY, sum = 0.0f;
         // the label's logit, before the gradient may take its place
-        const float at = counts ? (float)z[label] : 0.0f;
+        const float at = counts ? (float)((const T *)a.logits)[m * a.ldz + label] : 0.0f;
         if (counts)
 #pragma unroll
             for (int i = 0; i < NIT; ++i)
@@ -596,8 +615,11 @@ hipError_t launch_xent(const XentArgs &a, hipStream_t s)
         hipError_t e = hipSuccess;
         if (a.rows.M > 0 || whole)
             e = with_shape<T>(r, [&](auto nit, auto wide) {
+                // no more threads than a whole network's rows keep busy
+                int threads = r.threads;
+                while (whole && !wide.v && threads > 64 && a.rows.n * r.L <= threads / 2) threads /= 2;
                 hipLaunchKernelGGL((k_xent<T, nit.v, wide.v>),
-                                   net_grid(whole ? a.rows.G : net_tiles(a.rows, sh)), dim3(r.threads), 0, s, a,
+                                   net_grid(whole ? a.rows.G : net_tiles(a.rows, sh)), dim3(threads), 0, s, a,
                                    r.L, sh, whole);
             });
         if (e != hipSuccess || whole) return e;
