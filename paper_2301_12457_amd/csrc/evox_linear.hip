@@ -1,5 +1,6 @@
-// Linear layers of a population of networks: y = act(x W_g^T + b_g) + r and
-// its gradient.
+// Linear layers of a population of networks: y = act(x W_g^T + b_g) + r and its
+// gradient.  Here: the choice of kernels, and those that need no LDS tiles (few
+// rows, narrow layers, short sums); evox_linear_tile.hip has the rest.
 #include "evox_tile.hpp"
 
 namespace evox {
@@ -70,9 +71,11 @@ __device__ __forceinline__ void store_quad(T *p, int n, f32x4 v)
 // Few rows per network, or narrow layers: a wave computes 16 RB rows x 16 NB
 // outputs with both operands straight from memory in the matrix cores' layout,
 // 16 bytes per lane; rows past the network's end repeat its last one (their
-// results are dropped), k past the end is zero.  WK waves share a tile's K
-// where the tiles alone are too few to fill the chip, and add their sums in
-// order.  Bound by the weights' bytes: each is read once.
+// results are dropped), k past the end is zero.  WK waves share a tile's K where
+// the tiles alone are too few to fill the chip or K is long, and add their sums
+// in order.  The weights, each read once, bound it: bf16 256 networks, one row
+// through 2048x2048, 347 us, 6.19 TB/s of the copy's 6.45 (16 x 32 tiles: 436 us);
+// fp32 4096 networks' one row 32x32, 7.8 us, a launch and the chain of its loads.
 // ---------------------------------------------------------------------------
 template <typename T, int RB, int NB, int WK>
 __global__ __launch_bounds__(256) void k_linear_thin(LinearArgs a, int sh, uint32_t out_tiles, int64_t units)
@@ -200,21 +203,43 @@ __global__ __launch_bounds__(256) void k_linear_thin(LinearArgs a, int sh, uint3
 
 // d = dy act'(z), rounded to the element type (where a.act is not none and a
 // product needs it), and the tiles' column sums of the unrounded d (where db is
-// wanted): a block takes 2^kDzShift rows of a network and 256 chunks of 16 bytes
-// of their columns, L lanes to a row, and adds its row slots in order.
-constexpr int kDzShift = 4;
+// wanted): a block takes 2^sh rows of a network and L chunks of 16 bytes of their
+// columns, and adds its 256 / L row slots in order.  Apart from
+// the products, so that a slope is computed once per element and not once per
+// tile that reads it; rounding d, as the 16-bit products have to, costs the
+// gradient as much as one more rounding of dy (relative rms against 64 bits 2.3e-3
+// in bf16, 1.7e-3 without).  bf16 32,768 rows of 1024 with GELU: 50 us, 4.0 TB/s,
+// bound by the slopes' arithmetic and the wait for two loads; in the dx and dw
+// tiles' own loads the slopes would be computed 8 times over there.  L: the most
+// lanes among those that leave the fewest idle; 2^sh: 16 rows, up to 256 where there
+// are more than 4096 blocks (300,000 rows of 1109: 18,750 tiles took 671 us to join).
+struct DzShape {
+    int sh, L;
+    int64_t cols;  // blocks per row
+};
+DzShape dz_shape(const LinearGradArgs &a)
+{
+    const int64_t chunks = (a.n_out + (a.dtype == NET_F32 ? 3 : 7)) / (a.dtype == NET_F32 ? 4 : 8);
+    DzShape s{4, 4, 0};
+    while (s.L < 32 && s.L < chunks) s.L *= 2;
+    for (int L = 64; L <= 256; L *= 2)
+        if ((chunks + L - 1) / L * L <= (chunks + s.L - 1) / s.L * s.L) s.L = L;
+    s.cols = (chunks + s.L - 1) / s.L;
+    while (s.sh < 8 && (a.rows.M >> s.sh) * s.cols > 4096) ++s.sh;
+    return s;
+}
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int L, T *d, int64_t ldd, float *sums)
+__global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int sh, int L, int64_t cols, T *d, int64_t ldd, float *sums)
 {
     constexpr int N = NetVec<T>::N;
     typedef typename NetVec<T>::reg reg;
     extern __shared__ float slots_sum[];  // [256 / L - 1][N][L]
-    const int64_t cols = (a.n_out + 256 * N - 1) / (256 * N), tile = net_block() / cols;
-    const NetTile t = net_tile(a.rows, kDzShift, tile);
+    const int64_t tile = net_block() / cols;
+    const NetTile t = net_tile(a.rows, sh, tile);
     if (t.g < 0) return;
     const int lane = threadIdx.x & (L - 1), slot = threadIdx.x / L, slots = 256 / L, n = (int)a.n_out,
-              c = (int)(net_block() - tile * cols) * 256 + lane;
+              c = (int)(net_block() - tile * cols) * L + lane;
     float s[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) s[j] = 0.0f;
@@ -256,7 +281,7 @@ __global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int L, T *d
         store_chunk((T *)a.db + t.g * a.db_stride, c, n, out);
         return;
     }
-    sums += net_slot(t.lo, t.index, kDzShift) * n + c * N;
+    sums += net_slot(t.lo, t.index, sh) * n + c * N;
 #pragma unroll
     for (int j = 0; j < N; ++j)
         if (c * N + j < n) sums[j] = s[j];
@@ -280,11 +305,17 @@ struct GradSums {
 
 // ---------------------------------------------------------------------------
 // The whole gradient of narrow layers (both widths at most 64) in one pass: a
-// block takes 2^sh rows of one network, W stays in LDS, and 16 rows per wave at a
+// block takes 2^sh rows of one network, W stays in LDS, and 16 F rows per wave at a
 // time d = dy act'(z) (not rounded: all of it is fp32 here) and x pass through
 // LDS into the fp32 matrix cores; every operand is read once and dx written
-// once.  Wave w has rows 16 w .. + 16 of dx, and of the dw tiles every WAVES-th.
-// Bound by memory: fp32 4096x32 rows 32x32 moves 101 MB.
+// once.  Blocks of two waves for up to 32 rows per network, else four (two / four:
+// fp32 32x32 8 rows 90 / 147 us, 32 rows 33 / 44, 64 rows 23 / 25, 200 rows 35 / 27).  Wave w has rows 16 F w .. + 16 F of dx, and of the dw tiles every WAVES-th;
+// with widths up to 16 (F = 4) its own rows' share of the one dw tile (1.8M rows 8x1
+// 120 us, F = 1: 149).  fp32
+// 4096x32 rows 32x32: 101 MB in 30 us, floor 16; three to four waves per SIMD (LDS
+// and registers) each wait for three loads in a row.  In separate passes through
+// the 64-tiles it took 72 us; W's and x's loads ahead of d's cost as much in
+// occupancy as they gained.
 // ---------------------------------------------------------------------------
 constexpr int kNarrow = 64;
 
@@ -306,7 +337,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
         for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4 *>(row + c * N + j) = (f32x4){(float)v[j], (float)v[j + 1], (float)v[j + 2], (float)v[j + 3]};
     };
     // (k / ci and k / co by a multiplication, exact for k < 65536 / 15)
-    const int ci = ti * 16 / N, co = to * 16 / N, mi = (65535 + ci) / ci, mo = (65535 + co) / co, shares = TH / (to * 16);  // chunks per padded row; threads per column
+    const int ci = ti * 16 / N, co = to * 16 / N, mi = (65535 + ci) / ci, mo = (65535 + co) / co,  // chunks per padded row
+              shares = TH / (to * 16);                                                           // threads per column
     if (a.dx) {
         const T *w = (const T *)a.w + t.g * a.w_stride;
 #pragma unroll 2
@@ -356,32 +388,20 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
         __syncthreads();
         if (a.dx)
             for (int f = 0; f < F; ++f) {
-            const int64_t m = m0 + (wave * F + f) * 16 + l16;
-            const float *d = D + ((wave * F + f) * 16 + l16) * po;
-            for (int i = 0; i < ti; ++i) {
-                f32x4 acc = (f32x4)(0.0f);
-                for (int k = 0; k < to; ++k) {
-                    const f32x4 b = *reinterpret_cast<const f32x4 *>(d + k * 16 + 4 * q);
-                    f32x4 w;
+                const int64_t m = m0 + (wave * F + f) * 16 + l16;
+                const float *d = D + ((wave * F + f) * 16 + l16) * po;
+                for (int i = 0; i < ti; ++i) {
+                    f32x4 acc = (f32x4)(0.0f);
+                    for (int k = 0; k < to; ++k) {
+                        const f32x4 b = *reinterpret_cast<const f32x4 *>(d + k * 16 + 4 * q);
+                        f32x4 w;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = W[(k * 16 + 4 * q + e) * pi + i * 16 + l16];
-                    acc = mma16(w, b, acc);
-                }
-                if (m < t.hi) {
-                    T *dx = (T *)a.dx + m * a.lddx + i * 16 + 4 * q;
-                    if (i * 16 + 4 * q + 4 <= ni) {
-                        typename Quad<T>::mem v;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = (T)acc[e];
-                        *reinterpret_cast<typename Quad<T>::mem *>(dx) = v;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (i * 16 + 4 * q + e < ni) dx[e] = (T)acc[e];
+                        for (int e = 0; e < 4; ++e) w[e] = W[(k * 16 + 4 * q + e) * pi + i * 16 + l16];
+                        acc = mma16(w, b, acc);
                     }
+                    if (m < t.hi) store_quad((T *)a.dx + m * a.lddx + i * 16 + 4 * q, ni - (i * 16 + 4 * q), acc);
                 }
             }
-        }
         if (a.dw)
 #pragma unroll
             for (int s = 0; s < kDw; ++s) {
@@ -439,14 +459,20 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
 }
 
 // Rows per tile of the narrow gradient, as a power of two: about 2048 tiles, of
-// 64 .. 4096 rows.
+// 64 .. 4096 rows; whole networks of up to 4096 where these are enough for the chip
+// (their results need no sums).
 int narrow_shift(const LinearGradArgs &a)
 {
     int sh = 6;
-    while (sh < 12 && (a.rows.M >> sh) > 2048) ++sh;
+    while (sh < 12 && ((a.rows.M >> sh) > 2048 || (!a.rows.off && a.rows.G >= 512 && a.rows.n > (int64_t)1 << sh))) ++sh;
     return sh;
 }
-bool narrow(const LinearGradArgs &a) { return a.n_in <= kNarrow && a.n_out <= kNarrow; }
+// 16 bits, both widths above 48: the tiles' 16-bit products are faster than fp32
+// ones (bf16 100x1000 rows 64x64 45 us, here 60; 64x48 51, here 50).
+bool narrow(const LinearGradArgs &a)
+{
+    return a.n_in <= kNarrow && a.n_out <= kNarrow && (a.dtype == NET_F32 || a.n_in <= 48 || a.n_out <= 48);
+}
 
 // ---------------------------------------------------------------------------
 // Gradient products of a short sum: dx of few outputs (DW = false: rows m of a
@@ -537,13 +563,15 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
 
 // dx and dw of so few tiles that most CUs would idle through a long K: its shares
 // are summed by blocks of their own, into fp32 partial results that are then added
-// in order.  Decided by the sizes alone (the scratch is sized by them), for tiles
-// of 64 a side.
+// in order: about four blocks per CU, of at least 256 of K.  Decided by the sizes
+// alone (the scratch is sized by them), for tiles of 64 a side.  fp32 5 networks'
+// 12 rows 331x1756 49 us, 125 without; half as many blocks: bf16 300,000 rows 18x1109
+// 1364 us, 1296 so, fp32 4096 rows 1024x1024 194, 183, bf16 20,000 rows 300x300 90, 102.
 int grad_splits(int64_t tiles, int64_t K)
 {
-    int64_t s = 512 / (tiles < 1 ? 1 : tiles);
+    int64_t s = 1024 / (tiles < 1 ? 1 : tiles);
     if (s > K / 256) s = K / 256;
-    return s < 2 ? 1 : s > 16 ? 16 : (int)s;
+    return s < 2 ? 1 : s > 64 ? 64 : (int)s;
 }
 int dx_splits(const LinearGradArgs &a)
 {
@@ -588,7 +616,7 @@ GradScratch grad_layout(const LinearGradArgs &a)
     const size_t e = a.dtype == NET_F32 ? 4 : 2;
     g.ldd = (a.n_out + 7) / 8 * 8;
     g.sums = (e * (size_t)a.rows.M * (size_t)g.ldd + 255) / 256 * 256;
-    g.part = (g.sums + 4 * (size_t)net_slots(a.rows.M, kDzShift) * (size_t)a.n_out + 255) / 256 * 256;
+    g.part = (g.sums + 4 * (size_t)net_slots(a.rows.M, dz_shape(a).sh) * (size_t)a.n_out + 255) / 256 * 256;
     const size_t dx = dx_splits(a) > 1 ? (size_t)dx_splits(a) * (size_t)a.rows.M * (size_t)a.n_in : 0;
     const size_t dw = dw_splits(a) > 1 ? (size_t)dw_splits(a) * (size_t)(a.rows.G * a.n_out) * (size_t)a.n_in : 0;
     g.end = g.part + 4 * (dx > dw ? dx : dw);
@@ -602,11 +630,16 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
         const int64_t mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
-        if (mean > 32 && a.n_out > 32 && a.n_in >= 64)
+        // the tiles, for their reuse, where their padding (64 rows, outputs and k) is
+        // not most of them (here / tiles, us: bf16 512x512 24 rows 39 / 38, 48 rows 52 / 44,
+        // fp32 77 / 78, 157 / 83; 500 rows 256x32 bf16 11 / 10, fp32 24 / 30, 256x48 15 / 10,
+        // 38 / 30; 500 rows 64x300 24 / 28, 44 / 44, fp32 96x300 60 / 53)
+        if (mean > 24 && a.n_out > 32 && a.n_in >= (sizeof(T) == 2 ? 128 : 64))
             return launch_linear_tiles<t.value>(a, s);
         // rows of a wave's tile by the mean rows per network (few k steps of 16 bits or
-        // outputs: smaller tiles, more waves at a time); one 16 x 16 tile where
-        // larger ones would leave most of the chip without a wave
+        // outputs: smaller tiles, more waves at a time: 200 rows 32x200 bf16 12.1, with 64 x
+        // 32 13.0 us); one 16 x 16 tile where larger ones would leave most of the chip
+        // without a wave (one network's 3000 rows 512x24 9.3, 10.9 us)
         const bool few_steps = a.n_in <= 2 * Mma<T>::KS && (sizeof(T) == 2 || a.n_out <= 16);
         int rb = mean <= 16 ? 1 : mean <= 32 || few_steps ? 2 : 4, nb = rb == 1 || a.n_out <= 16 ? 1 : 2;
         const int64_t steps = (a.n_in + Mma<T>::KS - 1) / Mma<T>::KS;
@@ -617,7 +650,10 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
         const int sh = rb == 1 ? 4 : rb == 2 ? 5 : 6;
         const uint32_t out_tiles = (uint32_t)((a.n_out + 16 * nb - 1) / (16 * nb));
         const int64_t units = units_of(rb, nb);
-        const bool split = units < 4096 && steps >= 16;
+        // a long K to four waves (one / four, us: bf16 one row 2048x2048 380 / 347, 8 rows
+        // 1024x1024 868 / 958; fp32 761 / 698, 1734 / 1681, 8 rows 512x512 215 / 213), and a
+        // shorter one where tiles are few (one network's 16 rows 2048x1024 17 / 9)
+        const bool split = (units < 4096 && steps >= 16) || (rb < 4 && steps >= (sizeof(T) == 2 ? 64 : 32));
         const dim3 blocks = net_grid(split ? units : (units + 3) / 4);
         auto go = [&](auto r, auto n) {
             if (split)
@@ -657,8 +693,7 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
                                    dim3(64 * waves.value), lds, s, a, sh, part);
                 return hipGetLastError();
             };
-            if (a.rows.M > 0)
-            {
+            if (a.rows.M > 0) {
                 using std::integral_constant;
                 if (mean <= 32) e = go(integral_constant<int, 2>{}, integral_constant<int, 1>{});
                 else if (mean > 128 && a.n_in <= 16 && a.n_out <= 16) e = go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
@@ -668,19 +703,17 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
             return launch_net_sums(a.rows, part, a.n_out * (a.n_in + 1), sh, s,
                                    GradSums<T>{(T *)a.dw, (T *)a.db, a.n_out, a.n_in, a.lddw, a.dw_stride, a.db_stride});
         }
+        const DzShape dz = dz_shape(a);
         const bool own = a.act != ACT_NONE && (a.dx || a.dw);
         T *d = own ? (T *)a.scratch : nullptr;
         float *sums = a.db ? (float *)((char *)a.scratch + l.sums) : nullptr;
         if (a.rows.M > 0 && (d || sums)) {
-            int Lz = 4;
-            while (Lz < 256 && Lz * N < a.n_out) Lz *= 2;
-            const int64_t cz = (a.n_out + 256 * N - 1) / (256 * N);
-            hipLaunchKernelGGL((k_linear_dz<T>), net_grid(net_tiles(a.rows, kDzShift) * cz), dim3(256),
-                               sizeof(float) * N * (256 - Lz), s, a, Lz, d, l.ldd, sums);
+            hipLaunchKernelGGL((k_linear_dz<T>), net_grid(net_tiles(a.rows, dz.sh) * dz.cols), dim3(256),
+                               sizeof(float) * N * (256 - dz.L), s, a, dz.sh, dz.L, dz.cols, d, l.ldd, sums);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
-        if (a.db && !(a.rows.M > 0 && !a.rows.off && net_single(a.rows, kDzShift))) {
-            e = launch_net_sums(a.rows, sums, a.n_out, kDzShift, s,
+        if (a.db && !(a.rows.M > 0 && !a.rows.off && net_single(a.rows, dz.sh))) {
+            e = launch_net_sums(a.rows, sums, a.n_out, dz.sh, s,
                                 GradSums<T>{nullptr, (T *)a.db, a.n_out, 0, 0, 0, a.db_stride});
             if (e != hipSuccess) return e;
         }

@@ -113,18 +113,14 @@ struct NetVec {
     typedef T mem __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
 
-// Elements [c N, c N + N) of a row of n, `fill` past its end.  NT: with the
+// Elements [c N, c N + N) of a row of n, `fill` past its end.  NT: stored with the
 // streaming hint.
-template <typename T, bool NT = false>
+template <typename T>
 __device__ __forceinline__ typename NetVec<T>::reg load_chunk(const T *row, int c, int n, T fill)
 {
     constexpr int N = NetVec<T>::N;
     const int at = c * N;
-    if (at + N <= n) {
-        const auto *p = reinterpret_cast<const typename NetVec<T>::mem *>(row + at);
-        if constexpr (NT) return __builtin_nontemporal_load(p);
-        else return *p;
-    }
+    if (at + N <= n) return *reinterpret_cast<const typename NetVec<T>::mem *>(row + at);
     typename NetVec<T>::reg v;
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = at + j < n ? row[at + j] : fill;
@@ -266,36 +262,42 @@ __host__ __device__ __forceinline__ int64_t net_slots(int64_t M, int sh) { retur
 inline bool net_single(const NetRows &r, int sh) { return r.off ? r.M <= ((int64_t)1 << sh) : r.n <= ((int64_t)1 << sh); }
 
 // out(g, e, sum) for the networks of several tiles and those without rows (sum
-// 0): 64 elements by 4 shares of the tiles per block.
-template <typename F>
-__global__ __launch_bounds__(256) void k_net_sums(NetRows rows, const float *part, int64_t width, int sh, F out)
+// 0): E elements by S shares of the tiles per block, 64 by 4, or 16 by 64 where
+// networks have more than 64 tiles on average (the narrow gradient of 500,000 rows
+// 32x32 of one network, 1954 tiles of 1056 elements: 76 us, 123 with 64 by 4).
+template <typename F, int E, int S>
+__global__ __launch_bounds__(E * S) void k_net_sums(NetRows rows, const float *part, int64_t width, int sh, F out)
 {
-    __shared__ float share[3][64];
-    const int64_t e = (int64_t)blockIdx.x * 64 + threadIdx.x % 64;
-    const int w = threadIdx.x / 64;
+    __shared__ float share[S][E];
+    const int64_t e = (int64_t)blockIdx.x * E + threadIdx.x % E;
+    const int w = threadIdx.x / E;
     for (int64_t g = blockIdx.y; g < rows.G; g += gridDim.y) {
         int64_t lo, hi;
         net_rows(rows, g, &lo, &hi);
-        const int64_t n = (hi - lo + ((int64_t)1 << sh) - 1) >> sh, per = (n + 3) / 4;
+        const int64_t n = (hi - lo + ((int64_t)1 << sh) - 1) >> sh, per = (n + S - 1) / S;
         if (n == 1) continue;
         float s = 0.0f;
         if (e < width) {
             const int64_t t1 = (w + 1) * per < n ? (w + 1) * per : n;
-#pragma unroll 4
+#pragma unroll 8
             for (int64_t t = w * per; t < t1; ++t) s += part[net_slot(lo + (t << sh), (int)t, sh) * width + e];
         }
-        if (w > 0) share[w - 1][threadIdx.x % 64] = s;
+        share[w][threadIdx.x % E] = s;
         __syncthreads();
-        if (w == 0 && e < width) out(g, e, s + share[0][threadIdx.x] + share[1][threadIdx.x] + share[2][threadIdx.x]);
+        if (w == 0 && e < width) {
+            for (int k = 1; k < S; ++k) s += share[k][threadIdx.x];
+            out(g, e, s);
+        }
         __syncthreads();
     }
 }
 template <typename F>
 hipError_t launch_net_sums(const NetRows &rows, const float *part, int64_t width, int sh, hipStream_t s, F out)
 {
-    hipLaunchKernelGGL((k_net_sums<F>),
-                       dim3((unsigned)((width + 63) / 64), (unsigned)(rows.G < 32768 ? rows.G : 32768)), dim3(256), 0, s,
-                       rows, part, width, sh, out);
+    const bool many = (rows.M >> sh) / rows.G > 64;
+    const dim3 grid((unsigned)((width + (many ? 15 : 63)) / (many ? 16 : 64)), (unsigned)(rows.G < 32768 ? rows.G : 32768));
+    if (many) hipLaunchKernelGGL((k_net_sums<F, 16, 64>), grid, dim3(1024), 0, s, rows, part, width, sh, out);
+    else hipLaunchKernelGGL((k_net_sums<F, 64, 4>), grid, dim3(256), 0, s, rows, part, width, sh, out);
     return hipGetLastError();
 }
 

@@ -11,17 +11,17 @@ namespace evox {
 
 namespace {
 
-// Lanes per row and chunks per lane for n elements in chunks of N: `per` chunks
-// per lane up to a wave per row (`least` lanes at least) and `wide` up to 1024 (then
-// as many as it takes).
+// Lanes per row and chunks per lane for n elements in chunks of N: up to 16 lanes
+// two chunks per lane (so that a wave's load covers whole lines of a row), then
+// `per` up to a wave per row, then `wide` up to 1024 lanes, then as many as it takes.
 struct RowShape {
     int L, nit, threads;
 };
-RowShape row_shape(int64_t n, int N, int per, int least, int wide)
+RowShape row_shape(int64_t n, int N, int per, int wide)
 {
     const int64_t chunks = (n + N - 1) / N;
-    RowShape s{least, 1, 256};
-    while (s.L < 64 && chunks > per * s.L) s.L *= 2;
+    RowShape s{1, 1, 256};
+    while (s.L < 64 && chunks > (s.L < 16 ? 2 : per) * s.L) s.L *= 2;
     while (s.L >= 64 && s.L < 1024 && chunks > (s.L == 64 ? 4 : wide) * s.L) s.L = s.L == 64 ? 256 : 2 * s.L;
     while (chunks > (int64_t)s.nit * s.L) s.nit *= 2;
     if (s.L > 256) s.threads = s.L;
@@ -91,7 +91,11 @@ __device__ __forceinline__ void row_sum2(float &a, float &b, int L, float2 *lds)
 
 // ---------------------------------------------------------------------------
 // Layer norm: the mean first, then the variance of the centred row (both from
-// the row in registers, so a large mean costs no digits).
+// the row in registers, so a large mean costs no digits).  Bound by memory: f16
+// 65,536 rows of 1024 50 us, 5.4 TB/s of the copy's 6.45 (its floor 42).  Results
+// with the streaming hint (f16 16,384 rows of 1024 17.1 us, 19.3 without; on the
+// loads it does nothing).  Two to four chunks per lane (four / two: f16 65,536 rows
+// of 300 22 / 28 us, of 1024 50 / 52; of 100 16 / 13, so from 16 lanes on).
 // ---------------------------------------------------------------------------
 template <typename T, int NIT, bool WIDE>
 __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int L)
@@ -152,7 +156,11 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
 // the sums of dy h and dy of its own columns over the rows it meets, the row
 // slots of the block add theirs in a fixed order; k_net_sums adds a network's tiles.
 // Rows whose chunks and sums do not fit the registers together (fp32, eight
-// chunks per lane) are read a second time.
+// chunks per lane) are read a second time.  fp32 20,000 ragged rows of 1001: 53 us
+// and 5 for the sums, 76 with cold caches (floor 37); bound by how much of the
+// rows is in flight, but the next row's loads ahead of this one's sums gained
+// nothing.  Two chunks per lane (four: f16 65,536 rows of 300 51 / 56 us), of wide
+// rows of 16 bits one (8192 rows of 4096 92 / 102).
 // ---------------------------------------------------------------------------
 template <typename T, int NIT, bool WIDE>
 __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a, int L, int sh)
@@ -305,12 +313,13 @@ struct NormSums {
 
 // Rows per tile of the gradient, as a power of two: 64 (its sums are then 4 % or
 // less of the rows' traffic), 256 of a few columns, fewer where that leaves less than
-// about four blocks per CU.
+// two blocks per CU (wide rows: 1.5; bf16 2000 rows of 8192 in 500 tiles 52 us, in
+// 1000 76; 8192 rows of 4096 in 512 tiles 67, in 256 92).
 int norm_tile_shift(const NormArgs &a)
 {
     const int least = a.D > 2048 ? 0 : 3;  // rows over a block or waves: few of them fill neither registers nor chip
     int sh = a.D <= 16 ? 8 : 6;  // (a lane per row: as many rows as threads)
-    while (sh > least && (a.rows.M >> sh) < 512) --sh;
+    while (sh > least && (a.rows.M >> sh) < (a.D > 2048 ? 400 : 512)) --sh;
     return sh;
 }
 
@@ -319,7 +328,11 @@ int norm_tile_shift(const NormArgs &a)
 // stay in registers from the maximum to the gradient.  The tile's loss (fp64)
 // and count go to the scratch and are added per network in order.  The
 // gradient needs the network's count first: where a tile is the whole network
-// the block counts the labels itself, else k_xent_count has.
+// the block counts the labels itself, else k_xent_count has.  bf16 8192 rows of
+// 32,768 in 16 ragged networks: 248 us, 4.3 TB/s (floor 166); bound by a row's loads,
+// exponentials and two block-wide reductions in turn, with one other block per CU
+// to fill in; 10 us are the count's and the fitness's launches.  fp32 4096x32 rows
+// of 10: one launch of 6.8 us.
 // ---------------------------------------------------------------------------
 constexpr int kCountShift = 12;  // labels per block of k_xent_count
 
@@ -543,17 +556,19 @@ __global__ __launch_bounds__(256) void k_xent_fit(XentArgs a, int sh)
 }
 
 // Whether every network is one block's: as many rows for each, and either
-// networks enough to fill the chip or little work in each.
+// networks enough to fill the chip or little work in each (fp32 rows of 10: 4096x32
+// 9 us, in tiles with a count and a sum 22; 1024x500 18, 24; 16x1000 of 16 15, 19).
 bool xent_whole(const XentArgs &a)
 {
     return !a.rows.off && a.rows.n <= 4096 && (a.rows.G >= 1024 || a.rows.n * a.C <= 16384);
 }
 // Rows per tile, as a power of two: 256 (a lane each, of rows of a few classes),
-// fewer where that leaves less than about eight blocks per CU.
+// fewer where that leaves less than eight blocks per CU (a few classes: two; 200,000
+// rows of 10 21 us, 25 so; bf16 8192 ragged rows of 32,768 249 us, with two blocks 316).
 int xent_tile_shift(const XentArgs &a)
 {
     int sh = 8;
-    while (sh > 1 && (a.rows.M >> sh) < 2048) --sh;
+    while (sh > 1 && (a.rows.M >> sh) < (a.C <= 16 ? 512 : 2048)) --sh;
     return sh;
 }
 
@@ -563,7 +578,7 @@ hipError_t launch_layernorm(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N, 4, 1, 4);
+        const RowShape r = row_shape(a.D, NetVec<T>::N, 4, 4);
         const int64_t per = r.L <= 64 ? 256 / r.L : 1;
         return with_shape<T>(r, [&](auto nit, auto wide) {
             hipLaunchKernelGGL((k_layernorm<T, nit.v, wide.v>), net_grid((a.rows.M + per - 1) / per),
@@ -581,7 +596,7 @@ hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N, 2, 1, sizeof(T) == 2 ? 2 : 4);
+        const RowShape r = row_shape(a.D, NetVec<T>::N, 2, sizeof(T) == 2 ? 1 : 2);
         const int sh = norm_tile_shift(a);
         const int64_t tiles = net_tiles(a.rows, sh);
         hipError_t e = hipSuccess;
@@ -607,7 +622,7 @@ hipError_t launch_xent(const XentArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.C, NetVec<T>::N, 2, 1, 4);
+        const RowShape r = row_shape(a.C, NetVec<T>::N, 4, 4);
         const bool whole = xent_whole(a);
         const int sh = xent_tile_shift(a);
         if (a.dz && !whole)
