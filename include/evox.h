@@ -15,7 +15,9 @@
  *   - DE/rand/1/bin, OpenES, PGPE, CMA-ES in its matrix-adaptation form
  *     (MA-ES) and NSGA-II on DTLZ1 (Table II; Sec. VII-A and VII-B),
  * on six benchmark functions (Sphere, the function of Sec. VII-A-1, and the
- * textbook Ackley, Rastrigin, Griewank, Rosenbrock and Schwefel).
+ * textbook Ackley, Rastrigin, Griewank, Rosenbrock and Schwefel).  Where the
+ * individuals are networks, it also computes their layers, norms and losses
+ * (fitness) and the gradients of these.
  *
  * Everything runs in hand-written HIP kernels; every call enqueues work on the
  * caller's HIP stream and returns without waiting, except evox_best,
