@@ -245,13 +245,16 @@ __global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int sh, int
     for (int j = 0; j < N; ++j) s[j] = 0.0f;
     if (c * N < n)
         for (int64_t m = t.lo + slot; m < t.hi; m += slots) {
-            const reg dy = load_chunk((const T *)a.dy + m * a.lddy, c, n, (T)0.0f);
+            reg dy = load_early((const T *)a.dy + m * a.lddy, c, n);
             if (a.act == ACT_NONE) {
+                settle(dy, c, n, (T)0.0f);
 #pragma unroll
                 for (int j = 0; j < N; ++j) s[j] += (float)dy[j];
                 continue;
             }
-            const reg z = load_chunk((const T *)a.z + m * a.ldz, c, n, (T)0.0f);
+            reg z = load_early((const T *)a.z + m * a.ldz, c, n);
+            settle(dy, c, n, (T)0.0f);
+            settle(z, c, n, (T)0.0f);
             float v[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) v[j] = (float)z[j];
@@ -362,13 +365,15 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
             for (int u = 0; u < 2; ++u) {
                 const int k = k0 + u * TH, r = (k * mo >> 16), c = k - r * co;
                 if (k >= R * co || m0 + r >= t.hi) continue;
-                dy[u] = load_chunk((const T *)a.dy + (m0 + r) * a.lddy, c, no, (T)0.0f);
-                if (a.act != ACT_NONE) z[u] = load_chunk((const T *)a.z + (m0 + r) * a.ldz, c, no, (T)0.0f);
+                dy[u] = load_early((const T *)a.dy + (m0 + r) * a.lddy, c, no);
+                if (a.act != ACT_NONE) z[u] = load_early((const T *)a.z + (m0 + r) * a.ldz, c, no);
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int k = k0 + u * TH, r = (k * mo >> 16), c = k - r * co;
                 if (k >= R * co) continue;
+                settle(dy[u], c, no, (T)0.0f);
+                settle(z[u], c, no, (T)0.0f);
                 float v[N];
 #pragma unroll
                 for (int j = 0; j < N; ++j) v[j] = (float)z[u][j];

@@ -13,18 +13,26 @@ namespace {
 
 // Lanes per row and chunks per lane for n elements in chunks of N: up to 16 lanes
 // two chunks per lane (so that a wave's load covers whole lines of a row), then
-// `per` up to a wave per row, then `wide` up to 1024 lanes, then as many as it takes.
+// `per` up to a wave per row of at most PER, then a block per row: PER per lane of
+// 128 .. 1024 threads, then as many as it takes.
 struct RowShape {
     int L, nit, threads;
+    bool wide;
 };
-RowShape row_shape(int64_t n, int N, int per, int wide)
+template <int PER>
+RowShape row_shape(int64_t n, int N)
 {
     const int64_t chunks = (n + N - 1) / N;
-    RowShape s{1, 1, 256};
-    while (s.L < 64 && chunks > (s.L < 16 ? 2 : per) * s.L) s.L *= 2;
-    while (s.L >= 64 && s.L < 1024 && chunks > (s.L == 64 ? 4 : wide) * s.L) s.L = s.L == 64 ? 256 : 2 * s.L;
+    RowShape s{1, 1, 256, chunks > 64 * PER};
+    if (s.wide) {
+        s.L = 256;
+        while (s.L < 1024 && chunks > PER * s.L) s.L += 64;
+        while (chunks > (int64_t)s.nit * s.L) s.nit *= 2;
+        s.L = s.threads = (int)((chunks + s.nit * 64 - 1) / (s.nit * 64)) * 64;
+        return s;
+    }
+    while (s.L < 64 && chunks > (s.L < 16 ? 2 : PER) * s.L) s.L *= 2;
     while (chunks > (int64_t)s.nit * s.L) s.nit *= 2;
-    if (s.L > 256) s.threads = s.L;
     return s;
 }
 
@@ -33,15 +41,16 @@ template <int V>
 struct Int {
     static constexpr int v = V;
 };
-template <typename T, typename F>
+template <typename T, int PER, typename F>
 hipError_t with_shape(const RowShape &s, F &&f)
 {
-    if (s.L <= 64) {
+    if (!s.wide) {
         if (s.nit == 1) f(Int<1>{}, Int<0>{});
-        else if (s.nit == 2) f(Int<2>{}, Int<0>{});
-        else f(Int<4>{}, Int<0>{});
+        else if (PER == 2 || s.nit == 2) f(Int<2>{}, Int<0>{});
+        else f(Int<PER>{}, Int<0>{});
     } else {
-        if (s.nit <= 2) f(Int<2>{}, Int<1>{});
+        if (PER == 2 && s.nit == 1) f(Int<PER == 2 ? 1 : 2>{}, Int<1>{});  // (PER = 4: 257 chunks on 256 lanes at least)
+        else if (s.nit <= 2) f(Int<2>{}, Int<1>{});
         else if (s.nit == 4) f(Int<4>{}, Int<1>{});
         else if constexpr (sizeof(T) == 4) f(Int<8>{}, Int<1>{});  // 16 bits: 4 x 1024 chunks hold EVOX_MAX_D
     }
@@ -67,6 +76,7 @@ __device__ __forceinline__ float row_all(float v, int L, float *lds)
     }
     return v;
 }
+// lds: not the place of the call before (its reads need no wait then).
 template <bool WIDE>
 __device__ __forceinline__ void row_sum2(float &a, float &b, int L, float2 *lds)
 {
@@ -76,7 +86,6 @@ __device__ __forceinline__ void row_sum2(float &a, float &b, int L, float2 *lds)
     }
     if constexpr (WIDE) {
         const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
-        __syncthreads();
         if (threadIdx.x % 64 == 0) lds[wave] = make_float2(a, b);
         __syncthreads();
         float2 v = lds[0];
@@ -102,7 +111,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
 {
     constexpr int N = NetVec<T>::N;
     __shared__ float lds[16];
-    const int lane = threadIdx.x & (L - 1), D = (int)a.D;
+    const int lane = WIDE ? threadIdx.x : threadIdx.x & (L - 1), D = (int)a.D;
     const int64_t m = WIDE ? net_block() : net_block() * (256 / L) + threadIdx.x / L;
     const bool live = m < a.rows.M;
     const T *x = (const T *)a.x + m * a.ldx;
@@ -156,22 +165,27 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
 // the sums of dy h and dy of its own columns over the rows it meets, the row
 // slots of the block add theirs in a fixed order; k_net_sums adds a network's tiles.
 // Rows whose chunks and sums do not fit the registers together (fp32, eight
-// chunks per lane) are read a second time.  fp32 20,000 ragged rows of 1001: 53 us
-// and 5 for the sums, 76 with cold caches (floor 37); bound by how much of the
-// rows is in flight, but the next row's loads ahead of this one's sums gained
-// nothing.  Two chunks per lane (four: f16 65,536 rows of 300 51 / 56 us), of wide
-// rows of 16 bits one (8192 rows of 4096 92 / 102).
+// chunks per lane; 16 bits, four) are read a second time, the others' loads run a
+// row ahead of the sums.  fp32 20,000 ragged rows of 1001: 62 us with its sums' 5
+// (floor 37), 77 with four chunks per lane, where there is no room for the row
+// ahead; f16 134,784 rows of 1000 194 us, 239 without it and with gamma loaded per
+// row; 67,392 rows of 2625 285, of one chunk per lane 398.  fp32 rows of 1000 reach
+// 4.5 TB/s; bound by the loads in flight and, above 8192 fp32 columns, by the
+// second reading (f16 8192 rows of 32,768 522 us; held, with spills, 710).
 // ---------------------------------------------------------------------------
 template <typename T, int NIT, bool WIDE>
 __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a, int L, int sh)
 {
     constexpr int N = NetVec<T>::N;
-    constexpr bool kHold = NIT * (8 + 2 * N) <= 96;
+    typedef typename NetVec<T>::reg reg;
+    // which rows fit the registers: x and dy from one pass to the next; gamma; the row ahead
+    constexpr bool kHold = NIT * (8 + 2 * N) < 96, kGamma = NIT * (12 + 2 * N) <= 72, kAhead = NIT * (20 + 2 * N) <= 72;
     extern __shared__ float sums[];  // [3 waves][2][NIT][N][L] (narrow rows)
-    __shared__ float2 lds[16];
+    __shared__ float2 lds[2][16];
     const NetTile t = net_tile(a.rows, sh, net_block());
     if (t.g < 0) return;
-    const int lane = threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : 256 / L, D = (int)a.D;
+    const int lane = WIDE ? threadIdx.x : threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : 256 / L,
+              D = (int)a.D;
     const T *ga = (const T *)a.gamma + t.g * a.p_stride;
     float sg[NIT][N], sb[NIT][N];
 #pragma unroll
@@ -179,47 +193,64 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a
 #pragma unroll
         for (int j = 0; j < N; ++j) sg[i][j] = sb[i][j] = 0.0f;
     const float inv = 1.0f / (float)D;
+    struct Row {
+        reg x[kHold ? NIT : 1], dy[kHold ? NIT : 1];
+        float mean, rstd;
+    };
+    const auto load = [&](Row &r, int64_t m) {
+        r.mean = r.rstd = 0.0f;
+        if (m >= t.hi) return;
+        if constexpr (kHold)
+#pragma unroll
+            for (int i = 0; i < NIT; ++i) {
+                const int c = lane + i * L;
+                if (c * N >= D) continue;
+                r.x[i] = load_early((const T *)a.x + m * a.ldx, c, D);
+                r.dy[i] = load_early((const T *)a.dy + m * a.ldy, c, D);
+            }
+        r.mean = a.mean_in[m];
+        r.rstd = a.rstd_in[m];
+    };
+    reg g[kGamma ? NIT : 1];
+    if constexpr (kGamma)
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if ((lane + i * L) * N < D) g[i] = load_chunk(ga, lane + i * L, D, (T)0.0f);
+    Row next;
+    if constexpr (kAhead) load(next, t.lo + slot);
     // every slot makes as many rounds (the row sums need all lanes)
-    for (int64_t m0 = t.lo; m0 < t.hi; m0 += slots) {
+    int turn = 0;
+    for (int64_t m0 = t.lo; m0 < t.hi; m0 += slots, turn ^= 1) {
         const int64_t m = m0 + slot;
         const bool live = m < t.hi;
         const T *x = (const T *)a.x + m * a.ldx, *dy = (const T *)a.dy + m * a.ldy;
-        typename NetVec<T>::reg xv[kHold ? NIT : 1], dv[kHold ? NIT : 1];
-        float mean = 0.0f, rstd = 0.0f, s1 = 0.0f, s2 = 0.0f;
-        if (live) {
-            mean = a.mean_in[m];
-            rstd = a.rstd_in[m];
+        Row r;
+        if constexpr (kAhead) {
+            r = next;
+            load(next, m + slots);
+        } else load(r, m);
+        float s1 = 0.0f, s2 = 0.0f;
+        if (live)
 #pragma unroll
             for (int i = 0; i < NIT; ++i) {
                 const int c = lane + i * L, k = kHold ? i : 0;
                 if (c * N >= D) continue;
-                xv[k] = load_chunk(x, c, D, (T)0.0f);
-                dv[k] = load_chunk(dy, c, D, (T)0.0f);
-                if constexpr (!kHold) {
-                    const auto gv = load_chunk(ga, c, D, (T)0.0f);
+                if constexpr (kHold) {
+                    settle(r.x[i], c, D, (T)0.0f);
+                    settle(r.dy[i], c, D, (T)0.0f);
+                } else {
+                    r.x[0] = load_chunk(x, c, D, (T)0.0f);
+                    r.dy[0] = load_chunk(dy, c, D, (T)0.0f);
+                }
+                if constexpr (!kGamma) g[0] = load_chunk(ga, c, D, (T)0.0f);
 #pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float p = (float)dv[k][j] * (float)gv[j];
-                        s1 += p;
-                        s2 = fmaf(p, ((float)xv[k][j] - mean) * rstd, s2);
-                    }
+                for (int j = 0; j < N; ++j) {
+                    const float p = (float)r.dy[k][j] * (float)g[kGamma ? i : 0][j];
+                    s1 += p;
+                    s2 = fmaf(p, ((float)r.x[k][j] - r.mean) * r.rstd, s2);
                 }
             }
-            if constexpr (kHold)
-#pragma unroll
-                for (int i = 0; i < NIT; ++i) {
-                    const int c = lane + i * L;
-                    if (c * N >= D) continue;
-                    const auto gv = load_chunk(ga, c, D, (T)0.0f);
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float p = (float)dv[i][j] * (float)gv[j];
-                        s1 += p;
-                        s2 = fmaf(p, ((float)xv[i][j] - mean) * rstd, s2);
-                    }
-                }
-        }
-        row_sum2<WIDE>(s1, s2, L, lds);
+        row_sum2<WIDE>(s1, s2, L, lds[turn]);
         if (!live) continue;
         s1 *= inv;
         s2 *= inv;
@@ -228,17 +259,17 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm_grad(NormArgs a
             const int c = lane + i * L, k = kHold ? i : 0;
             if (c * N >= D) continue;
             if constexpr (!kHold) {
-                xv[0] = load_chunk(x, c, D, (T)0.0f);
-                dv[0] = load_chunk(dy, c, D, (T)0.0f);
+                r.x[0] = load_chunk(x, c, D, (T)0.0f);
+                r.dy[0] = load_chunk(dy, c, D, (T)0.0f);
             }
-            const auto gv = load_chunk(ga, c, D, (T)0.0f);
-            typename NetVec<T>::reg out;
+            if constexpr (!kGamma) g[0] = load_chunk(ga, c, D, (T)0.0f);
+            reg out;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float h = ((float)xv[k][j] - mean) * rstd, d = (float)dv[k][j];
+                const float h = ((float)r.x[k][j] - r.mean) * r.rstd, d = (float)r.dy[k][j];
                 sg[i][j] = fmaf(d, h, sg[i][j]);
                 sb[i][j] += d;
-                out[j] = (T)(rstd * (fmaf(d, (float)gv[j], -s1) - h * s2));
+                out[j] = (T)(r.rstd * (fmaf(d, (float)g[kGamma ? i : 0][j], -s1) - h * s2));
             }
             if (a.dx) store_chunk<T, true>((T *)a.dx + m * a.lddx, c, D, out);
         }
@@ -401,7 +432,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256, WIDE && NIT <= 4 ? 8 : 1) void k
         t = net_tile(a.rows, sh, net_block());
         if (t.g < 0) return;
     }
-    const int lane = threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : blockDim.x / L,
+    const int lane = WIDE ? threadIdx.x : threadIdx.x & (L - 1), slot = WIDE ? 0 : threadIdx.x / L, slots = WIDE ? 1 : blockDim.x / L,
               C = (int)a.C;
     // narrow rows: the first one's logits are on their way while the labels are
     // counted (a wide row's registers would not last)
@@ -578,9 +609,9 @@ hipError_t launch_layernorm(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N, 4, 4);
-        const int64_t per = r.L <= 64 ? 256 / r.L : 1;
-        return with_shape<T>(r, [&](auto nit, auto wide) {
+        const RowShape r = row_shape<4>(a.D, NetVec<T>::N);
+        const int64_t per = r.wide ? 1 : 256 / r.L;
+        return with_shape<T, 4>(r, [&](auto nit, auto wide) {
             hipLaunchKernelGGL((k_layernorm<T, nit.v, wide.v>), net_grid((a.rows.M + per - 1) / per),
                                dim3(r.threads), 0, s, a, r.L);
         });
@@ -596,12 +627,12 @@ hipError_t launch_layernorm_grad(const NormArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.D, NetVec<T>::N, 2, sizeof(T) == 2 ? 1 : 2);
+        const RowShape r = row_shape<2>(a.D, NetVec<T>::N);
         const int sh = norm_tile_shift(a);
         const int64_t tiles = net_tiles(a.rows, sh);
         hipError_t e = hipSuccess;
         if (a.rows.M > 0)
-            e = with_shape<T>(r, [&](auto nit, auto wide) {
+            e = with_shape<T, 2>(r, [&](auto nit, auto wide) {
                 const size_t lds = wide.v ? 0 : sizeof(float) * 2 * nit.v * NetVec<T>::N * 3 * r.L;
                 hipLaunchKernelGGL((k_layernorm_grad<T, nit.v, wide.v>), net_grid(tiles), dim3(r.threads), lds, s,
                                    a, r.L, sh);
@@ -622,14 +653,14 @@ hipError_t launch_xent(const XentArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const RowShape r = row_shape(a.C, NetVec<T>::N, 4, 4);
+        const RowShape r = row_shape<4>(a.C, NetVec<T>::N);
         const bool whole = xent_whole(a);
         const int sh = xent_tile_shift(a);
         if (a.dz && !whole)
             hipLaunchKernelGGL(k_xent_count, net_grid(net_tiles(a.rows, kCountShift)), dim3(256), 0, s, a, sh);
         hipError_t e = hipSuccess;
         if (a.rows.M > 0 || whole)
-            e = with_shape<T>(r, [&](auto nit, auto wide) {
+            e = with_shape<T, 4>(r, [&](auto nit, auto wide) {
                 // no more threads than a whole network's rows keep busy
                 int threads = r.threads;
                 while (whole && !wide.v && threads > 64 && a.rows.n * r.L <= threads / 2) threads /= 2;
