@@ -638,20 +638,25 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
         // the tiles, for their reuse, where their padding (64 rows, outputs and k) is
         // not most of them (here / tiles, us: bf16 512x512 24 rows 39 / 38, 48 rows 52 / 44,
         // fp32 77 / 78, 157 / 83; 500 rows 256x32 bf16 11 / 10, fp32 24 / 30, 256x48 15 / 10,
-        // 38 / 30; 500 rows 64x300 24 / 28, 44 / 44, fp32 96x300 60 / 53)
-        if (mean > 24 && a.n_out > 32 && a.n_in >= (sizeof(T) == 2 ? 128 : 64))
+        // 38 / 30; 500 rows 64x300 24 / 28, 44 / 44, fp32 96x300 60 / 53), and where they are
+        // not too few for the chip (tiles of 64 a side: 128, one network's 512 rows
+        // 2048x1024, 18 / 22, 34 / 64; 192, 1024 rows 4096x768, 46 / 39, 93 / 118; 256, 1024 rows
+        // 1024x1024, 18 / 14, 35 / 37; 384, 1024 rows 2048x1536, 46 / 24, 95 / 64)
+        const bool wide = mean > 24 && a.n_out > 32 && a.n_in >= (sizeof(T) == 2 ? 128 : 64);
+        if (wide && net_tiles(a.rows, 6) * ((a.n_out + 63) / 64) > (sizeof(T) == 2 ? 128 : 256))
             return launch_linear_tiles<t.value>(a, s);
         // rows of a wave's tile by the mean rows per network (few k steps of 16 bits or
         // outputs: smaller tiles, more waves at a time: 200 rows 32x200 bf16 12.1, with 64 x
         // 32 13.0 us); one 16 x 16 tile where larger ones would leave most of the chip
-        // without a wave (one network's 3000 rows 512x24 9.3, 10.9 us)
+        // without a wave (one network's 3000 rows 512x24 9.3, 10.9 us; fp32 512 rows 2048x256,
+        // 128 tiles of 32 x 32, 17.6, 19.0; 4x128 rows 1024x512, 256 of them, 17.4, 12.4)
         const bool few_steps = a.n_in <= 2 * Mma<T>::KS && (sizeof(T) == 2 || a.n_out <= 16);
-        int rb = mean <= 16 ? 1 : mean <= 32 || few_steps ? 2 : 4, nb = rb == 1 || a.n_out <= 16 ? 1 : 2;
+        int rb = mean <= 16 ? 1 : mean <= 32 || few_steps || wide ? 2 : 4, nb = rb == 1 || a.n_out <= 16 ? 1 : 2;
         const int64_t steps = (a.n_in + Mma<T>::KS - 1) / Mma<T>::KS;
         const auto units_of = [&](int r, int n) {
             return net_tiles(a.rows, r == 1 ? 4 : r == 2 ? 5 : 6) * ((a.n_out + 16 * n - 1) / (16 * n));
         };
-        if (steps >= 16 && units_of(rb, nb) < 512) rb = nb = 1;
+        if (steps >= 16 && units_of(rb, nb) < 192) rb = nb = 1;
         const int sh = rb == 1 ? 4 : rb == 2 ? 5 : 6;
         const uint32_t out_tiles = (uint32_t)((a.n_out + 16 * nb - 1) / (16 * nb));
         const int64_t units = units_of(rb, nb);
