@@ -480,6 +480,160 @@ bool narrow(const LinearGradArgs &a)
 }
 
 // ---------------------------------------------------------------------------
+// The whole gradient of few inputs (up to 32) and more than 64 outputs in one pass:
+// a block takes 64 rows of a network and goes over the outputs 64 at a time.  d
+// passes through LDS as above, dx's sums stay in registers, and dw and db of the 64
+// rows are written at every step, as results or as the tile's sums; dy and z are
+// read once and d is never stored.  Bound by the slopes, the fp32 matrix cores (whose
+// tiles one input fills as 16 do) and the steps' barriers, 3.4 us a step at three to
+// four blocks per CU: bf16 300,000 rows 16x1109 with GELU 627 us, in separate passes
+// through the tiles 1199 (fp32 950, 2599); fp32 1408x51 rows 1x564 143, 399; bf16 856x581
+// rows 29x408 657, 682.  Where blocks are few and their steps many the tiles are
+// faster (bf16 16x334 rows 6x2204: 100 blocks of 35 steps 121, 60; 10x320 rows 8x945:
+// 60 of 15, 50, 51; 2000 rows 16x300: 32 of 5, 21, 44).
+// ---------------------------------------------------------------------------
+constexpr int kFewInputs = 32, kFewShift = 6;
+
+template <typename T, int TI>
+__global__ __launch_bounds__(256, 3) void k_linear_grad_few(LinearGradArgs a, float *part)
+{
+    constexpr int N = NetVec<T>::N, R = 1 << kFewShift, C = 64, CI = TI * 16 / N, CO = C / N, pi = TI * 16 + 4, po = C + 4,
+                  KD = R * CO / 256, KW = (C * CI + 255) / 256;
+    typedef typename NetVec<T>::reg reg;
+    __shared__ __attribute__((aligned(16))) float X[R * pi], W[C * pi], D[R * po];
+    __shared__ float join[256];
+    const NetTile t = net_tile(a.rows, kFewShift, net_block());
+    if (t.g < 0) return;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l16 = tid % 16, q = tid % 64 / 16,
+              ni = (int)a.n_in, no = (int)a.n_out, rows = (int)(t.hi - t.lo);
+    auto put = [&](float *row, int c, reg v) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4 *>(row + c * N + j) = (f32x4){(float)v[j], (float)v[j + 1], (float)v[j + 2], (float)v[j + 3]};
+    };
+    if (a.dw) {
+        const T *x = (const T *)a.x + (t.lo - (a.x_shared ? (int64_t)t.g * a.rows.n : 0)) * a.ldx;
+#pragma unroll
+        for (int k = tid; k < R * CI; k += 256) {
+            const int r = k / CI, c = k % CI;
+            put(X + r * pi, c, r < rows ? load_chunk(x + r * a.ldx, c, ni, (T)0.0f) : (reg){});
+        }
+    }
+    const T *w = (const T *)a.w + t.g * a.w_stride, *pd = (const T *)a.dy + t.lo * a.lddy, *pz = (const T *)a.z + t.lo * a.ldz;
+    reg dy[KD], z[KD], wv[KW];
+    // the next 64 outputs' d and weights, in flight over a step
+    const auto load = [&](int o0) {
+#pragma unroll
+        for (int u = 0; u < KD; ++u) {
+            const int r = (tid + u * 256) / CO, c = (tid + u * 256) % CO + o0 / N;
+            dy[u] = z[u] = (reg){};
+            if (r >= rows || c * N >= no) continue;
+            dy[u] = load_early(pd + r * a.lddy, c, no);
+            if (a.act != ACT_NONE) z[u] = load_early(pz + r * a.ldz, c, no);
+        }
+        if (a.dx)
+#pragma unroll
+            for (int u = 0; u < KW; ++u) {
+                const int o = (tid + u * 256) / CI + o0, c = (tid + u * 256) % CI;
+                wv[u] = (reg){};
+                if (tid + u * 256 < C * CI && o < no && c * N < ni) wv[u] = load_early(w + o * a.ldw, c, ni);
+            }
+    };
+    f32x4 dx[TI];
+#pragma unroll
+    for (int i = 0; i < TI; ++i) dx[i] = (f32x4)(0.0f);
+    float *sums = part + net_slot(t.lo, t.index, kFewShift) * no * (ni + 1);
+    load(0);
+#pragma unroll 1
+    for (int o0 = 0; o0 < no; o0 += C) {
+        if (o0 > 0) __syncthreads();
+#pragma unroll
+        for (int u = 0; u < KD; ++u) {
+            const int r = (tid + u * 256) / CO, c = (tid + u * 256) % CO;
+            settle(dy[u], c + o0 / N, no, (T)0.0f);
+            settle(z[u], c + o0 / N, no, (T)0.0f);
+            float v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = (float)z[u][j];
+            act_slopes<sizeof(T) == 2, N>(a.act, v);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] *= (float)dy[u][j];
+#pragma unroll
+            for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4 *>(D + r * po + c * N + j) = (f32x4){v[j], v[j + 1], v[j + 2], v[j + 3]};
+        }
+        if (a.dx)
+#pragma unroll
+            for (int u = 0; u < KW; ++u) {
+                const int o = (tid + u * 256) / CI, c = (tid + u * 256) % CI;
+                settle(wv[u], c, ni, (T)0.0f);
+                if (tid + u * 256 < C * CI) put(W + o * pi, c, wv[u]);
+            }
+        if (o0 + C < no) load(o0 + C);
+        __syncthreads();
+        if (a.dx) {
+            const float *d = D + (wave * 16 + l16) * po + 4 * q;
+#pragma unroll
+            for (int k = 0; k < C; k += 16) {
+                const f32x4 b = *reinterpret_cast<const f32x4 *>(d + k);
+#pragma unroll
+                for (int i = 0; i < TI; ++i) {
+                    f32x4 p;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = W[(k + 4 * q + e) * pi + i * 16 + l16];
+                    dx[i] = mma16(p, b, dx[i]);
+                }
+            }
+        }
+        const int o = o0 + wave * 16 + l16;
+        if (a.dw) {
+            f32x4 dw[TI];
+#pragma unroll
+            for (int i = 0; i < TI; ++i) dw[i] = (f32x4)(0.0f);
+#pragma unroll
+            for (int k = 0; k < R; k += 16) {
+                f32x4 d;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[e] = D[(k + 4 * q + e) * po + wave * 16 + l16];
+#pragma unroll
+                for (int i = 0; i < TI; ++i) {
+                    f32x4 p;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = X[(k + 4 * q + e) * pi + i * 16 + l16];
+                    dw[i] = mma16(p, d, dw[i]);
+                }
+            }
+            if (o < no)
+#pragma unroll
+                for (int i = 0; i < TI; ++i) {
+                    const int at = i * 16 + 4 * q;
+                    if (t.only) store_quad((T *)a.dw + t.g * a.dw_stride + o * a.lddw + at, ni - at, dw[i]);
+                    else store_quad(sums + (int64_t)o * ni + at, ni - at, dw[i]);
+                }
+        }
+        if (a.db) {
+            float s = 0.0f;
+#pragma unroll
+            for (int r = 0; r < R / 4; ++r) s += D[(tid / 64 * (R / 4) + r) * po + tid % 64];
+            join[tid] = s;
+            __syncthreads();
+            if (tid < C && o0 + tid < no) {
+                s += join[C + tid] + join[2 * C + tid] + join[3 * C + tid];
+                if (t.only) ((T *)a.db)[t.g * a.db_stride + o0 + tid] = (T)s;
+                else sums[(int64_t)no * ni + o0 + tid] = s;
+            }
+        }
+    }
+    const int m = wave * 16 + l16;
+    if (a.dx && m < rows)
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+            store_quad((T *)a.dx + (t.lo + m) * a.lddx + i * 16 + 4 * q, ni - (i * 16 + 4 * q), dx[i]);
+}
+bool few_inputs(const LinearGradArgs &a)
+{
+    return a.n_in <= kFewInputs && a.n_out > kNarrow && (a.n_out <= 12 * 64 || net_tiles(a.rows, kFewShift) >= 512);
+}
+
+// ---------------------------------------------------------------------------
 // Gradient products of a short sum: dx of few outputs (DW = false: rows m of a
 // tile, k the outputs) and dw of few rows per network (rows o, k the network's
 // rows).  Either is out[r][c] = sum_k p[k][c] q(r, k) with p and the result dense
@@ -613,9 +767,8 @@ struct GradScratch {
 GradScratch grad_layout(const LinearGradArgs &a)
 {
     GradScratch g;
-    if (narrow(a)) {
-        g.sums = 0;
-        g.end = 4 * (size_t)net_slots(a.rows.M, narrow_shift(a)) * (size_t)(a.n_out * (a.n_in + 1));
+    if (narrow(a) || few_inputs(a)) {
+        g.end = 4 * (size_t)net_slots(a.rows.M, few_inputs(a) ? kFewShift : narrow_shift(a)) * (size_t)(a.n_out * (a.n_in + 1));
         return g;
     }
     const size_t e = a.dtype == NET_F32 ? 4 : 2;
@@ -693,8 +846,8 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         const GradScratch l = grad_layout(a);
         const int64_t mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
         hipError_t e = hipSuccess;
-        if (narrow(a)) {
-            const int sh = narrow_shift(a);
+        if (narrow(a) || few_inputs(a)) {
+            const int sh = few_inputs(a) ? kFewShift : narrow_shift(a);
             float *part = (float *)a.scratch;
             auto go = [&](auto waves, auto f) {
                 const int64_t ti = (a.n_in + 15) / 16 * 16, to = (a.n_out + 15) / 16 * 16;
@@ -705,7 +858,14 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
             };
             if (a.rows.M > 0) {
                 using std::integral_constant;
-                if (mean <= 32) e = go(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+                const dim3 few = net_grid(net_tiles(a.rows, sh));
+                if (few_inputs(a) && a.n_in <= 16) {
+                    hipLaunchKernelGGL((k_linear_grad_few<T, 1>), few, dim3(256), 0, s, a, part);
+                    e = hipGetLastError();
+                } else if (few_inputs(a)) {
+                    hipLaunchKernelGGL((k_linear_grad_few<T, 2>), few, dim3(256), 0, s, a, part);
+                    e = hipGetLastError();
+                } else if (mean <= 32) e = go(integral_constant<int, 2>{}, integral_constant<int, 1>{});
                 else if (mean > 128 && a.n_in <= 16 && a.n_out <= 16) e = go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
                 else e = go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
             }

@@ -293,7 +293,9 @@ inline bool net_single(const NetRows &r, int sh) { return r.off ? r.M <= ((int64
 // out(g, e, sum) for the networks of several tiles and those without rows (sum
 // 0): E elements by S shares of the tiles per block, 64 by 4, or 16 by 64 where
 // networks have more than 64 tiles on average (the narrow gradient of 500,000 rows
-// 32x32 of one network, 1954 tiles of 1056 elements: 76 us, 123 with 64 by 4).
+// 32x32 of one network, 1954 tiles of 1056 elements: 76 us, 123 with 64 by 4).  A
+// block takes several networks' where there would be more than 8192 blocks
+// (bf16 gradient of 517 networks' 38 rows 29x3006: 544 us, 679 with one per block).
 template <typename F, int E, int S>
 __global__ __launch_bounds__(E * S) void k_net_sums(NetRows rows, const float *part, int64_t width, int sh, F out)
 {
@@ -324,7 +326,8 @@ template <typename F>
 hipError_t launch_net_sums(const NetRows &rows, const float *part, int64_t width, int sh, hipStream_t s, F out)
 {
     const bool many = (rows.M >> sh) / rows.G > 64;
-    const dim3 grid((unsigned)((width + (many ? 15 : 63)) / (many ? 16 : 64)), (unsigned)(rows.G < 32768 ? rows.G : 32768));
+    const int64_t x = (width + (many ? 15 : 63)) / (many ? 16 : 64), most = x < 8192 ? 8192 / x : 1;
+    const dim3 grid((unsigned)x, (unsigned)(rows.G < most ? rows.G : most));
     if (many) hipLaunchKernelGGL((k_net_sums<F, 16, 64>), grid, dim3(1024), 0, s, rows, part, width, sh, out);
     else hipLaunchKernelGGL((k_net_sums<F, 64, 4>), grid, dim3(256), 0, s, rows, part, width, sh, out);
     return hipGetLastError();
