@@ -312,9 +312,10 @@ struct GradSums {
 // time d = dy act'(z) (not rounded: all of it is fp32 here) and x pass through
 // LDS into the fp32 matrix cores; every operand is read once and dx written
 // once.  Blocks of two waves for up to 32 rows per network, else four (two / four:
-// fp32 32x32 8 rows 90 / 147 us, 32 rows 33 / 44, 64 rows 23 / 25, 200 rows 35 / 27).  Wave w has rows 16 F w .. + 16 F of dx, and of the dw tiles every WAVES-th;
-// with widths up to 16 (F = 4) its own rows' share of the one dw tile (1.8M rows 8x1
-// 120 us, F = 1: 149).  fp32
+// fp32 32x32 8 rows 90 / 147 us, 32 rows 33 / 44, 64 rows 23 / 25, 200 rows 35 / 27).
+// Wave w has rows 16 F w .. + 16 F of dx, and of the dw tiles every WAVES-th; with widths
+// up to 16 (F = 4) its own rows' share of the one dw tile (1.8M rows 8x1
+// 89 us; before whole chunks of padding were left out 120, with F = 1 149).  fp32
 // 4096x32 rows 32x32: 101 MB in 30 us, floor 16; three to four waves per SIMD (LDS
 // and registers) each wait for three loads in a row.  In separate passes through
 // the 64-tiles it took 72 us; W's and x's loads ahead of d's cost as much in
@@ -334,14 +335,23 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
               po = to * 16 + 4;
     float *W = lds, *X = W + (a.dx ? to * 16 * pi : 0), *D = X + R * pi;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l16 = tid % 16, q = tid % 64 / 16;
-    // n elements of a row of the type (or zeros) to a row of LDS, padded with zeros to whole tiles
+    // a chunk of a row of the type to a row of LDS
     auto put = [&](float *row, int c, reg v) {
 #pragma unroll
         for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4 *>(row + c * N + j) = (f32x4){(float)v[j], (float)v[j + 1], (float)v[j + 2], (float)v[j + 3]};
     };
     // (k / ci and k / co by a multiplication, exact for k < 65536 / 15)
-    const int ci = ti * 16 / N, co = to * 16 / N, mi = (65535 + ci) / ci, mo = (65535 + co) / co,  // chunks per padded row
-              shares = TH / (to * 16);                                                           // threads per column
+    // chunks per row: in blocks of many rows those that hold anything, the tiles' padding
+    // being zero once and for all (1.8M rows 8x1 142 -> 89 us; of one or two rounds
+    // 4096x32 rows 31x20 31 -> 33, so not there)
+    const bool skip = t.hi - t.lo > 2 * R;
+    const int ci = skip ? (ni + N - 1) / N : ti * 16 / N, co = skip ? (no + N - 1) / N : to * 16 / N, mi = (65535 + ci) / ci,
+              mo = (65535 + co) / co, shares = TH / (to * 16);  // threads per column
+    if (skip) {
+        f32x4 *const all = reinterpret_cast<f32x4 *>(lds);
+        for (int k = tid; k < ((int)(X - lds) + R * (pi + po)) / 4; k += TH) all[k] = (f32x4)(0.0f);
+        __syncthreads();
+    }
     if (a.dx) {
         const T *w = (const T *)a.w + t.g * a.w_stride;
 #pragma unroll 2
@@ -465,11 +475,12 @@ __global__ __launch_bounds__(64 * WAVES, 3) void k_linear_grad_narrow(LinearGrad
 
 // Rows per tile of the narrow gradient, as a power of two: about 2048 tiles, of
 // 64 .. 4096 rows; whole networks of up to 4096 where these are enough for the chip
-// (their results need no sums).
-int narrow_shift(const LinearGradArgs &a)
+// (their results need no sums).  least: the fewest rows with or without offsets, for
+// the scratch's size, which is asked for without them.
+int narrow_shift(const LinearGradArgs &a, bool least = false)
 {
     int sh = 6;
-    while (sh < 12 && ((a.rows.M >> sh) > 2048 || (!a.rows.off && a.rows.G >= 512 && a.rows.n > (int64_t)1 << sh))) ++sh;
+    while (sh < 12 && ((a.rows.M >> sh) > 2048 || (!least && !a.rows.off && a.rows.G >= 512 && a.rows.n > (int64_t)1 << sh))) ++sh;
     return sh;
 }
 // 16 bits, both widths above 48: the tiles' 16-bit products are faster than fp32
@@ -630,7 +641,7 @@ __global__ __launch_bounds__(256, 3) void k_linear_grad_few(LinearGradArgs a, fl
 }
 bool few_inputs(const LinearGradArgs &a)
 {
-    return a.n_in <= kFewInputs && a.n_out > kNarrow && (a.n_out <= 12 * 64 || net_tiles(a.rows, kFewShift) >= 512);
+    return a.n_in <= kFewInputs && a.n_out > kNarrow && (a.n_out <= 12 * 64 || (a.rows.M >> kFewShift) + a.rows.G >= 512);
 }
 
 // ---------------------------------------------------------------------------
@@ -768,7 +779,7 @@ GradScratch grad_layout(const LinearGradArgs &a)
 {
     GradScratch g;
     if (narrow(a) || few_inputs(a)) {
-        g.end = 4 * (size_t)net_slots(a.rows.M, few_inputs(a) ? kFewShift : narrow_shift(a)) * (size_t)(a.n_out * (a.n_in + 1));
+        g.end = 4 * (size_t)net_slots(a.rows.M, few_inputs(a) ? kFewShift : narrow_shift(a, true)) * (size_t)(a.n_out * (a.n_in + 1));
         return g;
     }
     const size_t e = a.dtype == NET_F32 ? 4 : 2;
@@ -890,11 +901,13 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         const void *dd = own ? d : a.dy;
         const int64_t ldd = own ? l.ldd : a.lddy;
         float *part = (float *)((char *)a.scratch + l.part);
-        // short sums: of few outputs (dx) or rows (dw); else tiles
+        // short sums: of few outputs (dx) or rows (dw; in fp32 dx too, whose tiles would
+        // split every weight for two rows: 207x2 rows 3496x386 521 us, 611 in tiles, 1500x2 rows
+        // 520x300 428, 547; bf16 1500x1 rows 100x300 312, 98, others even); else tiles
         int L = 1;
         while (L < 256 && L * N < a.n_in) L *= 2;
         const int64_t cols = (a.n_in + L * N - 1) / (L * N);
-        if (a.dx && a.n_out <= kShortOutputs && a.n_in >= 64) {
+        if (a.dx && (a.n_out <= kShortOutputs || (sizeof(T) == 4 && mean <= kShortMean)) && a.n_in >= 64) {
             const int64_t units = net_tiles(a.rows, kShortShift);
             hipLaunchKernelGGL((k_linear_short<T, false>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, ldd,
                                L, units);

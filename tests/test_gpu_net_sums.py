@@ -15,6 +15,7 @@ LAYERS = [([70_000], 9, 130, "tanh", False), ([30_000, 0, 17, 1500], 20, 24, "ge
           ([128] * 600, 16, 16, "silu", True), ([70] * 520, 40, 33, "tanh", True), ([300, 0, 41] * 4, 64, 64, "gelu", False),
           ([300, 0, 41] * 4, 48, 64, "relu", False), ([1] * 5, 4100, 40, "none", False), ([7, 0, 20], 2100, 33, "silu", False),
           ([30, 32] * 3, 600, 100, "none", False), ([26, 40], 70, 120, "tanh", False), ([3000], 1100, 18, "gelu", False),
+          ([600] * 512, 8, 1, "tanh", True), ([150] * 520, 20, 24, "silu", True), ([140] * 515, 5, 33, "gelu", False),
           ([300, 0, 41, 64, 1] * 3, 18, 200, "gelu", False), ([70] * 40, 1, 77, "none", False), ([5000], 16, 700, "silu", False), ([33_000], 20, 1109, "gelu", False),
           ([128] * 4, 32, 65, "tanh", True), ([64] * 5, 7, 130, "relu", True), ([2] * 30, 9, 300, "silu", False)]
 
