@@ -251,16 +251,23 @@ def evox_sgemm(A, B, C, trans_a=False, trans_b=False, alpha=1.0, beta=0.0, strea
 # tensor and name what is wrong only once something is.
 # ---------------------------------------------------------------------------
 _DTYPES = {}
+_FLOAT, _INT = "float32", "int32"  # vectors' types, by name: torch is imported with the first call
 
 
 def _dtype(t):
-    """The element type's id."""
+    """The element type's id of a tensor on the GPU."""
     if not _DTYPES:
         import torch
         _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+        _DTYPES.update({_FLOAT: torch.float32, _INT: torch.int32})
+        # the current stream's handle without its object (3 us), where torch has it
+        raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+        _DTYPES["stream"] = (lambda: raw(device())) if raw and device else lambda: torch.cuda.current_stream().cuda_stream
     d = _DTYPES.get(t.dtype)
     if d is None:
         raise EvoxError(EINVAL, f"element type {t.dtype}: float32, bfloat16 or float16")
+    if t.get_device() < 0:
+        raise EvoxError(EINVAL, f"a tensor on {t.device}: the kernels read the GPU's memory")
     return d
 
 
@@ -284,15 +291,14 @@ def _vector(what, t, dtype, n, like):
     """Checks a dense vector (or None) of n elements on like's device.  Its address."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != like.get_device() or not t.is_contiguous():
+    if t.dtype is not _DTYPES[dtype] or t.shape != (n,) or t.get_device() != like.get_device() or not t.is_contiguous():
         raise EvoxError(EINVAL, f"{what}: a dense {dtype} tensor of {n} on {like.device}")
     return t.data_ptr()
 
 
 def _pitch(t):
     """The row pitch of an [M, n] tensor (of one row, or none: n)."""
-    shape = t.shape
-    return t.stride(-2) if shape[-2] > 1 else shape[-1]
+    return t.stride(-2) if t.size(-2) > 1 else t.size(-1)
 
 
 def _net_stride(t):
@@ -300,27 +306,20 @@ def _net_stride(t):
 
 
 def _offsets(off, like, G):
-    import torch
-    return _vector("off", off, torch.int32, G + 1, like)
+    return _vector("off", off, _INT, G + 1, like)
 
 
 def _raw_stream(stream):
     """The HIP stream of a call: the given one, or the current one of the current device."""
-    import torch
-    if stream is not None:
-        return stream.cuda_stream
-    try:  # what torch.cuda.current_stream().cuda_stream returns, without the object (3 us)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-    except AttributeError:
-        return torch.cuda.current_stream().cuda_stream
+    return _DTYPES["stream"]() if stream is None else stream.cuda_stream
 
 
 def _scratch(nbytes, like, scratch, stream):
     """The caller's scratch, or one of this size that lives until the stream is done with it."""
-    import torch
     if nbytes == 0:
         _check(EINVAL)
     if scratch is None:
+        import torch
         scratch = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
         if stream is not None:
             scratch.record_stream(stream)
@@ -331,6 +330,15 @@ def _scratch(nbytes, like, scratch, stream):
 
 def _layer(x, w, y, act, off):
     """The layer of weights w [G, n_out, n_in] between x and y (or dy)."""
+    # one pass for what most calls are; anything else is checked and named below
+    d, dev = _dtype(w), w.get_device()
+    ws, xs, ys, wt, xt, yt = w.shape, x.shape, y.shape, w.stride(), x.stride(), y.stride()
+    if (len(ws) == 3 and len(xs) == 2 and len(ys) == 2 and x.dtype is w.dtype and y.dtype is w.dtype
+            and x.get_device() == dev and y.get_device() == dev and wt[2] == 1 and xt[1] == 1 and yt[1] == 1):
+        (G, n_out, n_in), (R, k), (M, n) = ws, xs, ys
+        shared = off is None and G > 1 and R != M
+        if G > 1 and n_out > 1 and R > 1 and M > 1 and k == n_in and n == n_out and (R * G if shared else R) == M:
+            return Layer(d, act, G, M, n_in, n_out, _offsets(off, w, G), shared, xt[0], wt[1], wt[0], 0, 0, 0, yt[0])
     if w.dim() != 3 or x.dim() != 2 or y.dim() != 2:
         raise EvoxError(EINVAL, "w must be [G, n_out, n_in], x and y [rows, n]")
     (G, n_out, n_in), M = w.shape, y.shape[0]
@@ -413,7 +421,6 @@ def _norm(x, gamma, off, eps):
 def evox_layernorm(x, gamma, beta, y, mean=None, rstd=None, off=None, eps=1e-5, stream=None):
     """y = (x - mean) rstd gamma_g + beta_g over the rows of x [M, D], with gamma and
     beta [G, D]; mean and rstd (float32 [M]) receive the rows' statistics."""
-    import torch
     p = _norm(x, gamma, off, eps)
     _view("beta", beta, x, gamma.shape)
     _view("y", y, x, x.shape)
@@ -421,8 +428,8 @@ def evox_layernorm(x, gamma, beta, y, mean=None, rstd=None, off=None, eps=1e-5, 
         raise EvoxError(EINVAL, "gamma and beta have different strides")
     p.ldy = _pitch(y)
     _check(lib().evox_layernorm(ctypes.byref(p), x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), y.data_ptr(),
-                                _vector("mean", mean, torch.float32, p.M, x),
-                                _vector("rstd", rstd, torch.float32, p.M, x), _raw_stream(stream)))
+                                _vector("mean", mean, _FLOAT, p.M, x), _vector("rstd", rstd, _FLOAT, p.M, x),
+                                _raw_stream(stream)))
     return y
 
 
@@ -437,7 +444,6 @@ def evox_layernorm_grad_scratch(x, gamma):
 def evox_layernorm_grad(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=None, off=None, scratch=None,
                         stream=None):
     """The gradient of evox_layernorm: dx [M, D], dgamma and dbeta [G, D], where given."""
-    import torch
     p = _norm(x, gamma, off, 1.0)
     dy_at = _view("dy", dy, x, x.shape)
     dx_at = _view("dx", dx, x, x.shape)
@@ -452,8 +458,8 @@ def evox_layernorm_grad(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=No
             raise EvoxError(EINVAL, "dgamma and dbeta have different strides")
     scratch, nbytes = _scratch(lib().evox_layernorm_grad_scratch_bytes(ctypes.byref(p)), x, scratch, stream)
     _check(lib().evox_layernorm_grad(ctypes.byref(p), x.data_ptr(), gamma.data_ptr(),
-                                     _vector("mean", mean, torch.float32, p.M, x),
-                                     _vector("rstd", rstd, torch.float32, p.M, x), dy_at, dx_at, dg_at, db_at,
+                                     _vector("mean", mean, _FLOAT, p.M, x),
+                                     _vector("rstd", rstd, _FLOAT, p.M, x), dy_at, dx_at, dg_at, db_at,
                                      scratch.data_ptr(), nbytes, _raw_stream(stream)))
     return dx, dgamma, dbeta
 
@@ -478,13 +484,13 @@ def evox_xent(logits, labels, fit, dz=None, off=None, scratch=None, stream=None)
     """fit[g] = mean cross-entropy of network g's rows of logits [M, C] against labels
     (int32 [M], or [M / G]: the same for every network; rows whose label is outside
     0 .. C-1 do not count), and its gradient dz [M, C] where given."""
-    import torch
+    _dtype(logits)
     if fit.dim() != 1 or labels.dim() != 1:
         raise EvoxError(EINVAL, "fit and labels are vectors")
     G, M = fit.shape[0], logits.shape[0]
     shared = off is None and G > 1 and labels.shape[0] != M
-    fit_at = _vector("fit", fit, torch.float32, G, logits)
-    labels_at = _vector("labels", labels, torch.int32, M // G if shared else M, logits)
+    fit_at = _vector("fit", fit, _FLOAT, G, logits)
+    labels_at = _vector("labels", labels, _INT, M // G if shared else M, logits)
     p = _classes(logits, G, off, shared)
     dz_at = _view("dz", dz, logits, logits.shape)
     if dz is not None:

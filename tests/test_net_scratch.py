@@ -1,5 +1,5 @@
 """Scratch sizes: what the query answers covers a call with and without offsets
-(host arithmetic only)."""
+(host arithmetic only).  And tensors that are not on the GPU are refused."""
 import ctypes
 import os
 
@@ -32,3 +32,15 @@ def test_scratch_without_offsets(evox, G, M):
             a = [L.evox_layernorm_grad_scratch_bytes(ctypes.byref(evox.Norm(dt, G, M, D, off, D, D, D, D, D, 1e-5)))
                  for off in (None, P)]
             assert a[0] == a[1] > 0, (G, M, D, a)
+
+
+def test_tensors_of_the_host_are_refused(evox):
+    import torch
+    x, w, y, v = torch.zeros(6, 4), torch.zeros(2, 3, 4), torch.zeros(6, 3), torch.zeros(6)
+    for call in (lambda: evox.evox_linear(x, w, y), lambda: evox.evox_linear_grad(x, w, y, dx=x),
+                 lambda: evox.evox_linear_grad_scratch(x, w, y),
+                 lambda: evox.evox_layernorm(x, x[:2], x[:2], x), lambda: evox.evox_layernorm_grad(x, x[:2], v, v, x, dx=x),
+                 lambda: evox.evox_xent(x, torch.zeros(6, dtype=torch.int32), v[:2])):
+        with pytest.raises(evox.EvoxError) as e:
+            call()
+        assert e.value.args
