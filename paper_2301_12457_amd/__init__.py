@@ -301,6 +301,14 @@ def _pitch(t):
     return t.stride(-2) if t.size(-2) > 1 else t.size(-1)
 
 
+def _dense(what, t):
+    """The row pitch of an [M, n] tensor, whose rows have to be dense."""
+    (M, n), s = t.shape, t.stride()
+    if s[1] != 1:
+        _view(what, t, t, t.shape)
+    return s[0] if M > 1 else n
+
+
 def _net_stride(t):
     return t.stride(0) if t.shape[0] > 1 else 0
 
@@ -412,10 +420,9 @@ def evox_linear_grad(x, w, dy, z=None, dx=None, dw=None, db=None, off=None, act=
 def _norm(x, gamma, off, eps):
     if x.dim() != 2 or gamma.dim() != 2:
         raise EvoxError(EINVAL, "x must be [M, D], gamma [G, D]")
-    (M, D), G = x.shape, gamma.shape[0]
-    _view("x", x, x, x.shape)
+    (M, D), G, d = x.shape, gamma.shape[0], _dtype(x)
     _view("gamma", gamma, x, (G, D))
-    return Norm(_dtype(x), G, M, D, _offsets(off, x, G), _pitch(x), 0, 0, _net_stride(gamma), 0, eps)
+    return Norm(d, G, M, D, _offsets(off, x, G), _dense("x", x), 0, 0, _net_stride(gamma), 0, eps)
 
 
 def evox_layernorm(x, gamma, beta, y, mean=None, rstd=None, off=None, eps=1e-5, stream=None):
@@ -467,9 +474,8 @@ def evox_layernorm_grad(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=No
 def _classes(logits, G, off, shared):
     if logits.dim() != 2:
         raise EvoxError(EINVAL, "logits must be [M, C]")
-    M, C = logits.shape
-    _view("logits", logits, logits, logits.shape)
-    return Classes(_dtype(logits), G, M, C, _offsets(off, logits, G), shared, _pitch(logits), 0)
+    (M, C), d = logits.shape, _dtype(logits)
+    return Classes(d, G, M, C, _offsets(off, logits, G), shared, _dense("logits", logits), 0)
 
 
 def evox_xent_scratch(logits, fit):
@@ -484,14 +490,13 @@ def evox_xent(logits, labels, fit, dz=None, off=None, scratch=None, stream=None)
     """fit[g] = mean cross-entropy of network g's rows of logits [M, C] against labels
     (int32 [M], or [M / G]: the same for every network; rows whose label is outside
     0 .. C-1 do not count), and its gradient dz [M, C] where given."""
-    _dtype(logits)
     if fit.dim() != 1 or labels.dim() != 1:
         raise EvoxError(EINVAL, "fit and labels are vectors")
     G, M = fit.shape[0], logits.shape[0]
     shared = off is None and G > 1 and labels.shape[0] != M
+    p = _classes(logits, G, off, shared)
     fit_at = _vector("fit", fit, _FLOAT, G, logits)
     labels_at = _vector("labels", labels, _INT, M // G if shared else M, logits)
-    p = _classes(logits, G, off, shared)
     dz_at = _view("dz", dz, logits, logits.shape)
     if dz is not None:
         p.lddz = _pitch(dz)
