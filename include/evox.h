@@ -565,8 +565,9 @@ int evox_linear(const evox_layer *layer, const void *x, const void *w, const voi
  * it, unused for EVOX_ACT_NONE):
  *     dx = d W_g;   dW_g = d^T x and db_g = sum of d over the rows of g
  * (zero for a network without rows); the residual's gradient is dy itself.
- * relu has slope 0 at 0.  Any of dx, dw, db may be null.  In 16 bits d is
- * rounded once to the element type before the products.  EVOX_EINVAL for dx
+ * relu has slope 0 at 0.  Any of dx, dw, db may be null.  d is not rounded to
+ * 16 bits: it keeps at least twice the element type's bits, in f16 down to
+ * 2^-35 and beyond the type's largest number.  EVOX_EINVAL for dx
  * with x_shared (data has no gradient), and for w_stride = 0 with G > 1
  * (give the one network's rows as G = 1).  scratch: device,
  * evox_linear_grad_scratch_bytes(layer) bytes, 256-byte aligned. */

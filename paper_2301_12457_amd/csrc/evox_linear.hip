@@ -201,18 +201,22 @@ __global__ __launch_bounds__(256) void k_linear_thin(LinearArgs a, int sh, uint3
     }
 }
 
-// d = dy act'(z), rounded to the element type (where a.act is not none and a
-// product needs it), and the tiles' column sums of the unrounded d (where db is
+// d = dy act'(z) in the element type (where a.act is not none and a
+// product needs it), and the tiles' column sums of d in fp32 (where db is
 // wanted): a block takes 2^sh rows of a network and L chunks of 16 bytes of their
 // columns, and adds its 256 / L row slots in order.  Apart from
 // the products, so that a slope is computed once per element and not once per
-// tile that reads it; rounding d, as the 16-bit products have to, costs the
-// gradient as much as one more rounding of dy (relative rms against 64 bits 2.3e-3
-// in bf16, 1.7e-3 without).  bf16 32,768 rows of 1024 with GELU: 50 us, 4.0 TB/s,
-// bound by the slopes' arithmetic and the wait for two loads; in the dx and dw
-// tiles' own loads the slopes would be computed 8 times over there.  L: the most
-// lanes among those that leave the fewest idle; 2^sh: 16 rows, up to 256 where there
-// are more than 4096 blocks (300,000 rows of 1109: 18,750 tiles took 671 us to join).
+// tile that reads it.  In 16 bits d leaves as two numbers of the type (d_split; of
+// relu's d, dy or 0, one holds all), whose products are added: rounded to one, it
+// would put an error of sqrt(K) roundoffs into every sum of K terms, however small
+// the sum (relative rms of the bf16 gradient against 64 bits 2.3e-3 instead of
+// 1.7e-3, the results' own rounding).  That costs the products twice their time:
+// bf16 64x512 ragged rows 1024x1024 with GELU 450 us, 287 in one number.  bf16 32,768
+// rows of 1024 with GELU: 54 us, 5.0 TB/s (50 for one number), bound by the slopes'
+// arithmetic and the wait for two loads; in the dx and dw tiles' own loads the slopes
+// would be computed 8 times over there.  L: the most lanes among those that leave the
+// fewest idle; 2^sh: 16 rows, up to 256 where there are more than 4096 blocks (300,000
+// rows of 1109: 18,750 tiles took 671 us to join).
 struct DzShape {
     int sh, L;
     int64_t cols;  // blocks per row
@@ -230,7 +234,8 @@ DzShape dz_shape(const LinearGradArgs &a)
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int sh, int L, int64_t cols, T *d, int64_t ldd, float *sums)
+__global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int sh, int L, int64_t cols, T *d, T *low, int64_t ldd,
+                                                     float *sums)
 {
     constexpr int N = NetVec<T>::N;
     typedef typename NetVec<T>::reg reg;
@@ -259,14 +264,23 @@ __global__ __launch_bounds__(256) void k_linear_dz(LinearGradArgs a, int sh, int
 #pragma unroll
             for (int j = 0; j < N; ++j) v[j] = (float)z[j];
             act_slopes<sizeof(T) == 2, N>(a.act, v);
-            reg out;
+            reg out, rest;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 v[j] *= (float)dy[j];
                 s[j] += v[j];
                 out[j] = (T)v[j];
             }
+            if (low)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    T h, l;
+                    d_split(v[j], h, l);
+                    out[j] = h;
+                    rest[j] = l;
+                }
             if (d) store_chunk(d + m * ldd, c, n, out);
+            if (low) store_chunk(low + m * ldd, c, n, rest);
         }
     if (!sums) return;
     if (slot > 0)
@@ -483,8 +497,9 @@ int narrow_shift(const LinearGradArgs &a, bool least = false)
     while (sh < 12 && ((a.rows.M >> sh) > 2048 || (!least && !a.rows.off && a.rows.G >= 512 && a.rows.n > (int64_t)1 << sh))) ++sh;
     return sh;
 }
-// 16 bits, both widths above 48: the tiles' 16-bit products are faster than fp32
-// ones (bf16 100x1000 rows 64x64 45 us, here 60; 64x48 51, here 50).
+// 16 bits, both widths above 48: the tiles' 16-bit products are no slower than fp32
+// ones (bf16 100x1000 rows 64x64 without an activation 45 us, with tanh 58, here 60;
+// 64x48 51 without, here 50).
 bool narrow(const LinearGradArgs &a)
 {
     return a.n_in <= kNarrow && a.n_out <= kNarrow && (a.dtype == NET_F32 || a.n_in <= 48 || a.n_out <= 48);
@@ -498,10 +513,12 @@ bool narrow(const LinearGradArgs &a)
 // read once and d is never stored.  Bound by the slopes, the fp32 matrix cores (whose
 // tiles one input fills as 16 do) and the steps' barriers, 3.4 us a step at three to
 // four blocks per CU: bf16 300,000 rows 16x1109 with GELU 627 us, in separate passes
-// through the tiles 1199 (fp32 950, 2599); fp32 1408x51 rows 1x564 143, 399; bf16 856x581
-// rows 29x408 657, 682.  Where blocks are few and their steps many the tiles are
-// faster (bf16 16x334 rows 6x2204: 100 blocks of 35 steps 121, 60; 10x320 rows 8x945:
-// 60 of 15, 50, 51; 2000 rows 16x300: 32 of 5, 21, 44).
+// through the tiles 1199 with d in one number (fp32 950, 2599); fp32 1408x51 rows 1x564
+// 143, 399; bf16 856x581 rows 29x408 657, 682.  Where blocks are few and their steps
+// many the tiles are faster: in 16 bits from more than 16 steps on (bf16 with tanh
+// 16x334 rows 6x2204, 100 blocks of 35 steps, 108, 92; 10x320 rows 8x945, 60 of 15, 44,
+// 76, without an activation 40, 41; 8x1280, 20 steps, 55, 59, without 50, 36), in fp32
+// from 12.
 // ---------------------------------------------------------------------------
 constexpr int kFewInputs = 32, kFewShift = 6;
 
@@ -641,7 +658,8 @@ __global__ __launch_bounds__(256, 3) void k_linear_grad_few(LinearGradArgs a, fl
 }
 bool few_inputs(const LinearGradArgs &a)
 {
-    return a.n_in <= kFewInputs && a.n_out > kNarrow && (a.n_out <= 12 * 64 || (a.rows.M >> kFewShift) + a.rows.G >= 512);
+    const int64_t steps = a.dtype == NET_F32 ? 12 : 16;
+    return a.n_in <= kFewInputs && a.n_out > kNarrow && (a.n_out <= steps * 64 || (a.rows.M >> kFewShift) + a.rows.G >= 512);
 }
 
 // ---------------------------------------------------------------------------
@@ -657,7 +675,7 @@ bool few_inputs(const LinearGradArgs &a)
 constexpr int kShortRows = 16, kShortShift = 4, kShortOutputs = 8, kShortMean = 4;
 
 template <typename T, bool DW>
-__global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T *d, int64_t ldd, int L, int64_t units)
+__global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T *d, const T *low, int64_t ldd, int L, int64_t units)
 {
     constexpr int N = NetVec<T>::N;
     typedef typename NetVec<T>::reg reg;
@@ -667,7 +685,7 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
     if (unit >= units) return;
     int g, R;
     int64_t K;
-    const T *p, *q;
+    const T *p, *q, *ql;
     T *out;
     int64_t ldp, ldo;
     if constexpr (DW) {
@@ -681,6 +699,7 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
         p = (const T *)a.x + (a.x_shared ? 0 : lo) * a.ldx;
         ldp = a.ldx;
         q = d + lo * ldd + o0;
+        ql = low ? low + lo * ldd + o0 : nullptr;
         out = (T *)a.dw + g * a.dw_stride + o0 * a.lddw;
         ldo = a.lddw;
     } else {
@@ -691,10 +710,16 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
         p = (const T *)a.w + t.g * a.w_stride;
         ldp = a.ldw;
         q = d + t.lo * ldd;
+        ql = low ? low + t.lo * ldd : nullptr;
         out = (T *)a.dx + t.lo * a.lddx;
         ldo = a.lddx;
     }
     if (c * N >= ni) return;
+    // up to four of d's neighbours
+    const auto load_d = [&](int64_t at, int n) -> f32x4 {
+        const f32x4 h = load_quad(q + at, n);
+        return ql ? h * d_up<T> + load_quad(ql + at, n) * d_down<T> : h;
+    };
     for (int r0 = slot * 4; r0 < R; r0 += slots * 4) {
         float acc[4][N];
 #pragma unroll
@@ -711,8 +736,8 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
             for (int e = 0; e < 4; ++e) pv[e] = e < left ? load_chunk(p + (k + e) * ldp, c, ni, (T)0.0f) : (reg){};
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if constexpr (DW) qv[e] = e < left ? load_quad(q + (k + e) * ldd + r0, rows) : (f32x4)(0.0f);
-                else qv[e] = e < rows ? load_quad(q + (r0 + e) * ldd + k, left) : (f32x4)(0.0f);
+                if constexpr (DW) qv[e] = e < left ? load_d((k + e) * ldd + r0, rows) : (f32x4)(0.0f);
+                else qv[e] = e < rows ? load_d((r0 + e) * ldd + k, left) : (f32x4)(0.0f);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -769,11 +794,11 @@ __global__ __launch_bounds__(256) void k_linear_join(NetRows rows, const float *
     }
 }
 
-// The scratch: d, then the tiles' column sums, then the partial products; of narrow
-// layers, the tiles' sums.
+// The scratch: d (in 16 bits its two numbers, for any activation), then the tiles'
+// column sums, then the partial products; of narrow layers, the tiles' sums.
 struct GradScratch {
     int64_t ldd = 0;
-    size_t sums = 0, part = 0, end = 0;
+    size_t low = 0, sums = 0, part = 0, end = 0;
 };
 GradScratch grad_layout(const LinearGradArgs &a)
 {
@@ -784,7 +809,8 @@ GradScratch grad_layout(const LinearGradArgs &a)
     }
     const size_t e = a.dtype == NET_F32 ? 4 : 2;
     g.ldd = (a.n_out + 7) / 8 * 8;
-    g.sums = (e * (size_t)a.rows.M * (size_t)g.ldd + 255) / 256 * 256;
+    g.low = (e * (size_t)a.rows.M * (size_t)g.ldd + 255) / 256 * 256;
+    g.sums = a.dtype == NET_F32 ? g.low : 2 * g.low;
     g.part = (g.sums + 4 * (size_t)net_slots(a.rows.M, dz_shape(a).sh) * (size_t)a.n_out + 255) / 256 * 256;
     const size_t dx = dx_splits(a) > 1 ? (size_t)dx_splits(a) * (size_t)a.rows.M * (size_t)a.n_in : 0;
     const size_t dw = dw_splits(a) > 1 ? (size_t)dw_splits(a) * (size_t)(a.rows.G * a.n_out) * (size_t)a.n_in : 0;
@@ -887,10 +913,11 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         const DzShape dz = dz_shape(a);
         const bool own = a.act != ACT_NONE && (a.dx || a.dw);
         T *d = own ? (T *)a.scratch : nullptr;
+        T *low = own && sizeof(T) == 2 && a.act != ACT_RELU ? (T *)((char *)a.scratch + l.low) : nullptr;
         float *sums = a.db ? (float *)((char *)a.scratch + l.sums) : nullptr;
         if (a.rows.M > 0 && (d || sums)) {
             hipLaunchKernelGGL((k_linear_dz<T>), net_grid(net_tiles(a.rows, dz.sh) * dz.cols), dim3(256),
-                               sizeof(float) * N * (256 - dz.L), s, a, dz.sh, dz.L, dz.cols, d, l.ldd, sums);
+                               sizeof(float) * N * (256 - dz.L), s, a, dz.sh, dz.L, dz.cols, d, low, l.ldd, sums);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
         if (a.db && !(a.rows.M > 0 && !a.rows.off && net_single(a.rows, dz.sh))) {
@@ -909,12 +936,12 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         const int64_t cols = (a.n_in + L * N - 1) / (L * N);
         if (a.dx && (a.n_out <= kShortOutputs || (sizeof(T) == 4 && mean <= kShortMean)) && a.n_in >= 64) {
             const int64_t units = net_tiles(a.rows, kShortShift);
-            hipLaunchKernelGGL((k_linear_short<T, false>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, ldd,
-                               L, units);
+            hipLaunchKernelGGL((k_linear_short<T, false>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, low,
+                               ldd, L, units);
             e = hipGetLastError();
         } else if (a.dx) {
             const int splits = dx_splits(a);
-            e = launch_linear_dx_tiles<t.value>(a, dd, ldd, splits, part, s);
+            e = launch_linear_dx_tiles<t.value>(a, dd, low, ldd, splits, part, s);
             if (e == hipSuccess && splits > 1) {
                 hipLaunchKernelGGL((k_linear_join<T>), net_grid((a.rows.M * a.n_in + 255) / 256), dim3(256), 0, s, a.rows,
                                    part, splits, a.rows.M, a.n_in, (T *)a.dx, a.rows.M, (int64_t)0, a.lddx, true);
@@ -924,12 +951,12 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         if (e != hipSuccess || !a.dw) return e;
         if (mean <= kShortMean && a.n_in >= 64) {
             const int64_t units = a.rows.G * ((a.n_out + kShortRows - 1) / kShortRows);
-            hipLaunchKernelGGL((k_linear_short<T, true>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, ldd,
-                               L, units);
+            hipLaunchKernelGGL((k_linear_short<T, true>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, low,
+                               ldd, L, units);
             return hipGetLastError();
         }
         const int splits = dw_splits(a);
-        e = launch_linear_dw_tiles<t.value>(a, dd, ldd, splits, part, s);
+        e = launch_linear_dw_tiles<t.value>(a, dd, low, ldd, splits, part, s);
         if (e != hipSuccess || splits == 1) return e;
         const int64_t rows = a.rows.G * a.n_out;
         hipLaunchKernelGGL((k_linear_join<T>), net_grid((rows * a.n_in + 255) / 256), dim3(256), 0, s, a.rows, part, splits,

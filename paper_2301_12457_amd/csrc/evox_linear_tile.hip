@@ -132,6 +132,7 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_tile(LinearAr
     const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + i0 * a.ldw, a.ldw, ni},
         Q{(const Elem *)a.x + x0 * a.ldx, a.ldx, nj};
     Product<ID, false, false> p;
+    p.clear();
     p.run(P, Q, a.n_in, lds);
     LayerOut out{a.b ? (const Elem *)a.b + t.g * a.b_stride + i0 : nullptr,
                  a.r ? (const Elem *)a.r + t.lo * a.ldr + i0 : nullptr,
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_tile(LinearAr
 
 // dx = d W: i = input, j = row, k = output.
 template <int ID>
-__global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(LinearGradArgs a, const Elem *d,
+__global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(LinearGradArgs a, const Elem *d, const Elem *low,
                                                                                       int64_t ldd, int64_t ti, int64_t tj,
                                                                                       int splits, float *part, int64_t units)
 {
@@ -155,9 +156,10 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(Linea
     const NetTile t = net_tile(a.rows, Shape<ID>::sh, jt);
     if (t.g < 0) return;
     const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_in - i0, Shape<ID>::BI), nj = (int)(t.hi - t.lo);
-    const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + k0 * a.ldw + i0, a.ldw, ni}, Q{d + t.lo * ldd + k0, ldd, nj};
+    const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + k0 * a.ldw + i0, a.ldw, ni}, Q{d + t.lo * ldd + k0, ldd, nj},
+        R{low ? low + t.lo * ldd + k0 : nullptr, ldd, nj};
     Product<ID, true, false> p;
-    p.run(P, Q, k1 - k0, lds);
+    p.run_split(P, Q, R, k1 - k0, lds);
     if (splits > 1) {
         PartOut out{part + ((us - u * splits) * a.rows.M + t.lo) * a.n_in + i0, a.n_in};
         p.results(ni, nj, lds, out);
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(Linea
 
 // dW = d^T x: i = input, j = output, k = row of the network.
 template <int ID>
-__global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dw_tile(LinearGradArgs a, const Elem *d,
+__global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dw_tile(LinearGradArgs a, const Elem *d, const Elem *low,
                                                                                       int64_t ldd, int64_t ti, int64_t tj,
                                                                                       int splits, float *part, int64_t units)
 {
@@ -184,9 +186,10 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dw_tile(Linea
     share_of(hi - lo, splits, (int)z, &k0, &k1);
     const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_in - i0, Shape<ID>::BI), j0 = (int)jt * Shape<ID>::BJ,
               nj = min((int)a.n_out - j0, Shape<ID>::BJ);
-    const TileOp<Elem> P{(const Elem *)a.x + ((a.x_shared ? 0 : lo) + k0) * a.ldx + i0, a.ldx, ni}, Q{d + (lo + k0) * ldd + j0, ldd, nj};
+    const TileOp<Elem> P{(const Elem *)a.x + ((a.x_shared ? 0 : lo) + k0) * a.ldx + i0, a.ldx, ni}, Q{d + (lo + k0) * ldd + j0, ldd, nj},
+        R{low ? low + (lo + k0) * ldd + j0 : nullptr, ldd, nj};
     Product<ID, true, true> p;
-    p.run(P, Q, k1 - k0, lds);
+    p.run_split(P, Q, R, k1 - k0, lds);
     if (splits > 1) {
         PartOut out{part + ((z * a.rows.G + g) * a.n_out + j0) * a.n_in + i0, a.n_in};
         p.results(ni, nj, lds, out);
@@ -259,29 +262,31 @@ hipError_t launch_linear_tiles<EVOX_NET_TYPE>(const LinearArgs &a, hipStream_t s
 }
 
 template <>
-hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, int splits, float *part, hipStream_t s)
+hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd,
+                                                 int splits, float *part, hipStream_t s)
 {
     const auto go = [&](auto id) {
         constexpr int ID = id.value, B = Shape<ID>::BI;
         typedef Product<ID, true, false> G;
         const int64_t ti = (a.n_in + B - 1) / B, tj = net_tiles(a.rows, Shape<ID>::sh);
-        return launch_tiles<G>(k_linear_dx_tile<ID>, banded(tj) * ti * splits, s, a, (const Elem *)d, ldd, ti, tj, splits,
-                               part);
+        return launch_tiles<G>(k_linear_dx_tile<ID>, banded(tj) * ti * splits, s, a, (const Elem *)d, (const Elem *)low,
+                               ldd, ti, tj, splits, part);
     };
     if (splits > 1) return go(std::integral_constant<int, 0>{});
     return with_shape(a.n_in, row_tiles(a.rows), go);
 }
 
 template <>
-hipError_t launch_linear_dw_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, int64_t ldd, int splits, float *part, hipStream_t s)
+hipError_t launch_linear_dw_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd,
+                                                 int splits, float *part, hipStream_t s)
 {
     const auto out_tiles = [&](int BJ) { return a.rows.G * ((a.n_out + BJ - 1) / BJ); };
     const auto go = [&](auto id) {
         constexpr int ID = id.value, B = Shape<ID>::BI, BJ = Shape<ID>::BJ;
         typedef Product<ID, true, true> G;
         const int64_t ti = (a.n_in + B - 1) / B, tj = (a.n_out + BJ - 1) / BJ;
-        return launch_tiles<G>(k_linear_dw_tile<ID>, a.rows.G * banded(tj) * ti * splits, s, a, (const Elem *)d, ldd, ti, tj,
-                               splits, part);
+        return launch_tiles<G>(k_linear_dw_tile<ID>, a.rows.G * banded(tj) * ti * splits, s, a, (const Elem *)d,
+                               (const Elem *)low, ldd, ti, tj, splits, part);
     };
     if (splits > 1) return go(std::integral_constant<int, 0>{});
     return with_shape(a.n_in, out_tiles, go);

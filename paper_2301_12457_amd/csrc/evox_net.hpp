@@ -69,15 +69,16 @@ size_t xent_scratch(const XentArgs &a);
 hipError_t launch_xent(const XentArgs &a, hipStream_t s);
 
 // The large cases: tiles through LDS (one file per element type).  d: dy act'(z)
-// in the element type.  splits > 1: K in so many shares, partial results to part[z].
+// in the element type, low: its second number (d_split) or null.  splits > 1: K in so
+// many shares, partial results to part[z].
 template <int TYPE>
 hipError_t launch_linear_tiles(const LinearArgs &a, hipStream_t s);
 template <int TYPE>
-hipError_t launch_linear_dx_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, int splits, float *part,
-                                  hipStream_t s);
+hipError_t launch_linear_dx_tiles(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd, int splits,
+                                  float *part, hipStream_t s);
 template <int TYPE>
-hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, int64_t ldd, int splits, float *part,
-                                  hipStream_t s);
+hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd, int splits,
+                                  float *part, hipStream_t s);
 
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
@@ -94,6 +95,23 @@ template <>
 struct NetElement<NET_BF16> {
     typedef bf16_t type;
 };
+
+// d = dy act'(z) for 16-bit products as two numbers of the type: the rounded one and
+// what it leaves, d = d_up<T> high + d_down<T> low within u^2 |d| (u: the type's
+// roundoff).  f16's range is narrower than d's (a slope may be 1.13, or 2^-20): its
+// first number is d / 2, so that none overflows, its second 2^10 times as large, so
+// that 2^-35 is still kept.  An infinity or NaN is the first one's alone.
+template <typename T>
+inline constexpr float d_up = std::is_same<T, f16_t>::value ? 2.0f : 1.0f;
+template <typename T>
+inline constexpr float d_down = std::is_same<T, f16_t>::value ? 0x1p-10f : 1.0f;
+template <typename T>
+__device__ __forceinline__ void d_split(float d, T &high, T &low)
+{
+    high = (T)(d * (1.0f / d_up<T>));
+    const float r = d - (float)high * d_up<T>;
+    low = (T)(fabsf(r) < INFINITY ? r * (1.0f / d_down<T>) : 0.0f);
+}
 
 // Type-dependent launches: f is called with an integral constant, the type.
 template <typename F>

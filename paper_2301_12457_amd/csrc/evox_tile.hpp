@@ -355,6 +355,13 @@ struct TileProduct {
 #pragma unroll
             for (int j = 0; j < TJ; ++j) acc[i][j] = (f32x16)(0.0f);
     }
+    __device__ __forceinline__ void scale(float f)
+    {
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) acc[i][j] *= f;
+    }
 
     // One K tile (64 k) of 16-bit products in 4 TJ slots of TI products: slot k
     // reads the operand of slot k + 2, and with kNext writes a share of the next
@@ -503,12 +510,11 @@ struct TileProduct {
         for (int w = 0; w < SQ::kStores; ++w) sq.store_piece(w, lds + kStageBytes<T, BI>, big);
     }
 
-    // The whole product; ends with all waves past their last use of LDS.
+    // The product, added to acc; ends with all waves past their last use of LDS.
     __device__ __forceinline__ void run(const TileOp<T> &P, const TileOp<T> &Q, int64_t K, char *lds)
     {
         Stage<T, PM, BI, kThreads> sp;
         Stage<T, QM, BJ, kThreads> sq;
-        clear();
         if (K <= 0) return;
         sp.init(P.p, P.ld, P.n);
         sq.init(Q.p, Q.ld, Q.n);
@@ -542,6 +548,21 @@ struct TileProduct {
         }
         if constexpr (kSplit)
             if (__syncthreads_or(!(big < kTileBig))) again(P, Q, K);
+    }
+
+    // The product of P and d_up Q + d_down R (R.p null: of P and Q), K once for each
+    // of the two, the small one first.
+    __device__ __forceinline__ void run_split(const TileOp<T> &P, const TileOp<T> &Q, const TileOp<T> &R, int64_t K, char *lds)
+    {
+        clear();
+        if constexpr (!kSplit)
+            if (R.p) {
+                run(P, R, K, lds);
+                if constexpr (d_up<T> != 1.0f) scale(d_down<T> / d_up<T>);
+            }
+        run(P, Q, K, lds);
+        if constexpr (d_up<T> != 1.0f)
+            if (R.p) scale(d_up<T>);
     }
 
     // The results, S rows of every wave at a time through LDS (the wave's own part
