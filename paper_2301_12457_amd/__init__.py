@@ -322,15 +322,23 @@ def _raw_stream(stream):
     return _DTYPES["stream"]() if stream is None else stream.cuda_stream
 
 
+def _empty(nbytes, device, stream):
+    """Bytes of the memory pool of a stream (None: the current one)."""
+    import torch
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _scratch(nbytes, like, scratch, stream):
-    """The caller's scratch, or one of this size that lives until the stream is done with it."""
+    """The caller's scratch, or one of this size from the memory of the call's stream (a
+    block of the current stream's may be in use there, which nothing orders another
+    stream behind, and its next user would not wait for this one)."""
     if nbytes == 0:
         _check(EINVAL)
     if scratch is None:
-        import torch
-        scratch = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-        if stream is not None:
-            scratch.record_stream(stream)
+        scratch = _empty(nbytes, like.device, stream)
     elif scratch.get_device() != like.get_device() or not scratch.is_contiguous():
         raise EvoxError(EINVAL, f"scratch: a dense tensor on {like.device}")
     return scratch, scratch.numel() * scratch.element_size()

@@ -1,0 +1,34 @@
+"""The scratch that a call allocates for itself belongs to the stream that the call
+runs on: a block of the current stream's may still be in use there, and nothing
+orders another stream behind that."""
+import pytest
+import torch
+
+from host_tensors import Library, Streams, gpu
+
+
+@pytest.fixture
+def evox(monkeypatch):
+    import paper_2301_12457_amd as m
+    L = Library()
+    monkeypatch.setattr(m, "lib", lambda: L)
+    m.calls = L.calls
+    return m
+
+
+def calls(evox):
+    x, w, dy, v = gpu(torch.zeros(6, 4)), gpu(torch.zeros(2, 3, 4)), gpu(torch.zeros(6, 3)), gpu(torch.zeros(6))
+    p, lab, fit = gpu(torch.zeros(2, 4)), gpu(torch.zeros(6, dtype=torch.int32)), gpu(torch.zeros(2))
+    return {"evox_linear_grad": lambda s: evox.evox_linear_grad(x, w, dy, dw=w.clone(), stream=s),
+            "evox_layernorm_grad": lambda s: evox.evox_layernorm_grad(x, p, v, v, x, dx=x.clone(), stream=s),
+            "evox_xent": lambda s: evox.evox_xent(x, lab, fit, stream=s)}
+
+
+@pytest.mark.parametrize("name", ["evox_linear_grad", "evox_layernorm_grad", "evox_xent"])
+def test_scratch_of_the_call_s_stream(evox, monkeypatch, name):
+    streams = Streams(monkeypatch)
+    side = streams.stream(2)
+    calls(evox)[name](side)
+    assert [s.cuda_stream for s in streams.allocated] == [2]
+    (called, args), = [c for c in evox.calls if c[0] == name]
+    assert args[-1] == 2 and streams.now.cuda_stream == 1
