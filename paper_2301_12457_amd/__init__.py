@@ -517,15 +517,14 @@ def evox_xent(logits, labels, fit, dz=None, off=None, scratch=None, stream=None)
 def evox_nsga2_sort(F, front, crowd, scratch=None, stream=None):
     """Fronts (int32) and crowding distances (float64) of the rows of F
     [n, M] (fp32 device tensor), through the library's sort."""
-    import torch
     n, M = F.shape
     nbytes = int(lib().evox_nsga2_sort_scratch_bytes(n, M))
     if nbytes == 0:
         _check(EINVAL)
     if scratch is None:
-        scratch = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=F.device)
-    _check(lib().evox_nsga2_sort(_ptr(F), n, M, _ptr(front), _ptr(crowd), _ptr(scratch), scratch.numel() * 4,
-                                 _stream(stream)))
+        scratch = _empty(nbytes, F.device, stream)
+    _check(lib().evox_nsga2_sort(_ptr(F), n, M, _ptr(front), _ptr(crowd), _ptr(scratch),
+                                 scratch.numel() * scratch.element_size(), _stream(stream)))
     return front, crowd
 
 

@@ -55,3 +55,14 @@ def test_side_stream_with_its_own_scratch(evox_gpu, name):
         assert all(torch.equal(p, q) for p, q in zip(out, want))
         for t in out:
             t.fill_(float("nan"))
+
+
+def test_sort_on_a_side_stream(evox_gpu):
+    F = torch.rand(700, 3, generator=torch.Generator().manual_seed(2)).cuda()
+    new = lambda: (torch.empty(700, dtype=torch.int32, device="cuda"), torch.empty(700, dtype=torch.float64, device="cuda"))
+    want, got = new(), new()
+    evox_gpu.evox_nsga2_sort(F, *want)
+    torch.cuda.synchronize()
+    evox_gpu.evox_nsga2_sort(F, *got, stream=torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))

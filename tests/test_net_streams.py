@@ -32,3 +32,12 @@ def test_scratch_of_the_call_s_stream(evox, monkeypatch, name):
     assert [s.cuda_stream for s in streams.allocated] == [2]
     (called, args), = [c for c in evox.calls if c[0] == name]
     assert args[-1] == 2 and streams.now.cuda_stream == 1
+
+
+def test_scratch_of_the_sort_s_stream(evox, monkeypatch):
+    streams = Streams(monkeypatch)
+    evox.evox_nsga2_sort(gpu(torch.zeros(8, 3)), gpu(torch.zeros(8, dtype=torch.int32)),
+                         gpu(torch.zeros(8, dtype=torch.float64)), stream=streams.stream(2))
+    assert [s.cuda_stream for s in streams.allocated] == [2]
+    (called, args), = [c for c in evox.calls if c[0] == "evox_nsga2_sort"]
+    assert args[-2] >= 4096 and args[-1].value == 2
