@@ -639,6 +639,10 @@ class Swarm:
                                obj=_ptr(self.obj), front=_ptr(self.front), crowd=_ptr(self.crowd),
                                scratch=_ptr(self.scratch),
                                scratch_bytes=self.scratch.numel() * 4)
+        # the buffers are the current stream's memory, which work pending there may still read
+        current = torch.cuda.current_stream(device)
+        if self.stream.cuda_stream != current.cuda_stream:
+            self.stream.wait_stream(current)
         self.handle = ctypes.c_void_p()
         _check(lib().evox_state_create(ctypes.byref(self.P), ctypes.byref(self.buffers),
                                        _stream(self.stream), ctypes.byref(self.handle)))

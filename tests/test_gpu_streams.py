@@ -66,3 +66,23 @@ def test_sort_on_a_side_stream(evox_gpu):
     evox_gpu.evox_nsga2_sort(F, *got, stream=torch.cuda.Stream())
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_a_state_on_a_side_stream(evox_gpu):
+    """A state on another stream, started behind pending readers of freed memory."""
+    params = evox_gpu.make_params(evox_gpu.PSO, evox_gpu.SPHERE, 512, 64, -5.0, 5.0, seed=3)
+    want = evox_gpu.Swarm(params)
+    want.step(3)
+    torch.cuda.synchronize()
+    busy = torch.randn(2048, 2048, device="cuda")
+    held = [torch.full((512 * 64,), 3.0, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        busy = (busy @ busy).clamp(-1, 1)
+    copies = [t.clone() for t in held]
+    del held
+    got = evox_gpu.Swarm(params, stream=torch.cuda.Stream())
+    got.step(3)
+    torch.cuda.synchronize()
+    assert all((t == 3).all() for t in copies)
+    assert torch.equal(got.view("x"), want.view("x")) and torch.equal(got.gbest, want.gbest)

@@ -41,3 +41,14 @@ def test_scratch_of_the_sort_s_stream(evox, monkeypatch):
     assert [s.cuda_stream for s in streams.allocated] == [2]
     (called, args), = [c for c in evox.calls if c[0] == "evox_nsga2_sort"]
     assert args[-2] >= 4096 and args[-1].value == 2
+
+
+def test_a_state_waits_for_the_memory_it_takes(evox, monkeypatch):
+    """Its buffers are the current stream's, its kernels may run on another: behind
+    what is pending there."""
+    streams = Streams(monkeypatch)
+    params = evox.Params(algo=evox.PSO, fn_id=0, N=8, D=4, ldx=4)
+    for stream, waited in ((streams.stream(2), [(2, 1)]), (None, []), (streams.now, [])):
+        streams.waited.clear()
+        evox.Swarm(params, stream=stream)
+        assert streams.waited == waited
