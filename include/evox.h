@@ -535,7 +535,7 @@ int evox_profile_read(evox_state *state, double *fused_ms, int64_t *fused_launch
 enum evox_dtype { EVOX_F32 = 0, EVOX_BF16 = 1, EVOX_F16 = 2 };
 
 /* act(z): z, max(z, 0), tanh z, z Phi(z) (the normal distribution function, by
- * erf), z / (1 + exp(-z)).  NaN stays NaN. */
+ * erf), z / (1 + exp(-z)); at infinities their limits.  NaN stays NaN. */
 enum evox_act { EVOX_ACT_NONE = 0, EVOX_ACT_RELU = 1, EVOX_ACT_TANH = 2, EVOX_ACT_GELU = 3, EVOX_ACT_SILU = 4 };
 
 /* One layer of G networks (pitches and strides in elements). */

@@ -382,6 +382,7 @@ __device__ __forceinline__ float normal_tail(float z, float *e)
     return 0.5f * p * t * *e;
 }
 
+// (-inf has the value 0 of GELU's and SiLU's limits; NaN passes)
 template <bool FAST>
 __device__ __forceinline__ float act_value(int act, float z)
 {
@@ -394,13 +395,13 @@ __device__ __forceinline__ float act_value(int act, float z)
         return s < 0.0225f ? near : copysignf(r, z);
     }
     case ACT_GELU: {
-        if constexpr (!FAST) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+        if constexpr (!FAST) return 0.5f * fmaxf(z, -126.0f) * (1.0f + erff(z * 0.70710678f));
         float e;
         const float q = normal_tail(z, &e);  // NaN where z is
         return fmaf(-fminf(fabsf(z), 30.0f), q, fmaxf(z, 0.0f));
     }
     case ACT_SILU:
-        if constexpr (!FAST) return z / (1.0f + expf(-z));
+        if constexpr (!FAST) return fmaxf(z, -126.0f) / (1.0f + expf(-z));
         return fmaxf(z, -126.0f) * __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
     default: return z;
     }

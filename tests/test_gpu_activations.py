@@ -1,0 +1,52 @@
+"""Activations and their slopes one element at a time (layers 1 x 1 of weight 1):
+infinities and NaN alike in all types, and the small ends to the type's own
+rounding.
+
+Bounds, relative: the argument's square is rounded once where an exponential
+takes it, 2 u z^2 of it, u = 2^-24; a published or fitted polynomial, a
+reciprocal and the products 2^-15 in 16 bits, far below the type's roundoff, and
+16 u in fp32."""
+import math
+
+import pytest
+import torch
+
+import net_ref as nr
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+VALUES = {"none": (INF, -INF), "relu": (INF, 0.0), "tanh": (1.0, -1.0), "gelu": (INF, 0.0), "silu": (INF, 0.0)}
+SLOPES = {"none": (1.0, 1.0), "relu": (1.0, 0.0), "tanh": (0.0, 0.0), "gelu": (1.0, 0.0), "silu": (1.0, 0.0)}
+
+
+def value_and_slope(ev, z, act):
+    one = torch.ones(1, 1, 1, dtype=z.dtype, device="cuda")
+    y, dx = torch.empty_like(z), torch.empty_like(z)
+    ev.evox_linear(z, one, y, act=nr.ACTS.index(act))
+    ev.evox_linear_grad(z, one, torch.ones_like(z), z=z, dx=dx, act=nr.ACTS.index(act))
+    return y, dx
+
+
+@pytest.mark.parametrize("dtype", nr.DTYPES)
+@pytest.mark.parametrize("act", nr.ACTS)
+def test_infinities_and_nan(evox_gpu, dtype, act):
+    z = torch.tensor([INF, -INF, float("nan"), 1.0], device="cuda").to(dtype)[:, None]
+    y, dx = value_and_slope(evox_gpu, z, act)
+    assert y[:2, 0].tolist() == list(VALUES[act]) and dx[:2, 0].tolist() == list(SLOPES[act])
+    assert math.isnan(float(y[2])) and (act == "none" or math.isnan(float(dx[2])))
+    assert math.isfinite(float(y[3])) and math.isfinite(float(dx[3]))
+
+
+@pytest.mark.parametrize("dtype", nr.DTYPES)
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_infinities_through_tiles(evox_gpu, dtype, act):
+    """The same behind the layers' large products (their sums are -inf, inf and NaN)."""
+    G, n, n_in, n_out = 6, 300, 130, 520
+    x, w = torch.zeros(G * n, n_in, device="cuda", dtype=dtype), torch.ones(G, n_out, n_in, device="cuda", dtype=dtype)
+    x[1, 3], x[2, 4], x[5, 5], x[n + 7, 8] = -INF, INF, float("nan"), -INF
+    y = torch.empty(G * n, n_out, device="cuda", dtype=dtype)
+    evox_gpu.evox_linear(x, w, y, act=nr.ACTS.index(act))
+    want = torch.zeros(G * n, n_out, device="cuda", dtype=dtype)
+    want[2], want[5] = INF, float("nan")
+    assert torch.equal(torch.isnan(y), torch.isnan(want))
+    assert torch.equal(y[~torch.isnan(want)], want[~torch.isnan(want)])
