@@ -50,3 +50,29 @@ def test_infinities_through_tiles(evox_gpu, dtype, act):
     want[2], want[5] = INF, float("nan")
     assert torch.equal(torch.isnan(y), torch.isnan(want))
     assert torch.equal(y[~torch.isnan(want)], want[~torch.isnan(want)])
+
+
+def check_small_ends(evox_gpu, dtype, act):
+    """Values and slopes from -12 to 12 relative to themselves (slopes of GELU and
+    SiLU, which cross zero, to the sum of their terms)."""
+    z = torch.linspace(-12, 12, 20_001, device="cuda").to(dtype)[:, None]
+    y, dx = value_and_slope(evox_gpu, z, act)
+    zz = z.double()
+    want, slope = nr.act64(zz, act), nr.slope64(zz, act)
+    rel = (16 * nr.U32 if dtype == torch.float32 else 2.0 ** -15) + 4 * nr.U32 * zz * zz
+    terms = slope
+    if act == "gelu":
+        terms = 0.5 * torch.erfc(-zz / math.sqrt(2)) + zz.abs() * torch.exp(-zz * zz / 2) / math.sqrt(2 * math.pi)
+    elif act == "silu":
+        s = torch.sigmoid(zz)
+        terms = s * (1 + zz.abs() * torch.sigmoid(-zz))
+    for got, exact, scale in ((y, want, want.abs()), (dx, slope, terms)):
+        limit = rel * scale + (exact.abs() + rel * scale) * nr.U[dtype] * 1.0001 + nr.TINY[dtype]
+        bad = ~((got.double() - exact).abs() <= limit)
+        assert not bad.any(), (f"{act} {dtype}: {int(bad.sum())} off, e.g. at {z[bad][:3].tolist()}: {got[bad][:3].tolist()} for "
+                               f"{exact[bad][:3].tolist()} +- {limit[bad][:3].tolist()}")
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu", "tanh"])
+def test_small_ends_of_fp32(evox_gpu, act):
+    check_small_ends(evox_gpu, torch.float32, act)
