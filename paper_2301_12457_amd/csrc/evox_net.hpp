@@ -353,9 +353,11 @@ hipError_t launch_net_sums(const NetRows &rows, const float *part, int64_t width
 
 // Activations and their slopes.  For results of 16 bits the hardware's exp2
 // and reciprocal (1 ulp) stand in for expf and the division, and the normal
-// distribution's upper tail is Q(x) = e^(-x^2/2) t (a1 + .. + a5 t^4) / 2, t = 1 /
-// (1 + p x / sqrt 2) (Abramowitz and Stegun 7.1.26: 7.5e-8 off at most, and a
-// tail without cancellation); tanh below 0.15 is its series.  A GELU is then 14
+// distribution's upper tail is Q(x) = e^(-x^2/2) t (a1 + .. + a7 t^6) / 2, t = 1 /
+// (1 + p x) (the form of Abramowitz and Stegun 7.1.26; the coefficients minimise the
+// larger of the error over 1.5e-7 and the relative one over 1e-5, x up to 13.6: at most
+// 1e-7 and 3.1e-6.  Their own five are within 7.5e-8, but a bf16 GELU(-8) came out 1e-2
+// off); tanh below 0.15 is its series.  A GELU is then 16
 // multiply-adds and two transcendental instructions instead of about 60
 // instructions of erff, 268M of which cost more than a quarter of the layer that
 // they follow (16x2048 rows 4096x4096).  fp32 takes erfc, which keeps its digits where
@@ -376,11 +378,13 @@ __device__ __forceinline__ float exp_near(float x)
 __device__ __forceinline__ float normal_tail(float z, float *e)
 {
     *e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.0f));
-    float p = fmaf(t, 1.061405429f, -1.453152027f);
-    p = fmaf(t, p, 1.421413741f);
-    p = fmaf(t, p, -0.284496736f);
-    p = fmaf(t, p, 0.254829592f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.256326199f, 1.0f));
+    float p = fmaf(t, -0.157882705f, 0.528239012f);
+    p = fmaf(t, p, -0.305762857f);
+    p = fmaf(t, p, 0.39424786f);
+    p = fmaf(t, p, 0.1218144f);
+    p = fmaf(t, p, 0.215542689f);
+    p = fmaf(t, p, 0.203801587f);
     return 0.5f * p * t * *e;
 }
 

@@ -76,3 +76,9 @@ def check_small_ends(evox_gpu, dtype, act):
 @pytest.mark.parametrize("act", ["gelu", "silu", "tanh"])
 def test_small_ends_of_fp32(evox_gpu, act):
     check_small_ends(evox_gpu, torch.float32, act)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", ["gelu", "silu", "tanh"])
+def test_small_ends_of_16_bits(evox_gpu, dtype, act):
+    check_small_ends(evox_gpu, dtype, act)
