@@ -82,3 +82,15 @@ def test_small_ends_of_fp32(evox_gpu, act):
 @pytest.mark.parametrize("act", ["gelu", "silu", "tanh"])
 def test_small_ends_of_16_bits(evox_gpu, dtype, act):
     check_small_ends(evox_gpu, dtype, act)
+
+
+def test_tanh_slope_of_fp32(evox_gpu):
+    """No further from 64 bits (root of the mean square) than 1 - tanh^2 in fp32,
+    where that does not cancel."""
+    z = torch.linspace(-1, 1, 100_001, device="cuda")[:, None]
+    exact = nr.slope64(z.double(), "tanh")
+    rms = lambda t: float((t.double() - exact).square().mean().sqrt())
+    plain = rms(1 - torch.tanh(z).square())
+    own = rms(value_and_slope(evox_gpu, z, "tanh")[1])
+    print(f"tanh slope rms {own:.3g}, plain {plain:.3g}", flush=True)
+    assert own <= plain
