@@ -254,15 +254,20 @@ _DTYPES = {}
 _FLOAT, _INT = "float32", "int32"  # vectors' types, by name: torch is imported with the first call
 
 
+def _look_at_torch():
+    """Fills _DTYPES, whole or not at all for whoever reads it meanwhile."""
+    global _DTYPES
+    import torch
+    # the current stream's handle without its object (3 us), where torch has it
+    raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+    _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, _FLOAT: torch.float32, _INT: torch.int32,
+               "stream": (lambda: raw(device())) if raw and device else lambda: torch.cuda.current_stream().cuda_stream}
+
+
 def _dtype(t):
     """The element type's id of a tensor on the GPU."""
     if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
-        _DTYPES.update({_FLOAT: torch.float32, _INT: torch.int32})
-        # the current stream's handle without its object (3 us), where torch has it
-        raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
-        _DTYPES["stream"] = (lambda: raw(device())) if raw and device else lambda: torch.cuda.current_stream().cuda_stream
+        _look_at_torch()
     d = _DTYPES.get(t.dtype)
     if d is None:
         raise EvoxError(EINVAL, f"element type {t.dtype}: float32, bfloat16 or float16")
