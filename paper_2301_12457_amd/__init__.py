@@ -258,10 +258,11 @@ def _look_at_torch():
     """Fills _DTYPES, whole or not at all for whoever reads it meanwhile."""
     global _DTYPES
     import torch
-    # the current stream's handle without its object (3 us), where torch has it
+    # a device's current stream's handle without its object (3 us), where torch has it
     raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
     _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, _FLOAT: torch.float32, _INT: torch.int32,
-               "stream": (lambda: raw(device())) if raw and device else lambda: torch.cuda.current_stream().cuda_stream}
+               "stream": raw or (lambda d: torch.cuda.current_stream(d).cuda_stream),
+               "device": device or torch.cuda.current_device}
 
 
 def _dtype(t):
@@ -322,9 +323,14 @@ def _offsets(off, like, G):
     return _vector("off", off, _INT, G + 1, like)
 
 
-def _raw_stream(stream):
-    """The HIP stream of a call: the given one, or the current one of the current device."""
-    return _DTYPES["stream"]() if stream is None else stream.cuda_stream
+def _raw_stream(stream, like):
+    """The HIP stream of a call, the given one or the current one: of like's device, which
+    has to be the current one too (the handle of any device's default stream is 0)."""
+    d, current = like.get_device(), _DTYPES["device"]()
+    if current != d or stream is not None and stream.device.index != d:
+        raise EvoxError(EINVAL, f"tensors on device {d}: the current device is {current}"
+                                + ("" if stream is None else f", the stream's {stream.device.index}"))
+    return _DTYPES["stream"](d) if stream is None else stream.cuda_stream
 
 
 def _empty(nbytes, device, stream):
@@ -393,7 +399,7 @@ def evox_linear(x, w, y, b=None, r=None, z=None, off=None, act=ACT_NONE, stream=
         p.ldz = _pitch(z)
     rc = lib().evox_linear(ctypes.byref(p), x.data_ptr(), w.data_ptr(), None if b is None else b.data_ptr(),
                            None if r is None else r.data_ptr(), None if z is None else z.data_ptr(), y.data_ptr(),
-                           _raw_stream(stream))
+                           _raw_stream(stream, w))
     if rc != OK:
         _check(rc)
     return y
@@ -426,7 +432,7 @@ def evox_linear_grad(x, w, dy, z=None, dx=None, dw=None, db=None, off=None, act=
         p.db_stride = _net_stride(db)
     scratch, nbytes = _scratch(lib().evox_linear_grad_scratch_bytes(ctypes.byref(p)), w, scratch, stream)
     _check(lib().evox_linear_grad(ctypes.byref(p), x.data_ptr(), w.data_ptr(), z_at, dy.data_ptr(), dx_at, dw_at,
-                                  db_at, scratch.data_ptr(), nbytes, _raw_stream(stream)))
+                                  db_at, scratch.data_ptr(), nbytes, _raw_stream(stream, w)))
     return dx, dw, db
 
 
@@ -449,7 +455,7 @@ def evox_layernorm(x, gamma, beta, y, mean=None, rstd=None, off=None, eps=1e-5, 
     p.ldy = _pitch(y)
     _check(lib().evox_layernorm(ctypes.byref(p), x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), y.data_ptr(),
                                 _vector("mean", mean, _FLOAT, p.M, x), _vector("rstd", rstd, _FLOAT, p.M, x),
-                                _raw_stream(stream)))
+                                _raw_stream(stream, x)))
     return y
 
 
@@ -480,7 +486,7 @@ def evox_layernorm_grad(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=No
     _check(lib().evox_layernorm_grad(ctypes.byref(p), x.data_ptr(), gamma.data_ptr(),
                                      _vector("mean", mean, _FLOAT, p.M, x),
                                      _vector("rstd", rstd, _FLOAT, p.M, x), dy_at, dx_at, dg_at, db_at,
-                                     scratch.data_ptr(), nbytes, _raw_stream(stream)))
+                                     scratch.data_ptr(), nbytes, _raw_stream(stream, x)))
     return dx, dgamma, dbeta
 
 
@@ -515,7 +521,7 @@ def evox_xent(logits, labels, fit, dz=None, off=None, scratch=None, stream=None)
         p.lddz = _pitch(dz)
     scratch, nbytes = _scratch(lib().evox_xent_scratch_bytes(ctypes.byref(p)), logits, scratch, stream)
     _check(lib().evox_xent(ctypes.byref(p), logits.data_ptr(), labels_at, fit_at, dz_at, scratch.data_ptr(), nbytes,
-                           _raw_stream(stream)))
+                           _raw_stream(stream, logits)))
     return fit
 
 

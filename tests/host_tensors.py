@@ -66,3 +66,9 @@ class Streams:
             def __exit__(self, *args):
                 outer.now = self.before
         return Context()
+
+
+def on_host_device(evox, monkeypatch, current=0):
+    """The binding with this current device, whose current stream is 7."""
+    evox._look_at_torch()
+    monkeypatch.setattr(evox, "_DTYPES", dict(evox._DTYPES, stream=lambda device: 7, device=lambda: current))

@@ -4,7 +4,7 @@ orders another stream behind that."""
 import pytest
 import torch
 
-from host_tensors import Library, Streams, gpu
+from host_tensors import Library, Streams, gpu, on_host_device
 
 
 @pytest.fixture
@@ -13,6 +13,7 @@ def evox(monkeypatch):
     L = Library()
     monkeypatch.setattr(m, "lib", lambda: L)
     m.calls = L.calls
+    on_host_device(m, monkeypatch)
     return m
 
 
