@@ -65,3 +65,71 @@ def test_another_device_than_the_stream_s(evox, monkeypatch, tensors, current, s
             with pytest.raises(evox.EvoxError, match="device"):
                 call()
             assert all(name.endswith("_bytes") for name, _ in evox.calls)
+
+
+# what is wrong with one argument, and the words that say so
+LINEAR = [("x", lambda t: gpu(t.double()), "float64"), ("x", lambda t: t[:5], "networks|shape"),
+          ("x", lambda t: gpu(torch.zeros(6, 8))[:, ::2], "dense"), ("x", lambda t: gpu(torch.zeros(6, 5)), "x has shape"),
+          ("w", lambda t: t[0], r"must be \[G, n_out, n_in\]"), ("w", lambda t: t.transpose(1, 2), "x has shape|dense"),
+          ("w", lambda t: gpu(torch.zeros(2, 4, 3)).transpose(1, 2), "w: rows are not dense"),
+          ("w", lambda t: gpu(t.half()), "float32 on .*needs torch.float16"), ("y", lambda t: gpu(t.bfloat16()), "y: torch.bfloat16"),
+          ("y", lambda t: t[:, :2], "y has shape"), ("y", lambda t: gpu(torch.zeros(6, 3), 1), "y: "),
+          ("b", lambda t: t[0], "b has shape"), ("b", lambda t: gpu(torch.zeros(2, 6))[:, ::2], "b: rows are not dense"),
+          ("r", lambda t: gpu(torch.zeros(6, 4)), "r has shape"), ("z", lambda t: t[:5], "z has shape"),
+          ("z", lambda t: gpu(torch.zeros(6, 3, dtype=torch.float16)), "z: torch.float16"),
+          ("off", lambda t: gpu(torch.zeros(3)), "off: a dense int32"), ("off", lambda t: t[:2], "off: a dense int32 tensor of 3"),
+          ("off", lambda t: gpu(torch.zeros(6, dtype=torch.int32))[::2], "off: a dense int32")]
+LINEAR_GRAD = [("dx", lambda t: t[:, :3], "dx has shape"), ("dw", lambda t: t[:1], "dw has shape"),
+               ("dw", lambda t: gpu(torch.zeros(2, 4, 3)).transpose(1, 2), "dw: rows are not dense"),
+               ("db", lambda t: t[:, :2], "db has shape"), ("z", lambda t: t[:5], "z has shape"),
+               ("dy", lambda t: gpu(t.half()), "y: torch.float16"), ("scratch", lambda t: t.expand(2, -1)[:, ::2], "scratch: a dense"),
+               ("scratch", lambda t: gpu(torch.zeros(4096), 1), "scratch: a dense")]
+NORM = [("x", lambda t: t[0], r"x must be \[M, D\]"), ("x", lambda t: gpu(torch.zeros(6, 8))[:, ::2], "x: rows are not dense"),
+        ("gamma", lambda t: t[:, :3], "gamma has shape"), ("beta", lambda t: t[:, :3], "beta has shape"),
+        ("beta", lambda t: gpu(torch.zeros(2, 9))[:, :4], "different strides"), ("y", lambda t: gpu(t.half()), "y: torch.float16"),
+        ("mean", lambda t: gpu(t.double()), "mean: a dense float32"), ("rstd", lambda t: t[:5], "rstd: a dense float32 tensor of 6"),
+        ("off", lambda t: t[:2], "off: a dense int32 tensor of 3")]
+NORM_GRAD = [("mean", lambda t: t[:5], "mean: a dense float32"), ("rstd", lambda t: gpu(t.half()), "rstd: a dense float32"),
+             ("dy", lambda t: t[:, :3], "dy has shape"), ("dx", lambda t: gpu(torch.zeros(6, 8))[:, ::2], "dx: rows are not dense"),
+             ("dgamma", lambda t: t[:1], "dgamma has shape"), ("dbeta", lambda t: gpu(torch.zeros(2, 9))[:, :4], "different strides"),
+             ("scratch", lambda t: t.expand(2, -1)[:, ::2], "scratch: a dense")]
+XENT = [("logits", lambda t: t[0], r"logits must be \[M, C\]|vectors"), ("labels", lambda t: t.float(), "labels: a dense int32"),
+        ("labels", lambda t: t[:5], "labels: a dense int32 tensor of 3"), ("labels", lambda t: t[None], "fit and labels are vectors"),
+        ("fit", lambda t: gpu(t.double()), "fit: a dense float32"), ("fit", lambda t: t[:, None], "fit and labels are vectors"),
+        ("dz", lambda t: t[:, :3], "dz has shape"), ("dz", lambda t: gpu(t.half()), "dz: torch.float16"),
+        ("scratch", lambda t: t.expand(2, -1)[:, ::2], "scratch: a dense")]
+
+
+def arguments():
+    new = lambda *shape, **kw: gpu(torch.zeros(*shape, **kw))
+    off = gpu(torch.tensor([0, 2, 6], dtype=torch.int32))
+    x, w, y, v, p = new(6, 4), new(2, 3, 4), new(6, 3), new(6), new(2, 4)
+    return {"evox_linear": dict(x=x, w=w, y=y, b=new(2, 3), r=new(6, 3), z=new(6, 3), off=off),
+            "evox_linear_grad": dict(x=x, w=w, dy=y, z=new(6, 3), dx=new(6, 4), dw=new(2, 3, 4), db=new(2, 3), off=off, scratch=new(4096)),
+            "evox_layernorm": dict(x=x, gamma=p, beta=new(2, 4), y=new(6, 4), mean=v, rstd=new(6), off=off),
+            "evox_layernorm_grad": dict(x=x, gamma=p, mean=v, rstd=new(6), dy=new(6, 4), dx=new(6, 4), dgamma=new(2, 4),
+                                        dbeta=new(2, 4), off=off, scratch=new(4096)),
+            "evox_xent": dict(logits=x, labels=new(6, dtype=torch.int32), fit=new(2), dz=new(6, 4), off=off, scratch=new(4096))}
+
+
+@pytest.mark.parametrize("name", sorted(arguments()))
+def test_calls_reach_the_library(evox, monkeypatch, name):
+    """What the refusals below differ from in one argument is accepted."""
+    on_host_device(evox, monkeypatch)
+    getattr(evox, name)(**arguments()[name])
+    assert evox.calls[-1][0] == name
+
+
+@pytest.mark.parametrize("name,what,change,words", [(n, *c) for n, cases in (
+    ("evox_linear", LINEAR), ("evox_linear_grad", LINEAR_GRAD), ("evox_layernorm", NORM), ("evox_layernorm_grad", NORM_GRAD),
+    ("evox_xent", XENT)) for c in cases])
+def test_refusals_and_their_reasons(evox, monkeypatch, name, what, change, words):
+    on_host_device(evox, monkeypatch)
+    kw = arguments()[name]
+    if name == "evox_xent" and what == "labels" or name == "evox_linear" and what == "x":
+        kw["off"] = None  # (fewer rows could be rows that the networks share)
+    kw[what] = change(kw[what])
+    with pytest.raises(evox.EvoxError, match=words) as e:
+        getattr(evox, name)(**kw)
+    assert e.value.code == evox.EINVAL and not any(n == name for n, _ in evox.calls)
+    assert "kernels read the GPU's memory" not in str(e.value)
