@@ -20,6 +20,7 @@ OK, EINVAL, EHIP, ENOSPC, EALIGN = 0, -1, -2, -3, -4
 MAX_D = 32768
 F32, BF16, F16 = range(3)
 ACT_NONE, ACT_RELU, ACT_TANH, ACT_GELU, ACT_SILU = range(5)
+KERNEL_ROWS, KERNEL_NARROW, KERNEL_FEW_INPUTS, KERNEL_SHORT, KERNEL_SHARES, KERNEL_TILES = 0, 1, 2, 3, 8, 16
 
 # every symbol include/evox.h declares
 EXPORTS = (
@@ -35,7 +36,7 @@ EXPORTS = (
     "evox_permutation_scratch_bytes",
     "evox_permutation", "evox_argsort_u32",
     "evox_profile", "evox_profile_read", "evox_strerror", "evox_last_error",
-    "evox_linear", "evox_linear_grad_scratch_bytes", "evox_linear_grad",
+    "evox_layer_kernels", "evox_linear", "evox_linear_grad_scratch_bytes", "evox_linear_grad",
     "evox_layernorm", "evox_layernorm_grad_scratch_bytes", "evox_layernorm_grad",
     "evox_xent_scratch_bytes", "evox_xent",
 )
@@ -145,6 +146,7 @@ def lib():
             "evox_philox_fill": ([u64, u32, u32, u32, i64, P, P], i32),
             "evox_profile": ([P, i32], i32),
             "evox_profile_read": ([P, P, P, P], i32),
+            "evox_layer_kernels": ([P] * 4, i32),
             "evox_linear": ([P] * 8, i32),
             "evox_linear_grad_scratch_bytes": ([P], sz),
             "evox_linear_grad": ([P] * 9 + [sz, P], i32),
@@ -377,6 +379,15 @@ def _layer(x, w, y, act, off):
     _view("y", y, w, (M, n_out))
     return Layer(_dtype(w), act, G, M, n_in, n_out, _offsets(off, w, G), shared, _pitch(x), _pitch(w), _net_stride(w),
                  0, 0, 0, _pitch(y))
+
+
+def layer_kernels(dtype, G, M, n_in, n_out, ragged=False):
+    """(forward, dx, dw): the kernels of a layer of this type and these sizes, with
+    offsets or as many rows for each network (host arithmetic)."""
+    p = Layer(dtype, ACT_NONE, G, M, n_in, n_out, 4 if ragged else None)  # (the offsets are not read)
+    out = [ctypes.c_int32(0) for _ in range(3)]
+    _check(lib().evox_layer_kernels(ctypes.byref(p), *(ctypes.byref(o) for o in out)))
+    return tuple(o.value for o in out)
 
 
 def evox_linear(x, w, y, b=None, r=None, z=None, off=None, act=ACT_NONE, stream=None):

@@ -1674,6 +1674,16 @@ int evox_linear(const evox_layer *l, const void *x, const void *w, const void *b
     return EVOX_OK;
 }
 
+int evox_layer_kernels(const evox_layer *l, int32_t *forward, int32_t *dx, int32_t *dw)
+{
+    NetRows rows;
+    const int rc = check_layer(l, &rows);
+    if (rc != EVOX_OK) return rc;
+    if (!forward || !dx || !dw) return fail(EVOX_EINVAL, "forward, dx and dw are required");
+    linear_kernels(grad_args(l, rows), forward, dx, dw);
+    return EVOX_OK;
+}
+
 size_t evox_linear_grad_scratch_bytes(const evox_layer *l)
 {
     NetRows rows;

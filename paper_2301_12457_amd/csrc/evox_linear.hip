@@ -1,6 +1,7 @@
 // Linear layers of a population of networks: y = act(x W_g^T + b_g) + r and its
 // gradient.  Here: the choice of kernels, and those that need no LDS tiles (few
 // rows, narrow layers, short sums); evox_linear_tile.hip has the rest.
+#include "evox.h"
 #include "evox_tile.hpp"
 
 namespace evox {
@@ -818,30 +819,71 @@ GradScratch grad_layout(const LinearGradArgs &a)
     return g;
 }
 
+int64_t mean_rows(const NetRows &r) { return (r.M + r.G - 1) / r.G; }
+
+// The tiles, for their reuse, where their padding (64 rows, outputs and k) is
+// not most of them (without / with, us: bf16 512x512 24 rows 39 / 38, 48 rows 52 / 44,
+// fp32 77 / 78, 157 / 83; 500 rows 256x32 bf16 11 / 10, fp32 24 / 30, 256x48 15 / 10,
+// 38 / 30; 500 rows 64x300 24 / 28, 44 / 44, fp32 96x300 60 / 53), and where they are
+// not too few for the chip (tiles of 64 a side: 128, one network's 512 rows
+// 2048x1024, 18 / 22, 34 / 64; 192, 1024 rows 4096x768, 46 / 39, 93 / 118; 256, 1024 rows
+// 1024x1024, 18 / 14, 35 / 37; 384, 1024 rows 2048x1536, 46 / 24, 95 / 64).
+template <typename T>
+bool wide(const LinearArgs &a)
+{
+    return mean_rows(a.rows) > 24 && a.n_out > 32 && a.n_in >= (sizeof(T) == 2 ? 128 : 64);
+}
+template <typename T>
+bool tiles(const LinearArgs &a)
+{
+    return wide<T>(a) && net_tiles(a.rows, 6) * ((a.n_out + 63) / 64) > (sizeof(T) == 2 ? 128 : 256);
+}
+
+// Short sums: of few outputs (dx) or rows (dw; in fp32 dx too, whose tiles would
+// split every weight for two rows: 207x2 rows 3496x386 521 us, 611 in tiles, 1500x2 rows
+// 520x300 428, 547; bf16 1500x1 rows 100x300 312, 98, others even).
+template <typename T>
+bool short_dx(const LinearGradArgs &a)
+{
+    return (a.n_out <= kShortOutputs || (sizeof(T) == 4 && mean_rows(a.rows) <= kShortMean)) && a.n_in >= 64;
+}
+bool short_dw(const LinearGradArgs &a) { return mean_rows(a.rows) <= kShortMean && a.n_in >= 64; }
+
 }  // namespace
+
+void linear_kernels(const LinearGradArgs &a, int32_t *forward, int32_t *dx, int32_t *dw)
+{
+    net_dispatch(a.dtype, [&](auto t) {
+        using T = typename NetElement<t.value>::type;
+        LinearArgs l{};
+        l.rows = a.rows;
+        l.n_in = a.n_in;
+        l.n_out = a.n_out;
+        const auto of_tiles = [](int shape, int splits) { return EVOX_KERNEL_TILES + shape + (splits > 1 ? EVOX_KERNEL_SHARES : 0); };
+        *forward = tiles<T>(l) ? of_tiles(linear_tiles_shape<t.value>(l), 1) : EVOX_KERNEL_ROWS;
+        if (narrow(a)) *dx = *dw = EVOX_KERNEL_NARROW;
+        else if (few_inputs(a)) *dx = *dw = EVOX_KERNEL_FEW_INPUTS;
+        else {
+            *dx = short_dx<T>(a) ? (int)EVOX_KERNEL_SHORT : of_tiles(linear_dx_tiles_shape<t.value>(a, dx_splits(a)), dx_splits(a));
+            *dw = short_dw(a) ? (int)EVOX_KERNEL_SHORT : of_tiles(linear_dw_tiles_shape<t.value>(a, dw_splits(a)), dw_splits(a));
+        }
+        return hipSuccess;
+    });
+}
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto t) {
         using T = typename NetElement<t.value>::type;
-        const int64_t mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
-        // the tiles, for their reuse, where their padding (64 rows, outputs and k) is
-        // not most of them (here / tiles, us: bf16 512x512 24 rows 39 / 38, 48 rows 52 / 44,
-        // fp32 77 / 78, 157 / 83; 500 rows 256x32 bf16 11 / 10, fp32 24 / 30, 256x48 15 / 10,
-        // 38 / 30; 500 rows 64x300 24 / 28, 44 / 44, fp32 96x300 60 / 53), and where they are
-        // not too few for the chip (tiles of 64 a side: 128, one network's 512 rows
-        // 2048x1024, 18 / 22, 34 / 64; 192, 1024 rows 4096x768, 46 / 39, 93 / 118; 256, 1024 rows
-        // 1024x1024, 18 / 14, 35 / 37; 384, 1024 rows 2048x1536, 46 / 24, 95 / 64)
-        const bool wide = mean > 24 && a.n_out > 32 && a.n_in >= (sizeof(T) == 2 ? 128 : 64);
-        if (wide && net_tiles(a.rows, 6) * ((a.n_out + 63) / 64) > (sizeof(T) == 2 ? 128 : 256))
-            return launch_linear_tiles<t.value>(a, s);
+        if (tiles<T>(a)) return launch_linear_tiles<t.value>(a, s);
+        const int64_t mean = mean_rows(a.rows);
         // rows of a wave's tile by the mean rows per network (few k steps of 16 bits or
         // outputs: smaller tiles, more waves at a time: 200 rows 32x200 bf16 12.1, with 64 x
         // 32 13.0 us); one 16 x 16 tile where larger ones would leave most of the chip
         // without a wave (one network's 3000 rows 512x24 9.3, 10.9 us; fp32 512 rows 2048x256,
         // 128 tiles of 32 x 32, 17.6, 19.0; 4x128 rows 1024x512, 256 of them, 17.4, 12.4)
         const bool few_steps = a.n_in <= 2 * Mma<T>::KS && (sizeof(T) == 2 || a.n_out <= 16);
-        int rb = mean <= 16 ? 1 : mean <= 32 || few_steps || wide ? 2 : 4, nb = rb == 1 || a.n_out <= 16 ? 1 : 2;
+        int rb = mean <= 16 ? 1 : mean <= 32 || few_steps || wide<T>(a) ? 2 : 4, nb = rb == 1 || a.n_out <= 16 ? 1 : 2;
         const int64_t steps = (a.n_in + Mma<T>::KS - 1) / Mma<T>::KS;
         const auto units_of = [&](int r, int n) {
             return net_tiles(a.rows, r == 1 ? 4 : r == 2 ? 5 : 6) * ((a.n_out + 16 * n - 1) / (16 * n));
@@ -881,7 +923,7 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         using T = typename NetElement<t.value>::type;
         constexpr int N = NetVec<T>::N;
         const GradScratch l = grad_layout(a);
-        const int64_t mean = (a.rows.M + a.rows.G - 1) / a.rows.G;
+        const int64_t mean = mean_rows(a.rows);
         hipError_t e = hipSuccess;
         if (narrow(a) || few_inputs(a)) {
             const int sh = few_inputs(a) ? kFewShift : narrow_shift(a);
@@ -928,13 +970,10 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         const void *dd = own ? d : a.dy;
         const int64_t ldd = own ? l.ldd : a.lddy;
         float *part = (float *)((char *)a.scratch + l.part);
-        // short sums: of few outputs (dx) or rows (dw; in fp32 dx too, whose tiles would
-        // split every weight for two rows: 207x2 rows 3496x386 521 us, 611 in tiles, 1500x2 rows
-        // 520x300 428, 547; bf16 1500x1 rows 100x300 312, 98, others even); else tiles
-        int L = 1;
+        int L = 1;  // of short sums
         while (L < 256 && L * N < a.n_in) L *= 2;
         const int64_t cols = (a.n_in + L * N - 1) / (L * N);
-        if (a.dx && (a.n_out <= kShortOutputs || (sizeof(T) == 4 && mean <= kShortMean)) && a.n_in >= 64) {
+        if (a.dx && short_dx<T>(a)) {
             const int64_t units = net_tiles(a.rows, kShortShift);
             hipLaunchKernelGGL((k_linear_short<T, false>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, low,
                                ldd, L, units);
@@ -949,7 +988,7 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
             }
         }
         if (e != hipSuccess || !a.dw) return e;
-        if (mean <= kShortMean && a.n_in >= 64) {
+        if (short_dw(a)) {
             const int64_t units = a.rows.G * ((a.n_out + kShortRows - 1) / kShortRows);
             hipLaunchKernelGGL((k_linear_short<T, true>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, low,
                                ldd, L, units);

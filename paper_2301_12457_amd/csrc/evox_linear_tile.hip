@@ -207,8 +207,8 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dw_tile(Linea
 // 1024x1024 15 in shape 0, then 19, 22, 32).  jt(BJ): tiles along j.  A CU holds
 // (by LDS and registers) 3, 2, 1, 1 blocks of the fp32 shapes and 5, 2, 1, 1 of the
 // 16-bit ones.
-template <typename F, typename J>
-hipError_t with_shape(int64_t ni, J &&jt, F &&f)
+template <typename J>
+int best_shape(int64_t ni, J &&jt)
 {
     constexpr int per32[4] = {3, 2, 1, 1}, per16[4] = {5, 2, 1, 1};
     int best = 0;
@@ -229,7 +229,13 @@ hipError_t with_shape(int64_t ni, J &&jt, F &&f)
     cost(integral_constant<int, 1>{});
     cost(integral_constant<int, 2>{});
     cost(integral_constant<int, 3>{});
-    switch (best) {
+    return best;
+}
+template <typename F>
+hipError_t with_shape(int shape, F &&f)
+{
+    using std::integral_constant;
+    switch (shape) {
     case 0: return f(integral_constant<int, 0>{});
     case 1: return f(integral_constant<int, 1>{});
     case 2: return f(integral_constant<int, 2>{});
@@ -251,9 +257,26 @@ hipError_t launch_tiles(K *kernel, int64_t units, hipStream_t s, A... args)
 }  // namespace
 
 template <>
+int linear_tiles_shape<EVOX_NET_TYPE>(const LinearArgs &a)
+{
+    return best_shape(a.n_out, row_tiles(a.rows));
+}
+// (shares of K are for few tiles: the smallest ones)
+template <>
+int linear_dx_tiles_shape<EVOX_NET_TYPE>(const LinearGradArgs &a, int splits)
+{
+    return splits > 1 ? 0 : best_shape(a.n_in, row_tiles(a.rows));
+}
+template <>
+int linear_dw_tiles_shape<EVOX_NET_TYPE>(const LinearGradArgs &a, int splits)
+{
+    return splits > 1 ? 0 : best_shape(a.n_in, [&](int BJ) { return a.rows.G * ((a.n_out + BJ - 1) / BJ); });
+}
+
+template <>
 hipError_t launch_linear_tiles<EVOX_NET_TYPE>(const LinearArgs &a, hipStream_t s)
 {
-    return with_shape(a.n_out, row_tiles(a.rows), [&](auto id) {
+    return with_shape(linear_tiles_shape<EVOX_NET_TYPE>(a), [&](auto id) {
         constexpr int ID = id.value, B = Shape<ID>::BI;
         typedef Product<ID, false, false> G;
         const int64_t ti = (a.n_out + B - 1) / B, tj = net_tiles(a.rows, Shape<ID>::sh);
@@ -265,31 +288,26 @@ template <>
 hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd,
                                                  int splits, float *part, hipStream_t s)
 {
-    const auto go = [&](auto id) {
+    return with_shape(linear_dx_tiles_shape<EVOX_NET_TYPE>(a, splits), [&](auto id) {
         constexpr int ID = id.value, B = Shape<ID>::BI;
         typedef Product<ID, true, false> G;
         const int64_t ti = (a.n_in + B - 1) / B, tj = net_tiles(a.rows, Shape<ID>::sh);
         return launch_tiles<G>(k_linear_dx_tile<ID>, banded(tj) * ti * splits, s, a, (const Elem *)d, (const Elem *)low,
                                ldd, ti, tj, splits, part);
-    };
-    if (splits > 1) return go(std::integral_constant<int, 0>{});
-    return with_shape(a.n_in, row_tiles(a.rows), go);
+    });
 }
 
 template <>
 hipError_t launch_linear_dw_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd,
                                                  int splits, float *part, hipStream_t s)
 {
-    const auto out_tiles = [&](int BJ) { return a.rows.G * ((a.n_out + BJ - 1) / BJ); };
-    const auto go = [&](auto id) {
+    return with_shape(linear_dw_tiles_shape<EVOX_NET_TYPE>(a, splits), [&](auto id) {
         constexpr int ID = id.value, B = Shape<ID>::BI, BJ = Shape<ID>::BJ;
         typedef Product<ID, true, true> G;
         const int64_t ti = (a.n_in + B - 1) / B, tj = (a.n_out + BJ - 1) / BJ;
         return launch_tiles<G>(k_linear_dw_tile<ID>, a.rows.G * banded(tj) * ti * splits, s, a, (const Elem *)d,
                                (const Elem *)low, ldd, ti, tj, splits, part);
-    };
-    if (splits > 1) return go(std::integral_constant<int, 0>{});
-    return with_shape(a.n_in, out_tiles, go);
+    });
 }
 
 }  // namespace evox

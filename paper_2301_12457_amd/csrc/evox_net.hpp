@@ -80,6 +80,17 @@ template <int TYPE>
 hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd, int splits,
                                   float *part, hipStream_t s);
 
+// The tile shape that the same calls take (0 .. 3).
+template <int TYPE>
+int linear_tiles_shape(const LinearArgs &a);
+template <int TYPE>
+int linear_dx_tiles_shape(const LinearGradArgs &a, int splits);
+template <int TYPE>
+int linear_dw_tiles_shape(const LinearGradArgs &a, int splits);
+
+// Which kernels a layer and its gradient take (enum evox_layer_kernel).
+void linear_kernels(const LinearGradArgs &a, int32_t *forward, int32_t *dx, int32_t *dw);
+
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
