@@ -672,10 +672,12 @@ bool few_inputs(const LinearGradArgs &a)
 // rows (a tile's, or outputs) by L chunks.  For sums of at most 8 outputs or 4
 // rows over at least 64 columns: the whole gradient of 1566 networks' 2 rows
 // 304x1 takes 25 us, 101 in tiles; of 100,000 rows 1000x16 (bf16) 163, in tiles 143.
+// LOW: of both numbers of d, a kernel of its own: in one with a branch the gradient
+// without an activation of bf16 500x3 rows 1000x1000 took 577 us, 539 so.
 // ---------------------------------------------------------------------------
 constexpr int kShortRows = 16, kShortShift = 4, kShortOutputs = 8, kShortMean = 4;
 
-template <typename T, bool DW>
+template <typename T, bool DW, bool LOW>
 __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T *d, const T *low, int64_t ldd, int L, int64_t units)
 {
     constexpr int N = NetVec<T>::N;
@@ -700,7 +702,7 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
         p = (const T *)a.x + (a.x_shared ? 0 : lo) * a.ldx;
         ldp = a.ldx;
         q = d + lo * ldd + o0;
-        ql = low ? low + lo * ldd + o0 : nullptr;
+        ql = low + lo * ldd + o0;
         out = (T *)a.dw + g * a.dw_stride + o0 * a.lddw;
         ldo = a.lddw;
     } else {
@@ -711,7 +713,7 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
         p = (const T *)a.w + t.g * a.w_stride;
         ldp = a.ldw;
         q = d + t.lo * ldd;
-        ql = low ? low + t.lo * ldd : nullptr;
+        ql = low + t.lo * ldd;
         out = (T *)a.dx + t.lo * a.lddx;
         ldo = a.lddx;
     }
@@ -719,7 +721,8 @@ __global__ __launch_bounds__(256) void k_linear_short(LinearGradArgs a, const T 
     // up to four of d's neighbours
     const auto load_d = [&](int64_t at, int n) -> f32x4 {
         const f32x4 h = load_quad(q + at, n);
-        return ql ? h * d_up<T> + load_quad(ql + at, n) * d_down<T> : h;
+        if constexpr (LOW) return h * d_up<T> + load_quad(ql + at, n) * d_down<T>;
+        else return h;
     };
     for (int r0 = slot * 4; r0 < R; r0 += slots * 4) {
         float acc[4][N];
@@ -973,12 +976,16 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         int L = 1;  // of short sums
         while (L < 256 && L * N < a.n_in) L *= 2;
         const int64_t cols = (a.n_in + L * N - 1) / (L * N);
-        if (a.dx && short_dx<T>(a)) {
-            const int64_t units = net_tiles(a.rows, kShortShift);
-            hipLaunchKernelGGL((k_linear_short<T, false>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, low,
-                               ldd, L, units);
-            e = hipGetLastError();
-        } else if (a.dx) {
+        const auto short_sums = [&](auto dw, int64_t units) {
+            constexpr bool DW = dw.value;
+            auto kernel = k_linear_short<T, DW, false>;
+            if constexpr (sizeof(T) == 2)
+                if (low) kernel = k_linear_short<T, DW, true>;
+            hipLaunchKernelGGL(kernel, net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, low, ldd, L, units);
+            return hipGetLastError();
+        };
+        if (a.dx && short_dx<T>(a)) e = short_sums(std::false_type{}, net_tiles(a.rows, kShortShift));
+        else if (a.dx) {
             const int splits = dx_splits(a);
             e = launch_linear_dx_tiles<t.value>(a, dd, low, ldd, splits, part, s);
             if (e == hipSuccess && splits > 1) {
@@ -988,12 +995,7 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
             }
         }
         if (e != hipSuccess || !a.dw) return e;
-        if (short_dw(a)) {
-            const int64_t units = a.rows.G * ((a.n_out + kShortRows - 1) / kShortRows);
-            hipLaunchKernelGGL((k_linear_short<T, true>), net_grid(units * cols), dim3(256), 0, s, a, (const T *)dd, low,
-                               ldd, L, units);
-            return hipGetLastError();
-        }
+        if (short_dw(a)) return short_sums(std::true_type{}, a.rows.G * ((a.n_out + kShortRows - 1) / kShortRows));
         const int splits = dw_splits(a);
         e = launch_linear_dw_tiles<t.value>(a, dd, low, ldd, splits, part, s);
         if (e != hipSuccess || splits == 1) return e;

@@ -142,7 +142,8 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_tile(LinearAr
 }
 
 // dx = d W: i = input, j = row, k = output.
-template <int ID>
+// LOW: of both numbers of d.
+template <int ID, bool LOW>
 __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(LinearGradArgs a, const Elem *d, const Elem *low,
                                                                                       int64_t ldd, int64_t ti, int64_t tj,
                                                                                       int splits, float *part, int64_t units)
@@ -156,10 +157,13 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(Linea
     const NetTile t = net_tile(a.rows, Shape<ID>::sh, jt);
     if (t.g < 0) return;
     const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_in - i0, Shape<ID>::BI), nj = (int)(t.hi - t.lo);
-    const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + k0 * a.ldw + i0, a.ldw, ni}, Q{d + t.lo * ldd + k0, ldd, nj},
-        R{low ? low + t.lo * ldd + k0 : nullptr, ldd, nj};
+    const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + k0 * a.ldw + i0, a.ldw, ni}, Q{d + t.lo * ldd + k0, ldd, nj};
     Product<ID, true, false> p;
-    p.run_split(P, Q, R, k1 - k0, lds);
+    if constexpr (LOW) p.run_split(P, Q, TileOp<Elem>{low + t.lo * ldd + k0, ldd, nj}, k1 - k0, lds);
+    else {
+        p.clear();
+        p.run(P, Q, k1 - k0, lds);
+    }
     if (splits > 1) {
         PartOut out{part + ((us - u * splits) * a.rows.M + t.lo) * a.n_in + i0, a.n_in};
         p.results(ni, nj, lds, out);
@@ -170,7 +174,7 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(Linea
 }
 
 // dW = d^T x: i = input, j = output, k = row of the network.
-template <int ID>
+template <int ID, bool LOW>
 __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dw_tile(LinearGradArgs a, const Elem *d, const Elem *low,
                                                                                       int64_t ldd, int64_t ti, int64_t tj,
                                                                                       int splits, float *part, int64_t units)
@@ -186,10 +190,13 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dw_tile(Linea
     share_of(hi - lo, splits, (int)z, &k0, &k1);
     const int i0 = (int)it * Shape<ID>::BI, ni = min((int)a.n_in - i0, Shape<ID>::BI), j0 = (int)jt * Shape<ID>::BJ,
               nj = min((int)a.n_out - j0, Shape<ID>::BJ);
-    const TileOp<Elem> P{(const Elem *)a.x + ((a.x_shared ? 0 : lo) + k0) * a.ldx + i0, a.ldx, ni}, Q{d + (lo + k0) * ldd + j0, ldd, nj},
-        R{low ? low + (lo + k0) * ldd + j0 : nullptr, ldd, nj};
+    const TileOp<Elem> P{(const Elem *)a.x + ((a.x_shared ? 0 : lo) + k0) * a.ldx + i0, a.ldx, ni}, Q{d + (lo + k0) * ldd + j0, ldd, nj};
     Product<ID, true, true> p;
-    p.run_split(P, Q, R, k1 - k0, lds);
+    if constexpr (LOW) p.run_split(P, Q, TileOp<Elem>{low + (lo + k0) * ldd + j0, ldd, nj}, k1 - k0, lds);
+    else {
+        p.clear();
+        p.run(P, Q, k1 - k0, lds);
+    }
     if (splits > 1) {
         PartOut out{part + ((z * a.rows.G + g) * a.n_out + j0) * a.n_in + i0, a.n_in};
         p.results(ni, nj, lds, out);
@@ -292,8 +299,13 @@ hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const 
         constexpr int ID = id.value, B = Shape<ID>::BI;
         typedef Product<ID, true, false> G;
         const int64_t ti = (a.n_in + B - 1) / B, tj = net_tiles(a.rows, Shape<ID>::sh);
-        return launch_tiles<G>(k_linear_dx_tile<ID>, banded(tj) * ti * splits, s, a, (const Elem *)d, (const Elem *)low,
-                               ldd, ti, tj, splits, part);
+        const auto go = [&](auto kernel) {
+            return launch_tiles<G>(kernel, banded(tj) * ti * splits, s, a, (const Elem *)d, (const Elem *)low, ldd, ti, tj,
+                                   splits, part);
+        };
+        if constexpr (sizeof(Elem) == 2)
+            if (low) return go(k_linear_dx_tile<ID, true>);
+        return go(k_linear_dx_tile<ID, false>);
     });
 }
 
@@ -305,8 +317,13 @@ hipError_t launch_linear_dw_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const 
         constexpr int ID = id.value, B = Shape<ID>::BI, BJ = Shape<ID>::BJ;
         typedef Product<ID, true, true> G;
         const int64_t ti = (a.n_in + B - 1) / B, tj = (a.n_out + BJ - 1) / BJ;
-        return launch_tiles<G>(k_linear_dw_tile<ID>, a.rows.G * banded(tj) * ti * splits, s, a, (const Elem *)d,
-                               (const Elem *)low, ldd, ti, tj, splits, part);
+        const auto go = [&](auto kernel) {
+            return launch_tiles<G>(kernel, a.rows.G * banded(tj) * ti * splits, s, a, (const Elem *)d, (const Elem *)low, ldd,
+                                   ti, tj, splits, part);
+        };
+        if constexpr (sizeof(Elem) == 2)
+            if (low) return go(k_linear_dw_tile<ID, true>);
+        return go(k_linear_dw_tile<ID, false>);
     });
 }
 

@@ -550,19 +550,15 @@ struct TileProduct {
             if (__syncthreads_or(!(big < kTileBig))) again(P, Q, K);
     }
 
-    // The product of P and d_up Q + d_down R (R.p null: of P and Q), K once for each
-    // of the two, the small one first.
+    // The product of P and d_up Q + d_down R, K once for each of the two, the small one
+    // first.
     __device__ __forceinline__ void run_split(const TileOp<T> &P, const TileOp<T> &Q, const TileOp<T> &R, int64_t K, char *lds)
     {
         clear();
-        if constexpr (!kSplit)
-            if (R.p) {
-                run(P, R, K, lds);
-                if constexpr (d_up<T> != 1.0f) scale(d_down<T> / d_up<T>);
-            }
+        run(P, R, K, lds);
+        if constexpr (d_up<T> != 1.0f) scale(d_down<T> / d_up<T>);
         run(P, Q, K, lds);
-        if constexpr (d_up<T> != 1.0f)
-            if (R.p) scale(d_up<T>);
+        if constexpr (d_up<T> != 1.0f) scale(d_up<T>);
     }
 
     // The results, S rows of every wave at a time through LDS (the wave's own part
