@@ -576,10 +576,11 @@ int evox_linear_grad(const evox_layer *layer, const void *x, const void *w, cons
                      void *dw, void *db, void *scratch, size_t scratch_bytes, void *hip_stream);
 
 /* The kernels that a layer's products take, for tests and reports: by element type,
- * sizes and whether there are offsets alone, nothing else of *layer is looked at.
- * ROWS: operands straight from memory; NARROW, FEW_INPUTS: the whole gradient in one
- * pass; SHORT: sums of few terms; TILES + 0 .. 3: tiles through LDS, smallest first,
- * + SHARES: of parts of a long sum. */
+ * sizes, activation and whether there are offsets alone, nothing else of *layer is
+ * looked at.  ROWS: operands straight from memory; NARROW, FEW_INPUTS: the whole
+ * gradient in one pass; SHORT: sums of few terms; TILES + 0 .. 3: tiles through LDS,
+ * smallest first, + 4: of a 16-bit d's two numbers side by side, + SHARES: of parts of
+ * a long sum. */
 enum evox_layer_kernel { EVOX_KERNEL_ROWS = 0, EVOX_KERNEL_NARROW = 1, EVOX_KERNEL_FEW_INPUTS = 2, EVOX_KERNEL_SHORT = 3,
                          EVOX_KERNEL_TILES = 16, EVOX_KERNEL_SHARES = 8 };
 int evox_layer_kernels(const evox_layer *layer, int32_t *forward, int32_t *dx, int32_t *dw);

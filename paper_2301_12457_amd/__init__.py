@@ -381,10 +381,10 @@ def _layer(x, w, y, act, off):
                  0, 0, 0, _pitch(y))
 
 
-def layer_kernels(dtype, G, M, n_in, n_out, ragged=False):
+def layer_kernels(dtype, G, M, n_in, n_out, ragged=False, act=ACT_NONE):
     """(forward, dx, dw): the kernels of a layer of this type and these sizes, with
     offsets or as many rows for each network (host arithmetic)."""
-    p = Layer(dtype, ACT_NONE, G, M, n_in, n_out, 4 if ragged else None)  # (the offsets are not read)
+    p = Layer(dtype, act, G, M, n_in, n_out, 4 if ragged else None)  # (the offsets are not read)
     out = [ctypes.c_int32(0) for _ in range(3)]
     _check(lib().evox_layer_kernels(ctypes.byref(p), *(ctypes.byref(o) for o in out)))
     return tuple(o.value for o in out)

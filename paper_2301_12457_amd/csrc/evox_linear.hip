@@ -958,7 +958,7 @@ hipError_t launch_linear_grad(const LinearGradArgs &a, hipStream_t s)
         const DzShape dz = dz_shape(a);
         const bool own = a.act != ACT_NONE && (a.dx || a.dw);
         T *d = own ? (T *)a.scratch : nullptr;
-        T *low = own && sizeof(T) == 2 && a.act != ACT_RELU ? (T *)((char *)a.scratch + l.low) : nullptr;
+        T *low = own && sizeof(T) == 2 && a.act > ACT_RELU ? (T *)((char *)a.scratch + l.low) : nullptr;
         float *sums = a.db ? (float *)((char *)a.scratch + l.sums) : nullptr;
         if (a.rows.M > 0 && (d || sums)) {
             hipLaunchKernelGGL((k_linear_dz<T>), net_grid(net_tiles(a.rows, dz.sh) * dz.cols), dim3(256),

@@ -112,6 +112,9 @@ struct Shape {
     static constexpr int WI = BI / 64, WJ = 2, kThreads = 64 * WI * WJ;
     static constexpr int sh = BJ == 64 ? 6 : BJ == 128 ? 7 : 8;
 };
+constexpr int kPairShift = 5;  // rows of a network per pair tile, as a power of two
+bool pairs(const LinearGradArgs &a) { return (a.rows.M + a.rows.G - 1) / a.rows.G <= (int64_t)1 << kPairShift; }
+
 template <int ID, bool PM, bool QM>
 using Product = TileProduct<Elem, PM, QM, Shape<ID>::BI, Shape<ID>::BJ, Shape<ID>::WI, Shape<ID>::WJ>;
 
@@ -172,6 +175,38 @@ __global__ __launch_bounds__(Shape<ID>::kThreads, 2) void k_linear_dx_tile(Linea
     PlainOut out{(Elem *)a.dx + t.lo * a.lddx + i0, a.lddx};
     p.results(ni, nj, lds, out);
 }
+
+#if EVOX_NET_TYPE
+// dx of few rows per network from both numbers of d: 32 rows of the one and of the
+// other in a tile of 64, so that the weights, which bound it, are read once (bf16 1500x2
+// rows 520x300: the gradient 379 us, with the weights read twice 480).
+__global__ __launch_bounds__(Shape<0>::kThreads, 2) void k_linear_dx_pair(LinearGradArgs a, const Elem *d, const Elem *low, int64_t ldd,
+                                                                          int64_t ti, int64_t tj, int splits, float *part,
+                                                                          int64_t units)
+{
+    typedef Product<0, true, false> G;
+    __shared__ __attribute__((aligned(16))) char lds[G::kLds];
+    const int64_t us = xcd_unit(units), u = us / splits;
+    if (us < 0) return;
+    int64_t it, jt, k0, k1;
+    unit_ij(u, ti, tj, &it, &jt);
+    share_of(a.n_out, splits, (int)(us - u * splits), &k0, &k1);
+    const NetTile t = net_tile(a.rows, kPairShift, jt);
+    if (t.g < 0) return;
+    const int i0 = (int)it * 64, ni = min((int)a.n_in - i0, 64), nj = (int)(t.hi - t.lo);
+    const TileOp<Elem> P{(const Elem *)a.w + t.g * a.w_stride + k0 * a.ldw + i0, a.ldw, ni}, Q{d + t.lo * ldd + k0, ldd, nj};
+    G p;
+    p.clear();
+    p.run<true>(P, Q, k1 - k0, lds, low + t.lo * ldd + k0);
+    if (splits > 1) {
+        PartOut out{part + ((us - u * splits) * a.rows.M + t.lo) * a.n_in + i0, a.n_in};
+        p.results_pair(ni, nj, lds, out);
+        return;
+    }
+    PlainOut out{(Elem *)a.dx + t.lo * a.lddx + i0, a.lddx};
+    p.results_pair(ni, nj, lds, out);
+}
+#endif
 
 // dW = d^T x: i = input, j = output, k = row of the network.
 template <int ID, bool LOW>
@@ -268,10 +303,11 @@ int linear_tiles_shape<EVOX_NET_TYPE>(const LinearArgs &a)
 {
     return best_shape(a.n_out, row_tiles(a.rows));
 }
-// (shares of K are for few tiles: the smallest ones)
+// (shares of K are for few tiles: the smallest ones; 4: a pair)
 template <>
 int linear_dx_tiles_shape<EVOX_NET_TYPE>(const LinearGradArgs &a, int splits)
 {
+    if (sizeof(Elem) == 2 && a.act > ACT_RELU && pairs(a)) return 4;
     return splits > 1 ? 0 : best_shape(a.n_in, row_tiles(a.rows));
 }
 template <>
@@ -295,6 +331,13 @@ template <>
 hipError_t launch_linear_dx_tiles<EVOX_NET_TYPE>(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd,
                                                  int splits, float *part, hipStream_t s)
 {
+#if EVOX_NET_TYPE
+    if (low && pairs(a)) {
+        const int64_t ti = (a.n_in + 63) / 64, tj = net_tiles(a.rows, kPairShift);
+        return launch_tiles<Product<0, true, false>>(k_linear_dx_pair, banded(tj) * ti * splits, s, a, (const Elem *)d,
+                                                     (const Elem *)low, ldd, ti, tj, splits, part);
+    }
+#endif
     return with_shape(linear_dx_tiles_shape<EVOX_NET_TYPE>(a, splits), [&](auto id) {
         constexpr int ID = id.value, B = Shape<ID>::BI;
         typedef Product<ID, true, false> G;

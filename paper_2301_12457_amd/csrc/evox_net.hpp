@@ -80,7 +80,7 @@ template <int TYPE>
 hipError_t launch_linear_dw_tiles(const LinearGradArgs &a, const void *d, const void *low, int64_t ldd, int splits,
                                   float *part, hipStream_t s);
 
-// The tile shape that the same calls take (0 .. 3).
+// The tile shape that the same calls take (0 .. 3; 4: dx of a pair).
 template <int TYPE>
 int linear_tiles_shape(const LinearArgs &a);
 template <int TYPE>

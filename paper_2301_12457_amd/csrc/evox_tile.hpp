@@ -125,6 +125,15 @@ struct Stage16c {
             row[p] = src + (int64_t)(r < n ? r : n - 1) * ld;
         }
     }
+    // the first half of the rows of one operand, the second of another of as many rows
+    __device__ __forceinline__ void init_pair(const T *src, const T *other, int64_t ld, int n)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int r = threadIdx.x / 8 + p * (TH / 8), h = r % (R / 2);
+            row[p] = (r < R / 2 ? src : other) + (int64_t)(h < n ? h : n - 1) * ld;
+        }
+    }
     __device__ __forceinline__ bool whole() const { return true; }
     __device__ __forceinline__ void load_piece(int p, int64_t k0)  // k0 + 64 <= K
     {
@@ -510,14 +519,17 @@ struct TileProduct {
         for (int w = 0; w < SQ::kStores; ++w) sq.store_piece(w, lds + kStageBytes<T, BI>, big);
     }
 
-    // The product, added to acc; ends with all waves past their last use of LDS.
-    __device__ __forceinline__ void run(const TileOp<T> &P, const TileOp<T> &Q, int64_t K, char *lds)
+    // The product, added to acc; ends with all waves past their last use of LDS.  PAIR:
+    // Q's rows in the first half of the tile, R's (R.p, as many) in the second.
+    template <bool PAIR = false>
+    __device__ __forceinline__ void run(const TileOp<T> &P, const TileOp<T> &Q, int64_t K, char *lds, const T *R = nullptr)
     {
         Stage<T, PM, BI, kThreads> sp;
         Stage<T, QM, BJ, kThreads> sq;
         if (K <= 0) return;
         sp.init(P.p, P.ld, P.n);
-        sq.init(Q.p, Q.ld, Q.n);
+        if constexpr (PAIR) sq.init_pair(Q.p, R, Q.ld, Q.n);
+        else sq.init(Q.p, Q.ld, Q.n);
         float big = 0.0f;
         const int64_t tiles = (K + BK - 1) / BK;
         sp.load(0, K);
@@ -561,6 +573,40 @@ struct TileProduct {
         if constexpr (d_up<T> != 1.0f) scale(d_up<T>);
     }
 
+    // A wave's sub-tiles j to its own part of LDS, S rows of kPitch.
+    __device__ __forceinline__ void sub_tile(int j, float *mine) const
+    {
+#pragma unroll
+        for (int k = 0; k < TI; ++k)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {  // the lane's quads of the tile
+                f32x4 t;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = acc[k][j][4 * b + e];
+                *reinterpret_cast<f32x4 *>(mine + row * kPitch + k * S + 8 * b + 4 * q) = t;
+            }
+    }
+
+    // The results of a pair, two waves of one sub-tile each: row j of the one and of the
+    // other, d_up and d_down times; every wave stores half of the rows.
+    template <typename F>
+    __device__ __forceinline__ void results_pair(int ni, int nj, char *lds, F &out)
+    {
+        static_assert(WI == 1 && WJ == 2 && TJ == 1, "two waves");
+        constexpr int N = NetVec<T>::N, kLanes = BI / N, kRows = 64 / kLanes;
+        float *all = reinterpret_cast<float *>(lds);
+        sub_tile(0, all + wj * S * kPitch);
+        lds_barrier();
+        const int lane = threadIdx.x % 64, i = lane % kLanes * N, n = ni - i < N ? ni - i : N;
+        for (int r = wj * (S / 2) + lane / kLanes; r < (wj + 1) * (S / 2); r += kRows) {
+            if (r >= nj || n <= 0) continue;
+            float v[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = all[r * kPitch + i + e] * d_up<T> + all[(S + r) * kPitch + i + e] * d_down<T>;
+            out.store(r, i, v, n, {});
+        }
+    }
+
     // The results, S rows of every wave at a time through LDS (the wave's own part
     // of it).  A lane gets n <= N neighbours i .. i + n - 1 of a row j at a time (N:
     // 16 bytes of the element type, a row's in consecutive lanes), always the same
@@ -581,15 +627,7 @@ struct TileProduct {
 #pragma unroll
             for (int it = 0; it < kIter; ++it)
                 if (r0 + it * kRows < nj && n > 0) loaded[it] = out.load(r0 + it * kRows, i, n);
-#pragma unroll
-            for (int k = 0; k < TI; ++k)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {  // the lane's quads of the tile
-                    f32x4 t;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) t[e] = acc[k][j][4 * b + e];
-                    *reinterpret_cast<f32x4 *>(mine + row * kPitch + k * S + 8 * b + 4 * q) = t;
-                }
+            sub_tile(j, mine);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
             for (int it = 0; it < kIter; ++it) {

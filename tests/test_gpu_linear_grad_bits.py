@@ -85,3 +85,49 @@ def test_infinities_and_nan_in_dy(evox_gpu, dtype, n_in, n_out, n):
             assert torch.equal(torch.isnan(got), torch.isnan(want))
             inf = torch.isinf(want)
             assert torch.equal(got[inf], want[inf]) and inf.any()
+
+
+# few rows per network (both of d's numbers in one tile of dx): rows past one such
+# tile, none, odd widths, shares of a long fan-out
+PAIRS = [([9, 0, 32, 1, 70, 33, 2] * 3, 200, 260), ([32] * 20, 64, 128), ([12, 5, 20], 331, 1756), ([1] * 50, 130, 90),
+         ([5, 31] * 9, 515, 67), ([20], 49, 50)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", ["relu", "tanh", "gelu", "silu"])
+@pytest.mark.parametrize("i", range(len(PAIRS)))
+def test_one_rounding_of_few_rows(evox_gpu, dtype, act, i):
+    counts, n_in, n_out = PAIRS[i]
+    print(f"gradient bits {dtype} {counts[:4]} x{len(counts)} {n_in}x{n_out} {act}", flush=True)
+    check(evox_gpu, layer(dtype, counts, n_in, n_out, lead=i % 2, even=len(set(counts)) == 1, seed=110 + i), act, f"case {i} {act}")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_few_rows_leave_the_others(evox_gpu, dtype):
+    """Rows of no network stay, and offsets past the rows stay inside the buffers."""
+    s = layer(dtype, [10, 10, 10, 10], 130, 90, seed=120)
+    for off, mine in (([2, 4, 4, 30, 35], [(2, 4, 0), (4, 30, 2), (30, 35, 3)]), ([-5, 12, 8, 40, 4000], [(0, 8, 0), (12, 40, 2)])):
+        dx = torch.full((40, 130), 7.0, dtype=dtype, device="cuda")
+        evox_gpu.evox_linear_grad(s["x"], s["w"], s["dy"], z=s["z"], dx=dx, act=evox_gpu.ACT_TANH,
+                                  off=torch.tensor(off, dtype=torch.int32, device="cuda"))
+        d = s["dy"].double() * nr.slope64(s["z"].double(), "tanh")
+        for a, e, g in mine:
+            if off[0] < 0 and g == 2:
+                continue  # (rows of two networks)
+            want = d[a:e] @ s["w"][g].double()
+            close(dx[a:e], want, 1e-5 * (d[a:e].abs() @ s["w"][g].double().abs()), dtype, f"{off} {g}")
+        assert off[0] < 0 or ((dx[:2] == 7).all() and (dx[35:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_few_rows_with_infinities(evox_gpu, dtype):
+    s = layer(dtype, [20, 25], 200, 260, seed=121)
+    s["dy"][3, 5], s["dy"][7, 6], s["dy"][29, 8] = float("inf"), float("nan"), -float("inf")
+    dx = filled(45, 200, dtype)
+    evox_gpu.evox_linear_grad(s["x"], s["w"], s["dy"], z=s["z"], dx=dx, off=s["off"], act=evox_gpu.ACT_SILU)
+    d = s["dy"].double() * nr.slope64(s["z"].double(), "silu")
+    for g, (a, e) in enumerate(s["spans"]):
+        got, want = dx[a:e].double(), d[a:e] @ s["w"][g].double()
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        inf = torch.isinf(want)
+        assert torch.equal(got[inf], want[inf]) and inf.any()

@@ -55,3 +55,10 @@ def test_kernels_refuse(evox):
         evox.layer_kernels(evox.F32, 4, 6, 4, 3)
     with pytest.raises(evox.EvoxError):
         evox.layer_kernels(3, 2, 6, 4, 3)
+
+
+def test_pairs_of_both_kinds(evox):
+    import test_gpu_linear_grad_bits as t
+    reached = {evox.layer_kernels(dt, len(counts), sum(counts), n_in, n_out, len(set(counts)) > 1, evox.ACT_GELU)[1]
+               for counts, n_in, n_out in t.PAIRS for dt in (evox.BF16, evox.F16)}
+    assert {evox.KERNEL_TILES + 4, evox.KERNEL_TILES + 4 + evox.KERNEL_SHARES} <= reached, reached
