@@ -525,7 +525,10 @@ int evox_profile_read(evox_state *state, double *fused_ms, int64_t *fused_launch
  * may own no row.
  *
  * All operands of a call have one element type, sums are in fp32 (fp64 for the
- * fitness) and each result is rounded once.  Pointers and pitches need no more
+ * fitness) and each result is rounded once.  fp32 products of many rows run on the
+ * bf16 matrix cores, each number as the sum of three: a term is within 2^-24 of the
+ * exact one, as one fp32 rounding is, and numbers below 2^-100 keep what is above
+ * 2^-126 of them; other fp32 products are fp32 multiply-adds.  Pointers and pitches need no more
  * than the element's own alignment; row pitches are below 2^31 elements, strides
  * below 2^40, and all offsets 64 bits.  Outputs must not
  * overlap inputs, but for y = r (equal pitch) and dx = dy of the norm.  The
@@ -570,7 +573,10 @@ int evox_linear(const evox_layer *layer, const void *x, const void *w, const voi
  * 2^-35 and beyond the type's largest number.  EVOX_EINVAL for dx
  * with x_shared (data has no gradient), and for w_stride = 0 with G > 1
  * (give the one network's rows as G = 1).  scratch: device,
- * evox_linear_grad_scratch_bytes(layer) bytes, 256-byte aligned. */
+ * evox_linear_grad_scratch_bytes(layer) bytes, 256-byte aligned: about the size of
+ * dy (16 bits: twice) and the column sums and partial products of its tiles; of up to
+ * 32 inputs and more than 64 outputs (n_in + 1) / 8 bytes per element of dy, which in
+ * 16 bits is more than dy from 16 inputs on. */
 size_t evox_linear_grad_scratch_bytes(const evox_layer *layer);
 int evox_linear_grad(const evox_layer *layer, const void *x, const void *w, const void *z, const void *dy, void *dx,
                      void *dw, void *db, void *scratch, size_t scratch_bytes, void *hip_stream);

@@ -1,7 +1,8 @@
 // Layer norm and cross-entropy over the rows of a population of networks.
 //
 // All four kernels are bound by memory: they read every row once, keep it in
-// registers, and write their results once.  A row lies over L lanes (a power
+// registers (but the norm's gradient of the longest rows, which reads them twice), and
+// write their results once.  A row lies over L lanes (a power
 // of two, 1 .. 64, or a block of 256 .. 1024 threads), each with NIT chunks of
 // 16 bytes; row sums are butterflies over the L lanes (and LDS across waves)
 // in fp32.
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_layernorm(NormArgs a, int
 // (floor 37), 77 with four chunks per lane, where there is no room for the row
 // ahead; f16 134,784 rows of 1000 194 us, 239 without it and with gamma loaded per
 // row; 67,392 rows of 2625 285, of one chunk per lane 398.  fp32 rows of 1000 reach
-// 4.5 TB/s; bound by the loads in flight and, above 8192 fp32 columns, by the
+// 4.5 TB/s; bound by the loads in flight and, above 16,384 columns, by the
 // second reading (f16 8192 rows of 32,768 522 us; held, with spills, 710).
 // ---------------------------------------------------------------------------
 template <typename T, int NIT, bool WIDE>

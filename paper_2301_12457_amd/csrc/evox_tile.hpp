@@ -16,12 +16,16 @@
 //
 // 32 bits: an element is the exact sum of three bf16 numbers x = h + m + l (each
 // the rounding of what the ones before leave), staged as three planes; of the
-// nine products of pieces the six down to 2^-18 are summed, the rest are below
-// 2^-25 of the term.  Six bf16 products cost 6/16 of an fp32 one.  Sums cannot
-// overflow and no piece is infinite below 2^56; a block that meets a larger
+// nine products of pieces the six down to 2^-16 are summed, the rest are at most
+// 2^-24 of the term (rms 2^-27).  Six bf16 products cost 6/16 of an fp32 one.  Below
+// 2^56 no piece is infinite and no sum of up to 2^15 terms overflows (a longer one only
+// where its magnitudes' sum does); a block that meets a larger
 // number or an infinity computes its tile again with fp32 products
 // (v_mfma_f32_32x32x2f32).  A NaN is one in its own row either way.  A number
 // below 2^-100 loses its bits under 2^-126, as fp32 with flushed subnormals does.
+//
+// Gradients of 16 bits: d is two numbers of the type (d_split), K is run through once
+// for each, the small one first; their products are added in the same registers.
 //
 // What it reaches: bf16 16x2048 ragged rows 4096x4096 with GELU and residual 1.15 -
 // 1.25 ms, 880 - 960 TFLOP/s (a large library product 1440; the matrix cores are
