@@ -329,9 +329,10 @@ def _raw_stream(stream, like):
     """The HIP stream of a call, the given one or the current one: of like's device, which
     has to be the current one too (the handle of any device's default stream is 0)."""
     d, current = like.get_device(), _DTYPES["device"]()
-    if current != d or stream is not None and stream.device.index != d:
+    own = getattr(stream, "device", None)  # (a bare handle has none)
+    if current != d or own is not None and own.index != d:
         raise EvoxError(EINVAL, f"tensors on device {d}: the current device is {current}"
-                                + ("" if stream is None else f", the stream's {stream.device.index}"))
+                                + ("" if own is None else f", the stream's {own.index}"))
     return _DTYPES["stream"](d) if stream is None else stream.cuda_stream
 
 

@@ -133,3 +133,12 @@ def test_refusals_and_their_reasons(evox, monkeypatch, name, what, change, words
         getattr(evox, name)(**kw)
     assert e.value.code == evox.EINVAL and not any(n == name for n, _ in evox.calls)
     assert "kernels read the GPU's memory" not in str(e.value)
+
+
+def test_a_stream_that_is_only_a_handle(evox, monkeypatch):
+    """As the other calls of the binding take it."""
+    import types
+    on_host_device(evox, monkeypatch)
+    a = arguments()["evox_linear"]
+    evox.evox_linear(**a, stream=types.SimpleNamespace(cuda_stream=9))
+    assert evox.calls[-1][1][-1] == 9
