@@ -645,6 +645,125 @@ size_t evox_xent_scratch_bytes(const evox_classes *classes);
 int evox_xent(const evox_classes *classes, const void *logits, const int32_t *labels, float *fit, void *dz,
               void *scratch, size_t scratch_bytes, void *hip_stream);
 
+/* ---------------------------------------------------------------------------
+ * Mixtures of networks: every row of data goes to the k of the population's G
+ * networks that a gate chooses for it, is brought into the networks' grouping
+ * (where evox_linear and the others above run, with off), and back.  The rules
+ * above hold here too: element types, alignment, pitches, no memory read on the
+ * host, nothing allocated, the same bits on every run.
+ * ------------------------------------------------------------------------- */
+enum evox_gate_over { EVOX_GATE_CHOSEN = 0, EVOX_GATE_ALL = 1 };
+#define EVOX_GATE_MAX_K 32
+
+typedef struct evox_choice {
+    int32_t dtype;      /* enum evox_dtype, of the logits and their gradient */
+    int32_t over;       /* enum evox_gate_over: what the weights are a softmax over */
+    int64_t T, G, k;    /* rows 0 .. 2^31 - 1, networks 1 .. EVOX_MAX_D, choices 1 .. min(G, EVOX_GATE_MAX_K); T k < 2^31 */
+    int64_t ldz, lddz;  /* row pitches of the logits and of their gradient, >= G */
+} evox_choice;
+
+/* ids[t][0 .. k) = the networks of row t's k largest logits in descending order,
+ * equal ones by the lower index (-0 equals 0), and their weights
+ *     w[t][j] = exp(z_id(j)) / sum of exp(z_c) over the k chosen, or over all c
+ * (ids device int32 [T][k], w device fp32 [T][k], dense).  Logits of -inf are
+ * networks left out: where fewer than k are left the other ids are -1 with weight 0.
+ * NaN counts as above +inf; a row that has either gives NaN weights. */
+int evox_gate(const evox_choice *choice, const void *logits, int32_t *ids, float *w, void *hip_stream);
+
+/* Its gradient, from dw (fp32 [T][k]), with ids and w as evox_gate gave them and S =
+ * sum of w_j dw_j over the row's choices:
+ *     dz_id(j) = w_j (dw_j - S), and for the other columns 0 (EVOX_GATE_CHOSEN) or
+ *     -p_c S with p the softmax over the row (EVOX_GATE_ALL; logits are read for it
+ *     alone and may be null otherwise).
+ * Choices outside 0 .. G - 1 do not count, whatever their w and dw hold. */
+int evox_gate_grad(const evox_choice *choice, const void *logits, const int32_t *ids, const float *w,
+                   const float *dw, void *dz, void *hip_stream);
+
+/* The slots (t, j) of T rows with k choices each, and the rows of G networks that
+ * they become (pitches in elements). */
+typedef struct evox_slots {
+    int32_t dtype;      /* enum evox_dtype, of the rows (evox_route looks at T, k and G alone) */
+    int64_t T, k, G;    /* T k < 2^31, k 1 .. 1024, G 1 .. 2^20 */
+    int64_t M;          /* rows of the networks' side, 0 .. 2^31 - 1: T k for all that may come */
+    int64_t D;          /* row length 1 .. 2^20 */
+    int64_t ldx;        /* row pitch of x (of combine: r, of its gradient: dy), >= D */
+    int64_t ldy;        /* row pitch of y */
+    int64_t lds, ldds;  /* row pitches of xs and of dxs */
+} evox_slots;
+
+/* The slots sorted by network, in their order within one: network g's rows are
+ * off[g] .. off[g + 1) (device int32 [G + 1]; off[0] = 0), slot (t, j) = t k + j
+ * is row pos[t][j] (device int32 [T][k]) and row m is slot src[m] (device int32 [T k],
+ * or null).  Ids outside 0 .. G - 1 are of no network: pos -1; the entries of src from
+ * off[G] on are left as they were.  scratch: device, evox_route_scratch_bytes(slots)
+ * bytes, 256-byte aligned. */
+size_t evox_route_scratch_bytes(const evox_slots *slots);
+int evox_route(const evox_slots *slots, const int32_t *ids, int32_t *off, int32_t *pos, int32_t *src, void *scratch,
+               size_t scratch_bytes, void *hip_stream);
+
+/* Rows to the networks: xs[pos[t][j]] = w[t][j] x[t], or x[t] unchanged with w null
+ * (w device fp32 [T][k], dense).  Slots whose pos is outside 0 .. M - 1 go nowhere, rows
+ * that no slot has are left as they were; no two slots have the same row, as
+ * evox_route gives them.  The gradient: dx is evox_combine of dxs with the same w, dw is
+ * evox_combine_grad's with dy = x and xs = dxs. */
+int evox_dispatch(const evox_slots *slots, const void *x, const int32_t *pos, const float *w, void *xs,
+                  void *hip_stream);
+
+/* And back: y[t] = sum over j of w[t][j] xs[pos[t][j]] + r[t], summed in fp32 in j's
+ * order; w null: weights 1, r null: none.  Slots without a row add nothing, whatever
+ * their w holds. */
+int evox_combine(const evox_slots *slots, const void *xs, const int32_t *pos, const float *w, const void *r, void *y,
+                 void *hip_stream);
+
+/* Its gradient: dxs[pos[t][j]] = w[t][j] dy[t] (rows that no slot has are left as they
+ * were) and dw[t][j] = sum over the row of dy[t] xs[pos[t][j]], 0 for slots
+ * without a row (device fp32 [T][k]); r's is dy itself.  dxs or dw may be null, xs is
+ * read for dw alone.  dxs may be xs (equal pitch) where dw is null. */
+int evox_combine_grad(const evox_slots *slots, const void *xs, const int32_t *pos, const float *w, const void *dy,
+                      void *dxs, float *dw, void *hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * AdamW (Loshchilov and Hutter, 2019) over many tensors at once: the step that a
+ * center or a network takes along its gradient.
+ *     m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2,
+ *     p = p - lr weight_decay p - lr m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps)
+ * computed in fp32, t counted from 1.  A master is p in fp32, which the step then
+ * reads and writes in p's place, p being its rounding; without one a p of 16 bits loses
+ * updates below half of its last bit.
+ *
+ * States of 32 bits are fp32.  Of 8 bits m is e4m3 numbers (OCP: largest 448, least 2^-9)
+ * with one fp32 scale for each 256 elements of a row (a row's last ones may be
+ * fewer), the largest |m| / 448, and of v the root is held so; a root above 0 is at
+ * least the least e4m3 number.  |m| whose group is all below 2^-100 counts as 0.  The step
+ * is made from the new moments before they are rounded.  An infinity or NaN among a
+ * group's moments makes the group's scale NaN: its states are lost, not its parameters.
+ * ------------------------------------------------------------------------- */
+#define EVOX_ADAM_BLOCK 256
+
+/* A tensor as rows [rows][n] (a dense one: one row), pitches in elements. */
+typedef struct evox_parameter {
+    void *p;            /* enum evox_dtype of the call */
+    const void *g;      /* its gradient, of the same type */
+    void *m, *v;        /* fp32, or e4m3 bytes; 0 before the first step */
+    float *m_scale, *v_scale; /* 8 bits: [rows][ceil(n / 256)], dense; 0 before the first step */
+    float *master;      /* or null; all tensors of a call have one, or none */
+    int64_t rows, n;    /* 0 .. 2^31 - 1, 0 .. 2^38 */
+    int64_t ldp, ldg;   /* row pitches of p and g, >= n */
+    int64_t lds;        /* of m, v and the master */
+} evox_parameter;
+
+typedef struct evox_adam {
+    int32_t dtype;      /* enum evox_dtype of p and g */
+    int32_t bits;       /* of the states: 32 or 8 */
+    double lr, beta1, beta2, eps, weight_decay; /* betas 0 .. below 1, eps > 0 (as fp32 too) */
+    const float *lr_dev;/* device fp32, in lr's place; or null */
+} evox_adam;
+
+/* One step of `count` tensors (a host array, read in the call; no p twice).  clock:
+ * device int64 [2], {steps done, 0}: the call moves the count on, so a captured step
+ * goes on counting as it is replayed.  36 tensors per launch. */
+int evox_adamw(const evox_adam *adam, const evox_parameter *tensors, int64_t count, int64_t *clock, void *hip_stream);
+
 const char *evox_strerror(int code);
 const char *evox_last_error(void);
 

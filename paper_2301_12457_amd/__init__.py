@@ -20,6 +20,8 @@ OK, EINVAL, EHIP, ENOSPC, EALIGN = 0, -1, -2, -3, -4
 MAX_D = 32768
 F32, BF16, F16 = range(3)
 ACT_NONE, ACT_RELU, ACT_TANH, ACT_GELU, ACT_SILU = range(5)
+GATE_CHOSEN, GATE_ALL = range(2)
+GATE_MAX_K, ADAM_BLOCK = 32, 256
 KERNEL_ROWS, KERNEL_NARROW, KERNEL_FEW_INPUTS, KERNEL_SHORT, KERNEL_SHARES, KERNEL_TILES = 0, 1, 2, 3, 8, 16
 
 # every symbol include/evox.h declares
@@ -39,6 +41,8 @@ EXPORTS = (
     "evox_layer_kernels", "evox_linear", "evox_linear_grad_scratch_bytes", "evox_linear_grad",
     "evox_layernorm", "evox_layernorm_grad_scratch_bytes", "evox_layernorm_grad",
     "evox_xent_scratch_bytes", "evox_xent",
+    "evox_gate", "evox_gate_grad", "evox_route_scratch_bytes", "evox_route", "evox_dispatch", "evox_combine",
+    "evox_combine_grad", "evox_adamw",
 )
 
 
@@ -94,6 +98,30 @@ class Classes(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("G", "M", "C")] + [
         ("off", ctypes.c_void_p), ("labels_shared", ctypes.c_int32), ("ldz", ctypes.c_int64),
         ("lddz", ctypes.c_int64)]
+
+
+class Choice(ctypes.Structure):
+    """evox_choice: rows of logits of which a gate takes the largest."""
+    _fields_ = [("dtype", ctypes.c_int32), ("over", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("T", "G", "k", "ldz", "lddz")]
+
+
+class Slots(ctypes.Structure):
+    """evox_slots: rows with k choices each, and the networks' rows that they become."""
+    _fields_ = [("dtype", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("T", "k", "G", "M", "D", "ldx", "ldy", "lds", "ldds")]
+
+
+class Parameter(ctypes.Structure):
+    """evox_parameter: a tensor that an optimizer updates, as rows."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("p", "g", "m", "v", "m_scale", "v_scale", "master")] + [
+        (n, ctypes.c_int64) for n in ("rows", "n", "ldp", "ldg", "lds")]
+
+
+class Adam(ctypes.Structure):
+    """evox_adam: an optimizer's constants."""
+    _fields_ = [("dtype", ctypes.c_int32), ("bits", ctypes.c_int32)] + [
+        (n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [("lr_dev", ctypes.c_void_p)]
 
 
 _lib = None
@@ -155,6 +183,14 @@ def lib():
             "evox_layernorm_grad": ([P] * 10 + [sz, P], i32),
             "evox_xent_scratch_bytes": ([P], sz),
             "evox_xent": ([P] * 6 + [sz, P], i32),
+            "evox_gate": ([P] * 5, i32),
+            "evox_gate_grad": ([P] * 7, i32),
+            "evox_route_scratch_bytes": ([P], sz),
+            "evox_route": ([P] * 6 + [sz, P], i32),
+            "evox_dispatch": ([P] * 6, i32),
+            "evox_combine": ([P] * 7, i32),
+            "evox_combine_grad": ([P] * 8, i32),
+            "evox_adamw": ([P, P, i64, P, P], i32),
             "evox_strerror": ([i32], ctypes.c_char_p),
             "evox_last_error": ([], ctypes.c_char_p),
         }
@@ -535,6 +571,257 @@ def evox_xent(logits, labels, fit, dz=None, off=None, scratch=None, stream=None)
     _check(lib().evox_xent(ctypes.byref(p), logits.data_ptr(), labels_at, fit_at, dz_at, scratch.data_ptr(), nbytes,
                            _raw_stream(stream, logits)))
     return fit
+
+
+# ---------------------------------------------------------------------------
+# Mixtures of networks: T rows of data, each with k of G networks.  Tables by slot
+# ([T, k]: ids, w, pos, dw) are dense; rows are [T, D] and [M, D] tensors with dense rows.
+# ---------------------------------------------------------------------------
+def _table(what, t, dtype, shape, like):
+    """Checks a dense table (or None) of this type and shape on like's device.  Its address."""
+    if t is None:
+        return None
+    if t.dtype is not _DTYPES[dtype] or t.shape != shape or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise EvoxError(EINVAL, f"{what}: a dense {dtype} tensor of {tuple(shape)} on {like.device}")
+    return t.data_ptr()
+
+
+def _given(**tensors):
+    """Refuses None for what a call cannot do without."""
+    for what, t in tensors.items():
+        if t is None:
+            raise EvoxError(EINVAL, f"{what} is required")
+
+
+def _choice(logits, ids, over):
+    if logits.dim() != 2 or ids.dim() != 2:
+        raise EvoxError(EINVAL, "logits must be [T, G], ids [T, k]")
+    (T, G), d = logits.shape, _dtype(logits)
+    return Choice(d, over, T, G, ids.shape[1], _dense("logits", logits), 0)
+
+
+def evox_gate(logits, ids, w, over=GATE_CHOSEN, stream=None):
+    """ids (int32 [T, k]) and weights w (float32 [T, k]) of the k largest of every row of
+    logits [T, G], in descending order: a softmax over the chosen, or over all (GATE_ALL)."""
+    _given(logits=logits, ids=ids, w=w)
+    p = _choice(logits, ids, over)
+    shape = (p.T, p.k)
+    rc = lib().evox_gate(ctypes.byref(p), logits.data_ptr(), _table("ids", ids, _INT, shape, logits),
+                         _table("w", w, _FLOAT, shape, logits), _raw_stream(stream, logits))
+    if rc != OK:
+        _check(rc)
+    return ids, w
+
+
+def evox_gate_grad(logits, ids, w, dw, dz, over=GATE_CHOSEN, stream=None):
+    """The gradient dz [T, G] of evox_gate's logits from dw (float32 [T, k]), with the
+    ids and w that it gave."""
+    _given(logits=logits, ids=ids, w=w, dw=dw, dz=dz)
+    p = _choice(logits, ids, over)
+    dz_at = _view("dz", dz, logits, logits.shape)
+    p.lddz = _pitch(dz)
+    shape = (p.T, p.k)
+    rc = lib().evox_gate_grad(ctypes.byref(p), logits.data_ptr(), _table("ids", ids, _INT, shape, logits),
+                              _table("w", w, _FLOAT, shape, logits), _table("dw", dw, _FLOAT, shape, logits), dz_at,
+                              _raw_stream(stream, logits))
+    if rc != OK:
+        _check(rc)
+    return dz
+
+
+def _route(ids, off):
+    if ids.dim() != 2 or off.dim() != 1 or off.shape[0] < 2:
+        raise EvoxError(EINVAL, "ids must be [T, k], off [G + 1]")
+    if not _DTYPES:
+        _look_at_torch()
+    if ids.get_device() < 0:
+        raise EvoxError(EINVAL, f"a tensor on {ids.device}: the kernels read the GPU's memory")
+    T, k = ids.shape
+    return Slots(F32, T, k, off.shape[0] - 1)
+
+
+def evox_route_scratch(ids, off):
+    """Scratch for evox_route calls of these shapes."""
+    p = _route(ids, off)
+    return _scratch(lib().evox_route_scratch_bytes(ctypes.byref(p)), ids, None, None)[0]
+
+
+def evox_route(ids, off, pos, src=None, scratch=None, stream=None):
+    """The slots (row, choice) of ids (int32 [T, k]) sorted by network: network g has the
+    rows off[g] .. off[g + 1) (int32 [G + 1]); pos (int32 [T, k]) receives every slot's
+    row, -1 for ids outside 0 .. G - 1, src (int32 [T k]) every row's slot t k + j."""
+    _given(ids=ids, off=off, pos=pos)
+    p = _route(ids, off)
+    shape = tuple(ids.shape)
+    ids_at, off_at = _table("ids", ids, _INT, shape, ids), _vector("off", off, _INT, p.G + 1, ids)
+    pos_at, src_at = _table("pos", pos, _INT, shape, ids), _vector("src", src, _INT, p.T * p.k, ids)
+    scratch, nbytes = _scratch(lib().evox_route_scratch_bytes(ctypes.byref(p)), ids, scratch, stream)
+    rc = lib().evox_route(ctypes.byref(p), ids_at, off_at, pos_at, src_at, scratch.data_ptr(), nbytes,
+                          _raw_stream(stream, ids))
+    if rc != OK:
+        _check(rc)
+    return off, pos, src
+
+
+def _slots(rows, xs, pos, w):
+    """Slots of pos [T, k] between rows [T, D] and xs [M, D] (or None), pos' and w's addresses."""
+    if rows.dim() != 2 or pos.dim() != 2 or xs is not None and xs.dim() != 2:
+        raise EvoxError(EINVAL, "rows must be [T, D], xs [M, D], pos [T, k]")
+    (T, D), d, shape = rows.shape, _dtype(rows), (rows.shape[0], pos.shape[1])
+    if xs is not None:
+        _view("xs", xs, rows, (xs.shape[0], D))
+    return (Slots(d, T, pos.shape[1], 0, 0 if xs is None else xs.shape[0], D, 0, 0, 0 if xs is None else _pitch(xs), 0),
+            _table("pos", pos, _INT, shape, rows), _table("w", w, _FLOAT, shape, rows))
+
+
+def evox_dispatch(x, pos, xs, w=None, stream=None):
+    """xs[pos[t, j]] = w[t, j] x[t] (x[t] itself without w) for the rows of x [T, D]: the
+    rows xs [M, D] in the networks' grouping."""
+    _given(x=x, pos=pos, xs=xs)
+    p, pos_at, w_at = _slots(x, xs, pos, w)
+    p.ldx = _dense("x", x)
+    rc = lib().evox_dispatch(ctypes.byref(p), x.data_ptr(), pos_at, w_at, xs.data_ptr(), _raw_stream(stream, x))
+    if rc != OK:
+        _check(rc)
+    return xs
+
+
+def evox_combine(xs, pos, y, w=None, r=None, stream=None):
+    """y[t] = sum_j w[t, j] xs[pos[t, j]] + r[t] for the rows of y [T, D] (w None: 1)."""
+    _given(xs=xs, pos=pos, y=y)
+    p, pos_at, w_at = _slots(y, xs, pos, w)
+    p.ldy = _dense("y", y)
+    r_at = _view("r", r, y, y.shape)
+    if r is not None:
+        p.ldx = _pitch(r)
+    rc = lib().evox_combine(ctypes.byref(p), xs.data_ptr(), pos_at, w_at, r_at, y.data_ptr(), _raw_stream(stream, y))
+    if rc != OK:
+        _check(rc)
+    return y
+
+
+def evox_combine_grad(xs, pos, dy, w=None, dxs=None, dw=None, stream=None):
+    """The gradient of evox_combine from dy [T, D], each where given: dxs[pos[t, j]] =
+    w[t, j] dy[t] [M, D] and dw (float32 [T, k]), for which alone xs is read."""
+    _given(pos=pos, dy=dy)
+    if dw is not None:
+        _given(xs=xs)
+    p, pos_at, w_at = _slots(dy, xs, pos, w)
+    p.ldx = _dense("dy", dy)
+    if dxs is not None:
+        if dxs.dim() != 2:
+            raise EvoxError(EINVAL, "dxs must be [M, D]")
+        _view("dxs", dxs, dy, (dxs.shape[0] if xs is None else p.M, p.D))
+        p.M, p.ldds = dxs.shape[0], _pitch(dxs)
+    rc = lib().evox_combine_grad(ctypes.byref(p), None if xs is None else xs.data_ptr(), pos_at, w_at, dy.data_ptr(),
+                                 None if dxs is None else dxs.data_ptr(), _table("dw", dw, _FLOAT, (p.T, p.k), dy),
+                                 _raw_stream(stream, dy))
+    if rc != OK:
+        _check(rc)
+    return dxs, dw
+
+
+class AdamW:
+    """AdamW over a list of tensors at once (evox_adamw).
+
+    params and grads are tensors of one type on one device, [n], [G, n] or [G, n_out,
+    n_in], each dense or a view of the rows of a wider matrix (of a population's
+    parameters: Networks' views), a gradient of its parameter's shape.  Every step()
+    reads the gradients from these buffers and updates the parameters in place.
+
+    lr is a number (the attribute may change from step to step) or a float32 tensor [1]
+    on the device, which a captured step reads when it is replayed.  bits: of the
+    moments, 32, or 8 (e4m3 numbers and a scale per 256).  master: an fp32 copy of
+    16-bit parameters, which the steps update in their place.
+
+    state holds what a checkpoint saves, each for all tensors one behind the other:
+    "t" (steps done, int64 [1]), "m", "v" (float32, or float8_e4m3fn: of v the root), with
+    8 bits "m_scale" and "v_scale", and "master".
+    """
+
+    def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, master=False):
+        import torch
+        self.params, self.grads = list(params), list(grads)
+        if not self.params or len(self.params) != len(self.grads):
+            raise EvoxError(EINVAL, f"{len(self.params)} parameters and {len(self.grads)} gradients")
+        like = self.params[0]
+        d = _dtype(like)
+        if master and d == F32:
+            raise EvoxError(EINVAL, "fp32 parameters are their own master")
+        if bits not in (8, 32):
+            raise EvoxError(EINVAL, f"bits = {bits}: states of 32 or 8")
+        shapes = [self._rows(i, p, g, like) for i, (p, g) in enumerate(zip(self.params, self.grads))]
+        sizes = [rows * n for rows, n, *_ in shapes]
+        blocks = [rows * -(-n // ADAM_BLOCK) for rows, n, *_ in shapes]
+        device, N = like.device, sum(sizes)
+        zeros = lambda n, dtype=torch.float32: torch.zeros(n, dtype=dtype, device=device)
+        self._clock = zeros(2, torch.int64)
+        self.state = {"t": self._clock[:1]}
+        for name in ("m", "v"):
+            if bits == 32:
+                self.state[name] = zeros(N)
+            else:
+                self.state[name] = zeros(N, torch.uint8).view(torch.float8_e4m3fn)
+                self.state[name + "_scale"] = zeros(sum(blocks))
+        if master:
+            self.state["master"] = torch.cat([p.reshape(-1).float() for p in self.params])
+        width = {"m": bits // 8, "v": bits // 8, "m_scale": 4, "v_scale": 4, "master": 4}
+        at = {name: t.data_ptr() for name, t in self.state.items()}
+        self._tensors = (Parameter * len(shapes))()
+        for i, (rows, n, ldp, ldg) in enumerate(shapes):
+            self._tensors[i] = Parameter(self.params[i].data_ptr(), self.grads[i].data_ptr(), at["m"], at["v"],
+                                         at.get("m_scale"), at.get("v_scale"), at.get("master"), rows, n, ldp, ldg, n)
+            for name, t in self.state.items():
+                if name != "t":
+                    at[name] += width[name] * (blocks[i] if name.endswith("_scale") else sizes[i])
+        self._adam = Adam(d, bits, 0.0, betas[0], betas[1], eps, weight_decay, None)
+        self.lr, self._like, self._seen = lr, like, set()
+        # a step on another stream has to find the states there
+        torch.cuda.current_stream(device).synchronize()
+
+    @staticmethod
+    def _rows(i, p, g, like):
+        """(rows, n, pitch of p, pitch of g) of a parameter and its gradient."""
+        for what, t in ((f"params[{i}]", p), (f"grads[{i}]", g)):
+            if t.dtype != like.dtype or t.get_device() != like.get_device():
+                raise EvoxError(EINVAL, f"{what}: {t.dtype} on {t.device}, needs {like.dtype} on {like.device}")
+            if t.dim() > 1 and t.numel() and not t[0].is_contiguous() or t.dim() == 1 and not t.is_contiguous():
+                raise EvoxError(EINVAL, f"{what}: rows are not dense")
+        if p.shape != g.shape or p.dim() == 0:
+            raise EvoxError(EINVAL, f"params[{i}] has shape {tuple(p.shape)}, its gradient {tuple(g.shape)}")
+        if p.is_contiguous() and g.is_contiguous():
+            return 1, p.numel(), p.numel(), p.numel()
+        rows, n = p.shape[0], p.numel() // p.shape[0]
+        pitch = lambda t: t.stride(0) if rows > 1 else n
+        return rows, n, pitch(p), pitch(g)
+
+    def step(self, stream=None):
+        """One step of all parameters along their gradients."""
+        lr, a = self.lr, self._adam
+        if hasattr(lr, "data_ptr"):
+            a.lr_dev = _vector("lr", lr, _FLOAT, 1, self._like)
+        else:
+            a.lr, a.lr_dev = lr, None
+        raw = _raw_stream(stream, self._like)
+        if stream is not None and raw not in self._seen:
+            # the states' memory is not given to others while this stream works on it
+            self._seen.add(raw)
+            for t in (self._clock, *self.state.values()):
+                t.record_stream(stream)
+        rc = lib().evox_adamw(ctypes.byref(a), self._tensors, len(self._tensors), self._clock.data_ptr(), raw)
+        if rc != OK:
+            _check(rc)
+
+    def load(self, state):
+        """The states (and the count of steps) of a checkpoint, by the names of `state`."""
+        if set(state) != set(self.state):
+            raise EvoxError(EINVAL, f"states {sorted(state)}, needs {sorted(self.state)}")
+        for name, t in state.items():
+            if t.shape != self.state[name].shape or t.dtype != self.state[name].dtype:
+                raise EvoxError(EINVAL, f"{name}: {t.dtype} {tuple(t.shape)}, needs {self.state[name].dtype} "
+                                        f"{tuple(self.state[name].shape)}")
+        for name, t in state.items():
+            self.state[name].copy_(t)
 
 
 def evox_nsga2_sort(F, front, crowd, scratch=None, stream=None):

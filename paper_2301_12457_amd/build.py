@@ -3,8 +3,9 @@
 Every translation unit is compiled by hipcc for gfx950 only, in parallel:
 two per benchmark function (evox_fn.hip and evox_res.hip with -DEVOX_FN=<id>), one
 per element type of the networks' layers (evox_linear_tile.hip with
--DEVOX_NET_TYPE=<id>), the function-independent kernels (evox_common.hip) and the C ABI
-(evox_api.cpp), then linked into one shared library.
+-DEVOX_NET_TYPE=<id>), the mixtures' gate, sort and moves and the optimizer's step
+(evox_gate, evox_route, evox_slots, evox_adamw), the function-independent kernels
+(evox_common.hip) and the C ABI (evox_api.cpp), then linked into one shared library.
 
 Flags: -ffp-contract=off (fused multiply-adds only where fmaf() is written,
 so the elementwise updates are reproducible), and packed-fp32 instructions
@@ -46,6 +47,8 @@ def _units():
     for ty in range(N_NET_TYPES):
         units.append((os.path.join(CSRC, "evox_linear_tile.hip"), f"evox_linear_tile{ty}.o", [f"-DEVOX_NET_TYPE={ty}"]))
     units.append((os.path.join(CSRC, "evox_norm.hip"), "evox_norm.o", []))
+    for name in ("gate", "route", "slots", "adamw"):
+        units.append((os.path.join(CSRC, f"evox_{name}.hip"), f"evox_{name}.o", []))
     units.append((os.path.join(CSRC, "evox_api.cpp"), "evox_api.o", ["-x", "hip"]))
     return units
 

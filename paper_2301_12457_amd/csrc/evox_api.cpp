@@ -4,9 +4,12 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
+#include <cstddef>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <initializer_list>
 #include <limits>
@@ -15,6 +18,7 @@
 #include <vector>
 
 #include "evox_launch.hpp"
+#include "evox_mix.hpp"
 #include "evox_net.hpp"
 
 using namespace evox;
@@ -623,6 +627,60 @@ XentArgs xent_args(const evox_classes *c, const NetRows &rows)
     a.ldz = c->ldz;
     a.lddz = c->lddz;
     return a;
+}
+
+int check_choice(const evox_choice *c, GateArgs *a)
+{
+    if (!c) return fail(EVOX_EINVAL, "choice is null");
+    if (c->dtype != EVOX_F32 && c->dtype != EVOX_BF16 && c->dtype != EVOX_F16)
+        return fail(EVOX_EINVAL, "unknown dtype %d", c->dtype);
+    if (c->over != EVOX_GATE_CHOSEN && c->over != EVOX_GATE_ALL) return fail(EVOX_EINVAL, "unknown over %d", c->over);
+    if (c->G < 1 || c->G > EVOX_MAX_D) return fail(EVOX_EINVAL, "G = %lld out of range [1, %d]", (long long)c->G, EVOX_MAX_D);
+    if (c->k < 1 || c->k > EVOX_GATE_MAX_K || c->k > c->G)
+        return fail(EVOX_EINVAL, "k = %lld: need 1 .. min(G, %d)", (long long)c->k, EVOX_GATE_MAX_K);
+    if (c->T < 0 || c->T > INT32_MAX / c->k) return fail(EVOX_EINVAL, "T = %lld: need T k in [0, 2^31)", (long long)c->T);
+    *a = GateArgs{};
+    a->dtype = c->dtype;
+    a->over = c->over;
+    a->T = c->T;
+    a->G = (int32_t)c->G;
+    a->k = (int32_t)c->k;
+    a->ldz = c->ldz;
+    a->lddz = c->lddz;
+    return EVOX_OK;
+}
+
+int check_route(const evox_slots *p, RouteArgs *a)
+{
+    if (!p) return fail(EVOX_EINVAL, "slots is null");
+    if (p->k < 1 || p->k > kSlotsMaxK) return fail(EVOX_EINVAL, "k = %lld out of range [1, %d]", (long long)p->k, kSlotsMaxK);
+    if (p->T < 0 || p->T > INT32_MAX / p->k) return fail(EVOX_EINVAL, "T = %lld: need T k in [0, 2^31)", (long long)p->T);
+    if (p->G < 1 || p->G > kNetMaxG) return fail(EVOX_EINVAL, "G = %lld out of range [1, 2^20]", (long long)p->G);
+    *a = RouteArgs{};
+    a->n = p->T * p->k;
+    a->G = p->G;
+    return EVOX_OK;
+}
+
+int check_slots(const evox_slots *p, SlotArgs *a)
+{
+    if (!p) return fail(EVOX_EINVAL, "slots is null");
+    if (p->dtype != EVOX_F32 && p->dtype != EVOX_BF16 && p->dtype != EVOX_F16)
+        return fail(EVOX_EINVAL, "unknown dtype %d", p->dtype);
+    if (p->k < 1 || p->k > kSlotsMaxK) return fail(EVOX_EINVAL, "k = %lld out of range [1, %d]", (long long)p->k, kSlotsMaxK);
+    if (p->T < 0 || p->T > INT32_MAX / p->k) return fail(EVOX_EINVAL, "T = %lld: need T k in [0, 2^31)", (long long)p->T);
+    if (p->M < 0 || p->M > INT32_MAX) return fail(EVOX_EINVAL, "M = %lld out of range [0, 2^31)", (long long)p->M);
+    if (p->D < 1 || p->D > kNetMaxWidth) return fail(EVOX_EINVAL, "D = %lld out of range [1, 2^20]", (long long)p->D);
+    *a = SlotArgs{};
+    a->dtype = p->dtype;
+    a->T = p->T;
+    a->M = p->M;
+    a->D = p->D;
+    a->k = (int32_t)p->k;
+    a->ldx = p->ldx;
+    a->ldy = p->ldy;
+    a->lds = p->lds;
+    return EVOX_OK;
 }
 
 int check_scratch(const void *scratch, size_t have, size_t need)
@@ -1823,6 +1881,195 @@ int evox_xent(const evox_classes *c, const void *logits, const int32_t *labels, 
     a.scratch = scratch;
     const hipError_t e = launch_xent(a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail(e, "cross-entropy");
+    return EVOX_OK;
+}
+
+int evox_gate(const evox_choice *c, const void *logits, int32_t *ids, float *w, void *hip_stream)
+{
+    GateArgs a;
+    const int rc = check_choice(c, &a);
+    if (rc != EVOX_OK) return rc;
+    if (c->T == 0) return EVOX_OK;
+    if (!logits || !ids || !w) return fail(EVOX_EINVAL, "logits, ids and w are required");
+    if (!element_aligned(c->dtype, {logits}) || !element_aligned(EVOX_F32, {ids, w}))
+        return fail(EVOX_EALIGN, "an operand is misaligned");
+    if (!pitch_ok(c->ldz, c->G, c->T)) return fail(EVOX_EINVAL, "ldz is below G or too large");
+    a.z = logits;
+    a.ids = ids;
+    a.w = w;
+    const hipError_t e = launch_gate(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "gate");
+    return EVOX_OK;
+}
+
+int evox_gate_grad(const evox_choice *c, const void *logits, const int32_t *ids, const float *w, const float *dw, void *dz,
+                   void *hip_stream)
+{
+    GateArgs a;
+    const int rc = check_choice(c, &a);
+    if (rc != EVOX_OK) return rc;
+    if (c->T == 0) return EVOX_OK;
+    const bool all = c->over == EVOX_GATE_ALL;
+    if ((all && !logits) || !ids || !w || !dw || !dz)
+        return fail(EVOX_EINVAL, "ids, w, dw, dz and (for EVOX_GATE_ALL) logits are required");
+    if (!element_aligned(c->dtype, {logits, dz}) || !element_aligned(EVOX_F32, {ids, w, dw}))
+        return fail(EVOX_EALIGN, "an operand is misaligned");
+    if ((all && !pitch_ok(c->ldz, c->G, c->T)) || !pitch_ok(c->lddz, c->G, c->T))
+        return fail(EVOX_EINVAL, "ldz or lddz is below G or too large");
+    a.z = logits;
+    a.ids_in = ids;
+    a.w_in = w;
+    a.dw = dw;
+    a.dz = dz;
+    const hipError_t e = launch_gate_grad(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "gate gradient");
+    return EVOX_OK;
+}
+
+size_t evox_route_scratch_bytes(const evox_slots *p)
+{
+    RouteArgs a;
+    if (check_route(p, &a) != EVOX_OK) return 0;
+    return round256(route_scratch(a));
+}
+
+int evox_route(const evox_slots *p, const int32_t *ids, int32_t *off, int32_t *pos, int32_t *src, void *scratch,
+               size_t scratch_bytes, void *hip_stream)
+{
+    RouteArgs a;
+    int rc = check_route(p, &a);
+    if (rc != EVOX_OK) return rc;
+    if (!off || (a.n > 0 && (!ids || !pos))) return fail(EVOX_EINVAL, "ids, off and pos are required");
+    if (!element_aligned(EVOX_F32, {ids, off, pos, src})) return fail(EVOX_EALIGN, "an operand is misaligned");
+    rc = check_scratch(scratch, scratch_bytes, round256(route_scratch(a)));
+    if (rc != EVOX_OK) return rc;
+    a.ids = ids;
+    a.off = off;
+    a.pos = pos;
+    a.src = src;
+    a.scratch = scratch;
+    const hipError_t e = launch_route(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "route");
+    return EVOX_OK;
+}
+
+int evox_dispatch(const evox_slots *p, const void *x, const int32_t *pos, const float *w, void *xs, void *hip_stream)
+{
+    SlotArgs a;
+    const int rc = check_slots(p, &a);
+    if (rc != EVOX_OK) return rc;
+    if (p->T == 0 || p->M == 0) return EVOX_OK;
+    if (!x || !pos || !xs) return fail(EVOX_EINVAL, "x, pos and xs are required");
+    if (!element_aligned(p->dtype, {x, xs}) || !element_aligned(EVOX_F32, {pos, w}))
+        return fail(EVOX_EALIGN, "an operand is misaligned");
+    if (!pitch_ok(p->ldx, p->D, p->T) || !pitch_ok(p->lds, p->D, p->M))
+        return fail(EVOX_EINVAL, "a row pitch is below the row length or too large");
+    a.x = x;
+    a.pos = pos;
+    a.w = w;
+    a.out = xs;
+    a.ldo = p->lds;
+    const hipError_t e = launch_dispatch(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "dispatch");
+    return EVOX_OK;
+}
+
+int evox_combine(const evox_slots *p, const void *xs, const int32_t *pos, const float *w, const void *r, void *y,
+                 void *hip_stream)
+{
+    SlotArgs a;
+    const int rc = check_slots(p, &a);
+    if (rc != EVOX_OK) return rc;
+    if (p->T == 0) return EVOX_OK;
+    if ((p->M > 0 && !xs) || !pos || !y) return fail(EVOX_EINVAL, "xs, pos and y are required");
+    if (!element_aligned(p->dtype, {xs, r, y}) || !element_aligned(EVOX_F32, {pos, w}))
+        return fail(EVOX_EALIGN, "an operand is misaligned");
+    if ((r && !pitch_ok(p->ldx, p->D, p->T)) || !pitch_ok(p->ldy, p->D, p->T) || !pitch_ok(p->lds, p->D, p->M))
+        return fail(EVOX_EINVAL, "a row pitch is below the row length or too large");
+    a.xs = xs;
+    a.pos = pos;
+    a.w = w;
+    a.x = r;
+    a.y = y;
+    const hipError_t e = launch_combine(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "combine");
+    return EVOX_OK;
+}
+
+int evox_combine_grad(const evox_slots *p, const void *xs, const int32_t *pos, const float *w, const void *dy, void *dxs,
+                      float *dw, void *hip_stream)
+{
+    SlotArgs a;
+    const int rc = check_slots(p, &a);
+    if (rc != EVOX_OK) return rc;
+    if (p->T == 0 || (!dxs && !dw)) return EVOX_OK;
+    if (!pos || !dy || (dw && p->M > 0 && !xs)) return fail(EVOX_EINVAL, "dy, pos and (for dw) xs are required");
+    if (!element_aligned(p->dtype, {xs, dy, dxs}) || !element_aligned(EVOX_F32, {pos, w, dw}))
+        return fail(EVOX_EALIGN, "an operand is misaligned");
+    if (!pitch_ok(p->ldx, p->D, p->T) || (dw && !pitch_ok(p->lds, p->D, p->M)) || (dxs && !pitch_ok(p->ldds, p->D, p->M)))
+        return fail(EVOX_EINVAL, "a row pitch is below the row length or too large");
+    a.xs = xs;
+    a.pos = pos;
+    a.w = w;
+    a.x = dy;
+    a.out = dxs;
+    a.ldo = p->ldds;
+    a.dw = dw;
+    const hipError_t e = launch_combine_grad(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "combine gradient");
+    return EVOX_OK;
+}
+
+// (a caller's tensors are the kernels' own)
+static_assert(sizeof(evox_parameter) == sizeof(AdamTensor) && offsetof(evox_parameter, v_scale) == offsetof(AdamTensor, v_scale) &&
+                  offsetof(evox_parameter, rows) == offsetof(AdamTensor, rows) && offsetof(evox_parameter, lds) == offsetof(AdamTensor, lds),
+              "evox_parameter");
+
+int evox_adamw(const evox_adam *c, const evox_parameter *t, int64_t count, int64_t *clock, void *hip_stream)
+{
+    if (!c) return fail(EVOX_EINVAL, "adam is null");
+    if (c->dtype != EVOX_F32 && c->dtype != EVOX_BF16 && c->dtype != EVOX_F16)
+        return fail(EVOX_EINVAL, "unknown dtype %d", c->dtype);
+    if (c->bits != 32 && c->bits != 8) return fail(EVOX_EINVAL, "bits = %d: states of 32 or 8", c->bits);
+    if (!(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0))
+        return fail(EVOX_EINVAL, "beta1 and beta2 must be in [0, 1)");
+    if (!((float)c->eps > 0.0f && (float)c->eps < INFINITY)) return fail(EVOX_EINVAL, "eps must be > 0");
+    if (!std::isfinite(c->lr) || !std::isfinite(c->weight_decay)) return fail(EVOX_EINVAL, "lr and weight_decay must be finite");
+    if (count < 0 || (count > 0 && !t)) return fail(EVOX_EINVAL, "tensors are required");
+    if (!clock) return fail(EVOX_EINVAL, "clock is required");
+    if ((uintptr_t)clock & 7u || (uintptr_t)c->lr_dev & 3u) return fail(EVOX_EALIGN, "clock or lr_dev is misaligned");
+    const bool master = count > 0 && t[0].master;
+    for (int64_t i = 0; i < count; ++i) {
+        const evox_parameter &x = t[i];
+        if (x.rows < 0 || x.rows > INT32_MAX || x.n < 0 || x.n > (int64_t)1 << 38)
+            return fail(EVOX_EINVAL, "tensor %lld: rows = %lld, n = %lld out of range", (long long)i, (long long)x.rows, (long long)x.n);
+        if (!x.master != !master) return fail(EVOX_EINVAL, "tensor %lld: a master for all tensors, or for none", (long long)i);
+        if (x.rows == 0 || x.n == 0) continue;
+        if (!x.p || !x.g || !x.m || !x.v || (c->bits == 8 && (!x.m_scale || !x.v_scale)))
+            return fail(EVOX_EINVAL, "tensor %lld: p, g, m, v and (8 bits) their scales are required", (long long)i);
+        if (!element_aligned(c->dtype, {x.p, x.g}) || !element_aligned(EVOX_F32, {x.master, x.m_scale, x.v_scale}) ||
+            (c->bits == 32 && !element_aligned(EVOX_F32, {x.m, x.v})))
+            return fail(EVOX_EALIGN, "tensor %lld is misaligned", (long long)i);
+        const auto pitch = [&](int64_t ld) { return x.rows == 1 || (ld >= x.n && ld <= ((int64_t)1 << 46) / x.rows); };
+        if (!pitch(x.ldp) || !pitch(x.ldg) || !pitch(x.lds))
+            return fail(EVOX_EINVAL, "tensor %lld: a row pitch is below the row length or too large", (long long)i);
+        if (adam_tiles(c->bits, x.rows, x.n) > INT32_MAX)
+            return fail(EVOX_EINVAL, "tensor %lld is too large: %lld x %lld", (long long)i, (long long)x.rows, (long long)x.n);
+    }
+    if (count > 1) {  // a tensor twice would be two blocks' at once
+        const void **at = (const void **)malloc((size_t)count * sizeof(void *));
+        if (!at) return fail(EVOX_ENOSPC, "no host memory for %lld tensors", (long long)count);
+        int64_t n = 0;
+        for (int64_t i = 0; i < count; ++i)
+            if (t[i].rows && t[i].n) at[n++] = t[i].p;
+        std::sort(at, at + n);
+        const bool twice = std::adjacent_find(at, at + n) != at + n;
+        free(at);
+        if (twice) return fail(EVOX_EINVAL, "a tensor is there twice");
+    }
+    const AdamCall call{c->dtype, c->bits, c->lr, c->beta1, c->beta2, c->eps, c->weight_decay, c->lr_dev, clock};
+    const hipError_t e = launch_adamw(call, (const AdamTensor *)t, count, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail(e, "adamw");
     return EVOX_OK;
 }
 

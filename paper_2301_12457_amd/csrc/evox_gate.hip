@@ -1,0 +1,286 @@
+// The gate of a mixture: the k largest logits of every row and their softmax weights,
+// and the logits' gradient from the weights'.
+//
+// A row lies over L lanes of a wave (a power of two, k at least, so that lane j keeps
+// the j-th choice) or, above 64 lanes' worth, over a block; each lane has NIT chunks of
+// 16 bytes.
+#include "evox_mix.hpp"
+
+namespace evox {
+
+namespace {
+
+// Logits as numbers whose order is theirs, ties to the lower column: of 16 bits the
+// order in the upper half and 65535 - column below it, of 32 bits the same in 64.  0:
+// not there (-inf, past the row's end); -0 is 0, NaN above +inf.
+template <typename T>
+struct GateKey {
+    typedef uint32_t type;
+    static __device__ __forceinline__ uint32_t of(T v, int c)
+    {
+        constexpr uint32_t inf = std::is_same<T, bf16_t>::value ? 0x7f80u : 0x7c00u;
+        const uint32_t u = __builtin_bit_cast(uint16_t, v), a = u & 0x7fffu;
+        uint32_t o = u & 0x8000u ? 0x8000u - a : 0x8000u + a;  // -0 and 0 alike
+        o = a > inf ? 0xffffu : o;
+        return u == (0x8000u | inf) ? 0u : o << 16 | (0xffffu - (uint32_t)c);
+    }
+    static __device__ __forceinline__ int column(uint32_t k) { return (int)(0xffffu - (k & 0xffffu)); }
+    static __device__ __forceinline__ float value(uint32_t k)
+    {
+        const uint32_t o = k >> 16;
+        if (o == 0xffffu) return __builtin_nanf("");
+        const uint16_t u = (uint16_t)(o >= 0x8000u ? o - 0x8000u : (0x8000u - o) | 0x8000u);
+        return (float)__builtin_bit_cast(T, u);
+    }
+};
+template <>
+struct GateKey<float> {
+    typedef uint64_t type;
+    static __device__ __forceinline__ uint64_t of(float v, int c)
+    {
+        const uint32_t u = __float_as_uint(v), a = u & 0x7fffffffu;
+        uint32_t o = u & 0x80000000u ? 0x80000000u - a : 0x80000000u + a;
+        o = a > 0x7f800000u ? 0xffffffffu : o;
+        return u == 0xff800000u ? 0u : (uint64_t)o << 32 | (0xffffffffu - (uint32_t)c);
+    }
+    static __device__ __forceinline__ int column(uint64_t k) { return (int)(0xffffffffu - (uint32_t)k); }
+    static __device__ __forceinline__ float value(uint64_t k)
+    {
+        const uint32_t o = (uint32_t)(k >> 32);
+        if (o == 0xffffffffu) return __builtin_nanf("");
+        return __uint_as_float(o >= 0x80000000u ? o - 0x80000000u : (0x80000000u - o) | 0x80000000u);
+    }
+};
+
+// Over the block of a wide row: the waves meet in LDS (two places in turn, so that one
+// barrier is enough).
+template <typename V, typename F>
+__device__ __forceinline__ V block_all(V v, V *lds, F &&f)
+{
+    const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    if (threadIdx.x % 64 == 0) lds[wave] = v;
+    __syncthreads();
+    v = lds[0];
+    for (int w = 1; w < waves; ++w) v = f(v, lds[w]);
+    return v;
+}
+
+// ---------------------------------------------------------------------------
+// The j-th choice is the largest key below the one before it, K: with unsigned wrap,
+// key - K of the keys below K is larger than of all others, and the largest of them is
+// the nearest, so that a round is one subtraction and one maximum per logit and
+// nothing is marked as taken.
+// ---------------------------------------------------------------------------
+template <typename T, int NIT, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L)
+{
+    constexpr int N = NetVec<T>::N;
+    typedef typename GateKey<T>::type Key;
+    __shared__ Key lds_key[WIDE ? 2 : 1][16];
+    __shared__ float lds_sum[16];
+    const int lane = WIDE ? threadIdx.x : threadIdx.x & (L - 1), G = a.G;
+    const int64_t t = WIDE ? net_block() : net_block() * (256 / L) + threadIdx.x / L;
+    if (WIDE && t >= a.T) return;  // the whole block
+    const bool live = t < a.T;
+    const T *z = (const T *)a.z + t * a.ldz;
+    typename NetVec<T>::reg v[NIT];
+#pragma unroll
+    for (int i = 0; i < NIT; ++i) {
+        const int c = lane + i * L;
+        if (live && c * N < G) v[i] = load_chunk(z, c, G, (T)-INFINITY);
+        else
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[i][j] = (T)-INFINITY;
+    }
+    Key key[NIT][N];
+#pragma unroll
+    for (int i = 0; i < NIT; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) key[i][j] = GateKey<T>::of(v[i][j], (lane + i * L) * N + j);
+    Key K = 0, mine = 0, first = 0;
+    for (int r = 0; r < a.k; ++r) {
+        Key d = 0;
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const Key e = key[i][j] - K;
+                d = e > d ? e : d;
+            }
+        d = lanes_max(d, WIDE ? 64 : L);
+        if constexpr (WIDE) d = block_all(d, lds_key[r & 1], [](Key x, Key y) { return x > y ? x : y; });
+        const Key next = K + d;
+        // none left: all are at K or above it (or there was none)
+        K = r == 0 || (K != 0 && next < K) ? next : 0;
+        if (r == 0) first = K;
+        if (lane == r) mine = K;
+    }
+    const float top = GateKey<T>::value(first);
+    const float e = mine ? exp_near(GateKey<T>::value(mine) - top) : 0.0f;
+    float s = lane < a.k ? e : 0.0f;
+    if (a.over == GATE_ALL) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float x = (float)v[i][j] - top;
+                s += sizeof(T) == 2 ? exp_fast(x) : exp_near(x);
+            }
+    }
+    s = lanes_sum(s, WIDE ? 64 : L);
+    if constexpr (WIDE) s = block_all(s, lds_sum, [](float x, float y) { return x + y; });
+    if (live && lane < a.k) {
+        a.ids[t * a.k + lane] = mine ? GateKey<T>::column(mine) : -1;
+        a.w[t * a.k + lane] = mine ? e / s : 0.0f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Its gradient: S = sum of w dw; -p S everywhere (over the chosen: 0), then the chosen
+// columns' own values behind them, w (dw - S): lane j that of choice j (columns given
+// twice get the sum of all their slots, the same in every one's lane).  The block's or
+// wave's first values are in memory by then (the fence between).
+// ---------------------------------------------------------------------------
+template <typename T, int NIT, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate_grad(GateArgs a, int L)
+{
+    constexpr int N = NetVec<T>::N;
+    typedef typename NetVec<T>::reg reg;
+    __shared__ float lds[3][16];
+    const int lane = WIDE ? threadIdx.x : threadIdx.x & (L - 1), G = a.G, k = a.k;
+    const int64_t t = WIDE ? net_block() : net_block() * (256 / L) + threadIdx.x / L;
+    if (WIDE && t >= a.T) return;
+    const bool live = t < a.T;
+    T *dz = (T *)a.dz + t * a.lddz;
+    const bool all = a.over == GATE_ALL;
+    reg v[NIT];
+    if (all) {
+        const T *z = (const T *)a.z + t * a.ldz;
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if (live && (lane + i * L) * N < G) v[i] = load_chunk(z, lane + i * L, G, (T)-INFINITY);
+    }
+    int id = -1;
+    float w = 0.0f, dw = 0.0f;
+    if (live && lane < k) {
+        id = a.ids_in[t * k + lane];
+        if (id < 0 || id >= G) id = -1;
+        else {
+            w = a.w_in[t * k + lane];
+            dw = a.dw[t * k + lane];
+        }
+    }
+    float S = lanes_sum(id >= 0 ? w * dw : 0.0f, WIDE ? 64 : L);
+    const auto add = [](float x, float y) { return x + y; };
+    if constexpr (WIDE) S = block_all(S, lds[0], add);
+    if (all) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if (live && (lane + i * L) * N < G)
+#pragma unroll
+                for (int j = 0; j < N; ++j) top = fmaxf(top, (float)v[i][j]);
+        const auto most = [](float x, float y) { return fmaxf(x, y); };
+        top = __uint_as_float(lanes_all(__float_as_uint(top), WIDE ? 64 : L, [](uint32_t x, uint32_t y) {
+            return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y)));
+        }));
+        if constexpr (WIDE) top = block_all(top, lds[1], most);
+        if (top == -INFINITY) top = 0.0f;  // (nothing there: every probability 0)
+        float total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if (live && (lane + i * L) * N < G)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float x = (float)v[i][j] - top;
+                    total += sizeof(T) == 2 ? exp_fast(x) : exp_near(x);
+                }
+        total = lanes_sum(total, WIDE ? 64 : L);
+        if constexpr (WIDE) total = block_all(total, lds[2], add);
+        const float f = total == 0.0f ? 0.0f : -S / total;
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if (live && (lane + i * L) * N < G) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float x = (float)v[i][j] - top;
+                    v[i][j] = (T)(f * (sizeof(T) == 2 ? exp_fast(x) : exp_near(x)));
+                }
+                store_chunk(dz, lane + i * L, G, v[i]);
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NIT; ++i)
+            if (live && (lane + i * L) * N < G) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[i][j] = (T)0.0f;
+                store_chunk(dz, lane + i * L, G, v[i]);
+            }
+    }
+    // (the choices of a row are lanes of one wave, a wide row's of the first)
+    const float share = w * (dw - S);
+    float own = 0.0f;
+    for (int j = 0; j < k; ++j) {
+        const int other = __shfl(id, j, WIDE ? 64 : L);
+        const float more = __shfl(share, j, WIDE ? 64 : L);
+        if (other == id) own += more;
+    }
+    __threadfence_block();
+    if constexpr (WIDE) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+    if (id >= 0) dz[id] = (T)own;
+}
+
+// Lanes per row: two chunks each up to 16 lanes, four up to a wave, then a block per
+// row; at least k.
+template <typename T, typename F>
+hipError_t gate_launch(const GateArgs &a, F &&f)
+{
+    constexpr int N = NetVec<T>::N;
+    const int chunks = (a.G + N - 1) / N;
+    if (chunks > 256) {
+        int threads = 256;
+        while (threads < 1024 && chunks > 2 * threads) threads *= 2;
+        const dim3 grid = net_grid(a.T), block(threads);
+        if (chunks <= 2 * threads) f(std::integral_constant<int, 2>{}, std::true_type{}, grid, block, threads);
+        else if (chunks <= 4 * threads) f(std::integral_constant<int, 4>{}, std::true_type{}, grid, block, threads);
+        else f(std::integral_constant<int, 8>{}, std::true_type{}, grid, block, threads);
+        return hipGetLastError();
+    }
+    int L = 1;
+    while (L < 64 && chunks > (L < 16 ? 2 : 4) * L) L *= 2;
+    while (L < a.k) L *= 2;
+    const int nit = (chunks + L - 1) / L;
+    const dim3 grid = net_grid((a.T + 256 / L - 1) / (256 / L)), block(256);
+    if (nit <= 1) f(std::integral_constant<int, 1>{}, std::false_type{}, grid, block, L);
+    else if (nit <= 2) f(std::integral_constant<int, 2>{}, std::false_type{}, grid, block, L);
+    else f(std::integral_constant<int, 4>{}, std::false_type{}, grid, block, L);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_gate(const GateArgs &a, hipStream_t s)
+{
+    return net_dispatch(a.dtype, [&](auto type) {
+        typedef typename NetElement<decltype(type)::value>::type T;
+        return gate_launch<T>(a, [&](auto nit, auto wide, dim3 grid, dim3 block, int L) {
+            if constexpr (decltype(wide)::value && sizeof(T) == 2 && decltype(nit)::value == 8) return;  // (four hold any row)
+            else hipLaunchKernelGGL((k_gate<T, decltype(nit)::value, decltype(wide)::value>), grid, block, 0, s, a, L);
+        });
+    });
+}
+
+hipError_t launch_gate_grad(const GateArgs &a, hipStream_t s)
+{
+    return net_dispatch(a.dtype, [&](auto type) {
+        typedef typename NetElement<decltype(type)::value>::type T;
+        return gate_launch<T>(a, [&](auto nit, auto wide, dim3 grid, dim3 block, int L) {
+            if constexpr (decltype(wide)::value && sizeof(T) == 2 && decltype(nit)::value == 8) return;
+            else hipLaunchKernelGGL((k_gate_grad<T, decltype(nit)::value, decltype(wide)::value>), grid, block, 0, s, a, L);
+        });
+    });
+}
+
+}  // namespace evox
