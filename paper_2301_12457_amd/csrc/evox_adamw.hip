@@ -20,26 +20,74 @@ namespace evox {
 
 namespace {
 
-constexpr int kPasses = 2;  // groups per lane
+constexpr int kBatch = 2, kPasses = 8;  // groups per lane whose loads are in flight together, and per tile
+constexpr int kTensors = 36;            // per launch: the arguments hold 4 KB
+constexpr int kBlocks = 2048;           // eight per CU, which go on from tile to tile
 template <int BITS>
 inline constexpr int kWidth = BITS == 8 ? 8 : 4;  // elements per lane
 
+// A group is L lanes' elements of a row.
 struct Groups {
-    int L, per_row;  // lanes per group, groups per row
-    int64_t groups, tiles;
+    int shift;        // L = 2^shift
+    int64_t per_row, groups;
 };
-template <int BITS>
-__host__ __device__ __forceinline__ Groups groups_of(int64_t rows, int64_t n)
+Groups groups_of(int32_t bits, int64_t rows, int64_t n)
 {
-    constexpr int E = kWidth<BITS>, most = BITS == 8 ? kAdamBlock / E : 64;
+    const int E = bits == 8 ? kWidth<8> : kWidth<32>, most = bits == 8 ? 5 : 6;
     Groups g;
-    g.L = 1;
-    while (g.L < most && g.L * E < n) g.L *= 2;
-    g.per_row = (int)((n + g.L * E - 1) / (g.L * E));
+    g.shift = 0;
+    while (g.shift < most && ((int64_t)E << g.shift) < n) ++g.shift;
+    g.per_row = (n + ((int64_t)E << g.shift) - 1) / ((int64_t)E << g.shift);
     g.groups = rows * g.per_row;
-    const int per_tile = kPasses * 256 / g.L;
-    g.tiles = (g.groups + per_tile - 1) / per_tile;
     return g;
+}
+uint32_t tiles_of(const Groups &g) { return (uint32_t)((g.groups + (kPasses * 256 >> g.shift) - 1) / (kPasses * 256 >> g.shift)); }
+
+// A tensor in the kernel's arguments: the caller's, its groups, and a division by the
+// groups of a row (n / d = (t + (n - t) / 2) / 2^(s - 1) with t the upper half of n mul,
+// Granlund and Montgomery, 1994).
+struct Item {
+    void *p;
+    const void *g;
+    void *m, *v;
+    float *m_scale, *v_scale, *master;
+    int64_t n, ldp, ldg, lds;
+    uint32_t groups, per_row, mul;
+    uint16_t shift, lanes;
+};
+struct Step {
+    Item t[kTensors];
+    uint32_t start[kTensors + 1];  // first tile of each
+    int32_t count, last;
+    float beta1, beta2, one_minus1, one_minus2, eps;
+    float lr, decay, log1, log2;   // the betas' logarithms
+    const float *lr_dev;
+    int64_t *clock;                // steps done, and blocks of this one that have read it
+};
+static_assert(sizeof(Step) <= 4096, "kernel arguments");
+
+Item item_of(const AdamTensor &t, const Groups &g)
+{
+    Item x{};
+    x.p = t.p;
+    x.g = t.g;
+    x.m = t.m;
+    x.v = t.v;
+    x.m_scale = t.m_scale;
+    x.v_scale = t.v_scale;
+    x.master = t.master;
+    x.n = t.n;
+    x.ldp = t.ldp;
+    x.ldg = t.ldg;
+    x.lds = t.lds;
+    x.groups = (uint32_t)g.groups;
+    x.per_row = (uint32_t)g.per_row;
+    x.lanes = (uint16_t)g.shift;
+    int s = 0;
+    while (((uint64_t)1 << s) < x.per_row) ++s;
+    x.shift = (uint16_t)(s ? s - 1 : 0);
+    x.mul = (uint32_t)((((((uint64_t)1 << s) - x.per_row) << 32) / x.per_row) + 1);
+    return x;
 }
 
 template <typename T, int E>
@@ -47,59 +95,24 @@ struct Packed {
     typedef T reg __attribute__((ext_vector_type(E)));
     typedef T mem __attribute__((ext_vector_type(E), aligned(sizeof(T))));
 };
-template <typename T, int E>
-__device__ __forceinline__ void read(const T *p, int n, float *v)
+template <int E, typename T>
+__device__ __forceinline__ void put(T *p, int n, typename Packed<T, E>::reg v)
 {
-    if (n >= E) {
-        const typename Packed<T, E>::reg r = *reinterpret_cast<const typename Packed<T, E>::mem *>(p);
+    if (n >= E) *reinterpret_cast<typename Packed<T, E>::mem *>(p) = v;
+    else
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = (float)r[e];
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = e < n ? (float)p[e] : 0.0f;
-}
-template <typename T, int E>
-__device__ __forceinline__ void write(T *p, int n, const float *v)
-{
-    if (n >= E) {
-        typename Packed<T, E>::reg r;
-#pragma unroll
-        for (int e = 0; e < E; ++e) r[e] = (T)v[e];
-        *reinterpret_cast<typename Packed<T, E>::mem *>(p) = r;
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (e < n) p[e] = (T)v[e];
+        for (int e = 0; e < E; ++e)
+            if (e < n) p[e] = v[e];
 }
 
-struct Bytes8 {
-    uint32_t w[2];
-};
-__device__ __forceinline__ Bytes8 read8(const uint8_t *p, int n)
+typedef Packed<uint8_t, 8>::reg Bytes8;
+__device__ __forceinline__ void from8(Bytes8 bytes, float scale, float *v)
 {
-    Bytes8 b{{0, 0}};
-    if (n >= 8) __builtin_memcpy(&b, p, 8);
-    else
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) b.w[e / 4] |= (uint32_t)p[e] << e % 4 * 8;
-    return b;
-}
-__device__ __forceinline__ void write8(uint8_t *p, int n, Bytes8 b)
-{
-    if (n >= 8) __builtin_memcpy(p, &b, 8);
-    else
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = (uint8_t)(b.w[e / 4] >> e % 4 * 8);
-}
-__device__ __forceinline__ void from8(Bytes8 b, float scale, float *v)
-{
+    const uint2 b = __builtin_bit_cast(uint2, bytes);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)b.w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)b.w[i], true);
+        const int w = (int)(i ? b.y : b.x);
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
         v[4 * i] = lo[0] * scale;
         v[4 * i + 1] = lo[1] * scale;
         v[4 * i + 2] = hi[0] * scale;
@@ -124,7 +137,7 @@ __device__ __forceinline__ float scale8(const float *v, int L, float *ratio)
 template <bool ROOT>
 __device__ __forceinline__ Bytes8 to8(const float *v, float ratio)
 {
-    Bytes8 b;
+    uint32_t b[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         float q[4];
@@ -133,112 +146,158 @@ __device__ __forceinline__ Bytes8 to8(const float *v, float ratio)
             q[e] = ratio > 0.0f ? v[4 * i + e] * ratio : 0.0f;
             if (ROOT && v[4 * i + e] > 0.0f) q[e] = fmaxf(q[e], 0x1p-9f);
         }
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-        b.w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+        b[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
     }
-    return b;
-}
-
-// b^t
-__device__ __forceinline__ double power(double b, int64_t t)
-{
-    double r = 1.0;
-    for (; t > 0; t >>= 1, b *= b)
-        if (t & 1) r *= b;
-    return r;
+    return __builtin_bit_cast(Bytes8, make_uint2(b[0], b[1]));
 }
 
 template <typename T, int BITS, bool MASTER>
-__global__ __launch_bounds__(256) void k_adamw(AdamArgs a)
+__global__ __launch_bounds__(256) void k_adamw(const Step a)
 {
     constexpr int E = kWidth<BITS>;
-    int lo = 0, hi = a.count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.start[mid] <= blockIdx.x) lo = mid;
-        else hi = mid;
-    }
-    const AdamTensor &x = a.t[lo];
-    const Groups gr = groups_of<BITS>(x.rows, x.n);
-    const int L = gr.L, lane = threadIdx.x & (L - 1);
-    const int64_t tile = blockIdx.x - a.start[lo];
-
-    const int64_t t = max(a.clock[0] + 1, (int64_t)1);
-    const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
-    const float rate = (float)(lr / (1.0 - power(a.b1, t))), root = (float)(1.0 / sqrt(1.0 - power(a.b2, t))),
-                shrink = (float)(lr * a.decay);
-
-    for (int u = 0; u < kPasses; ++u) {
-        const int64_t group = (tile * kPasses + u) * (256 / L) + threadIdx.x / L;
-        const bool live = group < gr.groups;
-        const int64_t row = live ? group / gr.per_row : 0, b = live ? group - row * gr.per_row : 0;
-        const int64_t col = (b * L + lane) * E;
-        const int n = live ? (int)min(max(x.n - col, (int64_t)0), (int64_t)E) : 0;
-        float p[E], g[E], m[E], v[E], r[E];
-        read<T, E>((const T *)x.g + row * x.ldg + col, n, g);
-        if constexpr (MASTER) read<float, E>(x.master + row * x.lds + col, n, p);
-        else read<T, E>((const T *)x.p + row * x.ldp + col, n, p);
-        if constexpr (BITS == 8) {
-            const Bytes8 mb = read8((const uint8_t *)x.m + row * x.lds + col, n), vb = read8((const uint8_t *)x.v + row * x.lds + col, n);
-            const int64_t s = row * gr.per_row + b;
-            from8(mb, live ? x.m_scale[s] : 0.0f, m);
-            from8(vb, live ? x.v_scale[s] : 0.0f, v);
-#pragma unroll
-            for (int e = 0; e < E; ++e) v[e] *= v[e];
-        } else {
-            read<float, E>((const float *)x.m + row * x.lds + col, n, m);
-            read<float, E>((const float *)x.v + row * x.lds + col, n, v);
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            m[e] = m[e] * a.beta1 + g[e] * a.one_minus1;
-            v[e] = v[e] * a.beta2 + (g[e] * g[e]) * a.one_minus2;
-            r[e] = sqrtf(v[e]);
-            p[e] = (p[e] - p[e] * shrink) - rate * (m[e] / (r[e] * root + a.eps));
-        }
-        if constexpr (MASTER) write<float, E>(x.master + row * x.lds + col, n, p);
-        write<T, E>((T *)x.p + row * x.ldp + col, n, p);
-        if constexpr (BITS == 8) {
-            float mr, vr;
-            const float ms = scale8(m, L, &mr), vs = scale8(r, L, &vr);
-            write8((uint8_t *)x.m + row * x.lds + col, n, to8<false>(m, mr));
-            write8((uint8_t *)x.v + row * x.lds + col, n, to8<true>(r, vr));
-            if (live && lane == 0) {
-                x.m_scale[row * gr.per_row + b] = ms;
-                x.v_scale[row * gr.per_row + b] = vs;
-            }
-        } else {
-            write<float, E>((float *)x.m + row * x.lds + col, n, m);
-            write<float, E>((float *)x.v + row * x.lds + col, n, v);
-        }
-    }
-    // this block has its count (in every thread's registers behind the barrier)
-    if (!a.last) return;
+    typedef typename std::conditional<MASTER, float, T>::type P;
+    typedef typename std::conditional<BITS == 8, uint8_t, float>::type S;
+    // the step's number; 1 - b^t = -expm1(t log b) (fp32: within 3 roundings of it)
+    const int64_t t = max(__hip_atomic_load(a.clock, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1, (int64_t)1);
+    asm volatile("" ::"v"((uint32_t)t));  // (here it is in a register: the load is done)
+    const float lr = a.lr_dev ? *a.lr_dev : a.lr;
+    const float rate = lr / -expm1f((float)t * a.log1), root = 1.0f / sqrtf(-expm1f((float)t * a.log2)), shrink = lr * a.decay;
+    // every thread has t behind the barrier, and the block counts itself; what that finds is
+    // looked at when the block's work is done (asked for at the end, after 6000 blocks' work
+    // of 87 us, it took 260 more)
     __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        uint32_t *ticket = (uint32_t *)(a.clock + 1);
-        if (atomicAdd(ticket, 1u) == gridDim.x - 1) {
-            *ticket = 0;
-            a.clock[0] = t;
+    uint32_t ticket = 0;
+    if (a.last && threadIdx.x == 0)
+        ticket = __hip_atomic_fetch_add((uint32_t *)(a.clock + 1), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+
+    for (uint32_t tile = blockIdx.x; tile < a.start[a.count]; tile += gridDim.x) {
+        int lo = 0, hi = a.count;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (a.start[mid] <= tile) lo = mid;
+            else hi = mid;
         }
+        const Item &x = a.t[lo];
+        const int shift = x.lanes, lane = threadIdx.x & ((1 << shift) - 1);
+        const uint32_t first = (tile - a.start[lo]) * (kPasses * 256 >> shift) + (threadIdx.x >> shift);
+        for (int u0 = 0; u0 < kPasses; u0 += kBatch) {
+            if (((tile - a.start[lo]) * kPasses + u0) * (256 >> shift) >= x.groups) break;
+            typename Packed<P, E>::reg pv[kBatch];
+            typename Packed<T, E>::reg gv[kBatch];
+            typename Packed<S, E>::reg mv[kBatch], vv[kBatch];
+            float ms[kBatch], vs[kBatch];
+            int64_t row[kBatch], col[kBatch];
+            int n[kBatch];
+            uint32_t group[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                group[u] = first + (u0 + u) * (256 >> shift);
+                uint32_t r = 0;
+                if (x.per_row == 1) r = group[u];
+                else if (x.per_row != x.groups) {
+                    const uint32_t q = __umulhi(group[u], x.mul);
+                    r = (q + ((group[u] - q) >> 1)) >> x.shift;
+                }
+                row[u] = r;
+                col[u] = ((int64_t)(group[u] - r * x.per_row) << shift | lane) * E;
+                n[u] = group[u] < x.groups ? (int)min(max(x.n - col[u], (int64_t)0), (int64_t)E) : 0;
+                if (n[u] < E) continue;
+                gv[u] = *(const typename Packed<T, E>::mem *)((const T *)x.g + row[u] * x.ldg + col[u]);
+                pv[u] = *(const typename Packed<P, E>::mem *)(MASTER ? (const P *)x.master + row[u] * x.lds + col[u]
+                                                                      : (const P *)x.p + row[u] * x.ldp + col[u]);
+                mv[u] = *(const typename Packed<S, E>::mem *)((const S *)x.m + row[u] * x.lds + col[u]);
+                vv[u] = *(const typename Packed<S, E>::mem *)((const S *)x.v + row[u] * x.lds + col[u]);
+            }
+            if constexpr (BITS == 8)
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    ms[u] = group[u] < x.groups ? x.m_scale[group[u]] : 0.0f;
+                    vs[u] = group[u] < x.groups ? x.v_scale[group[u]] : 0.0f;
+                }
+            // rows' ends, element by element
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+                if (n[u] < E)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const bool in = e < n[u];
+                        gv[u][e] = in ? ((const T *)x.g)[row[u] * x.ldg + col[u] + e] : (T)0.0f;
+                        pv[u][e] = in ? (MASTER ? ((const P *)x.master)[row[u] * x.lds + col[u] + e]
+                                                : ((const P *)x.p)[row[u] * x.ldp + col[u] + e])
+                                      : (P)0.0f;
+                        mv[u][e] = in ? ((const S *)x.m)[row[u] * x.lds + col[u] + e] : (S)0;
+                        vv[u][e] = in ? ((const S *)x.v)[row[u] * x.lds + col[u] + e] : (S)0;
+                    }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                float m[E], v[E], r[E];
+                if constexpr (BITS == 8) {
+                    from8(mv[u], ms[u], m);
+                    from8(vv[u], vs[u], v);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[e] *= v[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        m[e] = mv[u][e];
+                        v[e] = vv[u][e];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float g = (float)gv[u][e], p = (float)pv[u][e];
+                    m[e] = m[e] * a.beta1 + g * a.one_minus1;
+                    v[e] = v[e] * a.beta2 + (g * g) * a.one_minus2;
+                    r[e] = __builtin_amdgcn_sqrtf(v[e]);
+                    pv[u][e] = (P)((p - p * shrink) - rate * (m[e] * __builtin_amdgcn_rcpf(r[e] * root + a.eps)));
+                }
+                if constexpr (BITS == 8) {
+                    float mr, vr;
+                    const float new_m = scale8(m, 1 << shift, &mr), new_v = scale8(r, 1 << shift, &vr);
+                    mv[u] = to8<false>(m, mr);
+                    vv[u] = to8<true>(r, vr);
+                    if (group[u] < x.groups && lane == 0) {
+                        x.m_scale[group[u]] = new_m;
+                        x.v_scale[group[u]] = new_v;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        mv[u][e] = m[e];
+                        vv[u][e] = v[e];
+                    }
+                }
+                const int64_t at = row[u] * x.lds + col[u];
+                put<E>((S *)x.m + at, n[u], mv[u]);
+                put<E>((S *)x.v + at, n[u], vv[u]);
+                if constexpr (MASTER) {
+                    put<E>(x.master + at, n[u], pv[u]);
+                    typename Packed<T, E>::reg low;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) low[e] = (T)pv[u][e];
+                    put<E>((T *)x.p + row[u] * x.ldp + col[u], n[u], low);
+                } else put<E>((T *)x.p + row[u] * x.ldp + col[u], n[u], pv[u]);
+            }
+        }
+    }
+    if (a.last && threadIdx.x == 0 && ticket == gridDim.x - 1) {
+        *(uint32_t *)(a.clock + 1) = 0;
+        a.clock[0] = t;
     }
 }
 
 }  // namespace
 
-int64_t adam_tiles(int32_t bits, int64_t rows, int64_t n)
-{
-    return bits == 8 ? groups_of<8>(rows, n).tiles : groups_of<32>(rows, n).tiles;
-}
+int64_t adam_groups(int32_t bits, int64_t rows, int64_t n) { return groups_of(bits, rows, n).groups; }
 
 hipError_t launch_adamw(const AdamCall &c, const AdamTensor *t, int64_t count, hipStream_t s)
 {
-    AdamArgs a{};
-    a.lr = c.lr;
-    a.decay = c.decay;
-    a.b1 = c.beta1;
-    a.b2 = c.beta2;
+    Step a{};
+    a.lr = (float)c.lr;
+    a.decay = (float)c.decay;
+    a.log1 = (float)log(c.beta1);  // (of 0: -inf, and 1 - b^t = 1)
+    a.log2 = (float)log(c.beta2);
     a.beta1 = (float)c.beta1;
     a.beta2 = (float)c.beta2;
     a.one_minus1 = (float)(1.0 - c.beta1);
@@ -246,34 +305,27 @@ hipError_t launch_adamw(const AdamCall &c, const AdamTensor *t, int64_t count, h
     a.eps = (float)c.eps;
     a.lr_dev = c.lr_dev;
     a.clock = c.clock;
+    const bool master = count > 0 && t[0].master;
     int64_t i = 0;
     do {
         a.count = 0;
         uint32_t tiles = 0;
-        // as many tensors as the arguments hold (tensors without elements are left out;
-        // all with a master or none)
-        for (; i < count && a.count < kAdamTensors; ++i) {
-            const int64_t n = t[i].rows && t[i].n ? adam_tiles(c.bits, t[i].rows, t[i].n) : 0;
-            if (n == 0) continue;
-            if (tiles + n > INT32_MAX) break;
+        // as many tensors as the arguments hold (those without elements are left out)
+        for (; i < count && a.count < kTensors; ++i) {
+            if (t[i].rows == 0 || t[i].n == 0) continue;
+            const Groups g = groups_of(c.bits, t[i].rows, t[i].n);
+            const uint32_t n = tiles_of(g);
+            if (n > UINT32_MAX / 2 - tiles) break;
             a.start[a.count] = tiles;
-            a.t[a.count++] = t[i];
-            tiles += (uint32_t)n;
+            a.t[a.count++] = item_of(t[i], g);
+            tiles += n;
         }
         a.start[a.count] = tiles;
         a.last = i == count;
-        if (tiles == 0) {
-            if (!a.last) continue;
-            // nothing to update in the last launch: the count moves on all the same
-            tiles = 1;
-            a.count = 1;
-            a.t[0] = AdamTensor{};
-            a.start[0] = 0;
-        }
-        const bool master = a.t[0].master != nullptr;
+        if (tiles == 0 && !a.last) continue;  // (in the last launch the count moves on all the same)
         const hipError_t e = net_dispatch(c.dtype, [&](auto type) {
             typedef typename NetElement<decltype(type)::value>::type T;
-            const dim3 grid(tiles), block(256);
+            const dim3 grid(tiles == 0 ? 1 : tiles < kBlocks ? tiles : kBlocks), block(256);
             if (c.bits == 8) {
                 if (master) hipLaunchKernelGGL((k_adamw<T, 8, true>), grid, block, 0, s, a);
                 else hipLaunchKernelGGL((k_adamw<T, 8, false>), grid, block, 0, s, a);

@@ -2053,7 +2053,7 @@ int evox_adamw(const evox_adam *c, const evox_parameter *t, int64_t count, int64
         const auto pitch = [&](int64_t ld) { return x.rows == 1 || (ld >= x.n && ld <= ((int64_t)1 << 46) / x.rows); };
         if (!pitch(x.ldp) || !pitch(x.ldg) || !pitch(x.lds))
             return fail(EVOX_EINVAL, "tensor %lld: a row pitch is below the row length or too large", (long long)i);
-        if (adam_tiles(c->bits, x.rows, x.n) > INT32_MAX)
+        if (adam_groups(c->bits, x.rows, x.n) > INT32_MAX)
             return fail(EVOX_EINVAL, "tensor %lld is too large: %lld x %lld", (long long)i, (long long)x.rows, (long long)x.n);
     }
     if (count > 1) {  // a tensor twice would be two blocks' at once

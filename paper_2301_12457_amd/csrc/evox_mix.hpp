@@ -59,16 +59,6 @@ struct AdamTensor {
     float *m_scale, *v_scale, *master;
     int64_t rows, n, ldp, ldg, lds;
 };
-constexpr int kAdamTensors = 36;  // per launch: they travel in the kernel's arguments, which hold 4 KB
-struct AdamArgs {
-    AdamTensor t[kAdamTensors];
-    uint32_t start[kAdamTensors + 1];  // first tile of each
-    int32_t count, last;
-    float one_minus1, one_minus2, beta1, beta2, eps;
-    double lr, decay, b1, b2;
-    const float *lr_dev;
-    int64_t *clock;  // steps done, and blocks of this one that have read it
-};
 struct AdamCall {
     int32_t dtype, bits;
     double lr, beta1, beta2, eps, decay;
@@ -76,7 +66,7 @@ struct AdamCall {
     int64_t *clock;
 };
 constexpr int kAdamBlock = 256;  // elements per scale of an 8-bit state
-int64_t adam_tiles(int32_t bits, int64_t rows, int64_t n);
+int64_t adam_groups(int32_t bits, int64_t rows, int64_t n);  // below 2^31 for each tensor
 hipError_t launch_adamw(const AdamCall &c, const AdamTensor *t, int64_t count, hipStream_t s);
 
 // Lanes of a wave in groups of L (a power of two): the maximum or sum over a group in

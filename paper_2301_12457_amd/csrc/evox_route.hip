@@ -31,11 +31,12 @@ struct Pass {
 
 __device__ __forceinline__ int64_t pass_size(const Pass &p) { return p.have ? *p.have : p.n; }
 
-// The digit of the i-th slot, -1: of no network, or past the end.
+// The network of the i-th slot, -1: none, or past the end (loaded from the last one
+// then: loads behind a branch wait for each other).
 __device__ __forceinline__ int slot_key(const Pass &p, int64_t i, int64_t n)
 {
-    const int key = i < n ? p.key[i] : -1;
-    return key >= 0 && key < p.G ? key : -1;
+    const int key = p.key[i < n ? i : n - 1];
+    return i < n && key >= 0 && key < p.G ? key : -1;
 }
 
 __global__ __launch_bounds__(kThreads) void k_route_count(Pass p)
@@ -45,8 +46,12 @@ __global__ __launch_bounds__(kThreads) void k_route_count(Pass p)
     __syncthreads();
     const int64_t n = pass_size(p), base = (int64_t)blockIdx.x * kTile;
     int key[kRounds];
+    if (base < n)
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) key[r] = slot_key(p, base + r * kThreads + threadIdx.x, n);
+        for (int r = 0; r < kRounds; ++r) key[r] = slot_key(p, base + r * kThreads + threadIdx.x, n);
+    else
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) key[r] = -1;
 #pragma unroll
     for (int r = 0; r < kRounds; ++r)
         if (key[r] >= 0) atomicAdd(&hist[key[r] >> p.shift & (p.bins - 1)], 1);
@@ -86,7 +91,7 @@ __global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
     extern __shared__ int lds[];  // [kWaves][bins], [bins]
     __shared__ int sums[kWaves];
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tile = blockIdx.x, bins = p.bins;
-    int *mine = lds + wave * bins, *base = lds + kWaves * bins;
+    const int mine = wave * bins, base = kWaves * bins;
     for (int b = threadIdx.x; b < kWaves * bins; b += kThreads) lds[b] = 0;
     const int64_t n = pass_size(p);
     const int64_t first = (int64_t)tile * kTile;
@@ -95,8 +100,9 @@ __global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
     const int rounds = left <= 0 ? 0 : left >= kTile ? kRounds : (int)((left + kThreads - 1) / kThreads);
     const int64_t at = first + (int64_t)wave * rounds * 64 + lane;
     int key[kRounds], rank[kRounds];
+    if (rounds)
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) key[r] = r < rounds ? slot_key(p, at + r * 64, n) : -1;
+        for (int r = 0; r < kRounds; ++r) key[r] = slot_key(p, r < rounds ? at + r * 64 : n, n);
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kRounds; ++r)
@@ -109,12 +115,12 @@ __global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
                 peers &= d >> b & 1 ? set : ~set;
             }
             const int before = __popcll(peers & (((uint64_t)1 << lane) - 1));
-            volatile int *c = mine + d;
-            const int so_far = in ? *c : 0;
+            const int so_far = lds[mine + d];
             rank[r] = so_far + before;
-            __builtin_amdgcn_wave_barrier();
-            if (in && before == 0) *c = so_far + __popcll(peers);
-            __builtin_amdgcn_wave_barrier();
+            // (a wave's LDS accesses stay in their order; the compiler is told to keep it)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (in && before == 0) lds[mine + d] = so_far + __popcll(peers);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     __syncthreads();
     // the digits' places: those of lower digits, of earlier tiles, of earlier waves
@@ -140,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
             lds[w * bins + b] = at_wave;
             at_wave += c;
         }
-        base[b] = s;
+        lds[base + b] = s;
         s += all;
     }
     int sum = s;
@@ -152,12 +158,12 @@ __global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
     __syncthreads();
     int lower = sum - s;
     for (int w = 0; w < wave; ++w) lower += sums[w];
-    for (int b = b0; b < b1; ++b) base[b] += lower;
+    for (int b = b0; b < b1; ++b) lds[base + b] += lower;
     if (tile == 0) {
         const int all = sums[0] + sums[1] + sums[2] + sums[3];
         if (p.off) {  // (the digit is the network)
             for (int b = b0; b < b1; ++b)
-                if (b <= p.G) p.off[b] = base[b];
+                if (b <= p.G) p.off[b] = lds[base + b];
             if (threadIdx.x == 0) p.off[p.G] = all;
         }
         if (p.have_out && threadIdx.x == 0) *p.have_out = all;
@@ -173,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
                 continue;
             }
             const int d = key[r] >> p.shift & (bins - 1);
-            const int to = base[d] + mine[d] + rank[r];
+            const int to = lds[base + d] + lds[mine + d] + rank[r];
             if (p.key_out) {
                 p.key_out[to] = key[r];
                 p.slot_out[to] = slot;
