@@ -739,6 +739,7 @@ int evox_combine_grad(const evox_slots *slots, const void *xs, const int32_t *po
  * group's moments makes the group's scale NaN: its states are lost, not its parameters.
  * ------------------------------------------------------------------------- */
 #define EVOX_ADAM_BLOCK 256
+#define EVOX_ADAM_CLOCK 528
 
 /* A tensor as rows [rows][n] (a dense one: one row), pitches in elements. */
 typedef struct evox_parameter {
@@ -760,8 +761,9 @@ typedef struct evox_adam {
 } evox_adam;
 
 /* One step of `count` tensors (a host array, read in the call; no p twice).  clock:
- * device int64 [2], {steps done, 0}: the call moves the count on, so a captured step
- * goes on counting as it is replayed.  36 tensors per launch. */
+ * device int64 [EVOX_ADAM_CLOCK], the number of steps done and the call's own zeros:
+ * the call moves the number on, so a captured step goes on counting as it is replayed.
+ * Calls with the same clock or tensors are one after the other.  36 tensors per launch. */
 int evox_adamw(const evox_adam *adam, const evox_parameter *tensors, int64_t count, int64_t *clock, void *hip_stream);
 
 const char *evox_strerror(int code);

@@ -21,7 +21,7 @@ MAX_D = 32768
 F32, BF16, F16 = range(3)
 ACT_NONE, ACT_RELU, ACT_TANH, ACT_GELU, ACT_SILU = range(5)
 GATE_CHOSEN, GATE_ALL = range(2)
-GATE_MAX_K, ADAM_BLOCK = 32, 256
+GATE_MAX_K, ADAM_BLOCK, ADAM_CLOCK = 32, 256, 528
 KERNEL_ROWS, KERNEL_NARROW, KERNEL_FEW_INPUTS, KERNEL_SHORT, KERNEL_SHARES, KERNEL_TILES = 0, 1, 2, 3, 8, 16
 
 # every symbol include/evox.h declares
@@ -755,7 +755,7 @@ class AdamW:
         blocks = [rows * -(-n // ADAM_BLOCK) for rows, n, *_ in shapes]
         device, N = like.device, sum(sizes)
         zeros = lambda n, dtype=torch.float32: torch.zeros(n, dtype=dtype, device=device)
-        self._clock = zeros(2, torch.int64)
+        self._clock = zeros(ADAM_CLOCK, torch.int64)
         self.state = {"t": self._clock[:1]}
         for name in ("m", "v"):
             if bits == 32:

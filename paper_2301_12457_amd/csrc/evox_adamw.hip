@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kBatch = 2, kPasses = 8;  // groups per lane whose loads are in flight together, and per tile
 constexpr int kTensors = 36;            // per launch: the arguments hold 4 KB
+constexpr uint32_t kPlaces = 32;        // counters of the blocks that have read the clock, 128 bytes apart
 constexpr int kBlocks = 2048;           // eight per CU, which go on from tile to tile
 template <int BITS>
 inline constexpr int kWidth = BITS == 8 ? 8 : 4;  // elements per lane
@@ -95,6 +96,32 @@ struct Packed {
     typedef T reg __attribute__((ext_vector_type(E)));
     typedef T mem __attribute__((ext_vector_type(E), aligned(sizeof(T))));
 };
+// A lane's E elements of a row: loaded from the row's last E where they pass its end (no
+// branch, so that all loads of a batch are on their way together), and then moved to their
+// places with 0 behind them.  TINY: rows of fewer than E, element by element.
+template <bool TINY, int E, typename T>
+__device__ __forceinline__ typename Packed<T, E>::reg get(const T *row, int64_t col, int64_t n)
+{
+    if constexpr (!TINY) return *reinterpret_cast<const typename Packed<T, E>::mem *>(row + min(col, n - E));
+    typename Packed<T, E>::reg v;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = e < n ? row[e] : (T)0;
+    return v;
+}
+template <int E, typename T>
+__device__ __forceinline__ void settle_row(typename Packed<T, E>::reg &v, int64_t col, int64_t n)
+{
+    const int past = (int)min(col + E - n, (int64_t)E);
+    if (past <= 0) return;
+#pragma unroll
+    for (int b = 1; b < E; b *= 2)
+        if (past & b)
+#pragma unroll
+            for (int j = 0; j + b < E; ++j) v[j] = v[j + b];
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        if (j >= E - past) v[j] = (T)0;
+}
 template <int E, typename T>
 __device__ __forceinline__ void put(T *p, int n, typename Packed<T, E>::reg v)
 {
@@ -120,34 +147,37 @@ __device__ __forceinline__ void from8(Bytes8 bytes, float scale, float *v)
     }
 }
 // The group's scale, and its numbers by it.  What is below 2^-100 counts as 0;
-// an infinity or NaN makes the scale NaN, and with it all that the group stands for.
+// an infinity or NaN makes the scale NaN, and with it all that the group stands for (its
+// numbers are then 0).
 __device__ __forceinline__ float scale8(const float *v, int L, float *ratio)
 {
-    uint32_t most = 0;  // as integers: NaN is above all
+    float most = 0.0f;  // NaN if one is
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t u = __float_as_uint(v[e]) & 0x7fffffffu;
-        most = u > most ? u : most;
-    }
-    const float m = __uint_as_float(lanes_max(most, L));
+    for (int e = 0; e < 8; ++e) most = __builtin_elementwise_maximum(most, fabsf(v[e]));
+    // (as integers: NaN is above all)
+    const float m = __uint_as_float(lanes_max(__float_as_uint(most) & 0x7fffffffu, L));
     const bool finite = m < INFINITY;
-    *ratio = finite && m > 0x1p-100f ? 448.0f / m : 0.0f;
+    *ratio = !finite ? -1.0f : m > 0x1p-100f ? 448.0f / m : 0.0f;
     return finite ? m * (1.0f / 448.0f) : __builtin_nanf("");
 }
 template <bool ROOT>
 __device__ __forceinline__ Bytes8 to8(const float *v, float ratio)
 {
+    float q[8], least = 1.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        q[e] = v[e] * ratio;
+        if (ROOT) least = fminf(least, q[e]);
+    }
+    if (ROOT && least < 0x1p-9f)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = v[e] > 0.0f ? fmaxf(q[e], 0x1p-9f) : q[e];
     uint32_t b[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        float q[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            q[e] = ratio > 0.0f ? v[4 * i + e] * ratio : 0.0f;
-            if (ROOT && v[4 * i + e] > 0.0f) q[e] = fmaxf(q[e], 0x1p-9f);
-        }
-        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-        b[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true);
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i], q[4 * i + 1], 0, false);
+        b[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i + 2], q[4 * i + 3], w, true);
+        if (ratio < 0.0f) b[i] = 0;
     }
     return __builtin_bit_cast(Bytes8, make_uint2(b[0], b[1]));
 }
@@ -163,13 +193,21 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
     asm volatile("" ::"v"((uint32_t)t));  // (here it is in a register: the load is done)
     const float lr = a.lr_dev ? *a.lr_dev : a.lr;
     const float rate = lr / -expm1f((float)t * a.log1), root = 1.0f / sqrtf(-expm1f((float)t * a.log2)), shrink = lr * a.decay;
-    // every thread has t behind the barrier, and the block counts itself; what that finds is
-    // looked at when the block's work is done (asked for at the end, after 6000 blocks' work
-    // of 87 us, it took 260 more)
+    // every thread has t behind the barrier, and the block counts itself: in one of 32 places,
+    // whose last block counts the place (one place for 1554 blocks: 44 us of 97)
     __syncthreads();
-    uint32_t ticket = 0;
-    if (a.last && threadIdx.x == 0)
-        ticket = __hip_atomic_fetch_add((uint32_t *)(a.clock + 1), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (a.last && threadIdx.x == 0) {
+        const uint32_t place = blockIdx.x % kPlaces, mates = (gridDim.x - place + kPlaces - 1) / kPlaces;
+        uint32_t *of = (uint32_t *)(a.clock + 16 * (1 + place)), *all = (uint32_t *)(a.clock + 1);
+        const auto count = [](uint32_t *c) { return __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+        if (count(of) == mates - 1) {
+            *of = 0;
+            if (count(all) == min(gridDim.x, kPlaces) - 1) {
+                *all = 0;
+                a.clock[0] = t;
+            }
+        }
+    }
 
     for (uint32_t tile = blockIdx.x; tile < a.start[a.count]; tile += gridDim.x) {
         int lo = 0, hi = a.count;
@@ -181,54 +219,54 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
         const Item &x = a.t[lo];
         const int shift = x.lanes, lane = threadIdx.x & ((1 << shift) - 1);
         const uint32_t first = (tile - a.start[lo]) * (kPasses * 256 >> shift) + (threadIdx.x >> shift);
-        for (int u0 = 0; u0 < kPasses; u0 += kBatch) {
-            if (((tile - a.start[lo]) * kPasses + u0) * (256 >> shift) >= x.groups) break;
+        const auto batch = [&](auto tiny, int u0) {
+            constexpr bool TINY = decltype(tiny)::value;
             typename Packed<P, E>::reg pv[kBatch];
             typename Packed<T, E>::reg gv[kBatch];
             typename Packed<S, E>::reg mv[kBatch], vv[kBatch];
             float ms[kBatch], vs[kBatch];
-            int64_t row[kBatch], col[kBatch];
+            int64_t op[kBatch], os[kBatch], col[kBatch];  // the rows' places in p, and in the states
             int n[kBatch];
             uint32_t group[kBatch];
+            bool inside = true;
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 group[u] = first + (u0 + u) * (256 >> shift);
+                const uint32_t gr = min(group[u], x.groups - 1);
                 uint32_t r = 0;
-                if (x.per_row == 1) r = group[u];
+                if (x.per_row == 1) r = gr;
                 else if (x.per_row != x.groups) {
-                    const uint32_t q = __umulhi(group[u], x.mul);
-                    r = (q + ((group[u] - q) >> 1)) >> x.shift;
+                    const uint32_t q = __umulhi(gr, x.mul);
+                    r = (q + ((gr - q) >> 1)) >> x.shift;
                 }
-                row[u] = r;
-                col[u] = ((int64_t)(group[u] - r * x.per_row) << shift | lane) * E;
+                int64_t og = 0;
+                op[u] = os[u] = 0;
+                if (x.per_row != x.groups) {
+                    op[u] = r * x.ldp;
+                    og = r * x.ldg;
+                    os[u] = r * x.lds;
+                }
+                col[u] = ((int64_t)(gr - r * x.per_row) << shift | lane) * E;
                 n[u] = group[u] < x.groups ? (int)min(max(x.n - col[u], (int64_t)0), (int64_t)E) : 0;
-                if (n[u] < E) continue;
-                gv[u] = *(const typename Packed<T, E>::mem *)((const T *)x.g + row[u] * x.ldg + col[u]);
-                pv[u] = *(const typename Packed<P, E>::mem *)(MASTER ? (const P *)x.master + row[u] * x.lds + col[u]
-                                                                      : (const P *)x.p + row[u] * x.ldp + col[u]);
-                mv[u] = *(const typename Packed<S, E>::mem *)((const S *)x.m + row[u] * x.lds + col[u]);
-                vv[u] = *(const typename Packed<S, E>::mem *)((const S *)x.v + row[u] * x.lds + col[u]);
+                inside &= n[u] >= E;
+                gv[u] = get<TINY, E>((const T *)x.g + og, col[u], x.n);
+                pv[u] = get<TINY, E>(MASTER ? (const P *)x.master + os[u] : (const P *)x.p + op[u], col[u], x.n);
+                mv[u] = get<TINY, E>((const S *)x.m + os[u], col[u], x.n);
+                vv[u] = get<TINY, E>((const S *)x.v + os[u], col[u], x.n);
+                if constexpr (BITS == 8) {
+                    ms[u] = x.m_scale[gr];
+                    vs[u] = x.v_scale[gr];
+                }
             }
-            if constexpr (BITS == 8)
+            inside = __all(inside);
+            if (!TINY && !inside)
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
-                    ms[u] = group[u] < x.groups ? x.m_scale[group[u]] : 0.0f;
-                    vs[u] = group[u] < x.groups ? x.v_scale[group[u]] : 0.0f;
+                    settle_row<E, T>(gv[u], col[u], x.n);
+                    settle_row<E, P>(pv[u], col[u], x.n);
+                    settle_row<E, S>(mv[u], col[u], x.n);
+                    settle_row<E, S>(vv[u], col[u], x.n);
                 }
-            // rows' ends, element by element
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-                if (n[u] < E)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const bool in = e < n[u];
-                        gv[u][e] = in ? ((const T *)x.g)[row[u] * x.ldg + col[u] + e] : (T)0.0f;
-                        pv[u][e] = in ? (MASTER ? ((const P *)x.master)[row[u] * x.lds + col[u] + e]
-                                                : ((const P *)x.p)[row[u] * x.ldp + col[u] + e])
-                                      : (P)0.0f;
-                        mv[u][e] = in ? ((const S *)x.m)[row[u] * x.lds + col[u] + e] : (S)0;
-                        vv[u][e] = in ? ((const S *)x.v)[row[u] * x.lds + col[u] + e] : (S)0;
-                    }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 float m[E], v[E], r[E];
@@ -247,10 +285,10 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const float g = (float)gv[u][e], p = (float)pv[u][e];
-                    m[e] = m[e] * a.beta1 + g * a.one_minus1;
-                    v[e] = v[e] * a.beta2 + (g * g) * a.one_minus2;
+                    m[e] = fmaf(m[e], a.beta1, g * a.one_minus1);
+                    v[e] = fmaf(v[e], a.beta2, (g * g) * a.one_minus2);
                     r[e] = __builtin_amdgcn_sqrtf(v[e]);
-                    pv[u][e] = (P)((p - p * shrink) - rate * (m[e] * __builtin_amdgcn_rcpf(r[e] * root + a.eps)));
+                    pv[u][e] = (P)fmaf(m[e] * __builtin_amdgcn_rcpf(fmaf(r[e], root, a.eps)), -rate, fmaf(p, -shrink, p));
                 }
                 if constexpr (BITS == 8) {
                     float mr, vr;
@@ -268,22 +306,24 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
                         vv[u][e] = v[e];
                     }
                 }
-                const int64_t at = row[u] * x.lds + col[u];
-                put<E>((S *)x.m + at, n[u], mv[u]);
-                put<E>((S *)x.v + at, n[u], vv[u]);
+                const int64_t at = os[u] + col[u];
+                const int left = inside ? E : n[u];
+                put<E>((S *)x.m + at, left, mv[u]);
+                put<E>((S *)x.v + at, left, vv[u]);
                 if constexpr (MASTER) {
-                    put<E>(x.master + at, n[u], pv[u]);
+                    put<E>(x.master + at, left, pv[u]);
                     typename Packed<T, E>::reg low;
 #pragma unroll
                     for (int e = 0; e < E; ++e) low[e] = (T)pv[u][e];
-                    put<E>((T *)x.p + row[u] * x.ldp + col[u], n[u], low);
-                } else put<E>((T *)x.p + row[u] * x.ldp + col[u], n[u], pv[u]);
+                    put<E>((T *)x.p + op[u] + col[u], left, low);
+                } else put<E>((T *)x.p + op[u] + col[u], left, pv[u]);
             }
+        };
+        for (int u0 = 0; u0 < kPasses; u0 += kBatch) {
+            if (((tile - a.start[lo]) * kPasses + u0) * (256 >> shift) >= x.groups) break;
+            if (x.n >= E) batch(std::false_type{}, u0);
+            else batch(std::true_type{}, u0);
         }
-    }
-    if (a.last && threadIdx.x == 0 && ticket == gridDim.x - 1) {
-        *(uint32_t *)(a.clock + 1) = 0;
-        a.clock[0] = t;
     }
 }
 

@@ -4,16 +4,23 @@
 // A counting sort.  A wave takes 64 slots at a time, in order: the lanes with the same
 // digit are found with a ballot per bit, a slot's rank is the wave's count of its digit
 // so far plus the lanes before it, and no atomic decides an order.  Up to 4096 slots are
-// one block's; more are counted per block, the counts summed over the blocks, and the
-// slots placed.  Up to 2048 networks are one digit, more two digits, the lower first.
+// one block's; more are counted per tile of as many and placed by a second launch, which
+// adds up the tiles' counts itself while they are few, else from a third one between.  Up
+// to 2048 networks are one digit, more two digits, the lower first.
+//
+// Bound by latency: few blocks, and in each a chain of loads, ranks and LDS sums.  So a
+// tile is 16 waves' of four rounds where the digits are few (LDS holds a count per wave and
+// digit) and the slots enough (20,014 slots of 100 networks: %PLACE%),
+// all rounds' ballots come before the first round's counts, and all loads before both.
 #include "evox_mix.hpp"
 
 namespace evox {
 
 namespace {
 
-constexpr int kWaves = 4, kRounds = 16, kThreads = 64 * kWaves, kTile = kThreads * kRounds;
-constexpr int kMaxBins = 2048, kFewTiles = 16;
+constexpr int kTile = 4096, kMaxBins = 2048;
+constexpr int kWideBins = 512, kWideSlots = 1024;  // digits at most, and slots above which, for 16 waves
+constexpr int kSummed = 16384;                     // counts of all tiles that each block adds up itself
 
 struct Pass {
     const int32_t *key;   // of the slots in this pass's order, outside 0 .. G - 1: none
@@ -31,32 +38,41 @@ struct Pass {
 
 __device__ __forceinline__ int64_t pass_size(const Pass &p) { return p.have ? *p.have : p.n; }
 
-// The network of the i-th slot, -1: none, or past the end (loaded from the last one
-// then: loads behind a branch wait for each other).
-__device__ __forceinline__ int slot_key(const Pass &p, int64_t i, int64_t n)
+// The networks of a thread's slots i0, i0 + step, ..: -1 for none and past the end, n.
+// All loads first (those past the end are of the last slot, and nothing is looked at
+// before the last is on its way).
+template <int ROUNDS>
+__device__ __forceinline__ void slot_keys(const Pass &p, int64_t base, int i0, int step, int64_t n, int *key)
 {
-    const int key = p.key[i < n ? i : n - 1];
-    return i < n && key >= 0 && key < p.G ? key : -1;
+    const int last = (int)min(n - base, (int64_t)kTile) - 1;
+    if (last < 0) {
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) key[r] = -1;
+        return;
+    }
+    const int32_t *k = p.key + base;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) key[r] = k[min(i0 + r * step, last)];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) key[r] = i0 + r * step <= last && key[r] >= 0 && key[r] < p.G ? key[r] : -1;
 }
 
-__global__ __launch_bounds__(kThreads) void k_route_count(Pass p)
+template <int W>
+__global__ __launch_bounds__(64 * W) void k_route_count(Pass p)
 {
-    __shared__ int hist[kMaxBins];
-    for (int b = threadIdx.x; b < p.bins; b += kThreads) hist[b] = 0;
-    __syncthreads();
+    constexpr int threads = 64 * W, rounds = kTile / threads;
+    __shared__ int hist[W == 16 ? kWideBins : kMaxBins];
+    for (int b = threadIdx.x; b < p.bins; b += threads) hist[b] = 0;
     const int64_t n = pass_size(p), base = (int64_t)blockIdx.x * kTile;
-    int key[kRounds];
-    if (base < n)
+    int key[rounds];
+    slot_keys<rounds>(p, base, threadIdx.x, threads, n, key);
+    __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) key[r] = slot_key(p, base + r * kThreads + threadIdx.x, n);
-    else
-#pragma unroll
-        for (int r = 0; r < kRounds; ++r) key[r] = -1;
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r)
+    for (int r = 0; r < rounds; ++r)
         if (key[r] >= 0) atomicAdd(&hist[key[r] >> p.shift & (p.bins - 1)], 1);
     __syncthreads();
-    for (int b = threadIdx.x; b < p.bins; b += kThreads) p.count[(int64_t)blockIdx.x * p.bins + b] = hist[b];
+    for (int b = threadIdx.x; b < p.bins; b += threads) p.count[(int64_t)blockIdx.x * p.bins + b] = hist[b];
 }
 
 // count[t][b] = sum of the counts of the tiles before t, total[b] = of all: a block per
@@ -84,70 +100,85 @@ __global__ __launch_bounds__(1024) void k_route_scan(Pass p)
 }
 
 // ONE: this tile is all.  SUMMED: count and total come from the scan; else the tile
-// adds the counts before it itself.
-template <bool ONE, bool SUMMED>
-__global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
+// adds the counts of all and of those before it itself.
+template <int W, bool ONE, bool SUMMED>
+__global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
 {
-    extern __shared__ int lds[];  // [kWaves][bins], [bins]
-    __shared__ int sums[kWaves];
+    constexpr int threads = 64 * W, kRounds = kTile / threads;
+    extern __shared__ int lds[];  // [W][bins] counts of the waves; places, all counts, counts before, [bins] each
+    __shared__ int sums[W];
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tile = blockIdx.x, bins = p.bins;
-    const int mine = wave * bins, base = kWaves * bins;
-    for (int b = threadIdx.x; b < kWaves * bins; b += kThreads) lds[b] = 0;
+    const int mine = wave * bins, base = W * bins, total = base + bins, before_at = total + bins;
     const int64_t n = pass_size(p);
     const int64_t first = (int64_t)tile * kTile;
     // rounds of this tile: the waves' shares follow each other
     const int64_t left = n - first;
-    const int rounds = left <= 0 ? 0 : left >= kTile ? kRounds : (int)((left + kThreads - 1) / kThreads);
-    const int64_t at = first + (int64_t)wave * rounds * 64 + lane;
-    int key[kRounds], rank[kRounds];
-    if (rounds)
+    const int rounds = left <= 0 ? 0 : left >= kTile ? kRounds : (int)((left + threads - 1) / threads);
+    const int at = wave * rounds * 64 + lane;
+    int key[kRounds], slot[kRounds];
+    slot_keys<kRounds>(p, first, at, 64, n, key);
+    if (p.slot && left > 0)
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) key[r] = slot_key(p, r < rounds ? at + r * 64 : n, n);
-    __syncthreads();
+        for (int r = 0; r < kRounds; ++r) slot[r] = p.slot[min(first + at + r * 64, n - 1)];
+    else
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r)
-        if (r < rounds) {
-            const int d = key[r] >> p.shift & (bins - 1);
-            const bool in = key[r] >= 0;
-            uint64_t peers = __ballot(in);
-            for (int b = 0; b < p.bits; ++b) {
-                const uint64_t set = __ballot(d >> b & 1);
-                peers &= d >> b & 1 ? set : ~set;
-            }
-            const int before = __popcll(peers & (((uint64_t)1 << lane) - 1));
-            const int so_far = lds[mine + d];
-            rank[r] = so_far + before;
-            // (a wave's LDS accesses stay in their order; the compiler is told to keep it)
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (in && before == 0) lds[mine + d] = so_far + __popcll(peers);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        }
+        for (int r = 0; r < kRounds; ++r) slot[r] = (int)first + at + r * 64;
+    for (int b = threadIdx.x; b < (W + 3) * bins; b += threads) lds[b] = 0;
     __syncthreads();
-    // the digits' places: those of lower digits, of earlier tiles, of earlier waves
-    const int per = (bins + kThreads - 1) / kThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, bins);
-    int s = 0;
-    for (int b = b0; b < b1; ++b) {
-        int all = 0, before = 0;
-        if constexpr (ONE) {
-            for (int w = 0; w < kWaves; ++w) all += lds[w * bins + b];
-        } else if constexpr (SUMMED) {
-            all = p.total[b];
-            before = p.count[(int64_t)tile * bins + b];
-        } else {
-            for (int t = 0; t < p.tiles; ++t) {
+    if constexpr (!ONE && !SUMMED) {
+        const int wide = min(bins, threads), part = threadIdx.x / wide, parts = threads / wide;
+        for (int b = threadIdx.x % wide; b < bins; b += wide) {
+            int all = 0, before = 0;
+#pragma unroll 4
+            for (int t = part; t < p.tiles; t += parts) {
                 const int c = p.count[(int64_t)t * bins + b];
                 all += c;
                 before += t < tile ? c : 0;
             }
+            atomicAdd(&lds[total + b], all);
+            atomicAdd(&lds[before_at + b], before);
         }
-        int at_wave = before;
-        for (int w = 0; w < kWaves; ++w) {
+    }
+    // the lanes of a slot's digit: how many in all, and before it
+    int many[kRounds], rank[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (r < rounds) {
+            const int d = key[r] >> p.shift & (bins - 1);
+            uint64_t peers = __ballot(key[r] >= 0);
+            for (int b = 0; b < p.bits; ++b) {
+                const uint64_t set = __ballot(d >> b & 1);
+                peers &= d >> b & 1 ? set : ~set;
+            }
+            rank[r] = __popcll(peers & (((uint64_t)1 << lane) - 1));
+            many[r] = __popcll(peers);
+        }
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (r < rounds) {
+            const int d = key[r] >> p.shift & (bins - 1);
+            const int so_far = lds[mine + d];
+            // (a wave's LDS accesses stay in their order; the compiler is told to keep it)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (key[r] >= 0 && rank[r] == 0) lds[mine + d] = so_far + many[r];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            rank[r] += so_far;
+        }
+    __syncthreads();
+    // the digits' places: those of lower digits, of earlier tiles, of earlier waves
+    const int per = (bins + threads - 1) / threads, b0 = min((int)threadIdx.x * per, bins), b1 = min(b0 + per, bins);
+    int s = 0;
+    for (int b = b0; b < b1; ++b) {
+        int at_wave = ONE ? 0 : SUMMED ? p.count[(int64_t)tile * bins + b] : lds[before_at + b], all = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
             const int c = lds[w * bins + b];
             lds[w * bins + b] = at_wave;
             at_wave += c;
+            all += c;
         }
         lds[base + b] = s;
-        s += all;
+        s += ONE ? all : SUMMED ? p.total[b] : lds[total + b];
     }
     int sum = s;
     for (int o = 1; o < 64; o *= 2) {
@@ -156,11 +187,14 @@ __global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
     }
     if (lane == 63) sums[wave] = sum;
     __syncthreads();
-    int lower = sum - s;
-    for (int w = 0; w < wave; ++w) lower += sums[w];
+    int lower = sum - s, all = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        lower += w < wave ? sums[w] : 0;
+        all += sums[w];
+    }
     for (int b = b0; b < b1; ++b) lds[base + b] += lower;
     if (tile == 0) {
-        const int all = sums[0] + sums[1] + sums[2] + sums[3];
         if (p.off) {  // (the digit is the network)
             for (int b = b0; b < b1; ++b)
                 if (b <= p.G) p.off[b] = lds[base + b];
@@ -171,21 +205,19 @@ __global__ __launch_bounds__(kThreads) void k_route_place(Pass p)
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kRounds; ++r)
-        if (r < rounds && at + r * 64 < n) {
-            const int64_t i = at + r * 64;
-            const int slot = p.slot ? p.slot[i] : (int)i;
+        if (r < rounds && first + at + r * 64 < n) {
             if (key[r] < 0) {
-                if (!p.slot) p.pos[slot] = -1;
+                if (!p.slot) p.pos[slot[r]] = -1;
                 continue;
             }
             const int d = key[r] >> p.shift & (bins - 1);
             const int to = lds[base + d] + lds[mine + d] + rank[r];
             if (p.key_out) {
                 p.key_out[to] = key[r];
-                p.slot_out[to] = slot;
+                p.slot_out[to] = slot[r];
             } else {
-                p.pos[slot] = to;
-                if (p.src) p.src[to] = slot;
+                p.pos[slot[r]] = to;
+                if (p.src) p.src[to] = slot[r];
                 if (p.sorted) p.sorted[to] = key[r];
             }
         }
@@ -234,18 +266,27 @@ Scratch layout(const RouteArgs &a)
     return s;
 }
 
-hipError_t run(Pass p, hipStream_t s)
+template <int W>
+void run(const Pass &p, hipStream_t s)
 {
-    const size_t lds = (size_t)(kWaves + 1) * p.bins * 4;
-    if (p.tiles <= 1) hipLaunchKernelGGL((k_route_place<true, false>), dim3(1), dim3(kThreads), lds, s, p);
-    else {
-        hipLaunchKernelGGL(k_route_count, dim3(p.tiles), dim3(kThreads), 0, s, p);
-        if (p.tiles <= kFewTiles) hipLaunchKernelGGL((k_route_place<false, false>), dim3(p.tiles), dim3(kThreads), lds, s, p);
-        else {
-            hipLaunchKernelGGL(k_route_scan, dim3((p.bins + 15) / 16), dim3(1024), 0, s, p);
-            hipLaunchKernelGGL((k_route_place<false, true>), dim3(p.tiles), dim3(kThreads), lds, s, p);
-        }
+    const size_t lds = (size_t)(W + 3) * p.bins * 4;
+    const dim3 grid(p.tiles), block(64 * W);
+    if (p.tiles <= 1) {
+        hipLaunchKernelGGL((k_route_place<W, true, false>), dim3(1), block, lds, s, p);
+        return;
     }
+    hipLaunchKernelGGL(k_route_count<W>, grid, block, 0, s, p);
+    if ((int64_t)p.tiles * p.bins <= kSummed) {
+        hipLaunchKernelGGL((k_route_place<W, false, false>), grid, block, lds, s, p);
+        return;
+    }
+    hipLaunchKernelGGL(k_route_scan, dim3((p.bins + 15) / 16), dim3(1024), 0, s, p);
+    hipLaunchKernelGGL((k_route_place<W, false, true>), grid, block, lds, s, p);
+}
+hipError_t run(const Pass &p, hipStream_t s)
+{
+    if (p.bins <= kWideBins && p.n > kWideSlots) run<16>(p, s);
+    else run<4>(p, s);
     return hipGetLastError();
 }
 
