@@ -20,10 +20,9 @@ namespace evox {
 
 namespace {
 
-constexpr int kBatch = 2, kPasses = 8;  // groups per lane whose loads are in flight together, and per tile
+constexpr int kPasses = 2;              // groups per lane and tile
 constexpr int kTensors = 36;            // per launch: the arguments hold 4 KB
 constexpr uint32_t kPlaces = 32;        // counters of the blocks that have read the clock, 128 bytes apart
-constexpr int kBlocks = 2048;           // eight per CU, which go on from tile to tile
 template <int BITS>
 inline constexpr int kWidth = BITS == 8 ? 8 : 4;  // elements per lane
 
@@ -60,7 +59,7 @@ struct Step {
     Item t[kTensors];
     uint32_t start[kTensors + 1];  // first tile of each
     int32_t count, last;
-    float beta1, beta2, one_minus1, one_minus2, eps;
+    float beta1, beta2, keep, in1, in2, eps;  // keep, in2: roots of beta2 and 1 - beta2
     float lr, decay, log1, log2;   // the betas' logarithms
     const float *lr_dev;
     int64_t *clock;                // steps done, and blocks of this one that have read it
@@ -148,7 +147,7 @@ __device__ __forceinline__ void from8(Bytes8 bytes, float scale, float *v)
 }
 // The group's scale, and its numbers by it.  What is below 2^-100 counts as 0;
 // an infinity or NaN makes the scale NaN, and with it all that the group stands for (its
-// numbers are then 0).
+// numbers are then 0).  L: lanes of the group.
 __device__ __forceinline__ float scale8(const float *v, int L, float *ratio)
 {
     float most = 0.0f;  // NaN if one is
@@ -157,7 +156,7 @@ __device__ __forceinline__ float scale8(const float *v, int L, float *ratio)
     // (as integers: NaN is above all)
     const float m = __uint_as_float(lanes_max(__float_as_uint(most) & 0x7fffffffu, L));
     const bool finite = m < INFINITY;
-    *ratio = !finite ? -1.0f : m > 0x1p-100f ? 448.0f / m : 0.0f;
+    *ratio = !finite ? -1.0f : m > 0x1p-100f ? 448.0f * __builtin_amdgcn_rcpf(m) : 0.0f;
     return finite ? m * (1.0f / 448.0f) : __builtin_nanf("");
 }
 template <bool ROOT>
@@ -182,149 +181,227 @@ __device__ __forceinline__ Bytes8 to8(const float *v, float ratio)
     return __builtin_bit_cast(Bytes8, make_uint2(b[0], b[1]));
 }
 
+// The constants of a step: m = beta1 m + in1 g, r^2 = (keep r)^2 + (in2 g)^2 (8 bits) or
+// beta2 v + (in2 g)^2, p - shrink p - m / (r root + eps) with the rate in root and eps.
+struct Rates {
+    float beta1, beta2, keep, in1, in2, root, eps, shrink;
+};
+
+// A lane's elements through the step, from their registers into them.
+template <typename T, int BITS, bool MASTER>
+struct Lane {
+    static constexpr int E = kWidth<BITS>;
+    typedef typename std::conditional<MASTER, float, T>::type P;      // what is updated: p or its master
+    typedef typename std::conditional<BITS == 8, uint8_t, float>::type S;
+    typename Packed<P, E>::reg p;
+    typename Packed<T, E>::reg g;
+    typename Packed<S, E>::reg m, v;
+    float m_scale, v_scale;
+
+    __device__ __forceinline__ void step(const Rates &a, int L)
+    {
+        float m1[E], v1[E], r[E];
+        if constexpr (BITS == 8) {
+            from8(m, m_scale * a.beta1, m1);
+            from8(v, v_scale * a.keep, r);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v1[e] = r[e] * r[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                m1[e] = m[e] * a.beta1;
+                v1[e] = v[e] * a.beta2;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float x = (float)p[e], d = (float)g[e], s = d * a.in2;
+            m1[e] = fmaf(d, a.in1, m1[e]);
+            v1[e] = fmaf(s, s, v1[e]);
+            r[e] = __builtin_amdgcn_sqrtf(v1[e]);
+            p[e] = (P)fmaf(m1[e], __builtin_amdgcn_rcpf(fmaf(r[e], a.root, a.eps)), fmaf(x, -a.shrink, x));
+        }
+        if constexpr (BITS == 8) {
+            float mr, vr;
+            m_scale = scale8(m1, L, &mr);
+            v_scale = scale8(r, L, &vr);
+            m = to8<false>(m1, mr);
+            v = to8<true>(r, vr);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                m[e] = m1[e];
+                v[e] = v1[e];
+            }
+        }
+    }
+    __device__ __forceinline__ typename Packed<T, E>::reg rounded() const
+    {
+        typename Packed<T, E>::reg low;
+#pragma unroll
+        for (int e = 0; e < E; ++e) low[e] = (T)p[e];
+        return low;
+    }
+};
+
 template <typename T, int BITS, bool MASTER>
 __global__ __launch_bounds__(256) void k_adamw(const Step a)
 {
-    constexpr int E = kWidth<BITS>;
-    typedef typename std::conditional<MASTER, float, T>::type P;
-    typedef typename std::conditional<BITS == 8, uint8_t, float>::type S;
-    // the step's number; 1 - b^t = -expm1(t log b) (fp32: within 3 roundings of it)
-    const int64_t t = max(__hip_atomic_load(a.clock, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1, (int64_t)1);
-    asm volatile("" ::"v"((uint32_t)t));  // (here it is in a register: the load is done)
-    const float lr = a.lr_dev ? *a.lr_dev : a.lr;
-    const float rate = lr / -expm1f((float)t * a.log1), root = 1.0f / sqrtf(-expm1f((float)t * a.log2)), shrink = lr * a.decay;
-    // every thread has t behind the barrier, and the block counts itself: in one of 32 places,
-    // whose last block counts the place (one place for 1554 blocks: 44 us of 97)
-    __syncthreads();
-    if (a.last && threadIdx.x == 0) {
-        const uint32_t place = blockIdx.x % kPlaces, mates = (gridDim.x - place + kPlaces - 1) / kPlaces;
-        uint32_t *of = (uint32_t *)(a.clock + 16 * (1 + place)), *all = (uint32_t *)(a.clock + 1);
-        const auto count = [](uint32_t *c) { return __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-        if (count(of) == mates - 1) {
-            *of = 0;
-            if (count(all) == min(gridDim.x, kPlaces) - 1) {
-                *all = 0;
-                a.clock[0] = t;
+    typedef Lane<T, BITS, MASTER> Mine;
+    typedef typename Mine::P P;
+    typedef typename Mine::S S;
+    constexpr int E = Mine::E;
+    const int64_t done = __hip_atomic_load(a.clock, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // the tensor of this tile: the last that starts at it or before
+    const int lane64 = threadIdx.x % 64;
+    const int lo = __popcll(__ballot(lane64 < a.count && a.start[min(lane64, kTensors)] <= blockIdx.x)) - 1;
+    const bool any = lo >= 0 && blockIdx.x < a.start[a.count];
+    const Item &x = a.t[max(__builtin_amdgcn_readfirstlane(lo), 0)];
+    const uint32_t index = blockIdx.x - a.start[max(__builtin_amdgcn_readfirstlane(lo), 0)];
+
+    // The step's number and what it makes of the constants, asked for after the first loads
+    // are on their way; 1 - b^t = -expm1(t log b) (fp32: within 3 roundings of it).  Once every
+    // thread has it (the barrier) the block counts itself: in one of 32 places, whose last
+    // block counts the place (one place for 1554 blocks: 44 us of 97).
+    const auto rates_of = [&]() {
+        asm volatile("" ::"v"((uint32_t)done));  // (here it is in a register: the load is done)
+        const int64_t t = max(done + 1, (int64_t)1);
+        __syncthreads();
+        if (a.last && threadIdx.x == 0) {
+            const uint32_t place = blockIdx.x % kPlaces, mates = (gridDim.x - place + kPlaces - 1) / kPlaces;
+            uint32_t *of = (uint32_t *)(a.clock + 16 * (1 + place)), *all = (uint32_t *)(a.clock + 1);
+            const auto count = [](uint32_t *c) { return __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+            if (count(of) == mates - 1) {
+                *of = 0;
+                if (count(all) == min(gridDim.x, kPlaces) - 1) {
+                    *all = 0;
+                    a.clock[0] = t;
+                }
             }
         }
+        const float lr = a.lr_dev ? *a.lr_dev : a.lr;
+        // (the quotient's sign is the rate's; a rate of 0, or one whose reciprocal is not a
+        // number of any use, is an infinite divisor)
+        const float rate = lr / expm1f((float)t * a.log1), turn = 1.0f / rate;
+        const bool some = fabsf(rate) > 1e-30f;
+        return Rates{a.beta1, a.beta2, a.keep, a.in1, a.in2, some ? turn / sqrtf(-expm1f((float)t * a.log2)) : 0.0f,
+                     some ? turn * a.eps : INFINITY, lr * a.decay};
+    };
+    if (!any) {
+        rates_of();
+        return;
     }
 
-    for (uint32_t tile = blockIdx.x; tile < a.start[a.count]; tile += gridDim.x) {
-        int lo = 0, hi = a.count;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (a.start[mid] <= tile) lo = mid;
-            else hi = mid;
-        }
-        const Item &x = a.t[lo];
-        const int shift = x.lanes, lane = threadIdx.x & ((1 << shift) - 1);
-        const uint32_t first = (tile - a.start[lo]) * (kPasses * 256 >> shift) + (threadIdx.x >> shift);
-        const auto batch = [&](auto tiny, int u0) {
-            constexpr bool TINY = decltype(tiny)::value;
-            typename Packed<P, E>::reg pv[kBatch];
-            typename Packed<T, E>::reg gv[kBatch];
-            typename Packed<S, E>::reg mv[kBatch], vv[kBatch];
-            float ms[kBatch], vs[kBatch];
-            int64_t op[kBatch], os[kBatch], col[kBatch];  // the rows' places in p, and in the states
-            int n[kBatch];
-            uint32_t group[kBatch];
-            bool inside = true;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                group[u] = first + (u0 + u) * (256 >> shift);
-                const uint32_t gr = min(group[u], x.groups - 1);
-                uint32_t r = 0;
-                if (x.per_row == 1) r = gr;
-                else if (x.per_row != x.groups) {
-                    const uint32_t q = __umulhi(gr, x.mul);
-                    r = (q + ((gr - q) >> 1)) >> x.shift;
-                }
-                int64_t og = 0;
-                op[u] = os[u] = 0;
-                if (x.per_row != x.groups) {
-                    op[u] = r * x.ldp;
-                    og = r * x.ldg;
-                    os[u] = r * x.lds;
-                }
-                col[u] = ((int64_t)(gr - r * x.per_row) << shift | lane) * E;
-                n[u] = group[u] < x.groups ? (int)min(max(x.n - col[u], (int64_t)0), (int64_t)E) : 0;
-                inside &= n[u] >= E;
-                gv[u] = get<TINY, E>((const T *)x.g + og, col[u], x.n);
-                pv[u] = get<TINY, E>(MASTER ? (const P *)x.master + os[u] : (const P *)x.p + op[u], col[u], x.n);
-                mv[u] = get<TINY, E>((const S *)x.m + os[u], col[u], x.n);
-                vv[u] = get<TINY, E>((const S *)x.v + os[u], col[u], x.n);
-                if constexpr (BITS == 8) {
-                    ms[u] = x.m_scale[gr];
-                    vs[u] = x.v_scale[gr];
-                }
+    constexpr int kElements = kPasses * 256 * E;
+    if (x.per_row == x.groups && (int64_t)(index + 1) * kElements <= x.n) {
+        // Within a tensor of one row: no ends to look at, addresses that differ by the lane
+        // alone.  Streamed past the caches (bf16 with 8-bit states, 37.7 million elements: 68 us,
+        // 77 without; stores alone 76, and 76 with next to no arithmetic).
+        const int64_t base = (int64_t)index * kElements;
+        const T *g = (const T *)x.g + base;
+        T *p = (T *)x.p + base;
+        P *q = MASTER ? (P *)x.master + base : (P *)p;
+        S *m = (S *)x.m + base, *v = (S *)x.v + base;
+        float *ms = x.m_scale + base / kAdamBlock, *vs = x.v_scale + base / kAdamBlock;
+        const auto load = [&](Mine &l, int u) {
+            const uint32_t i = (u * 256 + threadIdx.x) * E;
+            l.g = __builtin_nontemporal_load((const typename Packed<T, E>::mem *)(g + i));
+            l.p = __builtin_nontemporal_load((const typename Packed<P, E>::mem *)(q + i));
+            l.m = __builtin_nontemporal_load((const typename Packed<S, E>::mem *)(m + i));
+            l.v = __builtin_nontemporal_load((const typename Packed<S, E>::mem *)(v + i));
+            if constexpr (BITS == 8) {
+                l.m_scale = ms[i / kAdamBlock];
+                l.v_scale = vs[i / kAdamBlock];
             }
-            inside = __all(inside);
-            if (!TINY && !inside)
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    settle_row<E, T>(gv[u], col[u], x.n);
-                    settle_row<E, P>(pv[u], col[u], x.n);
-                    settle_row<E, S>(mv[u], col[u], x.n);
-                    settle_row<E, S>(vv[u], col[u], x.n);
-                }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                float m[E], v[E], r[E];
-                if constexpr (BITS == 8) {
-                    from8(mv[u], ms[u], m);
-                    from8(vv[u], vs[u], v);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) v[e] *= v[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        m[e] = mv[u][e];
-                        v[e] = vv[u][e];
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float g = (float)gv[u][e], p = (float)pv[u][e];
-                    m[e] = fmaf(m[e], a.beta1, g * a.one_minus1);
-                    v[e] = fmaf(v[e], a.beta2, (g * g) * a.one_minus2);
-                    r[e] = __builtin_amdgcn_sqrtf(v[e]);
-                    pv[u][e] = (P)fmaf(m[e] * __builtin_amdgcn_rcpf(fmaf(r[e], root, a.eps)), -rate, fmaf(p, -shrink, p));
-                }
-                if constexpr (BITS == 8) {
-                    float mr, vr;
-                    const float new_m = scale8(m, 1 << shift, &mr), new_v = scale8(r, 1 << shift, &vr);
-                    mv[u] = to8<false>(m, mr);
-                    vv[u] = to8<true>(r, vr);
-                    if (group[u] < x.groups && lane == 0) {
-                        x.m_scale[group[u]] = new_m;
-                        x.v_scale[group[u]] = new_v;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        mv[u][e] = m[e];
-                        vv[u][e] = v[e];
-                    }
-                }
-                const int64_t at = os[u] + col[u];
-                const int left = inside ? E : n[u];
-                put<E>((S *)x.m + at, left, mv[u]);
-                put<E>((S *)x.v + at, left, vv[u]);
-                if constexpr (MASTER) {
-                    put<E>(x.master + at, left, pv[u]);
-                    typename Packed<T, E>::reg low;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) low[e] = (T)pv[u][e];
-                    put<E>((T *)x.p + op[u] + col[u], left, low);
-                } else put<E>((T *)x.p + op[u] + col[u], left, pv[u]);
-            }
+            __builtin_amdgcn_sched_barrier(0);
         };
-        for (int u0 = 0; u0 < kPasses; u0 += kBatch) {
-            if (((tile - a.start[lo]) * kPasses + u0) * (256 >> shift) >= x.groups) break;
-            if (x.n >= E) batch(std::false_type{}, u0);
-            else batch(std::true_type{}, u0);
+        Mine l;
+        load(l, 0);
+        const Rates rates = rates_of();
+#pragma unroll
+        for (int u = 0; u < kPasses; ++u) {
+            if (u > 0) load(l, u);
+            const uint32_t i = (u * 256 + threadIdx.x) * E;
+            l.step(rates, 32);
+            __builtin_nontemporal_store((typename Packed<S, E>::mem)l.m, (typename Packed<S, E>::mem *)(m + i));
+            __builtin_nontemporal_store((typename Packed<S, E>::mem)l.v, (typename Packed<S, E>::mem *)(v + i));
+            __builtin_nontemporal_store((typename Packed<P, E>::mem)l.p, (typename Packed<P, E>::mem *)(q + i));
+            if constexpr (MASTER)
+                __builtin_nontemporal_store((typename Packed<T, E>::mem)l.rounded(), (typename Packed<T, E>::mem *)(p + i));
+            if constexpr (BITS == 8)
+                if (threadIdx.x % 32 == 0) {
+                    ms[i / kAdamBlock] = l.m_scale;
+                    vs[i / kAdamBlock] = l.v_scale;
+                }
         }
+        return;
     }
+
+    const int shift = x.lanes, lane = threadIdx.x & ((1 << shift) - 1);
+    const auto passes = [&](auto tiny) {
+        constexpr bool TINY = decltype(tiny)::value;
+        Mine l;
+        uint32_t group;
+        bool live;
+        int64_t op, os, col;  // the row's place in p and in the states, the lane's in the row
+        const auto load = [&](int u) {
+            group = (index * kPasses + u) * (256 >> shift) + (threadIdx.x >> shift);
+            live = group < x.groups;
+            const uint32_t gr = live ? group : x.groups - 1;
+            uint32_t r = 0;
+            if (x.per_row == 1) r = gr;
+            else if (x.per_row != x.groups) {
+                const uint32_t d = __umulhi(gr, x.mul);
+                r = (d + ((gr - d) >> 1)) >> x.shift;
+            }
+            int64_t og = 0;
+            op = os = 0;
+            if (x.per_row != x.groups) {
+                op = r * x.ldp;
+                og = r * x.ldg;
+                os = r * x.lds;
+            }
+            col = ((int64_t)(gr - r * x.per_row) << shift | lane) * E;
+            l.g = get<TINY, E>((const T *)x.g + og, col, x.n);
+            l.p = get<TINY, E>(MASTER ? (const P *)x.master + os : (const P *)x.p + op, col, x.n);
+            l.m = get<TINY, E>((const S *)x.m + os, col, x.n);
+            l.v = get<TINY, E>((const S *)x.v + os, col, x.n);
+            if constexpr (BITS == 8) {
+                l.m_scale = x.m_scale[gr];
+                l.v_scale = x.v_scale[gr];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        load(0);
+        const Rates rates = rates_of();
+        for (int u = 0;;) {
+            const int n = live ? (int)min(max(x.n - col, (int64_t)0), (int64_t)E) : 0;
+            const bool inside = __all(n >= E);
+            if (!TINY && !inside) {
+                settle_row<E, T>(l.g, col, x.n);
+                settle_row<E, P>(l.p, col, x.n);
+                settle_row<E, S>(l.m, col, x.n);
+                settle_row<E, S>(l.v, col, x.n);
+            }
+            l.step(rates, 1 << shift);
+            const int left = inside ? E : n;
+            put<E>((S *)x.m + os + col, left, l.m);
+            put<E>((S *)x.v + os + col, left, l.v);
+            if constexpr (MASTER) {
+                put<E>(x.master + os + col, left, l.p);
+                put<E>((T *)x.p + op + col, left, l.rounded());
+            } else put<E>((T *)x.p + op + col, left, l.p);
+            if constexpr (BITS == 8)
+                if (live && lane == 0) {
+                    x.m_scale[group] = l.m_scale;
+                    x.v_scale[group] = l.v_scale;
+                }
+            if (++u == kPasses || (index * kPasses + u) * (256 >> shift) >= x.groups) break;
+            load(u);
+        }
+    };
+    if (x.n >= E) passes(std::false_type{});
+    else passes(std::true_type{});
 }
 
 }  // namespace
@@ -340,8 +417,9 @@ hipError_t launch_adamw(const AdamCall &c, const AdamTensor *t, int64_t count, h
     a.log2 = (float)log(c.beta2);
     a.beta1 = (float)c.beta1;
     a.beta2 = (float)c.beta2;
-    a.one_minus1 = (float)(1.0 - c.beta1);
-    a.one_minus2 = (float)(1.0 - c.beta2);
+    a.keep = (float)sqrt(c.beta2);
+    a.in1 = (float)(1.0 - c.beta1);
+    a.in2 = (float)sqrt(1.0 - c.beta2);
     a.eps = (float)c.eps;
     a.lr_dev = c.lr_dev;
     a.clock = c.clock;
@@ -365,7 +443,7 @@ hipError_t launch_adamw(const AdamCall &c, const AdamTensor *t, int64_t count, h
         if (tiles == 0 && !a.last) continue;  // (in the last launch the count moves on all the same)
         const hipError_t e = net_dispatch(c.dtype, [&](auto type) {
             typedef typename NetElement<decltype(type)::value>::type T;
-            const dim3 grid(tiles == 0 ? 1 : tiles < kBlocks ? tiles : kBlocks), block(256);
+            const dim3 grid(tiles == 0 ? 1 : tiles), block(256);
             if (c.bits == 8) {
                 if (master) hipLaunchKernelGGL((k_adamw<T, 8, true>), grid, block, 0, s, a);
                 else hipLaunchKernelGGL((k_adamw<T, 8, false>), grid, block, 0, s, a);
