@@ -11,18 +11,36 @@ namespace evox {
 namespace {
 
 // Logits as numbers whose order is theirs, ties to the lower column: of 16 bits the
-// order in the upper half and 65535 - column below it, of 32 bits the same in 64.  0:
-// not there (-inf, past the row's end); -0 is 0, NaN above +inf.
+// order in the upper half and 65535 - column below it, of 32 bits the same in 64.  -0 is
+// 0, NaN above +inf; kNone and what is below it: not there (-inf).
 template <typename T>
 struct GateKey {
     typedef uint32_t type;
-    static __device__ __forceinline__ uint32_t of(T v, int c)
+    static constexpr uint32_t kInf = std::is_same<T, bf16_t>::value ? 0x7f80u : 0x7c00u;
+    static constexpr uint32_t kNone = (0x8000u - kInf) << 16 | 0xffffu;
+
+    // a chunk's keys: two logits at a time, o = 0x8000 +- |z|'s bits
+    static __device__ __forceinline__ void chunk(typename NetVec<T>::reg v, int column, uint32_t *key)
     {
-        constexpr uint32_t inf = std::is_same<T, bf16_t>::value ? 0x7f80u : 0x7c00u;
-        const uint32_t u = __builtin_bit_cast(uint16_t, v), a = u & 0x7fffu;
-        uint32_t o = u & 0x8000u ? 0x8000u - a : 0x8000u + a;  // -0 and 0 alike
-        o = a > inf ? 0xffffu : o;
-        return u == (0x8000u | inf) ? 0u : o << 16 | (0xffffu - (uint32_t)c);
+        typedef short two __attribute__((ext_vector_type(2)));
+        const uint4 w = __builtin_bit_cast(uint4, v);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const two sign = __builtin_bit_cast(two, u[i]) >> 15;
+            const uint32_t s = __builtin_bit_cast(uint32_t, sign);
+            const two a = __builtin_bit_cast(two, u[i] & 0x7fff7fffu);
+            const two o = __builtin_bit_cast(two, __builtin_bit_cast(uint32_t, a) ^ s) - sign;
+            const uint32_t order = __builtin_bit_cast(uint32_t, o) ^ 0x80008000u, below = 0xffffu - (uint32_t)column - 2 * i;
+            key[2 * i] = (order << 16) + below;
+            key[2 * i + 1] = (order & 0xffff0000u) | (below - 1);
+            most = max(most, max(u[i] & 0x7fffu, u[i] >> 16 & 0x7fffu));
+        }
+        if (most > kInf)  // a NaN
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if ((u[j / 2] >> j % 2 * 16 & 0x7fffu) > kInf) key[j] = 0xffff0000u | (0xffffu - (uint32_t)column - j);
     }
     static __device__ __forceinline__ int column(uint32_t k) { return (int)(0xffffu - (k & 0xffffu)); }
     static __device__ __forceinline__ float value(uint32_t k)
@@ -36,12 +54,16 @@ struct GateKey {
 template <>
 struct GateKey<float> {
     typedef uint64_t type;
-    static __device__ __forceinline__ uint64_t of(float v, int c)
+    static constexpr uint64_t kNone = (uint64_t)0x00800000u << 32 | 0xffffffffu;
+
+    static __device__ __forceinline__ void chunk(NetVec<float>::reg v, int column, uint64_t *key)
     {
-        const uint32_t u = __float_as_uint(v), a = u & 0x7fffffffu;
-        uint32_t o = u & 0x80000000u ? 0x80000000u - a : 0x80000000u + a;
-        o = a > 0x7f800000u ? 0xffffffffu : o;
-        return u == 0xff800000u ? 0u : (uint64_t)o << 32 | (0xffffffffu - (uint32_t)c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t u = __float_as_uint(v[j]), s = (uint32_t)((int32_t)u >> 31), a = u & 0x7fffffffu;
+            const uint32_t o = ((a ^ s) - s) ^ 0x80000000u;
+            key[j] = (uint64_t)(a > 0x7f800000u ? 0xffffffffu : o) << 32 | (0xffffffffu - (uint32_t)column - j);
+        }
     }
     static __device__ __forceinline__ int column(uint64_t k) { return (int)(0xffffffffu - (uint32_t)k); }
     static __device__ __forceinline__ float value(uint64_t k)
@@ -51,6 +73,35 @@ struct GateKey<float> {
         return __uint_as_float(o >= 0x80000000u ? o - 0x80000000u : (0x80000000u - o) | 0x80000000u);
     }
 };
+
+// A row's chunks, -inf past its end; whole: the lanes' chunks are the row's exactly.
+template <typename T, int NIT>
+__device__ __forceinline__ void load_row(const T *z, int lane, int L, int G, bool whole, typename NetVec<T>::reg *v)
+{
+    constexpr int N = NetVec<T>::N;
+    if (whole) {
+#pragma unroll
+        for (int i = 0; i < NIT; ++i) v[i] = *reinterpret_cast<const typename NetVec<T>::mem *>(z + (lane + i * L) * N);
+        return;
+    }
+    if (G >= N) {
+#pragma unroll
+        for (int i = 0; i < NIT; ++i) v[i] = load_early(z, lane + i * L, G);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NIT; ++i) {
+            if ((lane + i * L) * N < G) settle<T>(v[i], lane + i * L, G, (T)-INFINITY);
+            else
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[i][j] = (T)-INFINITY;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < NIT; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[i][j] = (lane + i * L) * N + j < G ? z[j] : (T)-INFINITY;
+}
 
 // Over the block of a wide row: the waves meet in LDS (two places in turn, so that one
 // barrier is enough).
@@ -68,11 +119,11 @@ __device__ __forceinline__ V block_all(V v, V *lds, F &&f)
 // ---------------------------------------------------------------------------
 // The j-th choice is the largest key below the one before it, K: with unsigned wrap,
 // key - K of the keys below K is larger than of all others, and the largest of them is
-// the nearest, so that a round is one subtraction and one maximum per logit and
-// nothing is marked as taken.
+// the nearest, so that a round is one subtraction and half a maximum per logit and
+// nothing is marked as taken (k <= G: there is always a key below).
 // ---------------------------------------------------------------------------
 template <typename T, int NIT, bool WIDE>
-__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L)
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L, bool whole)
 {
     constexpr int N = NetVec<T>::N;
     typedef typename GateKey<T>::type Key;
@@ -81,22 +132,11 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L)
     const int lane = WIDE ? threadIdx.x : threadIdx.x & (L - 1), G = a.G;
     const int64_t t = WIDE ? net_block() : net_block() * (256 / L) + threadIdx.x / L;
     if (WIDE && t >= a.T) return;  // the whole block
-    const bool live = t < a.T;
-    const T *z = (const T *)a.z + t * a.ldz;
     typename NetVec<T>::reg v[NIT];
-#pragma unroll
-    for (int i = 0; i < NIT; ++i) {
-        const int c = lane + i * L;
-        if (live && c * N < G) v[i] = load_chunk(z, c, G, (T)-INFINITY);
-        else
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[i][j] = (T)-INFINITY;
-    }
+    load_row<T, NIT>((const T *)a.z + min(t, a.T - 1) * a.ldz, lane, L, G, whole, v);
     Key key[NIT][N];
 #pragma unroll
-    for (int i = 0; i < NIT; ++i)
-#pragma unroll
-        for (int j = 0; j < N; ++j) key[i][j] = GateKey<T>::of(v[i][j], (lane + i * L) * N + j);
+    for (int i = 0; i < NIT; ++i) GateKey<T>::chunk(v[i], (lane + i * L) * N, key[i]);
     Key K = 0, mine = 0, first = 0;
     for (int r = 0; r < a.k; ++r) {
         Key d = 0;
@@ -109,14 +149,13 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L)
             }
         d = lanes_max(d, WIDE ? 64 : L);
         if constexpr (WIDE) d = block_all(d, lds_key[r & 1], [](Key x, Key y) { return x > y ? x : y; });
-        const Key next = K + d;
-        // none left: all are at K or above it (or there was none)
-        K = r == 0 || (K != 0 && next < K) ? next : 0;
+        K += d;
         if (r == 0) first = K;
         if (lane == r) mine = K;
     }
-    const float top = GateKey<T>::value(first);
-    const float e = mine ? exp_near(GateKey<T>::value(mine) - top) : 0.0f;
+    const bool there = mine > GateKey<T>::kNone;
+    const float top = first > GateKey<T>::kNone ? GateKey<T>::value(first) : 0.0f;
+    const float e = there ? exp_near(GateKey<T>::value(mine) - top) : 0.0f;
     float s = lane < a.k ? e : 0.0f;
     if (a.over == GATE_ALL) {
         s = 0.0f;
@@ -130,9 +169,9 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L)
     }
     s = lanes_sum(s, WIDE ? 64 : L);
     if constexpr (WIDE) s = block_all(s, lds_sum, [](float x, float y) { return x + y; });
-    if (live && lane < a.k) {
-        a.ids[t * a.k + lane] = mine ? GateKey<T>::column(mine) : -1;
-        a.w[t * a.k + lane] = mine ? e / s : 0.0f;
+    if (t < a.T && lane < a.k) {
+        a.ids[t * a.k + lane] = there ? GateKey<T>::column(mine) : -1;
+        a.w[t * a.k + lane] = there ? e / s : 0.0f;
     }
 }
 
@@ -143,7 +182,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L)
 // wave's first values are in memory by then (the fence between).
 // ---------------------------------------------------------------------------
 template <typename T, int NIT, bool WIDE>
-__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate_grad(GateArgs a, int L)
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate_grad(GateArgs a, int L, bool whole)
 {
     constexpr int N = NetVec<T>::N;
     typedef typename NetVec<T>::reg reg;
@@ -155,69 +194,60 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate_grad(GateArgs a, int
     T *dz = (T *)a.dz + t * a.lddz;
     const bool all = a.over == GATE_ALL;
     reg v[NIT];
-    if (all) {
-        const T *z = (const T *)a.z + t * a.ldz;
-#pragma unroll
-        for (int i = 0; i < NIT; ++i)
-            if (live && (lane + i * L) * N < G) v[i] = load_chunk(z, lane + i * L, G, (T)-INFINITY);
-    }
+    if (all) load_row<T, NIT>((const T *)a.z + min(t, a.T - 1) * a.ldz, lane, L, G, whole, v);
     int id = -1;
     float w = 0.0f, dw = 0.0f;
     if (live && lane < k) {
         id = a.ids_in[t * k + lane];
-        if (id < 0 || id >= G) id = -1;
-        else {
-            w = a.w_in[t * k + lane];
-            dw = a.dw[t * k + lane];
+        w = a.w_in[t * k + lane];
+        dw = a.dw[t * k + lane];
+        if (id < 0 || id >= G) {
+            id = -1;
+            w = dw = 0.0f;
         }
     }
-    float S = lanes_sum(id >= 0 ? w * dw : 0.0f, WIDE ? 64 : L);
+    float S = lanes_sum(w * dw, WIDE ? 64 : L);
     const auto add = [](float x, float y) { return x + y; };
     if constexpr (WIDE) S = block_all(S, lds[0], add);
     if (all) {
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NIT; ++i)
-            if (live && (lane + i * L) * N < G)
 #pragma unroll
-                for (int j = 0; j < N; ++j) top = fmaxf(top, (float)v[i][j]);
+            for (int j = 0; j < N; ++j) top = fmaxf(top, (float)v[i][j]);
         const auto most = [](float x, float y) { return fmaxf(x, y); };
         top = __uint_as_float(lanes_all(__float_as_uint(top), WIDE ? 64 : L, [](uint32_t x, uint32_t y) {
             return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y)));
         }));
         if constexpr (WIDE) top = block_all(top, lds[1], most);
         if (top == -INFINITY) top = 0.0f;  // (nothing there: every probability 0)
+        // fp32 exponentials take the logits' registers; of 16 bits up to 32 a lane have their own
+        float e[NIT][N];
         float total = 0.0f;
 #pragma unroll
         for (int i = 0; i < NIT; ++i)
-            if (live && (lane + i * L) * N < G)
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float x = (float)v[i][j] - top;
-                    total += sizeof(T) == 2 ? exp_fast(x) : exp_near(x);
-                }
+            for (int j = 0; j < N; ++j) {
+                const float x = (float)v[i][j] - top;
+                e[i][j] = sizeof(T) == 2 ? exp_fast(x) : exp_near(x);
+                total += e[i][j];
+            }
         total = lanes_sum(total, WIDE ? 64 : L);
         if constexpr (WIDE) total = block_all(total, lds[2], add);
         const float f = total == 0.0f ? 0.0f : -S / total;
 #pragma unroll
         for (int i = 0; i < NIT; ++i)
-            if (live && (lane + i * L) * N < G) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float x = (float)v[i][j] - top;
-                    v[i][j] = (T)(f * (sizeof(T) == 2 ? exp_fast(x) : exp_near(x)));
-                }
-                store_chunk(dz, lane + i * L, G, v[i]);
-            }
+            for (int j = 0; j < N; ++j) v[i][j] = (T)(f * e[i][j]);
     } else {
 #pragma unroll
         for (int i = 0; i < NIT; ++i)
-            if (live && (lane + i * L) * N < G) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[i][j] = (T)0.0f;
-                store_chunk(dz, lane + i * L, G, v[i]);
-            }
+            for (int j = 0; j < N; ++j) v[i][j] = (T)0.0f;
     }
+#pragma unroll
+    for (int i = 0; i < NIT; ++i)
+        if (live && (lane + i * L) * N < G) store_chunk(dz, lane + i * L, G, v[i]);
     // (the choices of a row are lanes of one wave, a wide row's of the first)
     const float share = w * (dw - S);
     float own = 0.0f;
@@ -232,8 +262,9 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate_grad(GateArgs a, int
     if (id >= 0) dz[id] = (T)own;
 }
 
-// Lanes per row: two chunks each up to 16 lanes, four up to a wave, then a block per
-// row; at least k.
+// Lanes per row: four chunks each (eight lanes of 32 logits share a round's exchanges and
+// bookkeeping among more rows than sixteen of 16), fewer where there are not four waves
+// for every SIMD then; at least k lanes.  Rows of more than a wave's over a block.
 template <typename T, typename F>
 hipError_t gate_launch(const GateArgs &a, F &&f)
 {
@@ -243,19 +274,20 @@ hipError_t gate_launch(const GateArgs &a, F &&f)
         int threads = 256;
         while (threads < 1024 && chunks > 2 * threads) threads *= 2;
         const dim3 grid = net_grid(a.T), block(threads);
-        if (chunks <= 2 * threads) f(std::integral_constant<int, 2>{}, std::true_type{}, grid, block, threads);
-        else if (chunks <= 4 * threads) f(std::integral_constant<int, 4>{}, std::true_type{}, grid, block, threads);
-        else f(std::integral_constant<int, 8>{}, std::true_type{}, grid, block, threads);
+        if (chunks <= 2 * threads) f(std::integral_constant<int, 2>{}, std::true_type{}, grid, block, threads, false);
+        else if (chunks <= 4 * threads) f(std::integral_constant<int, 4>{}, std::true_type{}, grid, block, threads, false);
+        else f(std::integral_constant<int, 8>{}, std::true_type{}, grid, block, threads, false);
         return hipGetLastError();
     }
     int L = 1;
-    while (L < 64 && chunks > (L < 16 ? 2 : 4) * L) L *= 2;
+    while (L < 64 && (chunks > 4 * L || (chunks > L && a.T * L < 64 * 4096))) L *= 2;
     while (L < a.k) L *= 2;
     const int nit = (chunks + L - 1) / L;
     const dim3 grid = net_grid((a.T + 256 / L - 1) / (256 / L)), block(256);
-    if (nit <= 1) f(std::integral_constant<int, 1>{}, std::false_type{}, grid, block, L);
-    else if (nit <= 2) f(std::integral_constant<int, 2>{}, std::false_type{}, grid, block, L);
-    else f(std::integral_constant<int, 4>{}, std::false_type{}, grid, block, L);
+    const auto whole = [&](int n) { return a.G == n * L * N; };
+    if (nit <= 1) f(std::integral_constant<int, 1>{}, std::false_type{}, grid, block, L, whole(1));
+    else if (nit <= 2) f(std::integral_constant<int, 2>{}, std::false_type{}, grid, block, L, whole(2));
+    else f(std::integral_constant<int, 4>{}, std::false_type{}, grid, block, L, whole(4));
     return hipGetLastError();
 }
 
@@ -265,9 +297,9 @@ hipError_t launch_gate(const GateArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
-        return gate_launch<T>(a, [&](auto nit, auto wide, dim3 grid, dim3 block, int L) {
+        return gate_launch<T>(a, [&](auto nit, auto wide, dim3 grid, dim3 block, int L, bool whole) {
             if constexpr (decltype(wide)::value && sizeof(T) == 2 && decltype(nit)::value == 8) return;  // (four hold any row)
-            else hipLaunchKernelGGL((k_gate<T, decltype(nit)::value, decltype(wide)::value>), grid, block, 0, s, a, L);
+            else hipLaunchKernelGGL((k_gate<T, decltype(nit)::value, decltype(wide)::value>), grid, block, 0, s, a, L, whole);
         });
     });
 }
@@ -276,9 +308,9 @@ hipError_t launch_gate_grad(const GateArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
-        return gate_launch<T>(a, [&](auto nit, auto wide, dim3 grid, dim3 block, int L) {
+        return gate_launch<T>(a, [&](auto nit, auto wide, dim3 grid, dim3 block, int L, bool whole) {
             if constexpr (decltype(wide)::value && sizeof(T) == 2 && decltype(nit)::value == 8) return;
-            else hipLaunchKernelGGL((k_gate_grad<T, decltype(nit)::value, decltype(wide)::value>), grid, block, 0, s, a, L);
+            else hipLaunchKernelGGL((k_gate_grad<T, decltype(nit)::value, decltype(wide)::value>), grid, block, 0, s, a, L, whole);
         });
     });
 }
