@@ -169,13 +169,14 @@ __global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
     const int per = (bins + threads - 1) / threads, b0 = min((int)threadIdx.x * per, bins), b1 = min(b0 + per, bins);
     int s = 0;
     for (int b = b0; b < b1; ++b) {
-        int at_wave = ONE ? 0 : SUMMED ? p.count[(int64_t)tile * bins + b] : lds[before_at + b], all = 0;
+        int at_wave = ONE ? 0 : SUMMED ? p.count[(int64_t)tile * bins + b] : lds[before_at + b], all = 0, c[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) c[w] = lds[w * bins + b];
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const int c = lds[w * bins + b];
             lds[w * bins + b] = at_wave;
-            at_wave += c;
-            all += c;
+            at_wave += c[w];
+            all += c[w];
         }
         lds[base + b] = s;
         s += ONE ? all : SUMMED ? p.total[b] : lds[total + b];
