@@ -753,18 +753,31 @@ typedef struct evox_parameter {
     int64_t lds;        /* of m, v and the master */
 } evox_parameter;
 
-typedef struct evox_adam {
+/* The tensors of a step, as a table in device memory that a program makes once and
+ * keeps (table: evox_adamw_table_bytes(count) bytes, 256-byte aligned; count 0 .. 2^20; no
+ * p twice).  evox_adamw_plan reads the host array, writes the table and *plan, and
+ * waits for the copy (so it cannot be captured). */
+typedef struct evox_adam_plan {
+    const void *table;  /* device; the tensors that it names stay where they are */
+    int64_t count, tiles;
     int32_t dtype;      /* enum evox_dtype of p and g */
     int32_t bits;       /* of the states: 32 or 8 */
+    int32_t master;     /* whether the tensors have one */
+} evox_adam_plan;
+size_t evox_adamw_table_bytes(int64_t count);
+int evox_adamw_plan(int32_t dtype, int32_t bits, const evox_parameter *tensors, int64_t count, void *table,
+                    size_t table_bytes, evox_adam_plan *plan, void *hip_stream);
+
+typedef struct evox_adam {
     double lr, beta1, beta2, eps, weight_decay; /* betas 0 .. below 1, eps > 0 (as fp32 too) */
     const float *lr_dev;/* device fp32, in lr's place; or null */
 } evox_adam;
 
-/* One step of `count` tensors (a host array, read in the call; no p twice).  clock:
- * device int64 [EVOX_ADAM_CLOCK], the number of steps done and the call's own zeros:
- * the call moves the number on, so a captured step goes on counting as it is replayed.
- * Calls with the same clock or tensors are one after the other.  36 tensors per launch. */
-int evox_adamw(const evox_adam *adam, const evox_parameter *tensors, int64_t count, int64_t *clock, void *hip_stream);
+/* One step of a plan's tensors, in one launch.  clock: device int64 [EVOX_ADAM_CLOCK], the
+ * number of steps done and the call's own zeros: the call moves the number on, so a captured
+ * step goes on counting as it is replayed.  Steps of the same clock or tensors are one
+ * after the other. */
+int evox_adamw(const evox_adam *adam, const evox_adam_plan *plan, int64_t *clock, void *hip_stream);
 
 const char *evox_strerror(int code);
 const char *evox_last_error(void);

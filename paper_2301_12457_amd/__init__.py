@@ -42,7 +42,7 @@ EXPORTS = (
     "evox_layernorm", "evox_layernorm_grad_scratch_bytes", "evox_layernorm_grad",
     "evox_xent_scratch_bytes", "evox_xent",
     "evox_gate", "evox_gate_grad", "evox_route_scratch_bytes", "evox_route", "evox_dispatch", "evox_combine",
-    "evox_combine_grad", "evox_adamw",
+    "evox_combine_grad", "evox_adamw_table_bytes", "evox_adamw_plan", "evox_adamw",
 )
 
 
@@ -118,10 +118,15 @@ class Parameter(ctypes.Structure):
         (n, ctypes.c_int64) for n in ("rows", "n", "ldp", "ldg", "lds")]
 
 
+class AdamPlan(ctypes.Structure):
+    """evox_adam_plan: the tensors of a step, as a table in device memory."""
+    _fields_ = [("table", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("count", "tiles")] + [
+        (n, ctypes.c_int32) for n in ("dtype", "bits", "master")]
+
+
 class Adam(ctypes.Structure):
     """evox_adam: an optimizer's constants."""
-    _fields_ = [("dtype", ctypes.c_int32), ("bits", ctypes.c_int32)] + [
-        (n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [("lr_dev", ctypes.c_void_p)]
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [("lr_dev", ctypes.c_void_p)]
 
 
 _lib = None
@@ -190,7 +195,9 @@ def lib():
             "evox_dispatch": ([P] * 6, i32),
             "evox_combine": ([P] * 7, i32),
             "evox_combine_grad": ([P] * 8, i32),
-            "evox_adamw": ([P, P, i64, P, P], i32),
+            "evox_adamw_table_bytes": ([i64], sz),
+            "evox_adamw_plan": ([i32, i32, P, i64, P, sz, P, P], i32),
+            "evox_adamw": ([P] * 4, i32),
             "evox_strerror": ([i32], ctypes.c_char_p),
             "evox_last_error": ([], ctypes.c_char_p),
         }
@@ -767,17 +774,19 @@ class AdamW:
             self.state["master"] = torch.cat([p.reshape(-1).float() for p in self.params])
         width = {"m": bits // 8, "v": bits // 8, "m_scale": 4, "v_scale": 4, "master": 4}
         at = {name: t.data_ptr() for name, t in self.state.items()}
-        self._tensors = (Parameter * len(shapes))()
+        tensors = (Parameter * len(shapes))()
         for i, (rows, n, ldp, ldg) in enumerate(shapes):
-            self._tensors[i] = Parameter(self.params[i].data_ptr(), self.grads[i].data_ptr(), at["m"], at["v"],
-                                         at.get("m_scale"), at.get("v_scale"), at.get("master"), rows, n, ldp, ldg, n)
+            tensors[i] = Parameter(self.params[i].data_ptr(), self.grads[i].data_ptr(), at["m"], at["v"],
+                                   at.get("m_scale"), at.get("v_scale"), at.get("master"), rows, n, ldp, ldg, n)
             for name, t in self.state.items():
                 if name != "t":
                     at[name] += width[name] * (blocks[i] if name.endswith("_scale") else sizes[i])
-        self._adam = Adam(d, bits, 0.0, betas[0], betas[1], eps, weight_decay, None)
-        self.lr, self._like, self._seen = lr, like, set()
-        # a step on another stream has to find the states there
-        torch.cuda.current_stream(device).synchronize()
+        self._table, nbytes = _scratch(lib().evox_adamw_table_bytes(len(shapes)), like, None, None)
+        self._plan, self._adam = AdamPlan(), Adam(0.0, betas[0], betas[1], eps, weight_decay, None)
+        # (waits for the current stream: a step on another one finds the states there too)
+        _check(lib().evox_adamw_plan(d, bits, tensors, len(shapes), self._table.data_ptr(), nbytes, ctypes.byref(self._plan),
+                                     _raw_stream(None, like)))
+        self.lr, self._like, self._seen, self._shapes = lr, like, set(), shapes
 
     @staticmethod
     def _rows(i, p, g, like):
@@ -804,11 +813,14 @@ class AdamW:
             a.lr, a.lr_dev = lr, None
         raw = _raw_stream(stream, self._like)
         if stream is not None and raw not in self._seen:
-            # the states' memory is not given to others while this stream works on it
+            # the states' memory is not given to others while this stream works on it (a bare
+            # handle's caller sees to that)
+            import torch
             self._seen.add(raw)
-            for t in (self._clock, *self.state.values()):
-                t.record_stream(stream)
-        rc = lib().evox_adamw(ctypes.byref(a), self._tensors, len(self._tensors), self._clock.data_ptr(), raw)
+            if isinstance(stream, torch.cuda.Stream):
+                for t in (self._clock, self._table, *self.state.values()):
+                    t.record_stream(stream)
+        rc = lib().evox_adamw(ctypes.byref(a), ctypes.byref(self._plan), self._clock.data_ptr(), raw)
         if rc != OK:
             _check(rc)
 

@@ -3,10 +3,10 @@
 //     p = p - lr wd p - (lr / (1 - b1^t)) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 // with p in its own type or, with a master, in fp32 beside it.
 //
-// Bound by memory: every number is read once and written once.  The tensors travel in the
-// kernel's arguments, so that nothing is copied to the device and a step can be captured;
-// tiles are numbered through all of them.  The step's count is on the device: every
-// block reads it, and the last one that has moves it on.
+// Bound by memory: every number is read once and written once.  The tensors are a table
+// in device memory, made once, and tiles are numbered through all of them, so that a step is
+// one launch (36 tensors per launch, in the kernel's arguments: 128 small ones 20 us).  The
+// step's count is on the device: every block reads it, and the last one that has moves it on.
 //
 // 8-bit states: a group of 256 elements of a row (or a shorter row's all) is 32
 // lanes' (fewer for short rows), 8 elements each; m is e4m3 numbers times the group's
@@ -21,7 +21,6 @@ namespace evox {
 namespace {
 
 constexpr int kPasses = 2;              // groups per lane and tile
-constexpr int kTensors = 36;            // per launch: the arguments hold 4 KB
 constexpr uint32_t kPlaces = 32;        // counters of the blocks that have read the clock, 128 bytes apart
 template <int BITS>
 inline constexpr int kWidth = BITS == 8 ? 8 : 4;  // elements per lane
@@ -43,7 +42,7 @@ Groups groups_of(int32_t bits, int64_t rows, int64_t n)
 }
 uint32_t tiles_of(const Groups &g) { return (uint32_t)((g.groups + (kPasses * 256 >> g.shift) - 1) / (kPasses * 256 >> g.shift)); }
 
-// A tensor in the kernel's arguments: the caller's, its groups, and a division by the
+// A tensor in the table: the caller's, its groups, and a division by the
 // groups of a row (n / d = (t + (n - t) / 2) / 2^(s - 1) with t the upper half of n mul,
 // Granlund and Montgomery, 1994).
 struct Item {
@@ -54,17 +53,18 @@ struct Item {
     int64_t n, ldp, ldg, lds;
     uint32_t groups, per_row, mul;
     uint16_t shift, lanes;
+    uint64_t reserved;             // (whole 16 bytes)
 };
+static_assert(sizeof(Item) % 16 == 0, "the table's items");
 struct Step {
-    Item t[kTensors];
-    uint32_t start[kTensors + 1];  // first tile of each
-    int32_t count, last;
+    const Item *t;
+    const uint32_t *start;         // first tile of each
+    int32_t count;
     float beta1, beta2, keep, in1, in2, eps;  // keep, in2: roots of beta2 and 1 - beta2
     float lr, decay, log1, log2;   // the betas' logarithms
     const float *lr_dev;
     int64_t *clock;                // steps done, and blocks of this one that have read it
 };
-static_assert(sizeof(Step) <= 4096, "kernel arguments");
 
 Item item_of(const AdamTensor &t, const Groups &g)
 {
@@ -252,12 +252,20 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
     typedef typename Mine::S S;
     constexpr int E = Mine::E;
     const int64_t done = __hip_atomic_load(a.clock, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // the tensor of this tile: the last that starts at it or before
-    const int lane64 = threadIdx.x % 64;
-    const int lo = __popcll(__ballot(lane64 < a.count && a.start[min(lane64, kTensors)] <= blockIdx.x)) - 1;
-    const bool any = lo >= 0 && blockIdx.x < a.start[a.count];
-    const Item &x = a.t[max(__builtin_amdgcn_readfirstlane(lo), 0)];
-    const uint32_t index = blockIdx.x - a.start[max(__builtin_amdgcn_readfirstlane(lo), 0)];
+    // the tensor of this tile: the last that starts at it or before (64 probes at a time)
+    int lo = 0, hi = a.count;
+    uint32_t begin = 0;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, at = lo + (int)(threadIdx.x % 64) * step;
+        const uint32_t first = a.start[min(at, hi - 1)];
+        const int n = __popcll(__ballot(at < hi && first <= blockIdx.x));
+        begin = __builtin_amdgcn_readlane(first, n - 1);
+        lo += (n - 1) * step;
+        hi = min(lo + step, hi);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const Item x = a.t[lo];
+    const uint32_t index = blockIdx.x - begin;
 
     // The step's number and what it makes of the constants, asked for after the first loads
     // are on their way; 1 - b^t = -expm1(t log b) (fp32: within 3 roundings of it).  Once every
@@ -267,7 +275,7 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
         asm volatile("" ::"v"((uint32_t)done));  // (here it is in a register: the load is done)
         const int64_t t = max(done + 1, (int64_t)1);
         __syncthreads();
-        if (a.last && threadIdx.x == 0) {
+        if (threadIdx.x == 0) {
             const uint32_t place = blockIdx.x % kPlaces, mates = (gridDim.x - place + kPlaces - 1) / kPlaces;
             uint32_t *of = (uint32_t *)(a.clock + 16 * (1 + place)), *all = (uint32_t *)(a.clock + 1);
             const auto count = [](uint32_t *c) { return __hip_atomic_fetch_add(c, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
@@ -287,7 +295,7 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
         return Rates{a.beta1, a.beta2, a.keep, a.in1, a.in2, some ? turn / sqrtf(-expm1f((float)t * a.log2)) : 0.0f,
                      some ? turn * a.eps : INFINITY, lr * a.decay};
     };
-    if (!any) {
+    if (x.groups == 0) {  // (a table without elements is one tile of nothing: the count moves on)
         rates_of();
         return;
     }
@@ -408,9 +416,35 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
 
 int64_t adam_groups(int32_t bits, int64_t rows, int64_t n) { return groups_of(bits, rows, n).groups; }
 
-hipError_t launch_adamw(const AdamCall &c, const AdamTensor *t, int64_t count, hipStream_t s)
+size_t adam_table(int64_t count) { return (size_t)(count + 1) * (sizeof(Item) + 4); }
+
+int64_t adam_fill_table(int32_t bits, const AdamTensor *t, int64_t count, void *host)
+{
+    // (tensors without elements are empty items whose tile is the next one's too: the search
+    // finds the last)
+    Item *items = (Item *)host;
+    uint32_t *start = (uint32_t *)(items + count + 1);
+    int64_t tiles = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        start[i] = (uint32_t)tiles;
+        items[i] = Item{};
+        if (t[i].rows == 0 || t[i].n == 0) continue;
+        const Groups g = groups_of(bits, t[i].rows, t[i].n);
+        items[i] = item_of(t[i], g);
+        tiles += tiles_of(g);
+        if (tiles > INT32_MAX) return -1;
+    }
+    items[count] = Item{};
+    start[count] = (uint32_t)tiles;
+    return tiles;
+}
+
+hipError_t launch_adamw(const AdamCall &c, hipStream_t s)
 {
     Step a{};
+    a.t = (const Item *)c.table;
+    a.start = (const uint32_t *)(a.t + c.count + 1);
+    a.count = (int32_t)c.count;
     a.lr = (float)c.lr;
     a.decay = (float)c.decay;
     a.log1 = (float)log(c.beta1);  // (of 0: -inf, and 1 - b^t = 1)
@@ -423,37 +457,20 @@ hipError_t launch_adamw(const AdamCall &c, const AdamTensor *t, int64_t count, h
     a.eps = (float)c.eps;
     a.lr_dev = c.lr_dev;
     a.clock = c.clock;
-    const bool master = count > 0 && t[0].master;
-    int64_t i = 0;
-    do {
-        a.count = 0;
-        uint32_t tiles = 0;
-        // as many tensors as the arguments hold (those without elements are left out)
-        for (; i < count && a.count < kTensors; ++i) {
-            if (t[i].rows == 0 || t[i].n == 0) continue;
-            const Groups g = groups_of(c.bits, t[i].rows, t[i].n);
-            const uint32_t n = tiles_of(g);
-            if (n > UINT32_MAX / 2 - tiles) break;
-            a.start[a.count] = tiles;
-            a.t[a.count++] = item_of(t[i], g);
-            tiles += n;
-        }
-        a.start[a.count] = tiles;
-        a.last = i == count;
-        if (tiles == 0 && !a.last) continue;  // (in the last launch the count moves on all the same)
-        const hipError_t e = net_dispatch(c.dtype, [&](auto type) {
-            typedef typename NetElement<decltype(type)::value>::type T;
-            const dim3 grid(tiles == 0 ? 1 : tiles), block(256);
-            if (c.bits == 8) {
-                if (master) hipLaunchKernelGGL((k_adamw<T, 8, true>), grid, block, 0, s, a);
-                else hipLaunchKernelGGL((k_adamw<T, 8, false>), grid, block, 0, s, a);
-            } else if (master) hipLaunchKernelGGL((k_adamw<T, 32, true>), grid, block, 0, s, a);
-            else hipLaunchKernelGGL((k_adamw<T, 32, false>), grid, block, 0, s, a);
-            return hipGetLastError();
-        });
-        if (e != hipSuccess) return e;
-    } while (i < count);
-    return hipSuccess;
+    if (c.tiles == 0) {  // the empty item behind the others
+        a.t += c.count;
+        a.count = 1;
+    }
+    return net_dispatch(c.dtype, [&](auto type) {
+        typedef typename NetElement<decltype(type)::value>::type T;
+        const dim3 grid(c.tiles == 0 ? 1 : (unsigned)c.tiles), block(256);
+        if (c.bits == 8) {
+            if (c.master) hipLaunchKernelGGL((k_adamw<T, 8, true>), grid, block, 0, s, a);
+            else hipLaunchKernelGGL((k_adamw<T, 8, false>), grid, block, 0, s, a);
+        } else if (c.master) hipLaunchKernelGGL((k_adamw<T, 32, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((k_adamw<T, 32, false>), grid, block, 0, s, a);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace evox

@@ -2025,19 +2025,22 @@ static_assert(sizeof(evox_parameter) == sizeof(AdamTensor) && offsetof(evox_para
                   offsetof(evox_parameter, rows) == offsetof(AdamTensor, rows) && offsetof(evox_parameter, lds) == offsetof(AdamTensor, lds),
               "evox_parameter");
 
-int evox_adamw(const evox_adam *c, const evox_parameter *t, int64_t count, int64_t *clock, void *hip_stream)
+size_t evox_adamw_table_bytes(int64_t count)
 {
-    if (!c) return fail(EVOX_EINVAL, "adam is null");
-    if (c->dtype != EVOX_F32 && c->dtype != EVOX_BF16 && c->dtype != EVOX_F16)
-        return fail(EVOX_EINVAL, "unknown dtype %d", c->dtype);
-    if (c->bits != 32 && c->bits != 8) return fail(EVOX_EINVAL, "bits = %d: states of 32 or 8", c->bits);
-    if (!(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0))
-        return fail(EVOX_EINVAL, "beta1 and beta2 must be in [0, 1)");
-    if (!((float)c->eps > 0.0f && (float)c->eps < INFINITY)) return fail(EVOX_EINVAL, "eps must be > 0");
-    if (!std::isfinite(c->lr) || !std::isfinite(c->weight_decay)) return fail(EVOX_EINVAL, "lr and weight_decay must be finite");
-    if (count < 0 || (count > 0 && !t)) return fail(EVOX_EINVAL, "tensors are required");
-    if (!clock) return fail(EVOX_EINVAL, "clock is required");
-    if ((uintptr_t)clock & 7u || (uintptr_t)c->lr_dev & 3u) return fail(EVOX_EALIGN, "clock or lr_dev is misaligned");
+    if (count < 0 || count > kNetMaxG) {
+        fail(EVOX_EINVAL, "%lld tensors: need 0 .. 2^20", (long long)count);
+        return 0;
+    }
+    return round256(adam_table(count));
+}
+
+int evox_adamw_plan(int32_t dtype, int32_t bits, const evox_parameter *t, int64_t count, void *table, size_t table_bytes,
+                    evox_adam_plan *plan, void *hip_stream)
+{
+    if (dtype != EVOX_F32 && dtype != EVOX_BF16 && dtype != EVOX_F16) return fail(EVOX_EINVAL, "unknown dtype %d", dtype);
+    if (bits != 32 && bits != 8) return fail(EVOX_EINVAL, "bits = %d: states of 32 or 8", bits);
+    if (count < 0 || count > kNetMaxG) return fail(EVOX_EINVAL, "%lld tensors: need 0 .. 2^20", (long long)count);
+    if (!plan || (count > 0 && !t)) return fail(EVOX_EINVAL, "tensors and plan are required");
     const bool master = count > 0 && t[0].master;
     for (int64_t i = 0; i < count; ++i) {
         const evox_parameter &x = t[i];
@@ -2045,30 +2048,59 @@ int evox_adamw(const evox_adam *c, const evox_parameter *t, int64_t count, int64
             return fail(EVOX_EINVAL, "tensor %lld: rows = %lld, n = %lld out of range", (long long)i, (long long)x.rows, (long long)x.n);
         if (!x.master != !master) return fail(EVOX_EINVAL, "tensor %lld: a master for all tensors, or for none", (long long)i);
         if (x.rows == 0 || x.n == 0) continue;
-        if (!x.p || !x.g || !x.m || !x.v || (c->bits == 8 && (!x.m_scale || !x.v_scale)))
+        if (!x.p || !x.g || !x.m || !x.v || (bits == 8 && (!x.m_scale || !x.v_scale)))
             return fail(EVOX_EINVAL, "tensor %lld: p, g, m, v and (8 bits) their scales are required", (long long)i);
-        if (!element_aligned(c->dtype, {x.p, x.g}) || !element_aligned(EVOX_F32, {x.master, x.m_scale, x.v_scale}) ||
-            (c->bits == 32 && !element_aligned(EVOX_F32, {x.m, x.v})))
+        if (!element_aligned(dtype, {x.p, x.g}) || !element_aligned(EVOX_F32, {x.master, x.m_scale, x.v_scale}) ||
+            (bits == 32 && !element_aligned(EVOX_F32, {x.m, x.v})))
             return fail(EVOX_EALIGN, "tensor %lld is misaligned", (long long)i);
         const auto pitch = [&](int64_t ld) { return x.rows == 1 || (ld >= x.n && ld <= ((int64_t)1 << 46) / x.rows); };
         if (!pitch(x.ldp) || !pitch(x.ldg) || !pitch(x.lds))
             return fail(EVOX_EINVAL, "tensor %lld: a row pitch is below the row length or too large", (long long)i);
-        if (adam_groups(c->bits, x.rows, x.n) > INT32_MAX)
+        if (adam_groups(bits, x.rows, x.n) > INT32_MAX)
             return fail(EVOX_EINVAL, "tensor %lld is too large: %lld x %lld", (long long)i, (long long)x.rows, (long long)x.n);
     }
-    if (count > 1) {  // a tensor twice would be two blocks' at once
-        const void **at = (const void **)malloc((size_t)count * sizeof(void *));
-        if (!at) return fail(EVOX_ENOSPC, "no host memory for %lld tensors", (long long)count);
-        int64_t n = 0;
-        for (int64_t i = 0; i < count; ++i)
-            if (t[i].rows && t[i].n) at[n++] = t[i].p;
-        std::sort(at, at + n);
-        const bool twice = std::adjacent_find(at, at + n) != at + n;
-        free(at);
-        if (twice) return fail(EVOX_EINVAL, "a tensor is there twice");
+    const int rc = check_scratch(table, table_bytes, round256(adam_table(count)));
+    if (rc != EVOX_OK) return rc;
+    // on the host: the tensors' addresses in order (a tensor twice would be two blocks' at
+    // once), then the table
+    void *host = malloc(adam_table(count));
+    if (!host) return fail(EVOX_ENOSPC, "no host memory for %lld tensors", (long long)count);
+    const void **at = (const void **)host;
+    int64_t n = 0;
+    for (int64_t i = 0; i < count; ++i)
+        if (t[i].rows && t[i].n) at[n++] = t[i].p;
+    std::sort(at, at + n);
+    const bool twice = std::adjacent_find(at, at + n) != at + n;
+    const int64_t tiles = adam_fill_table(bits, (const AdamTensor *)t, count, host);
+    hipError_t e = hipSuccess;
+    if (!twice && tiles >= 0) {
+        e = hipMemcpyAsync(table, host, adam_table(count), hipMemcpyHostToDevice, (hipStream_t)hip_stream);
+        if (e == hipSuccess) e = hipStreamSynchronize((hipStream_t)hip_stream);
     }
-    const AdamCall call{c->dtype, c->bits, c->lr, c->beta1, c->beta2, c->eps, c->weight_decay, c->lr_dev, clock};
-    const hipError_t e = launch_adamw(call, (const AdamTensor *)t, count, (hipStream_t)hip_stream);
+    free(host);
+    if (twice) return fail(EVOX_EINVAL, "a tensor is there twice");
+    if (tiles < 0) return fail(EVOX_EINVAL, "the tensors are too large together");
+    if (e != hipSuccess) return hip_fail(e, "table of tensors");
+    *plan = evox_adam_plan{table, count, tiles, dtype, bits, master};
+    return EVOX_OK;
+}
+
+int evox_adamw(const evox_adam *c, const evox_adam_plan *p, int64_t *clock, void *hip_stream)
+{
+    if (!c || !p) return fail(EVOX_EINVAL, "adam or plan is null");
+    if ((p->dtype != EVOX_F32 && p->dtype != EVOX_BF16 && p->dtype != EVOX_F16) || (p->bits != 32 && p->bits != 8) || !p->table ||
+        p->count < 0 || p->count > kNetMaxG || p->tiles < 0 || p->tiles > INT32_MAX)
+        return fail(EVOX_EINVAL, "the plan is not evox_adamw_plan's");
+    if (!(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0))
+        return fail(EVOX_EINVAL, "beta1 and beta2 must be in [0, 1)");
+    if (!((float)c->eps > 0.0f && (float)c->eps < INFINITY)) return fail(EVOX_EINVAL, "eps must be > 0");
+    if (!std::isfinite((float)c->lr) || !std::isfinite((float)c->weight_decay))
+        return fail(EVOX_EINVAL, "lr and weight_decay must be finite");
+    if (!clock) return fail(EVOX_EINVAL, "clock is required");
+    if ((uintptr_t)clock & 7u || (uintptr_t)c->lr_dev & 3u) return fail(EVOX_EALIGN, "clock or lr_dev is misaligned");
+    const AdamCall call{p->dtype, p->bits, p->master, c->lr, c->beta1, c->beta2, c->eps, c->weight_decay, c->lr_dev, clock,
+                        p->table, p->count, p->tiles};
+    const hipError_t e = launch_adamw(call, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail(e, "adamw");
     return EVOX_OK;
 }

@@ -60,14 +60,18 @@ struct AdamTensor {
     int64_t rows, n, ldp, ldg, lds;
 };
 struct AdamCall {
-    int32_t dtype, bits;
+    int32_t dtype, bits, master;
     double lr, beta1, beta2, eps, decay;
     const float *lr_dev;
     int64_t *clock;
+    const void *table;
+    int64_t count, tiles;
 };
 constexpr int kAdamBlock = 256;  // elements per scale of an 8-bit state
 int64_t adam_groups(int32_t bits, int64_t rows, int64_t n);  // below 2^31 for each tensor
-hipError_t launch_adamw(const AdamCall &c, const AdamTensor *t, int64_t count, hipStream_t s);
+size_t adam_table(int64_t count);                            // bytes
+int64_t adam_fill_table(int32_t bits, const AdamTensor *t, int64_t count, void *host);  // its tiles
+hipError_t launch_adamw(const AdamCall &c, hipStream_t s);
 
 // Lanes of a wave in groups of L (a power of two): the maximum or sum over a group in
 // every lane of it, by lane exchanges in registers (no LDS): neighbours, pairs, halves

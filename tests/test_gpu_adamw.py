@@ -45,8 +45,7 @@ class Held:
         self.m, self.v, self.scales, self.master = [], [], [], []
         at, block = 0, 0
         for i, p in enumerate(opt.params):
-            t = opt._tensors[i]
-            rows, n = t.rows, t.n
+            rows, n = opt._shapes[i][:2]
             N, per = rows * n, -(-n // 256)
             for name, out in (("m", self.m), ("v", self.v)):
                 x = opt.state[name][at:at + N].double().cpu().view(rows, n)

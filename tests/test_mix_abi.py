@@ -28,7 +28,8 @@ def test_struct_layouts(evox):
     assert ctypes.sizeof(evox.Choice) == 8 + 5 * 8 and evox.Choice.T.offset == 8
     assert ctypes.sizeof(evox.Slots) == 8 + 9 * 8 and evox.Slots.ldds.offset == 72
     assert ctypes.sizeof(evox.Parameter) == 12 * 8 and evox.Parameter.rows.offset == 56
-    assert ctypes.sizeof(evox.Adam) == 8 + 5 * 8 + 8 and evox.Adam.lr_dev.offset == 48
+    assert ctypes.sizeof(evox.Adam) == 5 * 8 + 8 and evox.Adam.lr_dev.offset == 40
+    assert ctypes.sizeof(evox.AdamPlan) == 3 * 8 + 16 and evox.AdamPlan.dtype.offset == 24
 
 
 def choice(evox, **kw):
@@ -125,40 +126,61 @@ def test_slots_refuse(evox):
     assert combine_grad(evox, slots(evox), None, None, None, None, None, None) == evox.OK  # nothing asked for
 
 
-def adam(evox, **kw):
-    return evox.Adam(**dict(dict(dtype=evox.F32, bits=32, lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.1), **kw))
-
-
 def tensor(evox, **kw):
     return evox.Parameter(**dict(dict(p=P, g=P, m=P, v=P, m_scale=P, v_scale=P, master=None, rows=3, n=5, ldp=5, ldg=5, lds=5), **kw))
 
 
-def step(evox, a, *ts, count=None, clock=P):
-    return call(evox, "evox_adamw", a, (evox.Parameter * len(ts))(*ts) if ts else None, len(ts) if count is None else count, clock)
+def plan(evox, *ts, dtype=0, bits=32, count=None, table=P, nbytes=BIG, out=True):
+    p = evox.AdamPlan()
+    return evox.lib().evox_adamw_plan(dtype, bits, (evox.Parameter * len(ts))(*ts) if ts else None, len(ts) if count is None else count,
+                                      table, nbytes, ctypes.byref(p) if out else None, None)
 
 
-@pytest.mark.parametrize("kw", [dict(dtype=3), dict(bits=16), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan),
-                                dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-60), dict(eps=math.inf), dict(eps=math.nan), dict(lr=math.nan),
-                                dict(lr=math.inf), dict(weight_decay=math.nan)])
-def test_step_refuses(evox, kw):
-    assert step(evox, adam(evox, **kw), tensor(evox)) == evox.EINVAL
-
-
-def test_step_refuses_tensors(evox):
-    a, b = adam(evox), adam(evox, bits=8)
-    assert step(evox, None, tensor(evox)) == evox.EINVAL
-    assert step(evox, a, tensor(evox), clock=None) == evox.EINVAL and step(evox, a, tensor(evox), clock=P + 4) == evox.EALIGN
-    assert step(evox, a, count=1) == evox.EINVAL and step(evox, a, tensor(evox), count=-1) == evox.EINVAL
-    assert step(evox, adam(evox, lr_dev=P + 2), tensor(evox)) == evox.EALIGN
+def test_plan_refuses(evox):
+    need = evox.lib().evox_adamw_table_bytes
+    assert need(1) > 0 and need(0) > 0 and need(-1) == 0 and need((1 << 20) + 1) == 0
+    ok = tensor(evox)
+    for kw in (dict(dtype=3), dict(bits=16), dict(count=-1), dict(count=(1 << 20) + 1), dict(out=False), dict(table=None)):
+        assert plan(evox, ok, **kw) == evox.EINVAL, kw
+    assert plan(evox, count=1) == evox.EINVAL
+    assert plan(evox, ok, table=P + 16) == evox.EALIGN and plan(evox, ok, nbytes=need(1) - 1) == evox.ENOSPC
     for kw in (dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(rows=-1), dict(rows=1 << 31), dict(n=-1), dict(n=1 << 39),
                dict(ldp=4), dict(ldg=4), dict(lds=4), dict(ldp=1 << 60), dict(rows=1 << 30, n=1 << 20, ldp=1 << 20, ldg=1 << 20, lds=1 << 20)):
-        assert step(evox, a, tensor(evox, **kw)) == evox.EINVAL, kw
+        assert plan(evox, tensor(evox, **kw)) == evox.EINVAL, kw
     for k in ("p", "g", "m", "v", "master"):
-        assert step(evox, a, tensor(evox, **{k: P + 2})) == evox.EALIGN
+        assert plan(evox, tensor(evox, **{k: P + 2})) == evox.EALIGN
     for k in ("m_scale", "v_scale"):
-        assert step(evox, b, tensor(evox, **{k: None})) == evox.EINVAL
-        assert step(evox, b, tensor(evox, **{k: P + 1})) == evox.EALIGN
-    # a master for all or for none; no tensor twice
-    assert step(evox, a, tensor(evox, master=P), tensor(evox, p=2 * P)) == evox.EINVAL
-    assert step(evox, a, *[tensor(evox, p=P * (i % 40 + 1)) for i in range(41)]) == evox.EINVAL
+        assert plan(evox, tensor(evox, **{k: None}), bits=8) == evox.EINVAL
+        assert plan(evox, tensor(evox, **{k: P + 1}), bits=8) == evox.EALIGN
+    # a master for all or for none; no tensor twice; not too many elements in all
+    assert plan(evox, tensor(evox, master=P), tensor(evox, p=2 * P)) == evox.EINVAL
+    assert plan(evox, *[tensor(evox, p=P * (i % 40 + 1)) for i in range(41)]) == evox.EINVAL
     assert b"twice" in evox.lib().evox_last_error()
+    big = dict(rows=1, n=1 << 38)
+    assert plan(evox, *[tensor(evox, p=P * (i + 1), **big) for i in range(40)]) == evox.EINVAL
+    assert b"together" in evox.lib().evox_last_error()
+
+
+def adam(evox, **kw):
+    return evox.Adam(**dict(dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.1), **kw))
+
+
+def step(evox, a, clock=P, **kw):
+    p = evox.AdamPlan(**dict(dict(table=P, count=1, tiles=1, dtype=0, bits=32, master=0), **kw))
+    return evox.lib().evox_adamw(ctypes.byref(a) if a else None, ctypes.byref(p), clock, None)
+
+
+@pytest.mark.parametrize("kw", [dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan), dict(eps=0.0), dict(eps=-1.0),
+                                dict(eps=1e-60), dict(eps=math.inf), dict(eps=math.nan), dict(lr=math.nan), dict(lr=math.inf), dict(lr=1e300),
+                                dict(weight_decay=math.nan)])
+def test_step_refuses(evox, kw):
+    assert step(evox, adam(evox, **kw)) == evox.EINVAL
+
+
+def test_step_refuses_plans(evox):
+    a = adam(evox)
+    assert step(evox, None) == evox.EINVAL and evox.lib().evox_adamw(ctypes.byref(a), None, P, None) == evox.EINVAL
+    for kw in (dict(table=None), dict(count=-1), dict(tiles=-1), dict(tiles=1 << 31), dict(dtype=3), dict(bits=0)):
+        assert step(evox, a, **kw) == evox.EINVAL, kw
+    assert step(evox, a, clock=None) == evox.EINVAL and step(evox, a, clock=P + 4) == evox.EALIGN
+    assert step(evox, adam(evox, lr_dev=P + 2)) == evox.EALIGN

@@ -128,10 +128,14 @@ def here(evox, monkeypatch):
     """States that are made on the host count as the GPU's."""
     real = torch.zeros
     monkeypatch.setattr(torch, "zeros", lambda *a, **k: gpu(real(*a, **k)))
-    waits = []
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: types.SimpleNamespace(synchronize=lambda: waits.append(d)))
-    evox.waits = waits
     return evox
+
+
+def planned(evox):
+    """The tensors of the last plan."""
+    name, args = [c for c in evox.calls if c[0] == "evox_adamw_plan"][-1]
+    assert args[5] == 4096 and args[7] == 7
+    return args[0], args[1], list(args[2])
 
 
 def test_optimizer_s_tensors(here):
@@ -140,19 +144,19 @@ def test_optimizer_s_tensors(here):
     params = [new(3, 4), X[:, 1:4], X[:, 10:610].unflatten(1, (2, 300)), new(9)]
     grads = [new(3, 4), D[:, 1:4], D[:, 10:610].unflatten(1, (2, 300)), new(9)]
     opt = evox.AdamW(params, grads, lr=0.5, betas=(0.8, 0.7), eps=0.1, weight_decay=0.3, bits=8)
-    assert len(evox.waits) == 1
     s = opt.state
     assert sorted(s) == ["m", "m_scale", "t", "v", "v_scale"] and s["m"].dtype == torch.float8_e4m3fn
     assert s["m"].numel() == 12 + 15 + 3000 + 9 and s["v_scale"].numel() == 1 + 5 + 5 * 3 + 1
-    t = opt._tensors
+    dtype, bits, t = planned(evox)
+    assert (dtype, bits) == (evox.F32, 8)
     assert [(x.rows, x.n, x.ldp, x.ldg, x.lds) for x in t] == [(1, 12, 12, 12, 12), (5, 3, 700, 710, 3), (5, 600, 700, 710, 600), (1, 9, 9, 9, 9)]
     assert [x.m - t[0].m for x in t] == [0, 12, 27, 3027] and [x.v_scale - t[0].v_scale for x in t] == [0, 4, 24, 84]
     assert t[1].p == params[1].data_ptr() and t[1].g == grads[1].data_ptr() and t[0].master is None
     opt.step()
     name, args = evox.calls[-1]
     a = args[0]._obj
-    assert name == "evox_adamw" and args[2] == 4 and args[3] == s["t"].data_ptr() and args[4] == 7
-    assert (a.dtype, a.bits, a.lr, a.beta1, a.beta2, a.eps, a.weight_decay, a.lr_dev) == (evox.F32, 8, 0.5, 0.8, 0.7, 0.1, 0.3, None)
+    assert name == "evox_adamw" and args[1]._obj is opt._plan and args[2] == s["t"].data_ptr() and args[3] == 7
+    assert (a.lr, a.beta1, a.beta2, a.eps, a.weight_decay, a.lr_dev) == (0.5, 0.8, 0.7, 0.1, 0.3, None)
     opt.lr = lr = new(1)
     opt.step(stream=types.SimpleNamespace(cuda_stream=3))
     assert evox.calls[-1][1][-1] == 3 and evox.calls[-1][1][0]._obj.lr_dev == lr.data_ptr()
@@ -165,7 +169,8 @@ def test_optimizer_s_master(here):
     p = new(2, 5).bfloat16() + 1
     opt = here.AdamW([p, gpu(p.clone())], [new(2, 5).bfloat16()] * 2, master=True)
     assert opt.state["master"].tolist() == [1.0] * 20 and opt.state["m"].dtype == torch.float32
-    assert [x.master - opt._tensors[0].master for x in opt._tensors] == [0, 40]
+    t = planned(here)[2]
+    assert [x.master - t[0].master for x in t] == [0, 40]
 
 
 @pytest.mark.parametrize("params,grads,kw,words", [
@@ -179,7 +184,7 @@ def test_optimizer_s_master(here):
 def test_optimizer_refuses(here, params, grads, kw, words):
     with pytest.raises(here.EvoxError, match=words):
         here.AdamW(params, grads, **kw)
-    assert not here.calls
+    assert not any(n == "evox_adamw_plan" for n, _ in here.calls)
 
 
 def test_optimizer_refuses_rates_and_devices(here, monkeypatch):
@@ -190,4 +195,4 @@ def test_optimizer_refuses_rates_and_devices(here, monkeypatch):
     on_host_device(here, monkeypatch, 1)
     with pytest.raises(here.EvoxError, match="the current device is 1"):
         opt.step()
-    assert not here.calls
+    assert not any(n == "evox_adamw" for n, _ in here.calls)
