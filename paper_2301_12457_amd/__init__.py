@@ -771,7 +771,7 @@ class AdamW:
                 self.state[name] = zeros(N, torch.uint8).view(torch.float8_e4m3fn)
                 self.state[name + "_scale"] = zeros(sum(blocks))
         if master:
-            self.state["master"] = torch.cat([p.reshape(-1).float() for p in self.params])
+            self.state["master"] = torch.cat([p.reshape(-1) for p in self.params]).float()
         width = {"m": bits // 8, "v": bits // 8, "m_scale": 4, "v_scale": 4, "master": 4}
         at = {name: t.data_ptr() for name, t in self.state.items()}
         tensors = (Parameter * len(shapes))()

@@ -95,13 +95,19 @@ struct Packed {
     typedef T reg __attribute__((ext_vector_type(E)));
     typedef T mem __attribute__((ext_vector_type(E), aligned(sizeof(T))));
 };
-// A lane's E elements of a row: loaded from the row's last E where they pass its end (no
-// branch, so that all loads of a batch are on their way together), and then moved to their
-// places with 0 behind them.  TINY: rows of fewer than E, element by element.
-template <bool TINY, int E, typename T>
+// What a lane does with its E elements where they pass the row's end: all load the row's
+// last E there (no branch, so that all loads are on their way together).
+//   OVERLAP  and update and store those; the elements that the lane before has too come out
+//            the same (it is of the same group, whose loads all come before its stores)
+//   SETTLE   moves them to their places, 0 behind them, and stores what is the row's: where a
+//            group has no more than part of one lane's, so that the lane before is of another
+//            group, in another wave perhaps, which may have stored already
+//   TINY     rows of fewer than E elements, one by one
+enum RowEnd { OVERLAP = 0, SETTLE = 1, TINY = 2 };
+template <int END, int E, typename T>
 __device__ __forceinline__ typename Packed<T, E>::reg get(const T *row, int64_t col, int64_t n)
 {
-    if constexpr (!TINY) return *reinterpret_cast<const typename Packed<T, E>::mem *>(row + min(col, n - E));
+    if constexpr (END != TINY) return __builtin_nontemporal_load(reinterpret_cast<const typename Packed<T, E>::mem *>(row + min(col, n - E)));
     typename Packed<T, E>::reg v;
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = e < n ? row[e] : (T)0;
@@ -124,7 +130,7 @@ __device__ __forceinline__ void settle_row(typename Packed<T, E>::reg &v, int64_
 template <int E, typename T>
 __device__ __forceinline__ void put(T *p, int n, typename Packed<T, E>::reg v)
 {
-    if (n >= E) *reinterpret_cast<typename Packed<T, E>::mem *>(p) = v;
+    if (n >= E) __builtin_nontemporal_store((typename Packed<T, E>::mem)v, reinterpret_cast<typename Packed<T, E>::mem *>(p));
     else
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -321,14 +327,15 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
                 l.m_scale = ms[i / kAdamBlock];
                 l.v_scale = vs[i / kAdamBlock];
             }
-            __builtin_amdgcn_sched_barrier(0);
         };
-        Mine l;
-        load(l, 0);
+        Mine ls[kPasses];
+#pragma unroll
+        for (int u = 0; u < kPasses; ++u) load(ls[u], u);
+        __builtin_amdgcn_sched_barrier(0);
         const Rates rates = rates_of();
 #pragma unroll
         for (int u = 0; u < kPasses; ++u) {
-            if (u > 0) load(l, u);
+            Mine &l = ls[u];
             const uint32_t i = (u * 256 + threadIdx.x) * E;
             l.step(rates, 32);
             __builtin_nontemporal_store((typename Packed<S, E>::mem)l.m, (typename Packed<S, E>::mem *)(m + i));
@@ -346,16 +353,18 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
     }
 
     const int shift = x.lanes, lane = threadIdx.x & ((1 << shift) - 1);
-    const auto passes = [&](auto tiny) {
-        constexpr bool TINY = decltype(tiny)::value;
-        Mine l;
-        uint32_t group;
-        bool live;
-        int64_t op, os, col;  // the row's place in p and in the states, the lane's in the row
-        const auto load = [&](int u) {
+    const auto passes = [&](auto end) {
+        constexpr int END = decltype(end)::value;
+        Mine ls[kPasses];
+        uint32_t groups[kPasses];
+        int64_t ops[kPasses], oss[kPasses], cols[kPasses];  // the rows' places in p and in the states, the lane's in the row
+#pragma unroll
+        for (int u = 0; u < kPasses; ++u) {
+            Mine &l = ls[u];
+            uint32_t &group = groups[u];
+            int64_t &op = ops[u], &os = oss[u], &col = cols[u];
             group = (index * kPasses + u) * (256 >> shift) + (threadIdx.x >> shift);
-            live = group < x.groups;
-            const uint32_t gr = live ? group : x.groups - 1;
+            const uint32_t gr = min(group, x.groups - 1);
             uint32_t r = 0;
             if (x.per_row == 1) r = gr;
             else if (x.per_row != x.groups) {
@@ -370,46 +379,59 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
                 os = r * x.lds;
             }
             col = ((int64_t)(gr - r * x.per_row) << shift | lane) * E;
-            l.g = get<TINY, E>((const T *)x.g + og, col, x.n);
-            l.p = get<TINY, E>(MASTER ? (const P *)x.master + os : (const P *)x.p + op, col, x.n);
-            l.m = get<TINY, E>((const S *)x.m + os, col, x.n);
-            l.v = get<TINY, E>((const S *)x.v + os, col, x.n);
+            l.g = get<END, E>((const T *)x.g + og, col, x.n);
+            l.p = get<END, E>(MASTER ? (const P *)x.master + os : (const P *)x.p + op, col, x.n);
+            l.m = get<END, E>((const S *)x.m + os, col, x.n);
+            l.v = get<END, E>((const S *)x.v + os, col, x.n);
             if constexpr (BITS == 8) {
                 l.m_scale = x.m_scale[gr];
                 l.v_scale = x.v_scale[gr];
             }
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        load(0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         const Rates rates = rates_of();
-        for (int u = 0;;) {
-            const int n = live ? (int)min(max(x.n - col, (int64_t)0), (int64_t)E) : 0;
-            const bool inside = __all(n >= E);
-            if (!TINY && !inside) {
+#pragma unroll
+        for (int u = 0; u < kPasses; ++u) {
+            Mine &l = ls[u];
+            const uint32_t group = groups[u];
+            const bool live = group < x.groups;
+            const int64_t op = ops[u], os = oss[u];
+            int64_t col = cols[u];
+            int n = live ? (int)min(max(x.n - col, (int64_t)0), (int64_t)E) : 0;
+            if constexpr (END == OVERLAP) {
+                if (n > 0) n = E;
+                col = min(col, x.n - E);
+            }
+            if (END == SETTLE && !__all(n >= E)) {
                 settle_row<E, T>(l.g, col, x.n);
                 settle_row<E, P>(l.p, col, x.n);
                 settle_row<E, S>(l.m, col, x.n);
                 settle_row<E, S>(l.v, col, x.n);
             }
             l.step(rates, 1 << shift);
-            const int left = inside ? E : n;
-            put<E>((S *)x.m + os + col, left, l.m);
-            put<E>((S *)x.v + os + col, left, l.v);
+            const auto store = [&](auto *to, auto v) {
+                if constexpr (END == OVERLAP) {
+                    typedef typename Packed<typename std::remove_pointer<decltype(to)>::type, E>::mem mem;
+                    if (n > 0) __builtin_nontemporal_store((mem)v, (mem *)to);
+                } else put<E>(to, n, v);
+            };
+            store((S *)x.m + os + col, l.m);
+            store((S *)x.v + os + col, l.v);
             if constexpr (MASTER) {
-                put<E>(x.master + os + col, left, l.p);
-                put<E>((T *)x.p + op + col, left, l.rounded());
-            } else put<E>((T *)x.p + op + col, left, l.p);
+                store(x.master + os + col, l.p);
+                store((T *)x.p + op + col, l.rounded());
+            } else store((T *)x.p + op + col, l.p);
             if constexpr (BITS == 8)
                 if (live && lane == 0) {
                     x.m_scale[group] = l.m_scale;
                     x.v_scale[group] = l.v_scale;
                 }
-            if (++u == kPasses || (index * kPasses + u) * (256 >> shift) >= x.groups) break;
-            load(u);
         }
     };
-    if (x.n >= E) passes(std::false_type{});
-    else passes(std::true_type{});
+    const int tail = (int)(x.n & ((E << shift) - 1));  // of the row's last group
+    if (x.n < E) passes(std::integral_constant<int, TINY>{});
+    else if (tail > 0 && tail < E) passes(std::integral_constant<int, SETTLE>{});
+    else passes(std::integral_constant<int, OVERLAP>{});
 }
 
 }  // namespace
