@@ -130,7 +130,7 @@ __device__ __forceinline__ void settle_row(typename Packed<T, E>::reg &v, int64_
 template <int E, typename T>
 __device__ __forceinline__ void put(T *p, int n, typename Packed<T, E>::reg v)
 {
-    if (n >= E) __builtin_nontemporal_store((typename Packed<T, E>::mem)v, reinterpret_cast<typename Packed<T, E>::mem *>(p));
+    if (n >= E) *reinterpret_cast<typename Packed<T, E>::mem *>(p) = v;
     else
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -309,8 +309,9 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
     constexpr int kElements = kPasses * 256 * E;
     if (x.per_row == x.groups && (int64_t)(index + 1) * kElements <= x.n) {
         // Within a tensor of one row: no ends to look at, addresses that differ by the lane
-        // alone.  Streamed past the caches (bf16 with 8-bit states, 37.7 million elements: 68 us,
-        // 77 without; stores alone 76, and 76 with next to no arithmetic).
+        // alone.  Streamed past the caches: bf16 with 8-bit states, 100.7 million elements 168 us,
+        // 6.0 TB/s, 192 with cached stores, 215 with cached loads too (and then as long with next
+        // to no arithmetic); f32, 16.8 million 78 us, 6.0 TB/s, 85 with cached stores.
         const int64_t base = (int64_t)index * kElements;
         const T *g = (const T *)x.g + base;
         T *p = (T *)x.p + base;
@@ -328,6 +329,10 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
                 l.v_scale = vs[i / kAdamBlock];
             }
         };
+        const auto stream = [](auto *to, auto v) {
+            typedef typename Packed<typename std::remove_pointer<decltype(to)>::type, E>::mem mem;
+            __builtin_nontemporal_store((mem)v, (mem *)to);
+        };
         Mine ls[kPasses];
 #pragma unroll
         for (int u = 0; u < kPasses; ++u) load(ls[u], u);
@@ -338,11 +343,11 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
             Mine &l = ls[u];
             const uint32_t i = (u * 256 + threadIdx.x) * E;
             l.step(rates, 32);
-            __builtin_nontemporal_store((typename Packed<S, E>::mem)l.m, (typename Packed<S, E>::mem *)(m + i));
-            __builtin_nontemporal_store((typename Packed<S, E>::mem)l.v, (typename Packed<S, E>::mem *)(v + i));
-            __builtin_nontemporal_store((typename Packed<P, E>::mem)l.p, (typename Packed<P, E>::mem *)(q + i));
+            stream(m + i, l.m);
+            stream(v + i, l.v);
+            stream(q + i, l.p);
             if constexpr (MASTER)
-                __builtin_nontemporal_store((typename Packed<T, E>::mem)l.rounded(), (typename Packed<T, E>::mem *)(p + i));
+                stream(p + i, l.rounded());
             if constexpr (BITS == 8)
                 if (threadIdx.x % 32 == 0) {
                     ms[i / kAdamBlock] = l.m_scale;
@@ -409,10 +414,12 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
                 settle_row<E, S>(l.v, col, x.n);
             }
             l.step(rates, 1 << shift);
+            // (rows rarely start with a cache line: stores of parts of one are put together in the
+            // cache, 37.5 us of 4096 rows of 1830, 40.7 past it)
             const auto store = [&](auto *to, auto v) {
                 if constexpr (END == OVERLAP) {
                     typedef typename Packed<typename std::remove_pointer<decltype(to)>::type, E>::mem mem;
-                    if (n > 0) __builtin_nontemporal_store((mem)v, (mem *)to);
+                    if (n > 0) *(mem *)to = v;
                 } else put<E>(to, n, v);
             };
             store((S *)x.m + os + col, l.m);
