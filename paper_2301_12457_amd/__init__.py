@@ -600,6 +600,10 @@ def _given(**tensors):
             raise EvoxError(EINVAL, f"{what} is required")
 
 
+def _is_table(t, dtype, shape, dev):
+    return t.dtype is _DTYPES[dtype] and t.shape == shape and t.get_device() == dev and t.is_contiguous()
+
+
 def _choice(logits, ids, over):
     if logits.dim() != 2 or ids.dim() != 2:
         raise EvoxError(EINVAL, "logits must be [T, G], ids [T, k]")
@@ -610,7 +614,8 @@ def _choice(logits, ids, over):
 def evox_gate(logits, ids, w, over=GATE_CHOSEN, stream=None):
     """ids (int32 [T, k]) and weights w (float32 [T, k]) of the k largest of every row of
     logits [T, G], in descending order: a softmax over the chosen, or over all (GATE_ALL)."""
-    _given(logits=logits, ids=ids, w=w)
+    if logits is None or ids is None or w is None:
+        _given(logits=logits, ids=ids, w=w)
     p = _choice(logits, ids, over)
     shape = (p.T, p.k)
     rc = lib().evox_gate(ctypes.byref(p), logits.data_ptr(), _table("ids", ids, _INT, shape, logits),
@@ -623,7 +628,8 @@ def evox_gate(logits, ids, w, over=GATE_CHOSEN, stream=None):
 def evox_gate_grad(logits, ids, w, dw, dz, over=GATE_CHOSEN, stream=None):
     """The gradient dz [T, G] of evox_gate's logits from dw (float32 [T, k]), with the
     ids and w that it gave."""
-    _given(logits=logits, ids=ids, w=w, dw=dw, dz=dz)
+    if logits is None or ids is None or w is None or dw is None or dz is None:
+        _given(logits=logits, ids=ids, w=w, dw=dw, dz=dz)
     p = _choice(logits, ids, over)
     dz_at = _view("dz", dz, logits, logits.shape)
     p.lddz = _pitch(dz)
@@ -657,12 +663,15 @@ def evox_route(ids, off, pos, src=None, scratch=None, stream=None):
     """The slots (row, choice) of ids (int32 [T, k]) sorted by network: network g has the
     rows off[g] .. off[g + 1) (int32 [G + 1]); pos (int32 [T, k]) receives every slot's
     row, -1 for ids outside 0 .. G - 1, src (int32 [T k]) every row's slot t k + j."""
-    _given(ids=ids, off=off, pos=pos)
+    if ids is None or off is None or pos is None:
+        _given(ids=ids, off=off, pos=pos)
     p = _route(ids, off)
-    shape = tuple(ids.shape)
+    shape = ids.shape
     ids_at, off_at = _table("ids", ids, _INT, shape, ids), _vector("off", off, _INT, p.G + 1, ids)
     pos_at, src_at = _table("pos", pos, _INT, shape, ids), _vector("src", src, _INT, p.T * p.k, ids)
-    scratch, nbytes = _scratch(lib().evox_route_scratch_bytes(ctypes.byref(p)), ids, scratch, stream)
+    # (the size of a scratch that the caller has is the call's own to check)
+    scratch, nbytes = _scratch(1 if scratch is not None else lib().evox_route_scratch_bytes(ctypes.byref(p)), ids, scratch,
+                               stream)
     rc = lib().evox_route(ctypes.byref(p), ids_at, off_at, pos_at, src_at, scratch.data_ptr(), nbytes,
                           _raw_stream(stream, ids))
     if rc != OK:
@@ -670,23 +679,33 @@ def evox_route(ids, off, pos, src=None, scratch=None, stream=None):
     return off, pos, src
 
 
-def _slots(rows, xs, pos, w):
-    """Slots of pos [T, k] between rows [T, D] and xs [M, D] (or None), pos' and w's addresses."""
+def _slots(what, rows, xs, pos, w):
+    """Slots of pos [T, k] between rows [T, D] and xs [M, D] (or None), with the pitch of the
+    rows as ldx, and pos' and w's addresses."""
+    # one pass for what most calls are; anything else is checked and named below
+    d, dev = _dtype(rows), rows.get_device()
+    if xs is not None and rows.dim() == 2 and xs.dim() == 2 and pos.dim() == 2:
+        (T, D), (M, n), (t, k), rt, st = rows.shape, xs.shape, pos.shape, rows.stride(), xs.stride()
+        if (n == D and t == T and rt[1] == 1 and st[1] == 1 and xs.dtype is rows.dtype and xs.get_device() == dev
+                and _is_table(pos, _INT, (T, k), dev) and (w is None or _is_table(w, _FLOAT, (T, k), dev))):
+            return (Slots(d, T, k, 0, M, D, rt[0] if T > 1 else D, 0, st[0] if M > 1 else D, 0), pos.data_ptr(),
+                    None if w is None else w.data_ptr())
     if rows.dim() != 2 or pos.dim() != 2 or xs is not None and xs.dim() != 2:
         raise EvoxError(EINVAL, "rows must be [T, D], xs [M, D], pos [T, k]")
-    (T, D), d, shape = rows.shape, _dtype(rows), (rows.shape[0], pos.shape[1])
+    (T, D), shape = rows.shape, (rows.shape[0], pos.shape[1])
     if xs is not None:
         _view("xs", xs, rows, (xs.shape[0], D))
-    return (Slots(d, T, pos.shape[1], 0, 0 if xs is None else xs.shape[0], D, 0, 0, 0 if xs is None else _pitch(xs), 0),
+    pitch = _pitch(xs) if xs is not None else 0
+    return (Slots(d, T, pos.shape[1], 0, 0 if xs is None else xs.shape[0], D, _dense(what, rows), 0, pitch, 0),
             _table("pos", pos, _INT, shape, rows), _table("w", w, _FLOAT, shape, rows))
 
 
 def evox_dispatch(x, pos, xs, w=None, stream=None):
     """xs[pos[t, j]] = w[t, j] x[t] (x[t] itself without w) for the rows of x [T, D]: the
     rows xs [M, D] in the networks' grouping."""
-    _given(x=x, pos=pos, xs=xs)
-    p, pos_at, w_at = _slots(x, xs, pos, w)
-    p.ldx = _dense("x", x)
+    if x is None or pos is None or xs is None:
+        _given(x=x, pos=pos, xs=xs)
+    p, pos_at, w_at = _slots("x", x, xs, pos, w)
     rc = lib().evox_dispatch(ctypes.byref(p), x.data_ptr(), pos_at, w_at, xs.data_ptr(), _raw_stream(stream, x))
     if rc != OK:
         _check(rc)
@@ -695,11 +714,12 @@ def evox_dispatch(x, pos, xs, w=None, stream=None):
 
 def evox_combine(xs, pos, y, w=None, r=None, stream=None):
     """y[t] = sum_j w[t, j] xs[pos[t, j]] + r[t] for the rows of y [T, D] (w None: 1)."""
-    _given(xs=xs, pos=pos, y=y)
-    p, pos_at, w_at = _slots(y, xs, pos, w)
-    p.ldy = _dense("y", y)
-    r_at = _view("r", r, y, y.shape)
+    if xs is None or pos is None or y is None:
+        _given(xs=xs, pos=pos, y=y)
+    p, pos_at, w_at = _slots("y", y, xs, pos, w)
+    p.ldy, r_at = p.ldx, None
     if r is not None:
+        r_at = _view("r", r, y, y.shape)
         p.ldx = _pitch(r)
     rc = lib().evox_combine(ctypes.byref(p), xs.data_ptr(), pos_at, w_at, r_at, y.data_ptr(), _raw_stream(stream, y))
     if rc != OK:
@@ -710,19 +730,19 @@ def evox_combine(xs, pos, y, w=None, r=None, stream=None):
 def evox_combine_grad(xs, pos, dy, w=None, dxs=None, dw=None, stream=None):
     """The gradient of evox_combine from dy [T, D], each where given: dxs[pos[t, j]] =
     w[t, j] dy[t] [M, D] and dw (float32 [T, k]), for which alone xs is read."""
-    _given(pos=pos, dy=dy)
-    if dw is not None:
-        _given(xs=xs)
-    p, pos_at, w_at = _slots(dy, xs, pos, w)
-    p.ldx = _dense("dy", dy)
+    if pos is None or dy is None or dw is not None and xs is None:
+        _given(pos=pos, dy=dy, xs=xs)
+    p, pos_at, w_at = _slots("dy", dy, xs, pos, w)
+    dxs_at = dw_at = None
     if dxs is not None:
         if dxs.dim() != 2:
             raise EvoxError(EINVAL, "dxs must be [M, D]")
-        _view("dxs", dxs, dy, (dxs.shape[0] if xs is None else p.M, p.D))
+        dxs_at = _view("dxs", dxs, dy, (dxs.shape[0] if xs is None else p.M, p.D))
         p.M, p.ldds = dxs.shape[0], _pitch(dxs)
+    if dw is not None:
+        dw_at = _table("dw", dw, _FLOAT, (p.T, p.k), dy)
     rc = lib().evox_combine_grad(ctypes.byref(p), None if xs is None else xs.data_ptr(), pos_at, w_at, dy.data_ptr(),
-                                 None if dxs is None else dxs.data_ptr(), _table("dw", dw, _FLOAT, (p.T, p.k), dy),
-                                 _raw_stream(stream, dy))
+                                 dxs_at, dw_at, _raw_stream(stream, dy))
     if rc != OK:
         _check(rc)
     return dxs, dw
