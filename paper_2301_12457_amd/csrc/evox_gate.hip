@@ -23,21 +23,22 @@ struct GateKey {
     static __device__ __forceinline__ void chunk(typename NetVec<T>::reg v, int column, uint32_t *key)
     {
         typedef short two __attribute__((ext_vector_type(2)));
+        typedef unsigned short utwo __attribute__((ext_vector_type(2)));
         const uint4 w = __builtin_bit_cast(uint4, v);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-        uint32_t most = 0;
+        utwo most = 0;
+        const uint32_t below = (0xffffu - (uint32_t)column) * 0x10001u - 0x10000u;  // of both columns of the first pair
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const two sign = __builtin_bit_cast(two, u[i]) >> 15;
-            const uint32_t s = __builtin_bit_cast(uint32_t, sign);
-            const two a = __builtin_bit_cast(two, u[i] & 0x7fff7fffu);
-            const two o = __builtin_bit_cast(two, __builtin_bit_cast(uint32_t, a) ^ s) - sign;
-            const uint32_t order = __builtin_bit_cast(uint32_t, o) ^ 0x80008000u, below = 0xffffu - (uint32_t)column - 2 * i;
-            key[2 * i] = (order << 16) + below;
-            key[2 * i + 1] = (order & 0xffff0000u) | (below - 1);
-            most = max(most, max(u[i] & 0x7fffu, u[i] >> 16 & 0x7fffu));
+            const uint32_t s = __builtin_bit_cast(uint32_t, sign), a = u[i] & 0x7fff7fffu;
+            const two o = __builtin_bit_cast(two, a ^ s) - sign;
+            const uint32_t order = __builtin_bit_cast(uint32_t, o) ^ 0x80008000u, c = below - 0x20002u * i;
+            key[2 * i] = __builtin_amdgcn_perm(order, c, 0x05040100u);
+            key[2 * i + 1] = __builtin_amdgcn_perm(order, c, 0x07060302u);
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(utwo, a));
         }
-        if (most > kInf)  // a NaN
+        if (max(most[0], most[1]) > kInf)  // a NaN
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if ((u[j / 2] >> j % 2 * 16 & 0x7fffu) > kInf) key[j] = 0xffff0000u | (0xffffu - (uint32_t)column - j);
@@ -103,6 +104,19 @@ __device__ __forceinline__ void load_row(const T *z, int lane, int L, int G, boo
         for (int j = 0; j < N; ++j) v[i][j] = (lane + i * L) * N + j < G ? z[j] : (T)-INFINITY;
 }
 
+// f(g) with g(z) = e^(z - top) times a factor that all of a row's have.  16 bits: 2^(z log2 e
+// - c), c the rounded top log2 e, in one multiply-add (what c is off by is the factor); of
+// tops where that would be more than e^0.04, and of fp32, the difference first, factor 1.
+template <typename T, typename F>
+__device__ __forceinline__ void with_exp(float top, F &&f)
+{
+    if constexpr (sizeof(T) == 2) {
+        const float c = top * 1.44269504f;
+        if (__all(fabsf(top) < 0x1p19f)) f([=](float z) { return __builtin_amdgcn_exp2f(fmaf(z, 1.44269504f, -c)); });
+        else f([=](float z) { return exp_fast(z - top); });
+    } else f([=](float z) { return exp_near(z - top); });
+}
+
 // Over the block of a wide row: the waves meet in LDS (two places in turn, so that one
 // barrier is enough).
 template <typename V, typename F>
@@ -137,8 +151,20 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L, b
     Key key[NIT][N];
 #pragma unroll
     for (int i = 0; i < NIT; ++i) GateKey<T>::chunk(v[i], (lane + i * L) * N, key[i]);
-    Key K = 0, mine = 0, first = 0;
-    for (int r = 0; r < a.k; ++r) {
+    const auto row_max = [&](Key d, int r) {
+        d = lanes_max(d, WIDE ? 64 : L);
+        if constexpr (WIDE) d = block_all(d, lds_key[r & 1], [](Key x, Key y) { return x > y ? x : y; });
+        return d;
+    };
+    Key K = 0;
+#pragma unroll
+    for (int i = 0; i < NIT; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) K = key[i][j] > K ? key[i][j] : K;
+    K = row_max(K, 0);
+    const Key first = K;
+    Key mine = lane == 0 ? K : 0;
+    for (int r = 1; r < a.k; ++r) {
         Key d = 0;
 #pragma unroll
         for (int i = 0; i < NIT; ++i)
@@ -147,26 +173,23 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L, b
                 const Key e = key[i][j] - K;
                 d = e > d ? e : d;
             }
-        d = lanes_max(d, WIDE ? 64 : L);
-        if constexpr (WIDE) d = block_all(d, lds_key[r & 1], [](Key x, Key y) { return x > y ? x : y; });
-        K += d;
-        if (r == 0) first = K;
+        K += row_max(d, r);
         if (lane == r) mine = K;
     }
     const bool there = mine > GateKey<T>::kNone;
     const float top = first > GateKey<T>::kNone ? GateKey<T>::value(first) : 0.0f;
-    const float e = there ? exp_near(GateKey<T>::value(mine) - top) : 0.0f;
-    float s = lane < a.k ? e : 0.0f;
-    if (a.over == GATE_ALL) {
-        s = 0.0f;
+    float e, s;
+    with_exp<T>(top, [&](auto above) {
+        e = there ? above(GateKey<T>::value(mine)) : 0.0f;
+        s = lane < a.k ? e : 0.0f;
+        if (a.over == GATE_ALL) {
+            s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NIT; ++i)
+            for (int i = 0; i < NIT; ++i)
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float x = (float)v[i][j] - top;
-                s += sizeof(T) == 2 ? exp_fast(x) : exp_near(x);
-            }
-    }
+                for (int j = 0; j < N; ++j) s += above((float)v[i][j]);
+        }
+    });
     s = lanes_sum(s, WIDE ? 64 : L);
     if constexpr (WIDE) s = block_all(s, lds_sum, [](float x, float y) { return x + y; });
     if (t < a.T && lane < a.k) {
