@@ -3,23 +3,26 @@
 //
 // A counting sort.  A wave takes 64 slots at a time, in order: the lanes with the same
 // digit are found with a ballot per bit, a slot's rank is the wave's count of its digit
-// so far plus the lanes before it, and no atomic decides an order.  Up to 4096 slots are
+// so far plus the lanes before it, and no atomic decides an order.  Up to 2048 slots are
 // one block's; more are counted per tile of as many and placed by a second launch, which
 // adds up the tiles' counts itself while they are few, else from a third one between.  Up
 // to 2048 networks are one digit, more two digits, the lower first.
 //
-// Bound by latency: few blocks, and in each a chain of loads, ranks and LDS sums.  So a
-// tile is 16 waves' of four rounds where the digits are few (LDS holds a count per wave and
-// digit) and the slots enough (20,014 slots of 100 networks: %PLACE%),
-// all rounds' ballots come before the first round's counts, and all loads before both.
+// Bound by latency: few blocks, and in each a chain of loads, ranks, LDS sums and scattered
+// stores (20,014 slots of 100 networks: 3.8 us to count and 7.2 to place, of which loads
+// and earlier tiles' counts 3, ranks 2, the digits' places 1, stores 1.5).  So a tile is 8
+// waves' of four rounds where the digits are few (LDS holds a count per wave and digit) and
+// the slots enough: 16 waves' of 4096 slots 8.4 us, 4 waves' of 1024 7.0, but 11.8 against
+// 7.9 of 262,144 slots, where each tile adds up four times as many counts; all ballots come
+// before the first count, and all loads before both.
 #include "evox_mix.hpp"
 
 namespace evox {
 
 namespace {
 
-constexpr int kTile = 4096, kMaxBins = 2048;
-constexpr int kWideBins = 512, kWideSlots = 1024;  // digits at most, and slots above which, for 16 waves
+constexpr int kTile = 2048, kMaxBins = 2048;
+constexpr int kWideBins = 512, kWideSlots = 1024;  // digits at most, and slots above which, for 8 waves
 constexpr int kSummed = 16384;                     // counts of all tiles that each block adds up itself
 
 struct Pass {
@@ -62,7 +65,7 @@ template <int W>
 __global__ __launch_bounds__(64 * W) void k_route_count(Pass p)
 {
     constexpr int threads = 64 * W, rounds = kTile / threads;
-    __shared__ int hist[W == 16 ? kWideBins : kMaxBins];
+    __shared__ int hist[W == 8 ? kWideBins : kMaxBins];
     for (int b = threadIdx.x; b < p.bins; b += threads) hist[b] = 0;
     const int64_t n = pass_size(p), base = (int64_t)blockIdx.x * kTile;
     int key[rounds];
@@ -286,7 +289,7 @@ void run(const Pass &p, hipStream_t s)
 }
 hipError_t run(const Pass &p, hipStream_t s)
 {
-    if (p.bins <= kWideBins && p.n > kWideSlots) run<16>(p, s);
+    if (p.bins <= kWideBins && p.n > kWideSlots) run<8>(p, s);
     else run<4>(p, s);
     return hipGetLastError();
 }
