@@ -735,8 +735,8 @@ int evox_combine_grad(const evox_slots *slots, const void *xs, const int32_t *po
  * with one fp32 scale for each 256 elements of a row (a row's last ones may be
  * fewer), the largest |m| / 448, and of v the root is held so; a root above 0 is at
  * least the least e4m3 number.  |m| whose group is all below 2^-100 counts as 0.  The step
- * is made from the new moments before they are rounded.  An infinity or NaN among a
- * group's moments makes the group's scale NaN: its states are lost, not its parameters.
+ * is made from the new moments before they are rounded.  An infinity or NaN stays its own
+ * element's, of 8 bits as NaN.
  * ------------------------------------------------------------------------- */
 #define EVOX_ADAM_BLOCK 256
 #define EVOX_ADAM_CLOCK 528

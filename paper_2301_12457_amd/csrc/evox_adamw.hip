@@ -151,22 +151,26 @@ __device__ __forceinline__ void from8(Bytes8 bytes, float scale, float *v)
         v[4 * i + 3] = hi[1] * scale;
     }
 }
-// The group's scale, and its numbers by it.  What is below 2^-100 counts as 0;
-// an infinity or NaN makes the scale NaN, and with it all that the group stands for (its
-// numbers are then 0).  L: lanes of the group.
-__device__ __forceinline__ float scale8(const float *v, int L, float *ratio)
+// The group's scale, and its numbers by it.  What is below 2^-100 counts as 0; infinities
+// and NaN count for nothing in it (*odd: some lane of the wave has one) and are held as NaN.
+// L: lanes of the group.
+__device__ __forceinline__ float scale8(const float *v, int L, float *ratio, bool *odd)
 {
     float most = 0.0f;  // NaN if one is
 #pragma unroll
     for (int e = 0; e < 8; ++e) most = __builtin_elementwise_maximum(most, fabsf(v[e]));
-    // (as integers: NaN is above all)
-    const float m = __uint_as_float(lanes_max(__float_as_uint(most) & 0x7fffffffu, L));
-    const bool finite = m < INFINITY;
-    *ratio = !finite ? -1.0f : m > 0x1p-100f ? 448.0f * __builtin_amdgcn_rcpf(m) : 0.0f;
-    return finite ? m * (1.0f / 448.0f) : __builtin_nanf("");
+    *odd = __any(!(most < INFINITY));
+    if (*odd) {
+        most = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fabsf(v[e]) < INFINITY ? fmaxf(most, fabsf(v[e])) : most;
+    }
+    const float m = __uint_as_float(lanes_max(__float_as_uint(most), L));
+    *ratio = m > 0x1p-100f ? 448.0f * __builtin_amdgcn_rcpf(m) : 0.0f;
+    return m * (1.0f / 448.0f);
 }
 template <bool ROOT>
-__device__ __forceinline__ Bytes8 to8(const float *v, float ratio)
+__device__ __forceinline__ Bytes8 to8(const float *v, float ratio, bool odd)
 {
     float q[8], least = 1.0f;
 #pragma unroll
@@ -177,12 +181,14 @@ __device__ __forceinline__ Bytes8 to8(const float *v, float ratio)
     if (ROOT && least < 0x1p-9f)
 #pragma unroll
         for (int e = 0; e < 8; ++e) q[e] = v[e] > 0.0f ? fmaxf(q[e], 0x1p-9f) : q[e];
+    if (odd)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = fabsf(v[e]) < INFINITY ? q[e] : __builtin_nanf("");
     uint32_t b[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i], q[4 * i + 1], 0, false);
         b[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i + 2], q[4 * i + 3], w, true);
-        if (ratio < 0.0f) b[i] = 0;
     }
     return __builtin_bit_cast(Bytes8, make_uint2(b[0], b[1]));
 }
@@ -229,10 +235,11 @@ struct Lane {
         }
         if constexpr (BITS == 8) {
             float mr, vr;
-            m_scale = scale8(m1, L, &mr);
-            v_scale = scale8(r, L, &vr);
-            m = to8<false>(m1, mr);
-            v = to8<true>(r, vr);
+            bool mo, vo;
+            m_scale = scale8(m1, L, &mr, &mo);
+            v_scale = scale8(r, L, &vr, &vo);
+            m = to8<false>(m1, mr, mo);
+            v = to8<true>(r, vr, vo);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) {

@@ -189,24 +189,35 @@ def test_rate_as_number_and_on_the_device_and_many_steps(evox_gpu):
         assert ((q.double().cpu() - want).abs() <= 4 * U32 * p.abs().double().cpu() + rate * 40 * U32 * mag).all()
 
 
+@pytest.mark.parametrize("n", [1024, 1021, 5])
 @pytest.mark.parametrize("bits", [32, 8])
-def test_infinities_and_nan(evox_gpu, bits):
-    """Of 32 bits they stay in their own numbers; of 8 bits the group of 256 loses its
-    states, its parameters are the ones that the new moments give."""
-    p, g = torch.ones(1024, device="cuda"), torch.ones(1024, device="cuda")
-    g[3], g[300], g[600:700] = math.nan, math.inf, 0.0
-    opt = evox_gpu.AdamW([p], [g], bits=bits)
-    opt.step()
-    bad = torch.zeros(1024, dtype=torch.bool, device="cuda")
-    bad[3] = bad[300] = True
-    assert torch.equal(p.isnan(), bad)
-    if bits == 32:
-        assert opt.state["m"].isnan().nonzero().flatten().tolist() == [3]
-        assert opt.state["m"][300] == math.inf and opt.state["v"][300] == math.inf
-    else:
-        assert opt.state["m_scale"].isnan().tolist() == [True, True, False, False]
-        assert opt.state["v_scale"].isnan().tolist() == [True, True, False, False]
-        assert torch.isfinite(opt.state["m"].float()).all()
+def test_infinities_and_nan(evox_gpu, bits, n):
+    """They stay in their own elements, step after step; the others are as without them."""
+    torch.manual_seed(1)
+    start, g = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    odd = torch.zeros(n, dtype=torch.bool, device="cuda")
+    odd[[3] if n < 300 else [3, 300]] = True
+    g[600:700] = 0.0
+    runs = []
+    for bad in (False, True):
+        p, d = start.clone(), g.clone()
+        d[odd] = 0.0  # (without them: nothing in these elements)
+        if bad:
+            d[3] = math.nan
+            if n > 300:
+                d[300] = math.inf
+        opt = evox_gpu.AdamW([p], [d], bits=bits)
+        opt.step()
+        d.masked_fill_(odd, 0.0)  # one such gradient, then none
+        opt.step()
+        runs.append((p, opt.state))
+    (p, a), (q, b) = runs
+    assert torch.equal(q.isnan(), odd) and torch.equal(p[~odd], q[~odd])
+    for name in "mv":
+        x, y = a[name].float(), b[name].float()
+        assert torch.equal(x[~odd], y[~odd]) and not torch.isfinite(y[odd]).any()
+        if bits == 8:
+            assert torch.equal(a[name + "_scale"], b[name + "_scale"])
 
 
 def test_8_bits_hold_every_e4m3_number(evox_gpu):
@@ -240,3 +251,34 @@ def test_load(evox_gpu, bits):
         b.load({"t": a.state["t"]})
     with pytest.raises(evox.EvoxError):
         b.load(dict(a.state, m=a.state["m"][:5]))
+
+
+def test_offsets_beyond_32_bits(evox_gpu):
+    """More than 2^31 elements, in bytes beyond 2^32: the last ones are where they belong."""
+    n = (1 << 31) + 4099
+    p = torch.full((n,), 1.0, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 5000, (1 << 31) - 1, 1 << 31, n - 4097, n - 260, n - 3, n - 1], device="cuda")
+    g[at] = 2.0
+    opt = evox_gpu.AdamW([p], [g], lr=0.25, weight_decay=0.0, bits=8)
+    opt.step()
+    assert (p[at] == 0.75).all() and int((p != 1.0).sum()) == len(at)
+    assert int((opt.state["m"].view(torch.uint8) != 0).sum()) == len(at)
+    held = opt.state["m"][at].float() * opt.state["m_scale"][at // 256]
+    assert ((held - 0.2).abs() <= 0.2 * 2.0 ** -4).all()
+
+
+def test_rates_of_zero_and_below(evox_gpu):
+    """A rate of 0 leaves the parameters and moves the states; a negative one ascends."""
+    p, g = torch.randn(700, device="cuda"), torch.randn(700, device="cuda")
+    g[:100] = 0.0
+    for bits in (32, 8):
+        q = p.clone()
+        opt = evox_gpu.AdamW([q], [g], lr=0.0, bits=bits)
+        opt.step()
+        assert torch.equal(q, p) and opt.state["t"].item() == 1 and (opt.state["m"].float() != 0).any()
+        up, down = p.clone(), p.clone()
+        for t, lr in ((up, -1e-2), (down, 1e-2)):
+            evox_gpu.AdamW([t], [g], lr=lr, weight_decay=0.0, bits=bits).step()
+        # (two roundings of p each)
+        assert ((up + down - 2 * p).abs() <= 8 * U32 * (p.abs() + 1)).all() and ((up - p) * g >= 0).all()

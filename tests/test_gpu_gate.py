@@ -181,3 +181,18 @@ def test_empty_and_inputs_kept(evox_gpu):
     keep = z.clone()
     a, b = run(evox_gpu, z, 3, "all"), run(evox_gpu, z, 3, "all")
     assert torch.equal(z, keep) and torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_offsets_beyond_32_bits(evox_gpu, dtype):
+    T, G, pitch = 70_000, 24, 65_536
+    big = torch.empty(T * pitch, dtype=dtype, device="cuda").view(T, pitch)
+    z = big[:, 100:100 + G]
+    z.copy_(logits(T, G, dtype, 1))
+    ids, w = run(evox_gpu, z, 3, "all")
+    near = run(evox_gpu, z.contiguous(), 3, "all")
+    assert torch.equal(ids, near[0]) and torch.equal(w, near[1])
+    dw, want = torch.ones_like(w).cumsum(1), torch.empty(T, G, dtype=dtype, device="cuda")
+    evox_gpu.evox_gate_grad(z.contiguous(), ids, w, dw, want, over=1)
+    evox_gpu.evox_gate_grad(z, ids, w, dw, big[:, 30_000:30_000 + G], over=1)
+    assert torch.equal(big[:, 30_000:30_000 + G], want)
