@@ -166,7 +166,7 @@ __device__ __forceinline__ float scale8(const float *v, int L, float *ratio, boo
         for (int e = 0; e < 8; ++e) most = fabsf(v[e]) < INFINITY ? fmaxf(most, fabsf(v[e])) : most;
     }
     const float m = __uint_as_float(lanes_max(__float_as_uint(most), L));
-    *ratio = m > 0x1p-100f ? 448.0f * __builtin_amdgcn_rcpf(m) : 0.0f;
+    *ratio = m > 0x1p-100f ? 448.0f / m : 0.0f;  // (rounded once: its error is all of the group's)
     return m * (1.0f / 448.0f);
 }
 template <bool ROOT>
