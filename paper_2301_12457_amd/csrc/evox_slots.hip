@@ -11,19 +11,38 @@ namespace evox {
 
 namespace {
 
-// load_early past the caches: the networks' rows are read once (bf16 combine of 262,144 rows
-// of 2048 225 us without, 212; f16 gradient of 65,536 rows of 4096 246, 223).
-template <typename T>
-__device__ __forceinline__ typename NetVec<T>::reg load_stream(const T *row, int c, int n)
+// How a row lies over lanes: TINY, one lane's and shorter than its 16 bytes; SOME lanes of a
+// wave; WAVES, whole ones (the row is then the same in all lanes of a wave, and so are its
+// slots).
+enum Spread { TINY = 0, SOME = 1, WAVES = 2 };
+
+// Chunk c of a row of n; the last one is the row's last N elements, of which the chunk before has
+// some too: two lanes store the same there, and loads and stores need no branch.  NT: past
+// the caches; the networks' rows are read once (bf16 combine of 262,144 rows of 2048 225 us
+// without, 212; f16 gradient of 65,536 rows of 4096 246, 223).
+template <int SPREAD, bool NT, typename T>
+__device__ __forceinline__ typename NetVec<T>::reg chunk_of(const T *row, int c, int n)
 {
     constexpr int N = NetVec<T>::N;
-    if (n < N) return load_chunk(row, c, n, (T)0.0f);
-    return __builtin_nontemporal_load(reinterpret_cast<const typename NetVec<T>::mem *>(row + min(c * N, n - N)));
+    typedef typename NetVec<T>::mem mem;
+    if constexpr (SPREAD == TINY) return load_chunk(row, c, n, (T)0.0f);
+    const mem *p = reinterpret_cast<const mem *>(row + min(c * N, n - N));
+    if constexpr (NT) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <int SPREAD, bool NT, typename T>
+__device__ __forceinline__ void put_chunk(T *row, int c, int n, typename NetVec<T>::reg v)
+{
+    constexpr int N = NetVec<T>::N;
+    typedef typename NetVec<T>::mem mem;
+    if constexpr (SPREAD == TINY) return store_chunk(row, c, n, v);
+    mem *p = reinterpret_cast<mem *>(row + min(c * N, n - N));
+    if constexpr (NT) __builtin_nontemporal_store((mem)v, p);
+    else *p = v;
 }
 
-// K slots of row t from j0 on: their rows, -1 where there is none, and weights.  UNI: t is
-// the same in all lanes of the wave (rows of a wave and more), and so is all of this.
-template <int K, bool UNI>
+// K slots of row t from j0 on: their rows, -1 where there is none, and weights.
+template <int K, int SPREAD>
 struct Places {
     int32_t m[K];
     float w[K];
@@ -38,7 +57,7 @@ struct Places {
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             if (m[j] >= a.M) m[j] = -1;
-            if constexpr (UNI) {
+            if constexpr (SPREAD == WAVES) {
                 m[j] = __builtin_amdgcn_readfirstlane(m[j]);
                 w[j] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(w[j])));
             }
@@ -47,25 +66,32 @@ struct Places {
 };
 
 // The row of this lane's group of L, over 256 threads per block.
-template <bool UNI>
+template <int SPREAD>
 __device__ __forceinline__ int64_t row_of(int L)
 {
     const int in_block = threadIdx.x / L;
-    return net_block() * (256 / L) + (UNI ? __builtin_amdgcn_readfirstlane(in_block) : in_block);
+    return net_block() * (256 / L) + (SPREAD == WAVES ? __builtin_amdgcn_readfirstlane(in_block) : in_block);
 }
 
-template <typename T, int K, bool UNI>
+// Stores to eight rows at a time go faster from fewer blocks at once, 32 KB of LDS that nothing
+// uses for each (five per CU): bf16 262,144 rows of 2048 238 us, 248 from eight; from two
+// 310, from blocks that go on from row to row 240 (1280) to 298 (768).  Fewer rows at a time do
+// not care (f32 k 2: 29.7 and 28.9, with the sort).  The stores bound it: in the rows' own
+// order 204 us, in the sorted one 225, by chance 234; the floor is 186.
+constexpr int kFewBlocksLds = 32768;
+
+template <typename T, int K, int SPREAD>
 __global__ __launch_bounds__(256) void k_dispatch(SlotArgs a, int L)
 {
     constexpr int N = NetVec<T>::N;
     const int lane = threadIdx.x & (L - 1), D = (int)a.D;
-    const int64_t t = row_of<UNI>(L);
+    const int64_t t = row_of<SPREAD>(L);
     if (t >= a.T) return;
     const T *x = (const T *)a.x + t * a.ldx;
     for (int j0 = 0; j0 < a.k; j0 += K) {
-        const Places<K, UNI> p(a, t, j0);
+        const Places<K, SPREAD> p(a, t, j0);
         for (int c = lane; c * N < D; c += L) {
-            const auto v = load_chunk(x, c, D, (T)0.0f);
+            const auto v = chunk_of<SPREAD, false>(x, c, D);
 #pragma unroll
             for (int j = 0; j < K; ++j) {
                 if (p.m[j] < 0) continue;
@@ -73,32 +99,32 @@ __global__ __launch_bounds__(256) void k_dispatch(SlotArgs a, int L)
                 if (a.w)
 #pragma unroll
                     for (int e = 0; e < N; ++e) o[e] = (T)(p.w[j] * (float)v[e]);
-                store_chunk<T, true>((T *)a.out + p.m[j] * a.ldo, c, D, o);
+                put_chunk<SPREAD, true>((T *)a.out + p.m[j] * a.ldo, c, D, o);
             }
         }
     }
 }
 
-template <typename T, int K, bool UNI>
+template <typename T, int K, int SPREAD>
 __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
 {
     constexpr int N = NetVec<T>::N;
     typedef typename NetVec<T>::reg reg;
     const int lane = threadIdx.x & (L - 1), D = (int)a.D;
-    const int64_t t = row_of<UNI>(L);
+    const int64_t t = row_of<SPREAD>(L);
     if (t >= a.T) return;
-    const Places<K, UNI> first(a, t, 0);
+    const Places<K, SPREAD> first(a, t, 0);
     for (int c = lane; c * N < D; c += L) {
         reg r;
-        if (a.x) r = load_early((const T *)a.x + t * a.ldx, c, D);
+        if (a.x) r = chunk_of<SPREAD, false>((const T *)a.x + t * a.ldx, c, D);
         float s[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) s[e] = 0.0f;
-        const auto add = [&](const Places<K, UNI> &p) {
+        const auto add = [&](const Places<K, SPREAD> &p) {
             reg v[K];
 #pragma unroll
             for (int j = 0; j < K; ++j)
-                if (p.m[j] >= 0) v[j] = load_stream((const T *)a.xs + p.m[j] * a.lds, c, D);
+                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, true>((const T *)a.xs + p.m[j] * a.lds, c, D);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < K; ++j)
@@ -107,58 +133,60 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
                     for (int e = 0; e < N; ++e) s[e] = fmaf(p.w[j], (float)v[j][e], s[e]);
         };
         add(first);
-        for (int j0 = K; j0 < a.k; j0 += K) add(Places<K, UNI>(a, t, j0));
+        for (int j0 = K; j0 < a.k; j0 += K) add(Places<K, SPREAD>(a, t, j0));
         if (a.x)
 #pragma unroll
             for (int e = 0; e < N; ++e) s[e] += (float)r[e];
         reg o;
 #pragma unroll
         for (int e = 0; e < N; ++e) o[e] = (T)s[e];
-        settle(o, c, D, (T)0.0f);  // (the row's last chunk was summed where it was loaded)
-        store_chunk((T *)a.y + t * a.ldy, c, D, o);
+        put_chunk<SPREAD, false>((T *)a.y + t * a.ldy, c, D, o);
     }
 }
 
 // A row lies over L lanes of a wave or, WIDE, over a block.
-template <typename T, int K, bool UNI, bool WIDE>
+template <typename T, int K, int SPREAD, bool WIDE>
 __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
 {
     constexpr int N = NetVec<T>::N;
     typedef typename NetVec<T>::reg reg;
     __shared__ float lds[2][4][K];
     const int lane = WIDE ? threadIdx.x : threadIdx.x & (L - 1), D = (int)a.D;
-    const int64_t t = WIDE ? net_block() : row_of<UNI>(L);
+    const int64_t t = WIDE ? net_block() : row_of<SPREAD>(L);
     if (WIDE && t >= a.T) return;
     const bool live = t < a.T;
     const T *dy = (const T *)a.x + t * a.ldx;
     int turn = 0;
     for (int j0 = 0; j0 < a.k; j0 += K, turn ^= 1) {
-        const Places<K, UNI> p(a, live ? t : 0, j0, live);
+        const Places<K, SPREAD> p(a, live ? t : 0, j0, live);
         float s[K];
 #pragma unroll
         for (int j = 0; j < K; ++j) s[j] = 0.0f;
         for (int c = lane; live && c * N < D; c += L) {
-            reg d = load_early(dy, c, D), v[K];
+            const reg d = chunk_of<SPREAD, false>(dy, c, D);
+            reg v[K];
             if (a.dw)
 #pragma unroll
                 for (int j = 0; j < K; ++j)
-                    if (p.m[j] >= 0) v[j] = load_stream((const T *)a.xs + p.m[j] * a.lds, c, D);
+                    if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, true>((const T *)a.xs + p.m[j] * a.lds, c, D);
             __builtin_amdgcn_sched_barrier(0);
-            settle(d, c, D, (T)0.0f);
+            // (of a last chunk, the elements that the one before it has are not this lane's to sum)
+            const int twice = SPREAD == TINY ? 0 : c * N + N - D;
+            float own[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) own[e] = e < twice ? 0.0f : (float)d[e];
 #pragma unroll
             for (int j = 0; j < K; ++j) {
                 if (p.m[j] < 0) continue;
-                if (a.dw) {
-                    settle(v[j], c, D, (T)0.0f);
+                if (a.dw)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) s[j] = fmaf((float)d[e], (float)v[j][e], s[j]);
-                }
+                    for (int e = 0; e < N; ++e) s[j] = e < twice ? s[j] : fmaf(own[e], (float)v[j][e], s[j]);
                 if (a.out) {
                     auto o = d;
                     if (a.w)
 #pragma unroll
                         for (int e = 0; e < N; ++e) o[e] = (T)(p.w[j] * (float)d[e]);
-                    store_chunk<T, true>((T *)a.out + p.m[j] * a.ldo, c, D, o);
+                    put_chunk<SPREAD, true>((T *)a.out + p.m[j] * a.ldo, c, D, o);
                 }
             }
         }
@@ -192,18 +220,19 @@ int row_lanes(int64_t D, int most)
 }
 dim3 row_grid(int64_t T, int L) { return net_grid((T + 256 / L - 1) / (256 / L)); }
 
-// f(integral K, bool UNI): slots at a time, by k, and whether a row takes whole waves.
-template <typename F>
-hipError_t with_slots(int k, int L, F &&f)
+// f(integral K, integral Spread): slots at a time, by k, and the row's lanes.
+template <typename T, typename F>
+hipError_t with_slots(const SlotArgs &a, int L, F &&f)
 {
-    const auto uni = [&](auto K) {
-        if (L >= 64) f(K, std::true_type{});
-        else f(K, std::false_type{});
+    const auto spread = [&](auto K) {
+        if (L >= 64) f(K, std::integral_constant<int, WAVES>{});
+        else if (a.D >= NetVec<T>::N) f(K, std::integral_constant<int, SOME>{});
+        else f(K, std::integral_constant<int, TINY>{});
     };
-    if (k == 1) uni(std::integral_constant<int, 1>{});
-    else if (k == 2) uni(std::integral_constant<int, 2>{});
-    else if (k <= 4) uni(std::integral_constant<int, 4>{});
-    else uni(std::integral_constant<int, 8>{});
+    if (a.k == 1) spread(std::integral_constant<int, 1>{});
+    else if (a.k == 2) spread(std::integral_constant<int, 2>{});
+    else if (a.k <= 4) spread(std::integral_constant<int, 4>{});
+    else spread(std::integral_constant<int, 8>{});
     return hipGetLastError();
 }
 
@@ -214,8 +243,9 @@ hipError_t launch_dispatch(const SlotArgs &a, hipStream_t s)
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
-        return with_slots(a.k, L, [&](auto K, auto uni) {
-            hipLaunchKernelGGL((k_dispatch<T, decltype(K)::value, decltype(uni)::value>), row_grid(a.T, L), dim3(256), 0, s, a, L);
+        return with_slots<T>(a, L, [&](auto K, auto spread) {
+            const int lds = decltype(K)::value == 8 && L == 256 ? kFewBlocksLds : 0;
+            hipLaunchKernelGGL((k_dispatch<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
         });
     });
 }
@@ -225,8 +255,8 @@ hipError_t launch_combine(const SlotArgs &a, hipStream_t s)
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
-        return with_slots(a.k, L, [&](auto K, auto uni) {
-            hipLaunchKernelGGL((k_combine<T, decltype(K)::value, decltype(uni)::value>), row_grid(a.T, L), dim3(256), 0, s, a, L);
+        return with_slots<T>(a, L, [&](auto K, auto spread) {
+            hipLaunchKernelGGL((k_combine<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), 0, s, a, L);
         });
     });
 }
@@ -236,11 +266,11 @@ hipError_t launch_combine_grad(const SlotArgs &a, hipStream_t s)
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
-        return with_slots(a.k, L, [&](auto K, auto uni) {
+        return with_slots<T>(a, L, [&](auto K, auto spread) {
             constexpr int k = decltype(K)::value;
-            constexpr bool u = decltype(uni)::value;
+            constexpr int u = decltype(spread)::value;
             if (L <= 64) hipLaunchKernelGGL((k_combine_grad<T, k, u, false>), row_grid(a.T, L), dim3(256), 0, s, a, L);
-            else if constexpr (u) hipLaunchKernelGGL((k_combine_grad<T, k, true, true>), net_grid(a.T), dim3(256), 0, s, a, 256);
+            else if constexpr (u == WAVES) hipLaunchKernelGGL((k_combine_grad<T, k, WAVES, true>), net_grid(a.T), dim3(256), 0, s, a, 256);
         });
     });
 }
