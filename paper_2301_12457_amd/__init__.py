@@ -737,8 +737,9 @@ def evox_combine_grad(xs, pos, dy, w=None, dxs=None, dw=None, stream=None):
     if dxs is not None:
         if dxs.dim() != 2:
             raise EvoxError(EINVAL, "dxs must be [M, D]")
-        dxs_at = _view("dxs", dxs, dy, (dxs.shape[0] if xs is None else p.M, p.D))
-        p.M, p.ldds = dxs.shape[0], _pitch(dxs)
+        M = dxs.shape[0]
+        dxs_at = _view("dxs", dxs, dy, (M if xs is None else p.M, p.D))
+        p.M, p.ldds = M, dxs.stride(0) if M > 1 else p.D
     if dw is not None:
         dw_at = _table("dw", dw, _FLOAT, (p.T, p.k), dy)
     rc = lib().evox_combine_grad(ctypes.byref(p), None if xs is None else xs.data_ptr(), pos_at, w_at, dy.data_ptr(),

@@ -19,7 +19,9 @@ enum Spread { TINY = 0, SOME = 1, WAVES = 2 };
 // Chunk c of a row of n; the last one is the row's last N elements, of which the chunk before has
 // some too: two lanes store the same there, and loads and stores need no branch.  NT: past
 // the caches; the networks' rows are read once (bf16 combine of 262,144 rows of 2048 225 us
-// without, 212; f16 gradient of 65,536 rows of 4096 246, 223).
+// without, 212; f16 gradient of 65,536 rows of 4096 246, 223), and stores of whole waves go
+// there too (dispatch 219, 232 through them; f32 20,014 rows of 1001 24, 29), those of
+// narrower rows do not (f16 562,000 rows of 40 54 us past them, 35 through).
 template <int SPREAD, bool NT, typename T>
 __device__ __forceinline__ typename NetVec<T>::reg chunk_of(const T *row, int c, int n)
 {
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(256) void k_dispatch(SlotArgs a, int L)
                 if (a.w)
 #pragma unroll
                     for (int e = 0; e < N; ++e) o[e] = (T)(p.w[j] * (float)v[e]);
-                put_chunk<SPREAD, true>((T *)a.out + p.m[j] * a.ldo, c, D, o);
+                put_chunk<SPREAD, SPREAD == WAVES>((T *)a.out + p.m[j] * a.ldo, c, D, o);
             }
         }
     }
@@ -186,7 +188,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
                     if (a.w)
 #pragma unroll
                         for (int e = 0; e < N; ++e) o[e] = (T)(p.w[j] * (float)d[e]);
-                    put_chunk<SPREAD, true>((T *)a.out + p.m[j] * a.ldo, c, D, o);
+                    put_chunk<SPREAD, SPREAD == WAVES>((T *)a.out + p.m[j] * a.ldo, c, D, o);
                 }
             }
         }
@@ -244,7 +246,7 @@ hipError_t launch_dispatch(const SlotArgs &a, hipStream_t s)
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
         return with_slots<T>(a, L, [&](auto K, auto spread) {
-            const int lds = decltype(K)::value == 8 && L == 256 ? kFewBlocksLds : 0;
+            const int lds = decltype(K)::value == 8 && L == 256 && a.T >= 8192 ? kFewBlocksLds : 0;
             hipLaunchKernelGGL((k_dispatch<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
         });
     });
