@@ -1,9 +1,12 @@
 // The gate of a mixture: the k largest logits of every row and their softmax weights,
 // and the logits' gradient from the weights'.
 //
-// A row lies over L lanes of a wave (a power of two, k at least, so that lane j keeps
-// the j-th choice) or, above 64 lanes' worth, over a block; each lane has NIT chunks of
-// 16 bytes.
+// Two ways to choose: k rounds over logits that lie in registers (a row over L lanes of a
+// wave, a power of two, k at least, so that lane j keeps the j-th choice; above 64 lanes'
+// worth over a block; each lane has NIT chunks of 16 bytes), or one pass over the row with
+// the best so far sorted over a wave's lanes.  Bound by instructions: bf16 65,536 x 256, k 8, weights
+// over all, 814 of a wave for eight rows, 13.9 us (floor 5.8); fp32 keys are of 64 bits.  The
+// gradient is bound by memory (f16 20,000 x 1001 17 us, 81 MB, floor 12.5).
 #include "evox_mix.hpp"
 
 namespace evox {
@@ -199,6 +202,145 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L, b
 }
 
 // ---------------------------------------------------------------------------
+// Many choices, or long rows: a wave takes a row in segments of 64 lanes' four chunks and
+// keeps the best so far sorted over its lanes.  What is above the k-th of them joins a list of
+// up to 64 in LDS (few do after the first segment: of N logits in any order about k ln N);
+// a full list is sorted over the lanes and its first 32 merged with the best (32 are k's
+// most).  Logits in ascending order, the worst, fill a list with every 64.  The softmax
+// over all runs along, each lane with its own maximum.
+// ---------------------------------------------------------------------------
+// The value of lane ^ M: neighbours and mirrors by DPP, rows and halves by gfx950's swaps.
+template <int M>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v)
+{
+    if constexpr (M == 1) return lane_dpp<0xB1>(v);
+    else if constexpr (M == 2) return lane_dpp<0x4E>(v);
+    else if constexpr (M == 3) return lane_dpp<0x1B>(v);
+    else if constexpr (M == 7) return lane_dpp<0x141>(v);
+    else if constexpr (M == 15) return lane_dpp<0x140>(v);
+    else if constexpr (M == 4) return lane_xor<3>(lane_xor<7>(v));
+    else if constexpr (M == 8) return lane_dpp<0x128>(v);
+    else if constexpr (M == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    } else if constexpr (M == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    } else if constexpr (M == 31) return lane_xor<16>(lane_xor<15>(v));
+    else return lane_xor<32>(lane_xor<31>(v));  // 63
+}
+template <int M>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v)
+{
+    return (uint64_t)lane_xor<M>((uint32_t)(v >> 32)) << 32 | lane_xor<M>((uint32_t)v);
+}
+// Of lanes l and l ^ M the larger to the one whose bit B is clear.
+template <int M, int B, typename Key>
+__device__ __forceinline__ Key exchange(Key v)
+{
+    const Key o = lane_xor<M>(v);
+    return (v > o) == !(threadIdx.x & B) ? v : o;
+}
+// Descending over 2 S lanes: of a bitonic sequence, and of any (S doubling; a mirror makes
+// two sorted halves bitonic).
+template <int S, typename Key>
+__device__ __forceinline__ Key merge_lanes(Key v)
+{
+    v = exchange<S, S>(v);
+    if constexpr (S > 1) v = merge_lanes<S / 2>(v);
+    return v;
+}
+template <int S, typename Key>
+__device__ __forceinline__ Key sort_lanes(Key v)
+{
+    if constexpr (S > 1) v = sort_lanes<S / 2>(v);
+    v = exchange<2 * S - 1, S>(v);
+    if constexpr (S > 1) v = merge_lanes<S / 2>(v);
+    return v;
+}
+__device__ __forceinline__ uint32_t lane_value(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int l)
+{
+    return (uint64_t)lane_value((uint32_t)(v >> 32), l) << 32 | lane_value((uint32_t)v, l);
+}
+
+constexpr int kStreamChunks = 4;  // per lane and segment
+template <typename T>
+__global__ __launch_bounds__(256) void k_gate_stream(GateArgs a)
+{
+    constexpr int N = NetVec<T>::N, C = kStreamChunks, kSegment = 64 * C * N;
+    typedef typename GateKey<T>::type Key;
+    __shared__ Key lists[4][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, G = a.G;
+    const int64_t t = net_block() * 4 + __builtin_amdgcn_readfirstlane(wave);
+    if (t >= a.T) return;  // the whole wave
+    const T *z = (const T *)a.z + t * a.ldz;
+    Key *list = lists[wave];
+    Key best = 0, bar = GateKey<T>::kNone;  // (lanes 0 .. 31), and what is not above it
+    int count = 0;
+    const auto flush = [&]() {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        Key v = lane < count ? list[lane] : 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        v = sort_lanes<32>(v);
+        v = lane_xor<31>(v);
+        best = merge_lanes<16>(v > best ? v : best);
+        const Key last = lane_value(best, a.k - 1);
+        bar = last > bar ? last : bar;
+        count = 0;
+    };
+    float run = -INFINITY, sum = 0.0f;
+    for (int base = 0; base < G; base += kSegment) {
+        typename NetVec<T>::reg v[C];
+        load_row<T, C>(z + base, lane, 64, G - base, G - base >= kSegment, v);
+        if (a.over == GATE_ALL) {
+            float top = run;
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) top = fmaxf(top, (float)v[i][j]);
+            const float from = top == -INFINITY ? 0.0f : top;  // (nothing yet: every term 0)
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float x = (float)v[i][j] - from;
+                    s += sizeof(T) == 2 ? exp_fast(x) : exp_near(x);
+                }
+            sum = fmaf(sum, exp_near(run - from), s);
+            run = top;
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            Key key[N];
+            GateKey<T>::chunk(v[i], base + (lane + i * 64) * N, key);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                uint64_t in = __ballot(key[j] > bar);
+                if (in == 0) continue;
+                if (count + __popcll(in) > 64) {
+                    flush();
+                    in = __ballot(key[j] > bar);
+                }
+                if (in >> lane & 1) list[count + __popcll(in & (((uint64_t)1 << lane) - 1))] = key[j];
+                count += __popcll(in);
+            }
+        }
+    }
+    if (count > 0) flush();
+    const bool there = lane < a.k && best > GateKey<T>::kNone;
+    const Key first = lane_value(best, 0);
+    const float top = first > GateKey<T>::kNone ? GateKey<T>::value(first) : 0.0f;
+    const float e = there ? exp_near(GateKey<T>::value(best) - top) : 0.0f;
+    const float s = lanes_sum(a.over == GATE_ALL ? sum * exp_near(run - top) : e, 64);
+    if (lane < a.k) {
+        a.ids[t * a.k + lane] = there ? GateKey<T>::column(best) : -1;
+        a.w[t * a.k + lane] = there ? e / s : 0.0f;
+    }
+}
+
+// ---------------------------------------------------------------------------
 // Its gradient: S = sum of w dw; -p S everywhere (over the chosen: 0), then the chosen
 // columns' own values behind them, w (dw - S): lane j that of choice j (columns given
 // twice get the sum of all their slots, the same in every one's lane).  The block's or
@@ -288,30 +430,63 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate_grad(GateArgs a, int
 // Lanes per row: four chunks each (eight lanes of 32 logits share a round's exchanges and
 // bookkeeping among more rows than sixteen of 16), fewer where there are not four waves
 // for every SIMD then; at least k lanes.  Rows of more than a wave's over a block.
+struct GateShape {
+    int L, nit;
+    bool wide;
+};
+template <typename T>
+GateShape gate_shape(const GateArgs &a)
+{
+    constexpr int N = NetVec<T>::N;
+    const int chunks = (a.G + N - 1) / N;
+    GateShape g{1, 1, chunks > 256};
+    if (g.wide) {
+        g.L = 256;
+        while (g.L < 1024 && chunks > 2 * g.L) g.L *= 2;
+        g.nit = 2;
+    } else {
+        while (g.L < 64 && (chunks > 4 * g.L || (chunks > g.L && a.T * g.L < 64 * 4096))) g.L *= 2;
+        while (g.L < a.k) g.L *= 2;
+    }
+    while (chunks > g.nit * g.L) g.nit *= 2;
+    return g;
+}
 template <typename T, typename F>
 hipError_t gate_launch(const GateArgs &a, F &&f)
 {
     constexpr int N = NetVec<T>::N;
-    const int chunks = (a.G + N - 1) / N;
-    if (chunks > 256) {
-        int threads = 256;
-        while (threads < 1024 && chunks > 2 * threads) threads *= 2;
-        const dim3 grid = net_grid(a.T), block(threads);
-        if (chunks <= 2 * threads) f(std::integral_constant<int, 2>{}, std::true_type{}, grid, block, threads, false);
-        else if (chunks <= 4 * threads) f(std::integral_constant<int, 4>{}, std::true_type{}, grid, block, threads, false);
-        else f(std::integral_constant<int, 8>{}, std::true_type{}, grid, block, threads, false);
-        return hipGetLastError();
-    }
-    int L = 1;
-    while (L < 64 && (chunks > 4 * L || (chunks > L && a.T * L < 64 * 4096))) L *= 2;
-    while (L < a.k) L *= 2;
-    const int nit = (chunks + L - 1) / L;
-    const dim3 grid = net_grid((a.T + 256 / L - 1) / (256 / L)), block(256);
-    const auto whole = [&](int n) { return a.G == n * L * N; };
-    if (nit <= 1) f(std::integral_constant<int, 1>{}, std::false_type{}, grid, block, L, whole(1));
-    else if (nit <= 2) f(std::integral_constant<int, 2>{}, std::false_type{}, grid, block, L, whole(2));
-    else f(std::integral_constant<int, 4>{}, std::false_type{}, grid, block, L, whole(4));
+    const GateShape g = gate_shape<T>(a);
+    const dim3 grid = net_grid(g.wide ? a.T : (a.T + 256 / g.L - 1) / (256 / g.L)), block(g.wide ? g.L : 256);
+    const bool whole = !g.wide && a.G == g.nit * g.L * N;
+    if (g.wide) {
+        if (g.nit <= 2) f(std::integral_constant<int, 2>{}, std::true_type{}, grid, block, g.L, whole);
+        else if (g.nit <= 4) f(std::integral_constant<int, 4>{}, std::true_type{}, grid, block, g.L, whole);
+        else f(std::integral_constant<int, 8>{}, std::true_type{}, grid, block, g.L, whole);
+    } else if (g.nit <= 1) f(std::integral_constant<int, 1>{}, std::false_type{}, grid, block, g.L, whole);
+    else if (g.nit <= 2) f(std::integral_constant<int, 2>{}, std::false_type{}, grid, block, g.L, whole);
+    else f(std::integral_constant<int, 4>{}, std::false_type{}, grid, block, g.L, whole);
     return hipGetLastError();
+}
+
+// Which of the two a gate takes, by instructions of a wave (fitted to 190 sizes: where the
+// faster one is 10 % ahead, the estimate names it): a round of the first is s subtractions and
+// maxima, of 64 bits five instructions, and the row's exchanges; the second has its
+// segments, a sort or two, and little for each choice.  Up to 2048 waves run at once at a
+// wave's own pace.  bf16 32,768 x 2048: k 8 40 us by rounds and 45 streamed, k 32 114 and 58;
+// fp32 4096 x 16,384, k 8: 276 and 48.
+template <typename T>
+bool gate_streams(const GateArgs &a)
+{
+    constexpr int N = NetVec<T>::N;
+    constexpr bool wide = sizeof(T) == 4;  // (keys of 64 bits)
+    const GateShape g = gate_shape<T>(a);
+    const int64_t s = (int64_t)g.nit * N, waves = g.wide ? g.L / 64 : 1;
+    const int64_t meet = g.wide ? 12 + (wide ? 8 : 2) * waves : (wide ? 25 : 12);
+    const int64_t rounds = 5 * s + a.k * (wide ? 5 * s + meet : 3 * s / 2 + meet);
+    const int64_t segments = (a.G + 64 * kStreamChunks * N - 1) / (64 * kStreamChunks * N);
+    const int64_t stream = wide ? segments * 352 + 370 + 13 * a.k : segments * 384 + 240 + 12 * a.k;
+    const auto time = [](int64_t c, int64_t w) { return c * (w < 2048 ? 2048 : w); };
+    return time(stream, a.T) < time(rounds, g.wide ? a.T * waves : (a.T * g.L + 63) / 64);
 }
 
 }  // namespace
@@ -320,6 +495,10 @@ hipError_t launch_gate(const GateArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
+        if (gate_streams<T>(a)) {
+            hipLaunchKernelGGL(k_gate_stream<T>, net_grid((a.T + 3) / 4), dim3(256), 0, s, a);
+            return hipGetLastError();
+        }
         return gate_launch<T>(a, [&](auto nit, auto wide, dim3 grid, dim3 block, int L, bool whole) {
             if constexpr (decltype(wide)::value && sizeof(T) == 2 && decltype(nit)::value == 8) return;  // (four hold any row)
             else hipLaunchKernelGGL((k_gate<T, decltype(nit)::value, decltype(wide)::value>), grid, block, 0, s, a, L, whole);

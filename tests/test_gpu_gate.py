@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from mix_ref import gate64, gate_grad64
+from mix_ref import gate64, gate_grad64, gate_weights64
 from net_ref import DTYPES, TINY, U, U32
 
 pytestmark = pytest.mark.gpu
@@ -196,3 +196,53 @@ def test_offsets_beyond_32_bits(evox_gpu, dtype):
     evox_gpu.evox_gate_grad(z.contiguous(), ids, w, dw, want, over=1)
     evox_gpu.evox_gate_grad(z, ids, w, dw, big[:, 30_000:30_000 + G], over=1)
     assert torch.equal(big[:, 30_000:30_000 + G], want)
+
+
+def sorted64(z, k, over):
+    """gate64 by a stable sort of all rows at once (no NaN or +inf)."""
+    top, order = torch.sort(z.cpu().double() + 0.0, dim=1, descending=True, stable=True)
+    ids = torch.where(top[:, :k] > -math.inf, order[:, :k], torch.full_like(order[:, :k], -1)).int()
+    return ids, gate_weights64(z, ids, over)
+
+
+@pytest.mark.parametrize("over", OVER)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,G,k", [(9001, 2100, 5), (6000, 700, 32), (3001, 9001, 29), (4500, 2048, 31), (2300, 33_000 - 233, 3),
+                                   (4100, 1024, 17), (20_000, 33, 33 - 1)])
+def test_many_rows_and_choices(evox_gpu, T, G, k, dtype, over):
+    """Batches whose rows are streamed, one wave each: ties, masks, rows in ascending and
+    descending order, rows that a mask leaves little or nothing of."""
+    z = logits(T, G, dtype, G + k, pad=G % 3, ties=True, mask=0.1)
+    z[::5] = logits((T + 4) // 5, G, dtype, 1)
+    z[1::7] = torch.sort(z[1::7], dim=1).values
+    z[2::7] = torch.sort(z[2::7], dim=1, descending=True).values
+    z[3::50] = -math.inf
+    z[4::50, 1:] = -math.inf
+    z[5::50, : G - 1] = -math.inf
+    z[6::50] = torch.finfo(dtype).min
+    ids, w = run(evox_gpu, z, k, over)
+    want_ids, want = sorted64(z, k, over)
+    assert torch.equal(ids.cpu(), want_ids)
+    bound = weights_bound(z, want)
+    bound[6::50] = want[6::50].abs() * (G + 64) * U32  # (equal logits: no span, but of the type's lowest value)
+    bad = ~((w.double().cpu() - want).abs() <= bound)
+    assert not bad.any(), (int(bad.sum()), w.cpu()[bad][:3], want[bad][:3])
+
+
+@pytest.mark.parametrize("over", OVER)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_infinities_and_nan_among_many_rows(evox_gpu, dtype, over):
+    T, G, k = 8200, 3001, 9
+    z = logits(T, G, dtype, 5)
+    some = torch.randperm(T, generator=torch.Generator().manual_seed(0))[:24]
+    for i, t in enumerate(some.tolist()):
+        z[t, (i * 131) % G] = (math.nan, math.inf, -math.nan)[i % 3]
+        z[t, (i * 777 + 2100) % G] = (math.inf, math.nan, math.inf)[i % 3]
+    ids, w = run(evox_gpu, z, k, over)
+    want_ids, want = gate64(z[some], k, over)
+    assert torch.equal(ids.cpu()[some], want_ids)
+    assert torch.equal(w.cpu()[some].isnan(), want.isnan()) and want.isnan().all()
+    rest = torch.ones(T, dtype=torch.bool)
+    rest[some] = False
+    want_ids, want = sorted64(z[rest.cuda()], k, over)
+    assert torch.equal(ids.cpu()[rest], want_ids) and torch.isfinite(w.cpu()[rest]).all()
