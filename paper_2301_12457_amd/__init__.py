@@ -666,12 +666,19 @@ def evox_route(ids, off, pos, src=None, scratch=None, stream=None):
     if ids is None or off is None or pos is None:
         _given(ids=ids, off=off, pos=pos)
     p = _route(ids, off)
-    shape = ids.shape
-    ids_at, off_at = _table("ids", ids, _INT, shape, ids), _vector("off", off, _INT, p.G + 1, ids)
-    pos_at, src_at = _table("pos", pos, _INT, shape, ids), _vector("src", src, _INT, p.T * p.k, ids)
-    # (the size of a scratch that the caller has is the call's own to check)
-    scratch, nbytes = _scratch(1 if scratch is not None else lib().evox_route_scratch_bytes(ctypes.byref(p)), ids, scratch,
-                               stream)
+    # one pass for what most calls are; anything else is checked and named below
+    shape, dev, n = ids.shape, ids.get_device(), p.T * p.k
+    if (_is_table(ids, _INT, shape, dev) and _is_table(pos, _INT, shape, dev) and _is_table(off, _INT, (p.G + 1,), dev)
+            and (src is None or _is_table(src, _INT, (n,), dev)) and scratch is not None and scratch.get_device() == dev
+            and scratch.is_contiguous()):
+        ids_at, off_at, pos_at = ids.data_ptr(), off.data_ptr(), pos.data_ptr()
+        src_at, nbytes = None if src is None else src.data_ptr(), scratch.numel() * scratch.element_size()
+    else:
+        ids_at, off_at = _table("ids", ids, _INT, shape, ids), _vector("off", off, _INT, p.G + 1, ids)
+        pos_at, src_at = _table("pos", pos, _INT, shape, ids), _vector("src", src, _INT, n, ids)
+        # (the size of a scratch that the caller has is the call's own to check)
+        scratch, nbytes = _scratch(1 if scratch is not None else lib().evox_route_scratch_bytes(ctypes.byref(p)), ids,
+                                   scratch, stream)
     rc = lib().evox_route(ctypes.byref(p), ids_at, off_at, pos_at, src_at, scratch.data_ptr(), nbytes,
                           _raw_stream(stream, ids))
     if rc != OK:
@@ -735,11 +742,14 @@ def evox_combine_grad(xs, pos, dy, w=None, dxs=None, dw=None, stream=None):
     p, pos_at, w_at = _slots("dy", dy, xs, pos, w)
     dxs_at = dw_at = None
     if dxs is not None:
-        if dxs.dim() != 2:
-            raise EvoxError(EINVAL, "dxs must be [M, D]")
-        M = dxs.shape[0]
-        dxs_at = _view("dxs", dxs, dy, (M if xs is None else p.M, p.D))
-        p.M, p.ldds = M, dxs.stride(0) if M > 1 else p.D
+        (M, *n), st = dxs.shape, dxs.stride()
+        if (xs is None or M == p.M) and n == [p.D] and st[1] == 1 and dxs.dtype is dy.dtype and dxs.get_device() == dy.get_device():
+            dxs_at = dxs.data_ptr()
+        else:
+            if dxs.dim() != 2:
+                raise EvoxError(EINVAL, "dxs must be [M, D]")
+            dxs_at = _view("dxs", dxs, dy, (M if xs is None else p.M, p.D))
+        p.M, p.ldds = M, st[0] if M > 1 else p.D
     if dw is not None:
         dw_at = _table("dw", dw, _FLOAT, (p.T, p.k), dy)
     rc = lib().evox_combine_grad(ctypes.byref(p), None if xs is None else xs.data_ptr(), pos_at, w_at, dy.data_ptr(),

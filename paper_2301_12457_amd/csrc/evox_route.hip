@@ -227,6 +227,50 @@ __global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
         }
 }
 
+// Up to 256 slots, any number of networks: a slot's row is the number of (network, slot)
+// pairs below its own, by comparison with all.  Every block ranks them and writes its share
+// of the offsets; the first one the rows (8 slots of 256 networks: 3.3 us, 3.7 by digits; 252 of
+// 8849: 6.8, 15 by two digits and the bounds).
+constexpr int kFew = 256, kFewOffsets = 1024;  // slots, and offsets per block
+__global__ __launch_bounds__(kFew) void k_route_few(Pass p)
+{
+    __shared__ __attribute__((aligned(16))) int pairs[kFew];
+    __shared__ int sorted[kFew];
+    const int i = threadIdx.x, n = (int)p.n;
+    const int key = i < n ? p.key[i] : -1;
+    const bool in = key >= 0 && key < p.G;
+    const int mine = in ? key << 8 | i : INT32_MAX;  // (networks are below 2^20)
+    pairs[i] = mine;
+    sorted[i] = INT32_MAX;
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; j += 4) {
+        const int4 q = *reinterpret_cast<const int4 *>(&pairs[j]);  // (behind the n-th: none, above all)
+        rank += (q.x < mine) + (q.y < mine) + (q.z < mine) + (q.w < mine);
+    }
+    if (in) sorted[rank] = key;
+    if (blockIdx.x == 0 && i < n) {
+        p.pos[i] = in ? rank : -1;
+        if (in && p.src) p.src[rank] = i;
+    }
+    __syncthreads();
+    // off[g]: how many sorted keys are below g, four of them per thread at a time
+    constexpr int each = kFewOffsets / kFew;
+    const int g0 = blockIdx.x * kFewOffsets + i;
+    int lo[each];
+#pragma unroll
+    for (int e = 0; e < each; ++e) lo[e] = sorted[kFew - 1] < g0 + e * kFew ? kFew : 0;
+#pragma unroll
+    for (int step = kFew / 2; step > 0; step /= 2)
+#pragma unroll
+        for (int e = 0; e < each; ++e)
+            if (lo[e] < kFew && sorted[lo[e] + step - 1] < g0 + e * kFew) lo[e] += step;
+#pragma unroll
+    for (int e = 0; e < each; ++e)
+        if (g0 + e * kFew <= p.G) p.off[g0 + e * kFew] = lo[e];
+}
+
 // off[g] = the first of the sorted keys that is g or more.
 __global__ __launch_bounds__(256) void k_route_bounds(Pass p, int32_t *off)
 {
@@ -312,6 +356,12 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t s)
     p.count = (int32_t *)(m + l.count);
     p.total = (int32_t *)(m + l.total);
     p.pos = a.pos;
+    if (a.n <= kFew) {
+        p.off = a.off;
+        p.src = a.src;
+        hipLaunchKernelGGL(k_route_few, dim3((unsigned)(a.G / kFewOffsets + 1)), dim3(kFew), 0, s, p);
+        return hipGetLastError();
+    }
     if (l.passes == 1) {
         p.off = a.off;
         p.src = a.src;
