@@ -650,7 +650,8 @@ int evox_xent(const evox_classes *classes, const void *logits, const int32_t *la
  * networks that a gate chooses for it, is brought into the networks' grouping
  * (where evox_linear and the others above run, with off), and back.  The rules
  * above hold here too: element types, alignment, pitches, no memory read on the
- * host, nothing allocated, the same bits on every run.
+ * host, nothing allocated, the same bits on every run, outputs that overlap no input
+ * but where a call says so.
  * ------------------------------------------------------------------------- */
 enum evox_gate_over { EVOX_GATE_CHOSEN = 0, EVOX_GATE_ALL = 1 };
 #define EVOX_GATE_MAX_K 32
@@ -711,12 +712,12 @@ int evox_dispatch(const evox_slots *slots, const void *x, const int32_t *pos, co
 
 /* And back: y[t] = sum over j of w[t][j] xs[pos[t][j]] + r[t], summed in fp32 in j's
  * order; w null: weights 1, r null: none.  Slots without a row add nothing, whatever
- * their w holds. */
+ * their w holds.  y may be r (equal pitch). */
 int evox_combine(const evox_slots *slots, const void *xs, const int32_t *pos, const float *w, const void *r, void *y,
                  void *hip_stream);
 
 /* Its gradient: dxs[pos[t][j]] = w[t][j] dy[t] (rows that no slot has are left as they
- * were) and dw[t][j] = sum over the row of dy[t] xs[pos[t][j]], 0 for slots
+ * were, as evox_dispatch does) and dw[t][j] = sum over the row of dy[t] xs[pos[t][j]], 0 for slots
  * without a row (device fp32 [T][k]); r's is dy itself.  dxs or dw may be null, xs is
  * read for dw alone.  dxs may be xs (equal pitch) where dw is null. */
 int evox_combine_grad(const evox_slots *slots, const void *xs, const int32_t *pos, const float *w, const void *dy,

@@ -142,7 +142,14 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
         reg o;
 #pragma unroll
         for (int e = 0; e < N; ++e) o[e] = (T)s[e];
-        put_chunk<SPREAD, false>((T *)a.y + t * a.ldy, c, D, o);
+        T *y = (T *)a.y + t * a.ldy;
+        const int twice = SPREAD == TINY ? 0 : c * N + N - D;
+        if (a.x == a.y && twice > 0) {
+            // r in y's place: of what the chunk before has too, r may be gone by now
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (e >= twice) y[D - N + e] = o[e];
+        } else put_chunk<SPREAD, false>(y, c, D, o);
     }
 }
 

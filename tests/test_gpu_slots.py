@@ -94,6 +94,18 @@ def test_combine(evox_gpu, T, k, D, dtype, drop, weighted, residual):
     close(y[:, 1:1 + D], want, (k + 2) * U32 * mag, dtype)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,k,D", SIZES + [(3000, 2, 1029), (2000, 3, 2051), (500, 1, 9001)])
+def test_residual_in_the_result_s_place(evox_gpu, T, k, D, dtype):
+    M, pad, pos, there, w = case(T, k, D, dtype, 0.2, T + k + D)
+    xs, r = rows(M, D, dtype, D, pad), rows(T, D, dtype, D + 1, 3)
+    want = evox_gpu.evox_combine(xs, pos, torch.empty(T, D, dtype=dtype, device="cuda"), w=w, r=r)
+    whole = r._base.clone()
+    got = evox_gpu.evox_combine(xs, pos, r, w=w, r=r)
+    assert torch.equal(got, want)
+    assert torch.equal(r._base[:, :1], whole[:, :1]) and torch.equal(r._base[:, 1 + D:], whole[:, 1 + D:])
+
+
 @pytest.mark.parametrize("weighted", [False, True])
 @pytest.mark.parametrize("drop", [0.0, 0.4])
 @pytest.mark.parametrize("dtype", DTYPES)
