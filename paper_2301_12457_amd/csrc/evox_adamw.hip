@@ -305,8 +305,11 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
         // number of any use, is an infinite divisor)
         const float rate = lr / expm1f((float)t * a.log1), turn = 1.0f / rate;
         const bool some = fabsf(rate) > 1e-30f;
+        // (an eps whose quotient is below 2^-126 counts as that: the reciprocal of less is infinite,
+        // and m = 0 by it no number)
+        const float eps = copysignf(fmaxf(fabsf(turn * a.eps), 0x1p-126f), turn);
         return Rates{a.beta1, a.beta2, a.keep, a.in1, a.in2, some ? turn / sqrtf(-expm1f((float)t * a.log2)) : 0.0f,
-                     some ? turn * a.eps : INFINITY, lr * a.decay};
+                     some ? eps : INFINITY, lr * a.decay};
     };
     if (x.groups == 0) {  // (a table without elements is one tile of nothing: the count moves on)
         rates_of();

@@ -282,3 +282,15 @@ def test_rates_of_zero_and_below(evox_gpu):
             evox_gpu.AdamW([t], [g], lr=lr, weight_decay=0.0, bits=bits).step()
         # (two roundings of p each)
         assert ((up + down - 2 * p).abs() <= 8 * U32 * (p.abs() + 1)).all() and ((up - p) * g >= 0).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr,eps", [(1.0, 1e-40), (1e3, 1e-36), (-1.0, 1e-42), (1e-3, 1e-30)])
+def test_eps_next_to_nothing(evox_gpu, bits, lr, eps):
+    """A gradient of 0 changes nothing, whatever divides it; the others move by the rate, m / sqrt(v)
+    being 1 at the first step (of 8 roundings)."""
+    g = torch.randn(700, device="cuda")
+    g[g.abs() < 0.1] = 0.0
+    p = torch.zeros(700, device="cuda")
+    evox_gpu.AdamW([p], [g], lr=lr, eps=eps, weight_decay=0.0, bits=bits).step()
+    assert ((p + lr * g.sign()).abs() <= 16 * U32 * abs(lr)).all()
