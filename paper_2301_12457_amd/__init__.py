@@ -720,7 +720,8 @@ def evox_dispatch(x, pos, xs, w=None, stream=None):
 
 
 def evox_combine(xs, pos, y, w=None, r=None, stream=None):
-    """y[t] = sum_j w[t, j] xs[pos[t, j]] + r[t] for the rows of y [T, D] (w None: 1)."""
+    """y[t] = sum_j w[t, j] xs[pos[t, j]] + r[t] for the rows of y [T, D] (w None: 1; r may
+    be y)."""
     if xs is None or pos is None or y is None:
         _given(xs=xs, pos=pos, y=y)
     p, pos_at, w_at = _slots("y", y, xs, pos, w)
@@ -742,12 +743,12 @@ def evox_combine_grad(xs, pos, dy, w=None, dxs=None, dw=None, stream=None):
     p, pos_at, w_at = _slots("dy", dy, xs, pos, w)
     dxs_at = dw_at = None
     if dxs is not None:
-        (M, *n), st = dxs.shape, dxs.stride()
-        if (xs is None or M == p.M) and n == [p.D] and st[1] == 1 and dxs.dtype is dy.dtype and dxs.get_device() == dy.get_device():
+        if dxs.dim() != 2:
+            raise EvoxError(EINVAL, "dxs must be [M, D]")
+        (M, n), st = dxs.shape, dxs.stride()
+        if (xs is None or M == p.M) and n == p.D and st[1] == 1 and dxs.dtype is dy.dtype and dxs.get_device() == dy.get_device():
             dxs_at = dxs.data_ptr()
         else:
-            if dxs.dim() != 2:
-                raise EvoxError(EINVAL, "dxs must be [M, D]")
             dxs_at = _view("dxs", dxs, dy, (M if xs is None else p.M, p.D))
         p.M, p.ldds = M, st[0] if M > 1 else p.D
     if dw is not None:
@@ -802,7 +803,7 @@ class AdamW:
                 self.state[name] = zeros(N, torch.uint8).view(torch.float8_e4m3fn)
                 self.state[name + "_scale"] = zeros(sum(blocks))
         if master:
-            self.state["master"] = torch.cat([p.reshape(-1) for p in self.params]).float()
+            self.state["master"] = torch.cat([p.detach().reshape(-1) for p in self.params]).float()
         width = {"m": bits // 8, "v": bits // 8, "m_scale": 4, "v_scale": 4, "master": 4}
         at = {name: t.data_ptr() for name, t in self.state.items()}
         tensors = (Parameter * len(shapes))()

@@ -171,6 +171,16 @@ def test_optimizer_s_master(here):
     assert opt.state["master"].tolist() == [1.0] * 20 and opt.state["m"].dtype == torch.float32
     t = planned(here)[2]
     assert [x.master - t[0].master for x in t] == [0, 40]
+    # of parameters that a program trains, no part of their graph
+    leaf = p.clone().requires_grad_()
+    opt = here.AdamW([gpu(leaf)], [new(2, 5).bfloat16()], master=True)
+    assert not opt.state["master"].requires_grad
+
+
+def test_scalar_gradient_rows(evox):
+    a = arguments()["evox_combine_grad"]
+    with pytest.raises(evox.EvoxError, match=r"dxs must be \[M, D\]"):
+        evox.evox_combine_grad(**dict(a, dxs=gpu(torch.tensor(1.0))))
 
 
 @pytest.mark.parametrize("params,grads,kw,words", [
