@@ -4,13 +4,14 @@
 // A counting sort.  A wave takes 64 slots at a time, in order: the lanes with the same
 // digit are found with a ballot per bit, a slot's rank is the wave's count of its digit
 // so far plus the lanes before it, and no atomic decides an order.  Up to 2048 slots are
-// one block's; more are counted per tile of as many and placed by a second launch, which
-// adds up the tiles' counts itself while they are few, else from a third one between.  Up
-// to 2048 networks are one digit, more two digits, the lower first.
+// one block's.  Of up to 16 tiles of as many each counts all slots itself, in one launch;
+// more are counted per tile and placed by a second launch, which adds up the tiles' counts
+// itself while they are few, else from a third one between.  Up to 2048 networks are one
+// digit, more two digits, the lower first.
 //
 // Bound by latency: few blocks, and in each a chain of loads, ranks, LDS sums and scattered
-// stores (20,014 slots of 100 networks: 3.8 us to count and 7.2 to place, of which loads
-// and earlier tiles' counts 3, ranks 2, the digits' places 1, stores 1.5).  So a tile is 8
+// stores (20,014 slots of 100 networks: loads and counts 3.5 us, ranks 2, the digits' places
+// 1, stores 1.5).  So a tile is 8
 // waves' of four rounds where the digits are few (LDS holds a count per wave and digit) and
 // the slots enough: 16 waves' of 4096 slots 8.4 us, 4 waves' of 1024 7.0, but 11.8 against
 // 7.9 of 262,144 slots, where each tile adds up four times as many counts; all ballots come
@@ -102,16 +103,82 @@ __global__ __launch_bounds__(1024) void k_route_scan(Pass p)
     if (w == 63) p.total[b] = s;
 }
 
-// ONE: this tile is all.  SUMMED: count and total come from the scan; else the tile
-// adds the counts of all and of those before it itself.
-template <int W, bool ONE, bool SUMMED>
+// Where a tile has the counts of all and of the tiles before it from: it is all (ONE), it
+// counts every slot itself (HERE), it adds the tiles' counts (ADDED), or from the scan (SUMMED).
+enum Counts { ONE = 0, HERE = 1, ADDED = 2, SUMMED = 3 };
+
+// HERE: each digit has `copies` places, a lane's own as far as they go, so that lanes of
+// one digit seldom wait for each other, however the slots lie; in one the slots of earlier
+// tiles are counted by 2^16 and the others by 1 (behind the last digit's: of no network).
+// By graph replays, 100 networks: 4096 slots 6.3 us, 7.3 (8.8 where one network has them all) by
+// two launches; 20,014 7.8, 8.1 (9.5); 32,768 8.8, 7.8 (9.2), where the host has a launch less to make
+// (3 us).  2048 digits have two places each, and 32,768 slots of one then take 29 us, 19 by
+// three launches: so many are for up to 8 tiles (16,384: 22 and 24).
+constexpr int kPlacesHere = 4096, kTilesHere = 16;
+typedef int Four __attribute__((ext_vector_type(4), aligned(4)));
+constexpr int kBatch = 4;  // loads at a time, of four slots each
+__device__ __forceinline__ void load_here(const Pass &p, int q0, int threads, int whole, Four *key)
+{
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) key[r] = *reinterpret_cast<const Four *>(p.key + 4 * max(min(q0 + r * threads, whole - 1), 0));
+}
+template <int W>
+__device__ __forceinline__ void count_here(const Pass &p, int n, Four *key, int *hist, int *total, int *before)
+{
+    constexpr int threads = 64 * W;
+    const int bins = p.bins, copies = min(kPlacesHere / bins, 64), mine = threadIdx.x & (copies - 1);
+    const int first = blockIdx.x * kTile, whole = n / 4;
+    const bool single = p.G <= bins;
+    const auto one = [&](int k, int by) {
+        const int digit = single ? k : k >> p.shift & (bins - 1), d = (uint32_t)k < (uint32_t)p.G ? digit : bins;
+        atomicAdd(&hist[d * copies + mine], by);
+    };
+    for (int q0 = threadIdx.x; q0 < whole;) {
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r)
+            if (q0 + r * threads < whole) {
+                const int by = 4 * (q0 + r * threads) < first ? 0x10000 : 1;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) one(key[r][e], by);
+            }
+        q0 += threads * kBatch;
+        if (q0 < whole) load_here(p, q0, threads, whole, key);
+    }
+    if ((int)threadIdx.x < n % 4) one(p.key[4 * whole + threadIdx.x], 4 * whole < first ? 0x10000 : 1);
+    __syncthreads();
+    if (copies >= 8) {
+        for (int u = threadIdx.x; u < bins * copies / 8; u += threads) {
+            const int4 x = reinterpret_cast<const int4 *>(hist)[2 * u], y = reinterpret_cast<const int4 *>(hist)[2 * u + 1];
+            const int s = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w, b = u * 8 / copies, early = (int)((uint32_t)s >> 16);
+            atomicAdd(&total[b], (s & 0xffff) + early);
+            atomicAdd(&before[b], early);
+        }
+    } else
+        for (int b = threadIdx.x; b < bins; b += threads) {
+            int s = 0;
+            for (int e = 0; e < copies; ++e) s += hist[b * copies + e];
+            before[b] = (int)((uint32_t)s >> 16);
+            total[b] = (s & 0xffff) + before[b];
+        }
+    __syncthreads();
+    for (int b = threadIdx.x; b < W * bins; b += threads) hist[b] = 0;
+    __syncthreads();
+}
+
+template <int W, int FROM>
+__host__ __device__ constexpr int lds_base(int bins)
+{
+    return FROM == HERE && W * bins < kPlacesHere + 64 ? kPlacesHere + 64 : W * bins;
+}
+
+template <int W, int FROM>
 __global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
 {
     constexpr int threads = 64 * W, kRounds = kTile / threads;
-    extern __shared__ int lds[];  // [W][bins] counts of the waves; places, all counts, counts before, [bins] each
+    extern __shared__ __attribute__((aligned(16))) int lds[];  // counts of the waves, [W][bins]; places, all counts, counts before, [bins] each
     __shared__ int sums[W];
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, tile = blockIdx.x, bins = p.bins;
-    const int mine = wave * bins, base = W * bins, total = base + bins, before_at = total + bins;
+    const int mine = wave * bins, base = lds_base<W, FROM>(bins), total = base + bins, before_at = total + bins;
     const int64_t n = pass_size(p);
     const int64_t first = (int64_t)tile * kTile;
     // rounds of this tile: the waves' shares follow each other
@@ -119,6 +186,8 @@ __global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
     const int rounds = left <= 0 ? 0 : left >= kTile ? kRounds : (int)((left + threads - 1) / threads);
     const int at = wave * rounds * 64 + lane;
     int key[kRounds], slot[kRounds];
+    Four others[FROM == HERE ? kBatch : 1];
+    if constexpr (FROM == HERE) load_here(p, threadIdx.x, threads, (int)n / 4, others);
     slot_keys<kRounds>(p, first, at, 64, n, key);
     if (p.slot && left > 0)
 #pragma unroll
@@ -126,9 +195,10 @@ __global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
     else
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) slot[r] = (int)first + at + r * 64;
-    for (int b = threadIdx.x; b < (W + 3) * bins; b += threads) lds[b] = 0;
+    for (int b = threadIdx.x; b < base + 3 * bins; b += threads) lds[b] = 0;
     __syncthreads();
-    if constexpr (!ONE && !SUMMED) {
+    if constexpr (FROM == HERE) count_here<W>(p, (int)n, others, lds, lds + total, lds + before_at);
+    if constexpr (FROM == ADDED) {
         const int wide = min(bins, threads), part = threadIdx.x / wide, parts = threads / wide;
         for (int b = threadIdx.x % wide; b < bins; b += wide) {
             int all = 0, before = 0;
@@ -172,7 +242,7 @@ __global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
     const int per = (bins + threads - 1) / threads, b0 = min((int)threadIdx.x * per, bins), b1 = min(b0 + per, bins);
     int s = 0;
     for (int b = b0; b < b1; ++b) {
-        int at_wave = ONE ? 0 : SUMMED ? p.count[(int64_t)tile * bins + b] : lds[before_at + b], all = 0, c[W];
+        int at_wave = FROM == ONE ? 0 : FROM == SUMMED ? p.count[(int64_t)tile * bins + b] : lds[before_at + b], all = 0, c[W];
 #pragma unroll
         for (int w = 0; w < W; ++w) c[w] = lds[w * bins + b];
 #pragma unroll
@@ -182,7 +252,7 @@ __global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
             all += c[w];
         }
         lds[base + b] = s;
-        s += ONE ? all : SUMMED ? p.total[b] : lds[total + b];
+        s += FROM == ONE ? all : FROM == SUMMED ? p.total[b] : lds[total + b];
     }
     int sum = s;
     for (int o = 1; o < 64; o *= 2) {
@@ -317,19 +387,18 @@ Scratch layout(const RouteArgs &a)
 template <int W>
 void run(const Pass &p, hipStream_t s)
 {
-    const size_t lds = (size_t)(W + 3) * p.bins * 4;
     const dim3 grid(p.tiles), block(64 * W);
-    if (p.tiles <= 1) {
-        hipLaunchKernelGGL((k_route_place<W, true, false>), dim3(1), block, lds, s, p);
-        return;
-    }
+    const auto place = [&](auto from) {
+        constexpr int FROM = decltype(from)::value;
+        const size_t lds = (size_t)(lds_base<W, FROM>(p.bins) + 3 * p.bins) * 4;
+        hipLaunchKernelGGL((k_route_place<W, FROM>), FROM == ONE ? dim3(1) : grid, block, lds, s, p);
+    };
+    if (p.tiles <= 1) return place(std::integral_constant<int, ONE>{});
+    if (p.tiles <= kTilesHere && p.tiles * p.bins <= kSummed) return place(std::integral_constant<int, HERE>{});
     hipLaunchKernelGGL(k_route_count<W>, grid, block, 0, s, p);
-    if ((int64_t)p.tiles * p.bins <= kSummed) {
-        hipLaunchKernelGGL((k_route_place<W, false, false>), grid, block, lds, s, p);
-        return;
-    }
+    if ((int64_t)p.tiles * p.bins <= kSummed) return place(std::integral_constant<int, ADDED>{});
     hipLaunchKernelGGL(k_route_scan, dim3((p.bins + 15) / 16), dim3(1024), 0, s, p);
-    hipLaunchKernelGGL((k_route_place<W, false, true>), grid, block, lds, s, p);
+    place(std::integral_constant<int, SUMMED>{});
 }
 hipError_t run(const Pass &p, hipStream_t s)
 {

@@ -42,7 +42,7 @@ def check(ids, G, off, pos, back):
 
 
 SLOTS = [(1, 1), (1, 8), (9, 7), (64, 1), (13, 5), (255, 1), (128, 2), (257, 1), (4095, 1), (512, 8), (4097, 1), (1366, 6),
-         (8192, 8), (65_537, 1), (25_000, 8)]
+         (8192, 8), (16_384, 2), (32_769, 1), (10_007, 2), (65_537, 1), (25_000, 8)]
 
 
 @pytest.mark.parametrize("kind", ["mixed", "few", "one", "none"])
