@@ -173,6 +173,28 @@ def test_gradient_of_the_same_choice_twice_and_of_none(evox_gpu, dtype, over):
     assert d[1, 2] == 0.25 * (2 - S[1]) + 0.25 * (3 - S[1]) + 0.25 * (4 - S[1])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("G", [32, 40, 333, 700, 5000])
+@pytest.mark.parametrize("k", [1, 2, 3, 5, 8, 13, 16, 17, 31, 32])
+def test_gradient_of_choices_by_chance(evox_gpu, k, G, dtype):
+    """Rows with and without a column twice, of numbers whose sums are exact."""
+    T = 77
+    rng = torch.Generator().manual_seed(k + G)
+    ids = torch.argsort(torch.rand(T, G, generator=rng), 1)[:, :k]
+    some = torch.rand(T, k, generator=rng) < torch.tensor([0.0, 0.0, 0.1, 0.7])[torch.arange(T) % 4][:, None]
+    ids = torch.where(some, ids[:, :1], ids).int()
+    ids[torch.rand(T, k, generator=rng) < 0.05] = -1
+    w = torch.randint(1, 5, (T, k), generator=rng) / 4
+    dw = torch.randint(-4, 5, (T, k), generator=rng).float()
+    z = torch.zeros(T, G, dtype=dtype, device="cuda")
+    dz = torch.empty_like(z)
+    evox_gpu.evox_gate_grad(z, ids.cuda(), w.cuda(), dw.cuda(), dz, over=OVER.index("chosen"))
+    there = (ids >= 0).double()
+    S = (w * dw * there).sum(1, keepdim=True)
+    want = torch.zeros(T, G, dtype=torch.float64).scatter_add_(1, ids.clamp_min(0).long(), w * (dw - S) * there)
+    assert torch.equal(dz.cpu(), want.to(dtype))
+
+
 def test_empty_and_inputs_kept(evox_gpu):
     z = torch.empty(0, 9, device="cuda")
     ids, w = run(evox_gpu, z, 3, "all")
