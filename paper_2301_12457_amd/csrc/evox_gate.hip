@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256) void k_gate_stream(GateArgs a)
 // ---------------------------------------------------------------------------
 // Whether another of the first k lanes (up to 32, and a group of at least as many) has this
 // lane's id too, -1 aside: all of them come by in the order of a Gray code, a step an exchange with
-// lane ^ a power of two (f16 16,680 x 4261, k 31: 31 us, 100 with every id and share by a permute
+// lane ^ a power of two (f16 16,680 x 4261, k 31: 61 us, 100 with every id and share by a permute
 // through LDS).
 __device__ __forceinline__ bool lane_twice(int id, int k)
 {

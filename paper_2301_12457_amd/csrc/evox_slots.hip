@@ -82,6 +82,53 @@ __device__ __forceinline__ int64_t row_of(int L)
 // order 204 us, in the sorted one 225, by chance 234; the floor is 186.
 constexpr int kFewBlocksLds = 32768;
 
+// Rows that do not start with a line, over whole waves: chunks are counted from the line in
+// which the row of the grouping starts, so that all stores but the row's first and last are
+// of whole lines, and each slot loads its own from the row of data, which the L1 has (bf16 k 8,
+// 146,408 rows of 2049 146 us, 171 by the row of data's own chunks; f32 k 2, 73,206 164, 185;
+// rows of up to a wave's 1 KB are as long or longer: of 257 246, 239).
+constexpr int kLine = 128;
+template <typename T, int K>
+__device__ __forceinline__ void put_lines(const SlotArgs &a, const T *x, const Places<K, WAVES> &p, int lane, int L)
+{
+    constexpr int N = NetVec<T>::N;
+    typedef typename NetVec<T>::mem mem;
+    const int D = (int)a.D;
+    int before[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) before[j] = (int)((uintptr_t)((T *)a.out + p.m[j] * a.ldo) % kLine / sizeof(T));
+    for (int c = lane * N; c < D + kLine / (int)sizeof(T) - 1; c += L * N) {
+        typename NetVec<T>::reg v[K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) v[j] = *reinterpret_cast<const mem *>(x + min(max(c - before[j], 0), D - N));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (p.m[j] < 0) continue;
+            auto o = v[j];
+            if (a.w)
+#pragma unroll
+                for (int e = 0; e < N; ++e) o[e] = (T)(p.w[j] * (float)v[j][e]);
+            const int at = c - before[j];
+            if (at > -N && at < D)
+                __builtin_nontemporal_store((mem)o, reinterpret_cast<mem *>((T *)a.out + p.m[j] * a.ldo + min(max(at, 0), D - N)));
+        }
+    }
+}
+template <typename T>
+bool by_lines(const SlotArgs &a, int L)
+{
+    return L > 64 && ((uintptr_t)a.out | a.ldo * sizeof(T)) % kLine;
+}
+template <typename T, int K>
+__global__ __launch_bounds__(256) void k_dispatch_lines(SlotArgs a, int L)
+{
+    const int64_t t = row_of<WAVES>(L);
+    if (t >= a.T) return;
+    for (int j0 = 0; j0 < a.k; j0 += K)
+        put_lines(a, (const T *)a.x + t * a.ldx, Places<K, WAVES>(a, t, j0), threadIdx.x & (L - 1), L);
+}
+
 template <typename T, int K, int SPREAD>
 __global__ __launch_bounds__(256) void k_dispatch(SlotArgs a, int L)
 {
@@ -153,7 +200,8 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
     }
 }
 
-// A row lies over L lanes of a wave or, WIDE, over a block.
+// dw, and dxs where given.  A row lies over L lanes of a wave or, WIDE, over a block of two
+// or four.
 template <typename T, int K, int SPREAD, bool WIDE>
 __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
 {
@@ -174,10 +222,9 @@ __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
         for (int c = lane; live && c * N < D; c += L) {
             const reg d = chunk_of<SPREAD, false>(dy, c, D);
             reg v[K];
-            if (a.dw)
 #pragma unroll
-                for (int j = 0; j < K; ++j)
-                    if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, true>((const T *)a.xs + p.m[j] * a.lds, c, D);
+            for (int j = 0; j < K; ++j)
+                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, true>((const T *)a.xs + p.m[j] * a.lds, c, D);
             __builtin_amdgcn_sched_barrier(0);
             // (of a last chunk, the elements that the one before it has are not this lane's to sum)
             const int twice = SPREAD == TINY ? 0 : c * N + N - D;
@@ -187,9 +234,8 @@ __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
 #pragma unroll
             for (int j = 0; j < K; ++j) {
                 if (p.m[j] < 0) continue;
-                if (a.dw)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) s[j] = e < twice ? s[j] : fmaf(own[e], (float)v[j][e], s[j]);
+                for (int e = 0; e < N; ++e) s[j] = e < twice ? s[j] : fmaf(own[e], (float)v[j][e], s[j]);
                 if (a.out) {
                     auto o = d;
                     if (a.w)
@@ -199,7 +245,6 @@ __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
                 }
             }
         }
-        if (!a.dw) continue;
 #pragma unroll
         for (int j = 0; j < K; ++j) s[j] = lanes_sum(s[j], WIDE ? 64 : L);
         if constexpr (WIDE) {
@@ -209,12 +254,64 @@ __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
                 for (int j = 0; j < K; ++j) lds[turn][wave][j] = s[j];
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < K; ++j) s[j] = ((lds[turn][0][j] + lds[turn][1][j]) + lds[turn][2][j]) + lds[turn][3][j];
+            for (int j = 0; j < K; ++j) {
+                s[j] = lds[turn][0][j] + lds[turn][1][j];
+                if (L == 256) s[j] = (s[j] + lds[turn][2][j]) + lds[turn][3][j];
+            }
         }
         if (live && lane == 0)
 #pragma unroll
             for (int j = 0; j < K; ++j)
                 if (j0 + j < a.k) a.dw[t * a.k + j0 + j] = s[j];
+    }
+}
+
+// dw alone of rows over whole waves, a wave each.  Its lanes add up in four parts what the
+// four waves of a block have, so that dw is the same bits with dxs and without.
+template <typename T, int K>
+__global__ __launch_bounds__(256) void k_combine_dw(SlotArgs a)
+{
+    constexpr int N = NetVec<T>::N;
+    typedef typename NetVec<T>::reg reg;
+    const int lane = threadIdx.x % 64, D = (int)a.D;
+    const int64_t t = row_of<WAVES>(64);
+    if (t >= a.T) return;
+    const T *dy = (const T *)a.x + t * a.ldx;
+    for (int j0 = 0; j0 < a.k; j0 += K) {
+        const Places<K, WAVES> p(a, t, j0);
+        float s[4][K];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int j = 0; j < K; ++j) s[q][j] = 0.0f;
+        for (int c0 = lane; c0 * N < D; c0 += 256)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = c0 + 64 * q;
+                if (c * N >= D) break;
+                const reg d = chunk_of<WAVES, false>(dy, c, D);
+                reg v[K];
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+                    if (p.m[j] >= 0) v[j] = chunk_of<WAVES, true>((const T *)a.xs + p.m[j] * a.lds, c, D);
+                __builtin_amdgcn_sched_barrier(0);
+                const int twice = c * N + N - D;
+                float own[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) own[e] = e < twice ? 0.0f : (float)d[e];
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+                    if (p.m[j] >= 0)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) s[q][j] = e < twice ? s[q][j] : fmaf(own[e], (float)v[j][e], s[q][j]);
+            }
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s[q][j] = lanes_sum(s[q][j], 64);
+            const float sum = ((s[0][j] + s[1][j]) + s[2][j]) + s[3][j];
+            if (lane == 0 && j0 + j < a.k) a.dw[t * a.k + j0 + j] = sum;
+        }
     }
 }
 
@@ -254,7 +351,10 @@ hipError_t launch_dispatch(const SlotArgs &a, hipStream_t s)
         const int L = row_lanes<T>(a.D, 256);
         return with_slots<T>(a, L, [&](auto K, auto spread) {
             const int lds = decltype(K)::value == 8 && L == 256 && a.T >= 8192 ? kFewBlocksLds : 0;
-            hipLaunchKernelGGL((k_dispatch<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
+            if (by_lines<T>(a, L))
+                hipLaunchKernelGGL((k_dispatch_lines<T, decltype(K)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
+            else
+                hipLaunchKernelGGL((k_dispatch<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
         });
     });
 }
@@ -270,16 +370,31 @@ hipError_t launch_combine(const SlotArgs &a, hipStream_t s)
     });
 }
 
+// Of many large rows both results are faster apart, all reads before all writes, though dy is
+// read for each (f16 k 4, 65,536 rows of 4096 209 us, 233 in one; k 2 as long or longer,
+// and what fits the last cache).
+constexpr int64_t kApart = (int64_t)1 << 28;  // bytes of the networks' rows
+constexpr int kWaveRows = 4096;               // rows that a wave each fills the chip with
 hipError_t launch_combine_grad(const SlotArgs &a, hipStream_t s)
 {
+    if (!a.dw) return launch_dispatch(a, s);  // (the rows alone are a dispatch of dy)
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
+        if (a.out && L == 256 && a.k >= 4 && a.T * a.k * a.D * (int64_t)sizeof(T) >= kApart) {
+            SlotArgs dw = a;
+            dw.out = nullptr;
+            const hipError_t e = launch_combine_grad(dw, s);
+            return e == hipSuccess ? launch_dispatch(a, s) : e;
+        }
         return with_slots<T>(a, L, [&](auto K, auto spread) {
             constexpr int k = decltype(K)::value;
             constexpr int u = decltype(spread)::value;
             if (L <= 64) hipLaunchKernelGGL((k_combine_grad<T, k, u, false>), row_grid(a.T, L), dim3(256), 0, s, a, L);
-            else if constexpr (u == WAVES) hipLaunchKernelGGL((k_combine_grad<T, k, WAVES, true>), net_grid(a.T), dim3(256), 0, s, a, 256);
+            else if constexpr (u == WAVES) {
+                if (!a.out && a.T >= kWaveRows) hipLaunchKernelGGL((k_combine_dw<T, k>), row_grid(a.T, 64), dim3(256), 0, s, a);
+                else hipLaunchKernelGGL((k_combine_grad<T, k, WAVES, true>), net_grid(a.T), dim3(L), 0, s, a, L);
+            }
         });
     });
 }
