@@ -4,7 +4,7 @@
 // Two ways to choose: k rounds over logits that lie in registers (a row over L lanes of a
 // wave, a power of two, k at least, so that lane j keeps the j-th choice; above 64 lanes'
 // worth over a block; each lane has NIT chunks of 16 bytes), or one pass over the row with
-// the best so far sorted over a wave's lanes.  Bound by instructions: bf16 65,536 x 256, k 8, weights
+// the best so far sorted over the lanes of a wave or several.  Bound by instructions: bf16 65,536 x 256, k 8, weights
 // over all, 814 of a wave for eight rows, 13.9 us (floor 5.8); fp32 keys are of 64 bits.  The
 // gradient is bound by memory (f16 20,000 x 1001 17 us, 81 MB, floor 12.5).
 #include "evox_mix.hpp"
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_gate(GateArgs a, int L, b
 }
 
 // ---------------------------------------------------------------------------
-// Many choices, or long rows: a wave takes a row in segments of 64 lanes' four chunks and
+// Many choices, or long rows: a wave (of few rows several) takes a row in segments of 64 lanes' four chunks and
 // keeps the best so far sorted over its lanes.  What is above the k-th of them joins a list of
 // up to 64 in LDS (few do after the first segment: of N logits in any order about k ln N);
 // a full list is sorted over the lanes and its first 32 merged with the best (32 are k's
@@ -264,16 +264,19 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int l)
     return (uint64_t)lane_value((uint32_t)(v >> 32), l) << 32 | lane_value((uint32_t)v, l);
 }
 
+// W: waves of a row (1, or a block's), each with its own segments, best and list; the best are
+// merged two at a time through LDS.
 constexpr int kStreamChunks = 4;  // per lane and segment
-template <typename T>
-__global__ __launch_bounds__(256) void k_gate_stream(GateArgs a)
+template <typename T, int W>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_gate_stream(GateArgs a)
 {
     constexpr int N = NetVec<T>::N, C = kStreamChunks, kSegment = 64 * C * N;
     typedef typename GateKey<T>::type Key;
-    __shared__ Key lists[4][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, G = a.G;
-    const int64_t t = net_block() * 4 + __builtin_amdgcn_readfirstlane(wave);
-    if (t >= a.T) return;  // the whole wave
+    __shared__ Key lists[W == 1 ? 4 : W][64];
+    __shared__ float sums[W];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), G = a.G;
+    const int64_t t = W == 1 ? net_block() * 4 + wave : net_block();
+    if (t >= a.T) return;  // the whole wave, or block
     const T *z = (const T *)a.z + t * a.ldz;
     Key *list = lists[wave];
     Key best = 0, bar = GateKey<T>::kNone;  // (lanes 0 .. 31), and what is not above it
@@ -290,7 +293,7 @@ __global__ __launch_bounds__(256) void k_gate_stream(GateArgs a)
         count = 0;
     };
     float run = -INFINITY, sum = 0.0f;
-    for (int base = 0; base < G; base += kSegment) {
+    for (int base = W == 1 ? 0 : wave * kSegment; base < G; base += W * kSegment) {
         typename NetVec<T>::reg v[C];
         load_row<T, C>(z + base, lane, 64, G - base, G - base >= kSegment, v);
         if (a.over == GATE_ALL) {
@@ -329,11 +332,30 @@ __global__ __launch_bounds__(256) void k_gate_stream(GateArgs a)
         }
     }
     if (count > 0) flush();
+    if constexpr (W > 1) {
+        for (int s = 1; s < W; s *= 2) {
+            list[lane] = best;
+            __syncthreads();
+            if (wave % (2 * s) == 0) {
+                const Key other = lists[wave + s][lane ^ 31];
+                best = merge_lanes<16>(other > best ? other : best);
+            }
+        }
+        if (threadIdx.x == 0) lists[1][0] = best;  // (read by wave 0 alone so far)
+        __syncthreads();
+    }
     const bool there = lane < a.k && best > GateKey<T>::kNone;
-    const Key first = lane_value(best, 0);
+    const Key first = W == 1 ? lane_value(best, 0) : lists[1][0];
     const float top = first > GateKey<T>::kNone ? GateKey<T>::value(first) : 0.0f;
     const float e = there ? exp_near(GateKey<T>::value(best) - top) : 0.0f;
-    const float s = lanes_sum(a.over == GATE_ALL ? sum * exp_near(run - top) : e, 64);
+    float s = lanes_sum(a.over == GATE_ALL ? sum * exp_near(run - top) : e, 64);
+    if constexpr (W > 1) {
+        if (lane == 0) sums[wave] = s;
+        __syncthreads();
+        if (wave > 0) return;
+        if (a.over == GATE_ALL)
+            for (int w = 1; w < W; ++w) s += sums[w];
+    }
     if (lane < a.k) {
         a.ids[t * a.k + lane] = there ? GateKey<T>::column(best) : -1;
         a.w[t * a.k + lane] = there ? e / s : 0.0f;
@@ -495,14 +517,15 @@ hipError_t gate_launch(const GateArgs &a, F &&f)
     return hipGetLastError();
 }
 
-// Which of the two a gate takes, by instructions of a wave (fitted to 190 sizes: where the
-// faster one is 10 % ahead, the estimate names it): a round of the first is s subtractions and
-// maxima, of 64 bits five instructions, and the row's exchanges; the second has its
-// segments, a sort or two, and little for each choice.  Up to 2048 waves run at once at a
-// wave's own pace.  bf16 32,768 x 2048: k 8 40 us by rounds and 45 streamed, k 32 114 and 58;
-// fp32 4096 x 16,384, k 8: 276 and 48.
+// How a gate is taken: 0 by rounds, else streamed by so many waves a row.  By instructions
+// of a wave (fitted to 430 sizes, within 2 % of the fastest in the mean, 35 % at worst): a
+// round of the first is s subtractions and maxima, of 64 bits five instructions, and the row's
+// exchanges; the second has its segments, a sort or two, little for each choice, and merges.
+// Up to 2048 waves run at once at a wave's own pace, 4096 of rows with several at 0.8 of it.  By rounds and
+// streamed by 1, 4 and 16 waves: bf16 32,768 x 2048, k 8 40 us and 45, k 32 114 and 58; fp32 256 x
+// 8192, k 16 28 us and 21, 11, 10; 1024 x 8192, k 16 71 and 22, 16, 34; 16 x 512, k 2 3.6 and 5.3.
 template <typename T>
-bool gate_streams(const GateArgs &a)
+int gate_streams(const GateArgs &a)
 {
     constexpr int N = NetVec<T>::N;
     constexpr bool wide = sizeof(T) == 4;  // (keys of 64 bits)
@@ -511,9 +534,19 @@ bool gate_streams(const GateArgs &a)
     const int64_t meet = g.wide ? 12 + (wide ? 8 : 2) * waves : (wide ? 25 : 12);
     const int64_t rounds = 5 * s + a.k * (wide ? 5 * s + meet : 3 * s / 2 + meet);
     const int64_t segments = (a.G + 64 * kStreamChunks * N - 1) / (64 * kStreamChunks * N);
-    const int64_t stream = wide ? segments * 352 + 370 + 13 * a.k : segments * 384 + 240 + 12 * a.k;
     const auto time = [](int64_t c, int64_t w) { return c * (w < 2048 ? 2048 : w); };
-    return time(stream, a.T) < time(rounds, g.wide ? a.T * waves : (a.T * g.L + 63) / 64);
+    int64_t best = time(rounds, g.wide ? a.T * waves : (a.T * g.L + 63) / 64);
+    int choice = 0;
+    for (int w = 1, step = 0; w <= 16; w *= 4, step += 2) {
+        const int64_t of = (segments + w - 1) / w;
+        const int64_t c = (wide ? of * 352 + 370 + 13 * a.k : of * 384 + 240 + 12 * a.k) + step * (wide ? 80 : 50);
+        const int64_t all = time(c, w > 1 && a.T * w <= 4096 ? a.T * w * 5 / 8 : a.T * w);
+        if (all < best) {
+            best = all;
+            choice = w;
+        }
+    }
+    return choice;
 }
 
 }  // namespace
@@ -522,10 +555,11 @@ hipError_t launch_gate(const GateArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
-        if (gate_streams<T>(a)) {
-            hipLaunchKernelGGL(k_gate_stream<T>, net_grid((a.T + 3) / 4), dim3(256), 0, s, a);
-            return hipGetLastError();
-        }
+        const int waves = gate_streams<T>(a);
+        if (waves == 1) hipLaunchKernelGGL((k_gate_stream<T, 1>), net_grid((a.T + 3) / 4), dim3(256), 0, s, a);
+        else if (waves == 4) hipLaunchKernelGGL((k_gate_stream<T, 4>), net_grid(a.T), dim3(256), 0, s, a);
+        else if (waves == 16) hipLaunchKernelGGL((k_gate_stream<T, 16>), net_grid(a.T), dim3(1024), 0, s, a);
+        if (waves) return hipGetLastError();
         return gate_launch<T>(a, [&](auto nit, auto wide, dim3 grid, dim3 block, int L, bool whole) {
             if constexpr (decltype(wide)::value && sizeof(T) == 2 && decltype(nit)::value == 8) return;  // (four hold any row)
             else hipLaunchKernelGGL((k_gate<T, decltype(nit)::value, decltype(wide)::value>), grid, block, 0, s, a, L, whole);

@@ -253,6 +253,32 @@ def test_many_rows_and_choices(evox_gpu, T, G, k, dtype, over):
 
 @pytest.mark.parametrize("over", OVER)
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,G,k", [(1, 16_384, 32), (3, 8191, 9), (57, 4097, 17), (200, 16_001, 8), (256, 9000, 2), (301, 2049, 32),
+                                   (1000, 5000, 12), (64, 32_768, 5), (7, 65_536 // 2 - 1, 31)])
+def test_few_long_rows(evox_gpu, T, G, k, dtype, over):
+    """Several waves a row: ties across their segments, masks, rows of which one wave has
+    all choices or nothing."""
+    z = logits(T, G, dtype, G + k, pad=G % 3, ties=True, mask=0.1)
+    z[::5] = logits((T + 4) // 5, G, dtype, 1)
+    z[1::7] = torch.sort(z[1::7], dim=1).values
+    z[2::7] = torch.sort(z[2::7], dim=1, descending=True).values
+    z[3::11] = -math.inf
+    z[4::11, 1:] = -math.inf
+    z[5::11, : G - 1] = -math.inf
+    z[6::11, 2048:] = -math.inf
+    z[0, G // 2:] = -30_000.0
+    ids, w = run(evox_gpu, z, k, over)
+    want_ids, want = sorted64(z, k, over)
+    assert torch.equal(ids.cpu(), want_ids)
+    bad = ~((w.double().cpu() - want).abs() <= weights_bound(z, want))
+    assert not bad.any(), (int(bad.sum()), w.cpu()[bad][:3], want[bad][:3])
+    z[0, G - 1], z[T // 2, G // 3] = math.nan, math.inf
+    ids, w = run(evox_gpu, z, k, over)
+    assert ids[0, 0] == G - 1 and w[0].isnan().all() and ids[T // 2, 0] == (G - 1 if T == 1 else G // 3)
+
+
+@pytest.mark.parametrize("over", OVER)
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_infinities_and_nan_among_many_rows(evox_gpu, dtype, over):
     T, G, k = 8200, 3001, 9
     z = logits(T, G, dtype, 5)
