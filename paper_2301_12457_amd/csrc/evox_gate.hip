@@ -518,7 +518,7 @@ hipError_t gate_launch(const GateArgs &a, F &&f)
 }
 
 // How a gate is taken: 0 by rounds, else streamed by so many waves a row.  By instructions
-// of a wave (fitted to 430 sizes, within 2 % of the fastest in the mean, 35 % at worst): a
+// of a wave (fitted to 430 sizes, within 2 % of the fastest in the mean, 30 % at worst): a
 // round of the first is s subtractions and maxima, of 64 bits five instructions, and the row's
 // exchanges; the second has its segments, a sort or two, little for each choice, and merges.
 // Up to 2048 waves run at once at a wave's own pace, 4096 of rows with several at 0.8 of it.  By rounds and

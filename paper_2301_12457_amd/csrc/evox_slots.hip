@@ -11,33 +11,39 @@ namespace evox {
 
 namespace {
 
-// How a row lies over lanes: TINY, one lane's and shorter than its 16 bytes; SOME lanes of a
-// wave; WAVES, whole ones (the row is then the same in all lanes of a wave, and so are its
-// slots).
-enum Spread { TINY = 0, SOME = 1, WAVES = 2 };
+// How a row lies over lanes: WAVES, whole ones (the row is then the same in all lanes of a wave,
+// and so are its slots), or SPREAD bytes a lane: 16, of shorter rows the largest power of two that
+// they have (f16 k 7, 714,000 rows of 7, combine 7 us and gradient 14; 13 and 35 with a lane per row
+// and its elements one by one).  EVEN: 16 bytes, and the networks' rows start with lines.
+constexpr int WAVES = 0, EVEN = 1;
+template <typename T, int SPREAD>
+struct Chunk {
+    static constexpr int N = (SPREAD <= EVEN ? 16 : SPREAD) / (int)sizeof(T);
+    typedef T reg __attribute__((ext_vector_type(N)));
+    typedef T mem __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
 
 // Chunk c of a row of n; the last one is the row's last N elements, of which the chunk before has
 // some too: two lanes store the same there, and loads and stores need no branch.  NT: past
-// the caches; the networks' rows are read once (bf16 combine of 262,144 rows of 2048 225 us
-// without, 212; f16 gradient of 65,536 rows of 4096 246, 223), and stores of whole waves go
-// there too (dispatch 219, 232 through them; f32 20,014 rows of 1001 24, 29), those of
-// narrower rows do not (f16 562,000 rows of 40 54 us past them, 35 through).
+// the caches.  So are the networks' rows read, once each, where they are whole waves' (bf16
+// combine of 262,144 rows of 2048 225 us without, 212) or start with lines (f16 2.3 million rows of
+// 64 66 us, 73 without), while other rows share their lines with the next one's reader (of 40 86 us
+// through the caches, 114 past them).  Stores of whole waves go past them too (dispatch 219 us, 232
+// through; f32 20,014 rows of 1001 24, 29), of narrower rows not (f16 562,000 rows of 40 35, 54 past).
 template <int SPREAD, bool NT, typename T>
-__device__ __forceinline__ typename NetVec<T>::reg chunk_of(const T *row, int c, int n)
+__device__ __forceinline__ typename Chunk<T, SPREAD>::reg chunk_of(const T *row, int c, int n)
 {
-    constexpr int N = NetVec<T>::N;
-    typedef typename NetVec<T>::mem mem;
-    if constexpr (SPREAD == TINY) return load_chunk(row, c, n, (T)0.0f);
+    constexpr int N = Chunk<T, SPREAD>::N;
+    typedef typename Chunk<T, SPREAD>::mem mem;
     const mem *p = reinterpret_cast<const mem *>(row + min(c * N, n - N));
     if constexpr (NT) return __builtin_nontemporal_load(p);
     else return *p;
 }
 template <int SPREAD, bool NT, typename T>
-__device__ __forceinline__ void put_chunk(T *row, int c, int n, typename NetVec<T>::reg v)
+__device__ __forceinline__ void put_chunk(T *row, int c, int n, typename Chunk<T, SPREAD>::reg v)
 {
-    constexpr int N = NetVec<T>::N;
-    typedef typename NetVec<T>::mem mem;
-    if constexpr (SPREAD == TINY) return store_chunk(row, c, n, v);
+    constexpr int N = Chunk<T, SPREAD>::N;
+    typedef typename Chunk<T, SPREAD>::mem mem;
     mem *p = reinterpret_cast<mem *>(row + min(c * N, n - N));
     if constexpr (NT) __builtin_nontemporal_store((mem)v, p);
     else *p = v;
@@ -132,7 +138,7 @@ __global__ __launch_bounds__(256) void k_dispatch_lines(SlotArgs a, int L)
 template <typename T, int K, int SPREAD>
 __global__ __launch_bounds__(256) void k_dispatch(SlotArgs a, int L)
 {
-    constexpr int N = NetVec<T>::N;
+    constexpr int N = Chunk<T, SPREAD>::N;
     const int lane = threadIdx.x & (L - 1), D = (int)a.D;
     const int64_t t = row_of<SPREAD>(L);
     if (t >= a.T) return;
@@ -157,8 +163,8 @@ __global__ __launch_bounds__(256) void k_dispatch(SlotArgs a, int L)
 template <typename T, int K, int SPREAD>
 __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
 {
-    constexpr int N = NetVec<T>::N;
-    typedef typename NetVec<T>::reg reg;
+    constexpr int N = Chunk<T, SPREAD>::N;
+    typedef typename Chunk<T, SPREAD>::reg reg;
     const int lane = threadIdx.x & (L - 1), D = (int)a.D;
     const int64_t t = row_of<SPREAD>(L);
     if (t >= a.T) return;
@@ -173,7 +179,7 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
             reg v[K];
 #pragma unroll
             for (int j = 0; j < K; ++j)
-                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, true>((const T *)a.xs + p.m[j] * a.lds, c, D);
+                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, SPREAD <= EVEN>((const T *)a.xs + p.m[j] * a.lds, c, D);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < K; ++j)
@@ -190,7 +196,7 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
 #pragma unroll
         for (int e = 0; e < N; ++e) o[e] = (T)s[e];
         T *y = (T *)a.y + t * a.ldy;
-        const int twice = SPREAD == TINY ? 0 : c * N + N - D;
+        const int twice = c * N + N - D;
         if (a.x == a.y && twice > 0) {
             // r in y's place: of what the chunk before has too, r may be gone by now
 #pragma unroll
@@ -205,8 +211,8 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
 template <typename T, int K, int SPREAD, bool WIDE>
 __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
 {
-    constexpr int N = NetVec<T>::N;
-    typedef typename NetVec<T>::reg reg;
+    constexpr int N = Chunk<T, SPREAD>::N;
+    typedef typename Chunk<T, SPREAD>::reg reg;
     __shared__ float lds[2][4][K];
     const int lane = WIDE ? threadIdx.x : threadIdx.x & (L - 1), D = (int)a.D;
     const int64_t t = WIDE ? net_block() : row_of<SPREAD>(L);
@@ -224,10 +230,10 @@ __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
             reg v[K];
 #pragma unroll
             for (int j = 0; j < K; ++j)
-                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, true>((const T *)a.xs + p.m[j] * a.lds, c, D);
+                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, SPREAD <= EVEN>((const T *)a.xs + p.m[j] * a.lds, c, D);
             __builtin_amdgcn_sched_barrier(0);
             // (of a last chunk, the elements that the one before it has are not this lane's to sum)
-            const int twice = SPREAD == TINY ? 0 : c * N + N - D;
+            const int twice = c * N + N - D;
             float own[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) own[e] = e < twice ? 0.0f : (float)d[e];
@@ -315,25 +321,42 @@ __global__ __launch_bounds__(256) void k_combine_dw(SlotArgs a)
     }
 }
 
-// Lanes per row: a chunk each, up to `most`.
+// Elements per lane, and lanes per row up to `most`.
+template <typename T>
+int chunk_elements(int64_t D)
+{
+    int n = NetVec<T>::N;
+    while (n > D) n /= 2;
+    return n;
+}
 template <typename T>
 int row_lanes(int64_t D, int most)
 {
-    const int64_t chunks = (D + NetVec<T>::N - 1) / NetVec<T>::N;
+    const int64_t n = chunk_elements<T>(D), chunks = (D + n - 1) / n;
     int L = 1;
     while (L < most && L < chunks) L *= 2;
     return L;
 }
 dim3 row_grid(int64_t T, int L) { return net_grid((T + 256 / L - 1) / (256 / L)); }
 
-// f(integral K, integral Spread): slots at a time, by k, and the row's lanes.
-template <typename T, typename F>
+// f(integral K, integral spread): slots at a time, by k, and the row's lanes.  READS: rows of
+// the networks are read.
+template <bool READS, typename T, typename F>
 hipError_t with_slots(const SlotArgs &a, int L, F &&f)
 {
     const auto spread = [&](auto K) {
+        const int bytes = chunk_elements<T>(a.D) * (int)sizeof(T);
+        const bool even = bytes == 16 && ((uintptr_t)a.xs | a.lds * sizeof(T)) % kLine == 0;
         if (L >= 64) f(K, std::integral_constant<int, WAVES>{});
-        else if (a.D >= NetVec<T>::N) f(K, std::integral_constant<int, SOME>{});
-        else f(K, std::integral_constant<int, TINY>{});
+        else if (bytes == 16) {
+            if constexpr (READS) {
+                if (even) return f(K, std::integral_constant<int, EVEN>{});
+            }
+            f(K, std::integral_constant<int, 16>{});
+        }
+        else if (bytes == 8) f(K, std::integral_constant<int, 8>{});
+        else if (bytes == 4) f(K, std::integral_constant<int, 4>{});
+        else if constexpr (sizeof(T) == 2) f(K, std::integral_constant<int, 2>{});
     };
     if (a.k == 1) spread(std::integral_constant<int, 1>{});
     else if (a.k == 2) spread(std::integral_constant<int, 2>{});
@@ -349,7 +372,7 @@ hipError_t launch_dispatch(const SlotArgs &a, hipStream_t s)
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
-        return with_slots<T>(a, L, [&](auto K, auto spread) {
+        return with_slots<false, T>(a, L, [&](auto K, auto spread) {
             const int lds = decltype(K)::value == 8 && L == 256 && a.T >= 8192 ? kFewBlocksLds : 0;
             if (by_lines<T>(a, L))
                 hipLaunchKernelGGL((k_dispatch_lines<T, decltype(K)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
@@ -364,7 +387,7 @@ hipError_t launch_combine(const SlotArgs &a, hipStream_t s)
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
-        return with_slots<T>(a, L, [&](auto K, auto spread) {
+        return with_slots<true, T>(a, L, [&](auto K, auto spread) {
             hipLaunchKernelGGL((k_combine<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), 0, s, a, L);
         });
     });
@@ -387,7 +410,7 @@ hipError_t launch_combine_grad(const SlotArgs &a, hipStream_t s)
             const hipError_t e = launch_combine_grad(dw, s);
             return e == hipSuccess ? launch_dispatch(a, s) : e;
         }
-        return with_slots<T>(a, L, [&](auto K, auto spread) {
+        return with_slots<true, T>(a, L, [&](auto K, auto spread) {
             constexpr int k = decltype(K)::value;
             constexpr int u = decltype(spread)::value;
             if (L <= 64) hipLaunchKernelGGL((k_combine_grad<T, k, u, false>), row_grid(a.T, L), dim3(256), 0, s, a, L);
