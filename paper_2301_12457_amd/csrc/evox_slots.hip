@@ -386,7 +386,11 @@ hipError_t launch_combine(const SlotArgs &a, hipStream_t s)
 {
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
-        const int L = row_lanes<T>(a.D, 256);
+        // (one or two slots: a chunk for every second lane is worse than two for each; f32 rows of 264
+        // 106 us, 88 on 64 lanes; k 7 as long)
+        int L = row_lanes<T>(a.D, 256);
+        const int64_t chunks = (a.D + NetVec<T>::N - 1) / NetVec<T>::N;
+        if (L > 64 && a.k <= 2 && 4 * chunks <= 3 * L) L /= 2;
         return with_slots<true, T>(a, L, [&](auto K, auto spread) {
             hipLaunchKernelGGL((k_combine<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), 0, s, a, L);
         });
@@ -394,8 +398,8 @@ hipError_t launch_combine(const SlotArgs &a, hipStream_t s)
 }
 
 // Of many large rows both results are faster apart, all reads before all writes, though dy is
-// read for each (f16 k 4, 65,536 rows of 4096 209 us, 233 in one; k 2 as long or longer,
-// and what fits the last cache).
+// read for each (f16 k 4, 65,536 rows of 4096 209 us, 233 in one; not for k 2,
+// nor what fits the last cache).
 constexpr int64_t kApart = (int64_t)1 << 28;  // bytes of the networks' rows
 constexpr int kWaveRows = 4096;               // rows that a wave each fills the chip with
 hipError_t launch_combine_grad(const SlotArgs &a, hipStream_t s)
