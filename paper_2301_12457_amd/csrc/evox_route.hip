@@ -11,11 +11,11 @@
 //
 // Bound by latency: few blocks, and in each a chain of loads, ranks, LDS sums and scattered
 // stores (20,014 slots of 100 networks: loads and counts 3.5 us, ranks 2, the digits' places
-// 1, stores 1.5).  So a tile is 8
-// waves' of four rounds where the digits are few (LDS holds a count per wave and digit) and
-// the slots enough: 16 waves' of 4096 slots 8.4 us, 4 waves' of 1024 7.0, but 11.8 against
-// 7.9 of 262,144 slots, where each tile adds up four times as many counts; all ballots come
-// before the first count, and all loads before both.
+// 1, stores 1.5).  So a tile is 8 waves' of four rounds where the digits are few (LDS holds a
+// count per wave and digit): 16 waves' of 4096 slots 8.4 us, 4 waves' of 1024 7.0, but 11.8
+// against 7.9 of 262,144 slots, where each tile adds up four times as many counts; all ballots
+// come before the first count, and all loads before both.  Up to 1024 slots, and up to 4096 where
+// digits would be wide or two, are ranked by comparison instead.
 #include "evox_mix.hpp"
 
 namespace evox {
@@ -23,8 +23,8 @@ namespace evox {
 namespace {
 
 constexpr int kTile = 2048, kMaxBins = 2048;
-constexpr int kWideBins = 512, kWideSlots = 1024;  // digits at most, and slots above which, for 8 waves
-constexpr int kSummed = 16384;                     // counts of all tiles that each block adds up itself
+constexpr int kWideBins = 512;   // digits at most, for 8 waves
+constexpr int kSummed = 16384;   // counts of all tiles that each block adds up itself
 
 struct Pass {
     const int32_t *key;   // of the slots in this pass's order, outside 0 .. G - 1: none
@@ -297,48 +297,61 @@ __global__ __launch_bounds__(64 * W) void k_route_place(Pass p)
         }
 }
 
-// Up to 256 slots, any number of networks: a slot's row is the number of (network, slot)
-// pairs below its own, by comparison with all.  Every block ranks them and writes its share
-// of the offsets; the first one the rows (8 slots of 256 networks: 3.3 us, 3.7 by digits; 252 of
-// 8849: 6.8, 15 by two digits and the bounds).
-constexpr int kFew = 256, kFewOffsets = 1024;  // slots, and offsets per block
-__global__ __launch_bounds__(kFew) void k_route_few(Pass p)
+// Few slots: a slot's row is the number of (network, slot) pairs below its own, by comparison
+// with all, 16 slots a block, each over 16 lanes that share the pairs between them.  They also
+// find the next pair above theirs: a network's last slot writes the offsets from its own
+// network's to the next one's.  Of n slots in n^2 comparisons: 8 of 256 networks 3.0 us (by digits
+// 3.7), 1000 of 512 4.5 (5.8), 2048 of 512 5.8 (5.7), of 8849 6.0 (18.6), 4096 of 1024 8.4 (11.6), of
+// 8849 8.6 (19.5); so up to 1024, and up to 4096 where a digit is wide or there are two.  More
+// networks than evox_gate chooses from go by digits: the one block of 8 slots of 200,000 24 us.
+constexpr int kRank = 4096, kRankAny = 1024, kRankG = 32768, kRankSlots = 16;
+constexpr int kRankOf = 12;  // bits of a pair that are the slot's
+static_assert(kRank <= 1 << kRankOf && kRankG <= 1 << (30 - kRankOf), "pairs are below INT32_MAX");
+__global__ __launch_bounds__(256) void k_route_rank(Pass p)
 {
-    __shared__ __attribute__((aligned(16))) int pairs[kFew];
-    __shared__ int sorted[kFew];
-    const int i = threadIdx.x, n = (int)p.n;
-    const int key = i < n ? p.key[i] : -1;
-    const bool in = key >= 0 && key < p.G;
-    const int mine = in ? key << 8 | i : INT32_MAX;  // (networks are below 2^20)
-    pairs[i] = mine;
-    sorted[i] = INT32_MAX;
+    constexpr int kNone = INT32_MAX;
+    __shared__ __attribute__((aligned(16))) int pairs[kRank];
+    __shared__ int keys[kRankSlots], ranks[kRankSlots], nexts[kRankSlots];
+    const int n = (int)p.n, padded = (n + 63) & ~63, base = blockIdx.x * kRankSlots;
+    for (int i = threadIdx.x; i < padded; i += 256) {
+        const int key = p.key[min(i, n - 1)];
+        pairs[i] = i < n && key >= 0 && key < p.G ? key << kRankOf | i : kNone;
+    }
     __syncthreads();
+    const int slot = threadIdx.x / 16, part = threadIdx.x % 16, i = base + slot;
+    const int mine = i < n ? pairs[i] : kNone;
     int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < n; j += 4) {
-        const int4 q = *reinterpret_cast<const int4 *>(&pairs[j]);  // (behind the n-th: none, above all)
+    uint32_t above = UINT32_MAX;  // the least distance to a pair above, less 1
+#pragma unroll 4
+    for (int j = 4 * part; j < padded; j += 64) {
+        const int4 q = *reinterpret_cast<const int4 *>(&pairs[j]);
         rank += (q.x < mine) + (q.y < mine) + (q.z < mine) + (q.w < mine);
+        // (those below, and itself, are 2^31 - 1 away or more)
+        above = min(min(above, min((uint32_t)(q.x - mine - 1), (uint32_t)(q.y - mine - 1))),
+                    min((uint32_t)(q.z - mine - 1), (uint32_t)(q.w - mine - 1)));
     }
-    if (in) sorted[rank] = key;
-    if (blockIdx.x == 0 && i < n) {
-        p.pos[i] = in ? rank : -1;
-        if (in && p.src) p.src[rank] = i;
+    rank = (int)lanes_all((uint32_t)rank, 16, [](uint32_t a, uint32_t b) { return a + b; });
+    above = lanes_all(above, 16, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+    if (part == 0) {
+        const bool in = mine != kNone;
+        // the network after this one that has slots, or the end: only the last slot of one differs
+        const int next = above < (uint32_t)(kNone - mine) ? mine + 1 + (int)above : kNone;
+        keys[slot] = in ? mine >> kRankOf : p.G;
+        ranks[slot] = rank;
+        nexts[slot] = !in ? -1 : next < kNone ? next >> kRankOf : p.G;
+        if (i < n) {
+            p.pos[i] = in ? rank : -1;
+            if (in && p.src) p.src[rank] = i;
+        }
     }
     __syncthreads();
-    // off[g]: how many sorted keys are below g, four of them per thread at a time
-    constexpr int each = kFewOffsets / kFew;
-    const int g0 = blockIdx.x * kFewOffsets + i;
-    int lo[each];
-#pragma unroll
-    for (int e = 0; e < each; ++e) lo[e] = sorted[kFew - 1] < g0 + e * kFew ? kFew : 0;
-#pragma unroll
-    for (int step = kFew / 2; step > 0; step /= 2)
-#pragma unroll
-        for (int e = 0; e < each; ++e)
-            if (lo[e] < kFew && sorted[lo[e] + step - 1] < g0 + e * kFew) lo[e] += step;
-#pragma unroll
-    for (int e = 0; e < each; ++e)
-        if (g0 + e * kFew <= p.G) p.off[g0 + e * kFew] = lo[e];
+    for (int e = 0; e < kRankSlots; ++e) {
+        const int key = keys[e], row = ranks[e];
+        for (int g = key + 1 + threadIdx.x; g <= nexts[e]; g += 256) p.off[g] = row + 1;
+        // the first of all, or (no slot has a network) slot 0
+        if (row == 0 && (key < p.G || base + e == 0))
+            for (int g = threadIdx.x; g <= key; g += 256) p.off[g] = 0;
+    }
 }
 
 // off[g] = the first of the sorted keys that is g or more.
@@ -402,7 +415,7 @@ void run(const Pass &p, hipStream_t s)
 }
 hipError_t run(const Pass &p, hipStream_t s)
 {
-    if (p.bins <= kWideBins && p.n > kWideSlots) run<8>(p, s);
+    if (p.bins <= kWideBins) run<8>(p, s);
     else run<4>(p, s);
     return hipGetLastError();
 }
@@ -425,10 +438,10 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t s)
     p.count = (int32_t *)(m + l.count);
     p.total = (int32_t *)(m + l.total);
     p.pos = a.pos;
-    if (a.n <= kFew) {
+    if (a.n <= (l.passes == 2 || l.bins > kWideBins ? kRank : kRankAny) && a.G <= kRankG) {
         p.off = a.off;
         p.src = a.src;
-        hipLaunchKernelGGL(k_route_few, dim3((unsigned)(a.G / kFewOffsets + 1)), dim3(kFew), 0, s, p);
+        hipLaunchKernelGGL(k_route_rank, dim3((unsigned)(a.n == 0 ? 1 : (a.n + kRankSlots - 1) / kRankSlots)), dim3(256), 0, s, p);
         return hipGetLastError();
     }
     if (l.passes == 1) {

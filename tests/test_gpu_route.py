@@ -41,7 +41,7 @@ def check(ids, G, off, pos, back):
         assert back[:n].cpu().tolist() == want_src and (back[n:] == -9).all()  # the rest as it was
 
 
-SLOTS = [(1, 1), (1, 8), (9, 7), (64, 1), (13, 5), (255, 1), (128, 2), (257, 1), (4095, 1), (512, 8), (4097, 1), (1366, 6),
+SLOTS = [(1, 1), (1, 8), (9, 7), (64, 1), (13, 5), (255, 1), (128, 2), (257, 1), (1024, 1), (205, 5), (2048, 1), (683, 3), (4095, 1), (512, 8), (4097, 1), (1366, 6),
          (8192, 8), (16_384, 2), (32_769, 1), (10_007, 2), (65_537, 1), (25_000, 8)]
 
 
@@ -54,8 +54,8 @@ def test_route(evox_gpu, T, k, G, kind):
 
 
 @pytest.mark.parametrize("kind", ["mixed", "few", "one", "none"])
-@pytest.mark.parametrize("G", [2049, 4097, 70_000, 1 << 20])
-@pytest.mark.parametrize("T,k", [(1, 8), (700, 3), (4097, 1), (30_000, 2), (100_003, 1)])
+@pytest.mark.parametrize("G", [2049, 4097, 32_768, 32_769, 70_000, 1 << 20])
+@pytest.mark.parametrize("T,k", [(1, 8), (1, 1), (63, 1), (700, 3), (4096, 1), (4097, 1), (30_000, 2), (100_003, 1)])
 def test_many_networks(evox_gpu, T, k, G, kind):
     ids = choices(T, k, G, kind, T + k + G)
     check(ids, G, *run(evox_gpu, ids, G))
