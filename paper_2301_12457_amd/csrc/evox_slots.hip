@@ -29,7 +29,8 @@ struct Chunk {
 // combine of 262,144 rows of 2048 225 us without, 212) or start with lines (f16 2.3 million rows of
 // 64 66 us, 73 without), while other rows share their lines with the next one's reader (of 40 86 us
 // through the caches, 114 past them).  Stores of whole waves go past them too (dispatch 219 us, 232
-// through; f32 20,014 rows of 1001 24, 29), of narrower rows not (f16 562,000 rows of 40 35, 54 past).
+// through; f32 20,014 rows of 1001 24, 29; combine's y, f16 k 4, 100,000 rows of 1001 168, 202; where
+// all fits the last cache as long), of narrower rows not (f16 562,000 rows of 40 35, 54 past).
 template <int SPREAD, bool NT, typename T>
 __device__ __forceinline__ typename Chunk<T, SPREAD>::reg chunk_of(const T *row, int c, int n)
 {
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
 #pragma unroll
             for (int e = 0; e < N; ++e)
                 if (e >= twice) y[D - N + e] = o[e];
-        } else put_chunk<SPREAD, false>(y, c, D, o);
+        } else put_chunk<SPREAD, SPREAD == WAVES>(y, c, D, o);
     }
 }
 
