@@ -14,23 +14,25 @@ namespace {
 // How a row lies over lanes: WAVES, whole ones (the row is then the same in all lanes of a wave,
 // and so are its slots), or SPREAD bytes a lane: 16, of shorter rows the largest power of two that
 // they have (f16 k 7, 714,000 rows of 7, combine 7 us and gradient 14; 13 and 35 with a lane per row
-// and its elements one by one).  EVEN: 16 bytes, and the networks' rows start with lines.
-constexpr int WAVES = 0, EVEN = 1;
+// and its elements one by one).
+constexpr int WAVES = 0;
 template <typename T, int SPREAD>
 struct Chunk {
-    static constexpr int N = (SPREAD <= EVEN ? 16 : SPREAD) / (int)sizeof(T);
+    static constexpr int N = (SPREAD == WAVES ? 16 : SPREAD) / (int)sizeof(T);
     typedef T reg __attribute__((ext_vector_type(N)));
     typedef T mem __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
 
 // Chunk c of a row of n; the last one is the row's last N elements, of which the chunk before has
 // some too: two lanes store the same there, and loads and stores need no branch.  NT: past
-// the caches.  So are the networks' rows read, once each, where they are whole waves' (bf16
-// combine of 262,144 rows of 2048 225 us without, 212) or start with lines (f16 2.3 million rows of
-// 64 66 us, 73 without), while other rows share their lines with the next one's reader (of 40 86 us
-// through the caches, 114 past them).  Stores of whole waves go past them too (dispatch 219 us, 232
-// through; f32 20,014 rows of 1001 24, 29; combine's y, f16 k 4, 100,000 rows of 1001 168, 202; where
-// all fits the last cache as long), of narrower rows not (f16 562,000 rows of 40 35, 54 past).
+// the caches.  So are the networks' rows read (PAST): whole waves' that start with lines (bf16 k 8,
+// 32,768 rows of 2048 27.8 us, 30.2 through), others where they are more than the last cache holds
+// (f32 k 2, 400 MB just written, rows of 2048: 100 us, 115 through; f16 k 8, 160 MB of 1001: 43, 31),
+// narrower ones where both hold (f16 2.3 million rows of 64 66 us, 73 through); narrow rows that
+// share their lines with the next one's reader do not (of 40 86 us through the caches, 114 past
+// them).  Stores of whole waves go past them too (dispatch 219 us, 232 through; f32 20,014 rows of
+// 1001 24, 29; combine's y, f16 k 4, 100,000 rows of 1001 168, 202; where all fits the last cache as
+// long), of narrower rows not (f16 562,000 rows of 40 35, 54 past).
 template <int SPREAD, bool NT, typename T>
 __device__ __forceinline__ typename Chunk<T, SPREAD>::reg chunk_of(const T *row, int c, int n)
 {
@@ -161,7 +163,7 @@ __global__ __launch_bounds__(256) void k_dispatch(SlotArgs a, int L)
     }
 }
 
-template <typename T, int K, int SPREAD>
+template <typename T, int K, int SPREAD, bool PAST>
 __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
 {
     constexpr int N = Chunk<T, SPREAD>::N;
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
             reg v[K];
 #pragma unroll
             for (int j = 0; j < K; ++j)
-                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, SPREAD <= EVEN>((const T *)a.xs + p.m[j] * a.lds, c, D);
+                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, PAST>((const T *)a.xs + p.m[j] * a.lds, c, D);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < K; ++j)
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(256) void k_combine(SlotArgs a, int L)
 
 // dw, and dxs where given.  A row lies over L lanes of a wave or, WIDE, over a block of two
 // or four.
-template <typename T, int K, int SPREAD, bool WIDE>
+template <typename T, int K, int SPREAD, bool PAST, bool WIDE>
 __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
 {
     constexpr int N = Chunk<T, SPREAD>::N;
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
             reg v[K];
 #pragma unroll
             for (int j = 0; j < K; ++j)
-                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, SPREAD <= EVEN>((const T *)a.xs + p.m[j] * a.lds, c, D);
+                if (p.m[j] >= 0) v[j] = chunk_of<SPREAD, PAST>((const T *)a.xs + p.m[j] * a.lds, c, D);
             __builtin_amdgcn_sched_barrier(0);
             // (of a last chunk, the elements that the one before it has are not this lane's to sum)
             const int twice = c * N + N - D;
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(SlotArgs a, int L)
 
 // dw alone of rows over whole waves, a wave each.  Its lanes add up in four parts what the
 // four waves of a block have, so that dw is the same bits with dxs and without.
-template <typename T, int K>
+template <typename T, int K, bool PAST>
 __global__ __launch_bounds__(256) void k_combine_dw(SlotArgs a)
 {
     constexpr int N = NetVec<T>::N;
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(256) void k_combine_dw(SlotArgs a)
                 reg v[K];
 #pragma unroll
                 for (int j = 0; j < K; ++j)
-                    if (p.m[j] >= 0) v[j] = chunk_of<WAVES, true>((const T *)a.xs + p.m[j] * a.lds, c, D);
+                    if (p.m[j] >= 0) v[j] = chunk_of<WAVES, PAST>((const T *)a.xs + p.m[j] * a.lds, c, D);
                 __builtin_amdgcn_sched_barrier(0);
                 const int twice = c * N + N - D;
                 float own[N];
@@ -340,24 +342,28 @@ int row_lanes(int64_t D, int most)
 }
 dim3 row_grid(int64_t T, int L) { return net_grid((T + 256 / L - 1) / (256 / L)); }
 
-// f(integral K, integral spread): slots at a time, by k, and the row's lanes.  READS: rows of
-// the networks are read.
+// f(integral K, integral spread, integral past): slots at a time, by k, the row's lanes, and
+// (READS: rows of the networks are read) whether past the caches.
+constexpr int64_t kLastCache = (int64_t)1 << 28;
+template <typename T>
+int64_t slot_bytes(const SlotArgs &a) { return a.T * a.k * a.D * (int64_t)sizeof(T); }
 template <bool READS, typename T, typename F>
 hipError_t with_slots(const SlotArgs &a, int L, F &&f)
 {
     const auto spread = [&](auto K) {
         const int bytes = chunk_elements<T>(a.D) * (int)sizeof(T);
-        const bool even = bytes == 16 && ((uintptr_t)a.xs | a.lds * sizeof(T)) % kLine == 0;
-        if (L >= 64) f(K, std::integral_constant<int, WAVES>{});
-        else if (bytes == 16) {
+        const bool even = ((uintptr_t)a.xs | a.lds * sizeof(T)) % kLine == 0, many = slot_bytes<T>(a) >= kLastCache;
+        const auto reads = [&](auto spread, bool past) {
             if constexpr (READS) {
-                if (even) return f(K, std::integral_constant<int, EVEN>{});
+                if (past) return f(K, spread, std::true_type{});
             }
-            f(K, std::integral_constant<int, 16>{});
-        }
-        else if (bytes == 8) f(K, std::integral_constant<int, 8>{});
-        else if (bytes == 4) f(K, std::integral_constant<int, 4>{});
-        else if constexpr (sizeof(T) == 2) f(K, std::integral_constant<int, 2>{});
+            f(K, spread, std::false_type{});
+        };
+        if (L >= 64) reads(std::integral_constant<int, WAVES>{}, even || many);
+        else if (bytes == 16) reads(std::integral_constant<int, 16>{}, even && many);
+        else if (bytes == 8) f(K, std::integral_constant<int, 8>{}, std::false_type{});
+        else if (bytes == 4) f(K, std::integral_constant<int, 4>{}, std::false_type{});
+        else if constexpr (sizeof(T) == 2) f(K, std::integral_constant<int, 2>{}, std::false_type{});
     };
     if (a.k == 1) spread(std::integral_constant<int, 1>{});
     else if (a.k == 2) spread(std::integral_constant<int, 2>{});
@@ -373,7 +379,7 @@ hipError_t launch_dispatch(const SlotArgs &a, hipStream_t s)
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
-        return with_slots<false, T>(a, L, [&](auto K, auto spread) {
+        return with_slots<false, T>(a, L, [&](auto K, auto spread, auto past) {
             const int lds = decltype(K)::value == 8 && L == 256 && a.T >= 8192 ? kFewBlocksLds : 0;
             if (by_lines<T>(a, L))
                 hipLaunchKernelGGL((k_dispatch_lines<T, decltype(K)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
@@ -392,8 +398,8 @@ hipError_t launch_combine(const SlotArgs &a, hipStream_t s)
         int L = row_lanes<T>(a.D, 256);
         const int64_t chunks = (a.D + NetVec<T>::N - 1) / NetVec<T>::N;
         if (L > 64 && a.k <= 2 && 4 * chunks <= 3 * L) L /= 2;
-        return with_slots<true, T>(a, L, [&](auto K, auto spread) {
-            hipLaunchKernelGGL((k_combine<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), 0, s, a, L);
+        return with_slots<true, T>(a, L, [&](auto K, auto spread, auto past) {
+            hipLaunchKernelGGL((k_combine<T, decltype(K)::value, decltype(spread)::value, decltype(past)::value>), row_grid(a.T, L), dim3(256), 0, s, a, L);
         });
     });
 }
@@ -401,27 +407,27 @@ hipError_t launch_combine(const SlotArgs &a, hipStream_t s)
 // Of many large rows both results are faster apart, all reads before all writes, though dy is
 // read for each (f16 k 4, 65,536 rows of 4096 209 us, 233 in one; not for k 2,
 // nor what fits the last cache).
-constexpr int64_t kApart = (int64_t)1 << 28;  // bytes of the networks' rows
-constexpr int kWaveRows = 4096;               // rows that a wave each fills the chip with
+constexpr int kWaveRows = 4096;  // rows that a wave each fills the chip with
 hipError_t launch_combine_grad(const SlotArgs &a, hipStream_t s)
 {
     if (!a.dw) return launch_dispatch(a, s);  // (the rows alone are a dispatch of dy)
     return net_dispatch(a.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
-        if (a.out && L == 256 && a.k >= 4 && a.T * a.k * a.D * (int64_t)sizeof(T) >= kApart) {
+        if (a.out && L == 256 && a.k >= 4 && slot_bytes<T>(a) >= kLastCache) {
             SlotArgs dw = a;
             dw.out = nullptr;
             const hipError_t e = launch_combine_grad(dw, s);
             return e == hipSuccess ? launch_dispatch(a, s) : e;
         }
-        return with_slots<true, T>(a, L, [&](auto K, auto spread) {
+        return with_slots<true, T>(a, L, [&](auto K, auto spread, auto past) {
             constexpr int k = decltype(K)::value;
             constexpr int u = decltype(spread)::value;
-            if (L <= 64) hipLaunchKernelGGL((k_combine_grad<T, k, u, false>), row_grid(a.T, L), dim3(256), 0, s, a, L);
+            constexpr bool n = decltype(past)::value;
+            if (L <= 64) hipLaunchKernelGGL((k_combine_grad<T, k, u, n, false>), row_grid(a.T, L), dim3(256), 0, s, a, L);
             else if constexpr (u == WAVES) {
-                if (!a.out && a.T >= kWaveRows) hipLaunchKernelGGL((k_combine_dw<T, k>), row_grid(a.T, 64), dim3(256), 0, s, a);
-                else hipLaunchKernelGGL((k_combine_grad<T, k, WAVES, true>), net_grid(a.T), dim3(L), 0, s, a, L);
+                if (!a.out && a.T >= kWaveRows) hipLaunchKernelGGL((k_combine_dw<T, k, n>), row_grid(a.T, 64), dim3(256), 0, s, a);
+                else hipLaunchKernelGGL((k_combine_grad<T, k, WAVES, n, true>), net_grid(a.T), dim3(L), 0, s, a, L);
             }
         });
     });
