@@ -742,7 +742,8 @@ int evox_combine_grad(const evox_slots *slots, const void *xs, const int32_t *po
 #define EVOX_ADAM_BLOCK 256
 #define EVOX_ADAM_CLOCK 528
 
-/* A tensor as rows [rows][n] (a dense one: one row), pitches in elements. */
+/* A tensor as rows [rows][n], pitches in elements.  A dense one may be one row: of 8 bits,
+ * if its rows may share scales, or n is a multiple of 256. */
 typedef struct evox_parameter {
     void *p;            /* enum evox_dtype of the call */
     const void *g;      /* its gradient, of the same type */

@@ -769,13 +769,17 @@ class AdamW:
     reads the gradients from these buffers and updates the parameters in place.
 
     lr is a number (the attribute may change from step to step) or a float32 tensor [1]
-    on the device, which a captured step reads when it is replayed.  bits: of the
-    moments, 32, or 8 (e4m3 numbers and a scale per 256).  master: an fp32 copy of
+    on the device, which a captured step reads when it is replayed.  master: an fp32 copy of
     16-bit parameters, which the steps update in their place.
+
+    bits: of the moments, 32, or 8 (e4m3 numbers and a scale per 256).  A scale is for
+    elements of one row of its parameter's first dimension (of one network, of [G, n]),
+    dense or not; a dense parameter of up to 256 elements in all, with a dense gradient,
+    has one.  Where rows are short and need none of their own, p.view(-1) has fewer.
 
     state holds what a checkpoint saves, each for all tensors one behind the other:
     "t" (steps done, int64 [1]), "m", "v" (float32, or float8_e4m3fn: of v the root), with
-    8 bits "m_scale" and "v_scale", and "master".
+    8 bits "m_scale" and "v_scale" (ceil(n / 256) for each row of n), and "master".
     """
 
     def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, bits=32, master=False):
@@ -789,7 +793,7 @@ class AdamW:
             raise EvoxError(EINVAL, "fp32 parameters are their own master")
         if bits not in (8, 32):
             raise EvoxError(EINVAL, f"bits = {bits}: states of 32 or 8")
-        shapes = [self._rows(i, p, g, like) for i, (p, g) in enumerate(zip(self.params, self.grads))]
+        shapes = [self._rows(i, p, g, like, bits) for i, (p, g) in enumerate(zip(self.params, self.grads))]
         sizes = [rows * n for rows, n, *_ in shapes]
         blocks = [rows * -(-n // ADAM_BLOCK) for rows, n, *_ in shapes]
         device, N = like.device, sum(sizes)
@@ -821,7 +825,7 @@ class AdamW:
         self.lr, self._like, self._seen, self._shapes = lr, like, set(), shapes
 
     @staticmethod
-    def _rows(i, p, g, like):
+    def _rows(i, p, g, like, bits):
         """(rows, n, pitch of p, pitch of g) of a parameter and its gradient."""
         for what, t in ((f"params[{i}]", p), (f"grads[{i}]", g)):
             if t.dtype != like.dtype or t.get_device() != like.get_device():
@@ -830,9 +834,11 @@ class AdamW:
                 raise EvoxError(EINVAL, f"{what}: rows are not dense")
         if p.shape != g.shape or p.dim() == 0:
             raise EvoxError(EINVAL, f"params[{i}] has shape {tuple(p.shape)}, its gradient {tuple(g.shape)}")
-        if p.is_contiguous() and g.is_contiguous():
-            return 1, p.numel(), p.numel(), p.numel()
-        rows, n = p.shape[0], p.numel() // p.shape[0]
+        dense, N = p.is_contiguous() and g.is_contiguous(), p.numel()
+        # (all elements as one row, but where scales would go from one row into the next)
+        if dense and (bits == 32 or p.dim() == 1 or N <= ADAM_BLOCK or N // p.shape[0] % ADAM_BLOCK == 0):
+            return 1, N, N, N
+        rows, n = p.shape[0], N // p.shape[0]
         pitch = lambda t: t.stride(0) if rows > 1 else n
         return rows, n, pitch(p), pitch(g)
 
