@@ -820,9 +820,21 @@ class AdamW:
         self._table, nbytes = _scratch(lib().evox_adamw_table_bytes(len(shapes)), like, None, None)
         self._plan, self._adam = AdamPlan(), Adam(0.0, betas[0], betas[1], eps, weight_decay, None)
         # (waits for the current stream: a step on another one finds the states there too)
-        _check(lib().evox_adamw_plan(d, bits, tensors, len(shapes), self._table.data_ptr(), nbytes, ctypes.byref(self._plan),
-                                     _raw_stream(None, like)))
-        self.lr, self._like, self._seen, self._shapes = lr, like, set(), shapes
+        own = _raw_stream(None, like)
+        _check(lib().evox_adamw_plan(d, bits, tensors, len(shapes), self._table.data_ptr(), nbytes, ctypes.byref(self._plan), own))
+        self.lr, self._like, self._seen, self._shapes = lr, like, {own}, shapes
+
+    def _used_on(self, stream, raw):
+        """The states' memory is not given to others while this stream, the given or the current one, works on
+        it (a bare handle's caller sees to that)."""
+        import torch
+        if stream is None:
+            stream = torch.cuda.current_stream(self._like.device)
+        elif not isinstance(stream, torch.cuda.Stream):
+            return
+        self._seen.add(raw)
+        for t in (self._clock, self._table, *self.state.values()):
+            t.record_stream(stream)
 
     @staticmethod
     def _rows(i, p, g, like, bits):
@@ -850,14 +862,8 @@ class AdamW:
         else:
             a.lr, a.lr_dev = lr, None
         raw = _raw_stream(stream, self._like)
-        if stream is not None and raw not in self._seen:
-            # the states' memory is not given to others while this stream works on it (a bare
-            # handle's caller sees to that)
-            import torch
-            self._seen.add(raw)
-            if isinstance(stream, torch.cuda.Stream):
-                for t in (self._clock, self._table, *self.state.values()):
-                    t.record_stream(stream)
+        if raw not in self._seen:
+            self._used_on(stream, raw)
         rc = lib().evox_adamw(ctypes.byref(a), ctypes.byref(self._plan), self._clock.data_ptr(), raw)
         if rc != OK:
             _check(rc)
@@ -870,6 +876,9 @@ class AdamW:
             if t.shape != self.state[name].shape or t.dtype != self.state[name].dtype:
                 raise EvoxError(EINVAL, f"{name}: {t.dtype} {tuple(t.shape)}, needs {self.state[name].dtype} "
                                         f"{tuple(self.state[name].shape)}")
+        raw = _DTYPES["stream"](self._like.get_device())
+        if raw not in self._seen:
+            self._used_on(None, raw)
         for name, t in state.items():
             self.state[name].copy_(t)
 
