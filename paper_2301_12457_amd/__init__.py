@@ -766,7 +766,10 @@ class AdamW:
     params and grads are tensors of one type on one device, [n], [G, n] or [G, n_out,
     n_in], each dense or a view of the rows of a wider matrix (of a population's
     parameters: Networks' views), a gradient of its parameter's shape.  Every step()
-    reads the gradients from these buffers and updates the parameters in place.
+    reads the gradients from the memory that they have now and updates the parameters in
+    theirs, which the optimizer keeps: a tensor that is given other memory (p.data = ..., a new
+    gradient in each backward pass) needs a new optimizer, which load() gives the states of
+    the one before.
 
     lr is a number (the attribute may change from step to step) or a float32 tensor [1]
     on the device, which a captured step reads when it is replayed.  master: an fp32 copy of
@@ -793,6 +796,8 @@ class AdamW:
             raise EvoxError(EINVAL, "fp32 parameters are their own master")
         if bits not in (8, 32):
             raise EvoxError(EINVAL, f"bits = {bits}: states of 32 or 8")
+        # (what the table's addresses are of, whatever becomes of the tensors)
+        self._memory = [t.detach() for t in self.params + self.grads]
         shapes = [self._rows(i, p, g, like, bits) for i, (p, g) in enumerate(zip(self.params, self.grads))]
         sizes = [rows * n for rows, n, *_ in shapes]
         blocks = [rows * -(-n // ADAM_BLOCK) for rows, n, *_ in shapes]
@@ -825,15 +830,15 @@ class AdamW:
         self.lr, self._like, self._seen, self._shapes = lr, like, {own}, shapes
 
     def _used_on(self, stream, raw):
-        """The states' memory is not given to others while this stream, the given or the current one, works on
-        it (a bare handle's caller sees to that)."""
+        """The memory that the optimizer keeps is not given to others while this stream, the given or the current
+        one, works on it (a bare handle's caller sees to that)."""
         import torch
         if stream is None:
             stream = torch.cuda.current_stream(self._like.device)
         elif not isinstance(stream, torch.cuda.Stream):
             return
         self._seen.add(raw)
-        for t in (self._clock, self._table, *self.state.values()):
+        for t in (self._clock, self._table, *self.state.values(), *self._memory):
             t.record_stream(stream)
 
     @staticmethod
