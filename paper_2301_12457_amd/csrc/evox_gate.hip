@@ -109,14 +109,18 @@ __device__ __forceinline__ void load_row(const T *z, int lane, int L, int G, boo
 
 // f(g) with g(z) = e^(z - top) times a factor that all of a row's have.  16 bits: 2^(z log2 e
 // - c), c the rounded top log2 e, in one multiply-add (what c is off by is the factor); of
-// tops where that would be more than e^0.04, and of fp32, the difference first, factor 1.
+// tops where that would be more than e^0.04, and of fp32, the difference first, factor 1.  The
+// row's own top decides, though a wave without such rows computes one form alone: a
+// row's bits are not its neighbours' to change.
 template <typename T, typename F>
 __device__ __forceinline__ void with_exp(float top, F &&f)
 {
     if constexpr (sizeof(T) == 2) {
         const float c = top * 1.44269504f;
-        if (__all(fabsf(top) < 0x1p19f)) f([=](float z) { return __builtin_amdgcn_exp2f(fmaf(z, 1.44269504f, -c)); });
-        else f([=](float z) { return exp_fast(z - top); });
+        const auto near = [=](float z) { return __builtin_amdgcn_exp2f(fmaf(z, 1.44269504f, -c)); };
+        const bool large = fabsf(top) >= 0x1p19f && fabsf(top) < INFINITY;  // (of NaN and infinities both are the same)
+        if (!__any(large)) f(near);
+        else f([=](float z) { return large ? exp_fast(z - top) : near(z); });
     } else f([=](float z) { return exp_near(z - top); });
 }
 
