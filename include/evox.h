@@ -749,7 +749,7 @@ typedef struct evox_parameter {
     const void *g;      /* its gradient, of the same type */
     void *m, *v;        /* fp32, or e4m3 bytes; 0 before the first step */
     float *m_scale, *v_scale; /* 8 bits: [rows][ceil(n / 256)], dense; 0 before the first step */
-    float *master;      /* or null; all tensors of a call have one, or none */
+    float *master;      /* or null; all tensors of a call have one (of 16 bits), or none */
     int64_t rows, n;    /* 0 .. 2^31 - 1, 0 .. 2^38 */
     int64_t ldp, ldg;   /* row pitches of p and g, >= n */
     int64_t lds;        /* of m, v and the master */

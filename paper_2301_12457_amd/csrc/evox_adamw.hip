@@ -503,11 +503,17 @@ hipError_t launch_adamw(const AdamCall &c, hipStream_t s)
     return net_dispatch(c.dtype, [&](auto type) {
         typedef typename NetElement<decltype(type)::value>::type T;
         const dim3 grid(c.tiles == 0 ? 1 : (unsigned)c.tiles), block(256);
-        if (c.bits == 8) {
-            if (c.master) hipLaunchKernelGGL((k_adamw<T, 8, true>), grid, block, 0, s, a);
-            else hipLaunchKernelGGL((k_adamw<T, 8, false>), grid, block, 0, s, a);
-        } else if (c.master) hipLaunchKernelGGL((k_adamw<T, 32, true>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((k_adamw<T, 32, false>), grid, block, 0, s, a);
+        const auto launch = [&](auto bits, auto master) {
+            hipLaunchKernelGGL((k_adamw<T, decltype(bits)::value, decltype(master)::value>), grid, block, 0, s, a);
+        };
+        const auto with = [&](auto master) {
+            if (c.bits == 8) launch(std::integral_constant<int, 8>{}, master);
+            else launch(std::integral_constant<int, 32>{}, master);
+        };
+        if constexpr (sizeof(T) == 2) {  // (fp32 parameters are their own)
+            if (c.master) with(std::true_type{});
+            else with(std::false_type{});
+        } else with(std::false_type{});
         return hipGetLastError();
     });
 }

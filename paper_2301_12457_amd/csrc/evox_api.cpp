@@ -2059,6 +2059,7 @@ int evox_adamw_plan(int32_t dtype, int32_t bits, const evox_parameter *t, int64_
         if (adam_groups(bits, x.rows, x.n) > INT32_MAX)
             return fail(EVOX_EINVAL, "tensor %lld is too large: %lld x %lld", (long long)i, (long long)x.rows, (long long)x.n);
     }
+    if (master && dtype == EVOX_F32) return fail(EVOX_EINVAL, "fp32 parameters are their own master");
     const int rc = check_scratch(table, table_bytes, round256(adam_table(count)));
     if (rc != EVOX_OK) return rc;
     // on the host: the tensors' addresses in order (a tensor twice would be two blocks' at
@@ -2089,7 +2090,7 @@ int evox_adamw(const evox_adam *c, const evox_adam_plan *p, int64_t *clock, void
 {
     if (!c || !p) return fail(EVOX_EINVAL, "adam or plan is null");
     if ((p->dtype != EVOX_F32 && p->dtype != EVOX_BF16 && p->dtype != EVOX_F16) || (p->bits != 32 && p->bits != 8) || !p->table ||
-        p->count < 0 || p->count > kNetMaxG || p->tiles < 0 || p->tiles > INT32_MAX)
+        p->count < 0 || p->count > kNetMaxG || p->tiles < 0 || p->tiles > INT32_MAX || (p->master && p->dtype == EVOX_F32))
         return fail(EVOX_EINVAL, "the plan is not evox_adamw_plan's");
     if (!(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0))
         return fail(EVOX_EINVAL, "beta1 and beta2 must be in [0, 1)");
