@@ -63,3 +63,23 @@ def evox_gpu():
     m.lib()
     torch.cuda.init()
     return m
+
+
+@pytest.fixture(autouse=True)
+def filled_before_calls_on_other_streams(request, monkeypatch):
+    """A GPU test module's `filled` gives buffers of NaN, which the current stream writes.  They are
+    written when it returns: a call on a stream that has waited for the current one before
+    that would race with the writing, and leave NaN where it lost.
+    """
+    fill = getattr(request.module, "filled", None)
+    if fill is None or request.node.get_closest_marker("gpu") is None:
+        return
+    import torch
+
+    def filled(*args, **kw):
+        t = fill(*args, **kw)
+        if t.is_cuda and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
+        return t
+
+    monkeypatch.setattr(request.module, "filled", filled)
