@@ -84,12 +84,27 @@ __device__ __forceinline__ int64_t row_of(int L)
     return net_block() * (256 / L) + (SPREAD == WAVES ? __builtin_amdgcn_readfirstlane(in_block) : in_block);
 }
 
-// Stores to eight rows at a time go faster from fewer blocks at once, 32 KB of LDS that nothing
-// uses for each (five per CU): bf16 262,144 rows of 2048 238 us, 248 from eight; from two
-// 310, from blocks that go on from row to row 240 (1280) to 298 (768).  Fewer rows at a time do
-// not care (f32 k 2: 29.7 and 28.9, with the sort).  The stores bound it: in the rows' own
-// order 204 us, in the sorted one 225, by chance 234; the floor is 186.
+// Stores to many long rows at a time go faster from fewer blocks at once, 32 KB of LDS that nothing
+// uses for each (five per CU): from two 310 us, from eight 248, from five 238 (bf16 262,144 rows of
+// 2048, with the sort), from blocks that go on from row to row 240 (1280) to 298 (768).  Taken by what a
+// row of data stores, as measured on 12,000 and 16,384 rows in 41 lengths and counts, with it and without:
+// bf16 rows of 1152, k 8 55 us and 60, k 12 80 and 89, of 1536, k 5 45 and 48, of 2048, k 8 100 and 102,
+// k 20 188 and 189; below the borders, not: of 1152, k 5 43 and 33, k 6 47 and 43, k 9 53 and 50.  By
+// lines (k_dispatch_lines) of 16 bits also not where a round has five slots or fewer: f16 rows of 2047, k 5
+// 82 and 79, k 9 115 and 108, but k 6 88 and 95, of 1029, k 8 67 and 73; f32 ones gain
+// at few (of 545, k 5 42 and 47) and else differ by 2 %.  Up to 4096 rows all is the same.
+// The stores bound it: of bf16 262,144 x 2048 in the rows' own order 204 us, in the sorted one 225,
+// by chance 234; the floor is 186.
 constexpr int kFewBlocksLds = 32768;
+template <typename T>
+bool few_blocks(const SlotArgs &a, bool lines)
+{
+    const int rounds = (a.k + 7) / 8;
+    if (a.T < 8192) return false;
+    if (lines && sizeof(T) == 4) return true;
+    if (lines && 2 * a.k < 11 * rounds) return false;
+    return a.k * a.D * (int64_t)sizeof(T) >= (rounds == 1 ? 15360 : 23040);
+}
 
 // Rows that do not start with a line, over whole waves: chunks are counted from the line in
 // which the row of the grouping starts, so that all stores but the row's first and last are
@@ -380,8 +395,9 @@ hipError_t launch_dispatch(const SlotArgs &a, hipStream_t s)
         typedef typename NetElement<decltype(type)::value>::type T;
         const int L = row_lanes<T>(a.D, 256);
         return with_slots<false, T>(a, L, [&](auto K, auto spread, auto past) {
-            const int lds = decltype(K)::value == 8 && L == 256 && a.T >= 8192 ? kFewBlocksLds : 0;
-            if (by_lines<T>(a, L))
+            const bool lines = by_lines<T>(a, L);
+            const int lds = decltype(K)::value == 8 && L == 256 && few_blocks<T>(a, lines) ? kFewBlocksLds : 0;
+            if (lines)
                 hipLaunchKernelGGL((k_dispatch_lines<T, decltype(K)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
             else
                 hipLaunchKernelGGL((k_dispatch<T, decltype(K)::value, decltype(spread)::value>), row_grid(a.T, L), dim3(256), lds, s, a, L);
@@ -405,8 +421,10 @@ hipError_t launch_combine(const SlotArgs &a, hipStream_t s)
 }
 
 // Of many large rows both results are faster apart, all reads before all writes, though dy is
-// read for each (f16 k 4, 65,536 rows of 4096 209 us, 233 in one; not for k 2,
-// nor what fits the last cache).
+// read for each: from four slots and what the last cache holds on.  In one kernel and in two, by bytes
+// of slots: f16 rows of 4096, k 4 128 MB 60 us and 65, 256 MB 105 and 104, 700 MB 318 and 290; k 2 102 and
+// 120, 351 and 364; k 3 101 and 110, 329 and 295; f32 rows of 4096, k 16 61 and 56, 128 and 110, 303 and
+// 259; of 1001, k 4 58 and 61, 110 and 119, 340 and 325, k 8 55 and 61, 117 and 118, 321 and 307.
 constexpr int kWaveRows = 4096;  // rows that a wave each fills the chip with
 hipError_t launch_combine_grad(const SlotArgs &a, hipStream_t s)
 {
