@@ -724,8 +724,8 @@ int evox_combine_grad(const evox_slots *slots, const void *xs, const int32_t *po
                       void *dxs, float *dw, void *hip_stream);
 
 /* ---------------------------------------------------------------------------
- * AdamW (Loshchilov and Hutter, 2019) over many tensors at once: the step that a
- * center or a network takes along its gradient.
+ * AdamW (Loshchilov and Hutter, 2019) over many tensors at once: the step that
+ * networks' parameters take along their gradients.
  *     m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2,
  *     p = p - lr weight_decay p - lr m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps)
  * computed in fp32, t counted from 1.  A master is p in fp32, which the step then
@@ -735,7 +735,10 @@ int evox_combine_grad(const evox_slots *slots, const void *xs, const int32_t *po
  * States of 32 bits are fp32.  Of 8 bits m is e4m3 numbers (OCP: largest 448, least 2^-9)
  * with one fp32 scale for each 256 elements of a row (a row's last ones may be
  * fewer), the largest |m| / 448, and of v the root is held so; a root above 0 is at
- * least the least e4m3 number.  |m| whose group is all below 2^-100 counts as 0.  The step
+ * least the least e4m3 number.  So a number is held within 2^-4 of itself where it is at
+ * least 1 / 28,672 of its group's largest, and below within 2^-10 of the scale; a root below
+ * 1 / 229,376 of the largest counts as that, and its element's next steps are as much smaller.
+ * |m| whose group is all below 2^-100 counts as 0.  The step
  * is made from the new moments before they are rounded.  An infinity or NaN stays its own
  * element's, of 8 bits as NaN.
  * ------------------------------------------------------------------------- */

@@ -11,9 +11,12 @@
 // 8-bit states: a group of 256 elements of a row (or a shorter row's all) is 32
 // lanes' (fewer for short rows), 8 elements each; m is e4m3 numbers times the group's
 // largest |m| / 448, and of v its root is held the same way: e4m3 spans 2^18 of the
-// group's largest number, for v then 2^36, with 2^-4 of a root's value at most in
-// rounding.  A root above 0 is never rounded to 0, where an m beside it would divide by eps
-// alone.  The update itself is made from the fp32 moments, before they are rounded.
+// group's largest number, for v then 2^36.  Rounding is 2^-4 of a number at most where it is
+// normal, at least 2^-6 of the scale (1 / 28,672 of the largest), and 2^-10 of the scale below.
+// A root above 0 is never rounded to 0, where an m beside it would divide by eps
+// alone: it is 2^-9 of the scale at least (1 / 229,376 of the largest), so an element whose gradients
+// are below that beside a large one's takes steps that are as much smaller.  The update itself
+// is made from the fp32 moments, before they are rounded.
 #include "evox_mix.hpp"
 
 namespace evox {
