@@ -777,8 +777,8 @@ class AdamW:
 
     bits: of the moments, 32, or 8 (e4m3 numbers and a scale per 256).  A scale is for
     elements of one row of its parameter's first dimension (of one network, of [G, n]),
-    dense or not; a dense parameter of up to 256 elements in all, with a dense gradient,
-    has one.  Where rows are short and need none of their own, p.view(-1) has fewer.
+    dense or not (but of up to 256 elements in dense rows of fewer than 8 all have one).
+    Where rows are short and need none of their own, p.view(-1) has fewer.
 
     state holds what a checkpoint saves, each for all tensors one behind the other:
     "t" (steps done, int64 [1]), "m", "v" (float32, or float8_e4m3fn: of v the root), with
@@ -852,10 +852,12 @@ class AdamW:
         if p.shape != g.shape or p.dim() == 0:
             raise EvoxError(EINVAL, f"params[{i}] has shape {tuple(p.shape)}, its gradient {tuple(g.shape)}")
         dense, N = p.is_contiguous() and g.is_contiguous(), p.numel()
-        # (all elements as one row, but where scales would go from one row into the next)
-        if dense and (bits == 32 or p.dim() == 1 or N <= ADAM_BLOCK or N // p.shape[0] % ADAM_BLOCK == 0):
-            return 1, N, N, N
+        if not N:
+            return 1, 0, 0, 0
         rows, n = p.shape[0], N // p.shape[0]
+        # (all elements as one row, but where scales would go from one row into the next)
+        if dense and (bits == 32 or p.dim() == 1 or n % ADAM_BLOCK == 0 or N <= ADAM_BLOCK and n < 8):
+            return 1, N, N, N
         pitch = lambda t: t.stride(0) if rows > 1 else n
         return rows, n, pitch(p), pitch(g)
 

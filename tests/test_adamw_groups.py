@@ -1,6 +1,6 @@
 """Which elements share a scale of 8-bit moments is the parameter's shape's to say: those of a
-row of its first dimension, however it and its gradient lie in memory.  (A dense parameter of
-up to a group's 256 elements in all, with a dense gradient, has one scale.)"""
+row of its first dimension, however it and its gradient lie in memory.  (A dense parameter of up to
+a group's 256 elements, in rows of fewer than the 8 of a lane, with a dense gradient, has one scale.)"""
 import math
 
 import pytest
@@ -13,7 +13,7 @@ from net_ref import DTYPES, TINY, U, U32
 BLOCK = 256
 HYPER = dict(lr=3e-3, betas=(0.9, 0.99), eps=1e-6, weight_decay=0.05)
 # of these the first two have as many scales by rows as through all elements
-SHAPES = [(2, 250), (40, 250), (7, 1824), (6, 300), (5, 3, 100), (300, 33), (9, 512), (3, 1027), (130, 7), (17, 16)]
+SHAPES = [(2, 250), (40, 250), (7, 1824), (6, 300), (5, 3, 100), (300, 33), (9, 512), (3, 1027), (130, 7), (17, 16), (8, 32), (2, 128), (3, 8), (2, 2, 4)]
 
 
 def memory(lead, pad, shape, **kw):
