@@ -329,8 +329,8 @@ __global__ __launch_bounds__(256) void k_adamw(const Step a)
     constexpr int kElements = kPasses * 256 * E;
     if (x.per_row == x.groups && (int64_t)(index + 1) * kElements <= x.n) {
         // Within a tensor of one row: no ends to look at, addresses that differ by the lane
-        // alone.  Streamed past the caches: bf16 with 8-bit states, 100.7 million elements 168 us,
-        // 6.0 TB/s, 192 with cached stores, 215 with cached loads too (and then as long with next
+        // alone.  Streamed past the caches: bf16 with 8-bit states, 100.7 million elements 166 us,
+        // 6.1 TB/s, 192 with cached stores, 215 with cached loads too (and then as long with next
         // to no arithmetic); f32, 16.8 million 78 us, 6.0 TB/s, 85 with cached stores.
         const int64_t base = (int64_t)index * kElements;
         const T *g = (const T *)x.g + base;

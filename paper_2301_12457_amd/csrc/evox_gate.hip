@@ -5,7 +5,7 @@
 // wave, a power of two, k at least, so that lane j keeps the j-th choice; above 64 lanes'
 // worth over a block; each lane has NIT chunks of 16 bytes), or one pass over the row with
 // the best so far sorted over the lanes of a wave or several.  Bound by instructions: bf16 65,536 x 256, k 8, weights
-// over all, 814 of a wave for eight rows, 13.9 us (floor 5.8); fp32 keys are of 64 bits.  The
+// over all, 815 of a wave for eight rows, 14.1 us (floor 5.8); fp32 keys are of 64 bits.  The
 // gradient is bound by memory (f16 20,000 x 1001 17 us, 81 MB, floor 12.5).
 #include "evox_mix.hpp"
 
